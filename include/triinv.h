@@ -284,6 +284,79 @@ int gdn_chunk_tri_solve_varlen(const void* K, const float* beta, const float* g,
                                int k_dtype, int gate_kind, int method, int op_dtype,
                                void* hip_stream, uint32_t flags);
 
+/*
+ * gdn_chunk_attn: what a linear-attention layer with one decay per head computes from a prompt, chunk by chunk, and the
+ * state after it.  Per sequence and head, with the state S (d_k x d_v, fp32) before a chunk and g the chunk-local cumulative
+ * log-decay of gdn_chunk_tri_inv (g_C its last value in the chunk):
+ *     V' = U - W S                                                     (without W: V' = U)
+ *     O_i = scale (exp(g_i) S^T q_i + sum_{j <= i} exp(g_i - g_j) <q_i, k_j> V'_j)
+ *     S  <- exp(g_C) S + sum_j exp(g_C - g_j) k_j V'_j^T
+ * Without W: linear attention with a decay, U the layer's values.  With W: the gated delta rule; U and W are the two results of
+ * gdn_chunk_tri_solve_multi with the same K, beta, g and C, of X = V with row_scale = beta and X = K with row_scale = beta exp(g).
+ *   Q, K         device, [B][Tlen][H_k][d_k], element type dtype (fp16 or bf16); H_k divides H, head h uses key head h / (H / H_k).
+ *   U, O         device, [B][Tlen][H][d_v], the same type; O is written.
+ *   W            device, [B][Tlen][H][d_k], the same type, or NULL.
+ *   g            device, fp32 [B][Tlen][H], or NULL for no decay.
+ *   state        device, fp32 [B][H][d_k][d_v], the state before the first token, or NULL for zeros.
+ *   final_state  device, fp32 [B][H][d_k][d_v], written, or NULL.  May be `state` itself.
+ *   workspace    device, workspace_bytes of it as gdn_chunk_attn_workspace says, 16-byte aligned (NULL where that is 0).
+ *   d_k          a multiple of 32, <= 128.   d_v  a multiple of 8, <= 512.   C  16, 32, 64 or 128.
+ * Tlen = 0 or empty sequences: nothing of O, final_state = state.  The rows a chunk covers (H * max(d_k, d_v) * C elements) must
+ * stay below 2^31 bytes.  The state is kept in fp32 and its products are carried out on 24 bits of it (22 with fp16); what is rounded to the
+ * operand type on the way to O has two parts.  fp16: |scale <q, k>| must stay below 65504.  Non-finite values stay in their
+ * sequence and head, from their chunk on (within the chunk earlier tokens may receive them).
+ * Two to three kernels instead of one where sequences and heads are few and prompts long (see the workspace), one otherwise; results may differ in their last bits
+ * between the two.  gdn_chunk_attn_varlen: sequences packed back to back, arrays as in gdn_chunk_tri_inv_varlen, states [n_seq][H][d_k][d_v].
+ */
+int gdn_chunk_attn(const void* Q, const void* K, const void* U, const void* W, const float* g, const float* state,
+                   void* O, float* final_state, void* workspace, int64_t workspace_bytes,
+                   int B, int64_t Tlen, int H, int H_k, int d_k, int d_v, int C, int dtype, float scale, void* hip_stream);
+int gdn_chunk_attn_varlen(const void* Q, const void* K, const void* U, const void* W, const float* g, const float* state,
+                          void* O, float* final_state, void* workspace, int64_t workspace_bytes,
+                          const int64_t* cu_seqlens, const int64_t* cu_chunks, int n_seq, int64_t total_tokens, int64_t total_chunks,
+                          int H, int H_k, int d_k, int d_v, int C, int dtype, float scale, void* hip_stream);
+/* Bytes of workspace the two need for n_seq sequences of total_chunks chunks (has_w: with W). */
+int gdn_chunk_attn_workspace(int n_seq, int64_t total_chunks, int H, int d_k, int d_v, int has_w, int64_t* bytes);
+
+/*
+ * gdn_step: the same layer's single token, the state updated in place.  Per sequence b and head:
+ *     S <- exp(g) S;   v' = beta (v - S^T k)   (beta NULL: v' = v);   S <- S + k v'^T;   o = scale S^T q
+ *   q, k    device, [B][H_k][d_k], element type dtype (fp32, fp16 or bf16);   v, o   [B][H][d_v], the same type; o is written.
+ *   g       device, fp32 [B][H], this token's log-decay, or NULL;   beta   device, fp32 [B][H], or NULL (no delta rule).
+ *   state   device, fp32 [n_slot][H][d_k][d_v], read and written.
+ *   slots   device, int32 [B]: sequence b's place in `state`, or NULL for b itself.  A place outside 0 .. n_slot - 1 (padding):
+ *           nothing is updated and o is zero.  No two sequences may have the same place.
+ *   d_k     1 to 256.   d_v   a multiple of 4, <= 512.
+ */
+int gdn_step(const void* q, const void* k, const void* v, const float* g, const float* beta, float* state, const int32_t* slots,
+             void* o, int B, int64_t n_slot, int H, int H_k, int d_k, int d_v, int dtype, float scale, void* hip_stream);
+
+/*
+ * add_rms_norm: root-mean-square norm of rows, with the residual's addition in front:
+ *     s = x + residual, rounded to x's type and written to `sum`;   y = s / sqrt(mean(s^2) + eps) . weight
+ *   x, residual, sum   device, [N][D], element type dtype (fp32, fp16 or bf16).  residual and sum NULL: s = x.  sum may be x or residual.
+ *   weight             device, [D], the same type.
+ *   y                  device, [N][D]: of x's type (group = -1), or 8-bit floating point (4 exponent, 3 mantissa bits, largest value
+ *                      448) of y / scale, rounded to nearest even.
+ *   scales             device, fp32: [N] (group = 0), or [N][D / 128] (group = 128): max |y| over the row or the 128 columns over 448, 1 where
+ *                      that is 0.  NULL with group = -1.
+ *   D                  a multiple of 8 (group = 128: of 128), <= 16384.
+ * Sums and the norm are fp32.  A row with a NaN or an infinity is NaN (and its scales).
+ */
+int add_rms_norm(const void* x, const void* residual, const void* weight, void* y, float* scales, void* sum,
+                 int64_t N, int D, int group, int dtype, float eps, void* hip_stream);
+
+/*
+ * add_rms_norm_bwd: its gradient, from s (the sum as it was written, or x) and dy, with r = 1 / sqrt(mean(s^2) + eps):
+ *     dx = dsum + r (dy . weight - s r^2 mean(dy . weight . s))   (of x and of the residual alike)
+ *     dweight = sum over rows of dy . s r
+ *   dy, s, dx, dsum   device, [N][D], element type dtype; dsum: the gradient that arrives at `sum` itself, or NULL; dx is written.
+ *   dweight           device, fp32 [D], written.
+ *   workspace         device, workspace_bytes >= 4 * D * min(N, 512), 16-byte aligned.  dweight's sums have a fixed order.
+ */
+int add_rms_norm_bwd(const void* dy, const void* s, const void* weight, const void* dsum, void* dx, float* dweight,
+                     void* workspace, int64_t workspace_bytes, int64_t N, int D, int dtype, float eps, void* hip_stream);
+
 /* Human-readable name of a status code (static storage, never NULL). */
 const char* triinv_status_string(int status);
 

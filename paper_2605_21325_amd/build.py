@@ -1,6 +1,6 @@
 """Build libtriinv.so (hand-written HIP for gfx950) in-tree with hipcc.
 
-One translation unit per (C, operand type) pair plus the C-ABI file, compiled in parallel and
+One translation unit per (C, operand type) pair, those of the layer's other operators and the C-ABI files, compiled in parallel and
 linked into paper_2605_21325_amd/libtriinv.so.  Packed-fp32 code generation is switched off
 for every device compile.  Beside it the host compiler builds the binding's native argument
 handling, paper_2605_21325_amd/_fastcall.so, from Python's and torch's headers; the binding does without it
@@ -42,7 +42,9 @@ UNITS = [
 ] + [
     (f"solve_nb{nb}_op{op}", "solve.hip", [f"-DTRIINV_INST_NB={nb}", f"-DTRIINV_INST_OP={op}"])
     for nb in (8, 4, 2, 1) for op in (0, 1, 2)
-] + [("api", "api.hip", [])]
+] + [
+    (f"attn_op{op}", "attn.hip", [f"-DTRIINV_INST_OP={op}"]) for op in (1, 2)
+] + [("norm", "norm.hip", []), ("step", "step.hip", []), ("layer", "layer.hip", []), ("api", "api.hip", [])]
 
 
 def _sources_mtime() -> float:

@@ -1,0 +1,54 @@
+// Instantiations of the chunk-attention kernels (attn.hpp) for one operand type, TRIINV_INST_OP.
+#include "attn.hpp"
+#include "layer.hpp"
+
+#ifndef TRIINV_INST_OP
+#error "compile with -DTRIINV_INST_OP=1|2"
+#endif
+
+namespace triinv {
+
+namespace {
+
+constexpr int OP = TRIINV_INST_OP;
+
+AttnArgs args_of(const AttnCall& c)
+{
+    AttnArgs a{};
+    a.Q = c.Q, a.K = c.K, a.U = c.U, a.W = c.W, a.g = c.g, a.state = c.state, a.O = c.O, a.final_state = c.final_state;
+    const int64_t heads = (int64_t)c.n_seq * c.H;
+    a.seg_state = reinterpret_cast<float*>(c.workspace);
+    a.seg_trans = a.seg_state + (c.n_seg - 1) * heads * c.d_k * c.d_v;
+    a.seg_decay = a.seg_trans;  // (one or the other)
+    a.map = SeqMap{c.cu_seqlens, c.cu_chunks, c.Tlen, c.n_seq};
+    a.H = c.H, a.group = c.H / c.H_k, a.d_k = c.d_k, a.d_v = c.d_v, a.C = c.C, a.n_seg = c.n_seg, a.scale = c.scale;
+    return a;
+}
+
+template <int MT, int KP, bool DELTA> int go(const AttnCall& c)
+{
+    constexpr int NT = 1, WAVES = 4, COLS = 16 * NT * WAVES;
+    const AttnArgs a = args_of(c);
+    const unsigned heads = (unsigned)(c.n_seq * c.H), groups = (unsigned)((c.d_v + COLS - 1) / COLS);
+    if (c.n_seg > 1) {
+        const unsigned more = DELTA ? (unsigned)((c.d_k + COLS - 1) / COLS) : 0u;
+        int rc = launch_kernel(false, k_chunk_attn<OP, MT, KP, NT, WAVES, DELTA, false>, dim3(heads * (groups + more), (unsigned)c.n_seg - 1), dim3(64 * WAVES), 0, c.stream, a);
+        if (rc != LAUNCHED) return rc;
+        rc = launch_kernel(false, k_attn_join<KP, 4, DELTA>, dim3(heads * ((c.d_v + 63) / 64)), dim3(256), 0, c.stream, a);
+        if (rc != LAUNCHED) return rc;
+    }
+    return launch_kernel(false, k_chunk_attn<OP, MT, KP, NT, WAVES, DELTA, true>, dim3(heads * groups, (unsigned)c.n_seg), dim3(64 * WAVES), 0, c.stream, a);
+}
+template <int MT, bool DELTA> int go_k(const AttnCall& c) { return c.d_k <= 64 ? go<MT, 2, DELTA>(c) : go<MT, 4, DELTA>(c); }
+template <int MT> int go_delta(const AttnCall& c) { return c.W ? go_k<MT, true>(c) : go_k<MT, false>(c); }
+
+}  // namespace
+
+#if TRIINV_INST_OP == 1
+#define LAUNCHER launch_chunk_attn_f16
+#else
+#define LAUNCHER launch_chunk_attn_bf16
+#endif
+int LAUNCHER(const AttnCall& c) { return c.C <= 32 ? go_delta<2>(c) : c.C == 64 ? go_delta<4>(c) : go_delta<8>(c); }
+
+}  // namespace triinv

@@ -1,0 +1,305 @@
+// Root-mean-square norm with the residual's addition in front:
+//     s = x + residual (rounded to x's type and written),   y = s / sqrt(mean(s^2) + eps) . weight
+// y in x's type, or in 8 bits (4 exponent and 3 mantissa bits, largest value 448) with an fp32 scale for every row or group of columns,
+// scale = max |y| / 448 (1 where that is 0).  The gradient, from s as it was written, with r = 1 / sqrt(mean(s^2) + eps):
+//     dx = dsum + r (dy . w - s r^2 mean(dy . w . s)),   dw = sum over the rows of dy . s r.
+//
+// Bound by memory, each element read once: a row stays in the registers of its wavefronts, 8 elements a piece, PIECES pieces a lane, all
+// requested at once.  One wavefront takes a row where there are many (no barrier anywhere), more of them where rows are few or long.
+#include "layer.hpp"
+#include "tile_ops.hpp"
+
+namespace triinv {
+
+namespace {
+
+typedef float v8f __attribute__((ext_vector_type(8)));
+
+template <int DT> __device__ __forceinline__ v8f load8(const void* p, int64_t i)
+{
+    v8f o;
+    if constexpr (DT == OP_F32) {
+        const v4f a = *reinterpret_cast<const v4f*>(static_cast<const float*>(p) + i), b = *reinterpret_cast<const v4f*>(static_cast<const float*>(p) + i + 4);
+        o = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+        const v4u u = *reinterpret_cast<const v4u*>(static_cast<const uint16_t*>(p) + i);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint16_t x = (uint16_t)(u[e >> 1] >> (16 * (e & 1)));
+            o[e] = DT == OP_F16 ? f16_to_f32(x) : bf16_to_f32(x);
+        }
+    }
+    return o;
+}
+// x rounded to the type, and written.
+template <int DT> __device__ __forceinline__ v8f store8(void* p, int64_t i, v8f x)
+{
+    if constexpr (DT == OP_F32) {
+        *reinterpret_cast<v4f*>(static_cast<float*>(p) + i) = __builtin_shufflevector(x, x, 0, 1, 2, 3);
+        *reinterpret_cast<v4f*>(static_cast<float*>(p) + i + 4) = __builtin_shufflevector(x, x, 4, 5, 6, 7);
+    } else {
+        v4u u;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) u[e] = DT == OP_F16 ? pack2_f16(x[2 * e], x[2 * e + 1]) : pack2_bf16(x[2 * e], x[2 * e + 1]);
+        *reinterpret_cast<v4u*>(static_cast<uint16_t*>(p) + i) = u;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint16_t h = (uint16_t)(u[e >> 1] >> (16 * (e & 1)));
+            x[e] = DT == OP_F16 ? f16_to_f32(h) : bf16_to_f32(h);
+        }
+    }
+    return x;
+}
+
+__device__ __forceinline__ float lanes_sum(float x, int width)
+{
+    for (int d = 1; d < width; d *= 2) x += __shfl_xor(x, d);
+    return x;
+}
+// Largest magnitude over `width` lanes; as bit patterns, which puts NaN on top.
+__device__ __forceinline__ uint32_t lanes_max(uint32_t x, int width)
+{
+    for (int d = 1; d < width; d *= 2) {
+        const uint32_t y = __shfl_xor(x, d);
+        x = x > y ? x : y;
+    }
+    return x;
+}
+__device__ __forceinline__ uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7fffffffu; }
+__device__ __forceinline__ uint32_t magnitude(v8f x)
+{
+    uint32_t m = magnitude(x[0]);
+#pragma unroll
+    for (int e = 1; e < 8; ++e) m = m > magnitude(x[e]) ? m : magnitude(x[e]);
+    return m;
+}
+__device__ __forceinline__ float scale_of(uint32_t most)
+{
+    const float s = __builtin_bit_cast(float, most) * (1.f / 448.f);
+    return s == 0.f ? 1.f : s;
+}
+// y / scale in 8 bits: what rounding carries past the largest value stays there, NaN stays NaN.
+__device__ __forceinline__ void store_fp8(void* p, int64_t i, v8f y, float scale)
+{
+    uint32_t u[2] = {0u, 0u};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float z = y[e] / scale;
+        y[e] = z > 448.f ? 448.f : z < -448.f ? -448.f : z;
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * h], y[4 * h + 1], 0, false);
+        u[h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * h + 2], y[4 * h + 3], w, true);
+    }
+    *reinterpret_cast<v2u*>(static_cast<uint8_t*>(p) + i) = v2u{u[0], u[1]};
+}
+
+// A value of all WAVES wavefronts of a row through LDS.
+template <int WAVES, class T, class F> __device__ __forceinline__ T across_waves(T x, T* lds, F join)
+{
+    if constexpr (WAVES == 1) return x;
+    const int w = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) lds[w] = x;
+    __syncthreads();
+    x = lds[0];
+#pragma unroll
+    for (int i = 1; i < WAVES; ++i) x = join(x, lds[i]);
+    __syncthreads();
+    return x;
+}
+
+// WAVES wavefronts a row; workgroups of 256 threads where that is one.
+enum : int { OUT_SAME = 0, OUT_ROW = 1, OUT_GROUP = 2 };
+template <int DT, int OUT, bool RESIDUAL, int WAVES, int PIECES>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void k_norm(NormCall a)
+{
+    constexpr int ROWS = WAVES == 1 ? 4 : 1, LANES = 64 * WAVES;
+    __shared__ float sums[WAVES];
+    __shared__ uint32_t mosts[WAVES];
+    const int lane = threadIdx.x % LANES;
+    const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES;
+    if (row >= a.N) return;  // (whole wavefronts; with more than one to a row there is one row a workgroup)
+    const int64_t at = row * a.D;
+    v8f x[PIECES];
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const int c = 8 * (lane + LANES * i);
+        x[i] = v8f{0, 0, 0, 0, 0, 0, 0, 0};
+        if (c < a.D) x[i] = load8<DT>(a.x, at + c);
+    }
+    if constexpr (RESIDUAL) {
+        v8f r[PIECES];
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int c = 8 * (lane + LANES * i);
+            r[i] = v8f{0, 0, 0, 0, 0, 0, 0, 0};
+            if (c < a.D) r[i] = load8<DT>(a.residual, at + c);
+        }
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int c = 8 * (lane + LANES * i);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[i][e] += r[i][e];
+            if (c < a.D) x[i] = store8<DT>(a.sum, at + c, x[i]);
+        }
+    }
+    float sq = 0.f;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sq += x[i][e] * x[i][e];
+    sq = across_waves<WAVES>(lanes_sum(sq, 64), sums, [](float p, float q) { return p + q; });
+    const float rstd = 1.f / sqrtf(sq / (float)a.D + a.eps);
+    uint32_t most = 0u;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const int c = 8 * (lane + LANES * i);
+        if (c < a.D) {
+            const v8f w = load8<DT>(a.weight, c);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[i][e] = x[i][e] * rstd * w[e];
+            if constexpr (OUT == OUT_SAME) store8<DT>(a.y, at + c, x[i]);
+        }
+        if constexpr (OUT == OUT_ROW) {
+            const uint32_t m = magnitude(x[i]);
+            most = most > m ? most : m;
+        }
+        if constexpr (OUT == OUT_GROUP) {  // 128 columns: sixteen lanes
+            const float scale = scale_of(lanes_max(magnitude(x[i]), 16));
+            if (c < a.D) {
+                store_fp8(a.y, at + c, x[i], scale);
+                if (lane % 16 == 0) a.scales[row * (a.D / 128) + c / 128] = scale;
+            }
+        }
+    }
+    if constexpr (OUT == OUT_ROW) {
+        most = across_waves<WAVES>(lanes_max(most, 64), mosts, [](uint32_t p, uint32_t q) { return p > q ? p : q; });
+        const float scale = scale_of(most);
+        if (lane == 0) a.scales[row] = scale;
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int c = 8 * (lane + LANES * i);
+            if (c < a.D) store_fp8(a.y, at + c, x[i], scale);
+        }
+    }
+}
+
+template <int DT, int OUT, bool RESIDUAL, int WAVES> int go_pieces(const NormCall& a)
+{
+    const int pieces = (a.D + 512 * WAVES - 1) / (512 * WAVES);
+    const dim3 grid((unsigned)(WAVES == 1 ? (a.N + 3) / 4 : a.N)), block(WAVES == 1 ? 256 : 64 * WAVES);
+    if (pieces <= 1) return launch_kernel(false, k_norm<DT, OUT, RESIDUAL, WAVES, 1>, grid, block, 0, a.stream, a);
+    if (pieces <= 2) return launch_kernel(false, k_norm<DT, OUT, RESIDUAL, WAVES, 2>, grid, block, 0, a.stream, a);
+    if (pieces <= 4) return launch_kernel(false, k_norm<DT, OUT, RESIDUAL, WAVES, 4>, grid, block, 0, a.stream, a);
+    return NOT_BUILT;
+}
+template <int DT, int OUT, bool RESIDUAL> int go_waves(const NormCall& a)
+{
+    if (a.D <= 2048 && a.N > 2048) return go_pieces<DT, OUT, RESIDUAL, 1>(a);
+    if (a.D <= 8192) return go_pieces<DT, OUT, RESIDUAL, 4>(a);
+    return go_pieces<DT, OUT, RESIDUAL, 16>(a);
+}
+template <int DT> int go_out(const NormCall& a)
+{
+    if (a.group < 0) return a.residual ? go_waves<DT, OUT_SAME, true>(a) : go_waves<DT, OUT_SAME, false>(a);
+    if (a.group == 0) return a.residual ? go_waves<DT, OUT_ROW, true>(a) : go_waves<DT, OUT_ROW, false>(a);
+    return a.residual ? go_waves<DT, OUT_GROUP, true>(a) : go_waves<DT, OUT_GROUP, false>(a);
+}
+
+// The gradient.  A workgroup takes rows in turn (row = group, group + groups, ...) and keeps its sum of dw in registers; the groups' sums
+// are written out and added up by k_norm_dweight, always in the same order.
+template <int DT, int PIECES, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void k_norm_bwd(NormBwdCall a)
+{
+    constexpr int LANES = 64 * WAVES;
+    __shared__ v2f sums[WAVES];
+    const int lane = threadIdx.x;
+    v8f w[PIECES], dw[PIECES];
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const int c = 8 * (lane + LANES * i);
+        dw[i] = w[i] = v8f{0, 0, 0, 0, 0, 0, 0, 0};
+        if (c < a.D) w[i] = load8<DT>(a.weight, c);
+    }
+    for (int64_t row = blockIdx.x; row < a.N; row += gridDim.x) {
+        const int64_t at = row * a.D;
+        v8f x[PIECES], d[PIECES];
+        v2f s = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int c = 8 * (lane + LANES * i);
+            x[i] = d[i] = v8f{0, 0, 0, 0, 0, 0, 0, 0};
+            if (c < a.D) x[i] = load8<DT>(a.x, at + c), d[i] = load8<DT>(a.dy, at + c);
+        }
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[0] += x[i][e] * x[i][e], s[1] += d[i][e] * w[i][e] * x[i][e];
+        s[0] = lanes_sum(s[0], 64), s[1] = lanes_sum(s[1], 64);
+        s = across_waves<WAVES>(s, sums, [](v2f p, v2f q) { return v2f{p[0] + q[0], p[1] + q[1]}; });
+        const float rstd = 1.f / sqrtf(s[0] / (float)a.D + a.eps), m = s[1] / (float)a.D * rstd * rstd;
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int c = 8 * (lane + LANES * i);
+            if (c >= a.D) continue;
+            v8f dx;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                dw[i][e] += d[i][e] * (x[i][e] * rstd);
+                dx[e] = rstd * (d[i][e] * w[i][e] - x[i][e] * m);
+            }
+            if (a.dsum) {
+                const v8f t = load8<DT>(a.dsum, at + c);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) dx[e] += t[e];
+            }
+            store8<DT>(a.dx, at + c, dx);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const int c = 8 * (lane + LANES * i);
+        if (c < a.D) store8<OP_F32>(a.partial, (int64_t)blockIdx.x * a.D + c, dw[i]);
+    }
+}
+
+// dweight[c] = sum of partial[group][c]: 64 columns a workgroup, 16 threads a column.
+__global__ __launch_bounds__(1024) void k_norm_dweight(const float* partial, float* dweight, int groups, int D)
+{
+    __shared__ float part[16][64];
+    const int cx = threadIdx.x & 63, y = threadIdx.x >> 6, c = 64 * blockIdx.x + cx;
+    float s = 0.f;
+    if (c < D)
+        for (int g = y; g < groups; g += 16) s += partial[(int64_t)g * D + c];
+    part[y][cx] = s;
+    __syncthreads();
+    if (y == 0 && c < D) {
+        for (int i = 1; i < 16; ++i) s += part[i][cx];
+        dweight[c] = s;
+    }
+}
+
+template <int DT, int WAVES> int bwd_pieces(const NormBwdCall& a)
+{
+    const int pieces = (a.D + 512 * WAVES - 1) / (512 * WAVES);
+    const dim3 grid((unsigned)a.groups), block(64 * WAVES);
+    if (pieces <= 1) return launch_kernel(false, k_norm_bwd<DT, 1, WAVES>, grid, block, 0, a.stream, a);
+    if (pieces <= 2) return launch_kernel(false, k_norm_bwd<DT, 2, WAVES>, grid, block, 0, a.stream, a);
+    if (pieces <= 4) return launch_kernel(false, k_norm_bwd<DT, 4, WAVES>, grid, block, 0, a.stream, a);
+    return NOT_BUILT;
+}
+template <int DT> int bwd(const NormBwdCall& a)
+{
+    if (a.groups == 0) return launch_kernel(false, k_norm_dweight, dim3((unsigned)((a.D + 63) / 64)), dim3(1024), 0, a.stream, a.partial, a.dweight, 0, a.D);
+    const int rc = a.D <= 512 ? bwd_pieces<DT, 1>(a) : a.D <= 4096 ? bwd_pieces<DT, 4>(a) : bwd_pieces<DT, 8>(a);
+    if (rc != LAUNCHED) return rc;
+    return launch_kernel(false, k_norm_dweight, dim3((unsigned)((a.D + 63) / 64)), dim3(1024), 0, a.stream, a.partial, a.dweight, a.groups, a.D);
+}
+
+}  // namespace
+
+int launch_norm(const NormCall& a) { return a.dtype == OP_F32 ? go_out<OP_F32>(a) : a.dtype == OP_F16 ? go_out<OP_F16>(a) : go_out<OP_BF16>(a); }
+int launch_norm_bwd(const NormBwdCall& a) { return a.dtype == OP_F32 ? bwd<OP_F32>(a) : a.dtype == OP_F16 ? bwd<OP_F16>(a) : bwd<OP_BF16>(a); }
+
+}  // namespace triinv
