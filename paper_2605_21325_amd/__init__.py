@@ -7,4 +7,4 @@ from .binding import (  # noqa: F401
     DTYPE_NAMES, EXPORTS, METHOD_NAMES, TriInvError,
     gdn_chunk_tri_inv, gdn_chunk_tri_inv_ex, gdn_chunk_tri_inv_varlen, gdn_chunk_build_A, gdn_chunk_tri_solve, gdn_chunk_tri_solve_multi, gdn_chunk_tri_solve_varlen, varlen_chunk_offsets, lib, status_string, tri_inv, tri_inv_ex, version,
 )
-from .layer import add_rms_norm, add_rms_norm_bwd, add_rms_norm_fp8, gdn_chunk_attn, gdn_chunk_attn_varlen, gdn_step  # noqa: F401
+from .layer import add_rms_norm, add_rms_norm_bwd, add_rms_norm_fp8, gdn_chunk_attn, gdn_chunk_attn_bwd, gdn_chunk_attn_bwd_varlen, gdn_chunk_attn_varlen, gdn_step  # noqa: F401

@@ -45,7 +45,8 @@ DTYPE_NAMES = {F32: "f32", F16: "f16", BF16: "bf16"}
 
 EXPORTS = ("tri_inv", "tri_inv_ex", "gdn_chunk_tri_inv", "gdn_chunk_tri_inv_ex", "gdn_chunk_tri_inv_varlen", "gdn_chunk_build_A",
            "gdn_chunk_tri_solve", "gdn_chunk_tri_solve_multi", "gdn_chunk_tri_solve_varlen",
-           "gdn_chunk_attn", "gdn_chunk_attn_varlen", "gdn_chunk_attn_workspace", "gdn_step", "add_rms_norm", "add_rms_norm_bwd", "triinv_status_string", "triinv_version")
+           "gdn_chunk_attn", "gdn_chunk_attn_varlen", "gdn_chunk_attn_workspace", "gdn_chunk_attn_bwd",
+           "gdn_chunk_attn_bwd_varlen", "gdn_chunk_attn_bwd_workspace", "gdn_step", "add_rms_norm", "add_rms_norm_bwd", "triinv_status_string", "triinv_version")
 
 _lib: Optional[ctypes.CDLL] = None
 
@@ -95,10 +96,14 @@ def lib() -> ctypes.CDLL:
         L.gdn_chunk_attn.argtypes = [vp] * 9 + [i64, i32, i64, i32, i32, i32, i32, i32, i32, f32, vp]
         L.gdn_chunk_attn_varlen.argtypes = [vp] * 9 + [i64, vp, vp, i32, i64, i64, i32, i32, i32, i32, i32, i32, f32, vp]
         L.gdn_chunk_attn_workspace.argtypes = [i32, i64, i32, i32, i32, i32, vp]
+        L.gdn_chunk_attn_bwd.argtypes = [vp] * 15 + [i64, i32, i64, i32, i32, i32, i32, i32, i32, f32, vp]
+        L.gdn_chunk_attn_bwd_varlen.argtypes = [vp] * 15 + [i64, vp, vp, i32, i64, i64, i32, i32, i32, i32, i32, i32, f32, vp]
+        L.gdn_chunk_attn_bwd_workspace.argtypes = [i64, i64, i32, i32, i32, i32, vp]
         L.gdn_step.argtypes = [vp] * 8 + [i32, i64, i32, i32, i32, i32, i32, f32, vp]
         L.add_rms_norm.argtypes = [vp] * 6 + [i64, i32, i32, i32, f32, vp]
         L.add_rms_norm_bwd.argtypes = [vp] * 7 + [i64, i64, i32, i32, f32, vp]
-        for f in (L.gdn_chunk_attn, L.gdn_chunk_attn_varlen, L.gdn_chunk_attn_workspace, L.gdn_step, L.add_rms_norm, L.add_rms_norm_bwd):
+        for f in (L.gdn_chunk_attn, L.gdn_chunk_attn_varlen, L.gdn_chunk_attn_workspace, L.gdn_chunk_attn_bwd, L.gdn_chunk_attn_bwd_varlen,
+                  L.gdn_chunk_attn_bwd_workspace, L.gdn_step, L.add_rms_norm, L.add_rms_norm_bwd):
             f.restype = i32
         L.triinv_detail_chunk_offsets.argtypes = [vp, i32, i32, i64, vp, vp, vp]
         L.triinv_detail_chunk_offsets.restype = i32

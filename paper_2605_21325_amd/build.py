@@ -43,7 +43,7 @@ UNITS = [
     (f"solve_nb{nb}_op{op}", "solve.hip", [f"-DTRIINV_INST_NB={nb}", f"-DTRIINV_INST_OP={op}"])
     for nb in (8, 4, 2, 1) for op in (0, 1, 2)
 ] + [
-    (f"attn_op{op}", "attn.hip", [f"-DTRIINV_INST_OP={op}"]) for op in (1, 2)
+    (f"{name}_op{op}", f"{name}.hip", [f"-DTRIINV_INST_OP={op}"]) for name in ("attn_bwd", "attn") for op in (1, 2)
 ] + [("norm", "norm.hip", []), ("step", "step.hip", []), ("layer", "layer.hip", []), ("api", "api.hip", [])]
 
 

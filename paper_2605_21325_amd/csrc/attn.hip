@@ -32,12 +32,12 @@ template <int MT, int KP, bool DELTA> int go(const AttnCall& c)
     const unsigned heads = (unsigned)(c.n_seq * c.H), groups = (unsigned)((c.d_v + COLS - 1) / COLS);
     if (c.n_seg > 1) {
         const unsigned more = DELTA ? (unsigned)((c.d_k + COLS - 1) / COLS) : 0u;
-        int rc = launch_kernel(false, k_chunk_attn<OP, MT, KP, NT, WAVES, DELTA, false>, dim3(heads * (groups + more), (unsigned)c.n_seg - 1), dim3(64 * WAVES), 0, c.stream, a);
+        int rc = launch_kernel(false, k_chunk_attn<OP, MT, KP, NT, WAVES, DELTA, ATTN_SEGMENT>, dim3(heads * (groups + more), (unsigned)c.n_seg - 1), dim3(64 * WAVES), 0, c.stream, a);
         if (rc != LAUNCHED) return rc;
         rc = launch_kernel(false, k_attn_join<KP, 4, DELTA>, dim3(heads * ((c.d_v + 63) / 64)), dim3(256), 0, c.stream, a);
         if (rc != LAUNCHED) return rc;
     }
-    return launch_kernel(false, k_chunk_attn<OP, MT, KP, NT, WAVES, DELTA, true>, dim3(heads * groups, (unsigned)c.n_seg), dim3(64 * WAVES), 0, c.stream, a);
+    return launch_kernel(false, k_chunk_attn<OP, MT, KP, NT, WAVES, DELTA, ATTN_OUT>, dim3(heads * groups, (unsigned)c.n_seg), dim3(64 * WAVES), 0, c.stream, a);
 }
 template <int MT, bool DELTA> int go_k(const AttnCall& c) { return c.d_k <= 64 ? go<MT, 2, DELTA>(c) : go<MT, 4, DELTA>(c); }
 template <int MT> int go_delta(const AttnCall& c) { return c.W ? go_k<MT, true>(c) : go_k<MT, false>(c); }

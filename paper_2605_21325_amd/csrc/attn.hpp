@@ -20,6 +20,7 @@ struct AttnArgs {
     // Segments of the sequences (a workgroup each), where there are too few heads: what a segment adds to a state and what it does to
     // the one before it, or the states before the segments from them.
     float *seg_state, *seg_trans, *seg_decay;
+    float *rec_state, *rec_value;  // for the gradient: the states before the chunks [chunk][H][d_k][d_v], and V' [token][H][d_v] where it is not U
     SeqMap map;
     int H, group, d_k, d_v, C;  // group: heads that share a key head
     int n_seg;
@@ -36,6 +37,32 @@ __device__ __forceinline__ void segment_chunks(int64_t n, int n_seg, int seg, in
 
 // Channel of row `row` (0..15) of state tile t (attn_ops.hpp).
 __device__ __forceinline__ int state_channel(int t, int row) { return 32 * (t >> 1) + 8 * (row >> 2) + 4 * (t & 1) + (row & 3); }
+
+// State tiles of a wavefront's columns from `col0` on, from and to memory [d_k][d_v].  No address: zeros, or the identity.
+template <int KP, int NT> __device__ __forceinline__ void get_state(const float* from, v4f (&S)[NT][2 * KP], int d_k, int d_v, int col0, bool identity, Lane ln)
+{
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 2 * KP; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int ch = state_channel(i, 4 * ln.q + r), col = col0 + 16 * t + ln.n;
+                S[t][i][r] = from && ch < d_k && col < d_v ? from[(int64_t)ch * d_v + col] : identity && ch == col ? 1.f : 0.f;
+            }
+}
+template <int KP, int NT> __device__ __forceinline__ void put_state(float* to, const v4f (&S)[NT][2 * KP], int d_k, int d_v, int col0, Lane ln)
+{
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 2 * KP; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int ch = state_channel(i, 4 * ln.q + r), col = col0 + 16 * t + ln.n;
+                if (ch < d_k && col < d_v) to[(int64_t)ch * d_v + col] = S[t][i][r];
+            }
+}
 
 // MT tiles of 16 token rows, KP pairs of tiles of 16 channels, NT column tiles a wavefront, WAVES wavefronts.
 template <int OP, int MT, int KP, int NT, int WAVES, bool DELTA> struct AttnLayout {
@@ -205,24 +232,27 @@ __device__ __forceinline__ void chunk_scores(char* lds, const float* gl, float s
     }
 }
 
-// OUT: the outputs and the final state.  Otherwise what a segment adds to a state (column groups of d_v) and, with W, what it does to
-// the one before it: the same recursion from the identity with U = 0 (column groups of d_k behind them).
-template <int OP, int MT, int KP, int NT, int WAVES, bool DELTA, bool OUT>
+// ATTN_OUT: the outputs and the final state.  ATTN_SEGMENT: what a segment adds to a state (column groups of d_v) and, with W, what it does to
+// the one before it: the same recursion from the identity with U = 0 (column groups of d_k behind them).  ATTN_RECORD: the states before
+// the chunks and the chunks' values, for the gradient.
+enum : int { ATTN_OUT = 0, ATTN_SEGMENT = 1, ATTN_RECORD = 2 };
+template <int OP, int MT, int KP, int NT, int WAVES, bool DELTA, int MODE>
 __global__ __launch_bounds__(64 * WAVES) void k_chunk_attn(AttnArgs a)
 {
     typedef AttnLayout<OP, MT, KP, NT, WAVES, DELTA> LY;
+    constexpr bool OUT = MODE == ATTN_OUT, SEGMENT = MODE == ATTN_SEGMENT;
     constexpr int THREADS = 64 * WAVES, R = LY::R;
     __shared__ __attribute__((aligned(16))) char lds[LY::BYTES];
     float* const gl = reinterpret_cast<float*>(lds + LY::G_AT);  // g, exp(g_C - g), scale exp(g)
     const Lane ln = lane_id();
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-    const unsigned groups_v = (a.d_v + LY::COLS - 1) / LY::COLS, groups = groups_v + (!OUT && DELTA ? (a.d_k + LY::COLS - 1) / LY::COLS : 0);
+    const unsigned groups_v = (a.d_v + LY::COLS - 1) / LY::COLS, groups = groups_v + (SEGMENT && DELTA ? (a.d_k + LY::COLS - 1) / LY::COLS : 0);
     const unsigned b = xcd_neighbours(blockIdx.x, gridDim.x);
     const unsigned cg = b % groups, hs = b / groups;
     const int seg = blockIdx.y;
     const int h = hs % a.H, s = hs / a.H;
-    const bool trans = !OUT && cg >= groups_v;
+    const bool trans = SEGMENT && cg >= groups_v;
     const int d_v = trans ? a.d_k : a.d_v;
     const int wg_col = (trans ? cg - groups_v : cg) * LY::COLS, col0 = 16 * NT * wave;  // of the workgroup, of the wavefront in it
     const SeqPos sq = seq_pos(a.map, s);
@@ -232,19 +262,8 @@ __global__ __launch_bounds__(64 * WAVES) void k_chunk_attn(AttnArgs a)
     const int hk = h / a.group, H_k = a.H / a.group;
 
     v4f S[NT][2 * KP];
-    {
-        const float* from = OUT ? (seg == 0 ? a.state : a.seg_state + (int64_t)(seg - 1) * a.map.n_seq * a.H * a.d_k * a.d_v) : nullptr;
-        if (from) from += (int64_t)hs * a.d_k * a.d_v;
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int i = 0; i < 2 * KP; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int ch = state_channel(i, 4 * ln.q + r), col = wg_col + col0 + 16 * t + ln.n;
-                    S[t][i][r] = from && ch < a.d_k && col < d_v ? from[(int64_t)ch * d_v + col] : trans && ch == col ? 1.f : 0.f;
-                }
-    }
+    const float* from = !SEGMENT ? (seg == 0 ? a.state : a.seg_state + (int64_t)(seg - 1) * a.map.n_seq * a.H * a.d_k * a.d_v) : nullptr;
+    get_state<KP, NT>(from ? from + (int64_t)hs * a.d_k * a.d_v : nullptr, S, a.d_k, d_v, wg_col + col0, trans, ln);
 
     RowLoader<LY::PIECES, R, THREADS> lq, lk, lw;
     RowLoader<LY::UPIECES, R, THREADS> lu;
@@ -283,13 +302,28 @@ __global__ __launch_bounds__(64 * WAVES) void k_chunk_attn(AttnArgs a)
 
         const float g_last = gl[R - 1], decay = expf(g_last);
         total += g_last;
+        if constexpr (MODE == ATTN_RECORD) {
+            const int64_t id = (a.map.cu_chunks ? a.map.cu_chunks[s] : s * n_chunk) + c;
+            put_state<KP, NT>(a.rec_state + (id * a.H + h) * a.d_k * a.d_v, S, a.d_k, a.d_v, wg_col + col0, ln);
+        }
         Parts<FULL_PARTS<OP>> sp[NT][KP];
         int s_shift = 0;
         if constexpr (DELTA || OUT) s_shift = split_state<OP, KP, NT>(S, sp);
         ChunkValues<OP, MT, KP, NT, DELTA> cv;
         chunk_values<OP, MT, KP, NT, DELTA, LY>(cv, lds, sp, s_shift, col0, ln);
+        if constexpr (MODE == ATTN_RECORD && DELTA) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int tb = 0; tb < MT; ++tb)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int i = 16 * tb + 4 * ln.q + r, col = wg_col + col0 + 16 * t + ln.n;
+                        if (i < valid && col < a.d_v) a.rec_value[((sq.tok0 + c * a.C + i) * a.H + h) * a.d_v + col] = cv.v[t][tb][r];
+                    }
+        }
         chunk_state<OP, MT, KP, NT, DELTA, LY>(S, cv, lds, gl + R, decay, ln);
-        __syncthreads();  // the scores are in LDS
+        if constexpr (OUT) __syncthreads();  // the scores are in LDS
         if constexpr (OUT) {
             Parts<2> vp[NT][MT / 2];
             const float up = OP == OP_F16 ? pow2(cv.shift) : 1.f, down = OP == OP_F16 ? pow2(-cv.shift) : 1.f;
@@ -351,21 +385,12 @@ __global__ __launch_bounds__(64 * WAVES) void k_chunk_attn(AttnArgs a)
         __syncthreads();  // the rows are not needed any more
     }
 
-    if (OUT && seg != a.n_seg - 1) return;
-    float* to = OUT ? a.final_state : trans ? a.seg_trans : a.seg_state;
+    if (!SEGMENT && seg != a.n_seg - 1) return;
+    float* to = !SEGMENT ? a.final_state : trans ? a.seg_trans : a.seg_state;
     if (!to) return;
-    if (!OUT) to += (int64_t)seg * a.map.n_seq * a.H * a.d_k * d_v;
-    to += (int64_t)hs * a.d_k * d_v;
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int i = 0; i < 2 * KP; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int ch = state_channel(i, 4 * ln.q + r), col = wg_col + col0 + 16 * t + ln.n;
-                if (ch < a.d_k && col < d_v) to[(int64_t)ch * d_v + col] = S[t][i][r];
-            }
-    if (!OUT && !DELTA && cg == 0 && tid == 0) a.seg_decay[(int64_t)seg * a.map.n_seq * a.H + hs] = expf(total);
+    if (SEGMENT) to += (int64_t)seg * a.map.n_seq * a.H * a.d_k * d_v;
+    put_state<KP, NT>(to + (int64_t)hs * a.d_k * d_v, S, a.d_k, d_v, wg_col + col0, ln);
+    if (SEGMENT && !DELTA && cg == 0 && tid == 0) a.seg_decay[(int64_t)seg * a.map.n_seq * a.H + hs] = expf(total);
 }
 
 // States before the segments, in place of what the segments add: S <- M_seg S + L_seg from the sequence's initial state.  M and S as

@@ -79,6 +79,36 @@ int attn_common(const void* Q, const void* K, const void* U, const void* W, cons
     return finish(dtype == TRIINV_F16 ? launch_chunk_attn_f16(a) : launch_chunk_attn_bf16(a));
 }
 
+// States before and gradients behind every chunk, and the values where they are not U.
+int64_t attn_bwd_workspace(int64_t n_token, int64_t n_chunk, int H, int d_k, int d_v, bool has_w)
+{
+    return 4 * H * (2 * n_chunk * d_k * d_v + (has_w ? n_token * d_v : 0));
+}
+
+int attn_bwd_common(const void* Q, const void* K, const void* U, const void* W, const float* g, const float* state, const void* dO, const float* dstate, void* dQ,
+                    void* dK, void* dU, void* dW, float* dg, float* dstate0, void* workspace, int64_t workspace_bytes, const int64_t* cu_seqlens,
+                    const int64_t* cu_chunks, int n_seq, int64_t Tlen, int64_t n_token, int64_t n_chunk, int H, int H_k, int d_k, int d_v, int C, int dtype, float scale,
+                    void* hip_stream)
+{
+    if (dtype == TRIINV_F32) return TRIINV_ERR_UNSUPPORTED;
+    if ((int64_t)H * d_v * C * 4 >= (1LL << 31)) return TRIINV_ERR_UNSUPPORTED;  // (values are read back in fp32)
+    const int64_t need = attn_bwd_workspace(n_token, n_chunk, H, d_k, d_v, W != nullptr);
+    if (n_token > 0 && (!Q || !K || !U || !dO || !dQ || !dK || !dU || !workspace || (W != nullptr) != (dW != nullptr))) return TRIINV_ERR_NULL;
+    if (dg && !g) return TRIINV_ERR_NULL;
+    if (workspace_bytes < need) return TRIINV_ERR_BAD_SHAPE;
+    for (const void* p : {Q, K, U, W, dO, (const void*)state, (const void*)dstate, (const void*)dQ, (const void*)dK, (const void*)dU, (const void*)dW, (const void*)dstate0, (const void*)workspace})
+        if (!aligned(p, 16)) return TRIINV_ERR_ALIGN;
+    if (!aligned(g, 4) || !aligned(dg, 4) || !aligned(cu_seqlens, 8) || !aligned(cu_chunks, 8)) return TRIINV_ERR_ALIGN;
+    const uint64_t qk = (uint64_t)n_token * H_k * d_k * 2, v = (uint64_t)n_token * H * d_v * 2, w = (uint64_t)n_token * H * d_k * 2, st = (uint64_t)n_seq * H * d_k * d_v * 4,
+                   gs = (uint64_t)n_token * H * 4, cu = (uint64_t)(n_seq + 1) * 8;
+    const Span in[] = {{Q, qk}, {K, qk}, {U, v}, {W, w}, {dO, v}, {g, gs}, {state, st}, {dstate == dstate0 ? nullptr : dstate, st}, {cu_seqlens, cu}, {cu_chunks, cu}};
+    const Span out[] = {{dQ, qk}, {dK, qk}, {dU, v}, {dW, w}, {dg, gs}, {dstate0, st}, {workspace, (uint64_t)need}};
+    if (aliased(in, out)) return TRIINV_ERR_ALIAS;
+    const AttnBwdCall a{Q, K, U, W, dO, g, state, dstate, dQ, dK, dU, dW, dg, dstate0, static_cast<char*>(workspace), cu_seqlens, cu_chunks, Tlen, n_seq, n_chunk, H, H_k,
+                        d_k, d_v, C, scale, static_cast<hipStream_t>(hip_stream)};
+    return finish(dtype == TRIINV_F16 ? launch_chunk_attn_bwd_f16(a) : launch_chunk_attn_bwd_bf16(a));
+}
+
 // Totals of packed sequences against each other.
 bool packed_totals_ok(int n_seq, int64_t n_token, int64_t n_chunk, int C)
 {
@@ -121,6 +151,41 @@ int gdn_chunk_attn_varlen(const void* Q, const void* K, const void* U, const voi
     if (!cu_seqlens || !cu_chunks) return TRIINV_ERR_NULL;
     return attn_common(Q, K, U, W, g, state, O, final_state, workspace, workspace_bytes, cu_seqlens, cu_chunks, n_seq, 0, total_tokens, total_chunks, H, H_k, d_k,
                        d_v, C, dtype, scale, hip_stream);
+}
+
+int gdn_chunk_attn_bwd_workspace(int64_t total_tokens, int64_t total_chunks, int H, int d_k, int d_v, int has_w, int64_t* bytes)
+{
+    if (!bytes) return TRIINV_ERR_NULL;
+    if (total_tokens < 0 || total_chunks < 0 || H <= 0 || d_k <= 0 || d_v <= 0) return TRIINV_ERR_BAD_SHAPE;
+    *bytes = attn_bwd_workspace(total_tokens, total_chunks, H, d_k, d_v, has_w != 0);
+    return TRIINV_OK;
+}
+
+int gdn_chunk_attn_bwd(const void* Q, const void* K, const void* U, const void* W, const float* g, const float* state, const void* dO, const float* dstate, void* dQ,
+                       void* dK, void* dU, void* dW, float* dg, float* dstate0, void* workspace, int64_t workspace_bytes, int B, int64_t Tlen, int H, int H_k, int d_k,
+                       int d_v, int C, int dtype, float scale, void* hip_stream)
+{
+    if (!any_dtype(dtype)) return TRIINV_ERR_BAD_DTYPE;
+    if (B <= 0 || Tlen < 0 || Tlen > 0x7fffffffLL) return TRIINV_ERR_BAD_SHAPE;
+    const int64_t n_chunk = C > 0 ? (int64_t)B * ((Tlen + C - 1) / C) : 0;
+    const int rc = attn_shape(B, (int64_t)B * Tlen, n_chunk, H, H_k, d_k, d_v, C);
+    if (rc) return rc;
+    return attn_bwd_common(Q, K, U, W, g, state, dO, dstate, dQ, dK, dU, dW, dg, dstate0, workspace, workspace_bytes, nullptr, nullptr, B, Tlen, (int64_t)B * Tlen, n_chunk,
+                           H, H_k, d_k, d_v, C, dtype, scale, hip_stream);
+}
+
+int gdn_chunk_attn_bwd_varlen(const void* Q, const void* K, const void* U, const void* W, const float* g, const float* state, const void* dO, const float* dstate,
+                              void* dQ, void* dK, void* dU, void* dW, float* dg, float* dstate0, void* workspace, int64_t workspace_bytes, const int64_t* cu_seqlens,
+                              const int64_t* cu_chunks, int n_seq, int64_t total_tokens, int64_t total_chunks, int H, int H_k, int d_k, int d_v, int C, int dtype,
+                              float scale, void* hip_stream)
+{
+    if (!any_dtype(dtype)) return TRIINV_ERR_BAD_DTYPE;
+    const int rc = attn_shape(n_seq, total_tokens, total_chunks, H, H_k, d_k, d_v, C);
+    if (rc) return rc;
+    if (!packed_totals_ok(n_seq, total_tokens, total_chunks, C)) return TRIINV_ERR_BAD_SHAPE;
+    if (!cu_seqlens || !cu_chunks) return TRIINV_ERR_NULL;
+    return attn_bwd_common(Q, K, U, W, g, state, dO, dstate, dQ, dK, dU, dW, dg, dstate0, workspace, workspace_bytes, cu_seqlens, cu_chunks, n_seq, 0, total_tokens,
+                           total_chunks, H, H_k, d_k, d_v, C, dtype, scale, hip_stream);
 }
 
 int gdn_step(const void* q, const void* k, const void* v, const float* g, const float* beta, float* state, const int32_t* slots, void* o, int B,

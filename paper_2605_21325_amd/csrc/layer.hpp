@@ -24,6 +24,23 @@ struct AttnCall {
 int launch_chunk_attn_f16(const AttnCall& a);
 int launch_chunk_attn_bf16(const AttnCall& a);
 
+struct AttnBwdCall {
+    const void *Q, *K, *U, *W, *dO;
+    const float *g, *state, *dstate;
+    void *dQ, *dK, *dU, *dW;
+    float *dg, *dstate0;
+    char* workspace;
+    const int64_t *cu_seqlens, *cu_chunks;
+    int64_t Tlen;
+    int n_seq;
+    int64_t n_chunk;
+    int H, H_k, d_k, d_v, C;
+    float scale;
+    hipStream_t stream;
+};
+int launch_chunk_attn_bwd_f16(const AttnBwdCall& a);
+int launch_chunk_attn_bwd_bf16(const AttnBwdCall& a);
+
 struct StepCall {
     const void *q, *k, *v;
     const float *g, *beta;

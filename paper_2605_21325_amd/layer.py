@@ -111,6 +111,48 @@ def gdn_chunk_attn_varlen(Q: torch.Tensor, K: torch.Tensor, U: torch.Tensor, g: 
     return O, final_state
 
 
+def _attn_bwd(where, Q, K, U, g, dO, C, W, state, dstate, scale, stream, lead, n_seq, n_token, n_chunk, map_args):
+    H, H_k, d_k, d_v = _attn_checked(Q, K, U, g, W, state, lead, n_seq)
+    _has(dO, "dO", U.shape, U.dtype)
+    _has(dstate, "dstate", (n_seq, H, d_k, d_v), torch.float32)
+    size = ctypes.c_int64()
+    st = binding.lib().gdn_chunk_attn_bwd_workspace(n_token, n_chunk, H, d_k, d_v, W is not None, ctypes.byref(size))
+    if st != OK:
+        raise TriInvError(st, where)
+    with _on(stream):
+        dQ, dK, dU = torch.empty_like(Q), torch.empty_like(K), torch.empty_like(U)
+        dW = None if W is None else torch.empty_like(W)
+        dg = None if g is None else torch.empty_like(g)
+        dstate0 = None if state is None else torch.empty_like(state)
+        ws = torch.empty(max(16, size.value), dtype=torch.uint8, device=U.device)
+    st = getattr(binding.lib(), where)(_dev(Q, "Q"), _dev(K, "K"), _dev(U, "U"), _opt(W, "W"), _opt(g, "g"), _opt(state, "state"), _dev(dO, "dO"), _opt(dstate, "dstate"),
+                                       _dev(dQ, "dQ"), _dev(dK, "dK"), _dev(dU, "dU"), _opt(dW, "dW"), _opt(dg, "dg"), _opt(dstate0, "dstate0"), _dev(ws, "workspace"),
+                                       ws.numel(), *map_args, H, H_k, d_k, d_v, C, dtype_code(Q.dtype), d_k ** -0.5 if scale is None else scale, _stream_ptr(stream))
+    if st != OK:
+        raise TriInvError(st, where)
+    return dQ, dK, dU, dW, dg, dstate0
+
+
+def gdn_chunk_attn_bwd(Q: torch.Tensor, K: torch.Tensor, U: torch.Tensor, g: Optional[torch.Tensor], dO: torch.Tensor, C: int, W: Optional[torch.Tensor] = None,
+                       state: Optional[torch.Tensor] = None, dstate: Optional[torch.Tensor] = None, scale: Optional[float] = None, stream=None):
+    """(dQ, dK, dU, dW, dg, dstate0) of gdn_chunk_attn, from its inputs and the gradients dO of O and dstate (or None) of final_state; None in the
+    place of the gradient of what was not given."""
+    B, T = Q.shape[:2]
+    return _attn_bwd("gdn_chunk_attn_bwd", Q, K, U, g, dO, C, W, state, dstate, scale, stream, (B, T), B, B * T, B * ((T + C - 1) // C) if C > 0 else 0, (B, T))
+
+
+def gdn_chunk_attn_bwd_varlen(Q: torch.Tensor, K: torch.Tensor, U: torch.Tensor, g: Optional[torch.Tensor], dO: torch.Tensor, seqlens, C: int,
+                              W: Optional[torch.Tensor] = None, state: Optional[torch.Tensor] = None, dstate: Optional[torch.Tensor] = None,
+                              scale: Optional[float] = None, stream=None):
+    """gdn_chunk_attn_bwd on packed sequences (see gdn_chunk_attn_varlen)."""
+    total = Q.shape[0]
+    cu_s, cu_c, n_seq, n_chunk, keep = _chunk_offsets(Q, seqlens if isinstance(seqlens, (list, tuple)) else list(seqlens), C, stream)
+    got = _attn_bwd("gdn_chunk_attn_bwd_varlen", Q, K, U, g, dO, C, W, state, dstate, scale, stream, (total,), n_seq, total, n_chunk,
+                    (cu_s, cu_c, n_seq, total, n_chunk))
+    got[0]._triinv_keepalive = keep  # the launch is asynchronous: the offsets live as long as the result
+    return got
+
+
 def gdn_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, g: Optional[torch.Tensor], state: torch.Tensor, beta: Optional[torch.Tensor] = None,
              slots: Optional[torch.Tensor] = None, scale: Optional[float] = None, o: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """One token of the layer: q, k [B, H_k, d_k], v [B, H, d_v], g [B, H] the token's log-decay or None; state [n_slot, H, d_k, d_v] fp32 is
