@@ -324,7 +324,7 @@ int gdn_chunk_attn_workspace(int n_seq, int64_t total_chunks, int H, int d_k, in
  *   dU, dW       device, like U and W, written (dW NULL without W).
  *   dg           device, fp32 [B][Tlen][H], written: the gradient of the chunk-local cumulative log-decay as it was given; or NULL.
  *   dstate0      device, fp32 [B][H][d_k][d_v], written: the gradient of `state`; or NULL.  May be dstate itself.
- *   workspace    device, workspace_bytes of it as gdn_chunk_attn_bwd_workspace says (8 H d_k d_v bytes a chunk and, with W, 4 H d_v a token), 16-byte aligned.
+ *   workspace    device, workspace_bytes of it as gdn_chunk_attn_bwd_workspace says (8 H d_k d_v bytes a chunk, twice that at C = 128, and, with W, 4 H d_v a token), 16-byte aligned.
  * The states are computed again, nothing of the forward call is needed.  Sums are fp32 and their order is fixed.  The rows a chunk covers must stay below
  * 2^31 bytes with d_v in fp32.  fp16: the chunk's values V' must stay below 65504.
  */
@@ -337,7 +337,7 @@ int gdn_chunk_attn_bwd_varlen(const void* Q, const void* K, const void* U, const
                               void* workspace, int64_t workspace_bytes,
                               const int64_t* cu_seqlens, const int64_t* cu_chunks, int n_seq, int64_t total_tokens, int64_t total_chunks,
                               int H, int H_k, int d_k, int d_v, int C, int dtype, float scale, void* hip_stream);
-int gdn_chunk_attn_bwd_workspace(int64_t total_tokens, int64_t total_chunks, int H, int d_k, int d_v, int has_w, int64_t* bytes);
+int gdn_chunk_attn_bwd_workspace(int64_t total_tokens, int64_t total_chunks, int H, int d_k, int d_v, int C, int has_w, int64_t* bytes);
 
 /*
  * gdn_step: the same layer's single token, the state updated in place.  Per sequence b and head:

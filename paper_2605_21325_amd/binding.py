@@ -98,7 +98,7 @@ def lib() -> ctypes.CDLL:
         L.gdn_chunk_attn_workspace.argtypes = [i32, i64, i32, i32, i32, i32, vp]
         L.gdn_chunk_attn_bwd.argtypes = [vp] * 15 + [i64, i32, i64, i32, i32, i32, i32, i32, i32, f32, vp]
         L.gdn_chunk_attn_bwd_varlen.argtypes = [vp] * 15 + [i64, vp, vp, i32, i64, i64, i32, i32, i32, i32, i32, i32, f32, vp]
-        L.gdn_chunk_attn_bwd_workspace.argtypes = [i64, i64, i32, i32, i32, i32, vp]
+        L.gdn_chunk_attn_bwd_workspace.argtypes = [i64, i64, i32, i32, i32, i32, i32, vp]
         L.gdn_step.argtypes = [vp] * 8 + [i32, i64, i32, i32, i32, i32, i32, f32, vp]
         L.add_rms_norm.argtypes = [vp] * 6 + [i64, i32, i32, i32, f32, vp]
         L.add_rms_norm_bwd.argtypes = [vp] * 7 + [i64, i64, i32, i32, f32, vp]

@@ -25,22 +25,22 @@ AttnArgs args_of(const AttnCall& c)
     return a;
 }
 
-template <int MT, int KP, bool DELTA> int go(const AttnCall& c)
+template <int MT, int KP, bool DELTA, bool TWO> int go(const AttnCall& c)
 {
-    constexpr int NT = 1, WAVES = 4, COLS = 16 * NT * WAVES;
     const AttnArgs a = args_of(c);
-    const unsigned heads = (unsigned)(c.n_seq * c.H), groups = (unsigned)((c.d_v + COLS - 1) / COLS);
+    const unsigned heads = (unsigned)(c.n_seq * c.H), groups = (unsigned)((c.d_v + ATTN_COLS - 1) / ATTN_COLS);
     if (c.n_seg > 1) {
-        const unsigned more = DELTA ? (unsigned)((c.d_k + COLS - 1) / COLS) : 0u;
-        int rc = launch_kernel(false, k_chunk_attn<OP, MT, KP, NT, WAVES, DELTA, ATTN_SEGMENT>, dim3(heads * (groups + more), (unsigned)c.n_seg - 1), dim3(64 * WAVES), 0, c.stream, a);
+        const unsigned more = DELTA ? (unsigned)((c.d_k + ATTN_COLS - 1) / ATTN_COLS) : 0u;
+        int rc = launch_kernel(false, k_chunk_attn<OP, MT, KP, DELTA, ATTN_SEGMENT, TWO>, dim3(heads * (groups + more), (unsigned)c.n_seg - 1), dim3(512), 0, c.stream, a);
         if (rc != LAUNCHED) return rc;
-        rc = launch_kernel(false, k_attn_join<KP, 4, DELTA>, dim3(heads * ((c.d_v + 63) / 64)), dim3(256), 0, c.stream, a);
+        rc = DELTA ? launch_kernel(false, k_attn_join<KP>, dim3(heads * ((c.d_v + 15) / 16)), dim3(256), 0, c.stream, a)
+                   : launch_kernel(false, k_attn_join_plain, dim3((unsigned)(((int64_t)heads * c.d_k * c.d_v + 255) / 256)), dim3(256), 0, c.stream, a);
         if (rc != LAUNCHED) return rc;
     }
-    return launch_kernel(false, k_chunk_attn<OP, MT, KP, NT, WAVES, DELTA, ATTN_OUT>, dim3(heads * groups, (unsigned)c.n_seg), dim3(64 * WAVES), 0, c.stream, a);
+    return launch_kernel(false, k_chunk_attn<OP, MT, KP, DELTA, ATTN_OUT, TWO>, dim3(heads * groups, (unsigned)c.n_seg), dim3(512), 0, c.stream, a);
 }
-template <int MT, bool DELTA> int go_k(const AttnCall& c) { return c.d_k <= 64 ? go<MT, 2, DELTA>(c) : go<MT, 4, DELTA>(c); }
-template <int MT> int go_delta(const AttnCall& c) { return c.W ? go_k<MT, true>(c) : go_k<MT, false>(c); }
+template <int MT, bool DELTA, bool TWO> int go_k(const AttnCall& c) { return c.d_k <= 64 ? go<MT, 2, DELTA, TWO>(c) : go<MT, 4, DELTA, TWO>(c); }
+template <int MT, bool TWO> int go_delta(const AttnCall& c) { return c.W ? go_k<MT, true, TWO>(c) : go_k<MT, false, false>(c); }
 
 }  // namespace
 
@@ -49,6 +49,6 @@ template <int MT> int go_delta(const AttnCall& c) { return c.W ? go_k<MT, true>(
 #else
 #define LAUNCHER launch_chunk_attn_bf16
 #endif
-int LAUNCHER(const AttnCall& c) { return c.C <= 32 ? go_delta<2>(c) : c.C == 64 ? go_delta<4>(c) : go_delta<8>(c); }
+int LAUNCHER(const AttnCall& c) { return c.C <= 32 ? go_delta<2, false>(c) : c.C == 64 ? go_delta<4, false>(c) : go_delta<4, true>(c); }
 
 }  // namespace triinv

@@ -4,10 +4,17 @@
 //     V' = U - W S                                     (plain decay, no W: V' = U)
 //     O  = scale (diag(G) Q S + (Q K^T . D) V')
 //     S <- G_C S + K^T diag(exp(g_C - g)) V'
-// A workgroup takes some columns of one head through all its chunks (or those of its segment), a wavefront 16 NT of them, S in its
-// registers; what all columns share (rows of Q, K, W; the tiles of (Q K^T . D)^T, formed once a workgroup, a share per wavefront)
-// goes through LDS.  Rows of the next chunk are requested before one is computed.
+// Everything but W S may be taken in smaller steps: a chunk of 128 goes in two of 64 tokens, with g counted from the step's beginning,
+// and W S with the state before the chunk for both.
+//
+// A workgroup takes 64 columns of one head through all its steps (or those of its segment).  Four wavefronts carry the recursion, 16 columns each,
+// S in their registers; four others bring the rows of the next step from memory to LDS, form the scores and the outputs, one product behind:
+//     first half     W S, V'                                    Q S, scores
+//     second half    K^T V', the new S and its parts            scores V', store; rows of the next step to LDS
+// The halves are separated by barriers, across which V' and the parts of S go through LDS.  (All of it in the same four wavefronts, one after the other, took
+// 2.6 times as long: a wavefront per SIMD that waits has nobody to take its place.)
 #pragma once
+
 #include "attn_ops.hpp"
 
 namespace triinv {
@@ -20,7 +27,7 @@ struct AttnArgs {
     // Segments of the sequences (a workgroup each), where there are too few heads: what a segment adds to a state and what it does to
     // the one before it, or the states before the segments from them.
     float *seg_state, *seg_trans, *seg_decay;
-    float *rec_state, *rec_value;  // for the gradient: the states before the chunks [chunk][H][d_k][d_v], and V' [token][H][d_v] where it is not U
+    float *rec_state, *rec_value;  // for the gradient: the states before the steps [step][H][d_k][d_v], and V' [token][H][d_v] where it is not U
     SeqMap map;
     int H, group, d_k, d_v, C;  // group: heads that share a key head
     int n_seg;
@@ -35,433 +42,536 @@ __device__ __forceinline__ void segment_chunks(int64_t n, int n_seg, int seg, in
     last = first + per < n ? first + per : n;
 }
 
-// Channel of row `row` (0..15) of state tile t (attn_ops.hpp).
-__device__ __forceinline__ int state_channel(int t, int row) { return 32 * (t >> 1) + 8 * (row >> 2) + 4 * (t & 1) + (row & 3); }
-
-// State tiles of a wavefront's columns from `col0` on, from and to memory [d_k][d_v].  No address: zeros, or the identity.
-template <int KP, int NT> __device__ __forceinline__ void get_state(const float* from, v4f (&S)[NT][2 * KP], int d_k, int d_v, int col0, bool identity, Lane ln)
+// (By value: the cast of an element of a vector where it stands takes the vector's first.)
+__device__ __forceinline__ uint32_t bits(float x) { return __builtin_bit_cast(uint32_t, x); }
+// State tiles of a wavefront's 16 columns from `col0` on, from and to memory [d_k][d_v].  No address: zeros, or the identity.
+template <int KP> __device__ __forceinline__ void get_state(const float* from, v4f (&S)[2 * KP], int d_k, int d_v, int col0, bool identity, Lane ln)
 {
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+    for (int i = 0; i < 2 * KP; ++i)
 #pragma unroll
-        for (int i = 0; i < 2 * KP; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int ch = state_channel(i, 4 * ln.q + r), col = col0 + 16 * t + ln.n;
-                S[t][i][r] = from && ch < d_k && col < d_v ? from[(int64_t)ch * d_v + col] : identity && ch == col ? 1.f : 0.f;
-            }
-}
-template <int KP, int NT> __device__ __forceinline__ void put_state(float* to, const v4f (&S)[NT][2 * KP], int d_k, int d_v, int col0, Lane ln)
-{
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int i = 0; i < 2 * KP; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int ch = state_channel(i, 4 * ln.q + r), col = col0 + 16 * t + ln.n;
-                if (ch < d_k && col < d_v) to[(int64_t)ch * d_v + col] = S[t][i][r];
-            }
-}
-
-// MT tiles of 16 token rows, KP pairs of tiles of 16 channels, NT column tiles a wavefront, WAVES wavefronts.
-template <int OP, int MT, int KP, int NT, int WAVES, bool DELTA> struct AttnLayout {
-    static constexpr int R = 16 * MT, PIECES = 4 * KP, COLS = 16 * NT * WAVES, UPIECES = COLS / 8;
-    static constexpr int ROWS_BYTES = R * PIECES * 16, U_BYTES = R * UPIECES * 16;
-    static constexpr int units_before(int it) { return (it / 2) * (it / 2 + 1) + (it % 2) * (it / 2 + 1); }  // pairs of tiles of P^T before tile column it
-    static constexpr int P_UNITS = units_before(MT), P_BYTES = P_UNITS * 2048;
-    static constexpr int K_AT = 0, Q_AT = ROWS_BYTES, W_AT = 2 * ROWS_BYTES, U_AT = (DELTA ? 3 : 2) * ROWS_BYTES, P_AT = U_AT + U_BYTES, G_AT = P_AT + P_BYTES;
-    static constexpr int BYTES = G_AT + 3 * R * 4;
-};
-
-// What a wavefront keeps of one chunk's rows of its columns.
-template <int OP, int MT, int KP, int NT, bool DELTA> struct ChunkValues {
-    v4f v[NT][MT];  // V', in units of 2^-shift
-    int shift;      // fp16: V' = v as it is; its parts are of v 2^shift
-};
-
-// V' of a chunk: U from LDS, minus W S.  sp: parts of S 2^s_shift.
-template <int OP, int MT, int KP, int NT, bool DELTA, class LY>
-__device__ __forceinline__ void chunk_values(ChunkValues<OP, MT, KP, NT, DELTA>& c, const char* lds, const Parts<FULL_PARTS<OP>> (&sp)[NT][KP], int s_shift, int col0, Lane ln)
-{
-    const float down = OP == OP_F16 ? pow2(-s_shift) : 1.f;
-#pragma unroll
-    for (int tb = 0; tb < MT; ++tb) {
-        v4f acc[NT];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) acc[t] = zero4();
-        if constexpr (DELTA) {
-#pragma unroll
-            for (int p = 0; p < KP; ++p) {
-                const v4u w = lds_row<LY::PIECES>(lds + LY::W_AT, 16 * tb + ln.n, 4 * p + ln.q);
-#pragma unroll
-                for (int part = FULL_PARTS<OP> - 1; part >= 0; --part)
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) acc[t] = mfma32<OP>(w, sp[t][p].u[part], acc[t]);
-            }
+        for (int r = 0; r < 4; ++r) {
+            const int ch = state_channel(i, 4 * ln.q + r), col = col0 + ln.n;
+            S[i][r] = from && ch < d_k && col < d_v ? from[(int64_t)ch * d_v + col] : identity && ch == col ? 1.f : 0.f;
         }
+}
+// (Buffer stores: what belongs to every lane of an address goes as a scalar, columns that are not there lie outside the buffer.)
+template <int KP> __device__ __forceinline__ void put_state(float* to, const v4f (&S)[2 * KP], int d_k, int d_v, int col0, Lane ln)
+{
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(to, 0, (uint32_t)d_k * d_v * 4u, 0x00020000);
+    const uint32_t at = col0 + ln.n < d_v ? (uint32_t)(8 * ln.q * d_v + col0 + ln.n) * 4u : 0x80000000u;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const v2u raw = lds_turned<LY::UPIECES>(lds + LY::U_AT, 16 * tb + 4 * ln.q + (ln.n >> 2), (col0 >> 2) + 4 * t + (ln.n & 3));
-            v4f u;
+    for (int i = 0; i < 2 * KP; ++i) {
+        if (32 * (i >> 1) >= d_k) continue;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const uint16_t x = (uint16_t)(raw[r >> 1] >> (16 * (r & 1)));
-                u[r] = OP == OP_F16 ? f16_to_f32(x) : bf16_to_f32(x);
-            }
-            if constexpr (DELTA) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) u[r] -= OP == OP_F16 ? acc[t][r] * down : acc[t][r];
-            }
-            c.v[t][tb] = u;
-        }
-    }
-    c.shift = 0;
-    if constexpr (OP == OP_F16) {
-        float most = 0.f;
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int tb = 0; tb < MT; ++tb)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) most = fmaxf(most, fabsf(c.v[t][tb][r]));
-        c.shift = f16_shift(wave_max(most));
+        for (int r = 0; r < 4; ++r) __builtin_amdgcn_raw_buffer_store_b32(bits(S[i][r]), rsrc, at, (state_channel(i, 0) + r) * d_v * 4, 0);
     }
 }
 
-// S <- G_C S + K^T diag(e) V'.  e: exp(g_C - g) of the chunk's rows, in LDS.
-template <int OP, int MT, int KP, int NT, bool DELTA, class LY>
-__device__ __forceinline__ void chunk_state(v4f (&S)[NT][2 * KP], const ChunkValues<OP, MT, KP, NT, DELTA>& c, const char* lds, const float* e, float decay, Lane ln)
+// Largest magnitude of some tiles.
+template <int N> __device__ __forceinline__ float most_of(const v4f (&x)[N])
 {
-    const float up = OP == OP_F16 ? pow2(c.shift) : 1.f, a = decay * up;
+    float most = 0.f;
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+    for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int i = 0; i < 2 * KP; ++i)
+        for (int r = 0; r < 4; ++r) most = fmaxf(most, fabsf(x[i][r]));
+    return most;
+}
+__device__ __forceinline__ v4f times(v4f x, float a)
+{
 #pragma unroll
-            for (int r = 0; r < 4; ++r) S[t][i][r] *= a;
+    for (int r = 0; r < 4; ++r) x[r] *= a;
+    return x;
+}
+
+// S + X^T V (channels x columns): rows of X read turned, vp the parts of V.  Here as everywhere, products that add to one tile are kept apart by those of
+// other tiles: one behind the other they take three times as long.
+template <int OP, int MT, int KP>
+__device__ __forceinline__ void add_turned(v4f (&S)[2 * KP], const char* rows, const Parts<FULL_PARTS<OP>> (&vp)[MT / 2], Lane ln)
+{
 #pragma unroll
     for (int tp = 0; tp < MT / 2; ++tp) {
-        Parts<FULL_PARTS<OP>> vp[NT];
-        const v4f e0 = *reinterpret_cast<const v4f*>(e + 32 * tp + 4 * ln.q), e1 = *reinterpret_cast<const v4f*>(e + 32 * tp + 16 + 4 * ln.q);
+        v4u k[2 * KP];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            v4f x = c.v[t][2 * tp], y = c.v[t][2 * tp + 1];
+        for (int i = 0; i < 2 * KP; ++i) k[i] = lds_turned_tile<4 * KP>(rows, tp, i, ln);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) x[r] *= e0[r] * up, y[r] *= e1[r] * up;
-            vp[t] = split_pair<OP, FULL_PARTS<OP>>(x, y);
-        }
+        for (int part = FULL_PARTS<OP> - 1; part >= 0; --part)
 #pragma unroll
-        for (int i = 0; i < 2 * KP; ++i) {
-            const int col4 = 8 * (i >> 1) + 2 * (ln.n & 3) + (i & 1), row = 32 * tp + 4 * ln.q + (ln.n >> 2);
-            const v2u k0 = lds_turned<LY::PIECES>(lds + LY::K_AT, row, col4), k1 = lds_turned<LY::PIECES>(lds + LY::K_AT, row + 16, col4);
-            const v4u k = {k0[0], k0[1], k1[0], k1[1]};
-#pragma unroll
-            for (int part = FULL_PARTS<OP> - 1; part >= 0; --part)
-#pragma unroll
-                for (int t = 0; t < NT; ++t) S[t][i] = mfma32<OP>(k, vp[t].u[part], S[t][i]);
-        }
-    }
-    if constexpr (OP == OP_F16) {
-        const float down = pow2(-c.shift);
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int i = 0; i < 2 * KP; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) S[t][i][r] *= down;
+            for (int i = 0; i < 2 * KP; ++i) S[i] = mfma32<OP>(k[i], vp[tp].u[part], S[i]);
     }
 }
 
-// Parts of S, fp16: of S 2^shift.
-template <int OP, int KP, int NT> __device__ __forceinline__ int split_state(const v4f (&S)[NT][2 * KP], Parts<FULL_PARTS<OP>> (&sp)[NT][KP])
+// A step's tokens: what of them there is, and their gates.
+struct StepPos {
+    int64_t row;  // of its first token
+    int valid;    // 0: no such step
+    bool inner;   // not a chunk's first step: g counts from the token before
+};
+template <int R> __device__ __forceinline__ StepPos step_pos(const SeqPos& sq, int64_t step, int64_t last, int C)
 {
-    int shift = 0;
-    float up = 1.f;
-    if constexpr (OP == OP_F16) {
-        float most = 0.f;
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int i = 0; i < 2 * KP; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) most = fmaxf(most, fabsf(S[t][i][r]));
-        shift = f16_shift(wave_max(most));
-        up = pow2(shift);
-    }
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int p = 0; p < KP; ++p) {
-            v4f x = S[t][2 * p], y = S[t][2 * p + 1];
-            if constexpr (OP == OP_F16) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) x[r] *= up, y[r] *= up;
-            }
-            sp[t][p] = split_pair<OP, FULL_PARTS<OP>>(x, y);
-        }
-    return shift;
+    const int tokens = C < R ? C : R;
+    const int64_t left = step >= 0 && step < last ? sq.len - step * tokens : 0;
+    return {sq.tok0 + step * tokens, left < tokens ? (int)left : tokens, C > R && (step & 1)};
 }
-
-// The tiles of (scale Q K^T . D)^T that this wavefront forms, two parts each, into LDS as operands.
-template <int OP, int MT, int KP, int WAVES, class LY>
-__device__ __forceinline__ void chunk_scores(char* lds, const float* gl, float scale, int wave, Lane ln)
+__device__ __forceinline__ float buffer_float(const void* base, uint32_t span, uint32_t at)
 {
-#pragma unroll
-    for (int k = 0; k < (MT * (MT + 1) / 2 + WAVES - 1) / WAVES; ++k) {
-        int idx = k * WAVES + wave, it = 0;
-        if (idx >= MT * (MT + 1) / 2) break;
-        while (idx > it) idx -= ++it;  // tile row idx <= it of tile column it
-        const int jt = idx;
-        v4f acc = zero4();
-#pragma unroll
-        for (int p = 0; p < KP; ++p)
-            acc = mfma32<OP>(lds_row<LY::PIECES>(lds + LY::K_AT, 16 * jt + ln.n, 4 * p + ln.q), lds_row<LY::PIECES>(lds + LY::Q_AT, 16 * it + ln.n, 4 * p + ln.q), acc);
-        const float gi = gl[16 * it + ln.n];
-        const v4f gj = *reinterpret_cast<const v4f*>(gl + 16 * jt + 4 * ln.q);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) acc[r] = jt < it || 4 * ln.q + r <= ln.n ? acc[r] * (scale * __expf(gi - gj[r])) : 0.f;
-        const v2u hi = pack4<OP>(acc), lo = pack4<OP>(minus16<OP>(acc, hi));
-        char* unit = lds + LY::P_AT + 2048 * (LY::units_before(it) + (jt >> 1)) + 16 * (16 * ln.q + ln.n) + 8 * (jt & 1);
-        *reinterpret_cast<v2u*>(unit) = hi;
-        *reinterpret_cast<v2u*>(unit + 1024) = lo;
-        if (jt == it && !(it & 1)) {  // the pair's other tile lies behind the diagonal
-            *reinterpret_cast<v2u*>(unit + 8) = v2u{0u, 0u};
-            *reinterpret_cast<v2u*>(unit + 1024 + 8) = v2u{0u, 0u};
-        }
-    }
+    return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, span, 0x00020000), at, 0, 0));
 }
+// g, exp(g_end - g), scale exp(g - base) of a step's tokens, its whole decay and that one's logarithm.  (Loads without a branch around them: what is not there,
+// or no g at all, lies outside a buffer of no bytes and reads as 0.  Behind a branch they made the wavefront wait for its stores.)
+template <int R> struct StepGates {
+    static constexpr int FLOATS = 3 * R + 4;
+    float g_row, g_end, g_base;
+    __device__ __forceinline__ void load(const float* g, const StepPos& at, int H, int h, int i)
+    {
+        const float* const first = g + at.row * H + h;
+        const uint32_t span = g && at.valid > 0 ? (uint32_t)(at.valid - 1) * H * 4u + 4u : 0u, end = (uint32_t)(at.valid > 0 ? at.valid - 1 : 0) * H * 4u;
+        g_row = buffer_float(first, span, i < at.valid ? (uint32_t)i * H * 4u : end);
+        g_end = buffer_float(first, span, end);
+        g_base = buffer_float(first - H, at.inner ? span : 0u, 0u);
+    }
+    __device__ __forceinline__ void store(float* gl, float scale, int i) const
+    {
+        if (i >= R) return;
+        gl[i] = g_row;
+        gl[R + i] = expf(g_end - g_row);
+        gl[2 * R + i] = scale * expf(g_row - g_base);
+        if (i == 0) gl[3 * R] = expf(g_end - g_base), gl[3 * R + 1] = g_end - g_base;
+    }
+};
 
+// MT tiles of 16 token rows a step, KP pairs of tiles of 16 channels; 64 columns, four wavefronts of 16.
 // ATTN_OUT: the outputs and the final state.  ATTN_SEGMENT: what a segment adds to a state (column groups of d_v) and, with W, what it does to
 // the one before it: the same recursion from the identity with U = 0 (column groups of d_k behind them).  ATTN_RECORD: the states before
-// the chunks and the chunks' values, for the gradient.
+// the steps and the values, for the gradient.
 enum : int { ATTN_OUT = 0, ATTN_SEGMENT = 1, ATTN_RECORD = 2 };
-template <int OP, int MT, int KP, int NT, int WAVES, bool DELTA, int MODE>
-__global__ __launch_bounds__(64 * WAVES) void k_chunk_attn(AttnArgs a)
-{
-    typedef AttnLayout<OP, MT, KP, NT, WAVES, DELTA> LY;
-    constexpr bool OUT = MODE == ATTN_OUT, SEGMENT = MODE == ATTN_SEGMENT;
-    constexpr int THREADS = 64 * WAVES, R = LY::R;
-    __shared__ __attribute__((aligned(16))) char lds[LY::BYTES];
-    float* const gl = reinterpret_cast<float*>(lds + LY::G_AT);  // g, exp(g_C - g), scale exp(g)
-    const Lane ln = lane_id();
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+constexpr int ATTN_COLS = 64;
+template <int OP, int MT, int KP, bool DELTA, int MODE> struct AttnLayout {
+    static constexpr bool OUT = MODE == ATTN_OUT;
+    static constexpr int R = 16 * MT, PIECES = 4 * KP, UPIECES = ATTN_COLS / 8;
+    static constexpr int ROWS = R * PIECES * 16, U_BYTES = R * UPIECES * 16;
+    static constexpr int K_AT = 0;  // twice: the second half of a step reads it while the next is brought
+    static constexpr int W_AT = 2 * ROWS, Q_AT = W_AT + (DELTA ? ROWS : 0), U_AT = Q_AT + (OUT ? ROWS : 0);
+    static constexpr int S_AT = U_AT + U_BYTES, S_WAVE = KP * 2048;  // two parts of S, a wavefront's columns one after the other
+    static constexpr int V_AT = S_AT + (OUT ? 4 * S_WAVE : 0), V_WAVE = MT * 1024;  // of V', twice
+    static constexpr int G_AT = V_AT + (OUT ? 8 * V_WAVE : 0), SHIFT_AT = G_AT + 2 * StepGates<R>::FLOATS * 4, BYTES = SHIFT_AT + 64;
+};
 
-    const unsigned groups_v = (a.d_v + LY::COLS - 1) / LY::COLS, groups = groups_v + (SEGMENT && DELTA ? (a.d_k + LY::COLS - 1) / LY::COLS : 0);
+template <int OP, int MT, int KP, bool DELTA, int MODE, bool TWO>
+__global__ __launch_bounds__(512) void k_chunk_attn(AttnArgs a)
+{
+    typedef AttnLayout<OP, MT, KP, DELTA, MODE> LY;
+    constexpr bool OUT = LY::OUT, SEGMENT = MODE == ATTN_SEGMENT;
+    constexpr int R = LY::R, FP = FULL_PARTS<OP>, PIECES = LY::PIECES;
+    __shared__ __attribute__((aligned(16))) char lds[LY::BYTES];
+    float* const gates = reinterpret_cast<float*>(lds + LY::G_AT);
+    int* const shifts = reinterpret_cast<int*>(lds + LY::SHIFT_AT);  // fp16: of the parts of S and V', by wavefront
+    const Lane ln = lane_id();
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane16 = 16 * (16 * ln.q + ln.n);
+
+    const unsigned groups_v = (a.d_v + ATTN_COLS - 1) / ATTN_COLS, groups = groups_v + (SEGMENT && DELTA ? (a.d_k + ATTN_COLS - 1) / ATTN_COLS : 0);
     const unsigned b = xcd_neighbours(blockIdx.x, gridDim.x);
     const unsigned cg = b % groups, hs = b / groups;
     const int seg = blockIdx.y;
     const int h = hs % a.H, s = hs / a.H;
     const bool trans = SEGMENT && cg >= groups_v;
     const int d_v = trans ? a.d_k : a.d_v;
-    const int wg_col = (trans ? cg - groups_v : cg) * LY::COLS, col0 = 16 * NT * wave;  // of the workgroup, of the wavefront in it
+    const int wg_col = (trans ? cg - groups_v : cg) * ATTN_COLS;
     const SeqPos sq = seq_pos(a.map, s);
     const int64_t n_chunk = (sq.len + a.C - 1) / a.C;
     int64_t c0, c1;
     segment_chunks(n_chunk, a.n_seg, seg, c0, c1);
-    const int hk = h / a.group, H_k = a.H / a.group;
+    const int tokens = a.C < R ? a.C : R, steps = a.C > R ? a.C / R : 1;  // of a step; of a chunk
+    const int64_t all = (sq.len + tokens - 1) / tokens, k0 = c0 * steps, k1 = c1 * steps < all ? c1 * steps : all;
 
-    v4f S[NT][2 * KP];
-    const float* from = !SEGMENT ? (seg == 0 ? a.state : a.seg_state + (int64_t)(seg - 1) * a.map.n_seq * a.H * a.d_k * a.d_v) : nullptr;
-    get_state<KP, NT>(from ? from + (int64_t)hs * a.d_k * a.d_v : nullptr, S, a.d_k, d_v, wg_col + col0, trans, ln);
-
-    RowLoader<LY::PIECES, R, THREADS> lq, lk, lw;
-    RowLoader<LY::UPIECES, R, THREADS> lu;
-    float g_row = 0.f, g_end = 0.f;
-    auto request = [&](int64_t c) {
-        const int64_t left = sq.len - c * a.C;
-        const int valid = left < a.C ? (int)left : a.C;
-        const int64_t row = sq.tok0 + c * a.C;
-        lk.load(a.K, (row * H_k + hk) * a.d_k, H_k * a.d_k, a.d_k, valid, tid);
-        if constexpr (DELTA) lw.load(a.W, (row * a.H + h) * a.d_k, a.H * a.d_k, a.d_k, valid, tid);
-        const int cols = a.d_v - wg_col;
-        lu.load(a.U, (row * a.H + h) * a.d_v + wg_col, a.H * a.d_v, cols < LY::COLS ? cols : LY::COLS, trans ? 0 : valid, tid);
-        if constexpr (OUT) lq.load(a.Q, (row * H_k + hk) * a.d_k, H_k * a.d_k, a.d_k, valid, tid);
-        if (a.g && tid < R) {
-            g_row = a.g[(row + (tid < valid ? tid : valid - 1)) * a.H + h];
-            g_end = a.g[(row + valid - 1) * a.H + h];
-        }
-    };
-    float total = 0.f;
-    if (c0 < c1) request(c0);
-    for (int64_t c = c0; c < c1; ++c) {
-        const int64_t left = sq.len - c * a.C;
-        const int valid = left < a.C ? (int)left : a.C;
-        lk.store(lds + LY::K_AT, tid);
-        if constexpr (OUT) lq.store(lds + LY::Q_AT, tid);
-        if constexpr (DELTA) lw.store(lds + LY::W_AT, tid);
-        lu.store(lds + LY::U_AT, tid);
-        if (tid < R) {
-            gl[tid] = g_row;
-            gl[R + tid] = expf(g_end - g_row);
-            gl[2 * R + tid] = a.scale * expf(g_row);
-        }
-        __syncthreads();
-        if (c + 1 < c1) request(c + 1);
-        if constexpr (OUT) chunk_scores<OP, MT, KP, WAVES, LY>(lds, gl, a.scale, wave, ln);
-
-        const float g_last = gl[R - 1], decay = expf(g_last);
-        total += g_last;
-        if constexpr (MODE == ATTN_RECORD) {
-            const int64_t id = (a.map.cu_chunks ? a.map.cu_chunks[s] : s * n_chunk) + c;
-            put_state<KP, NT>(a.rec_state + (id * a.H + h) * a.d_k * a.d_v, S, a.d_k, a.d_v, wg_col + col0, ln);
-        }
-        Parts<FULL_PARTS<OP>> sp[NT][KP];
+    if (wave < 4) {
+        // The recursion.
+        const int col0 = wg_col + 16 * wave;
+        const MinusOne<OP> minus(ln);
+        v4f S[2 * KP];
+        const float* from = !SEGMENT ? (seg == 0 ? a.state : a.seg_state + (int64_t)(seg - 1) * a.map.n_seq * a.H * a.d_k * a.d_v) : nullptr;
+        get_state<KP>(from ? from + (int64_t)hs * a.d_k * a.d_v : nullptr, S, a.d_k, d_v, col0, trans, ln);
+        Parts<FP> sp[KP];
         int s_shift = 0;
-        if constexpr (DELTA || OUT) s_shift = split_state<OP, KP, NT>(S, sp);
-        ChunkValues<OP, MT, KP, NT, DELTA> cv;
-        chunk_values<OP, MT, KP, NT, DELTA, LY>(cv, lds, sp, s_shift, col0, ln);
-        if constexpr (MODE == ATTN_RECORD && DELTA) {
+        const int64_t rec0 = MODE == ATTN_RECORD ? (a.map.cu_chunks ? a.map.cu_chunks[s] : s * n_chunk) * steps : 0;
+        // The parts of S: of the state before a chunk for W, two of them for Q in every step.
+        auto parts_of_state = [&](bool first) {
+            if (!OUT && !DELTA) return;
+            float up = 1.f;
+            int shift = 0;
+            if constexpr (OP == OP_F16) shift = f16_shift(wave_max(most_of(S))), up = pow2(shift);
+            v4f x[2 * KP];
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+            for (int i = 0; i < 2 * KP; ++i) x[i] = OP == OP_F16 ? times(S[i], up) : S[i];
+            Parts<DELTA ? FP : 2> t[KP];
+            split_pairs<OP, DELTA ? FP : 2, KP>(x, t, minus);
 #pragma unroll
-                for (int tb = 0; tb < MT; ++tb)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int i = 16 * tb + 4 * ln.q + r, col = wg_col + col0 + 16 * t + ln.n;
-                        if (i < valid && col < a.d_v) a.rec_value[((sq.tok0 + c * a.C + i) * a.H + h) * a.d_v + col] = cv.v[t][tb][r];
-                    }
-        }
-        chunk_state<OP, MT, KP, NT, DELTA, LY>(S, cv, lds, gl + R, decay, ln);
-        if constexpr (OUT) __syncthreads();  // the scores are in LDS
-        if constexpr (OUT) {
-            Parts<2> vp[NT][MT / 2];
-            const float up = OP == OP_F16 ? pow2(cv.shift) : 1.f, down = OP == OP_F16 ? pow2(-cv.shift) : 1.f;
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int tp = 0; tp < MT / 2; ++tp) {
-                    v4f x = cv.v[t][2 * tp], y = cv.v[t][2 * tp + 1];
-                    if constexpr (OP == OP_F16) {
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) x[r] *= up, y[r] *= up;
-                    }
-                    vp[t][tp] = split_pair<OP, 2>(x, y);
+            for (int p = 0; p < KP; ++p) {
+                if constexpr (OUT) {
+                    char* const to = lds + LY::S_AT + LY::S_WAVE * wave + 2048 * p + lane16;
+                    *reinterpret_cast<v4u*>(to) = t[p].u[0];
+                    *reinterpret_cast<v4u*>(to + 1024) = t[p].u[1];
                 }
-            const float across = OP == OP_F16 ? pow2(cv.shift - s_shift) : 1.f;
+                if constexpr (DELTA) {
+                    if (!TWO || first) sp[p] = t[p];
+                }
+            }
+            if (!TWO || first) s_shift = shift;
+            if (OUT && OP == OP_F16 && ln.q == 0 && ln.n == 0) shifts[wave] = shift;
+        };
+        parts_of_state(true);
+        __syncthreads();  // the first rows are in LDS
+        for (int64_t k = k0; k < k1; ++k) {
+            const float* const gl = gates + (k & 1) * StepGates<R>::FLOATS;
+            const char* const rows_k = lds + LY::K_AT + (k & 1) * LY::ROWS;
+            if constexpr (MODE == ATTN_RECORD) put_state<KP>(a.rec_state + ((rec0 + k) * a.H + h) * a.d_k * a.d_v, S, a.d_k, a.d_v, col0, ln);
+            v4f v[MT];
+            v2u u[MT];
+            const float down = OP == OP_F16 ? pow2(-s_shift) : 1.f;
 #pragma unroll
-            for (int it = 0; it < MT; ++it) {
-                v4f acc[NT];
+            for (int tb = 0; tb < MT; ++tb) v[tb] = zero4(), u[tb] = lds_turned<LY::UPIECES>(lds + LY::U_AT, 16 * tb + 4 * ln.q + (ln.n >> 2), 4 * wave + (ln.n & 3));
+            if constexpr (DELTA) {
+                v4u w[2][MT];
+                auto rows_of = [&](int p) {
 #pragma unroll
-                for (int t = 0; t < NT; ++t) acc[t] = zero4();
+                    for (int tb = 0; tb < MT; ++tb) w[p & 1][tb] = lds_row<PIECES>(lds + LY::W_AT, 16 * tb + ln.n, 4 * p + ln.q);
+                };
+                rows_of(0);
 #pragma unroll
                 for (int p = 0; p < KP; ++p) {
-                    const v4u q = lds_row<LY::PIECES>(lds + LY::Q_AT, 16 * it + ln.n, 4 * p + ln.q);
+                    if (p + 1 < KP) rows_of(p + 1);
+                    in_order();
 #pragma unroll
-                    for (int part = 1; part >= 0; --part)
+                    for (int part = FP - 1; part >= 0; --part)
 #pragma unroll
-                        for (int t = 0; t < NT; ++t) acc[t] = mfma32<OP>(sp[t][p].u[part], q, acc[t]);
+                        for (int tb = 0; tb < MT; ++tb) v[tb] = mfma32<OP>(w[p & 1][tb], sp[p].u[part], v[tb]);
                 }
-                const float gate = gl[2 * R + 16 * it + ln.n] * across;
+            }
+            __syncthreads();  // W, U, Q and the parts of S are in registers
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
+            for (int tb = 0; tb < MT; ++tb) {
+                const v4f x = unpack4<OP>(u[tb]);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[t][r] *= gate;
+                for (int r = 0; r < 4; ++r) v[tb][r] = DELTA ? x[r] - (OP == OP_F16 ? v[tb][r] * down : v[tb][r]) : x[r];
+            }
+            int v_shift = 0;
+            if constexpr (OP == OP_F16) v_shift = f16_shift(wave_max(most_of(v)));
+            const float up = OP == OP_F16 ? pow2(v_shift) : 1.f;
+            if constexpr (OUT) {
+                if (OP == OP_F16 && ln.q == 0 && ln.n == 0) shifts[4 + 4 * (k & 1) + wave] = v_shift;
+                v4f x[MT];
 #pragma unroll
-                for (int tp = 0; tp <= it / 2; ++tp) {
-                    const char* unit = lds + LY::P_AT + 2048 * (LY::units_before(it) + tp) + 16 * (16 * ln.q + ln.n);
-                    const v4u hi = *reinterpret_cast<const v4u*>(unit), lo = *reinterpret_cast<const v4u*>(unit + 1024);
+                for (int tb = 0; tb < MT; ++tb) x[tb] = OP == OP_F16 ? times(v[tb], up) : v[tb];
+                Parts<2> t[MT / 2];
+                split_pairs<OP, 2, MT / 2>(x, t, minus);
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) acc[t] = mfma32<OP>(vp[t][tp].u[0], lo, acc[t]);
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) acc[t] = mfma32<OP>(vp[t][tp].u[1], hi, acc[t]);
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) acc[t] = mfma32<OP>(vp[t][tp].u[0], hi, acc[t]);
+                for (int tp = 0; tp < MT / 2; ++tp) {
+                    char* to = lds + LY::V_AT + LY::V_WAVE * (4 * (k & 1) + wave) + 2048 * tp + lane16;
+                    *reinterpret_cast<v4u*>(to) = t[tp].u[0];
+                    *reinterpret_cast<v4u*>(to + 1024) = t[tp].u[1];
                 }
-                const int i = 16 * it + ln.n;
-                if (i < valid) {
-                    uint16_t* o = static_cast<uint16_t*>(a.O) + ((sq.tok0 + c * a.C + i) * a.H + h) * a.d_v + wg_col + col0 + 4 * ln.q;
+            }
+            if constexpr (MODE == ATTN_RECORD && DELTA) {
+                const StepPos at = step_pos<R>(sq, k, k1, a.C);
+                const uint32_t stride = 4u * a.H * a.d_v;
+                const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(a.rec_value + (at.row * a.H + h) * a.d_v, 0, (uint32_t)(at.valid - 1) * stride + 4u * a.d_v, 0x00020000);
+                uint32_t to = col0 + ln.n < a.d_v ? 4 * ln.q * stride + 4u * (col0 + ln.n) : 0x80000000u;
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        if constexpr (OP == OP_F16) {
+                for (int tb = 0; tb < MT; ++tb, to += 12 * stride)
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) acc[t][r] *= down;
-                        }
-                        if (wg_col + col0 + 16 * t + 4 * ln.q < a.d_v) *reinterpret_cast<v2u*>(o + 16 * t) = pack4<OP>(acc[t]);
-                    }
+                    for (int r = 0; r < 4; ++r, to += stride) __builtin_amdgcn_raw_buffer_store_b32(bits(v[tb][r]), rsrc, to, 0, 0);
+            }
+            Parts<FP> vp[MT / 2];
+#pragma unroll
+            for (int tb = 0; tb < MT; ++tb) {
+                const v4f e = *reinterpret_cast<const v4f*>(gl + R + 16 * tb + 4 * ln.q);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[tb][r] *= OP == OP_F16 ? e[r] * up : e[r];
+            }
+            split_pairs<OP, FP, MT / 2>(v, vp, minus);
+            const float decay = gl[3 * R];
+#pragma unroll
+            for (int i = 0; i < 2 * KP; ++i) S[i] = times(S[i], decay * up);
+            add_turned<OP, MT, KP>(S, rows_k, vp, ln);
+            if constexpr (OP == OP_F16) {
+#pragma unroll
+                for (int i = 0; i < 2 * KP; ++i) S[i] = times(S[i], pow2(-v_shift));
+            }
+            parts_of_state(((k + 1) & 1) == 0);
+            __syncthreads();  // the parts of S and the next rows are in LDS
+        }
+        if (!SEGMENT && seg != a.n_seg - 1) return;
+        float* to = !SEGMENT ? a.final_state : trans ? a.seg_trans : a.seg_state;
+        if (!to) return;
+        if (SEGMENT) to += (int64_t)seg * a.map.n_seq * a.H * a.d_k * d_v;
+        put_state<KP>(to + (int64_t)hs * a.d_k * d_v, S, a.d_k, d_v, col0, ln);
+        return;
+    }
+
+    // Rows, scores and outputs.
+    const int tid = threadIdx.x - 256;
+    const int hk = h / a.group, H_k = a.H / a.group;
+    RowLoader<PIECES, R, 256> lq, lk, lw;
+    RowLoader<LY::UPIECES, R, 256> lu;
+    StepGates<R> lg;
+    // addresses of the next step to be requested
+    const int cols = a.d_v - wg_col < ATTN_COLS ? a.d_v - wg_col : ATTN_COLS;
+    const uint32_t stride_k = 2u * H_k * a.d_k, stride_w = 2u * a.H * a.d_k, stride_u = 2u * a.H * a.d_v;
+    const int64_t row0 = sq.tok0 + k0 * tokens;
+    const char *at_k = static_cast<const char*>(a.K) + row0 * stride_k + 2 * hk * a.d_k, *at_q = static_cast<const char*>(a.Q) + row0 * stride_k + 2 * hk * a.d_k,
+               *at_w = static_cast<const char*>(a.W) + row0 * stride_w + 2 * h * a.d_k, *at_u = static_cast<const char*>(a.U) + row0 * stride_u + 2 * (h * a.d_v + (trans ? 0 : wg_col));
+    auto request = [&](int64_t k) {
+        const StepPos at = step_pos<R>(sq, k, k1, a.C);
+        lk.load(at_k, stride_k, a.d_k, at.valid, tid);
+        if constexpr (DELTA) lw.load(at_w, stride_w, a.d_k, at.valid, tid);
+        lu.load(at_u, stride_u, cols, trans ? 0 : at.valid, tid);
+        if constexpr (OUT) lq.load(at_q, stride_k, a.d_k, at.valid, tid);
+        lg.load(a.g, at, a.H, h, tid);
+        at_k += (int64_t)tokens * stride_k, at_q += (int64_t)tokens * stride_k, at_w += (int64_t)tokens * stride_w, at_u += (int64_t)tokens * stride_u;
+    };
+    auto bring = [&](int64_t k) {
+        lk.store(lds + LY::K_AT + (k & 1) * LY::ROWS, tid);
+        if constexpr (DELTA) lw.store(lds + LY::W_AT, tid);
+        if constexpr (OUT) lq.store(lds + LY::Q_AT, tid);
+        lu.store(lds + LY::U_AT, tid);
+        lg.store(gates + (k & 1) * StepGates<R>::FLOATS, a.scale, tid);
+    };
+    float total = 0.f;
+    request(k0);
+    bring(k0);
+    request(k0 + 1);
+    __syncthreads();
+    const MinusOne<OP> minus(ln);
+    // This wavefront's outputs: two column tiles, and of MT = 4 token tiles the outer or the inner two (so that all have six pairs' worth of scores).
+    constexpr int NI = MT / 2;
+    const int ct = 2 * (wave & 1), half = (wave >> 1) & 1;
+    // What is added to the exponents of its score tiles 2 tp and 2 tp + 1 next to the diagonal: nothing, or minus infinity behind it.
+    v4f edge[NI][2];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const float none = -__builtin_inff(), on = 4 * ln.q + r <= ln.n ? 0.f : none;
+        edge[0][0][r] = half == 0 ? on : 0.f, edge[0][1][r] = half == 0 ? none : on;
+        if constexpr (NI == 2) edge[1][0][r] = half == 1 ? on : 0.f, edge[1][1][r] = half == 1 ? none : on;
+    }
+    v4f acc[NI][2];
+    Parts<2> pp[NI][NI];  // scores: pairs of tiles, two parts
+    // The outputs of step k, whose Q S and scores are there: the scores' product with V', and the store.
+    auto finish = [&](int64_t k) {
+        const StepPos at = step_pos<R>(sq, k, k1, a.C);
+        if constexpr (OP == OP_F16) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int ii = 0; ii < NI; ++ii) acc[ii][t] = times(acc[ii][t], pow2(shifts[4 + 4 * (k & 1) + ct + t]));
+        }
+        v4u vs[NI][2][2];
+#pragma unroll
+        for (int tp = 0; tp < NI; ++tp)
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int part = 0; part < 2; ++part)
+                    vs[tp][t][part] = *reinterpret_cast<const v4u*>(lds + LY::V_AT + LY::V_WAVE * (4 * (k & 1) + ct + t) + 2048 * tp + 1024 * part + lane16);
+        in_order();
+#pragma unroll
+        for (int tp = 0; tp < NI; ++tp)
+#pragma unroll
+            for (int order = 0; order < 3; ++order)
+#pragma unroll
+                for (int ii = tp; ii < NI; ++ii)
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) acc[ii][t] = mfma32<OP>(vs[tp][t][order == 1], pp[ii][tp].u[order == 0], acc[ii][t]);
+        const int left = a.d_v - wg_col;
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(static_cast<char*>(a.O) + at.row * stride_u + 2 * ((int64_t)h * a.d_v + wg_col), 0,
+                                                            at.valid > 0 ? (uint32_t)(at.valid - 1) * stride_u + 2u * left : 0u, 0x00020000);
+#pragma unroll
+        for (int ii = 0; ii < NI; ++ii)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int i = 16 * (ii == 0 ? half : 3 - half) + ln.n, col = 16 * (ct + t) + 4 * ln.q;
+                const v4f x = OP == OP_F16 ? times(acc[ii][t], pow2(-shifts[4 + 4 * (k & 1) + ct + t])) : acc[ii][t];
+                __builtin_amdgcn_raw_buffer_store_b64(pack4<OP>(x), rsrc, col < left ? (uint32_t)i * stride_u + 2u * col : 0x80000000u, 0, 0);
+            }
+    };
+    for (int64_t k = k0; k < k1; ++k) {
+        const float* const gl = gates + (k & 1) * StepGates<R>::FLOATS;
+        const char* const rows_k = lds + LY::K_AT + (k & 1) * LY::ROWS;
+        v4u q[NI][KP];
+        if constexpr (OUT) {
+            if (k > k0) finish(k - 1);
+            v4u sf[2][2][2];
+            auto parts_of = [&](int p) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int part = 0; part < 2; ++part) sf[p & 1][t][part] = *reinterpret_cast<const v4u*>(lds + LY::S_AT + LY::S_WAVE * (ct + t) + 2048 * p + 1024 * part + lane16);
+            };
+#pragma unroll
+            for (int p = 0; p < KP; ++p)
+#pragma unroll
+                for (int ii = 0; ii < NI; ++ii) q[ii][p] = lds_row<PIECES>(lds + LY::Q_AT, 16 * (ii == 0 ? half : 3 - half) + ln.n, 4 * p + ln.q);
+            parts_of(0);
+#pragma unroll
+            for (int ii = 0; ii < NI; ++ii) acc[ii][0] = acc[ii][1] = zero4();
+#pragma unroll
+            for (int p = 0; p < KP; ++p) {
+                if (p + 1 < KP) parts_of(p + 1);
+                in_order();
+#pragma unroll
+                for (int part = 1; part >= 0; --part)
+#pragma unroll
+                    for (int ii = 0; ii < NI; ++ii)
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) acc[ii][t] = mfma32<OP>(sf[p & 1][t][part], q[ii][p], acc[ii][t]);
+            }
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const float down = OP == OP_F16 ? pow2(-shifts[ct + t]) : 1.f;  // (fp16: Q S is of S 2^shift)
+#pragma unroll
+                for (int ii = 0; ii < NI; ++ii) acc[ii][t] = times(acc[ii][t], gl[2 * R + 16 * (ii == 0 ? half : 3 - half) + ln.n] * down);
+            }
+        }
+        if (SEGMENT && !DELTA && cg == 0 && tid == 0) total += gl[3 * R + 1];
+        __syncthreads();  // W, U, Q and the parts of S are in registers
+        bring(k + 1);
+        request(k + 2);
+        in_order();
+        if constexpr (OUT) {
+            v4u kf[2][2 * NI];
+            v4f x[NI][2 * NI];  // scores, turned: x[ii][jt], jt <= 2 ii + 1
+            auto keys_of = [&](int p) {
+#pragma unroll
+                for (int jt = 0; jt < 2 * NI; ++jt) kf[p & 1][jt] = lds_row<PIECES>(rows_k, 16 * jt + ln.n, 4 * p + ln.q);
+            };
+            keys_of(0);
+#pragma unroll
+            for (int ii = 0; ii < NI; ++ii)
+#pragma unroll
+                for (int jt = 0; jt < 2 * NI; ++jt) x[ii][jt] = zero4();
+#pragma unroll
+            for (int p = 0; p < KP; ++p) {
+                if (p + 1 < KP) keys_of(p + 1);
+                in_order();
+#pragma unroll
+                for (int ii = 0; ii < NI; ++ii)
+#pragma unroll
+                    for (int jt = 0; jt < 2 * ii + 2; ++jt) x[ii][jt] = mfma32<OP>(kf[p & 1][jt], q[ii][p], x[ii][jt]);
+            }
+            v4f gj[2 * NI];
+#pragma unroll
+            for (int jt = 0; jt < 2 * NI; ++jt) gj[jt] = *reinterpret_cast<const v4f*>(gl + 16 * jt + 4 * ln.q);
+#pragma unroll
+            for (int ii = 0; ii < NI; ++ii) {
+                const float gi = gl[16 * (ii == 0 ? half : 3 - half) + ln.n];
+#pragma unroll
+                for (int jt = 0; jt < 2 * ii + 2; ++jt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[ii][jt][r] *= a.scale * __expf(jt >= 2 * ii ? gi - gj[jt][r] + edge[ii][jt & 1][r] : gi - gj[jt][r]);
+#pragma unroll
+                for (int tp = 0; tp <= ii; ++tp) {
+                    v4f two[2] = {x[ii][2 * tp], x[ii][2 * tp + 1]};
+                    Parts<2> one[1];
+                    split_pairs<OP, 2, 1>(two, one, minus);
+                    pp[ii][tp] = one[0];
                 }
             }
         }
-        __syncthreads();  // the rows are not needed any more
+        __syncthreads();
     }
-
-    if (!SEGMENT && seg != a.n_seg - 1) return;
-    float* to = !SEGMENT ? a.final_state : trans ? a.seg_trans : a.seg_state;
-    if (!to) return;
-    if (SEGMENT) to += (int64_t)seg * a.map.n_seq * a.H * a.d_k * d_v;
-    put_state<KP, NT>(to + (int64_t)hs * a.d_k * d_v, S, a.d_k, d_v, wg_col + col0, ln);
+    if constexpr (OUT) {
+        if (k0 < k1) finish(k1 - 1);
+    }
     if (SEGMENT && !DELTA && cg == 0 && tid == 0) a.seg_decay[(int64_t)seg * a.map.n_seq * a.H + hs] = expf(total);
 }
 
-// States before the segments, in place of what the segments add: S <- M_seg S + L_seg from the sequence's initial state.  M and S as
-// three bf16 parts each, the six products that matter.
-template <int KP, int WAVES, bool DELTA> __global__ __launch_bounds__(64 * WAVES) void k_attn_join(AttnArgs a)
+// States before the segments, in place of what the segments add: S <- M S + L from the sequence's initial state, segment by segment.  M and S as three
+// bf16 parts each, the six products that matter.  A workgroup takes 16 columns, a wavefront KP / 2 tiles of their rows; the parts of S go round
+// through LDS.
+template <int KP> __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a)
 {
-    constexpr int COLS = 16 * WAVES;
+    constexpr int TI = KP / 2;
+    __shared__ __attribute__((aligned(16))) char lds[2][KP * 3 * 1024];
     const Lane ln = lane_id();
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const unsigned groups = (a.d_v + COLS - 1) / COLS, cg = blockIdx.x % groups, hs = blockIdx.x / groups;
-    const int col = cg * COLS + 16 * wave + ln.n;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane16 = 16 * (16 * ln.q + ln.n);
+    const unsigned groups = (a.d_v + 15) / 16, hs = blockIdx.x / groups;
+    const int col = 16 * (blockIdx.x % groups) + ln.n;
     const int64_t heads = (int64_t)a.map.n_seq * a.H;
     const bool mine = col < a.d_v;
-    v4f S[2 * KP];
+    v4f S[TI];
+    auto at = [&](int t, int r) { return state_channel(TI * wave + t, 4 * ln.q + r); };
 #pragma unroll
-    for (int i = 0; i < 2 * KP; ++i)
+    for (int t = 0; t < TI; ++t)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int ch = state_channel(i, 4 * ln.q + r);
-            S[i][r] = a.state && mine && ch < a.d_k ? a.state[((int64_t)hs * a.d_k + ch) * a.d_v + col] : 0.f;
-        }
+        for (int r = 0; r < 4; ++r) S[t][r] = a.state && mine && at(t, r) < a.d_k ? a.state[((int64_t)hs * a.d_k + at(t, r)) * a.d_v + col] : 0.f;
     for (int seg = 0; seg + 1 < a.n_seg; ++seg) {
         float* const L = a.seg_state + (seg * heads + hs) * a.d_k * a.d_v;
-        v4f next[2 * KP];
+        const float* const M = a.seg_trans + (seg * heads + hs) * a.d_k * a.d_k;
+        v4f m[TI][KP][2], next[TI];
 #pragma unroll
-        for (int i = 0; i < 2 * KP; ++i)
+        for (int t = 0; t < TI; ++t) {
+            const int row = state_channel(TI * wave + t, ln.n);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int ch = state_channel(i, 4 * ln.q + r);
-                next[i][r] = mine && ch < a.d_k ? L[(int64_t)ch * a.d_v + col] : 0.f;
+            for (int p = 0; p < KP; ++p) {
+                const bool there = row < a.d_k && 32 * p < a.d_k;
+                const float* x = M + (int64_t)row * a.d_k + 32 * p + 8 * ln.q;
+                m[t][p][0] = there ? *reinterpret_cast<const v4f*>(x) : zero4();
+                m[t][p][1] = there ? *reinterpret_cast<const v4f*>(x + 4) : zero4();
             }
-        if constexpr (DELTA) {
-            const float* const M = a.seg_trans + (seg * heads + hs) * a.d_k * a.d_k;
-            Parts<3> sp[KP];
 #pragma unroll
-            for (int p = 0; p < KP; ++p) sp[p] = split_pair<OP_BF16, 3>(S[2 * p], S[2 * p + 1]);
-#pragma unroll
-            for (int i = 0; i < 2 * KP; ++i) {
-                const int ch = state_channel(i, ln.n);
-#pragma unroll
-                for (int p = 0; p < KP; ++p) {
-                    v4f x = zero4(), y = zero4();
-                    if (ch < a.d_k && 32 * p < a.d_k) {
-                        const float* m = M + (int64_t)ch * a.d_k + 32 * p + 8 * ln.q;
-                        x = *reinterpret_cast<const v4f*>(m), y = *reinterpret_cast<const v4f*>(m + 4);
-                    }
-                    const Parts<3> mp = split_pair<OP_BF16, 3>(x, y);
-                    next[i] = mfma32<OP_BF16>(mp.u[2], sp[p].u[0], next[i]);
-                    next[i] = mfma32<OP_BF16>(mp.u[0], sp[p].u[2], next[i]);
-                    next[i] = mfma32<OP_BF16>(mp.u[1], sp[p].u[1], next[i]);
-                    next[i] = mfma32<OP_BF16>(mp.u[1], sp[p].u[0], next[i]);
-                    next[i] = mfma32<OP_BF16>(mp.u[0], sp[p].u[1], next[i]);
-                    next[i] = mfma32<OP_BF16>(mp.u[0], sp[p].u[0], next[i]);
-                }
-            }
-        } else {
-            const float decay = a.seg_decay[seg * heads + hs];
-#pragma unroll
-            for (int i = 0; i < 2 * KP; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) next[i][r] += decay * S[i][r];
+            for (int r = 0; r < 4; ++r) next[t][r] = mine && at(t, r) < a.d_k ? L[(int64_t)at(t, r) * a.d_v + col] : 0.f;
         }
+        // this wavefront's parts of S: half a pair of tiles (KP = 2), or a whole one
+        char* const buf = lds[seg & 1];
 #pragma unroll
-        for (int i = 0; i < 2 * KP; ++i) {
-            S[i] = next[i];
+        for (int t = 0; t < TI; ++t) {
+            const int i = TI * wave + t;
+            v4f x = S[t];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int ch = state_channel(i, 4 * ln.q + r);
-                if (mine && ch < a.d_k) L[(int64_t)ch * a.d_v + col] = S[i][r];
+            for (int part = 0; part < 3; ++part) {
+                const v2u u = pack4<OP_BF16>(x);
+                *reinterpret_cast<v2u*>(buf + ((i >> 1) * 3 + part) * 1024 + lane16 + 8 * (i & 1)) = u;
+                x = minus16<OP_BF16>(x, u);
             }
         }
+        __syncthreads();
+#pragma unroll
+        for (int p = 0; p < KP; ++p) {
+            v4u sp[3];
+#pragma unroll
+            for (int part = 0; part < 3; ++part) sp[part] = *reinterpret_cast<const v4u*>(buf + (p * 3 + part) * 1024 + lane16);
+#pragma unroll
+            for (int t = 0; t < TI; ++t) {
+                const Parts<3> mp = split_pair<OP_BF16, 3>(m[t][p][0], m[t][p][1]);
+                next[t] = mfma32<OP_BF16>(mp.u[2], sp[0], next[t]);
+                next[t] = mfma32<OP_BF16>(mp.u[0], sp[2], next[t]);
+                next[t] = mfma32<OP_BF16>(mp.u[1], sp[1], next[t]);
+                next[t] = mfma32<OP_BF16>(mp.u[1], sp[0], next[t]);
+                next[t] = mfma32<OP_BF16>(mp.u[0], sp[1], next[t]);
+                next[t] = mfma32<OP_BF16>(mp.u[0], sp[0], next[t]);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < TI; ++t) {
+            S[t] = next[t];
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (mine && at(t, r) < a.d_k) L[(int64_t)at(t, r) * a.d_v + col] = S[t][r];
+        }
+    }
+}
+
+// The same without W, where a segment multiplies a state by one number: an element of the state a thread.
+static __global__ __launch_bounds__(256) void k_attn_join_plain(AttnArgs a)
+{
+    const int64_t heads = (int64_t)a.map.n_seq * a.H, size = (int64_t)a.d_k * a.d_v, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= heads * size) return;
+    const int64_t hs = i / size;
+    float S = a.state ? a.state[i] : 0.f;
+    for (int seg = 0; seg + 1 < a.n_seg; ++seg) {
+        float* const L = a.seg_state + seg * heads * size + i;
+        S = a.seg_decay[seg * heads + hs] * S + *L;
+        *L = S;
     }
 }
 

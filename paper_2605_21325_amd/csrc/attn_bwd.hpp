@@ -6,8 +6,9 @@
 //     M   = scale (dO V'^T) . D
 //     dQ  = scale diag(G) dO S^T + M K,   dK = diag(e) V' dS'^T + M^T Q
 //     dg_i = <q_i, dQ_i> - <k_i, dK_i>,   and at the chunk's last token + <S', dS'>,  S' = G_C S + K^T diag(e) V' the state after it.
-// Three kernels: the states and values again, chunk after chunk (k_chunk_attn, ATTN_RECORD); dS, last chunk first, with dU (k_attn_bwd_state);
-// everything else, all chunks at once (k_attn_bwd_chunk).  The first two are the walk of the forward pass, bound by the chain from chunk
+// In steps as there: inside a chunk of two, S and dS are those at the step's ends, W and dW go with the state before the chunk.
+// Three kernels: the states and values again, step after step (k_chunk_attn, ATTN_RECORD); dS, last step first, with dU (k_attn_bwd_state);
+// everything else, all steps at once (k_attn_bwd_chunk).  The first two are the walk of the forward pass, bound by the chain from chunk
 // to chunk; the states between them go through memory in fp32.  dg is the difference of large sums, so what enters it (dO S^T, V' dS'^T, M) is
 // formed from all 24 bits (fp16: 22) of its fp32 operands; what only ends in 16 bits (dW) from 16 of them.
 #pragma once
@@ -20,17 +21,15 @@ struct AttnBwdArgs {
     const float *g, *dstate;
     void *dQ, *dK, *dU, *dW;
     float *dg, *dstate0;
-    const float *rec_state, *rec_value;  // states before the chunks, values (rec_value null: U)
-    float* rec_dstate;                   // gradients at the states after the chunks
+    const float *rec_state, *rec_value;  // states before the steps, values (with W)
+    float* rec_dstate;                   // gradients at the states after the steps
     SeqMap map;
-    int64_t n_chunk;
     int H, group, d_k, d_v, C;
     float scale;
 };
 
-template <int OP, int MT, int KP, int NT, int WAVES, bool DELTA> struct BwdStateLayout {
-    static constexpr int R = 16 * MT, PIECES = 4 * KP, COLS = 16 * NT * WAVES, UPIECES = COLS / 8;
-    static constexpr int ROWS_BYTES = R * PIECES * 16, O_BYTES = R * UPIECES * 16;
+template <int OP, int MT, int KP, bool DELTA> struct BwdStateLayout {
+    static constexpr int R = 16 * MT, PIECES = 4 * KP, UPIECES = ATTN_COLS / 8, ROWS = R * PIECES * 16;
     // Pairs of tiles of P (two tile rows, one tile column jt), tile columns one after the other.
     static constexpr int units_before(int jt)
     {
@@ -38,9 +37,10 @@ template <int OP, int MT, int KP, int NT, int WAVES, bool DELTA> struct BwdState
         for (int j = 0; j < jt; ++j) n += MT / 2 - j / 2;
         return n;
     }
-    static constexpr int UNIT = 1024 * FULL_PARTS<OP>, P_BYTES = units_before(MT) * UNIT;
-    static constexpr int PW_BYTES = DELTA && ROWS_BYTES > P_BYTES ? ROWS_BYTES : P_BYTES;  // W takes P's place when that is used up
-    static constexpr int K_AT = 0, Q_AT = ROWS_BYTES, O_AT = 2 * ROWS_BYTES, P_AT = O_AT + O_BYTES, G_AT = P_AT + PW_BYTES, BYTES = G_AT + 3 * R * 4;
+    static constexpr int UNIT = 1024 * FULL_PARTS<OP>;
+    static constexpr int K_AT = 0, W_AT = 2 * ROWS, Q_AT = W_AT + (DELTA ? ROWS : 0), O_AT = Q_AT + ROWS, P_AT = O_AT + R * UPIECES * 16;
+    static constexpr int X_AT = P_AT + units_before(MT) * UNIT, X_WAVE = 2 * KP * 1024, Y_AT = X_AT + 4 * X_WAVE, Y_WAVE = MT * 1024;  // fp32 tiles, a wavefront's columns
+    static constexpr int G_AT = Y_AT + 4 * Y_WAVE, BYTES = G_AT + 2 * StepGates<R>::FLOATS * 4;
 };
 
 template <class LY> __device__ __forceinline__ int unit_at(int jt)  // units_before at run time
@@ -50,286 +50,300 @@ template <class LY> __device__ __forceinline__ int unit_at(int jt)  // units_bef
     return n;
 }
 
-template <int OP> __device__ __forceinline__ v4f unpack4(v2u raw)
+// dS from the last step to the first, a workgroup per head and 64 columns as in the forward pass.  Four wavefronts carry the recursion (K dS', W^T dV'); four others
+// are a step ahead with what does not depend on it: P, P^T dO and scale Q^T diag(G) dO, which go through LDS in fp32.
+//     first part     K dS', dV'                                 rows of the step before to LDS | its P
+//     second part    dU, W^T dV', the new dS and its parts      P^T dO and Q^T dO of the step before
+template <int OP, int MT, int KP, bool DELTA, bool TWO>
+__global__ __launch_bounds__(512) void k_attn_bwd_state(AttnBwdArgs a)
 {
-    v4f u;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const uint16_t x = (uint16_t)(raw[r >> 1] >> (16 * (r & 1)));
-        u[r] = OP == OP_F16 ? f16_to_f32(x) : bf16_to_f32(x);
-    }
-    return u;
-}
-
-// acc + X^T V (channels x columns): rows of X read turned, vp the parts of V.
-template <int OP, int MT, int KP, int NT, class LY>
-__device__ __forceinline__ void add_turned(v4f (&S)[NT][2 * KP], const char* rows, const Parts<FULL_PARTS<OP>> (&vp)[NT], int tp, Lane ln)
-{
-#pragma unroll
-    for (int i = 0; i < 2 * KP; ++i) {
-        const int col4 = 8 * (i >> 1) + 2 * (ln.n & 3) + (i & 1), row = 32 * tp + 4 * ln.q + (ln.n >> 2);
-        const v2u k0 = lds_turned<LY::PIECES>(rows, row, col4), k1 = lds_turned<LY::PIECES>(rows, row + 16, col4);
-        const v4u k = {k0[0], k0[1], k1[0], k1[1]};
-#pragma unroll
-        for (int part = FULL_PARTS<OP> - 1; part >= 0; --part)
-#pragma unroll
-            for (int t = 0; t < NT; ++t) S[t][i] = mfma32<OP>(k, vp[t].u[part], S[t][i]);
-    }
-}
-
-// dS from the last chunk to the first, a workgroup per head and column group as in the forward pass.
-template <int OP, int MT, int KP, int NT, int WAVES, bool DELTA>
-__global__ __launch_bounds__(64 * WAVES) void k_attn_bwd_state(AttnBwdArgs a)
-{
-    typedef BwdStateLayout<OP, MT, KP, NT, WAVES, DELTA> LY;
-    constexpr int THREADS = 64 * WAVES, R = LY::R, TILES = MT * (MT + 1) / 2;
+    typedef BwdStateLayout<OP, MT, KP, DELTA> LY;
+    constexpr int R = LY::R, FP = FULL_PARTS<OP>, PIECES = LY::PIECES, TILES = MT * (MT + 1) / 2;
     __shared__ __attribute__((aligned(16))) char lds[LY::BYTES];
-    float* const gl = reinterpret_cast<float*>(lds + LY::G_AT);  // g, exp(g_C - g), scale exp(g)
+    float* const gates = reinterpret_cast<float*>(lds + LY::G_AT);
     const Lane ln = lane_id();
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const unsigned groups = (a.d_v + LY::COLS - 1) / LY::COLS;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane16 = 16 * (16 * ln.q + ln.n);
+    const unsigned groups = (a.d_v + ATTN_COLS - 1) / ATTN_COLS;
     const unsigned b = xcd_neighbours(blockIdx.x, gridDim.x);
     const unsigned cg = b % groups, hs = b / groups;
-    const int h = hs % a.H, s = hs / a.H;
-    const int wg_col = cg * LY::COLS, col0 = 16 * NT * wave;
+    const int h = hs % a.H, s = hs / a.H, wg_col = cg * ATTN_COLS;
     const SeqPos sq = seq_pos(a.map, s);
-    const int64_t n_chunk = (sq.len + a.C - 1) / a.C, first_id = a.map.cu_chunks ? a.map.cu_chunks[s] : s * n_chunk;
-    const int hk = h / a.group, H_k = a.H / a.group;
+    const int64_t n_chunk = (sq.len + a.C - 1) / a.C;
+    const int tokens = a.C < R ? a.C : R, steps = a.C > R ? a.C / R : 1;
+    const int64_t k1 = (sq.len + tokens - 1) / tokens;
+    const uint32_t stride_u = 2u * a.H * a.d_v;
+    const MinusOne<OP> minus(ln);
 
-    v4f S[NT][2 * KP];
-    get_state<KP, NT>(a.dstate ? a.dstate + (int64_t)hs * a.d_k * a.d_v : nullptr, S, a.d_k, a.d_v, wg_col + col0, false, ln);
+    if (wave < 4) {
+        const int col0 = wg_col + 16 * wave;
+        const int64_t rec0 = (a.map.cu_chunks ? a.map.cu_chunks[s] : s * n_chunk) * steps;
+        v4f S[2 * KP], E[TWO ? 2 * KP : 1];  // dS; what the chunk's values pass on to the state before it
+        get_state<KP>(a.dstate ? a.dstate + (int64_t)hs * a.d_k * a.d_v : nullptr, S, a.d_k, a.d_v, col0, false, ln);
+        if constexpr (TWO) {
+#pragma unroll
+            for (int i = 0; i < 2 * KP; ++i) E[i] = zero4();
+        }
+        Parts<FP> sp[KP];
+        int s_shift = 0;
+        auto parts_of_state = [&]() {
+            if constexpr (OP == OP_F16) s_shift = f16_shift(wave_max(most_of(S)));
+            v4f x[2 * KP];
+#pragma unroll
+            for (int i = 0; i < 2 * KP; ++i) x[i] = OP == OP_F16 ? times(S[i], pow2(s_shift)) : S[i];
+            split_pairs<OP, FP, KP>(x, sp, minus);
+        };
+        parts_of_state();
+        __syncthreads();
+        __syncthreads();
+        __syncthreads();  // the last step's rows, P^T dO and Q^T dO are in LDS
+        for (int64_t k = k1 - 1; k >= 0; --k) {
+            const float* const gl = gates + (k & 1) * StepGates<R>::FLOATS;
+            const char* const rows_k = lds + LY::K_AT + (k & 1) * LY::ROWS;
+            put_state<KP>(a.rec_dstate + ((rec0 + k) * a.H + h) * a.d_k * a.d_v, S, a.d_k, a.d_v, col0, ln);
+            v4f dv[MT];
+#pragma unroll
+            for (int tb = 0; tb < MT; ++tb) dv[tb] = zero4();
+            {
+                v4u w[2][MT];
+                auto rows_of = [&](int p) {
+#pragma unroll
+                    for (int tb = 0; tb < MT; ++tb) w[p & 1][tb] = lds_row<PIECES>(rows_k, 16 * tb + ln.n, 4 * p + ln.q);
+                };
+                rows_of(0);
+#pragma unroll
+                for (int p = 0; p < KP; ++p) {
+                    if (p + 1 < KP) rows_of(p + 1);
+                    in_order();
+#pragma unroll
+                    for (int part = FP - 1; part >= 0; --part)
+#pragma unroll
+                        for (int tb = 0; tb < MT; ++tb) dv[tb] = mfma32<OP>(w[p & 1][tb], sp[p].u[part], dv[tb]);
+                    if (p == 0) __syncthreads();  // the others' rows are in LDS
+                }
+            }
+            const float s_down = OP == OP_F16 ? pow2(-s_shift) : 1.f, decay = gl[3 * R];
+#pragma unroll
+            for (int tb = 0; tb < MT; ++tb) {
+                const v4f e = *reinterpret_cast<const v4f*>(gl + R + 16 * tb + 4 * ln.q), y = *reinterpret_cast<const v4f*>(lds + LY::Y_AT + LY::Y_WAVE * wave + 1024 * tb + lane16);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) dv[tb][r] = dv[tb][r] * (OP == OP_F16 ? e[r] * s_down : e[r]) + y[r];
+            }
+#pragma unroll
+            for (int i = 0; i < 2 * KP; ++i) {
+                const v4f x = *reinterpret_cast<const v4f*>(lds + LY::X_AT + LY::X_WAVE * wave + 1024 * i + lane16);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) S[i][r] = decay * S[i][r] + x[r];
+            }
+            __syncthreads();  // P^T dO and Q^T dO of this step are used up, W is in LDS
+            {
+                const StepPos at = step_pos<R>(sq, k, k1, a.C);
+                const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(static_cast<char*>(a.dU) + at.row * stride_u + 2 * ((int64_t)h * a.d_v), 0,
+                                                                    (uint32_t)(at.valid - 1) * stride_u + 2u * a.d_v, 0x00020000);
+                uint32_t to = col0 + ln.n < a.d_v ? 4 * ln.q * stride_u + 2u * (col0 + ln.n) : 0x80000000u;
+#pragma unroll
+                for (int tb = 0; tb < MT; ++tb, to += 12 * stride_u) {
+                    const v2u x = pack4<OP>(dv[tb]);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r, to += stride_u) __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(x[r >> 1] >> (16 * (r & 1))), rsrc, to, 0, 0);
+                }
+            }
+            if constexpr (DELTA) {
+                int shift = 0;
+                if constexpr (OP == OP_F16) shift = f16_shift(wave_max(most_of(dv)));
+                const float up = OP == OP_F16 ? -pow2(shift) : -1.f;
+#pragma unroll
+                for (int tb = 0; tb < MT; ++tb) dv[tb] = times(dv[tb], up);
+                Parts<FP> vp[MT / 2];
+                split_pairs<OP, FP, MT / 2>(dv, vp, minus);
+                if constexpr (TWO) {  // dS takes it at the chunk's first step
+#pragma unroll
+                    for (int i = 0; i < 2 * KP; ++i) E[i] = OP == OP_F16 ? times(E[i], pow2(shift)) : E[i];
+                    add_turned<OP, MT, KP>(E, lds + LY::W_AT, vp, ln);
+#pragma unroll
+                    for (int i = 0; i < 2 * KP; ++i) {
+                        if constexpr (OP == OP_F16) E[i] = times(E[i], pow2(-shift));
+                        if ((k & 1) == 0) {
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) S[i][r] += E[i][r];
+                            E[i] = zero4();
+                        }
+                    }
+                } else {
+                    if constexpr (OP == OP_F16) {
+#pragma unroll
+                        for (int i = 0; i < 2 * KP; ++i) S[i] = times(S[i], pow2(shift));
+                    }
+                    add_turned<OP, MT, KP>(S, lds + LY::W_AT, vp, ln);
+                    if constexpr (OP == OP_F16) {
+#pragma unroll
+                        for (int i = 0; i < 2 * KP; ++i) S[i] = times(S[i], pow2(-shift));
+                    }
+                }
+            }
+            parts_of_state();
+            __syncthreads();  // the next step's P^T dO and Q^T dO are in LDS
+        }
+        if (a.dstate0) put_state<KP>(a.dstate0 + (int64_t)hs * a.d_k * a.d_v, S, a.d_k, a.d_v, col0, ln);
+        return;
+    }
 
-    RowLoader<LY::PIECES, R, THREADS> lq, lk, lw;
-    RowLoader<LY::UPIECES, R, THREADS> lo;
-    float g_row = 0.f, g_end = 0.f;
-    auto request = [&](int64_t c) {
-        const int64_t left = sq.len - c * a.C;
-        const int valid = left < a.C ? (int)left : a.C;
-        const int64_t row = sq.tok0 + c * a.C;
-        lk.load(a.K, (row * H_k + hk) * a.d_k, H_k * a.d_k, a.d_k, valid, tid);
-        lq.load(a.Q, (row * H_k + hk) * a.d_k, H_k * a.d_k, a.d_k, valid, tid);
-        const int cols = a.d_v - wg_col;
-        lo.load(a.dO, (row * a.H + h) * a.d_v + wg_col, a.H * a.d_v, cols < LY::COLS ? cols : LY::COLS, valid, tid);
-        if constexpr (DELTA) lw.load(a.W, (row * a.H + h) * a.d_k, a.H * a.d_k, a.d_k, valid, tid);
-        if (a.g && tid < R) {
-            g_row = a.g[(row + (tid < valid ? tid : valid - 1)) * a.H + h];
-            g_end = a.g[(row + valid - 1) * a.H + h];
+    // A step ahead: what does not depend on dS.
+    const int tid = threadIdx.x - 256, w4 = wave - 4, hk = h / a.group, H_k = a.H / a.group, cols = a.d_v - wg_col < ATTN_COLS ? a.d_v - wg_col : ATTN_COLS;
+    RowLoader<PIECES, R, 256> lq, lk, lw;
+    RowLoader<LY::UPIECES, R, 256> lo;
+    StepGates<R> lg;
+    const uint32_t stride_k = 2u * H_k * a.d_k, stride_w = 2u * a.H * a.d_k;
+    auto request = [&](int64_t k) {  // K, Q, dO and the gates of step k, W of the one behind it
+        const StepPos at = step_pos<R>(sq, k, k1, a.C);
+        lk.load(static_cast<const char*>(a.K) + at.row * stride_k + 2 * hk * a.d_k, stride_k, a.d_k, at.valid, tid);
+        lq.load(static_cast<const char*>(a.Q) + at.row * stride_k + 2 * hk * a.d_k, stride_k, a.d_k, at.valid, tid);
+        lo.load(static_cast<const char*>(a.dO) + at.row * stride_u + 2 * ((int64_t)h * a.d_v + wg_col), stride_u, cols, at.valid, tid);
+        lg.load(a.g, at, a.H, h, tid);
+        if constexpr (DELTA) {
+            const StepPos of_w = step_pos<R>(sq, k + 1, k1, a.C);
+            lw.load(static_cast<const char*>(a.W) + of_w.row * stride_w + 2 * (int64_t)h * a.d_k, stride_w, a.d_k, of_w.valid, tid);
         }
     };
-    if (n_chunk > 0) request(n_chunk - 1);
-    for (int64_t c = n_chunk - 1; c >= 0; --c) {
-        const int64_t left = sq.len - c * a.C;
-        const int valid = left < a.C ? (int)left : a.C;
-        lk.store(lds + LY::K_AT, tid);
+    auto bring = [&](int64_t k) {
+        lk.store(lds + LY::K_AT + (k & 1) * LY::ROWS, tid);
         lq.store(lds + LY::Q_AT, tid);
         lo.store(lds + LY::O_AT, tid);
-        if (tid < R) {
-            gl[tid] = g_row;
-            gl[R + tid] = expf(g_end - g_row);
-            gl[2 * R + tid] = a.scale * expf(g_row);
-        }
-        __syncthreads();
-        // P, as operands of P^T: token rows 4 q + r, column n.
+        lg.store(gates + (k & 1) * StepGates<R>::FLOATS, a.scale, tid);
+        if constexpr (DELTA) lw.store(lds + LY::W_AT, tid);
+    };
+    auto scores = [&](int64_t k) {  // P, as operands of P^T: token rows 4 q + r, column n; a share of the tiles a wavefront
+        const float* const gl = gates + (k & 1) * StepGates<R>::FLOATS;
+        const char* const rows_k = lds + LY::K_AT + (k & 1) * LY::ROWS;
+        constexpr int SHARE = (TILES + 3) / 4;
+        v4f x[SHARE];
+        int its[SHARE], jts[SHARE];
 #pragma unroll
-        for (int k = 0; k < (TILES + WAVES - 1) / WAVES; ++k) {
-            int idx = k * WAVES + wave, it = 0;
-            if (idx >= TILES) break;
+        for (int j = 0; j < SHARE; ++j) {
+            int idx = j * 4 + w4 < TILES ? j * 4 + w4 : TILES - 1, it = 0;  // (a wavefront without a tile forms the last one again)
             while (idx > it) idx -= ++it;
-            const int jt = idx;
-            v4f acc = zero4();
+            its[j] = it, jts[j] = idx, x[j] = zero4();
+        }
 #pragma unroll
-            for (int p = 0; p < KP; ++p)
-                acc = mfma32<OP>(lds_row<LY::PIECES>(lds + LY::Q_AT, 16 * it + ln.n, 4 * p + ln.q), lds_row<LY::PIECES>(lds + LY::K_AT, 16 * jt + ln.n, 4 * p + ln.q), acc);
+        for (int p = 0; p < KP; ++p)
+#pragma unroll
+            for (int j = 0; j < SHARE; ++j)
+                x[j] = mfma32<OP>(lds_row<PIECES>(lds + LY::Q_AT, 16 * its[j] + ln.n, 4 * p + ln.q), lds_row<PIECES>(rows_k, 16 * jts[j] + ln.n, 4 * p + ln.q), x[j]);
+#pragma unroll
+        for (int j = 0; j < SHARE; ++j) {
+            const int it = its[j], jt = jts[j];
             const float gj = gl[16 * jt + ln.n];
             const v4f gi = *reinterpret_cast<const v4f*>(gl + 16 * it + 4 * ln.q);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) acc[r] = jt < it || ln.n <= 4 * ln.q + r ? acc[r] * (a.scale * expf(gi[r] - gj)) : 0.f;
-            char* unit = lds + LY::P_AT + LY::UNIT * (unit_at<LY>(jt) + (it >> 1) - (jt >> 1)) + 16 * (16 * ln.q + ln.n) + 8 * (it & 1);
+            for (int r = 0; r < 4; ++r) x[j][r] *= a.scale * expf(jt < it || ln.n <= 4 * ln.q + r ? gi[r] - gj : -__builtin_inff());
+            char* unit = lds + LY::P_AT + LY::UNIT * (unit_at<LY>(jt) + (it >> 1) - (jt >> 1)) + lane16 + 8 * (it & 1);
 #pragma unroll
-            for (int part = 0; part < FULL_PARTS<OP>; ++part) {
-                const v2u x = pack4<OP>(acc);
-                *reinterpret_cast<v2u*>(unit + 1024 * part) = x;
+            for (int part = 0; part < FP; ++part) {
+                const v2u u = pack4<OP>(x[j]);
+                *reinterpret_cast<v2u*>(unit + 1024 * part) = u;
                 if (jt == it && (it & 1)) *reinterpret_cast<v2u*>(unit + 1024 * part - 8) = v2u{0u, 0u};  // the pair's other tile lies above the diagonal
-                acc = minus16<OP>(acc, x);
+                x[j] = minus16<OP>(x[j], u);
             }
         }
-        put_state<KP, NT>(a.rec_dstate + ((first_id + c) * a.H + h) * a.d_k * a.d_v, S, a.d_k, a.d_v, wg_col + col0, ln);
-        Parts<FULL_PARTS<OP>> sp[NT][KP];
-        const int s_shift = split_state<OP, KP, NT>(S, sp);
-        const float s_down = OP == OP_F16 ? pow2(-s_shift) : 1.f;
-        v4f dv[NT][MT];
-#pragma unroll
-        for (int tb = 0; tb < MT; ++tb) {
-            v4f acc[NT];
-#pragma unroll
-            for (int t = 0; t < NT; ++t) acc[t] = zero4();
-#pragma unroll
-            for (int p = 0; p < KP; ++p) {
-                const v4u k = lds_row<LY::PIECES>(lds + LY::K_AT, 16 * tb + ln.n, 4 * p + ln.q);
-#pragma unroll
-                for (int part = FULL_PARTS<OP> - 1; part >= 0; --part)
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) acc[t] = mfma32<OP>(k, sp[t][p].u[part], acc[t]);
-            }
-            const v4f e = *reinterpret_cast<const v4f*>(gl + R + 16 * tb + 4 * ln.q);
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) dv[t][tb][r] = acc[t][r] * (e[r] * s_down);
-        }
-        __syncthreads();  // P is in LDS
-        v4u o[NT][MT / 2];
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int tp = 0; tp < MT / 2; ++tp) {
-                const int row = 32 * tp + 4 * ln.q + (ln.n >> 2), col4 = (col0 >> 2) + 4 * t + (ln.n & 3);
-                const v2u x = lds_turned<LY::UPIECES>(lds + LY::O_AT, row, col4), y = lds_turned<LY::UPIECES>(lds + LY::O_AT, row + 16, col4);
-                o[t][tp] = v4u{x[0], x[1], y[0], y[1]};
-            }
-#pragma unroll
-        for (int jt = 0; jt < MT; ++jt)
-#pragma unroll
-            for (int tp = jt / 2; tp < MT / 2; ++tp) {
-                const char* unit = lds + LY::P_AT + LY::UNIT * (LY::units_before(jt) + tp - jt / 2) + 16 * (16 * ln.q + ln.n);
-#pragma unroll
-                for (int part = FULL_PARTS<OP> - 1; part >= 0; --part) {
-                    const v4u p = *reinterpret_cast<const v4u*>(unit + 1024 * part);
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) dv[t][jt] = mfma32<OP>(p, o[t][tp], dv[t][jt]);
-                }
-            }
-        // dU
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int tb = 0; tb < MT; ++tb) {
-                const v2u x = pack4<OP>(dv[t][tb]);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int i = 16 * tb + 4 * ln.q + r, col = wg_col + col0 + 16 * t + ln.n;
-                    if (i < valid && col < a.d_v) static_cast<uint16_t*>(a.dU)[((sq.tok0 + c * a.C + i) * a.H + h) * a.d_v + col] = (uint16_t)(x[r >> 1] >> (16 * (r & 1)));
-                }
-            }
-        const float decay = expf(gl[R - 1]);
-        // scale G dO in place of dO, row by row; the shift that suits it and dV'.
-        v4f od[NT][MT];
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int tb = 0; tb < MT; ++tb) {
-                const v4f e = *reinterpret_cast<const v4f*>(gl + 2 * R + 16 * tb + 4 * ln.q);
-                od[t][tb] = unpack4<OP>(v2u{o[t][tb / 2][2 * (tb & 1)], o[t][tb / 2][2 * (tb & 1) + 1]});
-#pragma unroll
-                for (int r = 0; r < 4; ++r) od[t][tb][r] *= e[r];
-            }
-        int shift = 0;
-        if constexpr (OP == OP_F16) {
-            float most = 0.f;
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int tb = 0; tb < MT; ++tb)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        most = fmaxf(most, fabsf(od[t][tb][r]));
-                        if (DELTA) most = fmaxf(most, fabsf(dv[t][tb][r]));
-                    }
-            shift = f16_shift(wave_max(most));
-        }
-        const float up = OP == OP_F16 ? pow2(shift) : 1.f;
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int i = 0; i < 2 * KP; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) S[t][i][r] *= decay * up;
+    };
+    auto products = [&](int64_t k) {  // P^T dO and scale Q^T diag(G) dO of this wavefront's columns
+        const float* const gl = gates + (k & 1) * StepGates<R>::FLOATS;
+        v4u o[MT / 2];
+        v4f y[MT], od[MT], x[2 * KP];
 #pragma unroll
         for (int tp = 0; tp < MT / 2; ++tp) {
-            Parts<FULL_PARTS<OP>> vp[NT];
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                v4f x = od[t][2 * tp], y = od[t][2 * tp + 1];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) x[r] *= up, y[r] *= up;
-                vp[t] = split_pair<OP, FULL_PARTS<OP>>(x, y);
-            }
-            add_turned<OP, MT, KP, NT, LY>(S, lds + LY::Q_AT, vp, tp, ln);
+            const int row = 32 * tp + 4 * ln.q + (ln.n >> 2), col4 = 4 * w4 + (ln.n & 3);
+            const v2u u = lds_turned<LY::UPIECES>(lds + LY::O_AT, row, col4), v = lds_turned<LY::UPIECES>(lds + LY::O_AT, row + 16, col4);
+            o[tp] = v4u{u[0], u[1], v[0], v[1]};
         }
-        if constexpr (DELTA) {
-            __syncthreads();  // P is used up
-            lw.store(lds + LY::P_AT, tid);
-            __syncthreads();
+#pragma unroll
+        for (int jt = 0; jt < MT; ++jt) y[jt] = zero4();
+#pragma unroll
+        for (int tp = 0; tp < MT / 2; ++tp)
+#pragma unroll
+            for (int part = FP - 1; part >= 0; --part)
+#pragma unroll
+                for (int jt = 0; jt <= 2 * tp + 1; ++jt)
+                    y[jt] = mfma32<OP>(*reinterpret_cast<const v4u*>(lds + LY::P_AT + LY::UNIT * (LY::units_before(jt) + tp - jt / 2) + 1024 * part + lane16), o[tp], y[jt]);
+#pragma unroll
+        for (int jt = 0; jt < MT; ++jt) *reinterpret_cast<v4f*>(lds + LY::Y_AT + LY::Y_WAVE * w4 + 1024 * jt + lane16) = y[jt];
+#pragma unroll
+        for (int tb = 0; tb < MT; ++tb) {
+            const v4f e = *reinterpret_cast<const v4f*>(gl + 2 * R + 16 * tb + 4 * ln.q);
+            od[tb] = unpack4<OP>(v2u{o[tb / 2][2 * (tb & 1)], o[tb / 2][2 * (tb & 1) + 1]});
+#pragma unroll
+            for (int r = 0; r < 4; ++r) od[tb][r] *= e[r];
         }
-        if (c > 0) request(c - 1);
-        if constexpr (DELTA) {
-#pragma unroll
-            for (int tp = 0; tp < MT / 2; ++tp) {
-                Parts<FULL_PARTS<OP>> vp[NT];
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    v4f x = dv[t][2 * tp], y = dv[t][2 * tp + 1];
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) x[r] *= -up, y[r] *= -up;
-                    vp[t] = split_pair<OP, FULL_PARTS<OP>>(x, y);
-                }
-                add_turned<OP, MT, KP, NT, LY>(S, lds + LY::P_AT, vp, tp, ln);
-            }
-        }
+        int shift = 0;
         if constexpr (OP == OP_F16) {
-            const float down = pow2(-shift);
+            shift = f16_shift(wave_max(most_of(od)));
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int i = 0; i < 2 * KP; ++i)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) S[t][i][r] *= down;
+            for (int tb = 0; tb < MT; ++tb) od[tb] = times(od[tb], pow2(shift));
         }
-        __syncthreads();  // the rows are not needed any more
+        Parts<FP> vp[MT / 2];
+        split_pairs<OP, FP, MT / 2>(od, vp, minus);
+#pragma unroll
+        for (int i = 0; i < 2 * KP; ++i) x[i] = zero4();
+        add_turned<OP, MT, KP>(x, lds + LY::Q_AT, vp, ln);
+#pragma unroll
+        for (int i = 0; i < 2 * KP; ++i) *reinterpret_cast<v4f*>(lds + LY::X_AT + LY::X_WAVE * w4 + 1024 * i + lane16) = OP == OP_F16 ? times(x[i], pow2(-shift)) : x[i];
+    };
+    request(k1 - 1);
+    bring(k1 - 1);
+    request(k1 - 2);
+    __syncthreads();
+    scores(k1 - 1);
+    __syncthreads();
+    products(k1 - 1);
+    __syncthreads();
+    for (int64_t k = k1 - 1; k >= 0; --k) {
+        bring(k - 1);
+        request(k - 2);
+        __syncthreads();  // the rows are in LDS
+        scores(k - 1);
+        __syncthreads();  // P is in LDS
+        products(k - 1);
+        __syncthreads();
     }
-    if (a.dstate0) put_state<KP, NT>(a.dstate0 + (int64_t)hs * a.d_k * a.d_v, S, a.d_k, a.d_v, wg_col + col0, ln);
 }
 
-// Everything that needs the states at both ends of a chunk: a workgroup per chunk and key head, which takes the heads that share it one
+// Everything that needs the states at both ends of a step: a workgroup per step and key head, which takes the heads that share it one
 // after the other and d_v in blocks of 64 columns.  A wavefront has KT tiles of 16 channels of all tokens; the products stand turned
-// (channels down, tokens across), so that a lane's four values are neighbours in memory.
-template <int OP, int MT, int KT, int WAVES, bool DELTA> struct BwdChunkLayout {
-    static constexpr int R = 16 * MT, PIECES = 2 * KT * WAVES, CB = 8;  // CB: pieces of a block of d_v
+// (channels down, tokens across), so that a lane's four values are neighbours in memory.  The next block's rows are requested before one is used.
+template <int OP, int MT, int KT, bool DELTA> struct BwdChunkLayout {
+    static constexpr int R = 16 * MT, PIECES = 8 * KT, CB = 8;  // CB: pieces of a block of d_v
     static constexpr int VP = DELTA ? FULL_PARTS<OP> : 1;
-    static constexpr int ROWS_BYTES = R * PIECES * 16, BLOCK = R * CB * 16;
+    static constexpr int ROWS = R * PIECES * 16, BLOCK = R * CB * 16;
     static constexpr int TILES = MT * (MT + 1) / 2, M_BYTES = TILES * FULL_PARTS<OP> * TURN16_BYTES;
     static constexpr int COLS_BYTES = (1 + VP + (DELTA ? 1 : 0)) * BLOCK;  // dO, V', dV'
-    static constexpr int K_AT = 0, Q_AT = ROWS_BYTES, O_AT = 2 * ROWS_BYTES, V_AT = O_AT + BLOCK, DV_AT = V_AT + VP * BLOCK;
+    static constexpr int K_AT = 0, Q_AT = ROWS, O_AT = 2 * ROWS, V_AT = O_AT + BLOCK, DV_AT = V_AT + VP * BLOCK;
     static constexpr int M_AT = O_AT;  // when the blocks of d_v are used up
-    static constexpr int G_AT = O_AT + (COLS_BYTES > M_BYTES ? COLS_BYTES : M_BYTES), RED_AT = G_AT + 3 * R * 4;
-    static constexpr int BYTES = RED_AT + (2 * WAVES * R + 4 * WAVES) * 4;
+    static constexpr int G_AT = O_AT + (COLS_BYTES > M_BYTES ? COLS_BYTES : M_BYTES), RED_AT = G_AT + StepGates<R>::FLOATS * 4;
+    static constexpr int BYTES = RED_AT + (8 * R + 16) * 4;
 };
 
 // fp32 rows of a head on their way to LDS as 16-bit parts.
-template <int OP, int N, int PIECES, int ROWS, int THREADS> struct SplitLoader {
-    static constexpr int COUNT = (PIECES * ROWS + THREADS - 1) / THREADS;
+template <int OP, int N, int PIECES, int ROWS> struct SplitLoader {
+    static constexpr int STRIDE = 256 / PIECES, COUNT = (ROWS + STRIDE - 1) / STRIDE;
     v4f v[COUNT][2];
-    __device__ __forceinline__ void load(const float* base, int64_t first, int row_elems, int d, int valid, int tid)
+    __device__ __forceinline__ void load(const float* first, uint32_t stride, int d, int valid, int tid)
     {
-        const uint32_t stride = (uint32_t)row_elems * 4u, span = valid > 0 ? (uint32_t)(valid - 1) * stride + (uint32_t)d * 4u : 0u;
-        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(reinterpret_cast<const char*>(base + first)), 0, span, 0x00020000);
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(first), 0, valid > 0 ? (uint32_t)(valid - 1) * stride + (uint32_t)d * 4u : 0u, 0x00020000);
+        const int row = tid / PIECES, piece = tid % PIECES;
+        uint32_t at = 8 * piece < d ? (uint32_t)row * stride + 32u * piece : 0x80000000u;
 #pragma unroll
-        for (int i = 0; i < COUNT; ++i) {
-            const int k = tid + i * THREADS, row = k / PIECES, piece = k % PIECES;
-            const uint32_t at = row < ROWS && 8 * piece < d ? (uint32_t)row * stride + 32u * piece : 0x80000000u;
+        for (int i = 0; i < COUNT; ++i, at += STRIDE * stride) {
             v[i][0] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0));
-            v[i][1] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 16, 0));
+            v[i][1] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at + 16u, 0, 0));
         }
     }
     __device__ __forceinline__ void store(char* m, int plane, int tid) const
     {
+        char* const to = m + LdsRows<PIECES>::at(tid / PIECES, tid % PIECES);
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) {
-            const int k = tid + i * THREADS;
-            if (k >= PIECES * ROWS) continue;
             const Parts<N> p = split_pair<OP, N>(v[i][0], v[i][1]);
 #pragma unroll
-            for (int j = 0; j < N; ++j) *reinterpret_cast<v4u*>(m + j * plane + LdsRows<PIECES>::at(k / PIECES, k % PIECES)) = p.u[j];
+            for (int j = 0; j < N; ++j) *reinterpret_cast<v4u*>(to + j * plane + i * STRIDE * LdsRows<PIECES>::BYTES) = p.u[j];
         }
     }
 };
@@ -340,120 +354,150 @@ __device__ __forceinline__ float wave_sum(float x)
     return x;
 }
 
-template <int OP, int MT, int KT, int WAVES, bool DELTA>
-__global__ __launch_bounds__(64 * WAVES) void k_attn_bwd_chunk(AttnBwdArgs a)
+// Tokens 32 tp .. 32 tp + 31 of the channels ch .. ch + 15, as an operand over the tokens.
+template <int PIECES> __device__ __forceinline__ v4u lds_turned_channels(const char* m, int tp, int ch, Lane ln)
 {
-    typedef BwdChunkLayout<OP, MT, KT, WAVES, DELTA> LY;
-    constexpr int THREADS = 64 * WAVES, R = LY::R, SHARE = (LY::TILES + WAVES - 1) / WAVES, FP = FULL_PARTS<OP>;
+    const int row = 32 * tp + 4 * ln.q + (ln.n >> 2), col4 = (ch >> 2) + (ln.n & 3);
+    const v2u a = lds_turned<PIECES>(m, row, col4), b = lds_turned<PIECES>(m, row + 16, col4);
+    return v4u{a[0], a[1], b[0], b[1]};
+}
+
+// SHARED: heads share a key head, whose dQ and dK are summed in registers.
+template <int OP, int MT, int KT, bool DELTA, bool TWO, bool SHARED>
+__global__ __launch_bounds__(256) void k_attn_bwd_chunk(AttnBwdArgs a)
+{
+    typedef BwdChunkLayout<OP, MT, KT, DELTA> LY;
+    constexpr int R = LY::R, SHARE = (LY::TILES + 3) / 4, FP = FULL_PARTS<OP>;
     __shared__ __attribute__((aligned(16))) char lds[LY::BYTES];
-    float* const gl = reinterpret_cast<float*>(lds + LY::G_AT);    // g, exp(g_C - g), scale exp(g)
+    float* const gl = reinterpret_cast<float*>(lds + LY::G_AT);
     float* const red = reinterpret_cast<float*>(lds + LY::RED_AT);  // sums over channels: [2][wavefront][token], then [4][wavefront]
-    float* const red1 = red + 2 * WAVES * R;
+    float* const red1 = red + 8 * R;
     const Lane ln = lane_id();
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), H_k = a.H / a.group;
     const unsigned b = xcd_neighbours(blockIdx.x, gridDim.x);
-    const int hk = b % H_k;
-    const int64_t id = b / H_k;
-    // which sequence and chunk
-    int64_t c;
+    const int hk = b % H_k, steps = a.C > R ? a.C / R : 1, tokens = a.C < R ? a.C : R;
+    const int64_t id = b / H_k, chunk = id / steps;  // of the step, and its chunk
     SeqPos sq;
+    int64_t k;  // the step in its sequence
     if (a.map.cu_chunks) {
         int lo = 0, hi = a.map.n_seq - 1;
         while (lo < hi) {
             const int mid = (lo + hi + 1) / 2;
-            if (a.map.cu_chunks[mid] <= id) lo = mid;
+            if (a.map.cu_chunks[mid] <= chunk) lo = mid;
             else hi = mid - 1;
         }
-        sq = seq_pos(a.map, lo), c = id - a.map.cu_chunks[lo];
+        sq = seq_pos(a.map, lo), k = id - a.map.cu_chunks[lo] * steps;
     } else {
         const int64_t cps = (a.map.Tlen + a.C - 1) / a.C;
-        sq = SeqPos{id / cps * a.map.Tlen, a.map.Tlen}, c = id % cps;
+        sq = SeqPos{chunk / cps * a.map.Tlen, a.map.Tlen}, k = chunk % cps * steps + id % steps;
     }
-    const int64_t left = sq.len - c * a.C, row0 = sq.tok0 + c * a.C;
-    const int valid = left < a.C ? (int)left : a.C;
+    const int64_t all = (sq.len + tokens - 1) / tokens;
+    if (k >= all) return;  // (the second step of a chunk that ends in its first)
+    const StepPos at = step_pos<R>(sq, k, all, a.C);
+    const bool chunk_ends = steps == 1 || (k & 1) || k + 1 == all;
     const int ch0 = 16 * KT * wave;  // this wavefront's first channel
+    const uint32_t stride_k = 2u * H_k * a.d_k, stride_u = 2u * a.H * a.d_v;
+    const MinusOne<OP> minus(ln);
+    RowLoader<LY::CB, R, 256> lo, lu;  // dO; dV', or V' itself
+    SplitLoader<OP, FP, LY::CB, R> lv;
+    StepGates<R> lg;
+    auto request = [&](int h, int v0) {
+        const int cols = a.d_v - v0 < 64 ? a.d_v - v0 : 64;
+        const int64_t first = (at.row * a.H + h) * a.d_v + v0;
+        lo.load(static_cast<const uint16_t*>(a.dO) + first, stride_u, cols, at.valid, tid);
+        lu.load(static_cast<const uint16_t*>(DELTA ? a.dU : a.U) + first, stride_u, cols, at.valid, tid);
+        if constexpr (DELTA) lv.load(a.rec_value + first, 2u * stride_u, cols, at.valid, tid);
+    };
+    v4f sv[KT][2][2], dsv[KT][2][2];  // this wavefront's rows of S and dS', the block's columns
+    v4f szv[TWO ? KT : 1][2][2];      // of the state before the chunk, in its second step
+    const bool second = TWO && (k & 1);
+    auto request_states = [&](int h, int v0) {
+        const uint32_t span = (uint32_t)a.d_k * a.d_v * 4u;
+        const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(a.rec_state) + (id * a.H + h) * a.d_k * a.d_v, 0, span, 0x00020000);
+        const auto rd = __builtin_amdgcn_make_buffer_rsrc(a.rec_dstate + (id * a.H + h) * a.d_k * a.d_v, 0, span, 0x00020000);
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                const int ch = ch0 + 16 * kt + ln.n, col = v0 + 32 * ks + 8 * ln.q;
+                const uint32_t from = ch < a.d_k && col < a.d_v ? (uint32_t)(ch * a.d_v + col) * 4u : 0x80000000u;
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    sv[kt][ks][half] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(rs, from + 16u * half, 0, 0));
+                    dsv[kt][ks][half] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(rd, from + 16u * half, 0, 0));
+                    if constexpr (TWO) {
+                        const auto rz = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(a.rec_state) + ((id - second) * a.H + h) * a.d_k * a.d_v, 0, span, 0x00020000);
+                        szv[kt][ks][half] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(rz, from + 16u * half, 0, 0));
+                    }
+                }
+            }
+    };
+    const int h0 = hk * a.group;
+    request(h0, 0);
     {
-        RowLoader<LY::PIECES, R, THREADS> lk, lq;
-        lk.load(a.K, (row0 * H_k + hk) * a.d_k, H_k * a.d_k, a.d_k, valid, tid);
-        lq.load(a.Q, (row0 * H_k + hk) * a.d_k, H_k * a.d_k, a.d_k, valid, tid);
+        RowLoader<LY::PIECES, R, 256> lk, lq;
+        lk.load(static_cast<const char*>(a.K) + at.row * stride_k + 2 * hk * a.d_k, stride_k, a.d_k, at.valid, tid);
+        lq.load(static_cast<const char*>(a.Q) + at.row * stride_k + 2 * hk * a.d_k, stride_k, a.d_k, at.valid, tid);
+        lg.load(a.g, at, a.H, h0, tid);
+        request_states(h0, 0);
         lk.store(lds + LY::K_AT, tid);
         lq.store(lds + LY::Q_AT, tid);
     }
-    v4f sum_q[KT][MT], sum_k[KT][MT];
+    v4f sum_q[SHARED ? KT : 1][MT], sum_k[SHARED ? KT : 1][MT];
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt)
+    for (int kt = 0; kt < (SHARED ? KT : 1); ++kt)
 #pragma unroll
         for (int it = 0; it < MT; ++it) sum_q[kt][it] = sum_k[kt][it] = zero4();
+    auto put_rows = [&](void* to, const v4f x, int heads, int head, int ch, int it) {
+        const int i = 16 * it + ln.n;
+        if (i < at.valid && ch < a.d_k) *reinterpret_cast<v2u*>(static_cast<uint16_t*>(to) + ((at.row + i) * heads + head) * a.d_k + ch) = pack4<OP>(x);
+    };
 
-    for (int h = hk * a.group; h < (hk + 1) * a.group; ++h) {
-        if (tid < R) {
-            float g_row = 0.f, g_end = 0.f;
-            if (a.g) g_row = a.g[(row0 + (tid < valid ? tid : valid - 1)) * a.H + h], g_end = a.g[(row0 + valid - 1) * a.H + h];
-            gl[tid] = g_row, gl[R + tid] = expf(g_end - g_row), gl[2 * R + tid] = a.scale * expf(g_row);
-        }
-        const float* const S = a.rec_state + (id * a.H + h) * a.d_k * a.d_v;
-        const float* const dS = a.rec_dstate + (id * a.H + h) * a.d_k * a.d_v;
+    for (int h = h0; h < h0 + (SHARED ? a.group : 1); ++h) {
+        lg.store(gl, a.scale, tid);
         v4f X[KT][MT], Y[KT][MT], Z[KT][MT], M[SHARE];
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
             for (int it = 0; it < MT; ++it) X[kt][it] = Y[kt][it] = Z[kt][it] = zero4();
 #pragma unroll
-        for (int k = 0; k < SHARE; ++k) M[k] = zero4();
+        for (int j = 0; j < SHARE; ++j) M[j] = zero4();
+        // this wavefront's tiles of M (one without a tile forms the last one again, and writes the same)
+        int its[SHARE], jts[SHARE], idx[SHARE];
+#pragma unroll
+        for (int j = 0; j < SHARE; ++j) {
+            int x = j * 4 + wave < LY::TILES ? j * 4 + wave : LY::TILES - 1, it = 0;
+            idx[j] = x;
+            while (x > it) x -= ++it;
+            its[j] = it, jts[j] = x;
+        }
         float s_ds = 0.f;
-        int s_shift = 0, d_shift = 0;
+        int s_shift = 0, d_shift = 0, z_shift = 0;
         for (int v0 = 0; v0 < a.d_v; v0 += 64) {
-            const int cols = a.d_v - v0 < 64 ? a.d_v - v0 : 64;
-            {
-                RowLoader<LY::CB, R, THREADS> lo;
-                lo.load(a.dO, (row0 * a.H + h) * a.d_v + v0, a.H * a.d_v, cols, valid, tid);
-                if constexpr (DELTA) {
-                    RowLoader<LY::CB, R, THREADS> ld;
-                    SplitLoader<OP, FP, LY::CB, R, THREADS> lv;
-                    ld.load(a.dU, (row0 * a.H + h) * a.d_v + v0, a.H * a.d_v, cols, valid, tid);
-                    lv.load(a.rec_value, (row0 * a.H + h) * a.d_v + v0, a.H * a.d_v, cols, valid, tid);
-                    lo.store(lds + LY::O_AT, tid);
-                    ld.store(lds + LY::DV_AT, tid);
-                    lv.store(lds + LY::V_AT, LY::BLOCK, tid);
-                } else {
-                    RowLoader<LY::CB, R, THREADS> lv;
-                    lv.load(a.U, (row0 * a.H + h) * a.d_v + v0, a.H * a.d_v, cols, valid, tid);
-                    lo.store(lds + LY::O_AT, tid);
-                    lv.store(lds + LY::V_AT, tid);
-                }
+            lo.store(lds + LY::O_AT, tid);
+            if constexpr (DELTA) {
+                lu.store(lds + LY::DV_AT, tid);
+                lv.store(lds + LY::V_AT, LY::BLOCK, tid);
+            } else {
+                lu.store(lds + LY::V_AT, tid);
             }
             __syncthreads();
+            const bool last_block = v0 + 64 >= a.d_v;
+            const int next_h = last_block ? (SHARED && h + 1 < h0 + a.group ? h + 1 : h) : h, next_v = last_block ? (SHARED && h + 1 < h0 + a.group ? 0 : a.d_v) : v0 + 64;
+            if (next_v < a.d_v) request(next_h, next_v);
             // dO V'^T, turned: value tokens down, output tokens across
 #pragma unroll
-            for (int k = 0; k < SHARE; ++k) {
-                int idx = k * WAVES + wave, it = 0;
-                if (idx >= LY::TILES) break;
-                while (idx > it) idx -= ++it;
+            for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-                for (int ks = 0; ks < 2; ++ks) {
-                    const v4u o = lds_row<LY::CB>(lds + LY::O_AT, 16 * it + ln.n, 4 * ks + ln.q);
+                for (int part = LY::VP - 1; part >= 0; --part)
 #pragma unroll
-                    for (int part = LY::VP - 1; part >= 0; --part)
-                        M[k] = mfma32<OP>(lds_row<LY::CB>(lds + LY::V_AT + part * LY::BLOCK, 16 * idx + ln.n, 4 * ks + ln.q), o, M[k]);
-                }
-            }
+                    for (int j = 0; j < SHARE; ++j)
+                        M[j] = mfma32<OP>(lds_row<LY::CB>(lds + LY::V_AT + part * LY::BLOCK, 16 * jts[j] + ln.n, 4 * ks + ln.q), lds_row<LY::CB>(lds + LY::O_AT, 16 * its[j] + ln.n, 4 * ks + ln.q), M[j]);
             // S dO^T, S dV'^T and dS' V'^T
-            v4f sv[KT][2][2], dsv[KT][2][2];
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-                for (int ks = 0; ks < 2; ++ks) {
-                    const int ch = ch0 + 16 * kt + ln.n, col = v0 + 32 * ks + 8 * ln.q;
-                    const bool there = ch < a.d_k && col < a.d_v;
-                    const int64_t at = (int64_t)ch * a.d_v + col;
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        sv[kt][ks][half] = there ? *reinterpret_cast<const v4f*>(S + at + 4 * half) : zero4();
-                        dsv[kt][ks][half] = there ? *reinterpret_cast<const v4f*>(dS + at + 4 * half) : zero4();
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) s_ds += sv[kt][ks][half][r] * dsv[kt][ks][half][r];
-                    }
-                }
+                for (int i = 0; i < 16; ++i) s_ds += sv[kt][i >> 3][i >> 2 & 1][i & 3] * dsv[kt][i >> 3][i >> 2 & 1][i & 3];
             if constexpr (OP == OP_F16) {  // both into fp16's range, and what there is of the products with them
                 float most_s = 0.f, most_d = 0.f;
 #pragma unroll
@@ -463,6 +507,23 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_bwd_chunk(AttnBwdArgs a)
                 const int ns = f16_shift(wave_max(most_s)), nd = f16_shift(wave_max(most_d));
                 const float us = pow2(ns), ud = pow2(nd), cs = v0 ? pow2(ns - s_shift) : 1.f, cd = v0 ? pow2(nd - d_shift) : 1.f;
                 s_shift = ns, d_shift = nd;
+                float cz = cs;
+                if constexpr (TWO) {
+                    float most_z = 0.f;
+#pragma unroll
+                    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) most_z = fmaxf(most_z, fabsf(szv[kt][i >> 3][i >> 2 & 1][i & 3]));
+                    const int nz = f16_shift(wave_max(most_z));
+                    cz = v0 ? pow2(nz - z_shift) : 1.f;
+                    z_shift = nz;
+#pragma unroll
+                    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) szv[kt][i >> 3][i >> 2 & 1][i & 3] *= pow2(nz);
+                } else {
+                    z_shift = ns;
+                }
 #pragma unroll
                 for (int kt = 0; kt < KT; ++kt) {
 #pragma unroll
@@ -470,71 +531,87 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_bwd_chunk(AttnBwdArgs a)
 #pragma unroll
                     for (int it = 0; it < MT; ++it)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) X[kt][it][r] *= cs, Z[kt][it][r] *= cs, Y[kt][it][r] *= cd;
+                        for (int r = 0; r < 4; ++r) X[kt][it][r] *= cs, Z[kt][it][r] *= cz, Y[kt][it][r] *= cd;
                 }
             }
 #pragma unroll
-            for (int ks = 0; ks < 2; ++ks)
+            for (int ks = 0; ks < 2; ++ks) {
+                Parts<FP> sp[KT], dp[KT];
+                {
+                    v4f x[2 * KT], y[2 * KT];
 #pragma unroll
-                for (int kt = 0; kt < KT; ++kt) {
-                    const Parts<FP> sp = split_pair<OP, FP>(sv[kt][ks][0], sv[kt][ks][1]), dp = split_pair<OP, FP>(dsv[kt][ks][0], dsv[kt][ks][1]);
-#pragma unroll
-                    for (int it = 0; it < MT; ++it) {
-                        const v4u o = lds_row<LY::CB>(lds + LY::O_AT, 16 * it + ln.n, 4 * ks + ln.q);
-#pragma unroll
-                        for (int part = FP - 1; part >= 0; --part) X[kt][it] = mfma32<OP>(sp.u[part], o, X[kt][it]);
-                        if constexpr (DELTA) {
-                            const v4u d = lds_row<LY::CB>(lds + LY::DV_AT, 16 * it + ln.n, 4 * ks + ln.q);
-                            Z[kt][it] = mfma32<OP>(sp.u[1], d, Z[kt][it]);
-                            Z[kt][it] = mfma32<OP>(sp.u[0], d, Z[kt][it]);
-                        }
-                        // parts of both sides: what is left out is below the last bit kept
-#pragma unroll
-                        for (int order = FP - 1; order >= 0; --order)
-#pragma unroll
-                            for (int j = order < LY::VP - 1 ? order : LY::VP - 1; j >= 0; --j)
-                                Y[kt][it] = mfma32<OP>(dp.u[order - j], lds_row<LY::CB>(lds + LY::V_AT + j * LY::BLOCK, 16 * it + ln.n, 4 * ks + ln.q), Y[kt][it]);
-                    }
+                    for (int kt = 0; kt < KT; ++kt) x[2 * kt] = sv[kt][ks][0], x[2 * kt + 1] = sv[kt][ks][1], y[2 * kt] = dsv[kt][ks][0], y[2 * kt + 1] = dsv[kt][ks][1];
+                    split_pairs<OP, FP, KT>(x, sp, minus);
+                    split_pairs<OP, FP, KT>(y, dp, minus);
                 }
+                Parts<2> zp[KT];
+                if constexpr (TWO) {
+                    v4f x[2 * KT];
+#pragma unroll
+                    for (int kt = 0; kt < KT; ++kt) x[2 * kt] = szv[kt][ks][0], x[2 * kt + 1] = szv[kt][ks][1];
+                    split_pairs<OP, 2, KT>(x, zp, minus);
+                } else {
+#pragma unroll
+                    for (int kt = 0; kt < KT; ++kt) zp[kt].u[0] = sp[kt].u[0], zp[kt].u[1] = sp[kt].u[1];
+                }
+                v4u o[MT], d[MT];
+#pragma unroll
+                for (int it = 0; it < MT; ++it) {
+                    o[it] = lds_row<LY::CB>(lds + LY::O_AT, 16 * it + ln.n, 4 * ks + ln.q);
+                    if constexpr (DELTA) d[it] = lds_row<LY::CB>(lds + LY::DV_AT, 16 * it + ln.n, 4 * ks + ln.q);
+                }
+#pragma unroll
+                for (int part = FP - 1; part >= 0; --part)
+#pragma unroll
+                    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                        for (int it = 0; it < MT; ++it) {
+                            X[kt][it] = mfma32<OP>(sp[kt].u[part], o[it], X[kt][it]);
+                            if constexpr (DELTA) {
+                                if (part < 2) Z[kt][it] = mfma32<OP>(zp[kt].u[part < 2 ? part : 0], d[it], Z[kt][it]);
+                            }
+                        }
+                // parts of both sides: what is left out is below the last bit kept
+#pragma unroll
+                for (int j = LY::VP - 1; j >= 0; --j) {
+                    v4u v[MT];
+#pragma unroll
+                    for (int it = 0; it < MT; ++it) v[it] = lds_row<LY::CB>(lds + LY::V_AT + j * LY::BLOCK, 16 * it + ln.n, 4 * ks + ln.q);
+#pragma unroll
+                    for (int i = FP - 1 - j; i >= 0; --i)
+#pragma unroll
+                        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                            for (int it = 0; it < MT; ++it) Y[kt][it] = mfma32<OP>(dp[kt].u[i], v[it], Y[kt][it]);
+                }
+            }
+            if (next_v < a.d_v) request_states(next_h, next_v);
             __syncthreads();  // the block is used up
         }
+        if (SHARED && h + 1 < h0 + a.group) lg.load(a.g, at, a.H, h + 1, tid);
         // M = scale (dO V'^T) . D, in parts; fp16: times a power of two that all wavefronts agree on
-        float most = 0.f;
 #pragma unroll
-        for (int k = 0; k < SHARE; ++k) {
-            int idx = k * WAVES + wave, it = 0;
-            if (idx >= LY::TILES) break;
-            while (idx > it) idx -= ++it;
-            const float gi = gl[16 * it + ln.n];
-            const v4f gj = *reinterpret_cast<const v4f*>(gl + 16 * idx + 4 * ln.q);
+        for (int j = 0; j < SHARE; ++j) {
+            const float gi = gl[16 * its[j] + ln.n];
+            const v4f gj = *reinterpret_cast<const v4f*>(gl + 16 * jts[j] + 4 * ln.q);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                M[k][r] = idx < it || 4 * ln.q + r <= ln.n ? M[k][r] * (a.scale * expf(gi - gj[r])) : 0.f;
-                most = fmaxf(most, fabsf(M[k][r]));
-            }
+            for (int r = 0; r < 4; ++r) M[j][r] *= a.scale * expf(jts[j] < its[j] || 4 * ln.q + r <= ln.n ? gi - gj[r] : -__builtin_inff());
         }
         int m_shift = 0;
         if constexpr (OP == OP_F16) {
-            most = wave_max(most);
-            if (ln.q == 0 && ln.n == 0) red1[wave] = most;
+            const float mine = wave_max(most_of(M));
+            if (ln.q == 0 && ln.n == 0) red1[wave] = mine;
             __syncthreads();
-            for (int w = 0; w < WAVES; ++w) most = fmaxf(most, red1[w]);
-            m_shift = f16_shift(most);
+            m_shift = f16_shift(fmaxf(fmaxf(red1[0], red1[1]), fmaxf(red1[2], red1[3])));
         }
         const Turn16 turn(reinterpret_cast<float*>(lds + LY::M_AT), ln);
 #pragma unroll
-        for (int k = 0; k < SHARE; ++k) {
-            const int idx = k * WAVES + wave;
-            if (idx >= LY::TILES) break;
-            v4f m = M[k];
-            if constexpr (OP == OP_F16) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) m[r] *= pow2(m_shift);
-            }
+        for (int j = 0; j < SHARE; ++j) {
+            v4f m = OP == OP_F16 ? times(M[j], pow2(m_shift)) : M[j];
 #pragma unroll
             for (int part = 0; part < FP; ++part) {
                 const v2u x = pack4<OP>(m);
-                turn.put(part * LY::TILES + idx, x);
+                turn.put(part * LY::TILES + idx[j], x);
                 m = minus16<OP>(m, x);
             }
         }
@@ -543,91 +620,92 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_bwd_chunk(AttnBwdArgs a)
         const float up = OP == OP_F16 ? pow2(m_shift) : 1.f, down = OP == OP_F16 ? pow2(-m_shift) : 1.f;
         const float s_down = OP == OP_F16 ? pow2(-s_shift) : 1.f, d_down = OP == OP_F16 ? pow2(-d_shift) : 1.f;
         float inter = 0.f;
+        v4u kt_op[KT][MT / 2], qt_op[KT][MT / 2];
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int tp = 0; tp < MT / 2; ++tp) {
+                kt_op[kt][tp] = lds_turned_channels<LY::PIECES>(lds + LY::K_AT, tp, ch0 + 16 * kt, ln);
+                qt_op[kt][tp] = lds_turned_channels<LY::PIECES>(lds + LY::Q_AT, tp, ch0 + 16 * kt, ln);
+            }
 #pragma unroll
         for (int it = 0; it < MT; ++it) {
+            v4f q[KT], kk[KT];
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) {
+                const int ch = ch0 + 16 * kt, piece = (ch >> 3) + (ln.q >> 1), byte = 8 * (ln.q & 1);
+                q[kt] = unpack4<OP>(*reinterpret_cast<const v2u*>(lds + LY::Q_AT + LdsRows<LY::PIECES>::at(16 * it + ln.n, piece) + byte));
+                kk[kt] = unpack4<OP>(*reinterpret_cast<const v2u*>(lds + LY::K_AT + LdsRows<LY::PIECES>::at(16 * it + ln.n, piece) + byte));
+                const float gx = gl[2 * R + 16 * it + ln.n] * s_down, gy = gl[R + 16 * it + ln.n] * d_down;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    X[kt][it][r] *= gx, Y[kt][it][r] *= gy;
+                    inter += kk[kt][r] * Y[kt][it][r];
+                    if constexpr (OP == OP_F16) X[kt][it][r] *= up, Y[kt][it][r] *= up;
+                }
+            }
+#pragma unroll
+            for (int tp = 0; tp < MT / 2; ++tp)
+#pragma unroll
+                for (int part = FP - 1; part >= 0; --part) {
+                    if (tp <= it / 2) {
+                        const v2u m0 = *reinterpret_cast<const v2u*>(turn.put_at + (part * LY::TILES + tix(it, 2 * tp)) * TURN16_BYTES);
+                        v2u m1 = {0u, 0u};
+                        if (2 * tp + 1 <= it) m1 = *reinterpret_cast<const v2u*>(turn.put_at + (part * LY::TILES + tix(it, 2 * tp + 1)) * TURN16_BYTES);
+#pragma unroll
+                        for (int kt = 0; kt < KT; ++kt) X[kt][it] = mfma32<OP>(kt_op[kt][tp], v4u{m0[0], m0[1], m1[0], m1[1]}, X[kt][it]);
+                    }
+                    if (tp >= it / 2) {
+                        v2u m0 = {0u, 0u};
+                        if (2 * tp >= it) m0 = turn.get(part * LY::TILES + tix(2 * tp, it));
+                        const v2u m1 = turn.get(part * LY::TILES + tix(2 * tp + 1, it));
+#pragma unroll
+                        for (int kt = 0; kt < KT; ++kt) Y[kt][it] = mfma32<OP>(qt_op[kt][tp], v4u{m0[0], m0[1], m1[0], m1[1]}, Y[kt][it]);
+                    }
+                }
             float dot_q = 0.f, dot_k = 0.f;
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt) {
-                v4f x = X[kt][it], y = Y[kt][it];
-                const float gx = gl[2 * R + 16 * it + ln.n] * s_down, gy = gl[R + 16 * it + ln.n] * d_down;
-                const int ch = ch0 + 16 * kt, piece = (ch >> 3) + (ln.q >> 1), byte = 8 * (ln.q & 1);
-                const v4f q = unpack4<OP>(*reinterpret_cast<const v2u*>(lds + LY::Q_AT + LdsRows<LY::PIECES>::at(16 * it + ln.n, piece) + byte));
-                const v4f kk = unpack4<OP>(*reinterpret_cast<const v2u*>(lds + LY::K_AT + LdsRows<LY::PIECES>::at(16 * it + ln.n, piece) + byte));
+                const int ch = ch0 + 16 * kt + 4 * ln.q;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    x[r] *= gx, y[r] *= gy;
-                    inter += kk[r] * y[r];
-                    if constexpr (OP == OP_F16) x[r] *= up, y[r] *= up;
+                    if constexpr (OP == OP_F16) X[kt][it][r] *= down, Y[kt][it][r] *= down;
+                    dot_q += q[kt][r] * X[kt][it][r], dot_k += kk[kt][r] * Y[kt][it][r];
+                    if constexpr (SHARED) sum_q[kt][it][r] += X[kt][it][r], sum_k[kt][it][r] += Y[kt][it][r];
                 }
-#pragma unroll
-                for (int tp = 0; tp < MT / 2; ++tp) {
-                    const int row = 32 * tp + 4 * ln.q + (ln.n >> 2), col4 = (ch >> 2) + (ln.n & 3);
-                    if (tp <= it / 2) {
-                        const v2u k0 = lds_turned<LY::PIECES>(lds + LY::K_AT, row, col4), k1 = lds_turned<LY::PIECES>(lds + LY::K_AT, row + 16, col4);
-#pragma unroll
-                        for (int part = FP - 1; part >= 0; --part) {
-                            const v2u m0 = *reinterpret_cast<const v2u*>(turn.put_at + (part * LY::TILES + tix(it, 2 * tp)) * TURN16_BYTES);
-                            v2u m1 = {0u, 0u};
-                            if (2 * tp + 1 <= it) m1 = *reinterpret_cast<const v2u*>(turn.put_at + (part * LY::TILES + tix(it, 2 * tp + 1)) * TURN16_BYTES);
-                            x = mfma32<OP>(v4u{k0[0], k0[1], k1[0], k1[1]}, v4u{m0[0], m0[1], m1[0], m1[1]}, x);
-                        }
-                    }
-                    if (tp >= it / 2) {
-                        const v2u q0 = lds_turned<LY::PIECES>(lds + LY::Q_AT, row, col4), q1 = lds_turned<LY::PIECES>(lds + LY::Q_AT, row + 16, col4);
-#pragma unroll
-                        for (int part = FP - 1; part >= 0; --part) {
-                            v2u m0 = {0u, 0u};
-                            if (2 * tp >= it) m0 = turn.get(part * LY::TILES + tix(2 * tp, it));
-                            const v2u m1 = turn.get(part * LY::TILES + tix(2 * tp + 1, it));
-                            y = mfma32<OP>(v4u{q0[0], q0[1], q1[0], q1[1]}, v4u{m0[0], m0[1], m1[0], m1[1]}, y);
-                        }
-                    }
-                }
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    if constexpr (OP == OP_F16) x[r] *= down, y[r] *= down;
-                    dot_q += q[r] * x[r], dot_k += kk[r] * y[r];
-                    sum_q[kt][it][r] += x[r], sum_k[kt][it][r] += y[r];
-                }
-                const int i = 16 * it + ln.n;
-                if constexpr (DELTA) {
-                    v4f z = Z[kt][it];
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) z[r] *= -s_down;
-                    if (i < valid && ch + 4 * ln.q < a.d_k) *reinterpret_cast<v2u*>(static_cast<uint16_t*>(a.dW) + ((row0 + i) * a.H + h) * a.d_k + ch + 4 * ln.q) = pack4<OP>(z);
-                }
+                if constexpr (DELTA) put_rows(a.dW, times(Z[kt][it], OP == OP_F16 ? -pow2(-z_shift) : -1.f), a.H, h, ch, it);
+                if constexpr (!SHARED) put_rows(a.dQ, X[kt][it], H_k, hk, ch, it), put_rows(a.dK, Y[kt][it], H_k, hk, ch, it);
             }
             dot_q += __shfl_xor(dot_q, 16), dot_k += __shfl_xor(dot_k, 16);
             dot_q += __shfl_xor(dot_q, 32), dot_k += __shfl_xor(dot_k, 32);
-            if (ln.q == 0) red[wave * R + 16 * it + ln.n] = dot_q, red[(WAVES + wave) * R + 16 * it + ln.n] = dot_k;
+            if (ln.q == 0) red[wave * R + 16 * it + ln.n] = dot_q, red[(4 + wave) * R + 16 * it + ln.n] = dot_k;
         }
         if (a.dg) {
             const float x = wave_sum(inter), y = wave_sum(s_ds);
-            if (ln.q == 0 && ln.n == 0) red1[wave] = x, red1[WAVES + wave] = y;
+            if (ln.q == 0 && ln.n == 0) red1[4 + wave] = x, red1[8 + wave] = y;
             __syncthreads();
-            if (tid < valid) {
-                float q = 0.f, k = 0.f, last = 0.f;
-                for (int w = 0; w < WAVES; ++w) q += red[w * R + tid], k += red[(WAVES + w) * R + tid];
-                if (tid == valid - 1) {
+            if (tid < at.valid) {
+                float q = 0.f, kd = 0.f, last = 0.f;
+                for (int w = 0; w < 4; ++w) q += red[w * R + tid], kd += red[(4 + w) * R + tid];
+                if (chunk_ends && tid == at.valid - 1) {
                     float t = 0.f;
-                    for (int w = 0; w < WAVES; ++w) last += red1[w], t += red1[WAVES + w];
-                    last += expf(gl[R - 1]) * t;
+                    for (int w = 0; w < 4; ++w) last += red1[4 + w], t += red1[8 + w];
+                    last += gl[3 * R] * t;
                 }
-                a.dg[(row0 + tid) * a.H + h] = q - k + last;
+                a.dg[(at.row + tid) * a.H + h] = q - kd + last;
             }
         }
-        __syncthreads();  // M and the sums are not needed any more
+        if constexpr (SHARED) __syncthreads();  // M, the gates and the sums are not needed any more
     }
+    if constexpr (SHARED) {
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt)
+        for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-        for (int it = 0; it < MT; ++it) {
-            const int i = 16 * it + ln.n, ch = ch0 + 16 * kt + 4 * ln.q;
-            if (i >= valid || ch >= a.d_k) continue;
-            const int64_t at = ((row0 + i) * H_k + hk) * a.d_k + ch;
-            *reinterpret_cast<v2u*>(static_cast<uint16_t*>(a.dQ) + at) = pack4<OP>(sum_q[kt][it]);
-            *reinterpret_cast<v2u*>(static_cast<uint16_t*>(a.dK) + at) = pack4<OP>(sum_k[kt][it]);
-        }
+            for (int it = 0; it < MT; ++it) {
+                put_rows(a.dQ, sum_q[kt][it], H_k, hk, ch0 + 16 * kt + 4 * ln.q, it);
+                put_rows(a.dK, sum_k[kt][it], H_k, hk, ch0 + 16 * kt + 4 * ln.q, it);
+            }
+    }
 }
 
 }  // namespace triinv

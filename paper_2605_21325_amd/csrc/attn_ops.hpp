@@ -1,9 +1,8 @@
 // What the chunk-attention kernels share: 16-bit parts of fp32 tiles, chunk rows staged in LDS, where a sequence's tokens are.
 //
-// The state S (d_k x d_v, fp32) stays in registers as 16 x 16 tiles in the accumulator layout (tile_ops.hpp), a wavefront holding all
-// d_k rows of its columns.  Tile 2 p + h of a column holds, in row 4 q + r, channel 32 p + 8 q + 4 h + r: the two packed tiles of a
-// pair then are, register for register, the operand that meets 16 consecutive bytes of a token's row (8 channels a lane), on either
-// side of a product:
+// The state S (d_k x d_v, fp32) stays in registers as 16 x 16 tiles in the accumulator layout (tile_ops.hpp): tile 2 p + e of a column tile holds, in
+// register r of lane 16 q + n, channel 32 p + 8 q + 4 e + r of column n.  The two packed tiles of a pair then are, register for register, the operand
+// that meets 16 consecutive bytes of a token's row (8 channels a lane), on either side of a product:
 //   W S        A = rows of W,  B = tiles of S;       S^T Q^T    A = tiles of S,  B = rows of Q;
 //   V'^T P^T   A = tiles of V', B = tiles of P^T;     K^T V'     A = K read transposed from LDS, B = tiles of V'.
 // No accumulator crosses lanes on its way to the next product.
@@ -82,6 +81,35 @@ template <int OP, int N> __device__ __forceinline__ Parts<N> split_pair(v4f a, v
     return o;
 }
 
+// The same for some pairs at once, the rests formed by the matrix cores (x - part = x + (-1) part, exact): one instruction a tile in place of eight, and the
+// vector unit is what these kernels run out of first.
+template <int OP> struct MinusOne {
+    v4u of_first, of_second;  // left operands that pick one tile of a pair, negated
+    __device__ __forceinline__ explicit MinusOne(Lane ln)
+    {
+        constexpr uint32_t m = OP == OP_F16 ? 0xbc00u : 0xbf80u;
+        const v2u one = {4 * ln.q == ln.n ? m : 4 * ln.q + 1 == ln.n ? m << 16 : 0u, 4 * ln.q + 2 == ln.n ? m : 4 * ln.q + 3 == ln.n ? m << 16 : 0u};
+        of_first = v4u{one[0], one[1], 0u, 0u}, of_second = v4u{0u, 0u, one[0], one[1]};
+    }
+};
+template <int OP, int N, int COUNT> __device__ __forceinline__ void split_pairs(v4f (&x)[2 * COUNT], Parts<N> (&o)[COUNT], const MinusOne<OP>& minus)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+#pragma unroll
+        for (int k = 0; k < COUNT; ++k) {
+            const v2u a = pack4<OP>(x[2 * k]), b = pack4<OP>(x[2 * k + 1]);
+            o[k].u[i] = v4u{a[0], a[1], b[0], b[1]};
+        }
+        if (i + 1 < N) {
+#pragma unroll
+            for (int k = 0; k < COUNT; ++k) {
+                x[2 * k] = mfma32<OP>(minus.of_first, o[k].u[i], x[2 * k]), x[2 * k + 1] = mfma32<OP>(minus.of_second, o[k].u[i], x[2 * k + 1]);
+            }
+        }
+    }
+}
+
 // Largest of a non-negative value over the wavefront, as a uniform value.
 __device__ __forceinline__ float wave_max(float x)
 {
@@ -106,51 +134,75 @@ __device__ __forceinline__ int f16_shift(float most)
 }
 __device__ __forceinline__ float pow2(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }
 
-// Rows of 16-byte pieces in LDS; a row's pieces are permuted by the row, so that sixteen lanes reading one piece of sixteen rows, or
-// transposing reads of four rows, meet different banks.
+// Rows of 16-byte pieces in LDS, a row's pieces permuted by the row: sixteen lanes that read one piece of sixteen rows find it in sixteen places, and eight
+// rows of a transposing read lie as far apart as they can (with the low bits of the row alone, four of them met in the same banks, and the kernels
+// waited for LDS half of their time).
 template <int PIECES> struct LdsRows {
-    static constexpr int BYTES = PIECES * 16, TURN = (PIECES < 16 ? PIECES : 16) - 1;
-    static_assert((PIECES & (PIECES - 1)) == 0, "a power of two");
-    static __device__ __forceinline__ int at(int row, int piece) { return row * BYTES + ((piece ^ (row & TURN)) << 4); }
+    static constexpr int BYTES = PIECES * 16;
+    static_assert(PIECES == 8 || PIECES == 16, "rows of 128 or 256 bytes");
+    static __device__ __forceinline__ int at(int row, int piece)
+    {
+        const int turn = PIECES == 16 ? (row & 3) << 2 | (row >> 2 & 3) : (row << 1 & 4) | (row >> 1 & 2) | (row >> 3 & 1);
+        return row * BYTES + ((piece ^ turn) << 4);
+    }
 };
-template <int PIECES> __device__ __forceinline__ v4u lds_row(const char* m, int row, int piece)
-{
-    return *reinterpret_cast<const v4u*>(m + LdsRows<PIECES>::at(row, piece));
-}
+// Eight columns from 8 `piece` on.
+template <int PIECES> __device__ __forceinline__ v4u lds_row(const char* m, int row, int piece) { return *reinterpret_cast<const v4u*>(m + LdsRows<PIECES>::at(row, piece)); }
 typedef __attribute__((address_space(3))) v4s* lds_v4s_ptr;
-// Rows 16 tb + 4 q + r (r = 0..3) of column 4 * (piece of lane n / 4) + n % 4: columns are given by the lane's own 4-column piece `col4`.
+// Rows `row` .. `row` + 3 of a lane group, turned: the group's lane n points at row n / 4 of them and at the columns 4 col4 .. 4 col4 + 3, and receives
+// column n % 16 of the four rows.
 template <int PIECES> __device__ __forceinline__ v2u lds_turned(const char* m, int row, int col4)
 {
     const char* p = m + LdsRows<PIECES>::at(row, col4 >> 1) + ((col4 & 1) << 3);
     return __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_ptr)(p)));
 }
+// Tokens 32 tp .. 32 tp + 31 of the channels of state tile i, as an operand over the tokens.
+template <int PIECES> __device__ __forceinline__ v4u lds_turned_tile(const char* m, int tp, int i, Lane ln)
+{
+    const int row = 32 * tp + 4 * ln.q + (ln.n >> 2), col4 = 8 * (i >> 1) + 2 * (ln.n & 3) + (i & 1);
+    const v2u a = lds_turned<PIECES>(m, row, col4), b = lds_turned<PIECES>(m, row + 16, col4);
+    return v4u{a[0], a[1], b[0], b[1]};
+}
+// Channel of row `row` of state tile i.
+__device__ __forceinline__ int state_channel(int i, int row) { return 32 * (i >> 1) + 8 * (row >> 2) + 4 * (i & 1) + (row & 3); }
 
-// Rows of one head of a [token][heads][d] tensor on their way from memory to LDS: `rows` of them, what is not there (rows from
-// `valid` on, columns from d on) as zeros, by the bounds check of buffer loads.
-template <int PIECES, int ROWS, int THREADS> struct RowLoader {
-    static constexpr int N = (PIECES * ROWS + THREADS - 1) / THREADS;
-    v4u v[N];
-    static __device__ __forceinline__ constexpr bool whole() { return PIECES * ROWS % THREADS == 0; }
-    __device__ __forceinline__ void load(const void* base, int64_t first_elem, int row_elems, int d, int valid, int tid)
-    {
-        const uint32_t stride = (uint32_t)row_elems * 2u;
-        const uint32_t span = valid > 0 ? (uint32_t)(valid - 1) * stride + (uint32_t)d * 2u : 0u;
-        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(base)) + first_elem * 2, 0, span, 0x00020000);
+template <int OP> __device__ __forceinline__ v4f unpack4(v2u raw)
+{
+    v4f u;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int k = tid + i * THREADS, row = k / PIECES, piece = k % PIECES;
-            const bool there = (whole() || row < ROWS) && 8 * piece < d;
-            v[i] = __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(rsrc, there ? (uint32_t)row * stride + 16u * piece : 0x80000000u, 0, 0));
-        }
+    for (int r = 0; r < 4; ++r) {
+        const uint16_t x = (uint16_t)(raw[r >> 1] >> (16 * (r & 1)));
+        u[r] = OP == OP_F16 ? f16_to_f32(x) : bf16_to_f32(x);
+    }
+    return u;
+}
+
+// Rows of one head of a [token][heads][d] tensor on their way from memory to LDS: `ROWS` of them, what is not there (rows from
+// `valid` on, columns from d on) as zeros, by the bounds check of buffer loads.  A thread has one piece of every THREADS / PIECES-th row.
+template <int PIECES, int ROWS, int THREADS> struct RowLoader {
+    static constexpr int STRIDE = THREADS / PIECES, N = (ROWS + STRIDE - 1) / STRIDE;
+    static_assert(THREADS % PIECES == 0 && (STRIDE % 16 == 0 || N == 1), "a thread's rows are permuted alike");
+    v4u v[N];
+    __device__ __forceinline__ void load(const void* first, uint32_t stride, int d, int valid, int tid)
+    {
+        const uint32_t span = valid > 0 ? (uint32_t)(valid - 1) * stride + (uint32_t)d * 2u : 0u;
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(first), 0, span, 0x00020000);
+        const int row = tid / PIECES, piece = tid % PIECES;
+        uint32_t at = 8 * piece < d && (ROWS >= STRIDE || row < ROWS) ? (uint32_t)row * stride + 16u * piece : 0x80000000u;
+#pragma unroll
+        for (int i = 0; i < N; ++i, at += STRIDE * stride) v[i] = __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0));
     }
     __device__ __forceinline__ void store(char* m, int tid) const
     {
+        const int row = tid / PIECES;
+        if (ROWS < STRIDE && row >= ROWS) return;
+        char* const to = m + LdsRows<PIECES>::at(row, tid % PIECES);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int k = tid + i * THREADS;
-            if (whole() || k < PIECES * ROWS) *reinterpret_cast<v4u*>(m + LdsRows<PIECES>::at(k / PIECES, k % PIECES)) = v[i];
-        }
+        for (int i = 0; i < N; ++i) *reinterpret_cast<v4u*>(to + i * STRIDE * LdsRows<PIECES>::BYTES) = v[i];
     }
 };
+
+// Nothing is moved across: what stands before is issued before (the scheduler, left alone, waits for every read from LDS right where it asked for it).
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
 
 }  // namespace triinv

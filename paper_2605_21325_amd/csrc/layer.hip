@@ -79,10 +79,10 @@ int attn_common(const void* Q, const void* K, const void* U, const void* W, cons
     return finish(dtype == TRIINV_F16 ? launch_chunk_attn_f16(a) : launch_chunk_attn_bf16(a));
 }
 
-// States before and gradients behind every chunk, and the values where they are not U.
-int64_t attn_bwd_workspace(int64_t n_token, int64_t n_chunk, int H, int d_k, int d_v, bool has_w)
+// States before and gradients behind every 64 tokens or chunk, and the values where they are not U.
+int64_t attn_bwd_workspace(int64_t n_token, int64_t n_chunk, int H, int d_k, int d_v, int C, bool has_w)
 {
-    return 4 * H * (2 * n_chunk * d_k * d_v + (has_w ? n_token * d_v : 0));
+    return 4 * H * (2 * n_chunk * (C > 64 ? 2 : 1) * d_k * d_v + (has_w ? n_token * d_v : 0));
 }
 
 int attn_bwd_common(const void* Q, const void* K, const void* U, const void* W, const float* g, const float* state, const void* dO, const float* dstate, void* dQ,
@@ -92,7 +92,7 @@ int attn_bwd_common(const void* Q, const void* K, const void* U, const void* W, 
 {
     if (dtype == TRIINV_F32) return TRIINV_ERR_UNSUPPORTED;
     if ((int64_t)H * d_v * C * 4 >= (1LL << 31)) return TRIINV_ERR_UNSUPPORTED;  // (values are read back in fp32)
-    const int64_t need = attn_bwd_workspace(n_token, n_chunk, H, d_k, d_v, W != nullptr);
+    const int64_t need = attn_bwd_workspace(n_token, n_chunk, H, d_k, d_v, C, W != nullptr);
     if (n_token > 0 && (!Q || !K || !U || !dO || !dQ || !dK || !dU || !workspace || (W != nullptr) != (dW != nullptr))) return TRIINV_ERR_NULL;
     if (dg && !g) return TRIINV_ERR_NULL;
     if (workspace_bytes < need) return TRIINV_ERR_BAD_SHAPE;
@@ -153,11 +153,11 @@ int gdn_chunk_attn_varlen(const void* Q, const void* K, const void* U, const voi
                        d_v, C, dtype, scale, hip_stream);
 }
 
-int gdn_chunk_attn_bwd_workspace(int64_t total_tokens, int64_t total_chunks, int H, int d_k, int d_v, int has_w, int64_t* bytes)
+int gdn_chunk_attn_bwd_workspace(int64_t total_tokens, int64_t total_chunks, int H, int d_k, int d_v, int C, int has_w, int64_t* bytes)
 {
     if (!bytes) return TRIINV_ERR_NULL;
     if (total_tokens < 0 || total_chunks < 0 || H <= 0 || d_k <= 0 || d_v <= 0) return TRIINV_ERR_BAD_SHAPE;
-    *bytes = attn_bwd_workspace(total_tokens, total_chunks, H, d_k, d_v, has_w != 0);
+    *bytes = attn_bwd_workspace(total_tokens, total_chunks, H, d_k, d_v, C, has_w != 0);
     return TRIINV_OK;
 }
 

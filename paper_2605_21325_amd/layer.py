@@ -116,7 +116,7 @@ def _attn_bwd(where, Q, K, U, g, dO, C, W, state, dstate, scale, stream, lead, n
     _has(dO, "dO", U.shape, U.dtype)
     _has(dstate, "dstate", (n_seq, H, d_k, d_v), torch.float32)
     size = ctypes.c_int64()
-    st = binding.lib().gdn_chunk_attn_bwd_workspace(n_token, n_chunk, H, d_k, d_v, W is not None, ctypes.byref(size))
+    st = binding.lib().gdn_chunk_attn_bwd_workspace(n_token, n_chunk, H, d_k, d_v, C, W is not None, ctypes.byref(size))
     if st != OK:
         raise TriInvError(st, where)
     with _on(stream):

@@ -97,8 +97,8 @@ def test_workspaces(L):
     assert L.gdn_chunk_attn_workspace(1, 2, 4, 128, 128, 1, ctypes.byref(n)) == OK and n.value == 0
     assert L.gdn_chunk_attn_workspace(0, 2, 4, 128, 128, 1, ctypes.byref(n)) == BAD_SHAPE
     assert L.gdn_chunk_attn_workspace(1, 2, 4, 128, 128, 1, None) == NULL
-    assert L.gdn_chunk_attn_bwd_workspace(100, 2, 4, 128, 64, 1, ctypes.byref(n)) == OK and n.value == 4 * 4 * (2 * 2 * 128 * 64 + 100 * 64)
-    assert L.gdn_chunk_attn_bwd_workspace(-1, 2, 4, 128, 64, 1, ctypes.byref(n)) == BAD_SHAPE
+    assert L.gdn_chunk_attn_bwd_workspace(100, 2, 4, 128, 64, 64, 1, ctypes.byref(n)) == OK and n.value == 4 * 4 * (2 * 2 * 128 * 64 + 100 * 64)
+    assert L.gdn_chunk_attn_bwd_workspace(-1, 2, 4, 128, 64, 64, 1, ctypes.byref(n)) == BAD_SHAPE
 
 
 def test_the_binding_refuses_what_a_kernel_would_misread():
