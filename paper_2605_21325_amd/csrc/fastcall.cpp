@@ -17,6 +17,8 @@
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <stdint.h>
+#include <cmath>
+#include <cstring>
 #include <vector>
 
 namespace {
@@ -39,6 +41,23 @@ struct Abi {
     int (*solve_packed)(const void*, const void*, const void*, const void*, const void*, void*, const int64_t*, int, int64_t, int, int, int, int, int,
                         int, int, int, void*, uint32_t);
 } abi;
+
+// The layer's other operators (connect_layer).
+struct LayerAbi {
+    int (*attn)(const void*, const void*, const void*, const void*, const void*, const void*, void*, void*, void*, int64_t, int, int64_t, int, int, int, int, int, int, float,
+                void*);
+    int (*attn_varlen)(const void*, const void*, const void*, const void*, const void*, const void*, void*, void*, void*, int64_t, const int64_t*, const int64_t*, int, int64_t,
+                       int64_t, int, int, int, int, int, int, float, void*);
+    int (*attn_workspace)(int, int64_t, int, int, int, int, int64_t*);
+    int (*attn_bwd)(const void*, const void*, const void*, const void*, const void*, const void*, const void*, const void*, void*, void*, void*, void*, void*, void*, void*,
+                    int64_t, int, int64_t, int, int, int, int, int, int, float, void*);
+    int (*attn_bwd_varlen)(const void*, const void*, const void*, const void*, const void*, const void*, const void*, const void*, void*, void*, void*, void*, void*, void*, void*,
+                           int64_t, const int64_t*, const int64_t*, int, int64_t, int64_t, int, int, int, int, int, int, float, void*);
+    int (*attn_bwd_workspace)(int64_t, int64_t, int, int, int, int, int, int64_t*);
+    int (*step)(const void*, const void*, const void*, const void*, const void*, void*, const void*, void*, int, int64_t, int, int, int, int, int, float, void*);
+    int (*norm)(const void*, const void*, const void*, void*, void*, void*, int64_t, int, int, int, float, void*);
+    int (*norm_bwd)(const void*, const void*, const void*, const void*, void*, void*, void*, int64_t, int64_t, int, int, float, void*);
+} layer;
 
 int code_of(at::ScalarType t) { return t == at::kFloat ? F32 : t == at::kHalf ? F16 : t == at::kBFloat16 ? BF16 : -1; }
 
@@ -70,6 +89,30 @@ public:
         at::Tensor t = THPVariable_Unpack(o);
         if ((device_ < 0 ? !t.is_cpu() : !t.is_cuda() || t.get_device() != device_) || t.is_nested() || t.layout() != at::kStrided ||
             !t.is_contiguous() || (dims >= 0 && t.dim() != dims) || code_of(t.scalar_type()) < 0)
+            return fail(), at::Tensor();
+        return t;
+    }
+    double number()
+    {
+        PyObject* const o = next();
+        if (!ok_ || (!PyFloat_Check(o) && !PyLong_CheckExact(o))) return fail();
+        const double x = PyFloat_AsDouble(o);
+        if (x == -1.0 && PyErr_Occurred()) {
+            PyErr_Clear();
+            return fail();
+        }
+        return x;
+    }
+    double number_or(double otherwise) { return ok_ && *v_ == Py_None ? (next(), otherwise) : number(); }
+    // a contiguous int32 tensor on the device of the call, or None
+    at::Tensor places()
+    {
+        PyObject* const o = next();
+        if (!ok_ || o == Py_None) return {};
+        if (!THPVariable_CheckExact(o)) return fail(), at::Tensor();
+        at::Tensor t = THPVariable_Unpack(o);
+        if ((device_ < 0 ? !t.is_cpu() : !t.is_cuda() || t.get_device() != device_) || t.is_nested() || t.layout() != at::kStrided || !t.is_contiguous() || t.dim() != 1 ||
+            t.scalar_type() != at::kInt)
             return fail(), at::Tensor();
         return t;
     }
@@ -354,6 +397,236 @@ PyObject* gdn_solve_varlen(PyObject*, PyObject* const* v, Py_ssize_t n)
     return with_offsets(W, cu);
 }
 
+// Whether a tensor that may be absent has this shape and element type.
+bool has(const at::Tensor& t, at::IntArrayRef shape, at::ScalarType type) { return !t.defined() || (t.sizes() == shape && t.scalar_type() == type); }
+const void* opt(const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
+PyObject* wrap(const at::Tensor& t) { return t.defined() ? THPVariable_Wrap(t) : none(); }
+template <size_t N> PyObject* tuple_of(const at::Tensor (&t)[N])
+{
+    PyObject* const r = PyTuple_New(N);
+    for (size_t i = 0; r && i < N; ++i) {
+        PyObject* const x = wrap(t[i]);
+        if (!x) return Py_DECREF(r), nullptr;
+        PyTuple_SET_ITEM(r, i, x);
+    }
+    return r;
+}
+
+// What the forms of the chunk attention share: tensors of the tokens with `lead` dimensions in front of the heads, states of n_seq sequences.
+struct AttnArguments {
+    at::Tensor Q, K, U, g, W, state, cu;
+    std::vector<int64_t> lens;
+    int64_t n_seq = 0, T = 0, n_token = 0, n_chunk = 0, H = 0, Hk = 0, dk = 0, dv = 0;
+    int C = 0;
+    bool packed = false;
+    at::TensorOptions fp32() const { return Q.options().dtype(at::kFloat); }
+    // Q, K, U, g[, dO][, seqlens], C, W, state
+    bool read(Args& a, bool is_packed, at::Tensor* dO)
+    {
+        packed = is_packed;
+        const int lead = packed ? 1 : 2;
+        Q = a.tensor(lead + 2), K = a.tensor(lead + 2), U = a.tensor(lead + 2), g = a.tensor(lead + 1, true);
+        if (dO) *dO = a.tensor(lead + 2);
+        PyObject* const seqlens = packed ? a.next() : nullptr;
+        C = a.small(), W = a.tensor(lead + 2, true), state = a.tensor(4, true);
+        if (!a.ok() || !chunk_ok(C) || (packed && !lengths(seqlens, lens))) return false;
+        Hk = Q.size(lead), dk = Q.size(lead + 1), H = U.size(lead), dv = U.size(lead + 1);
+        n_token = packed ? Q.size(0) : Q.size(0) * Q.size(1);
+        n_seq = packed ? (int64_t)lens.size() : Q.size(0), T = packed ? n_token : Q.size(1);
+        std::vector<int64_t> shape(Q.sizes().begin(), Q.sizes().end());
+        const at::ScalarType type = Q.scalar_type();
+        if (!has(K, shape, type)) return false;
+        shape[lead] = H;
+        if (!has(W, shape, type)) return false;
+        shape[lead + 1] = dv;
+        if (!has(U, shape, type) || (dO && !has(*dO, shape, type))) return false;
+        shape.pop_back();
+        if (!has(g, shape, at::kFloat) || !has(state, {n_seq, H, dk, dv}, at::kFloat)) return false;
+        for (const int64_t x : {n_seq, H, Hk, dk, dv}) a.narrow(x);
+        n_chunk = packed ? 0 : n_seq * ((T + C - 1) / C);
+        return a.ok() && n_token > 0;
+    }
+    bool offsets(void* stream)
+    {
+        if (!packed) return true;
+        cu = at::empty({2 * (n_seq + 1)}, Q.options().dtype(at::kLong));
+        return abi.offsets(lens.data(), (int)n_seq, C, n_token, cu.data_ptr<int64_t>(), &n_chunk, stream) == 0;
+    }
+};
+
+PyObject* keep_offsets(PyObject* r, Py_ssize_t at, const at::Tensor& cu)
+{
+    if (!r || !cu.defined()) return r;
+    PyObject* const c = THPVariable_Wrap(cu);
+    PyObject* const keep = c ? PyTuple_Pack(1, c) : nullptr;
+    const bool good = keep && PyObject_SetAttrString(PyTuple_GET_ITEM(r, at), "_triinv_keepalive", keep) == 0;
+    Py_XDECREF(c);
+    Py_XDECREF(keep);
+    if (good) return r;
+    Py_DECREF(r);
+    return nullptr;
+}
+
+// (device, stream, Q, K, U, g, [seqlens,] C, W, state, scale, O, final_state): (O, final_state)
+PyObject* attn_call(PyObject* const* v, Py_ssize_t n, bool packed)
+{
+    Args a(v, n, packed ? 13 : 12);
+    a.device_and_stream();
+    AttnArguments x;
+    if (!x.read(a, packed, nullptr)) return none();
+    const float scale = (float)a.number_or(1.0 / std::sqrt((double)x.dk));
+    at::Tensor r[2] = {a.tensor(packed ? 3 : 4, true), a.tensor(4, true)};
+    if (!a.ok() || !has(r[0], x.U.sizes(), x.U.scalar_type()) || !has(r[1], {x.n_seq, x.H, x.dk, x.dv}, at::kFloat)) return none();
+    if (!unlocked([&] {
+            if (!x.offsets(a.stream())) return false;
+            int64_t bytes = 0;
+            if (layer.attn_workspace((int)x.n_seq, x.n_chunk, (int)x.H, (int)x.dk, (int)x.dv, x.W.defined(), &bytes) != 0) return false;
+            at::Tensor ws;
+            if (bytes > 0) ws = at::empty({bytes}, x.Q.options().dtype(at::kByte));
+            if (!r[0].defined()) r[0] = at::empty(x.U.sizes(), x.U.options());
+            if (!r[1].defined()) r[1] = at::empty({x.n_seq, x.H, x.dk, x.dv}, x.fp32());
+            const int type = code_of(x.Q.scalar_type());
+            const int64_t* const c = packed ? x.cu.data_ptr<int64_t>() : nullptr;
+            return (packed ? layer.attn_varlen(x.Q.data_ptr(), x.K.data_ptr(), x.U.data_ptr(), opt(x.W), opt(x.g), opt(x.state), r[0].data_ptr(), r[1].data_ptr(),
+                                               const_cast<void*>(opt(ws)), bytes, c, c + x.n_seq + 1, (int)x.n_seq, x.n_token, x.n_chunk, (int)x.H, (int)x.Hk, (int)x.dk, (int)x.dv,
+                                               x.C, type, scale, a.stream())
+                           : layer.attn(x.Q.data_ptr(), x.K.data_ptr(), x.U.data_ptr(), opt(x.W), opt(x.g), opt(x.state), r[0].data_ptr(), r[1].data_ptr(),
+                                        const_cast<void*>(opt(ws)), bytes, (int)x.n_seq, x.T, (int)x.H, (int)x.Hk, (int)x.dk, (int)x.dv, x.C, type, scale, a.stream())) == 0;
+        }))
+        return none();
+    return keep_offsets(tuple_of(r), 1, x.cu);
+}
+PyObject* chunk_attn(PyObject*, PyObject* const* v, Py_ssize_t n) { return attn_call(v, n, false); }
+PyObject* chunk_attn_varlen(PyObject*, PyObject* const* v, Py_ssize_t n) { return attn_call(v, n, true); }
+
+// (device, stream, Q, K, U, g, dO, [seqlens,] C, W, state, dstate, scale): (dQ, dK, dU, dW, dg, dstate0)
+PyObject* attn_bwd_call(PyObject* const* v, Py_ssize_t n, bool packed)
+{
+    Args a(v, n, packed ? 13 : 12);
+    a.device_and_stream();
+    AttnArguments x;
+    at::Tensor dO;
+    if (!x.read(a, packed, &dO)) return none();
+    const at::Tensor dstate = a.tensor(4, true);
+    const float scale = (float)a.number_or(1.0 / std::sqrt((double)x.dk));
+    if (!a.ok() || !has(dstate, {x.n_seq, x.H, x.dk, x.dv}, at::kFloat)) return none();
+    at::Tensor r[6];
+    if (!unlocked([&] {
+            if (!x.offsets(a.stream())) return false;
+            int64_t bytes = 0;
+            if (layer.attn_bwd_workspace(x.n_token, x.n_chunk, (int)x.H, (int)x.dk, (int)x.dv, x.C, x.W.defined(), &bytes) != 0) return false;
+            const at::Tensor ws = at::empty({bytes < 16 ? 16 : bytes}, x.Q.options().dtype(at::kByte)), like[6] = {x.Q, x.K, x.U, x.W, x.g, x.state};
+            for (int i = 0; i < 6; ++i)
+                if (like[i].defined()) r[i] = at::empty(like[i].sizes(), like[i].options());
+            const auto p = [&](int i) { return const_cast<void*>(opt(r[i])); };
+            const int type = code_of(x.Q.scalar_type());
+            const int64_t* const c = packed ? x.cu.data_ptr<int64_t>() : nullptr;
+            return (packed ? layer.attn_bwd_varlen(x.Q.data_ptr(), x.K.data_ptr(), x.U.data_ptr(), opt(x.W), opt(x.g), opt(x.state), dO.data_ptr(), opt(dstate), p(0), p(1), p(2),
+                                                   p(3), p(4), p(5), ws.data_ptr(), ws.numel(), c, c + x.n_seq + 1, (int)x.n_seq, x.n_token, x.n_chunk, (int)x.H, (int)x.Hk, (int)x.dk,
+                                                   (int)x.dv, x.C, type, scale, a.stream())
+                           : layer.attn_bwd(x.Q.data_ptr(), x.K.data_ptr(), x.U.data_ptr(), opt(x.W), opt(x.g), opt(x.state), dO.data_ptr(), opt(dstate), p(0), p(1), p(2), p(3),
+                                            p(4), p(5), ws.data_ptr(), ws.numel(), (int)x.n_seq, x.T, (int)x.H, (int)x.Hk, (int)x.dk, (int)x.dv, x.C, type, scale, a.stream())) == 0;
+        }))
+        return none();
+    return keep_offsets(tuple_of(r), 0, x.cu);
+}
+PyObject* chunk_attn_bwd(PyObject*, PyObject* const* v, Py_ssize_t n) { return attn_bwd_call(v, n, false); }
+PyObject* chunk_attn_bwd_varlen(PyObject*, PyObject* const* v, Py_ssize_t n) { return attn_bwd_call(v, n, true); }
+
+// (device, stream, q, k, v, g, state, beta, slots, scale, o): o
+PyObject* step(PyObject*, PyObject* const* v, Py_ssize_t n)
+{
+    Args a(v, n, 11);
+    a.device_and_stream();
+    const at::Tensor q = a.tensor(3), k = a.tensor(3), x = a.tensor(3), g = a.tensor(2, true), state = a.tensor(4), beta = a.tensor(2, true), slots = a.places();
+    if (!a.ok() || !q.numel() || !x.numel() || !state.numel()) return none();
+    const int64_t B = q.size(0), Hk = q.size(1), dk = q.size(2), H = x.size(1), dv = x.size(2);
+    const float scale = (float)a.number_or(1.0 / std::sqrt((double)dk));
+    at::Tensor o = a.tensor(3, true);
+    const at::ScalarType type = q.scalar_type();
+    if (!a.ok() || !has(k, q.sizes(), type) || !has(x, {B, H, dv}, type) || !has(g, {B, H}, at::kFloat) || !has(beta, {B, H}, at::kFloat) || !has(slots, {B}, at::kInt) ||
+        !has(state, {state.size(0), H, dk, dv}, at::kFloat) || !has(o, x.sizes(), type))
+        return none();
+    for (const int64_t i : {B, Hk, dk, H, dv}) a.narrow(i);
+    if (!a.ok() || !unlocked([&] {
+            if (!o.defined()) o = at::empty(x.sizes(), x.options());
+            return layer.step(q.data_ptr(), k.data_ptr(), x.data_ptr(), opt(g), opt(beta), state.data_ptr(), opt(slots), o.data_ptr(), (int)B, state.size(0), (int)H, (int)Hk, (int)dk,
+                              (int)dv, code_of(type), scale, a.stream()) == 0;
+        }))
+        return none();
+    return THPVariable_Wrap(o);
+}
+
+// (device, stream, x, weight, residual, eps, group): (y, s) or, group >= 0, (y, scales, s)
+PyObject* norm(PyObject*, PyObject* const* v, Py_ssize_t n)
+{
+    Args a(v, n, 7);
+    a.device_and_stream();
+    const at::Tensor x = a.tensor(-1), weight = a.tensor(1), residual = a.tensor(-1, true);
+    const float eps = (float)a.number();
+    const int group = a.small();
+    if (!a.ok() || x.dim() < 1 || !x.numel() || (group != -1 && group != 0 && group != 128)) return none();
+    const int64_t D = x.size(-1), N = x.numel() / D;
+    if (!has(weight, {D}, x.scalar_type()) || !has(residual, x.sizes(), x.scalar_type()) || (a.narrow(D), !a.ok())) return none();
+    at::Tensor y, scales, s;
+    if (!unlocked([&] {
+            y = at::empty(x.sizes(), group < 0 ? x.options() : x.options().dtype(at::kFloat8_e4m3fn));
+            if (group >= 0) {
+                std::vector<int64_t> shape(x.sizes().begin(), x.sizes().end());
+                shape.back() = group ? D / group : 1;
+                scales = at::empty(shape, x.options().dtype(at::kFloat));
+            }
+            if (residual.defined()) s = at::empty(x.sizes(), x.options());
+            return layer.norm(x.data_ptr(), opt(residual), weight.data_ptr(), y.data_ptr(), const_cast<void*>(opt(scales)), const_cast<void*>(opt(s)), N, (int)D, group,
+                              code_of(x.scalar_type()), eps, a.stream()) == 0;
+        }))
+        return none();
+    if (!s.defined()) s = x;
+    if (group < 0) {
+        const at::Tensor r[2] = {y, s};
+        return tuple_of(r);
+    }
+    const at::Tensor r[3] = {y, scales, s};
+    return tuple_of(r);
+}
+
+// (device, stream, dy, s, weight, eps, dsum): (dx, dweight)
+PyObject* norm_bwd(PyObject*, PyObject* const* v, Py_ssize_t n)
+{
+    Args a(v, n, 7);
+    a.device_and_stream();
+    const at::Tensor dy = a.tensor(-1), s = a.tensor(-1), weight = a.tensor(1);
+    const float eps = (float)a.number();
+    const at::Tensor dsum = a.tensor(-1, true);
+    if (!a.ok() || s.dim() < 1 || !s.numel()) return none();
+    const int64_t D = s.size(-1), N = s.numel() / D;
+    if (!has(dy, s.sizes(), s.scalar_type()) || !has(weight, {D}, s.scalar_type()) || !has(dsum, s.sizes(), s.scalar_type()) || (a.narrow(D), !a.ok())) return none();
+    at::Tensor r[2];
+    if (!unlocked([&] {
+            r[0] = at::empty(s.sizes(), s.options());
+            r[1] = at::empty({D}, s.options().dtype(at::kFloat));
+            const at::Tensor ws = at::empty({(N < 512 ? N : 512) * D}, s.options().dtype(at::kFloat));
+            return layer.norm_bwd(dy.data_ptr(), s.data_ptr(), weight.data_ptr(), opt(dsum), r[0].data_ptr(), r[1].data_ptr(), ws.data_ptr(), ws.numel() * 4, N, (int)D,
+                                  code_of(s.scalar_type()), eps, a.stream()) == 0;
+        }))
+        return none();
+    return tuple_of(r);
+}
+
+// connect_layer(addresses): the C-ABI functions in the order of LayerAbi
+PyObject* connect_layer(PyObject*, PyObject* const* v, Py_ssize_t n)
+{
+    constexpr int N = sizeof(LayerAbi) / sizeof(void*);
+    void* p[N] = {};
+    if (n != N) return PyErr_SetString(PyExc_TypeError, "nine addresses"), nullptr;
+    for (int i = 0; i < N; ++i) {
+        p[i] = PyLong_AsVoidPtr(v[i]);
+        if (!p[i]) return PyErr_Occurred() ? nullptr : (PyErr_SetString(PyExc_ValueError, "null address"), nullptr);
+    }
+    std::memcpy(&layer, p, sizeof layer);
+    Py_RETURN_NONE;
+}
+
 // connect(addresses): the C-ABI functions in the order of Abi, without or with the last two
 PyObject* connect(PyObject*, PyObject* const* v, Py_ssize_t n)
 {
@@ -387,7 +660,9 @@ template <PyObject* (*f)(PyObject*, PyObject* const*, Py_ssize_t)> PyObject* gua
 
 #define TRIINV_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<f>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {TRIINV_METHOD(connect), TRIINV_METHOD(tri_inv), TRIINV_METHOD(gdn_inv), TRIINV_METHOD(gdn_solve),
-                         TRIINV_METHOD(gdn_inv_varlen), TRIINV_METHOD(gdn_solve_varlen), {nullptr, nullptr, 0, nullptr}};
+                         TRIINV_METHOD(gdn_inv_varlen), TRIINV_METHOD(gdn_solve_varlen),
+                         TRIINV_METHOD(connect_layer), TRIINV_METHOD(chunk_attn), TRIINV_METHOD(chunk_attn_varlen), TRIINV_METHOD(chunk_attn_bwd),
+                         TRIINV_METHOD(chunk_attn_bwd_varlen), TRIINV_METHOD(step), TRIINV_METHOD(norm), TRIINV_METHOD(norm_bwd), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -33,6 +33,28 @@ def _on(stream):
     return torch.cuda.stream(stream) if isinstance(stream, torch.cuda.Stream) else _NOWHERE
 
 
+_connected = None  # the native argument handling that knows these entry points
+
+
+def _fast(t: torch.Tensor, stream):
+    """(native argument handling, device, stream) for a plain call on the current stream, or None (see binding.py)."""
+    if binding._lib is not binding._fast_lib or stream is not None or not t.is_cuda:
+        return None
+    if binding._fast is not _connected:
+        _connect()
+    dev = binding._device_index()
+    return binding._fast, dev, binding._raw_stream(dev)
+
+
+def _connect() -> None:
+    global _connected
+    L = binding.lib()
+    binding._fast.connect_layer(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+        L.gdn_chunk_attn, L.gdn_chunk_attn_varlen, L.gdn_chunk_attn_workspace, L.gdn_chunk_attn_bwd, L.gdn_chunk_attn_bwd_varlen,
+        L.gdn_chunk_attn_bwd_workspace, L.gdn_step, L.add_rms_norm, L.add_rms_norm_bwd)))
+    _connected = binding._fast
+
+
 class _Nothing:
     def __enter__(self):
         return self
@@ -70,6 +92,11 @@ def gdn_chunk_attn(Q: torch.Tensor, K: torch.Tensor, U: torch.Tensor, g: Optiona
     """(O, final_state) of linear attention with one decay per head, chunk by chunk: Q, K [B, Tlen, H_k, d_k], U [B, Tlen, H, d_v], g the
     chunk-local cumulative log-decay [B, Tlen, H] or None.  With W [B, Tlen, H, d_k] the gated delta rule: U and W as gdn_chunk_tri_solve_multi
     gives them.  state: [B, H, d_k, d_v] fp32, the state before the first token (None: zeros).  scale: d_k ** -0.5 by default."""
+    f = _fast(Q, stream)
+    if f:
+        r = f[0].chunk_attn(f[1], f[2], Q, K, U, g, C, W, state, scale, O, final_state)
+        if r is not None:
+            return r
     B, T = Q.shape[:2]
     H, H_k, d_k, d_v = _attn_checked(Q, K, U, g, W, state, (B, T), B)
     _has(O, "O", U.shape, U.dtype)
@@ -91,6 +118,11 @@ def gdn_chunk_attn_varlen(Q: torch.Tensor, K: torch.Tensor, U: torch.Tensor, g: 
                           O: Optional[torch.Tensor] = None, final_state: Optional[torch.Tensor] = None, stream=None):
     """gdn_chunk_attn on packed sequences: Q, K [total, H_k, d_k], U [total, H, d_v], W [total, H, d_k], g [total, H]; seqlens = host sequence of
     lengths; states [len(seqlens), H, d_k, d_v]."""
+    f = _fast(Q, stream)
+    if f:
+        r = f[0].chunk_attn_varlen(f[1], f[2], Q, K, U, g, seqlens, C, W, state, scale, O, final_state)
+        if r is not None:
+            return r
     total = Q.shape[0]
     seqlens = seqlens if isinstance(seqlens, (list, tuple)) else list(seqlens)
     n_seq = len(seqlens)
@@ -137,6 +169,11 @@ def gdn_chunk_attn_bwd(Q: torch.Tensor, K: torch.Tensor, U: torch.Tensor, g: Opt
                        state: Optional[torch.Tensor] = None, dstate: Optional[torch.Tensor] = None, scale: Optional[float] = None, stream=None):
     """(dQ, dK, dU, dW, dg, dstate0) of gdn_chunk_attn, from its inputs and the gradients dO of O and dstate (or None) of final_state; None in the
     place of the gradient of what was not given."""
+    f = _fast(Q, stream)
+    if f:
+        r = f[0].chunk_attn_bwd(f[1], f[2], Q, K, U, g, dO, C, W, state, dstate, scale)
+        if r is not None:
+            return r
     B, T = Q.shape[:2]
     return _attn_bwd("gdn_chunk_attn_bwd", Q, K, U, g, dO, C, W, state, dstate, scale, stream, (B, T), B, B * T, B * ((T + C - 1) // C) if C > 0 else 0, (B, T))
 
@@ -145,6 +182,11 @@ def gdn_chunk_attn_bwd_varlen(Q: torch.Tensor, K: torch.Tensor, U: torch.Tensor,
                               W: Optional[torch.Tensor] = None, state: Optional[torch.Tensor] = None, dstate: Optional[torch.Tensor] = None,
                               scale: Optional[float] = None, stream=None):
     """gdn_chunk_attn_bwd on packed sequences (see gdn_chunk_attn_varlen)."""
+    f = _fast(Q, stream)
+    if f:
+        r = f[0].chunk_attn_bwd_varlen(f[1], f[2], Q, K, U, g, dO, seqlens, C, W, state, dstate, scale)
+        if r is not None:
+            return r
     total = Q.shape[0]
     cu_s, cu_c, n_seq, n_chunk, keep = _chunk_offsets(Q, seqlens if isinstance(seqlens, (list, tuple)) else list(seqlens), C, stream)
     got = _attn_bwd("gdn_chunk_attn_bwd_varlen", Q, K, U, g, dO, C, W, state, dstate, scale, stream, (total,), n_seq, total, n_chunk,
@@ -157,6 +199,11 @@ def gdn_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, g: Optional[torc
              slots: Optional[torch.Tensor] = None, scale: Optional[float] = None, o: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """One token of the layer: q, k [B, H_k, d_k], v [B, H, d_v], g [B, H] the token's log-decay or None; state [n_slot, H, d_k, d_v] fp32 is
     updated in place.  beta [B, H]: the delta rule.  slots [B] int32: each sequence's place in state (outside of it: padding)."""
+    f = _fast(q, stream)
+    if f:
+        r = f[0].step(f[1], f[2], q, k, v, g, state, beta, slots, scale, o)
+        if r is not None:
+            return r
     B, H_k, d_k = q.shape
     H, d_v = v.shape[1:]
     _has(k, "k", q.shape, q.dtype)
@@ -192,6 +239,11 @@ def _norm(x, weight, residual, eps, group, y, scales, stream):
 
 def add_rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6, stream=None):
     """(y, s): s = x + residual in x's type (x itself without one), y = s / sqrt(mean(s^2) + eps) * weight over the last dimension."""
+    f = _fast(x, stream)
+    if f:
+        r = f[0].norm(f[1], f[2], x, weight, residual, eps, -1)
+        if r is not None:
+            return r
     with _on(stream):
         y = torch.empty_like(x)
     return y, _norm(x, weight, residual, eps, -1, y, None, stream)
@@ -200,6 +252,11 @@ def add_rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch
 def add_rms_norm_fp8(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6, group: int = 0, stream=None):
     """(y, scales, s): as add_rms_norm with y / scale in torch.float8_e4m3fn; scales fp32, one a row [...] (group = 0) or one for every 128
     columns [..., D / 128] (group = 128)."""
+    f = _fast(x, stream) if group >= 0 else None
+    if f:
+        r = f[0].norm(f[1], f[2], x, weight, residual, eps, group)
+        if r is not None:
+            return r
     with _on(stream):
         y = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device)
         # (one a row: a trailing dimension of one group)
@@ -209,6 +266,11 @@ def add_rms_norm_fp8(x: torch.Tensor, weight: torch.Tensor, residual: Optional[t
 
 def add_rms_norm_bwd(dy: torch.Tensor, s: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6, dsum: Optional[torch.Tensor] = None, stream=None):
     """(dx, dweight) of add_rms_norm: s as it returned it, dsum the gradient that arrives at s itself; dx is that of x and of the residual, dweight fp32."""
+    f = _fast(s, stream)
+    if f:
+        r = f[0].norm_bwd(f[1], f[2], dy, s, weight, eps, dsum)
+        if r is not None:
+            return r
     D = s.shape[-1]
     N = s.numel() // D if D else 0
     _has(dy, "dy", s.shape, s.dtype)
