@@ -30,14 +30,15 @@ template <int MT, int KP, bool DELTA, bool TWO> int go(const AttnCall& c)
     const AttnArgs a = args_of(c);
     const unsigned heads = (unsigned)(c.n_seq * c.H), groups = (unsigned)((c.d_v + ATTN_COLS - 1) / ATTN_COLS);
     if (c.n_seg > 1) {
-        const unsigned more = DELTA ? (unsigned)((c.d_k + ATTN_COLS - 1) / ATTN_COLS) : 0u;
-        int rc = launch_kernel(false, k_chunk_attn<OP, MT, KP, DELTA, ATTN_SEGMENT, TWO>, dim3(heads * (groups + more), (unsigned)c.n_seg - 1), dim3(512), 0, c.stream, a);
+        const auto by = [&](unsigned cols) { return dim3(heads * ((c.d_v + cols - 1) / cols + (DELTA ? (c.d_k + cols - 1) / cols : 0)), (unsigned)c.n_seg - 1); };
+        int rc = c.d_v > 64 ? launch_kernel(false, k_attn_states<OP, MT, KP, DELTA, ATTN_SEGMENT, TWO, 8>, by(128), dim3(512), 0, c.stream, a)
+                            : launch_kernel(false, k_attn_states<OP, MT, KP, DELTA, ATTN_SEGMENT, TWO, 4>, by(64), dim3(256), 0, c.stream, a);
         if (rc != LAUNCHED) return rc;
         rc = DELTA ? launch_kernel(false, k_attn_join<KP>, dim3(heads * ((c.d_v + 15) / 16)), dim3(256), 0, c.stream, a)
                    : launch_kernel(false, k_attn_join_plain, dim3((unsigned)(((int64_t)heads * c.d_k * c.d_v + 255) / 256)), dim3(256), 0, c.stream, a);
         if (rc != LAUNCHED) return rc;
     }
-    return launch_kernel(false, k_chunk_attn<OP, MT, KP, DELTA, ATTN_OUT, TWO>, dim3(heads * groups, (unsigned)c.n_seg), dim3(512), 0, c.stream, a);
+    return launch_kernel(false, k_chunk_attn<OP, MT, KP, DELTA, TWO>, dim3(heads * groups, (unsigned)c.n_seg), dim3(512), 0, c.stream, a);
 }
 template <int MT, bool DELTA, bool TWO> int go_k(const AttnCall& c) { return c.d_k <= 64 ? go<MT, 2, DELTA, TWO>(c) : go<MT, 4, DELTA, TWO>(c); }
 template <int MT, bool TWO> int go_delta(const AttnCall& c) { return c.W ? go_k<MT, true, TWO>(c) : go_k<MT, false, false>(c); }

@@ -102,6 +102,59 @@ __device__ __forceinline__ void add_turned(v4f (&S)[2 * KP], const char* rows, c
     }
 }
 
+// v = X S (tokens x columns), sp the parts of S: rows of X, the next pair's requested before one is used.
+template <int OP, int MT, int KP> __device__ __forceinline__ void rows_times(v4f (&v)[MT], const char* rows, const Parts<FULL_PARTS<OP>> (&sp)[KP], Lane ln)
+{
+    v4u w[2][MT];
+    auto rows_of = [&](int p) {
+#pragma unroll
+        for (int tb = 0; tb < MT; ++tb) w[p & 1][tb] = lds_row<4 * KP>(rows, 16 * tb + ln.n, 4 * p + ln.q);
+    };
+    rows_of(0);
+#pragma unroll
+    for (int tb = 0; tb < MT; ++tb) v[tb] = zero4();
+#pragma unroll
+    for (int p = 0; p < KP; ++p) {
+        if (p + 1 < KP) rows_of(p + 1);
+        in_order();
+#pragma unroll
+        for (int part = FULL_PARTS<OP> - 1; part >= 0; --part)
+#pragma unroll
+            for (int tb = 0; tb < MT; ++tb) v[tb] = mfma32<OP>(w[p & 1][tb], sp[p].u[part], v[tb]);
+    }
+}
+// V' = U - W S of 16 columns from LDS; v holds W S 2^shift (DELTA).
+template <int OP, int MT, int UPIECES, bool DELTA> __device__ __forceinline__ void values_of(v4f (&v)[MT], const v2u (&u)[MT], int shift)
+{
+    const float down = OP == OP_F16 ? pow2(-shift) : 1.f;
+#pragma unroll
+    for (int tb = 0; tb < MT; ++tb) {
+        const v4f x = unpack4<OP>(u[tb]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[tb][r] = DELTA ? x[r] - (OP == OP_F16 ? v[tb][r] * down : v[tb][r]) : x[r];
+    }
+}
+// S <- decay S + K^T diag(e) V'; v is used up.
+template <int OP, int MT, int KP> __device__ __forceinline__ void state_after(v4f (&S)[2 * KP], v4f (&v)[MT], int shift, const char* rows_k, const float* e, float decay, const MinusOne<OP>& minus, Lane ln)
+{
+    const float up = OP == OP_F16 ? pow2(shift) : 1.f;
+    Parts<FULL_PARTS<OP>> vp[MT / 2];
+#pragma unroll
+    for (int tb = 0; tb < MT; ++tb) {
+        const v4f x = *reinterpret_cast<const v4f*>(e + 16 * tb + 4 * ln.q);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[tb][r] *= OP == OP_F16 ? x[r] * up : x[r];
+    }
+    split_pairs<OP, FULL_PARTS<OP>, MT / 2>(v, vp, minus);
+#pragma unroll
+    for (int i = 0; i < 2 * KP; ++i) S[i] = times(S[i], decay * up);
+    add_turned<OP, MT, KP>(S, rows_k, vp, ln);
+    if constexpr (OP == OP_F16) {
+#pragma unroll
+        for (int i = 0; i < 2 * KP; ++i) S[i] = times(S[i], pow2(-shift));
+    }
+}
+
 // A step's tokens: what of them there is, and their gates.
 struct StepPos {
     int64_t row;  // of its first token
@@ -142,27 +195,22 @@ template <int R> struct StepGates {
 };
 
 // MT tiles of 16 token rows a step, KP pairs of tiles of 16 channels; 64 columns, four wavefronts of 16.
-// ATTN_OUT: the outputs and the final state.  ATTN_SEGMENT: what a segment adds to a state (column groups of d_v) and, with W, what it does to
-// the one before it: the same recursion from the identity with U = 0 (column groups of d_k behind them).  ATTN_RECORD: the states before
-// the steps and the values, for the gradient.
-enum : int { ATTN_OUT = 0, ATTN_SEGMENT = 1, ATTN_RECORD = 2 };
 constexpr int ATTN_COLS = 64;
-template <int OP, int MT, int KP, bool DELTA, int MODE> struct AttnLayout {
-    static constexpr bool OUT = MODE == ATTN_OUT;
+template <int OP, int MT, int KP, bool DELTA> struct AttnLayout {
     static constexpr int R = 16 * MT, PIECES = 4 * KP, UPIECES = ATTN_COLS / 8;
     static constexpr int ROWS = R * PIECES * 16, U_BYTES = R * UPIECES * 16;
     static constexpr int K_AT = 0;  // twice: the second half of a step reads it while the next is brought
-    static constexpr int W_AT = 2 * ROWS, Q_AT = W_AT + (DELTA ? ROWS : 0), U_AT = Q_AT + (OUT ? ROWS : 0);
+    static constexpr int W_AT = 2 * ROWS, Q_AT = W_AT + (DELTA ? ROWS : 0), U_AT = Q_AT + ROWS;
     static constexpr int S_AT = U_AT + U_BYTES, S_WAVE = KP * 2048;  // two parts of S, a wavefront's columns one after the other
-    static constexpr int V_AT = S_AT + (OUT ? 4 * S_WAVE : 0), V_WAVE = MT * 1024;  // of V', twice
-    static constexpr int G_AT = V_AT + (OUT ? 8 * V_WAVE : 0), SHIFT_AT = G_AT + 2 * StepGates<R>::FLOATS * 4, BYTES = SHIFT_AT + 64;
+    static constexpr int V_AT = S_AT + 4 * S_WAVE, V_WAVE = MT * 1024;  // of V', twice
+    static constexpr int G_AT = V_AT + 8 * V_WAVE, SHIFT_AT = G_AT + 2 * StepGates<R>::FLOATS * 4, BYTES = SHIFT_AT + 64;
 };
 
-template <int OP, int MT, int KP, bool DELTA, int MODE, bool TWO>
+// Outputs and the final state.
+template <int OP, int MT, int KP, bool DELTA, bool TWO>
 __global__ __launch_bounds__(512) void k_chunk_attn(AttnArgs a)
 {
-    typedef AttnLayout<OP, MT, KP, DELTA, MODE> LY;
-    constexpr bool OUT = LY::OUT, SEGMENT = MODE == ATTN_SEGMENT;
+    typedef AttnLayout<OP, MT, KP, DELTA> LY;
     constexpr int R = LY::R, FP = FULL_PARTS<OP>, PIECES = LY::PIECES;
     __shared__ __attribute__((aligned(16))) char lds[LY::BYTES];
     float* const gates = reinterpret_cast<float*>(lds + LY::G_AT);
@@ -170,14 +218,12 @@ __global__ __launch_bounds__(512) void k_chunk_attn(AttnArgs a)
     const Lane ln = lane_id();
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane16 = 16 * (16 * ln.q + ln.n);
 
-    const unsigned groups_v = (a.d_v + ATTN_COLS - 1) / ATTN_COLS, groups = groups_v + (SEGMENT && DELTA ? (a.d_k + ATTN_COLS - 1) / ATTN_COLS : 0);
+    const unsigned groups = (a.d_v + ATTN_COLS - 1) / ATTN_COLS;
     const unsigned b = xcd_neighbours(blockIdx.x, gridDim.x);
     const unsigned cg = b % groups, hs = b / groups;
     const int seg = blockIdx.y;
     const int h = hs % a.H, s = hs / a.H;
-    const bool trans = SEGMENT && cg >= groups_v;
-    const int d_v = trans ? a.d_k : a.d_v;
-    const int wg_col = (trans ? cg - groups_v : cg) * ATTN_COLS;
+    const int wg_col = cg * ATTN_COLS;
     const SeqPos sq = seq_pos(a.map, s);
     const int64_t n_chunk = (sq.len + a.C - 1) / a.C;
     int64_t c0, c1;
@@ -190,14 +236,12 @@ __global__ __launch_bounds__(512) void k_chunk_attn(AttnArgs a)
         const int col0 = wg_col + 16 * wave;
         const MinusOne<OP> minus(ln);
         v4f S[2 * KP];
-        const float* from = !SEGMENT ? (seg == 0 ? a.state : a.seg_state + (int64_t)(seg - 1) * a.map.n_seq * a.H * a.d_k * a.d_v) : nullptr;
-        get_state<KP>(from ? from + (int64_t)hs * a.d_k * a.d_v : nullptr, S, a.d_k, d_v, col0, trans, ln);
+        const float* from = seg == 0 ? a.state : a.seg_state + (int64_t)(seg - 1) * a.map.n_seq * a.H * a.d_k * a.d_v;
+        get_state<KP>(from ? from + (int64_t)hs * a.d_k * a.d_v : nullptr, S, a.d_k, a.d_v, col0, false, ln);
         Parts<FP> sp[KP];
         int s_shift = 0;
-        const int64_t rec0 = MODE == ATTN_RECORD ? (a.map.cu_chunks ? a.map.cu_chunks[s] : s * n_chunk) * steps : 0;
         // The parts of S: of the state before a chunk for W, two of them for Q in every step.
         auto parts_of_state = [&](bool first) {
-            if (!OUT && !DELTA) return;
             float up = 1.f;
             int shift = 0;
             if constexpr (OP == OP_F16) shift = f16_shift(wave_max(most_of(S))), up = pow2(shift);
@@ -208,104 +252,48 @@ __global__ __launch_bounds__(512) void k_chunk_attn(AttnArgs a)
             split_pairs<OP, DELTA ? FP : 2, KP>(x, t, minus);
 #pragma unroll
             for (int p = 0; p < KP; ++p) {
-                if constexpr (OUT) {
-                    char* const to = lds + LY::S_AT + LY::S_WAVE * wave + 2048 * p + lane16;
-                    *reinterpret_cast<v4u*>(to) = t[p].u[0];
-                    *reinterpret_cast<v4u*>(to + 1024) = t[p].u[1];
-                }
+                char* const to = lds + LY::S_AT + LY::S_WAVE * wave + 2048 * p + lane16;
+                *reinterpret_cast<v4u*>(to) = t[p].u[0];
+                *reinterpret_cast<v4u*>(to + 1024) = t[p].u[1];
                 if constexpr (DELTA) {
                     if (!TWO || first) sp[p] = t[p];
                 }
             }
             if (!TWO || first) s_shift = shift;
-            if (OUT && OP == OP_F16 && ln.q == 0 && ln.n == 0) shifts[wave] = shift;
+            if (OP == OP_F16 && ln.q == 0 && ln.n == 0) shifts[wave] = shift;
         };
         parts_of_state(true);
         __syncthreads();  // the first rows are in LDS
         for (int64_t k = k0; k < k1; ++k) {
             const float* const gl = gates + (k & 1) * StepGates<R>::FLOATS;
-            const char* const rows_k = lds + LY::K_AT + (k & 1) * LY::ROWS;
-            if constexpr (MODE == ATTN_RECORD) put_state<KP>(a.rec_state + ((rec0 + k) * a.H + h) * a.d_k * a.d_v, S, a.d_k, a.d_v, col0, ln);
             v4f v[MT];
             v2u u[MT];
-            const float down = OP == OP_F16 ? pow2(-s_shift) : 1.f;
 #pragma unroll
-            for (int tb = 0; tb < MT; ++tb) v[tb] = zero4(), u[tb] = lds_turned<LY::UPIECES>(lds + LY::U_AT, 16 * tb + 4 * ln.q + (ln.n >> 2), 4 * wave + (ln.n & 3));
-            if constexpr (DELTA) {
-                v4u w[2][MT];
-                auto rows_of = [&](int p) {
-#pragma unroll
-                    for (int tb = 0; tb < MT; ++tb) w[p & 1][tb] = lds_row<PIECES>(lds + LY::W_AT, 16 * tb + ln.n, 4 * p + ln.q);
-                };
-                rows_of(0);
-#pragma unroll
-                for (int p = 0; p < KP; ++p) {
-                    if (p + 1 < KP) rows_of(p + 1);
-                    in_order();
-#pragma unroll
-                    for (int part = FP - 1; part >= 0; --part)
-#pragma unroll
-                        for (int tb = 0; tb < MT; ++tb) v[tb] = mfma32<OP>(w[p & 1][tb], sp[p].u[part], v[tb]);
-                }
-            }
+            for (int tb = 0; tb < MT; ++tb) u[tb] = lds_turned<LY::UPIECES>(lds + LY::U_AT, 16 * tb + 4 * ln.q + (ln.n >> 2), 4 * wave + (ln.n & 3));
+            if constexpr (DELTA) rows_times<OP, MT, KP>(v, lds + LY::W_AT, sp, ln);
             __syncthreads();  // W, U, Q and the parts of S are in registers
-#pragma unroll
-            for (int tb = 0; tb < MT; ++tb) {
-                const v4f x = unpack4<OP>(u[tb]);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) v[tb][r] = DELTA ? x[r] - (OP == OP_F16 ? v[tb][r] * down : v[tb][r]) : x[r];
-            }
+            values_of<OP, MT, LY::UPIECES, DELTA>(v, u, s_shift);
             int v_shift = 0;
             if constexpr (OP == OP_F16) v_shift = f16_shift(wave_max(most_of(v)));
-            const float up = OP == OP_F16 ? pow2(v_shift) : 1.f;
-            if constexpr (OUT) {
+            {
                 if (OP == OP_F16 && ln.q == 0 && ln.n == 0) shifts[4 + 4 * (k & 1) + wave] = v_shift;
                 v4f x[MT];
 #pragma unroll
-                for (int tb = 0; tb < MT; ++tb) x[tb] = OP == OP_F16 ? times(v[tb], up) : v[tb];
+                for (int tb = 0; tb < MT; ++tb) x[tb] = OP == OP_F16 ? times(v[tb], pow2(v_shift)) : v[tb];
                 Parts<2> t[MT / 2];
                 split_pairs<OP, 2, MT / 2>(x, t, minus);
 #pragma unroll
                 for (int tp = 0; tp < MT / 2; ++tp) {
-                    char* to = lds + LY::V_AT + LY::V_WAVE * (4 * (k & 1) + wave) + 2048 * tp + lane16;
+                    char* const to = lds + LY::V_AT + LY::V_WAVE * (4 * (k & 1) + wave) + 2048 * tp + lane16;
                     *reinterpret_cast<v4u*>(to) = t[tp].u[0];
                     *reinterpret_cast<v4u*>(to + 1024) = t[tp].u[1];
                 }
             }
-            if constexpr (MODE == ATTN_RECORD && DELTA) {
-                const StepPos at = step_pos<R>(sq, k, k1, a.C);
-                const uint32_t stride = 4u * a.H * a.d_v;
-                const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(a.rec_value + (at.row * a.H + h) * a.d_v, 0, (uint32_t)(at.valid - 1) * stride + 4u * a.d_v, 0x00020000);
-                uint32_t to = col0 + ln.n < a.d_v ? 4 * ln.q * stride + 4u * (col0 + ln.n) : 0x80000000u;
-#pragma unroll
-                for (int tb = 0; tb < MT; ++tb, to += 12 * stride)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r, to += stride) __builtin_amdgcn_raw_buffer_store_b32(bits(v[tb][r]), rsrc, to, 0, 0);
-            }
-            Parts<FP> vp[MT / 2];
-#pragma unroll
-            for (int tb = 0; tb < MT; ++tb) {
-                const v4f e = *reinterpret_cast<const v4f*>(gl + R + 16 * tb + 4 * ln.q);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) v[tb][r] *= OP == OP_F16 ? e[r] * up : e[r];
-            }
-            split_pairs<OP, FP, MT / 2>(v, vp, minus);
-            const float decay = gl[3 * R];
-#pragma unroll
-            for (int i = 0; i < 2 * KP; ++i) S[i] = times(S[i], decay * up);
-            add_turned<OP, MT, KP>(S, rows_k, vp, ln);
-            if constexpr (OP == OP_F16) {
-#pragma unroll
-                for (int i = 0; i < 2 * KP; ++i) S[i] = times(S[i], pow2(-v_shift));
-            }
+            state_after<OP, MT, KP>(S, v, v_shift, lds + LY::K_AT + (k & 1) * LY::ROWS, gl + R, gl[3 * R], minus, ln);
             parts_of_state(((k + 1) & 1) == 0);
             __syncthreads();  // the parts of S and the next rows are in LDS
         }
-        if (!SEGMENT && seg != a.n_seg - 1) return;
-        float* to = !SEGMENT ? a.final_state : trans ? a.seg_trans : a.seg_state;
-        if (!to) return;
-        if (SEGMENT) to += (int64_t)seg * a.map.n_seq * a.H * a.d_k * d_v;
-        put_state<KP>(to + (int64_t)hs * a.d_k * d_v, S, a.d_k, d_v, col0, ln);
+        if (seg == a.n_seg - 1 && a.final_state) put_state<KP>(a.final_state + (int64_t)hs * a.d_k * a.d_v, S, a.d_k, a.d_v, col0, ln);
         return;
     }
 
@@ -320,24 +308,23 @@ __global__ __launch_bounds__(512) void k_chunk_attn(AttnArgs a)
     const uint32_t stride_k = 2u * H_k * a.d_k, stride_w = 2u * a.H * a.d_k, stride_u = 2u * a.H * a.d_v;
     const int64_t row0 = sq.tok0 + k0 * tokens;
     const char *at_k = static_cast<const char*>(a.K) + row0 * stride_k + 2 * hk * a.d_k, *at_q = static_cast<const char*>(a.Q) + row0 * stride_k + 2 * hk * a.d_k,
-               *at_w = static_cast<const char*>(a.W) + row0 * stride_w + 2 * h * a.d_k, *at_u = static_cast<const char*>(a.U) + row0 * stride_u + 2 * (h * a.d_v + (trans ? 0 : wg_col));
+               *at_w = static_cast<const char*>(a.W) + row0 * stride_w + 2 * h * a.d_k, *at_u = static_cast<const char*>(a.U) + row0 * stride_u + 2 * (h * a.d_v + wg_col);
     auto request = [&](int64_t k) {
         const StepPos at = step_pos<R>(sq, k, k1, a.C);
         lk.load(at_k, stride_k, a.d_k, at.valid, tid);
         if constexpr (DELTA) lw.load(at_w, stride_w, a.d_k, at.valid, tid);
-        lu.load(at_u, stride_u, cols, trans ? 0 : at.valid, tid);
-        if constexpr (OUT) lq.load(at_q, stride_k, a.d_k, at.valid, tid);
+        lu.load(at_u, stride_u, cols, at.valid, tid);
+        lq.load(at_q, stride_k, a.d_k, at.valid, tid);
         lg.load(a.g, at, a.H, h, tid);
         at_k += (int64_t)tokens * stride_k, at_q += (int64_t)tokens * stride_k, at_w += (int64_t)tokens * stride_w, at_u += (int64_t)tokens * stride_u;
     };
     auto bring = [&](int64_t k) {
         lk.store(lds + LY::K_AT + (k & 1) * LY::ROWS, tid);
         if constexpr (DELTA) lw.store(lds + LY::W_AT, tid);
-        if constexpr (OUT) lq.store(lds + LY::Q_AT, tid);
+        lq.store(lds + LY::Q_AT, tid);
         lu.store(lds + LY::U_AT, tid);
         lg.store(gates + (k & 1) * StepGates<R>::FLOATS, a.scale, tid);
     };
-    float total = 0.f;
     request(k0);
     bring(k0);
     request(k0 + 1);
@@ -398,7 +385,7 @@ __global__ __launch_bounds__(512) void k_chunk_attn(AttnArgs a)
         const float* const gl = gates + (k & 1) * StepGates<R>::FLOATS;
         const char* const rows_k = lds + LY::K_AT + (k & 1) * LY::ROWS;
         v4u q[NI][KP];
-        if constexpr (OUT) {
+        {
             if (k > k0) finish(k - 1);
             v4u sf[2][2][2];
             auto parts_of = [&](int p) {
@@ -432,12 +419,11 @@ __global__ __launch_bounds__(512) void k_chunk_attn(AttnArgs a)
                 for (int ii = 0; ii < NI; ++ii) acc[ii][t] = times(acc[ii][t], gl[2 * R + 16 * (ii == 0 ? half : 3 - half) + ln.n] * down);
             }
         }
-        if (SEGMENT && !DELTA && cg == 0 && tid == 0) total += gl[3 * R + 1];
         __syncthreads();  // W, U, Q and the parts of S are in registers
         bring(k + 1);
         request(k + 2);
         in_order();
-        if constexpr (OUT) {
+        {
             v4u kf[2][2 * NI];
             v4f x[NI][2 * NI];  // scores, turned: x[ii][jt], jt <= 2 ii + 1
             auto keys_of = [&](int p) {
@@ -479,10 +465,119 @@ __global__ __launch_bounds__(512) void k_chunk_attn(AttnArgs a)
         }
         __syncthreads();
     }
-    if constexpr (OUT) {
-        if (k0 < k1) finish(k1 - 1);
+    if (k0 < k1) finish(k1 - 1);
+}
+
+// The recursion alone, 16 WAVES columns of a head, every wavefront with a share of the rows to bring.  ATTN_SEGMENT: what a segment adds to a state (column groups
+// of d_v) and, with W, what it does to the one before it: the same recursion from the identity with U = 0 (column groups of d_k behind them).
+// ATTN_RECORD: the states before the steps and the values, for the gradient.
+enum : int { ATTN_SEGMENT = 1, ATTN_RECORD = 2 };
+template <int OP, int MT, int KP, bool DELTA, int WAVES> struct StatesLayout {
+    static constexpr int R = 16 * MT, PIECES = 4 * KP, COLS = 16 * WAVES, UPIECES = COLS / 8, ROWS = R * PIECES * 16;
+    static constexpr int K_AT = 0, W_AT = 2 * ROWS, U_AT = W_AT + (DELTA ? ROWS : 0), G_AT = U_AT + R * UPIECES * 16, BYTES = G_AT + 2 * StepGates<R>::FLOATS * 4;
+};
+
+template <int OP, int MT, int KP, bool DELTA, int MODE, bool TWO, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void k_attn_states(AttnArgs a)
+{
+    typedef StatesLayout<OP, MT, KP, DELTA, WAVES> LY;
+    constexpr bool SEGMENT = MODE == ATTN_SEGMENT;
+    constexpr int R = LY::R, FP = FULL_PARTS<OP>, THREADS = 64 * WAVES;
+    __shared__ __attribute__((aligned(16))) char lds[LY::BYTES];
+    float* const gates = reinterpret_cast<float*>(lds + LY::G_AT);
+    const Lane ln = lane_id();
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+    const unsigned groups_v = (a.d_v + LY::COLS - 1) / LY::COLS, groups = groups_v + (SEGMENT && DELTA ? (a.d_k + LY::COLS - 1) / LY::COLS : 0);
+    const unsigned b = xcd_neighbours(blockIdx.x, gridDim.x);
+    const unsigned cg = b % groups, hs = b / groups;
+    const int seg = blockIdx.y;
+    const int h = hs % a.H, s = hs / a.H, hk = h / a.group, H_k = a.H / a.group;
+    const bool trans = SEGMENT && cg >= groups_v;
+    const int d_v = trans ? a.d_k : a.d_v, wg_col = (trans ? cg - groups_v : cg) * LY::COLS, col0 = wg_col + 16 * wave;
+    const SeqPos sq = seq_pos(a.map, s);
+    const int64_t n_chunk = (sq.len + a.C - 1) / a.C;
+    int64_t c0, c1;
+    segment_chunks(n_chunk, a.n_seg, seg, c0, c1);
+    const int tokens = a.C < R ? a.C : R, steps = a.C > R ? a.C / R : 1;
+    const int64_t all = (sq.len + tokens - 1) / tokens, k0 = c0 * steps, k1 = c1 * steps < all ? c1 * steps : all;
+    const int64_t rec0 = (!SEGMENT && a.map.cu_chunks ? a.map.cu_chunks[s] : s * n_chunk) * steps;
+
+    RowLoader<LY::PIECES, R, THREADS> lk, lw;
+    RowLoader<LY::UPIECES, R, THREADS> lu;
+    StepGates<R> lg;
+    const int cols = a.d_v - wg_col < LY::COLS ? a.d_v - wg_col : LY::COLS;
+    const uint32_t stride_k = 2u * H_k * a.d_k, stride_w = 2u * a.H * a.d_k, stride_u = 2u * a.H * a.d_v;
+    const int64_t row0 = sq.tok0 + k0 * tokens;
+    const char *at_k = static_cast<const char*>(a.K) + row0 * stride_k + 2 * hk * a.d_k, *at_w = static_cast<const char*>(a.W) + row0 * stride_w + 2 * h * a.d_k,
+               *at_u = static_cast<const char*>(a.U) + row0 * stride_u + 2 * (h * a.d_v + (trans ? 0 : wg_col));
+    auto request = [&](int64_t k) {
+        const StepPos at = step_pos<R>(sq, k, k1, a.C);
+        lk.load(at_k, stride_k, a.d_k, at.valid, tid);
+        if constexpr (DELTA) lw.load(at_w, stride_w, a.d_k, at.valid, tid);
+        lu.load(at_u, stride_u, cols, trans ? 0 : at.valid, tid);
+        lg.load(a.g, at, a.H, h, tid);
+        at_k += (int64_t)tokens * stride_k, at_w += (int64_t)tokens * stride_w, at_u += (int64_t)tokens * stride_u;
+    };
+    auto bring = [&](int64_t k) {
+        lk.store(lds + LY::K_AT + (k & 1) * LY::ROWS, tid);
+        if constexpr (DELTA) lw.store(lds + LY::W_AT, tid);
+        lu.store(lds + LY::U_AT, tid);
+        lg.store(gates + (k & 1) * StepGates<R>::FLOATS, a.scale, tid);
+    };
+    request(k0);
+    bring(k0);
+    request(k0 + 1);
+    const MinusOne<OP> minus(ln);
+    v4f S[2 * KP];
+    const float* const from = SEGMENT || !a.state ? nullptr : a.state + (int64_t)hs * a.d_k * a.d_v;
+    get_state<KP>(from, S, a.d_k, d_v, col0, trans, ln);
+    Parts<FP> sp[KP];
+    int s_shift = 0;
+    auto parts_of_state = [&]() {
+        if constexpr (OP == OP_F16) s_shift = f16_shift(wave_max(most_of(S)));
+        v4f x[2 * KP];
+#pragma unroll
+        for (int i = 0; i < 2 * KP; ++i) x[i] = OP == OP_F16 ? times(S[i], pow2(s_shift)) : S[i];
+        split_pairs<OP, FP, KP>(x, sp, minus);
+    };
+    if constexpr (DELTA) parts_of_state();
+    float total = 0.f;
+    __syncthreads();
+    for (int64_t k = k0; k < k1; ++k) {
+        const float* const gl = gates + (k & 1) * StepGates<R>::FLOATS;
+        if constexpr (!SEGMENT) put_state<KP>(a.rec_state + ((rec0 + k) * a.H + h) * a.d_k * a.d_v, S, a.d_k, a.d_v, col0, ln);
+        v4f v[MT];
+        v2u u[MT];
+#pragma unroll
+        for (int tb = 0; tb < MT; ++tb) u[tb] = lds_turned<LY::UPIECES>(lds + LY::U_AT, 16 * tb + 4 * ln.q + (ln.n >> 2), 4 * wave + (ln.n & 3));
+        if constexpr (DELTA) rows_times<OP, MT, KP>(v, lds + LY::W_AT, sp, ln);
+        __syncthreads();  // W and U are in registers
+        bring(k + 1);
+        request(k + 2);
+        values_of<OP, MT, LY::UPIECES, DELTA>(v, u, s_shift);
+        if constexpr (!SEGMENT && DELTA) {
+            const StepPos at = step_pos<R>(sq, k, k1, a.C);
+            const uint32_t stride = 4u * a.H * a.d_v;
+            const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(a.rec_value + (at.row * a.H + h) * a.d_v, 0, (uint32_t)(at.valid - 1) * stride + 4u * a.d_v, 0x00020000);
+            uint32_t to = col0 + ln.n < a.d_v ? 4 * ln.q * stride + 4u * (col0 + ln.n) : 0x80000000u;
+#pragma unroll
+            for (int tb = 0; tb < MT; ++tb, to += 12 * stride)
+#pragma unroll
+                for (int r = 0; r < 4; ++r, to += stride) __builtin_amdgcn_raw_buffer_store_b32(bits(v[tb][r]), rsrc, to, 0, 0);
+        }
+        int v_shift = 0;
+        if constexpr (OP == OP_F16) v_shift = f16_shift(wave_max(most_of(v)));
+        if (SEGMENT && !DELTA) total += gl[3 * R + 1];
+        state_after<OP, MT, KP>(S, v, v_shift, lds + LY::K_AT + (k & 1) * LY::ROWS, gl + R, gl[3 * R], minus, ln);
+        if constexpr (DELTA) {
+            if (!TWO || ((k + 1) & 1) == 0) parts_of_state();
+        }
+        __syncthreads();  // the next rows are in LDS
     }
-    if (SEGMENT && !DELTA && cg == 0 && tid == 0) a.seg_decay[(int64_t)seg * a.map.n_seq * a.H + hs] = expf(total);
+    if constexpr (!SEGMENT) return;
+    put_state<KP>((trans ? a.seg_trans : a.seg_state) + ((int64_t)seg * a.map.n_seq * a.H + hs) * a.d_k * d_v, S, a.d_k, d_v, col0, ln);
+    if (!DELTA && cg == 0 && tid == 0) a.seg_decay[(int64_t)seg * a.map.n_seq * a.H + hs] = expf(total);
 }
 
 // States before the segments, in place of what the segments add: S <- M S + L from the sequence's initial state, segment by segment.  M and S as three
@@ -504,23 +599,28 @@ template <int KP> __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a)
     for (int t = 0; t < TI; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) S[t][r] = a.state && mine && at(t, r) < a.d_k ? a.state[((int64_t)hs * a.d_k + at(t, r)) * a.d_v + col] : 0.f;
-    for (int seg = 0; seg + 1 < a.n_seg; ++seg) {
-        float* const L = a.seg_state + (seg * heads + hs) * a.d_k * a.d_v;
-        const float* const M = a.seg_trans + (seg * heads + hs) * a.d_k * a.d_k;
-        v4f m[TI][KP][2], next[TI];
+    const MinusOne<OP_BF16> minus(ln);
+    v4f m[TI][2 * KP], add[TI];  // rows of M and L, of the segment behind the one at hand
+    auto request = [&](int seg) {
+        const bool there = seg + 1 < a.n_seg;
+        const float* const M = a.seg_trans + ((there ? seg : 0) * heads + hs) * a.d_k * a.d_k;
+        const float* const L = a.seg_state + ((there ? seg : 0) * heads + hs) * a.d_k * a.d_v;
 #pragma unroll
         for (int t = 0; t < TI; ++t) {
             const int row = state_channel(TI * wave + t, ln.n);
 #pragma unroll
-            for (int p = 0; p < KP; ++p) {
-                const bool there = row < a.d_k && 32 * p < a.d_k;
-                const float* x = M + (int64_t)row * a.d_k + 32 * p + 8 * ln.q;
-                m[t][p][0] = there ? *reinterpret_cast<const v4f*>(x) : zero4();
-                m[t][p][1] = there ? *reinterpret_cast<const v4f*>(x + 4) : zero4();
-            }
+            for (int i = 0; i < 2 * KP; ++i) m[t][i] = there && row < a.d_k && 16 * i < a.d_k ? *reinterpret_cast<const v4f*>(M + (int64_t)row * a.d_k + 32 * (i >> 1) + 8 * ln.q + 4 * (i & 1)) : zero4();
 #pragma unroll
-            for (int r = 0; r < 4; ++r) next[t][r] = mine && at(t, r) < a.d_k ? L[(int64_t)at(t, r) * a.d_v + col] : 0.f;
+            for (int r = 0; r < 4; ++r) add[t][r] = there && mine && at(t, r) < a.d_k ? L[(int64_t)at(t, r) * a.d_v + col] : 0.f;
         }
+    };
+    request(0);
+    for (int seg = 0; seg + 1 < a.n_seg; ++seg) {
+        Parts<3> mp[TI][KP];
+        v4f next[TI];
+#pragma unroll
+        for (int t = 0; t < TI; ++t) next[t] = add[t], split_pairs<OP_BF16, 3, KP>(m[t], mp[t], minus);
+        request(seg + 1);
         // this wavefront's parts of S: half a pair of tiles (KP = 2), or a whole one
         char* const buf = lds[seg & 1];
 #pragma unroll
@@ -535,28 +635,29 @@ template <int KP> __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a)
             }
         }
         __syncthreads();
+        v4f low[TI];  // half of the products, in chains of their own
+#pragma unroll
+        for (int t = 0; t < TI; ++t) low[t] = zero4();
 #pragma unroll
         for (int p = 0; p < KP; ++p) {
             v4u sp[3];
 #pragma unroll
             for (int part = 0; part < 3; ++part) sp[part] = *reinterpret_cast<const v4u*>(buf + (p * 3 + part) * 1024 + lane16);
 #pragma unroll
-            for (int t = 0; t < TI; ++t) {
-                const Parts<3> mp = split_pair<OP_BF16, 3>(m[t][p][0], m[t][p][1]);
-                next[t] = mfma32<OP_BF16>(mp.u[2], sp[0], next[t]);
-                next[t] = mfma32<OP_BF16>(mp.u[0], sp[2], next[t]);
-                next[t] = mfma32<OP_BF16>(mp.u[1], sp[1], next[t]);
-                next[t] = mfma32<OP_BF16>(mp.u[1], sp[0], next[t]);
-                next[t] = mfma32<OP_BF16>(mp.u[0], sp[1], next[t]);
-                next[t] = mfma32<OP_BF16>(mp.u[0], sp[0], next[t]);
+            for (int j = 0; j < 6; ++j) {
+                constexpr int of_m[6] = {2, 0, 1, 1, 0, 0}, of_s[6] = {0, 2, 1, 0, 1, 0};
+#pragma unroll
+                for (int t = 0; t < TI; ++t) (j & 1 ? next : low)[t] = mfma32<OP_BF16>(mp[t][p].u[of_m[j]], sp[of_s[j]], (j & 1 ? next : low)[t]);
             }
         }
+        float* const L = a.seg_state + (seg * heads + hs) * a.d_k * a.d_v;
 #pragma unroll
         for (int t = 0; t < TI; ++t) {
-            S[t] = next[t];
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
+            for (int r = 0; r < 4; ++r) {
+                S[t][r] = next[t][r] + low[t][r];
                 if (mine && at(t, r) < a.d_k) L[(int64_t)at(t, r) * a.d_v + col] = S[t][r];
+            }
         }
     }
 }

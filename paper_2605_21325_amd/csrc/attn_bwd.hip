@@ -27,7 +27,7 @@ template <int MT, int KP, bool DELTA, bool TWO> int go(const AttnBwdCall& c)
     a.rec_state = rec, a.rec_dstate = rec + states, a.rec_value = rec + 2 * states;
     a.map = f.map, a.H = c.H, a.group = f.group, a.d_k = c.d_k, a.d_v = c.d_v, a.C = c.C, a.scale = c.scale;
     if (c.n_chunk > 0) {
-        const int rc = launch_kernel(false, k_chunk_attn<OP, MT, KP, DELTA, ATTN_RECORD, TWO>, dim3(heads * groups), dim3(512), 0, c.stream, f);
+        const int rc = launch_kernel(false, k_attn_states<OP, MT, KP, DELTA, ATTN_RECORD, TWO, 4>, dim3(heads * groups), dim3(256), 0, c.stream, f);
         if (rc != LAUNCHED) return rc;
     }
     const int rc = launch_kernel(false, k_attn_bwd_state<OP, MT, KP, DELTA, TWO>, dim3(heads * groups), dim3(512), 0, c.stream, a);

@@ -7,7 +7,7 @@
 //     dQ  = scale diag(G) dO S^T + M K,   dK = diag(e) V' dS'^T + M^T Q
 //     dg_i = <q_i, dQ_i> - <k_i, dK_i>,   and at the chunk's last token + <S', dS'>,  S' = G_C S + K^T diag(e) V' the state after it.
 // In steps as there: inside a chunk of two, S and dS are those at the step's ends, W and dW go with the state before the chunk.
-// Three kernels: the states and values again, step after step (k_chunk_attn, ATTN_RECORD); dS, last step first, with dU (k_attn_bwd_state);
+// Three kernels: the states and values again, step after step (k_attn_states, ATTN_RECORD); dS, last step first, with dU (k_attn_bwd_state);
 // everything else, all steps at once (k_attn_bwd_chunk).  The first two are the walk of the forward pass, bound by the chain from chunk
 // to chunk; the states between them go through memory in fp32.  dg is the difference of large sums, so what enters it (dO S^T, V' dS'^T, M) is
 // formed from all 24 bits (fp16: 22) of its fp32 operands; what only ends in 16 bits (dW) from 16 of them.
@@ -103,7 +103,7 @@ __global__ __launch_bounds__(512) void k_attn_bwd_state(AttnBwdArgs a)
             v4f dv[MT];
 #pragma unroll
             for (int tb = 0; tb < MT; ++tb) dv[tb] = zero4();
-            {
+            {  // (rows_times with a barrier in it)
                 v4u w[2][MT];
                 auto rows_of = [&](int p) {
 #pragma unroll
