@@ -478,20 +478,17 @@ template <int OP, int MT, int KP, bool DELTA, int WAVES> struct StatesLayout {
 };
 
 template <int OP, int MT, int KP, bool DELTA, int MODE, bool TWO, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void k_attn_states(AttnArgs a)
+__device__ __forceinline__ void attn_states(const AttnArgs& a, char* const lds, unsigned b, int seg)
 {
     typedef StatesLayout<OP, MT, KP, DELTA, WAVES> LY;
     constexpr bool SEGMENT = MODE == ATTN_SEGMENT;
     constexpr int R = LY::R, FP = FULL_PARTS<OP>, THREADS = 64 * WAVES;
-    __shared__ __attribute__((aligned(16))) char lds[LY::BYTES];
     float* const gates = reinterpret_cast<float*>(lds + LY::G_AT);
     const Lane ln = lane_id();
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
     const unsigned groups_v = (a.d_v + LY::COLS - 1) / LY::COLS, groups = groups_v + (SEGMENT && DELTA ? (a.d_k + LY::COLS - 1) / LY::COLS : 0);
-    const unsigned b = xcd_neighbours(blockIdx.x, gridDim.x);
     const unsigned cg = b % groups, hs = b / groups;
-    const int seg = blockIdx.y;
     const int h = hs % a.H, s = hs / a.H, hk = h / a.group, H_k = a.H / a.group;
     const bool trans = SEGMENT && cg >= groups_v;
     const int d_v = trans ? a.d_k : a.d_v, wg_col = (trans ? cg - groups_v : cg) * LY::COLS, col0 = wg_col + 16 * wave;
@@ -578,6 +575,13 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_states(AttnArgs a)
     if constexpr (!SEGMENT) return;
     put_state<KP>((trans ? a.seg_trans : a.seg_state) + ((int64_t)seg * a.map.n_seq * a.H + hs) * a.d_k * d_v, S, a.d_k, d_v, col0, ln);
     if (!DELTA && cg == 0 && tid == 0) a.seg_decay[(int64_t)seg * a.map.n_seq * a.H + hs] = expf(total);
+}
+
+template <int OP, int MT, int KP, bool DELTA, int MODE, bool TWO, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void k_attn_states(AttnArgs a)
+{
+    __shared__ __attribute__((aligned(16))) char lds[StatesLayout<OP, MT, KP, DELTA, WAVES>::BYTES];
+    attn_states<OP, MT, KP, DELTA, MODE, TWO, WAVES>(a, lds, xcd_neighbours(blockIdx.x, gridDim.x), blockIdx.y);
 }
 
 // States before the segments, in place of what the segments add: S <- M S + L from the sequence's initial state, segment by segment.  M and S as three

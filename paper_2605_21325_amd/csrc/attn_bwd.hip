@@ -26,15 +26,11 @@ template <int MT, int KP, bool DELTA, bool TWO> int go(const AttnBwdCall& c)
     a.dQ = c.dQ, a.dK = c.dK, a.dU = c.dU, a.dW = c.dW, a.dg = c.dg, a.dstate0 = c.dstate0;
     a.rec_state = rec, a.rec_dstate = rec + states, a.rec_value = rec + 2 * states;
     a.map = f.map, a.H = c.H, a.group = f.group, a.d_k = c.d_k, a.d_v = c.d_v, a.C = c.C, a.scale = c.scale;
-    if (c.n_chunk > 0) {
-        const int rc = launch_kernel(false, k_attn_states<OP, MT, KP, DELTA, ATTN_RECORD, TWO, 4>, dim3(heads * groups), dim3(256), 0, c.stream, f);
-        if (rc != LAUNCHED) return rc;
-    }
-    const int rc = launch_kernel(false, k_attn_bwd_state<OP, MT, KP, DELTA, TWO>, dim3(heads * groups), dim3(512), 0, c.stream, a);
+    const int rc = launch_kernel(false, k_attn_bwd_walks<OP, MT, KP, DELTA, TWO>, dim3(2 * heads * groups), dim3(512), 0, c.stream, a, f);
     if (rc != LAUNCHED || c.n_chunk == 0) return rc;
     const dim3 grid((unsigned)(n_step * c.H_k));
-    return f.group > 1 ? launch_kernel(false, k_attn_bwd_chunk<OP, MT, KP / 2, DELTA, TWO, true>, grid, dim3(256), 0, c.stream, a)
-                       : launch_kernel(false, k_attn_bwd_chunk<OP, MT, KP / 2, DELTA, TWO, false>, grid, dim3(256), 0, c.stream, a);
+    return f.group > 1 ? launch_kernel(false, k_attn_bwd_chunk<OP, MT, KP, DELTA, TWO, true>, grid, dim3(128 * KP), 0, c.stream, a)
+                       : launch_kernel(false, k_attn_bwd_chunk<OP, MT, KP, DELTA, TWO, false>, grid, dim3(128 * KP), 0, c.stream, a);
 }
 template <int MT, bool DELTA, bool TWO> int go_k(const AttnBwdCall& c) { return c.d_k <= 64 ? go<MT, 2, DELTA, TWO>(c) : go<MT, 4, DELTA, TWO>(c); }
 template <int MT, bool TWO> int go_delta(const AttnBwdCall& c) { return c.W ? go_k<MT, true, TWO>(c) : go_k<MT, false, false>(c); }

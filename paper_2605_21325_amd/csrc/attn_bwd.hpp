@@ -55,16 +55,14 @@ template <class LY> __device__ __forceinline__ int unit_at(int jt)  // units_bef
 //     first part     K dS', dV'                                 rows of the step before to LDS | its P
 //     second part    dU, W^T dV', the new dS and its parts      P^T dO and Q^T dO of the step before
 template <int OP, int MT, int KP, bool DELTA, bool TWO>
-__global__ __launch_bounds__(512) void k_attn_bwd_state(AttnBwdArgs a)
+__device__ __forceinline__ void attn_bwd_state(const AttnBwdArgs& a, char* const lds, unsigned b)
 {
     typedef BwdStateLayout<OP, MT, KP, DELTA> LY;
     constexpr int R = LY::R, FP = FULL_PARTS<OP>, PIECES = LY::PIECES, TILES = MT * (MT + 1) / 2;
-    __shared__ __attribute__((aligned(16))) char lds[LY::BYTES];
     float* const gates = reinterpret_cast<float*>(lds + LY::G_AT);
     const Lane ln = lane_id();
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane16 = 16 * (16 * ln.q + ln.n);
     const unsigned groups = (a.d_v + ATTN_COLS - 1) / ATTN_COLS;
-    const unsigned b = xcd_neighbours(blockIdx.x, gridDim.x);
     const unsigned cg = b % groups, hs = b / groups;
     const int h = hs % a.H, s = hs / a.H, wg_col = cg * ATTN_COLS;
     const SeqPos sq = seq_pos(a.map, s);
@@ -306,11 +304,25 @@ __global__ __launch_bounds__(512) void k_attn_bwd_state(AttnBwdArgs a)
     }
 }
 
+// The two walks do not need each other: the first half of the grid takes dS, the longer one, the second half the states.
+template <int OP, int MT, int KP, bool DELTA, bool TWO>
+__global__ __launch_bounds__(512) void k_attn_bwd_walks(AttnBwdArgs a, AttnArgs f)
+{
+    constexpr int OF_STATES = StatesLayout<OP, MT, KP, DELTA, 4>::BYTES, OF_DS = BwdStateLayout<OP, MT, KP, DELTA>::BYTES;
+    __shared__ __attribute__((aligned(16))) char lds[OF_DS > OF_STATES ? OF_DS : OF_STATES];
+    const unsigned units = gridDim.x / 2;
+    if (blockIdx.x < units) {
+        attn_bwd_state<OP, MT, KP, DELTA, TWO>(a, lds, xcd_neighbours(blockIdx.x, units));
+    } else if (threadIdx.x < 256) {
+        attn_states<OP, MT, KP, DELTA, ATTN_RECORD, TWO, 4>(f, lds, xcd_neighbours(blockIdx.x - units, units), 0);
+    }
+}
+
 // Everything that needs the states at both ends of a step: a workgroup per step and key head, which takes the heads that share it one
 // after the other and d_v in blocks of 64 columns.  A wavefront has KT tiles of 16 channels of all tokens; the products stand turned
 // (channels down, tokens across), so that a lane's four values are neighbours in memory.  The next block's rows are requested before one is used.
-template <int OP, int MT, int KT, bool DELTA> struct BwdChunkLayout {
-    static constexpr int R = 16 * MT, PIECES = 8 * KT, CB = 8;  // CB: pieces of a block of d_v
+template <int OP, int MT, int KP, bool DELTA> struct BwdChunkLayout {
+    static constexpr int R = 16 * MT, PIECES = 4 * KP, WAVES = 2 * KP, CB = 8;  // CB: pieces of a block of d_v
     static constexpr int VP = DELTA ? FULL_PARTS<OP> : 1;
     static constexpr int ROWS = R * PIECES * 16, BLOCK = R * CB * 16;
     static constexpr int TILES = MT * (MT + 1) / 2, M_BYTES = TILES * FULL_PARTS<OP> * TURN16_BYTES;
@@ -318,18 +330,18 @@ template <int OP, int MT, int KT, bool DELTA> struct BwdChunkLayout {
     static constexpr int K_AT = 0, Q_AT = ROWS, O_AT = 2 * ROWS, V_AT = O_AT + BLOCK, DV_AT = V_AT + VP * BLOCK;
     static constexpr int M_AT = O_AT;  // when the blocks of d_v are used up
     static constexpr int G_AT = O_AT + (COLS_BYTES > M_BYTES ? COLS_BYTES : M_BYTES), RED_AT = G_AT + StepGates<R>::FLOATS * 4;
-    static constexpr int BYTES = RED_AT + (8 * R + 16) * 4;
+    static constexpr int BYTES = RED_AT + (2 * R + 3) * WAVES * 4;
 };
 
 // fp32 rows of a head on their way to LDS as 16-bit parts.
-template <int OP, int N, int PIECES, int ROWS> struct SplitLoader {
-    static constexpr int STRIDE = 256 / PIECES, COUNT = (ROWS + STRIDE - 1) / STRIDE;
+template <int OP, int N, int PIECES, int ROWS, int THREADS> struct SplitLoader {
+    static constexpr int STRIDE = THREADS / PIECES, COUNT = (ROWS + STRIDE - 1) / STRIDE;
     v4f v[COUNT][2];
     __device__ __forceinline__ void load(const float* first, uint32_t stride, int d, int valid, int tid)
     {
         const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(first), 0, valid > 0 ? (uint32_t)(valid - 1) * stride + (uint32_t)d * 4u : 0u, 0x00020000);
         const int row = tid / PIECES, piece = tid % PIECES;
-        uint32_t at = 8 * piece < d ? (uint32_t)row * stride + 32u * piece : 0x80000000u;
+        uint32_t at = 8 * piece < d && (ROWS >= STRIDE || row < ROWS) ? (uint32_t)row * stride + 32u * piece : 0x80000000u;
 #pragma unroll
         for (int i = 0; i < COUNT; ++i, at += STRIDE * stride) {
             v[i][0] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0));
@@ -338,6 +350,7 @@ template <int OP, int N, int PIECES, int ROWS> struct SplitLoader {
     }
     __device__ __forceinline__ void store(char* m, int plane, int tid) const
     {
+        if (ROWS < STRIDE && tid / PIECES >= ROWS) return;
         char* const to = m + LdsRows<PIECES>::at(tid / PIECES, tid % PIECES);
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) {
@@ -363,15 +376,15 @@ template <int PIECES> __device__ __forceinline__ v4u lds_turned_channels(const c
 }
 
 // SHARED: heads share a key head, whose dQ and dK are summed in registers.
-template <int OP, int MT, int KT, bool DELTA, bool TWO, bool SHARED>
-__global__ __launch_bounds__(256) void k_attn_bwd_chunk(AttnBwdArgs a)
+template <int OP, int MT, int KP, bool DELTA, bool TWO, bool SHARED>
+__global__ __launch_bounds__(128 * KP) void k_attn_bwd_chunk(AttnBwdArgs a)
 {
-    typedef BwdChunkLayout<OP, MT, KT, DELTA> LY;
-    constexpr int R = LY::R, SHARE = (LY::TILES + 3) / 4, FP = FULL_PARTS<OP>;
+    typedef BwdChunkLayout<OP, MT, KP, DELTA> LY;
+    constexpr int R = LY::R, WAVES = LY::WAVES, THREADS = 64 * WAVES, KT = 1, SHARE = (LY::TILES + WAVES - 1) / WAVES, FP = FULL_PARTS<OP>;
     __shared__ __attribute__((aligned(16))) char lds[LY::BYTES];
     float* const gl = reinterpret_cast<float*>(lds + LY::G_AT);
-    float* const red = reinterpret_cast<float*>(lds + LY::RED_AT);  // sums over channels: [2][wavefront][token], then [4][wavefront]
-    float* const red1 = red + 8 * R;
+    float* const red = reinterpret_cast<float*>(lds + LY::RED_AT);  // sums over channels: [2][wavefront][token], then [3][wavefront]
+    float* const red1 = red + 2 * WAVES * R;
     const Lane ln = lane_id();
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), H_k = a.H / a.group;
     const unsigned b = xcd_neighbours(blockIdx.x, gridDim.x);
@@ -398,8 +411,8 @@ __global__ __launch_bounds__(256) void k_attn_bwd_chunk(AttnBwdArgs a)
     const int ch0 = 16 * KT * wave;  // this wavefront's first channel
     const uint32_t stride_k = 2u * H_k * a.d_k, stride_u = 2u * a.H * a.d_v;
     const MinusOne<OP> minus(ln);
-    RowLoader<LY::CB, R, 256> lo, lu;  // dO; dV', or V' itself
-    SplitLoader<OP, FP, LY::CB, R> lv;
+    RowLoader<LY::CB, R, THREADS> lo, lu;  // dO; dV', or V' itself
+    SplitLoader<OP, FP, LY::CB, R, THREADS> lv;
     StepGates<R> lg;
     auto request = [&](int h, int v0) {
         const int cols = a.d_v - v0 < 64 ? a.d_v - v0 : 64;
@@ -435,7 +448,7 @@ __global__ __launch_bounds__(256) void k_attn_bwd_chunk(AttnBwdArgs a)
     const int h0 = hk * a.group;
     request(h0, 0);
     {
-        RowLoader<LY::PIECES, R, 256> lk, lq;
+        RowLoader<LY::PIECES, R, THREADS> lk, lq;
         lk.load(static_cast<const char*>(a.K) + at.row * stride_k + 2 * hk * a.d_k, stride_k, a.d_k, at.valid, tid);
         lq.load(static_cast<const char*>(a.Q) + at.row * stride_k + 2 * hk * a.d_k, stride_k, a.d_k, at.valid, tid);
         lg.load(a.g, at, a.H, h0, tid);
@@ -466,7 +479,7 @@ __global__ __launch_bounds__(256) void k_attn_bwd_chunk(AttnBwdArgs a)
         int its[SHARE], jts[SHARE], idx[SHARE];
 #pragma unroll
         for (int j = 0; j < SHARE; ++j) {
-            int x = j * 4 + wave < LY::TILES ? j * 4 + wave : LY::TILES - 1, it = 0;
+            int x = j * WAVES + wave < LY::TILES ? j * WAVES + wave : LY::TILES - 1, it = 0;
             idx[j] = x;
             while (x > it) x -= ++it;
             its[j] = it, jts[j] = x;
@@ -602,7 +615,10 @@ __global__ __launch_bounds__(256) void k_attn_bwd_chunk(AttnBwdArgs a)
             const float mine = wave_max(most_of(M));
             if (ln.q == 0 && ln.n == 0) red1[wave] = mine;
             __syncthreads();
-            m_shift = f16_shift(fmaxf(fmaxf(red1[0], red1[1]), fmaxf(red1[2], red1[3])));
+            float most = red1[0];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) most = fmaxf(most, red1[w]);
+            m_shift = f16_shift(most);
         }
         const Turn16 turn(reinterpret_cast<float*>(lds + LY::M_AT), ln);
 #pragma unroll
@@ -678,18 +694,18 @@ __global__ __launch_bounds__(256) void k_attn_bwd_chunk(AttnBwdArgs a)
             }
             dot_q += __shfl_xor(dot_q, 16), dot_k += __shfl_xor(dot_k, 16);
             dot_q += __shfl_xor(dot_q, 32), dot_k += __shfl_xor(dot_k, 32);
-            if (ln.q == 0) red[wave * R + 16 * it + ln.n] = dot_q, red[(4 + wave) * R + 16 * it + ln.n] = dot_k;
+            if (ln.q == 0) red[wave * R + 16 * it + ln.n] = dot_q, red[(WAVES + wave) * R + 16 * it + ln.n] = dot_k;
         }
         if (a.dg) {
             const float x = wave_sum(inter), y = wave_sum(s_ds);
-            if (ln.q == 0 && ln.n == 0) red1[4 + wave] = x, red1[8 + wave] = y;
+            if (ln.q == 0 && ln.n == 0) red1[WAVES + wave] = x, red1[2 * WAVES + wave] = y;
             __syncthreads();
             if (tid < at.valid) {
                 float q = 0.f, kd = 0.f, last = 0.f;
-                for (int w = 0; w < 4; ++w) q += red[w * R + tid], kd += red[(4 + w) * R + tid];
+                for (int w = 0; w < WAVES; ++w) q += red[w * R + tid], kd += red[(WAVES + w) * R + tid];
                 if (chunk_ends && tid == at.valid - 1) {
                     float t = 0.f;
-                    for (int w = 0; w < 4; ++w) last += red1[4 + w], t += red1[8 + w];
+                    for (int w = 0; w < WAVES; ++w) last += red1[WAVES + w], t += red1[2 * WAVES + w];
                     last += gl[3 * R] * t;
                 }
                 a.dg[(at.row + tid) * a.H + h] = q - kd + last;
