@@ -27,7 +27,7 @@ struct AttnArgs {
     // Segments of the sequences (a workgroup each), where there are too few heads: what a segment adds to a state and what it does to
     // the one before it, or the states before the segments from them.
     float *seg_state, *seg_trans, *seg_decay;
-    float *rec_state, *rec_value;  // for the gradient: the states before the steps [step][H][d_k][d_v], and V' [token][H][d_v] where it is not U
+    float *rec_state, *rec_value;  // for the gradient: the states before the steps [step][H], and V' where it is not U, [first token of the step][H], as put_turned leaves them
     SeqMap map;
     int H, group, d_k, d_v, C;  // group: heads that share a key head
     int n_seg;
@@ -90,20 +90,26 @@ __device__ __forceinline__ v4f times(v4f x, float a)
 template <int OP, int MT, int KP>
 __device__ __forceinline__ void add_turned(v4f (&S)[2 * KP], const char* rows, const Parts<FULL_PARTS<OP>> (&vp)[MT / 2], Lane ln)
 {
+    // the next KP tiles are requested before one is used
+    v4u k[2][KP];
+    auto rows_of = [&](int stage) {
 #pragma unroll
-    for (int tp = 0; tp < MT / 2; ++tp) {
-        v4u k[2 * KP];
+        for (int i = 0; i < KP; ++i) k[stage & 1][i] = lds_turned_tile<4 * KP>(rows, stage >> 1, KP * (stage & 1) + i, ln);
+    };
+    rows_of(0);
 #pragma unroll
-        for (int i = 0; i < 2 * KP; ++i) k[i] = lds_turned_tile<4 * KP>(rows, tp, i, ln);
+    for (int stage = 0; stage < MT; ++stage) {
+        if (stage + 1 < MT) rows_of(stage + 1);
+        in_order();
 #pragma unroll
         for (int part = FULL_PARTS<OP> - 1; part >= 0; --part)
 #pragma unroll
-            for (int i = 0; i < 2 * KP; ++i) S[i] = mfma32<OP>(k[i], vp[tp].u[part], S[i]);
+            for (int i = 0; i < KP; ++i) S[KP * (stage & 1) + i] = mfma32<OP>(k[stage & 1][i], vp[stage >> 1].u[part], S[KP * (stage & 1) + i]);
     }
 }
 
-// v = X S (tokens x columns), sp the parts of S: rows of X, the next pair's requested before one is used.
-template <int OP, int MT, int KP> __device__ __forceinline__ void rows_times(v4f (&v)[MT], const char* rows, const Parts<FULL_PARTS<OP>> (&sp)[KP], Lane ln)
+// v = X S (tokens x columns), sp the parts of S: rows of X, the next pair's requested before one is used; `also` follows each pair's products.
+template <int OP, int MT, int KP, class Also> __device__ __forceinline__ void rows_times(v4f (&v)[MT], const char* rows, const Parts<FULL_PARTS<OP>> (&sp)[KP], Lane ln, Also also)
 {
     v4u w[2][MT];
     auto rows_of = [&](int p) {
@@ -121,6 +127,7 @@ template <int OP, int MT, int KP> __device__ __forceinline__ void rows_times(v4f
         for (int part = FULL_PARTS<OP> - 1; part >= 0; --part)
 #pragma unroll
             for (int tb = 0; tb < MT; ++tb) v[tb] = mfma32<OP>(w[p & 1][tb], sp[p].u[part], v[tb]);
+        also(p);
     }
 }
 // V' = U - W S of 16 columns from LDS; v holds W S 2^shift (DELTA).
@@ -270,7 +277,7 @@ __global__ __launch_bounds__(512) void k_chunk_attn(AttnArgs a)
             v2u u[MT];
 #pragma unroll
             for (int tb = 0; tb < MT; ++tb) u[tb] = lds_turned<LY::UPIECES>(lds + LY::U_AT, 16 * tb + 4 * ln.q + (ln.n >> 2), 4 * wave + (ln.n & 3));
-            if constexpr (DELTA) rows_times<OP, MT, KP>(v, lds + LY::W_AT, sp, ln);
+            if constexpr (DELTA) rows_times<OP, MT, KP>(v, lds + LY::W_AT, sp, ln, [](int) {});
             __syncthreads();  // W, U, Q and the parts of S are in registers
             values_of<OP, MT, LY::UPIECES, DELTA>(v, u, s_shift);
             int v_shift = 0;
@@ -482,10 +489,11 @@ __device__ __forceinline__ void attn_states(const AttnArgs& a, char* const lds, 
 {
     typedef StatesLayout<OP, MT, KP, DELTA, WAVES> LY;
     constexpr bool SEGMENT = MODE == ATTN_SEGMENT;
-    constexpr int R = LY::R, FP = FULL_PARTS<OP>, THREADS = 64 * WAVES;
+    constexpr int R = LY::R, FP = FULL_PARTS<OP>, THREADS = 64 * WAVES;  // that bring rows
     float* const gates = reinterpret_cast<float*>(lds + LY::G_AT);
     const Lane ln = lane_id();
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tid = threadIdx.x & (THREADS - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const bool brings = SEGMENT || threadIdx.x >= THREADS;
 
     const unsigned groups_v = (a.d_v + LY::COLS - 1) / LY::COLS, groups = groups_v + (SEGMENT && DELTA ? (a.d_k + LY::COLS - 1) / LY::COLS : 0);
     const unsigned cg = b % groups, hs = b / groups;
@@ -522,53 +530,81 @@ __device__ __forceinline__ void attn_states(const AttnArgs& a, char* const lds, 
         lu.store(lds + LY::U_AT, tid);
         lg.store(gates + (k & 1) * StepGates<R>::FLOATS, a.scale, tid);
     };
-    request(k0);
-    bring(k0);
-    request(k0 + 1);
+    if (brings) {
+        request(k0);
+        bring(k0);
+        request(k0 + 1);
+    }
+    if (!SEGMENT && brings) {
+        __syncthreads();
+        for (int64_t k = k0; k < k1; ++k) {
+            __syncthreads();  // W and U are in registers
+            bring(k + 1);
+            request(k + 2);
+            __syncthreads();
+        }
+        return;
+    }
     const MinusOne<OP> minus(ln);
     v4f S[2 * KP];
     const float* const from = SEGMENT || !a.state ? nullptr : a.state + (int64_t)hs * a.d_k * a.d_v;
     get_state<KP>(from, S, a.d_k, d_v, col0, trans, ln);
     Parts<FP> sp[KP];
     int s_shift = 0;
-    auto parts_of_state = [&]() {
-        if constexpr (OP == OP_F16) s_shift = f16_shift(wave_max(most_of(S)));
+    auto parts_of_state = [&](Parts<FP>(&to)[KP], int& shift) {
+        if constexpr (OP == OP_F16) shift = f16_shift(wave_max(most_of(S)));
         v4f x[2 * KP];
 #pragma unroll
-        for (int i = 0; i < 2 * KP; ++i) x[i] = OP == OP_F16 ? times(S[i], pow2(s_shift)) : S[i];
-        split_pairs<OP, FP, KP>(x, sp, minus);
+        for (int i = 0; i < 2 * KP; ++i) x[i] = OP == OP_F16 ? times(S[i], pow2(shift)) : S[i];
+        split_pairs<OP, FP, KP>(x, to, minus);
     };
-    if constexpr (DELTA) parts_of_state();
+    if constexpr (DELTA) parts_of_state(sp, s_shift);
+    const TurnOne<OP> one_k(ln, true), one_t(ln, false);
     float total = 0.f;
     __syncthreads();
     for (int64_t k = k0; k < k1; ++k) {
         const float* const gl = gates + (k & 1) * StepGates<R>::FLOATS;
-        if constexpr (!SEGMENT) put_state<KP>(a.rec_state + ((rec0 + k) * a.H + h) * a.d_k * a.d_v, S, a.d_k, a.d_v, col0, ln);
+        float* const state_to = SEGMENT ? nullptr : a.rec_state + ((rec0 + k) * a.H + h) * a.d_k * a.d_v;
+        if constexpr (!SEGMENT) {
+            if constexpr (TWO || !DELTA) {
+                Parts<FP> now[KP];
+                int shift = 0;
+                parts_of_state(now, shift);
+#pragma unroll
+                for (int p = 0; p < KP; ++p) put_turned<OP>(state_to, p, now[p], pow2(-shift), a.d_k, a.d_v, col0, one_k, ln);
+            }
+        }
         v4f v[MT];
         v2u u[MT];
 #pragma unroll
         for (int tb = 0; tb < MT; ++tb) u[tb] = lds_turned<LY::UPIECES>(lds + LY::U_AT, 16 * tb + 4 * ln.q + (ln.n >> 2), 4 * wave + (ln.n & 3));
-        if constexpr (DELTA) rows_times<OP, MT, KP>(v, lds + LY::W_AT, sp, ln);
-        __syncthreads();  // W and U are in registers
-        bring(k + 1);
-        request(k + 2);
-        values_of<OP, MT, LY::UPIECES, DELTA>(v, u, s_shift);
-        if constexpr (!SEGMENT && DELTA) {
-            const StepPos at = step_pos<R>(sq, k, k1, a.C);
-            const uint32_t stride = 4u * a.H * a.d_v;
-            const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(a.rec_value + (at.row * a.H + h) * a.d_v, 0, (uint32_t)(at.valid - 1) * stride + 4u * a.d_v, 0x00020000);
-            uint32_t to = col0 + ln.n < a.d_v ? 4 * ln.q * stride + 4u * (col0 + ln.n) : 0x80000000u;
-#pragma unroll
-            for (int tb = 0; tb < MT; ++tb, to += 12 * stride)
-#pragma unroll
-                for (int r = 0; r < 4; ++r, to += stride) __builtin_amdgcn_raw_buffer_store_b32(bits(v[tb][r]), rsrc, to, 0, 0);
+        if constexpr (DELTA) {
+            rows_times<OP, MT, KP>(v, lds + LY::W_AT, sp, ln, [&](int p) {
+                if constexpr (!SEGMENT && !TWO) put_turned<OP>(state_to, p, sp[p], pow2(-s_shift), a.d_k, a.d_v, col0, one_k, ln);
+            });
         }
+        __syncthreads();  // W and U are in registers
+        if constexpr (SEGMENT) {
+            bring(k + 1);
+            request(k + 2);
+        }
+        values_of<OP, MT, LY::UPIECES, DELTA>(v, u, s_shift);
         int v_shift = 0;
         if constexpr (OP == OP_F16) v_shift = f16_shift(wave_max(most_of(v)));
+        if constexpr (!SEGMENT && DELTA) {
+            v4f x[MT];
+            Parts<FP> vp[MT / 2];
+#pragma unroll
+            for (int tb = 0; tb < MT; ++tb) x[tb] = OP == OP_F16 ? times(v[tb], pow2(v_shift)) : v[tb];
+            split_pairs<OP, FP, MT / 2>(x, vp, minus);
+            const StepPos at = step_pos<R>(sq, k, k1, a.C);
+#pragma unroll
+            for (int tp = 0; tp < MT / 2; ++tp) put_turned<OP>(a.rec_value + (at.row * a.H + h * at.valid) * a.d_v, tp, vp[tp], pow2(-v_shift), at.valid, a.d_v, col0, one_t, ln);
+        }
         if (SEGMENT && !DELTA) total += gl[3 * R + 1];
         state_after<OP, MT, KP>(S, v, v_shift, lds + LY::K_AT + (k & 1) * LY::ROWS, gl + R, gl[3 * R], minus, ln);
         if constexpr (DELTA) {
-            if (!TWO || ((k + 1) & 1) == 0) parts_of_state();
+            if (!TWO || ((k + 1) & 1) == 0) parts_of_state(sp, s_shift);
         }
         __syncthreads();  // the next rows are in LDS
     }

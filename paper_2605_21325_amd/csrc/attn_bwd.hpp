@@ -74,6 +74,7 @@ __device__ __forceinline__ void attn_bwd_state(const AttnBwdArgs& a, char* const
 
     if (wave < 4) {
         const int col0 = wg_col + 16 * wave;
+        const TurnOne<OP> one_k(ln, true);
         const int64_t rec0 = (a.map.cu_chunks ? a.map.cu_chunks[s] : s * n_chunk) * steps;
         v4f S[2 * KP], E[TWO ? 2 * KP : 1];  // dS; what the chunk's values pass on to the state before it
         get_state<KP>(a.dstate ? a.dstate + (int64_t)hs * a.d_k * a.d_v : nullptr, S, a.d_k, a.d_v, col0, false, ln);
@@ -97,7 +98,6 @@ __device__ __forceinline__ void attn_bwd_state(const AttnBwdArgs& a, char* const
         for (int64_t k = k1 - 1; k >= 0; --k) {
             const float* const gl = gates + (k & 1) * StepGates<R>::FLOATS;
             const char* const rows_k = lds + LY::K_AT + (k & 1) * LY::ROWS;
-            put_state<KP>(a.rec_dstate + ((rec0 + k) * a.H + h) * a.d_k * a.d_v, S, a.d_k, a.d_v, col0, ln);
             v4f dv[MT];
 #pragma unroll
             for (int tb = 0; tb < MT; ++tb) dv[tb] = zero4();
@@ -117,6 +117,7 @@ __device__ __forceinline__ void attn_bwd_state(const AttnBwdArgs& a, char* const
 #pragma unroll
                         for (int tb = 0; tb < MT; ++tb) dv[tb] = mfma32<OP>(w[p & 1][tb], sp[p].u[part], dv[tb]);
                     if (p == 0) __syncthreads();  // the others' rows are in LDS
+                    put_turned<OP>(a.rec_dstate + ((rec0 + k) * a.H + h) * a.d_k * a.d_v, p, sp[p], pow2(-s_shift), a.d_k, a.d_v, col0, one_k, ln);
                 }
             }
             const float s_down = OP == OP_F16 ? pow2(-s_shift) : 1.f, decay = gl[3 * R];
@@ -209,44 +210,74 @@ __device__ __forceinline__ void attn_bwd_state(const AttnBwdArgs& a, char* const
         lg.store(gates + (k & 1) * StepGates<R>::FLOATS, a.scale, tid);
         if constexpr (DELTA) lw.store(lds + LY::W_AT, tid);
     };
-    auto scores = [&](int64_t k) {  // P, as operands of P^T: token rows 4 q + r, column n; a share of the tiles a wavefront
+    // P, as operands of P^T: token rows 4 q + r, column n; a share of the tiles a wavefront (one without a tile forms the last one again)
+    constexpr int SHARE = (TILES + 3) / 4;
+    int its[SHARE], jts[SHARE], units[SHARE];
+#pragma unroll
+    for (int j = 0; j < SHARE; ++j) {
+        int idx = j * 4 + w4 < TILES ? j * 4 + w4 : TILES - 1, it = 0;
+        while (idx > it) idx -= ++it;
+        its[j] = it, jts[j] = idx, units[j] = LY::UNIT * (unit_at<LY>(idx) + (it >> 1) - (idx >> 1)) + 8 * (it & 1);
+    }
+    auto scores = [&](int64_t k) {
         const float* const gl = gates + (k & 1) * StepGates<R>::FLOATS;
         const char* const rows_k = lds + LY::K_AT + (k & 1) * LY::ROWS;
-        constexpr int SHARE = (TILES + 3) / 4;
-        v4f x[SHARE];
-        int its[SHARE], jts[SHARE];
+        v4f x[SHARE], gi[SHARE];
+        float gj[SHARE];
+        v4u qs[2][SHARE], ks[2][SHARE];
+        auto rows_of = [&](int p) {
+            const uint32_t at = in_place(LdsRows<PIECES>::at(ln.n, 4 * p + ln.q));
+#pragma unroll
+            for (int j = 0; j < SHARE; ++j) {
+                qs[p & 1][j] = *reinterpret_cast<const v4u*>(lds + LY::Q_AT + 16 * LdsRows<PIECES>::BYTES * its[j] + at);
+                ks[p & 1][j] = *reinterpret_cast<const v4u*>(rows_k + 16 * LdsRows<PIECES>::BYTES * jts[j] + at);
+            }
+        };
+        rows_of(0);
 #pragma unroll
         for (int j = 0; j < SHARE; ++j) {
-            int idx = j * 4 + w4 < TILES ? j * 4 + w4 : TILES - 1, it = 0;  // (a wavefront without a tile forms the last one again)
-            while (idx > it) idx -= ++it;
-            its[j] = it, jts[j] = idx, x[j] = zero4();
+            gj[j] = gl[16 * jts[j] + ln.n];
+            gi[j] = *reinterpret_cast<const v4f*>(gl + 16 * its[j] + 4 * ln.q);
+            x[j] = zero4();
         }
 #pragma unroll
-        for (int p = 0; p < KP; ++p)
+        for (int p = 0; p < KP; ++p) {
+            if (p + 1 < KP) rows_of(p + 1);
+            in_order();
 #pragma unroll
-            for (int j = 0; j < SHARE; ++j)
-                x[j] = mfma32<OP>(lds_row<PIECES>(lds + LY::Q_AT, 16 * its[j] + ln.n, 4 * p + ln.q), lds_row<PIECES>(rows_k, 16 * jts[j] + ln.n, 4 * p + ln.q), x[j]);
+            for (int j = 0; j < SHARE; ++j) x[j] = mfma32<OP>(qs[p & 1][j], ks[p & 1][j], x[j]);
+        }
 #pragma unroll
         for (int j = 0; j < SHARE; ++j) {
-            const int it = its[j], jt = jts[j];
-            const float gj = gl[16 * jt + ln.n];
-            const v4f gi = *reinterpret_cast<const v4f*>(gl + 16 * it + 4 * ln.q);
+            const bool on = jts[j] == its[j];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) x[j][r] *= a.scale * expf(jt < it || ln.n <= 4 * ln.q + r ? gi[r] - gj : -__builtin_inff());
-            char* unit = lds + LY::P_AT + LY::UNIT * (unit_at<LY>(jt) + (it >> 1) - (jt >> 1)) + lane16 + 8 * (it & 1);
+            for (int r = 0; r < 4; ++r) x[j][r] *= a.scale * __expf(on && ln.n > 4 * ln.q + r ? -__builtin_inff() : gi[j][r] - gj[j]);
+            char* unit = lds + LY::P_AT + units[j] + in_place(lane16);
 #pragma unroll
             for (int part = 0; part < FP; ++part) {
                 const v2u u = pack4<OP>(x[j]);
                 *reinterpret_cast<v2u*>(unit + 1024 * part) = u;
-                if (jt == it && (it & 1)) *reinterpret_cast<v2u*>(unit + 1024 * part - 8) = v2u{0u, 0u};  // the pair's other tile lies above the diagonal
+                if (on && (its[j] & 1)) *reinterpret_cast<v2u*>(unit + 1024 * part - 8) = v2u{0u, 0u};  // the pair's other tile lies above the diagonal
                 x[j] = minus16<OP>(x[j], u);
             }
         }
     };
     auto products = [&](int64_t k) {  // P^T dO and scale Q^T diag(G) dO of this wavefront's columns
         const float* const gl = gates + (k & 1) * StepGates<R>::FLOATS;
-        v4u o[MT / 2];
+        v4u o[MT / 2], pt[FP][MT], qt[2][KP];
         v4f y[MT], od[MT], x[2 * KP];
+        auto scores_of = [&](int tp, int part) {
+#pragma unroll
+            for (int jt = 0; jt <= 2 * tp + 1; ++jt) pt[part][jt] = *reinterpret_cast<const v4u*>(lds + LY::P_AT + LY::UNIT * (LY::units_before(jt) + tp - jt / 2) + 1024 * part + lane16);
+        };
+        auto queries_of = [&](int stage) {
+#pragma unroll
+            for (int i = 0; i < KP; ++i) qt[stage & 1][i] = lds_turned_tile<PIECES>(lds + LY::Q_AT, stage >> 1, KP * (stage & 1) + i, ln);
+        };
+        auto add_y = [&](int tp, int part) {
+#pragma unroll
+            for (int jt = 0; jt <= 2 * tp + 1; ++jt) y[jt] = mfma32<OP>(pt[part][jt], o[tp], y[jt]);
+        };
 #pragma unroll
         for (int tp = 0; tp < MT / 2; ++tp) {
             const int row = 32 * tp + 4 * ln.q + (ln.n >> 2), col4 = 4 * w4 + (ln.n & 3);
@@ -254,22 +285,15 @@ __device__ __forceinline__ void attn_bwd_state(const AttnBwdArgs& a, char* const
             o[tp] = v4u{u[0], u[1], v[0], v[1]};
         }
 #pragma unroll
-        for (int jt = 0; jt < MT; ++jt) y[jt] = zero4();
+        for (int tb = 0; tb < MT; ++tb) od[tb] = *reinterpret_cast<const v4f*>(gl + 2 * R + 16 * tb + 4 * ln.q);
 #pragma unroll
-        for (int tp = 0; tp < MT / 2; ++tp)
-#pragma unroll
-            for (int part = FP - 1; part >= 0; --part)
-#pragma unroll
-                for (int jt = 0; jt <= 2 * tp + 1; ++jt)
-                    y[jt] = mfma32<OP>(*reinterpret_cast<const v4u*>(lds + LY::P_AT + LY::UNIT * (LY::units_before(jt) + tp - jt / 2) + 1024 * part + lane16), o[tp], y[jt]);
-#pragma unroll
-        for (int jt = 0; jt < MT; ++jt) *reinterpret_cast<v4f*>(lds + LY::Y_AT + LY::Y_WAVE * w4 + 1024 * jt + lane16) = y[jt];
+        for (int part = FP - 1; part >= 0; --part) scores_of(0, part);
+        in_order();
 #pragma unroll
         for (int tb = 0; tb < MT; ++tb) {
-            const v4f e = *reinterpret_cast<const v4f*>(gl + 2 * R + 16 * tb + 4 * ln.q);
-            od[tb] = unpack4<OP>(v2u{o[tb / 2][2 * (tb & 1)], o[tb / 2][2 * (tb & 1) + 1]});
+            const v4f u = unpack4<OP>(v2u{o[tb / 2][2 * (tb & 1)], o[tb / 2][2 * (tb & 1) + 1]});
 #pragma unroll
-            for (int r = 0; r < 4; ++r) od[tb][r] *= e[r];
+            for (int r = 0; r < 4; ++r) od[tb][r] *= u[r];
         }
         int shift = 0;
         if constexpr (OP == OP_F16) {
@@ -278,10 +302,39 @@ __device__ __forceinline__ void attn_bwd_state(const AttnBwdArgs& a, char* const
             for (int tb = 0; tb < MT; ++tb) od[tb] = times(od[tb], pow2(shift));
         }
         Parts<FP> vp[MT / 2];
+        queries_of(0);
         split_pairs<OP, FP, MT / 2>(od, vp, minus);
 #pragma unroll
         for (int i = 0; i < 2 * KP; ++i) x[i] = zero4();
-        add_turned<OP, MT, KP>(x, lds + LY::Q_AT, vp, ln);
+#pragma unroll
+        for (int jt = 0; jt < MT; ++jt) y[jt] = zero4();
+        auto add_x = [&](int stage) {
+            if (stage + 1 < MT) queries_of(stage + 1);
+            in_order();
+#pragma unroll
+            for (int part = FP - 1; part >= 0; --part)
+#pragma unroll
+                for (int i = 0; i < KP; ++i) x[KP * (stage & 1) + i] = mfma32<OP>(qt[stage & 1][i], vp[stage >> 1].u[part], x[KP * (stage & 1) + i]);
+        };
+        in_order();
+#pragma unroll
+        for (int part = FP - 1; part >= 0; --part) add_y(0, part);
+        if constexpr (MT == 4) {
+#pragma unroll
+            for (int part = FP - 1; part >= 1; --part) scores_of(1, part);
+        }
+        add_x(0);
+        add_x(1);
+        if constexpr (MT == 4) {
+#pragma unroll
+            for (int part = FP - 1; part >= 1; --part) add_y(1, part);
+            scores_of(1, 0);
+            add_x(2);
+            add_y(1, 0);
+            add_x(3);
+        }
+#pragma unroll
+        for (int jt = 0; jt < MT; ++jt) *reinterpret_cast<v4f*>(lds + LY::Y_AT + LY::Y_WAVE * w4 + 1024 * jt + lane16) = y[jt];
 #pragma unroll
         for (int i = 0; i < 2 * KP; ++i) *reinterpret_cast<v4f*>(lds + LY::X_AT + LY::X_WAVE * w4 + 1024 * i + lane16) = OP == OP_F16 ? times(x[i], pow2(-shift)) : x[i];
     };
@@ -313,7 +366,7 @@ __global__ __launch_bounds__(512) void k_attn_bwd_walks(AttnBwdArgs a, AttnArgs 
     const unsigned units = gridDim.x / 2;
     if (blockIdx.x < units) {
         attn_bwd_state<OP, MT, KP, DELTA, TWO>(a, lds, xcd_neighbours(blockIdx.x, units));
-    } else if (threadIdx.x < 256) {
+    } else {
         attn_states<OP, MT, KP, DELTA, ATTN_RECORD, TWO, 4>(f, lds, xcd_neighbours(blockIdx.x - units, units), 0);
     }
 }
@@ -330,33 +383,35 @@ template <int OP, int MT, int KP, bool DELTA> struct BwdChunkLayout {
     static constexpr int K_AT = 0, Q_AT = ROWS, O_AT = 2 * ROWS, V_AT = O_AT + BLOCK, DV_AT = V_AT + VP * BLOCK;
     static constexpr int M_AT = O_AT;  // when the blocks of d_v are used up
     static constexpr int G_AT = O_AT + (COLS_BYTES > M_BYTES ? COLS_BYTES : M_BYTES), RED_AT = G_AT + StepGates<R>::FLOATS * 4;
-    static constexpr int BYTES = RED_AT + (2 * R + 3) * WAVES * 4;
+    static constexpr int BYTES = RED_AT + (2 * R + 3) * WAVES * 4, SUM_BYTES = 2 * WAVES * MT * 1024;
 };
 
-// fp32 rows of a head on their way to LDS as 16-bit parts.
-template <int OP, int N, int PIECES, int ROWS, int THREADS> struct SplitLoader {
-    static constexpr int STRIDE = THREADS / PIECES, COUNT = (ROWS + STRIDE - 1) / STRIDE;
+// Recorded values, as put_turned left them, on their way to LDS as rows of 16-bit parts: 64 columns a time.
+template <int OP, int N, int MT, int THREADS> struct ValueLoader {
+    static constexpr int BAND = THREADS / 128, COUNT = (MT + BAND - 1) / BAND;  // tiles of tokens at once
     v4f v[COUNT][2];
-    __device__ __forceinline__ void load(const float* first, uint32_t stride, int d, int valid, int tid)
+    __device__ __forceinline__ void load(const float* first, int v0, int d_v, int valid, int tid)
     {
-        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(first), 0, valid > 0 ? (uint32_t)(valid - 1) * stride + (uint32_t)d * 4u : 0u, 0x00020000);
-        const int row = tid / PIECES, piece = tid % PIECES;
-        uint32_t at = 8 * piece < d && (ROWS >= STRIDE || row < ROWS) ? (uint32_t)row * stride + 32u * piece : 0x80000000u;
+        const int n = tid & 15, col = v0 + 8 * ((tid >> 4) & 7);
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(first), 0, (uint32_t)valid * d_v * 4u, 0x00020000);
 #pragma unroll
-        for (int i = 0; i < COUNT; ++i, at += STRIDE * stride) {
+        for (int i = 0; i < COUNT; ++i) {
+            const int band = (tid >> 7) + i * BAND, of_band = valid - 16 * band < 16 ? valid - 16 * band : 16;
+            const uint32_t at = n < of_band && col < d_v ? 4u * (16 * band * d_v + col * of_band + 4 * n) : 0x80000000u;
             v[i][0] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0));
-            v[i][1] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at + 16u, 0, 0));
+            v[i][1] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at + 16u * of_band, 0, 0));
         }
     }
     __device__ __forceinline__ void store(char* m, int plane, int tid) const
     {
-        if (ROWS < STRIDE && tid / PIECES >= ROWS) return;
-        char* const to = m + LdsRows<PIECES>::at(tid / PIECES, tid % PIECES);
+        const int tb = tid >> 7;
+        if (MT < BAND && tb >= MT) return;
+        char* const to = m + LdsRows<8>::at(16 * tb + (tid & 15), (tid >> 4) & 7);
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) {
             const Parts<N> p = split_pair<OP, N>(v[i][0], v[i][1]);
 #pragma unroll
-            for (int j = 0; j < N; ++j) *reinterpret_cast<v4u*>(to + j * plane + i * STRIDE * LdsRows<PIECES>::BYTES) = p.u[j];
+            for (int j = 0; j < N; ++j) *reinterpret_cast<v4u*>(to + j * plane + i * BAND * 16 * LdsRows<8>::BYTES) = p.u[j];
         }
     }
 };
@@ -375,13 +430,13 @@ template <int PIECES> __device__ __forceinline__ v4u lds_turned_channels(const c
     return v4u{a[0], a[1], b[0], b[1]};
 }
 
-// SHARED: heads share a key head, whose dQ and dK are summed in registers.
+// SHARED: heads share a key head, whose dQ and dK are summed in LDS.
 template <int OP, int MT, int KP, bool DELTA, bool TWO, bool SHARED>
 __global__ __launch_bounds__(128 * KP) void k_attn_bwd_chunk(AttnBwdArgs a)
 {
     typedef BwdChunkLayout<OP, MT, KP, DELTA> LY;
     constexpr int R = LY::R, WAVES = LY::WAVES, THREADS = 64 * WAVES, KT = 1, SHARE = (LY::TILES + WAVES - 1) / WAVES, FP = FULL_PARTS<OP>;
-    __shared__ __attribute__((aligned(16))) char lds[LY::BYTES];
+    __shared__ __attribute__((aligned(16))) char lds[LY::BYTES + (SHARED ? LY::SUM_BYTES : 0)];
     float* const gl = reinterpret_cast<float*>(lds + LY::G_AT);
     float* const red = reinterpret_cast<float*>(lds + LY::RED_AT);  // sums over channels: [2][wavefront][token], then [3][wavefront]
     float* const red1 = red + 2 * WAVES * R;
@@ -412,35 +467,35 @@ __global__ __launch_bounds__(128 * KP) void k_attn_bwd_chunk(AttnBwdArgs a)
     const uint32_t stride_k = 2u * H_k * a.d_k, stride_u = 2u * a.H * a.d_v;
     const MinusOne<OP> minus(ln);
     RowLoader<LY::CB, R, THREADS> lo, lu;  // dO; dV', or V' itself
-    SplitLoader<OP, FP, LY::CB, R, THREADS> lv;
+    ValueLoader<OP, FP, MT, THREADS> lv;
     StepGates<R> lg;
     auto request = [&](int h, int v0) {
         const int cols = a.d_v - v0 < 64 ? a.d_v - v0 : 64;
         const int64_t first = (at.row * a.H + h) * a.d_v + v0;
         lo.load(static_cast<const uint16_t*>(a.dO) + first, stride_u, cols, at.valid, tid);
         lu.load(static_cast<const uint16_t*>(DELTA ? a.dU : a.U) + first, stride_u, cols, at.valid, tid);
-        if constexpr (DELTA) lv.load(a.rec_value + first, 2u * stride_u, cols, at.valid, tid);
+        if constexpr (DELTA) lv.load(a.rec_value + (at.row * a.H + h * at.valid) * a.d_v, v0, a.d_v, at.valid, tid);
     };
     v4f sv[KT][2][2], dsv[KT][2][2];  // this wavefront's rows of S and dS', the block's columns
     v4f szv[TWO ? KT : 1][2][2];      // of the state before the chunk, in its second step
     const bool second = TWO && (k & 1);
     auto request_states = [&](int h, int v0) {
-        const uint32_t span = (uint32_t)a.d_k * a.d_v * 4u;
-        const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(a.rec_state) + (id * a.H + h) * a.d_k * a.d_v, 0, span, 0x00020000);
-        const auto rd = __builtin_amdgcn_make_buffer_rsrc(a.rec_dstate + (id * a.H + h) * a.d_k * a.d_v, 0, span, 0x00020000);
+        const int64_t size = a.d_k * a.d_v;
+        const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(a.rec_state) + (id * a.H + h) * size, 0, (uint32_t)size * 4u, 0x00020000);
+        const auto rd = __builtin_amdgcn_make_buffer_rsrc(a.rec_dstate + (id * a.H + h) * size, 0, (uint32_t)size * 4u, 0x00020000);
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) {
-                const int ch = ch0 + 16 * kt + ln.n, col = v0 + 32 * ks + 8 * ln.q;
-                const uint32_t from = ch < a.d_k && col < a.d_v ? (uint32_t)(ch * a.d_v + col) * 4u : 0x80000000u;
+                const int ch = ch0 + 16 * kt, col = v0 + 32 * ks + 8 * ln.q;
+                const uint32_t from = ch < a.d_k && col < a.d_v ? 4u * (ch * a.d_v + 16 * col + 4 * ln.n) : 0x80000000u;
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
-                    sv[kt][ks][half] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(rs, from + 16u * half, 0, 0));
-                    dsv[kt][ks][half] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(rd, from + 16u * half, 0, 0));
+                    sv[kt][ks][half] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(rs, from + 256u * half, 0, 0));
+                    dsv[kt][ks][half] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(rd, from + 256u * half, 0, 0));
                     if constexpr (TWO) {
-                        const auto rz = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(a.rec_state) + ((id - second) * a.H + h) * a.d_k * a.d_v, 0, span, 0x00020000);
-                        szv[kt][ks][half] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(rz, from + 16u * half, 0, 0));
+                        const auto rz = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(a.rec_state) + ((id - second) * a.H + h) * size, 0, (uint32_t)size * 4u, 0x00020000);
+                        szv[kt][ks][half] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(rz, from + 256u * half, 0, 0));
                     }
                 }
             }
@@ -456,17 +511,13 @@ __global__ __launch_bounds__(128 * KP) void k_attn_bwd_chunk(AttnBwdArgs a)
         lk.store(lds + LY::K_AT, tid);
         lq.store(lds + LY::Q_AT, tid);
     }
-    v4f sum_q[SHARED ? KT : 1][MT], sum_k[SHARED ? KT : 1][MT];
-#pragma unroll
-    for (int kt = 0; kt < (SHARED ? KT : 1); ++kt)
-#pragma unroll
-        for (int it = 0; it < MT; ++it) sum_q[kt][it] = sum_k[kt][it] = zero4();
     auto put_rows = [&](void* to, const v4f x, int heads, int head, int ch, int it) {
         const int i = 16 * it + ln.n;
         if (i < at.valid && ch < a.d_k) *reinterpret_cast<v2u*>(static_cast<uint16_t*>(to) + ((at.row + i) * heads + head) * a.d_k + ch) = pack4<OP>(x);
     };
 
     for (int h = h0; h < h0 + (SHARED ? a.group : 1); ++h) {
+        const bool last_h = !SHARED || h + 1 == h0 + a.group;
         lg.store(gl, a.scale, tid);
         v4f X[KT][MT], Y[KT][MT], Z[KT][MT], M[SHARE];
 #pragma unroll
@@ -549,6 +600,7 @@ __global__ __launch_bounds__(128 * KP) void k_attn_bwd_chunk(AttnBwdArgs a)
             }
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) {
+                in_order();  // (or it takes registers for both at once)
                 Parts<FP> sp[KT], dp[KT];
                 {
                     v4f x[2 * KT], y[2 * KT];
@@ -687,10 +739,18 @@ __global__ __launch_bounds__(128 * KP) void k_attn_bwd_chunk(AttnBwdArgs a)
                 for (int r = 0; r < 4; ++r) {
                     if constexpr (OP == OP_F16) X[kt][it][r] *= down, Y[kt][it][r] *= down;
                     dot_q += q[kt][r] * X[kt][it][r], dot_k += kk[kt][r] * Y[kt][it][r];
-                    if constexpr (SHARED) sum_q[kt][it][r] += X[kt][it][r], sum_k[kt][it][r] += Y[kt][it][r];
                 }
                 if constexpr (DELTA) put_rows(a.dW, times(Z[kt][it], OP == OP_F16 ? -pow2(-z_shift) : -1.f), a.H, h, ch, it);
-                if constexpr (!SHARED) put_rows(a.dQ, X[kt][it], H_k, hk, ch, it), put_rows(a.dK, Y[kt][it], H_k, hk, ch, it);
+                if constexpr (SHARED) {
+                    v4f* const sum = reinterpret_cast<v4f*>(lds + LY::BYTES + 1024 * (2 * (wave * MT + it)) + 16 * (16 * ln.q + ln.n));  // the lane's own
+                    if (h > h0) {
+                        const v4f x = sum[0], y = sum[64];
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) X[kt][it][r] += x[r], Y[kt][it][r] += y[r];
+                    }
+                    if (!last_h) sum[0] = X[kt][it], sum[64] = Y[kt][it];
+                }
+                if (last_h) put_rows(a.dQ, X[kt][it], H_k, hk, ch, it), put_rows(a.dK, Y[kt][it], H_k, hk, ch, it);
             }
             dot_q += __shfl_xor(dot_q, 16), dot_k += __shfl_xor(dot_k, 16);
             dot_q += __shfl_xor(dot_q, 32), dot_k += __shfl_xor(dot_k, 32);
@@ -712,15 +772,6 @@ __global__ __launch_bounds__(128 * KP) void k_attn_bwd_chunk(AttnBwdArgs a)
             }
         }
         if constexpr (SHARED) __syncthreads();  // M, the gates and the sums are not needed any more
-    }
-    if constexpr (SHARED) {
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-            for (int it = 0; it < MT; ++it) {
-                put_rows(a.dQ, sum_q[kt][it], H_k, hk, ch0 + 16 * kt + 4 * ln.q, it);
-                put_rows(a.dK, sum_k[kt][it], H_k, hk, ch0 + 16 * kt + 4 * ln.q, it);
-            }
     }
 }
 

@@ -110,6 +110,44 @@ template <int OP, int N, int COUNT> __device__ __forceinline__ void split_pairs(
     }
 }
 
+// Tiles turned by the matrix cores, X^T 1 from parts of X, exact: columns down and rows across, so that a lane's four values are neighbours in a row.
+// In memory a band of 16 rows is [4 columns][row of the band][4]: a tile is 1 KB in one piece, to be read by rows or by columns.
+// Rows of a pair of tiles: 32 channels as they follow each other, or two tiles of 16 tokens.
+template <int OP> struct TurnOne {
+    v4u of[2];
+    __device__ __forceinline__ TurnOne(Lane ln, bool channels)
+    {
+        constexpr uint32_t m = OP == OP_F16 ? 0x3c00u : 0x3f80u;
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const int first = channels ? 8 * ln.q + 2 * w : 16 * (w >> 1) + 4 * ln.q + 2 * (w & 1), row = ln.n + 16 * half;
+                of[half][w] = first == row ? m : first + 1 == row ? m << 16 : 0u;
+            }
+    }
+};
+// The columns col0 .. col0 + 15 of pair number `pair` of tiles; `rows` of them there are in all, of d columns.
+template <int OP, int N> __device__ __forceinline__ void put_turned(float* to, int pair, const Parts<N>& p, float down, int rows, int d, int col0, const TurnOne<OP>& one, Lane ln)
+{
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(to, 0, (uint32_t)rows * d * 4u, 0x00020000);
+    v4f x[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int part = N - 1; part >= 0; --part)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) x[i] = mfma32<OP>(p.u[part], one.of[i], x[i]);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int band = 2 * pair + i, of_band = rows - 16 * band < 16 ? rows - 16 * band : 16;
+        const uint32_t at = ln.n < of_band && col0 + 4 * ln.q < d ? 4u * (16 * band * d + (col0 + 4 * ln.q) * of_band + 4 * ln.n) : 0x80000000u;
+        if constexpr (OP == OP_F16) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[i][r] *= down;
+        }
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, x[i]), rsrc, at, 0, 0);
+    }
+}
+
 // Largest of a non-negative value over the wavefront, as a uniform value.
 __device__ __forceinline__ float wave_max(float x)
 {
@@ -179,6 +217,13 @@ template <int OP> __device__ __forceinline__ v4f unpack4(v2u raw)
 
 // Rows of one head of a [token][heads][d] tensor on their way from memory to LDS: `ROWS` of them, what is not there (rows from
 // `valid` on, columns from d on) as zeros, by the bounds check of buffer loads.  A thread has one piece of every THREADS / PIECES-th row.
+// The same value, as one that a loop must not take for its own: sums with it are formed where they are used instead of being kept in a register each.
+__device__ __forceinline__ uint32_t in_place(uint32_t x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 template <int PIECES, int ROWS, int THREADS> struct RowLoader {
     static constexpr int STRIDE = THREADS / PIECES, N = (ROWS + STRIDE - 1) / STRIDE;
     static_assert(THREADS % PIECES == 0 && (STRIDE % 16 == 0 || N == 1), "a thread's rows are permuted alike");
@@ -188,7 +233,7 @@ template <int PIECES, int ROWS, int THREADS> struct RowLoader {
         const uint32_t span = valid > 0 ? (uint32_t)(valid - 1) * stride + (uint32_t)d * 2u : 0u;
         const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(first), 0, span, 0x00020000);
         const int row = tid / PIECES, piece = tid % PIECES;
-        uint32_t at = 8 * piece < d && (ROWS >= STRIDE || row < ROWS) ? (uint32_t)row * stride + 16u * piece : 0x80000000u;
+        uint32_t at = in_place(8 * piece < d && (ROWS >= STRIDE || row < ROWS) ? (uint32_t)row * stride + 16u * piece : 0x80000000u);
 #pragma unroll
         for (int i = 0; i < N; ++i, at += STRIDE * stride) v[i] = __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0));
     }
