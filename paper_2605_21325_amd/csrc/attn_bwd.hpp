@@ -38,9 +38,9 @@ template <int OP, int MT, int KP, bool DELTA> struct BwdStateLayout {
         return n;
     }
     static constexpr int UNIT = 1024 * FULL_PARTS<OP>;
-    static constexpr int K_AT = 0, W_AT = 2 * ROWS, Q_AT = W_AT + (DELTA ? ROWS : 0), O_AT = Q_AT + ROWS, P_AT = O_AT + R * UPIECES * 16;
-    static constexpr int X_AT = P_AT + units_before(MT) * UNIT, X_WAVE = 2 * KP * 1024, Y_AT = X_AT + 4 * X_WAVE, Y_WAVE = MT * 1024;  // fp32 tiles, a wavefront's columns
-    static constexpr int G_AT = Y_AT + 4 * Y_WAVE, BYTES = G_AT + 2 * StepGates<R>::FLOATS * 4;
+    static constexpr int K_AT = 0, W_AT = 2 * ROWS, Q_AT = W_AT + (DELTA ? ROWS : 0), O_AT = Q_AT + ROWS, O_ROWS = R * UPIECES * 16, P_AT = O_AT + 2 * O_ROWS;
+    static constexpr int X_AT = P_AT + units_before(MT) * UNIT, X_WAVE = 2 * KP * 1024;  // fp32 tiles, a wavefront's columns
+    static constexpr int G_AT = X_AT + 4 * X_WAVE, BYTES = G_AT + 2 * StepGates<R>::FLOATS * 4;
 };
 
 template <class LY> __device__ __forceinline__ int unit_at(int jt)  // units_before at run time
@@ -50,10 +50,10 @@ template <class LY> __device__ __forceinline__ int unit_at(int jt)  // units_bef
     return n;
 }
 
-// dS from the last step to the first, a workgroup per head and 64 columns as in the forward pass.  Four wavefronts carry the recursion (K dS', W^T dV'); four others
-// are a step ahead with what does not depend on it: P, P^T dO and scale Q^T diag(G) dO, which go through LDS in fp32.
-//     first part     K dS', dV'                                 rows of the step before to LDS | its P
-//     second part    dU, W^T dV', the new dS and its parts      P^T dO and Q^T dO of the step before
+// dS from the last step to the first, a workgroup per head and 64 columns as in the forward pass.  Four wavefronts carry the recursion; four others are a step
+// ahead with what does not depend on it: P, whose parts go round through LDS, and X = scale Q^T diag(G) dO in fp32.
+//     first half     K dS', dV', G_C dS' + X            P and X of the step before, in registers; W to LDS
+//     second half    dU, W^T dV', the parts of dS       P and X to LDS, and the rows of the step before that
 template <int OP, int MT, int KP, bool DELTA, bool TWO>
 __device__ __forceinline__ void attn_bwd_state(const AttnBwdArgs& a, char* const lds, unsigned b)
 {
@@ -94,46 +94,47 @@ __device__ __forceinline__ void attn_bwd_state(const AttnBwdArgs& a, char* const
         parts_of_state();
         __syncthreads();
         __syncthreads();
-        __syncthreads();  // the last step's rows, P^T dO and Q^T dO are in LDS
+        __syncthreads();  // the last step's rows, P and X are in LDS
         for (int64_t k = k1 - 1; k >= 0; --k) {
             const float* const gl = gates + (k & 1) * StepGates<R>::FLOATS;
             const char* const rows_k = lds + LY::K_AT + (k & 1) * LY::ROWS;
             v4f dv[MT];
+            rows_times<OP, MT, KP>(dv, rows_k, sp, ln, [&](int p) {
+                put_turned<OP>(a.rec_dstate + ((rec0 + k) * a.H + h) * a.d_k * a.d_v, p, sp[p], pow2(-s_shift), a.d_k, a.d_v, col0, one_k, ln);
+            });
+            v4u pt[MT / 2][FP][MT], o[MT / 2];
 #pragma unroll
-            for (int tb = 0; tb < MT; ++tb) dv[tb] = zero4();
-            {  // (rows_times with a barrier in it)
-                v4u w[2][MT];
-                auto rows_of = [&](int p) {
+            for (int tp = 0; tp < MT / 2; ++tp) {
+                const char* const rows_o = lds + LY::O_AT + (k & 1) * LY::O_ROWS;
+                const int row = 32 * tp + 4 * ln.q + (ln.n >> 2), col4 = 4 * wave + (ln.n & 3);
+                const v2u u = lds_turned<LY::UPIECES>(rows_o, row, col4), v = lds_turned<LY::UPIECES>(rows_o, row + 16, col4);
+                o[tp] = v4u{u[0], u[1], v[0], v[1]};
 #pragma unroll
-                    for (int tb = 0; tb < MT; ++tb) w[p & 1][tb] = lds_row<PIECES>(rows_k, 16 * tb + ln.n, 4 * p + ln.q);
-                };
-                rows_of(0);
+                for (int part = 0; part < FP; ++part)
 #pragma unroll
-                for (int p = 0; p < KP; ++p) {
-                    if (p + 1 < KP) rows_of(p + 1);
-                    in_order();
-#pragma unroll
-                    for (int part = FP - 1; part >= 0; --part)
-#pragma unroll
-                        for (int tb = 0; tb < MT; ++tb) dv[tb] = mfma32<OP>(w[p & 1][tb], sp[p].u[part], dv[tb]);
-                    if (p == 0) __syncthreads();  // the others' rows are in LDS
-                    put_turned<OP>(a.rec_dstate + ((rec0 + k) * a.H + h) * a.d_k * a.d_v, p, sp[p], pow2(-s_shift), a.d_k, a.d_v, col0, one_k, ln);
-                }
+                    for (int jt = 0; jt <= 2 * tp + 1; ++jt) pt[tp][part][jt] = *reinterpret_cast<const v4u*>(lds + LY::P_AT + LY::UNIT * (LY::units_before(jt) + tp - jt / 2) + 1024 * part + lane16);
             }
             const float s_down = OP == OP_F16 ? pow2(-s_shift) : 1.f, decay = gl[3 * R];
 #pragma unroll
             for (int tb = 0; tb < MT; ++tb) {
-                const v4f e = *reinterpret_cast<const v4f*>(gl + R + 16 * tb + 4 * ln.q), y = *reinterpret_cast<const v4f*>(lds + LY::Y_AT + LY::Y_WAVE * wave + 1024 * tb + lane16);
+                const v4f e = *reinterpret_cast<const v4f*>(gl + R + 16 * tb + 4 * ln.q);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) dv[tb][r] = dv[tb][r] * (OP == OP_F16 ? e[r] * s_down : e[r]) + y[r];
+                for (int r = 0; r < 4; ++r) dv[tb][r] *= OP == OP_F16 ? e[r] * s_down : e[r];
             }
+            in_order();
+#pragma unroll
+            for (int tp = 0; tp < MT / 2; ++tp)
+#pragma unroll
+                for (int part = FP - 1; part >= 0; --part)
+#pragma unroll
+                    for (int jt = 0; jt <= 2 * tp + 1; ++jt) dv[jt] = mfma32<OP>(pt[tp][part][jt], o[tp], dv[jt]);
 #pragma unroll
             for (int i = 0; i < 2 * KP; ++i) {
                 const v4f x = *reinterpret_cast<const v4f*>(lds + LY::X_AT + LY::X_WAVE * wave + 1024 * i + lane16);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) S[i][r] = decay * S[i][r] + x[r];
             }
-            __syncthreads();  // P^T dO and Q^T dO of this step are used up, W is in LDS
+            __syncthreads();  // this step's P, X, K and dO are used up, W is in LDS
             {
                 const StepPos at = step_pos<R>(sq, k, k1, a.C);
                 const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(static_cast<char*>(a.dU) + at.row * stride_u + 2 * ((int64_t)h * a.d_v), 0,
@@ -180,7 +181,7 @@ __device__ __forceinline__ void attn_bwd_state(const AttnBwdArgs& a, char* const
                 }
             }
             parts_of_state();
-            __syncthreads();  // the next step's P^T dO and Q^T dO are in LDS
+            __syncthreads();  // P and X of the next step are in LDS
         }
         if (a.dstate0) put_state<KP>(a.dstate0 + (int64_t)hs * a.d_k * a.d_v, S, a.d_k, a.d_v, col0, ln);
         return;
@@ -192,23 +193,24 @@ __device__ __forceinline__ void attn_bwd_state(const AttnBwdArgs& a, char* const
     RowLoader<LY::UPIECES, R, 256> lo;
     StepGates<R> lg;
     const uint32_t stride_k = 2u * H_k * a.d_k, stride_w = 2u * a.H * a.d_k;
-    auto request = [&](int64_t k) {  // K, Q, dO and the gates of step k, W of the one behind it
+    auto request = [&](int64_t k) {
         const StepPos at = step_pos<R>(sq, k, k1, a.C);
         lk.load(static_cast<const char*>(a.K) + at.row * stride_k + 2 * hk * a.d_k, stride_k, a.d_k, at.valid, tid);
         lq.load(static_cast<const char*>(a.Q) + at.row * stride_k + 2 * hk * a.d_k, stride_k, a.d_k, at.valid, tid);
         lo.load(static_cast<const char*>(a.dO) + at.row * stride_u + 2 * ((int64_t)h * a.d_v + wg_col), stride_u, cols, at.valid, tid);
         lg.load(a.g, at, a.H, h, tid);
-        if constexpr (DELTA) {
-            const StepPos of_w = step_pos<R>(sq, k + 1, k1, a.C);
-            lw.load(static_cast<const char*>(a.W) + of_w.row * stride_w + 2 * (int64_t)h * a.d_k, stride_w, a.d_k, of_w.valid, tid);
-        }
     };
     auto bring = [&](int64_t k) {
         lk.store(lds + LY::K_AT + (k & 1) * LY::ROWS, tid);
         lq.store(lds + LY::Q_AT, tid);
-        lo.store(lds + LY::O_AT, tid);
+        lo.store(lds + LY::O_AT + (k & 1) * LY::O_ROWS, tid);
         lg.store(gates + (k & 1) * StepGates<R>::FLOATS, a.scale, tid);
-        if constexpr (DELTA) lw.store(lds + LY::W_AT, tid);
+    };
+    auto request_w = [&](int64_t k) {
+        if constexpr (DELTA) {
+            const StepPos at = step_pos<R>(sq, k, k1, a.C);
+            lw.load(static_cast<const char*>(a.W) + at.row * stride_w + 2 * (int64_t)h * a.d_k, stride_w, a.d_k, at.valid, tid);
+        }
     };
     // P, as operands of P^T: token rows 4 q + r, column n; a share of the tiles a wavefront (one without a tile forms the last one again)
     constexpr int SHARE = (TILES + 3) / 4;
@@ -219,6 +221,8 @@ __device__ __forceinline__ void attn_bwd_state(const AttnBwdArgs& a, char* const
         while (idx > it) idx -= ++it;
         its[j] = it, jts[j] = idx, units[j] = LY::UNIT * (unit_at<LY>(idx) + (it >> 1) - (idx >> 1)) + 8 * (it & 1);
     }
+    v2u p_parts[SHARE][FP];
+    v4f x_tiles[2 * KP];
     auto scores = [&](int64_t k) {
         const float* const gl = gates + (k & 1) * StepGates<R>::FLOATS;
         const char* const rows_k = lds + LY::K_AT + (k & 1) * LY::ROWS;
@@ -252,48 +256,23 @@ __device__ __forceinline__ void attn_bwd_state(const AttnBwdArgs& a, char* const
             const bool on = jts[j] == its[j];
 #pragma unroll
             for (int r = 0; r < 4; ++r) x[j][r] *= a.scale * __expf(on && ln.n > 4 * ln.q + r ? -__builtin_inff() : gi[j][r] - gj[j]);
-            char* unit = lds + LY::P_AT + units[j] + in_place(lane16);
 #pragma unroll
             for (int part = 0; part < FP; ++part) {
-                const v2u u = pack4<OP>(x[j]);
-                *reinterpret_cast<v2u*>(unit + 1024 * part) = u;
-                if (on && (its[j] & 1)) *reinterpret_cast<v2u*>(unit + 1024 * part - 8) = v2u{0u, 0u};  // the pair's other tile lies above the diagonal
-                x[j] = minus16<OP>(x[j], u);
+                p_parts[j][part] = pack4<OP>(x[j]);
+                x[j] = minus16<OP>(x[j], p_parts[j][part]);
             }
         }
     };
-    auto products = [&](int64_t k) {  // P^T dO and scale Q^T diag(G) dO of this wavefront's columns
+    auto products = [&](int64_t k) {  // X of this wavefront's columns
         const float* const gl = gates + (k & 1) * StepGates<R>::FLOATS;
-        v4u o[MT / 2], pt[FP][MT], qt[2][KP];
-        v4f y[MT], od[MT], x[2 * KP];
-        auto scores_of = [&](int tp, int part) {
-#pragma unroll
-            for (int jt = 0; jt <= 2 * tp + 1; ++jt) pt[part][jt] = *reinterpret_cast<const v4u*>(lds + LY::P_AT + LY::UNIT * (LY::units_before(jt) + tp - jt / 2) + 1024 * part + lane16);
-        };
-        auto queries_of = [&](int stage) {
-#pragma unroll
-            for (int i = 0; i < KP; ++i) qt[stage & 1][i] = lds_turned_tile<PIECES>(lds + LY::Q_AT, stage >> 1, KP * (stage & 1) + i, ln);
-        };
-        auto add_y = [&](int tp, int part) {
-#pragma unroll
-            for (int jt = 0; jt <= 2 * tp + 1; ++jt) y[jt] = mfma32<OP>(pt[part][jt], o[tp], y[jt]);
-        };
-#pragma unroll
-        for (int tp = 0; tp < MT / 2; ++tp) {
-            const int row = 32 * tp + 4 * ln.q + (ln.n >> 2), col4 = 4 * w4 + (ln.n & 3);
-            const v2u u = lds_turned<LY::UPIECES>(lds + LY::O_AT, row, col4), v = lds_turned<LY::UPIECES>(lds + LY::O_AT, row + 16, col4);
-            o[tp] = v4u{u[0], u[1], v[0], v[1]};
-        }
-#pragma unroll
-        for (int tb = 0; tb < MT; ++tb) od[tb] = *reinterpret_cast<const v4f*>(gl + 2 * R + 16 * tb + 4 * ln.q);
-#pragma unroll
-        for (int part = FP - 1; part >= 0; --part) scores_of(0, part);
-        in_order();
+        const char* const rows_o = lds + LY::O_AT + (k & 1) * LY::O_ROWS;
+        v4f od[MT];
 #pragma unroll
         for (int tb = 0; tb < MT; ++tb) {
-            const v4f u = unpack4<OP>(v2u{o[tb / 2][2 * (tb & 1)], o[tb / 2][2 * (tb & 1) + 1]});
+            const v4f u = unpack4<OP>(lds_turned<LY::UPIECES>(rows_o, 16 * tb + 4 * ln.q + (ln.n >> 2), 4 * w4 + (ln.n & 3)));
+            const v4f e = *reinterpret_cast<const v4f*>(gl + 2 * R + 16 * tb + 4 * ln.q);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) od[tb][r] *= u[r];
+            for (int r = 0; r < 4; ++r) od[tb][r] = u[r] * e[r];
         }
         int shift = 0;
         if constexpr (OP == OP_F16) {
@@ -302,57 +281,49 @@ __device__ __forceinline__ void attn_bwd_state(const AttnBwdArgs& a, char* const
             for (int tb = 0; tb < MT; ++tb) od[tb] = times(od[tb], pow2(shift));
         }
         Parts<FP> vp[MT / 2];
-        queries_of(0);
         split_pairs<OP, FP, MT / 2>(od, vp, minus);
 #pragma unroll
-        for (int i = 0; i < 2 * KP; ++i) x[i] = zero4();
+        for (int i = 0; i < 2 * KP; ++i) x_tiles[i] = zero4();
+        add_turned<OP, MT, KP>(x_tiles, lds + LY::Q_AT, vp, ln);
+        if constexpr (OP == OP_F16) {
 #pragma unroll
-        for (int jt = 0; jt < MT; ++jt) y[jt] = zero4();
-        auto add_x = [&](int stage) {
-            if (stage + 1 < MT) queries_of(stage + 1);
-            in_order();
-#pragma unroll
-            for (int part = FP - 1; part >= 0; --part)
-#pragma unroll
-                for (int i = 0; i < KP; ++i) x[KP * (stage & 1) + i] = mfma32<OP>(qt[stage & 1][i], vp[stage >> 1].u[part], x[KP * (stage & 1) + i]);
-        };
-        in_order();
-#pragma unroll
-        for (int part = FP - 1; part >= 0; --part) add_y(0, part);
-        if constexpr (MT == 4) {
-#pragma unroll
-            for (int part = FP - 1; part >= 1; --part) scores_of(1, part);
+            for (int i = 0; i < 2 * KP; ++i) x_tiles[i] = times(x_tiles[i], pow2(-shift));
         }
-        add_x(0);
-        add_x(1);
-        if constexpr (MT == 4) {
+    };
+    auto put = [&]() {
 #pragma unroll
-            for (int part = FP - 1; part >= 1; --part) add_y(1, part);
-            scores_of(1, 0);
-            add_x(2);
-            add_y(1, 0);
-            add_x(3);
+        for (int i = 0; i < 2 * KP; ++i) *reinterpret_cast<v4f*>(lds + LY::X_AT + LY::X_WAVE * w4 + 1024 * i + lane16) = x_tiles[i];
+#pragma unroll
+        for (int j = 0; j < SHARE; ++j) {
+            char* unit = lds + LY::P_AT + units[j] + in_place(lane16);
+#pragma unroll
+            for (int part = 0; part < FP; ++part) {
+                *reinterpret_cast<v2u*>(unit + 1024 * part) = p_parts[j][part];
+                if (jts[j] == its[j] && (its[j] & 1)) *reinterpret_cast<v2u*>(unit + 1024 * part - 8) = v2u{0u, 0u};  // the pair's other tile lies above the diagonal
+            }
         }
-#pragma unroll
-        for (int jt = 0; jt < MT; ++jt) *reinterpret_cast<v4f*>(lds + LY::Y_AT + LY::Y_WAVE * w4 + 1024 * jt + lane16) = y[jt];
-#pragma unroll
-        for (int i = 0; i < 2 * KP; ++i) *reinterpret_cast<v4f*>(lds + LY::X_AT + LY::X_WAVE * w4 + 1024 * i + lane16) = OP == OP_F16 ? times(x[i], pow2(-shift)) : x[i];
     };
     request(k1 - 1);
     bring(k1 - 1);
     request(k1 - 2);
+    request_w(k1 - 1);
     __syncthreads();
     scores(k1 - 1);
-    __syncthreads();
     products(k1 - 1);
     __syncthreads();
+    put();
+    bring(k1 - 2);
+    request(k1 - 3);
+    __syncthreads();
     for (int64_t k = k1 - 1; k >= 0; --k) {
-        bring(k - 1);
-        request(k - 2);
-        __syncthreads();  // the rows are in LDS
+        if constexpr (DELTA) lw.store(lds + LY::W_AT, tid);
+        request_w(k - 1);
         scores(k - 1);
-        __syncthreads();  // P is in LDS
         products(k - 1);
+        __syncthreads();  // K, Q, dO, P and X in LDS are used up
+        put();
+        bring(k - 2);
+        request(k - 3);
         __syncthreads();
     }
 }
