@@ -52,8 +52,8 @@ template <class LY> __device__ __forceinline__ int unit_at(int jt)  // units_bef
 
 // dS from the last step to the first, a workgroup per head and 64 columns as in the forward pass.  Four wavefronts carry the recursion; four others are a step
 // ahead with what does not depend on it: P, whose parts go round through LDS, and X = scale Q^T diag(G) dO in fp32.
-//     first half     K dS', dV', G_C dS' + X            P and X of the step before, in registers; W to LDS
-//     second half    dU, W^T dV', the parts of dS       P and X to LDS, and the rows of the step before that
+//     first half     K dS', dV', G_C dS' + X            W and the rows of the step before to LDS
+//     second half    dU, W^T dV', the parts of dS       P and X of the step before
 template <int OP, int MT, int KP, bool DELTA, bool TWO>
 __device__ __forceinline__ void attn_bwd_state(const AttnBwdArgs& a, char* const lds, unsigned b)
 {
@@ -92,7 +92,6 @@ __device__ __forceinline__ void attn_bwd_state(const AttnBwdArgs& a, char* const
             split_pairs<OP, FP, KP>(x, sp, minus);
         };
         parts_of_state();
-        __syncthreads();
         __syncthreads();
         __syncthreads();  // the last step's rows, P and X are in LDS
         for (int64_t k = k1 - 1; k >= 0; --k) {
@@ -221,8 +220,6 @@ __device__ __forceinline__ void attn_bwd_state(const AttnBwdArgs& a, char* const
         while (idx > it) idx -= ++it;
         its[j] = it, jts[j] = idx, units[j] = LY::UNIT * (unit_at<LY>(idx) + (it >> 1) - (idx >> 1)) + 8 * (it & 1);
     }
-    v2u p_parts[SHARE][FP];
-    v4f x_tiles[2 * KP];
     auto scores = [&](int64_t k) {
         const float* const gl = gates + (k & 1) * StepGates<R>::FLOATS;
         const char* const rows_k = lds + LY::K_AT + (k & 1) * LY::ROWS;
@@ -256,17 +253,20 @@ __device__ __forceinline__ void attn_bwd_state(const AttnBwdArgs& a, char* const
             const bool on = jts[j] == its[j];
 #pragma unroll
             for (int r = 0; r < 4; ++r) x[j][r] *= a.scale * __expf(on && ln.n > 4 * ln.q + r ? -__builtin_inff() : gi[j][r] - gj[j]);
+            char* unit = lds + LY::P_AT + units[j] + in_place(lane16);
 #pragma unroll
             for (int part = 0; part < FP; ++part) {
-                p_parts[j][part] = pack4<OP>(x[j]);
-                x[j] = minus16<OP>(x[j], p_parts[j][part]);
+                const v2u u = pack4<OP>(x[j]);
+                *reinterpret_cast<v2u*>(unit + 1024 * part) = u;
+                if (on && (its[j] & 1)) *reinterpret_cast<v2u*>(unit + 1024 * part - 8) = v2u{0u, 0u};  // the pair's other tile lies above the diagonal
+                x[j] = minus16<OP>(x[j], u);
             }
         }
     };
     auto products = [&](int64_t k) {  // X of this wavefront's columns
         const float* const gl = gates + (k & 1) * StepGates<R>::FLOATS;
         const char* const rows_o = lds + LY::O_AT + (k & 1) * LY::O_ROWS;
-        v4f od[MT];
+        v4f od[MT], x[2 * KP];
 #pragma unroll
         for (int tb = 0; tb < MT; ++tb) {
             const v4f u = unpack4<OP>(lds_turned<LY::UPIECES>(rows_o, 16 * tb + 4 * ln.q + (ln.n >> 2), 4 * w4 + (ln.n & 3)));
@@ -283,47 +283,27 @@ __device__ __forceinline__ void attn_bwd_state(const AttnBwdArgs& a, char* const
         Parts<FP> vp[MT / 2];
         split_pairs<OP, FP, MT / 2>(od, vp, minus);
 #pragma unroll
-        for (int i = 0; i < 2 * KP; ++i) x_tiles[i] = zero4();
-        add_turned<OP, MT, KP>(x_tiles, lds + LY::Q_AT, vp, ln);
-        if constexpr (OP == OP_F16) {
+        for (int i = 0; i < 2 * KP; ++i) x[i] = zero4();
+        add_turned<OP, MT, KP>(x, lds + LY::Q_AT, vp, ln);
 #pragma unroll
-            for (int i = 0; i < 2 * KP; ++i) x_tiles[i] = times(x_tiles[i], pow2(-shift));
-        }
-    };
-    auto put = [&]() {
-#pragma unroll
-        for (int i = 0; i < 2 * KP; ++i) *reinterpret_cast<v4f*>(lds + LY::X_AT + LY::X_WAVE * w4 + 1024 * i + lane16) = x_tiles[i];
-#pragma unroll
-        for (int j = 0; j < SHARE; ++j) {
-            char* unit = lds + LY::P_AT + units[j] + in_place(lane16);
-#pragma unroll
-            for (int part = 0; part < FP; ++part) {
-                *reinterpret_cast<v2u*>(unit + 1024 * part) = p_parts[j][part];
-                if (jts[j] == its[j] && (its[j] & 1)) *reinterpret_cast<v2u*>(unit + 1024 * part - 8) = v2u{0u, 0u};  // the pair's other tile lies above the diagonal
-            }
-        }
+        for (int i = 0; i < 2 * KP; ++i) *reinterpret_cast<v4f*>(lds + LY::X_AT + LY::X_WAVE * w4 + 1024 * i + lane16) = OP == OP_F16 ? times(x[i], pow2(-shift)) : x[i];
     };
     request(k1 - 1);
+    request_w(k1 - 1);
     bring(k1 - 1);
     request(k1 - 2);
-    request_w(k1 - 1);
     __syncthreads();
     scores(k1 - 1);
     products(k1 - 1);
     __syncthreads();
-    put();
-    bring(k1 - 2);
-    request(k1 - 3);
-    __syncthreads();
     for (int64_t k = k1 - 1; k >= 0; --k) {
         if constexpr (DELTA) lw.store(lds + LY::W_AT, tid);
+        bring(k - 1);
+        __syncthreads();  // P and X in LDS are used up, the rows are there
         request_w(k - 1);
         scores(k - 1);
+        request(k - 2);
         products(k - 1);
-        __syncthreads();  // K, Q, dO, P and X in LDS are used up
-        put();
-        bring(k - 2);
-        request(k - 3);
         __syncthreads();
     }
 }
