@@ -31,17 +31,19 @@ template <size_t NI, size_t NO> bool aliased(const Span (&in)[NI], const Span (&
     return false;
 }
 
-// Segments of a sequence, each a workgroup per head and 64 columns.
-int attn_segments(int n_seq, int64_t n_chunk, int H, int d_v)
+// Segments of a sequence, so that its heads and groups of 64 columns fill the 256 compute units.  With W a segment's state costs as much as its outputs: it pays where
+// there are four of them at least (8192 tokens in chunks of 64, d_k = d_v = 128, in us, segments in brackets: 8 heads 376 [1], 110 [16]; 16 heads 371 [1], 135 [8]; 32
+// heads 382 [1], 232 [4], 253 [8]; 48 heads 407 [1], 418 [2], 387 [5]; 64 heads 384 [1], 452 [4]; 96 heads 417 [1], 686 [4]).  Without W the states are half the
+// work, and twice the segments: 16 heads 328 [1], 88 [16]; 32 heads 327 [1], 150 [8]; 64 heads 337 [1], 257 [4]; 80 heads 341 [1], 336 [3]; 96 heads 348 [1], 446 [3].
+int attn_segments(int n_seq, int64_t n_chunk, int H, int d_v, bool has_w)
 {
-    const int64_t units = (int64_t)n_seq * H * ((d_v + 63) / 64);
-    if (units >= 192 || n_chunk < 16 * (int64_t)n_seq) return 1;
-    const int64_t by_units = 512 / units, by_chunks = n_chunk / n_seq / 8;
+    const int64_t units = (int64_t)n_seq * H * ((d_v + 63) / 64), by_units = (has_w ? 256 : 512) / units, by_chunks = n_chunk / n_seq / 8;
+    if (by_units < 4 || by_chunks < 2) return 1;
     return (int)(by_units < by_chunks ? by_units : by_chunks);
 }
 int64_t attn_workspace(int n_seq, int64_t n_chunk, int H, int d_k, int d_v, bool has_w)
 {
-    const int64_t n_seg = attn_segments(n_seq, n_chunk, H, d_v);
+    const int64_t n_seg = attn_segments(n_seq, n_chunk, H, d_v, has_w);
     return (n_seg - 1) * n_seq * H * 4 * ((int64_t)d_k * d_v + (has_w ? (int64_t)d_k * d_k : 1));
 }
 
@@ -75,7 +77,7 @@ int attn_common(const void* Q, const void* K, const void* U, const void* W, cons
     if (aliased(in, out)) return TRIINV_ERR_ALIAS;
     if (state && state == final_state && (overlap(state, st, O, v) || overlap(state, st, workspace, need))) return TRIINV_ERR_ALIAS;
     const AttnCall a{Q, K, U, W, g, state, O, final_state, static_cast<char*>(workspace), cu_seqlens, cu_chunks, Tlen, n_seq, n_chunk, H, H_k, d_k, d_v, C,
-                     attn_segments(n_seq, n_chunk, H, d_v), scale, static_cast<hipStream_t>(hip_stream)};
+                     attn_segments(n_seq, n_chunk, H, d_v, W != nullptr), scale, static_cast<hipStream_t>(hip_stream)};
     return finish(dtype == TRIINV_F16 ? launch_chunk_attn_f16(a) : launch_chunk_attn_bf16(a));
 }
 

@@ -15,21 +15,40 @@ namespace {
 
 typedef float v8f __attribute__((ext_vector_type(8)));
 
+// Eight elements as they are in memory, and widened.
+template <int DT> struct Raw8 {
+    v4u u[DT == OP_F32 ? 2 : 1];
+    __device__ __forceinline__ void load(const void* p, int64_t i)
+    {
+        const v4u* const from = reinterpret_cast<const v4u*>(static_cast<const char*>(p) + i * (DT == OP_F32 ? 4 : 2));
+        u[0] = from[0];
+        if constexpr (DT == OP_F32) u[1] = from[1];
+    }
+    __device__ __forceinline__ void clear()
+    {
+        u[0] = v4u{0u, 0u, 0u, 0u};
+        if constexpr (DT == OP_F32) u[1] = u[0];
+    }
+    __device__ __forceinline__ v8f wide() const
+    {
+        v8f o;
+        if constexpr (DT == OP_F32) {
+            o = __builtin_shufflevector(__builtin_bit_cast(v4f, u[0]), __builtin_bit_cast(v4f, u[1]), 0, 1, 2, 3, 4, 5, 6, 7);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint16_t x = (uint16_t)(u[0][e >> 1] >> (16 * (e & 1)));
+                o[e] = DT == OP_F16 ? f16_to_f32(x) : bf16_to_f32(x);
+            }
+        }
+        return o;
+    }
+};
 template <int DT> __device__ __forceinline__ v8f load8(const void* p, int64_t i)
 {
-    v8f o;
-    if constexpr (DT == OP_F32) {
-        const v4f a = *reinterpret_cast<const v4f*>(static_cast<const float*>(p) + i), b = *reinterpret_cast<const v4f*>(static_cast<const float*>(p) + i + 4);
-        o = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-    } else {
-        const v4u u = *reinterpret_cast<const v4u*>(static_cast<const uint16_t*>(p) + i);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint16_t x = (uint16_t)(u[e >> 1] >> (16 * (e & 1)));
-            o[e] = DT == OP_F16 ? f16_to_f32(x) : bf16_to_f32(x);
-        }
-    }
-    return o;
+    Raw8<DT> r;
+    r.load(p, i);
+    return r.wide();
 }
 // x rounded to the type, and written.
 template <int DT> __device__ __forceinline__ v8f store8(void* p, int64_t i, v8f x)
@@ -213,8 +232,8 @@ template <int DT, int PIECES, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void k_norm_bwd(NormBwdCall a)
 {
     constexpr int LANES = 64 * WAVES;
-    __shared__ v2f sums[WAVES];
-    const int lane = threadIdx.x;
+    __shared__ v2f sums[2][WAVES];  // of one row and the next: one barrier a row
+    const int lane = threadIdx.x, wave = lane >> 6;
     v8f w[PIECES], dw[PIECES];
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
@@ -222,22 +241,39 @@ __global__ __launch_bounds__(64 * WAVES) void k_norm_bwd(NormBwdCall a)
         dw[i] = w[i] = v8f{0, 0, 0, 0, 0, 0, 0, 0};
         if (c < a.D) w[i] = load8<DT>(a.weight, c);
     }
-    for (int64_t row = blockIdx.x; row < a.N; row += gridDim.x) {
-        const int64_t at = row * a.D;
-        v8f x[PIECES], d[PIECES];
-        v2f s = {0.f, 0.f};
+    Raw8<DT> rx[PIECES], rd[PIECES], rt[PIECES];
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) rx[i].clear(), rd[i].clear(), rt[i].clear();
+    auto request = [&](int64_t row) {
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             const int c = 8 * (lane + LANES * i);
-            x[i] = d[i] = v8f{0, 0, 0, 0, 0, 0, 0, 0};
-            if (c < a.D) x[i] = load8<DT>(a.x, at + c), d[i] = load8<DT>(a.dy, at + c);
+            if (c >= a.D) continue;
+            rx[i].load(a.x, row * a.D + c), rd[i].load(a.dy, row * a.D + c);
+            if (a.dsum) rt[i].load(a.dsum, row * a.D + c);
         }
+    };
+    if (blockIdx.x < a.N) request(blockIdx.x);
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < a.N; row += gridDim.x, turn ^= 1) {
+        const int64_t at = row * a.D;
+        v8f x[PIECES], d[PIECES], t[PIECES];
+        v2f s = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) x[i] = rx[i].wide(), d[i] = rd[i].wide(), t[i] = rt[i].wide();
+        if (row + gridDim.x < a.N) request(row + gridDim.x);  // the next row comes while this one is at work
 #pragma unroll
         for (int i = 0; i < PIECES; ++i)
 #pragma unroll
             for (int e = 0; e < 8; ++e) s[0] += x[i][e] * x[i][e], s[1] += d[i][e] * w[i][e] * x[i][e];
         s[0] = lanes_sum(s[0], 64), s[1] = lanes_sum(s[1], 64);
-        s = across_waves<WAVES>(s, sums, [](v2f p, v2f q) { return v2f{p[0] + q[0], p[1] + q[1]}; });
+        if constexpr (WAVES > 1) {
+            if ((lane & 63) == 0) sums[turn][wave] = s;
+            __syncthreads();
+            s = sums[turn][0];
+#pragma unroll
+            for (int i = 1; i < WAVES; ++i) s[0] += sums[turn][i][0], s[1] += sums[turn][i][1];
+        }
         const float rstd = 1.f / sqrtf(s[0] / (float)a.D + a.eps), m = s[1] / (float)a.D * rstd * rstd;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
@@ -247,12 +283,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_norm_bwd(NormBwdCall a)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 dw[i][e] += d[i][e] * (x[i][e] * rstd);
-                dx[e] = rstd * (d[i][e] * w[i][e] - x[i][e] * m);
-            }
-            if (a.dsum) {
-                const v8f t = load8<DT>(a.dsum, at + c);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) dx[e] += t[e];
+                dx[e] = rstd * (d[i][e] * w[i][e] - x[i][e] * m) + t[i][e];
             }
             store8<DT>(a.dx, at + c, dx);
         }
@@ -264,20 +295,23 @@ __global__ __launch_bounds__(64 * WAVES) void k_norm_bwd(NormBwdCall a)
     }
 }
 
-// dweight[c] = sum of partial[group][c]: 64 columns a workgroup, 16 threads a column.
+// dweight[c] = sum of partial[group][c]: 16 columns a workgroup, 64 threads a column, in the same order every time.
 __global__ __launch_bounds__(1024) void k_norm_dweight(const float* partial, float* dweight, int groups, int D)
 {
-    __shared__ float part[16][64];
-    const int cx = threadIdx.x & 63, y = threadIdx.x >> 6, c = 64 * blockIdx.x + cx;
+    __shared__ float part[64][17];
+    const int cx = threadIdx.x & 15, y = threadIdx.x >> 4, c = 16 * blockIdx.x + cx;
     float s = 0.f;
-    if (c < D)
-        for (int g = y; g < groups; g += 16) s += partial[(int64_t)g * D + c];
+    if (c < D) {
+#pragma unroll 8
+        for (int g = y; g < groups; g += 64) s += partial[(int64_t)g * D + c];
+    }
     part[y][cx] = s;
     __syncthreads();
-    if (y == 0 && c < D) {
-        for (int i = 1; i < 16; ++i) s += part[i][cx];
-        dweight[c] = s;
+    for (int half = 32; half > 0; half /= 2) {
+        if (y < half) part[y][cx] = s += part[y + half][cx];
+        __syncthreads();
     }
+    if (y == 0 && c < D) dweight[c] = s;
 }
 
 template <int DT, int WAVES> int bwd_pieces(const NormBwdCall& a)
@@ -286,15 +320,14 @@ template <int DT, int WAVES> int bwd_pieces(const NormBwdCall& a)
     const dim3 grid((unsigned)a.groups), block(64 * WAVES);
     if (pieces <= 1) return launch_kernel(false, k_norm_bwd<DT, 1, WAVES>, grid, block, 0, a.stream, a);
     if (pieces <= 2) return launch_kernel(false, k_norm_bwd<DT, 2, WAVES>, grid, block, 0, a.stream, a);
-    if (pieces <= 4) return launch_kernel(false, k_norm_bwd<DT, 4, WAVES>, grid, block, 0, a.stream, a);
     return NOT_BUILT;
 }
 template <int DT> int bwd(const NormBwdCall& a)
 {
-    if (a.groups == 0) return launch_kernel(false, k_norm_dweight, dim3((unsigned)((a.D + 63) / 64)), dim3(1024), 0, a.stream, a.partial, a.dweight, 0, a.D);
-    const int rc = a.D <= 512 ? bwd_pieces<DT, 1>(a) : a.D <= 4096 ? bwd_pieces<DT, 4>(a) : bwd_pieces<DT, 8>(a);
+    if (a.groups == 0) return launch_kernel(false, k_norm_dweight, dim3((unsigned)((a.D + 15) / 16)), dim3(1024), 0, a.stream, a.partial, a.dweight, 0, a.D);
+    const int rc = a.D <= 512 ? bwd_pieces<DT, 1>(a) : a.D <= 4096 ? bwd_pieces<DT, 4>(a) : a.D <= 8192 ? bwd_pieces<DT, 8>(a) : bwd_pieces<DT, 16>(a);
     if (rc != LAUNCHED) return rc;
-    return launch_kernel(false, k_norm_dweight, dim3((unsigned)((a.D + 63) / 64)), dim3(1024), 0, a.stream, a.partial, a.dweight, a.groups, a.D);
+    return launch_kernel(false, k_norm_dweight, dim3((unsigned)((a.D + 15) / 16)), dim3(1024), 0, a.stream, a.partial, a.dweight, a.groups, a.D);
 }
 
 }  // namespace
