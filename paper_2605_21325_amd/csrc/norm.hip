@@ -253,15 +253,17 @@ __global__ __launch_bounds__(64 * WAVES) void k_norm_bwd(NormBwdCall a)
             if (a.dsum) rt[i].load(a.dsum, row * a.D + c);
         }
     };
-    if (blockIdx.x < a.N) request(blockIdx.x);
+    constexpr bool AHEAD = PIECES <= 2;  // the next row comes while one is at work; four pieces of both do not fit in registers
+    if (AHEAD && blockIdx.x < a.N) request(blockIdx.x);
     int turn = 0;
     for (int64_t row = blockIdx.x; row < a.N; row += gridDim.x, turn ^= 1) {
         const int64_t at = row * a.D;
+        if (!AHEAD) request(row);
         v8f x[PIECES], d[PIECES], t[PIECES];
         v2f s = {0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) x[i] = rx[i].wide(), d[i] = rd[i].wide(), t[i] = rt[i].wide();
-        if (row + gridDim.x < a.N) request(row + gridDim.x);  // the next row comes while this one is at work
+        if (AHEAD && row + gridDim.x < a.N) request(row + gridDim.x);
 #pragma unroll
         for (int i = 0; i < PIECES; ++i)
 #pragma unroll
@@ -320,12 +322,15 @@ template <int DT, int WAVES> int bwd_pieces(const NormBwdCall& a)
     const dim3 grid((unsigned)a.groups), block(64 * WAVES);
     if (pieces <= 1) return launch_kernel(false, k_norm_bwd<DT, 1, WAVES>, grid, block, 0, a.stream, a);
     if (pieces <= 2) return launch_kernel(false, k_norm_bwd<DT, 2, WAVES>, grid, block, 0, a.stream, a);
+    if constexpr (WAVES == 8) {
+        if (pieces <= 4) return launch_kernel(false, k_norm_bwd<DT, 4, WAVES>, grid, block, 0, a.stream, a);
+    }
     return NOT_BUILT;
 }
 template <int DT> int bwd(const NormBwdCall& a)
 {
     if (a.groups == 0) return launch_kernel(false, k_norm_dweight, dim3((unsigned)((a.D + 15) / 16)), dim3(1024), 0, a.stream, a.partial, a.dweight, 0, a.D);
-    const int rc = a.D <= 512 ? bwd_pieces<DT, 1>(a) : a.D <= 4096 ? bwd_pieces<DT, 4>(a) : a.D <= 8192 ? bwd_pieces<DT, 8>(a) : bwd_pieces<DT, 16>(a);
+    const int rc = a.D <= 512 ? bwd_pieces<DT, 1>(a) : a.D <= 4096 ? bwd_pieces<DT, 4>(a) : bwd_pieces<DT, 8>(a);
     if (rc != LAUNCHED) return rc;
     return launch_kernel(false, k_norm_dweight, dim3((unsigned)((a.D + 15) / 16)), dim3(1024), 0, a.stream, a.partial, a.dweight, a.groups, a.D);
 }
