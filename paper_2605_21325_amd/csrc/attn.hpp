@@ -238,9 +238,27 @@ __global__ __launch_bounds__(512) void k_chunk_attn(AttnArgs a)
     const int tokens = a.C < R ? a.C : R, steps = a.C > R ? a.C / R : 1;  // of a step; of a chunk
     const int64_t all = (sq.len + tokens - 1) / tokens, k0 = c0 * steps, k1 = c1 * steps < all ? c1 * steps : all;
 
+    const int cols = a.d_v - wg_col < ATTN_COLS ? a.d_v - wg_col : ATTN_COLS;
+    const uint32_t stride_w = 2u * a.H * a.d_k, stride_u = 2u * a.H * a.d_v;
+    const int64_t row0 = sq.tok0 + k0 * tokens;
+
     if (wave < 4) {
-        // The recursion.
+        // The recursion, and W and U.
         const int col0 = wg_col + 16 * wave;
+        RowLoader<PIECES, R, 256> lw;
+        RowLoader<LY::UPIECES, R, 256> lu;
+        const char *at_w = static_cast<const char*>(a.W) + row0 * stride_w + 2 * h * a.d_k, *at_u = static_cast<const char*>(a.U) + row0 * stride_u + 2 * (h * a.d_v + wg_col);
+        auto request = [&](int64_t k) {
+            const StepPos at = step_pos<R>(sq, k, k1, a.C);
+            if constexpr (DELTA) lw.load(at_w, stride_w, a.d_k, at.valid, threadIdx.x);
+            lu.load(at_u, stride_u, cols, at.valid, threadIdx.x);
+            at_w += (int64_t)tokens * stride_w, at_u += (int64_t)tokens * stride_u;
+        };
+        auto bring = [&]() {
+            if constexpr (DELTA) lw.store(lds + LY::W_AT, threadIdx.x);
+            lu.store(lds + LY::U_AT, threadIdx.x);
+        };
+        request(k0);
         const MinusOne<OP> minus(ln);
         v4f S[2 * KP];
         const float* from = seg == 0 ? a.state : a.seg_state + (int64_t)(seg - 1) * a.map.n_seq * a.H * a.d_k * a.d_v;
@@ -270,6 +288,7 @@ __global__ __launch_bounds__(512) void k_chunk_attn(AttnArgs a)
             if (OP == OP_F16 && ln.q == 0 && ln.n == 0) shifts[wave] = shift;
         };
         parts_of_state(true);
+        bring();
         __syncthreads();  // the first rows are in LDS
         for (int64_t k = k0; k < k1; ++k) {
             const float* const gl = gates + (k & 1) * StepGates<R>::FLOATS;
@@ -278,6 +297,7 @@ __global__ __launch_bounds__(512) void k_chunk_attn(AttnArgs a)
 #pragma unroll
             for (int tb = 0; tb < MT; ++tb) u[tb] = lds_turned<LY::UPIECES>(lds + LY::U_AT, 16 * tb + 4 * ln.q + (ln.n >> 2), 4 * wave + (ln.n & 3));
             if constexpr (DELTA) rows_times<OP, MT, KP>(v, lds + LY::W_AT, sp, ln, [](int) {});
+            request(k + 1);
             __syncthreads();  // W, U, Q and the parts of S are in registers
             values_of<OP, MT, LY::UPIECES, DELTA>(v, u, s_shift);
             int v_shift = 0;
@@ -298,38 +318,31 @@ __global__ __launch_bounds__(512) void k_chunk_attn(AttnArgs a)
             }
             state_after<OP, MT, KP>(S, v, v_shift, lds + LY::K_AT + (k & 1) * LY::ROWS, gl + R, gl[3 * R], minus, ln);
             parts_of_state(((k + 1) & 1) == 0);
+            bring();
             __syncthreads();  // the parts of S and the next rows are in LDS
         }
         if (seg == a.n_seg - 1 && a.final_state) put_state<KP>(a.final_state + (int64_t)hs * a.d_k * a.d_v, S, a.d_k, a.d_v, col0, ln);
         return;
     }
 
-    // Rows, scores and outputs.
+    // K, Q and the gates, scores and outputs.
     const int tid = threadIdx.x - 256;
     const int hk = h / a.group, H_k = a.H / a.group;
-    RowLoader<PIECES, R, 256> lq, lk, lw;
-    RowLoader<LY::UPIECES, R, 256> lu;
+    RowLoader<PIECES, R, 256> lq, lk;
     StepGates<R> lg;
     // addresses of the next step to be requested
-    const int cols = a.d_v - wg_col < ATTN_COLS ? a.d_v - wg_col : ATTN_COLS;
-    const uint32_t stride_k = 2u * H_k * a.d_k, stride_w = 2u * a.H * a.d_k, stride_u = 2u * a.H * a.d_v;
-    const int64_t row0 = sq.tok0 + k0 * tokens;
-    const char *at_k = static_cast<const char*>(a.K) + row0 * stride_k + 2 * hk * a.d_k, *at_q = static_cast<const char*>(a.Q) + row0 * stride_k + 2 * hk * a.d_k,
-               *at_w = static_cast<const char*>(a.W) + row0 * stride_w + 2 * h * a.d_k, *at_u = static_cast<const char*>(a.U) + row0 * stride_u + 2 * (h * a.d_v + wg_col);
+    const uint32_t stride_k = 2u * H_k * a.d_k;
+    const char *at_k = static_cast<const char*>(a.K) + row0 * stride_k + 2 * hk * a.d_k, *at_q = static_cast<const char*>(a.Q) + row0 * stride_k + 2 * hk * a.d_k;
     auto request = [&](int64_t k) {
         const StepPos at = step_pos<R>(sq, k, k1, a.C);
         lk.load(at_k, stride_k, a.d_k, at.valid, tid);
-        if constexpr (DELTA) lw.load(at_w, stride_w, a.d_k, at.valid, tid);
-        lu.load(at_u, stride_u, cols, at.valid, tid);
         lq.load(at_q, stride_k, a.d_k, at.valid, tid);
         lg.load(a.g, at, a.H, h, tid);
-        at_k += (int64_t)tokens * stride_k, at_q += (int64_t)tokens * stride_k, at_w += (int64_t)tokens * stride_w, at_u += (int64_t)tokens * stride_u;
+        at_k += (int64_t)tokens * stride_k, at_q += (int64_t)tokens * stride_k;
     };
     auto bring = [&](int64_t k) {
         lk.store(lds + LY::K_AT + (k & 1) * LY::ROWS, tid);
-        if constexpr (DELTA) lw.store(lds + LY::W_AT, tid);
         lq.store(lds + LY::Q_AT, tid);
-        lu.store(lds + LY::U_AT, tid);
         lg.store(gates + (k & 1) * StepGates<R>::FLOATS, a.scale, tid);
     };
     request(k0);
