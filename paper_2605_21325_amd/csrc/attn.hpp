@@ -642,8 +642,8 @@ template <int KP> __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a)
     __shared__ __attribute__((aligned(16))) char lds[2][KP * 3 * 1024];
     const Lane ln = lane_id();
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane16 = 16 * (16 * ln.q + ln.n);
-    const unsigned groups = (a.d_v + 15) / 16, hs = blockIdx.x / groups;
-    const int col = 16 * (blockIdx.x % groups) + ln.n;
+    const unsigned groups = (a.d_v + 15) / 16, b = xcd_neighbours(blockIdx.x, gridDim.x), hs = b / groups;  // (a head's groups read the same M: from one L2)
+    const int col = 16 * (b % groups) + ln.n;
     const int64_t heads = (int64_t)a.map.n_seq * a.H;
     const bool mine = col < a.d_v;
     v4f S[TI];
