@@ -173,8 +173,8 @@ __device__ __forceinline__ int f16_shift(float most)
 __device__ __forceinline__ float pow2(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }
 
 // Rows of 16-byte pieces in LDS, a row's pieces permuted by the row: sixteen lanes that read one piece of sixteen rows find it in sixteen places, and eight
-// rows of a transposing read lie as far apart as they can (with the low bits of the row alone, four of them met in the same banks, and the kernels
-// waited for LDS half of their time).
+// rows of a transposing read lie as far apart as they can (with the low bits of the row alone four of them meet in the same banks: 4.1 of 7.1 thousand
+// cycles of LDS a step were conflicts).
 template <int PIECES> struct LdsRows {
     static constexpr int BYTES = PIECES * 16;
     static_assert(PIECES == 8 || PIECES == 16, "rows of 128 or 256 bytes");
