@@ -3,8 +3,8 @@
 //
 // Bound by memory: every element of S (fp32) is read and written once, 8 bytes for 6 operations.  A workgroup takes some columns of one
 // head, all its rows; a thread holds four columns of ROWS rows in registers, all loads in flight before the first is used; the two sums
-// over the rows (S^T k, then S^T q of the new state) are closed through LDS in a fixed order.  Measured: 256 sequences of 32 heads of 128 x 128, bf16, 214 us
-// (5.0 TB/s), one of 16 heads 4.6 (a launch).
+// over the rows (S^T k, then S^T q of the new state) are closed through LDS in a fixed order.  Measured: 256 sequences of 32 heads of 128 x 128 in the slots of a pool, bf16,
+// 200 us (5.4 TB/s), one of 16 heads 4.6 (a launch).
 #include "layer.hpp"
 #include "tile_ops.hpp"
 
@@ -30,10 +30,11 @@ template <int DT> __device__ __forceinline__ void put_elem(void* p, int64_t i, f
 
 constexpr int THREADS = 256;
 
-// CG threads side by side, four columns each; THREADS / CG of them take a row in turn.
+// CG threads side by side, four columns each; THREADS / CG of them take a row in turn.  PASSING: states that no cache keeps until the next token.
 template <int DT, int CG, int ROWS> __global__ __launch_bounds__(THREADS) void k_gdn_step(StepCall a)
 {
     constexpr int RG = THREADS / CG;
+    constexpr bool PASSING = CG == 16;
     __shared__ float kq[2][RG * ROWS];
     __shared__ v4f part[RG][CG + 1];
     const int tid = threadIdx.x, cx = tid % CG, rg = tid / CG;
@@ -53,7 +54,8 @@ template <int DT, int CG, int ROWS> __global__ __launch_bounds__(THREADS) void k
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
         const int row = rg + RG * i;
-        s[i] = mine && row < a.d_k ? *reinterpret_cast<const v4f*>(S + (int64_t)row * a.d_v) : zero4();
+        const v4f* const from = reinterpret_cast<const v4f*>(S + (int64_t)row * a.d_v);
+        s[i] = !mine || row >= a.d_k ? zero4() : PASSING ? __builtin_nontemporal_load(from) : *from;
     }
     for (int i = tid; i < RG * ROWS; i += THREADS) {
         kq[0][i] = i < a.d_k ? elem<DT>(a.k, ((int64_t)b * a.H_k + hk) * a.d_k + i) : 0.f;
@@ -97,7 +99,11 @@ template <int DT, int CG, int ROWS> __global__ __launch_bounds__(THREADS) void k
         const int row = rg + RG * i;
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[i][e] += kq[0][row] * v[e];
-        if (mine && row < a.d_k) *reinterpret_cast<v4f*>(S + (int64_t)row * a.d_v) = s[i];
+        v4f* const to = reinterpret_cast<v4f*>(S + (int64_t)row * a.d_v);
+        if (mine && row < a.d_k) {
+            if constexpr (PASSING) __builtin_nontemporal_store(s[i], to);
+            else *to = s[i];
+        }
     }
     const v4f o = sum_rows(kq[1]);
     if (mine && rg == 0)
@@ -113,9 +119,9 @@ template <int DT, int CG> int go(const StepCall& a)
     if (a.d_k <= 128) return launch_kernel(false, k_gdn_step<DT, CG, 128 / RG>, grid, dim3(THREADS), 0, a.stream, a);
     return launch_kernel(false, k_gdn_step<DT, CG, 256 / RG>, grid, dim3(THREADS), 0, a.stream, a);
 }
-// 32 columns a workgroup where those of 128 would leave compute units without work (16 heads of 128 x 128, bf16, one and the other in us: one sequence 4.6 and 5.3,
-// four 5.1 and 5.7, eight 6.8 and 6.8, sixteen 11.4 and 8.3, 64 34 and 33; 256 of 32 heads 217 and 210).
-template <int DT> int pick(const StepCall& a) { return (int64_t)a.B * a.H * ((a.d_v + 31) / 32) <= 512 ? go<DT, 8>(a) : go<DT, 32>(a); }
+// 32 columns a workgroup where those of 64 would leave compute units without work (16 heads of 128 x 128, bf16, in us: one sequence 4.6 and 4.6, four 5.1 and 5.4,
+// eight 6.7 and 6.2, sixteen 11.4 and 7.8, 64 34 and 26; 256 of 32 heads 217 and 187, where loads and stores that stay in the caches take 209).
+template <int DT> int pick(const StepCall& a) { return (int64_t)a.B * a.H * ((a.d_v + 31) / 32) < 512 ? go<DT, 8>(a) : go<DT, 16>(a); }
 
 }  // namespace
 
