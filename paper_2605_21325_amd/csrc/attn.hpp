@@ -32,6 +32,7 @@ struct AttnArgs {
     // the one before it, or the states before the segments from them.
     float *seg_state, *seg_trans, *seg_decay;
     float *rec_state, *rec_value;  // for the gradient: the states before the steps [step][H], and V' where it is not U, [first token of the step][H], as put_turned leaves them
+    float* rec_dg;                 // zeroed where two workgroups add to it
     SeqMap map;
     int H, group, d_k, d_v, C;  // group: heads that share a key head
     int n_seg;
@@ -41,7 +42,7 @@ struct AttnArgs {
 // Chunks of segment `seg` of a sequence of n.
 __device__ __forceinline__ void segment_chunks(int64_t n, int n_seg, int seg, int64_t& first, int64_t& last)
 {
-    const int64_t per = (n + n_seg - 1) / n_seg;
+    const int64_t per = ((uint32_t)n + n_seg - 1u) / (uint32_t)n_seg;  // (a sequence of 2^31 chunks fits in no memory)
     first = per * seg < n ? per * seg : n;
     last = first + per < n ? first + per : n;
 }
@@ -236,11 +237,11 @@ __global__ __launch_bounds__(512) void k_chunk_attn(AttnArgs a)
     const int h = hs % a.H, s = hs / a.H;
     const int wg_col = cg * ATTN_COLS;
     const SeqPos sq = seq_pos(a.map, s);
-    const int64_t n_chunk = (sq.len + a.C - 1) / a.C;
+    const int64_t n_chunk = pieces_of(sq.len, a.C);
     int64_t c0, c1;
     segment_chunks(n_chunk, a.n_seg, seg, c0, c1);
     const int tokens = a.C < R ? a.C : R, steps = a.C > R ? a.C / R : 1;  // of a step; of a chunk
-    const int64_t all = (sq.len + tokens - 1) / tokens, k0 = c0 * steps, k1 = c1 * steps < all ? c1 * steps : all;
+    const int64_t all = pieces_of(sq.len, tokens), k0 = c0 * steps, k1 = c1 * steps < all ? c1 * steps : all;
 
     const int cols = a.d_v - wg_col < ATTN_COLS ? a.d_v - wg_col : ATTN_COLS;
     const uint32_t stride_w = 2u * a.H * a.d_k, stride_u = 2u * a.H * a.d_v;
@@ -518,11 +519,11 @@ __device__ __forceinline__ void attn_states(const AttnArgs& a, char* const lds, 
     const bool trans = SEGMENT && cg >= groups_v;
     const int d_v = trans ? a.d_k : a.d_v, wg_col = (trans ? cg - groups_v : cg) * LY::COLS, col0 = wg_col + 16 * wave;
     const SeqPos sq = seq_pos(a.map, s);
-    const int64_t n_chunk = (sq.len + a.C - 1) / a.C;
+    const int64_t n_chunk = pieces_of(sq.len, a.C);
     int64_t c0, c1;
     segment_chunks(n_chunk, a.n_seg, seg, c0, c1);
     const int tokens = a.C < R ? a.C : R, steps = a.C > R ? a.C / R : 1;
-    const int64_t all = (sq.len + tokens - 1) / tokens, k0 = c0 * steps, k1 = c1 * steps < all ? c1 * steps : all;
+    const int64_t all = pieces_of(sq.len, tokens), k0 = c0 * steps, k1 = c1 * steps < all ? c1 * steps : all;
     const int64_t rec0 = (!SEGMENT && a.map.cu_chunks ? a.map.cu_chunks[s] : s * n_chunk) * steps;
 
     RowLoader<LY::PIECES, R, THREADS> lk, lw;
@@ -558,6 +559,11 @@ __device__ __forceinline__ void attn_states(const AttnArgs& a, char* const lds, 
             __syncthreads();  // W and U are in registers
             bring(k + 1);
             request(k + 2);
+            if constexpr (KP == 4) {
+                const StepPos at = step_pos<R>(sq, k, k1, a.C);
+                const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(a.rec_dg + at.row * a.H + h, 0, a.rec_dg && cg == 0 ? (uint32_t)(at.valid - 1) * a.H * 4u + 4u : 0u, 0x00020000);
+                __builtin_amdgcn_raw_buffer_store_b32(0u, rsrc, tid < at.valid ? (uint32_t)tid * a.H * 4u : 0x80000000u, 0, 0);
+            }
             __syncthreads();
         }
         return;

@@ -66,9 +66,9 @@ __device__ __forceinline__ void attn_bwd_state(const AttnBwdArgs& a, char* const
     const unsigned cg = b % groups, hs = b / groups;
     const int h = hs % a.H, s = hs / a.H, wg_col = cg * ATTN_COLS;
     const SeqPos sq = seq_pos(a.map, s);
-    const int64_t n_chunk = (sq.len + a.C - 1) / a.C;
+    const int64_t n_chunk = pieces_of(sq.len, a.C);
     const int tokens = a.C < R ? a.C : R, steps = a.C > R ? a.C / R : 1;
-    const int64_t k1 = (sq.len + tokens - 1) / tokens;
+    const int64_t k1 = pieces_of(sq.len, tokens);
     const uint32_t stride_u = 2u * a.H * a.d_v;
     const MinusOne<OP> minus(ln);
 
@@ -326,7 +326,7 @@ __global__ __launch_bounds__(512) void k_attn_bwd_walks(AttnBwdArgs a, AttnArgs 
 // after the other and d_v in blocks of 64 columns.  A wavefront has KT tiles of 16 channels of all tokens; the products stand turned
 // (channels down, tokens across), so that a lane's four values are neighbours in memory.  The next block's rows are requested before one is used.
 template <int OP, int MT, int KP, bool DELTA> struct BwdChunkLayout {
-    static constexpr int R = 16 * MT, PIECES = 4 * KP, WAVES = 2 * KP, CB = 8;  // CB: pieces of a block of d_v
+    static constexpr int R = 16 * MT, PIECES = 8, WAVES = 4, CB = 8;  // pieces of 64 channels; of a block of d_v
     static constexpr int VP = DELTA ? FULL_PARTS<OP> : 1;
     static constexpr int ROWS = R * PIECES * 16, BLOCK = R * CB * 16;
     static constexpr int TILES = MT * (MT + 1) / 2, M_BYTES = TILES * FULL_PARTS<OP> * TURN16_BYTES;
@@ -383,7 +383,7 @@ template <int PIECES> __device__ __forceinline__ v4u lds_turned_channels(const c
 
 // SHARED: heads share a key head, whose dQ and dK are summed in LDS.
 template <int OP, int MT, int KP, bool DELTA, bool TWO, bool SHARED>
-__global__ __launch_bounds__(128 * KP) void k_attn_bwd_chunk(AttnBwdArgs a)
+__global__ __launch_bounds__(256, 2) void k_attn_bwd_chunk(AttnBwdArgs a)
 {
     typedef BwdChunkLayout<OP, MT, KP, DELTA> LY;
     constexpr int R = LY::R, WAVES = LY::WAVES, THREADS = 64 * WAVES, KT = 1, SHARE = (LY::TILES + WAVES - 1) / WAVES, FP = FULL_PARTS<OP>;
@@ -393,9 +393,11 @@ __global__ __launch_bounds__(128 * KP) void k_attn_bwd_chunk(AttnBwdArgs a)
     float* const red1 = red + 2 * WAVES * R;
     const Lane ln = lane_id();
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), H_k = a.H / a.group;
-    const unsigned b = xcd_neighbours(blockIdx.x, gridDim.x);
+    constexpr int HALVES = KP / 2;
+    const unsigned bh = xcd_neighbours(blockIdx.x, gridDim.x), b = bh / HALVES;
+    const int half0 = 64 * (bh % HALVES);  // the workgroup's first channel
     const int hk = b % H_k, steps = a.C > R ? a.C / R : 1, tokens = a.C < R ? a.C : R;
-    const int64_t id = b / H_k, chunk = id / steps;  // of the step, and its chunk
+    const unsigned id = b / H_k, chunk = id >> (steps - 1);  // of the step, and its chunk
     SeqPos sq;
     int64_t k;  // the step in its sequence
     if (a.map.cu_chunks) {
@@ -405,16 +407,16 @@ __global__ __launch_bounds__(128 * KP) void k_attn_bwd_chunk(AttnBwdArgs a)
             if (a.map.cu_chunks[mid] <= chunk) lo = mid;
             else hi = mid - 1;
         }
-        sq = seq_pos(a.map, lo), k = id - a.map.cu_chunks[lo] * steps;
+        sq = seq_pos(a.map, lo), k = (int64_t)id - a.map.cu_chunks[lo] * steps;
     } else {
-        const int64_t cps = (a.map.Tlen + a.C - 1) / a.C;
-        sq = SeqPos{chunk / cps * a.map.Tlen, a.map.Tlen}, k = chunk % cps * steps + id % steps;
+        const unsigned cps = (unsigned)pieces_of(a.map.Tlen, a.C);
+        sq = SeqPos{(int64_t)(chunk / cps) * a.map.Tlen, a.map.Tlen}, k = (int64_t)(chunk % cps) * steps + (id & (steps - 1));
     }
-    const int64_t all = (sq.len + tokens - 1) / tokens;
+    const int64_t all = pieces_of(sq.len, tokens);
     if (k >= all) return;  // (the second step of a chunk that ends in its first)
     const StepPos at = step_pos<R>(sq, k, all, a.C);
     const bool chunk_ends = steps == 1 || (k & 1) || k + 1 == all;
-    const int ch0 = 16 * KT * wave;  // this wavefront's first channel
+    const int ch0 = 16 * KT * wave;  // this wavefront's first, of those
     const uint32_t stride_k = 2u * H_k * a.d_k, stride_u = 2u * a.H * a.d_v;
     const MinusOne<OP> minus(ln);
     RowLoader<LY::CB, R, THREADS> lo, lu;  // dO; dV', or V' itself
@@ -432,20 +434,20 @@ __global__ __launch_bounds__(128 * KP) void k_attn_bwd_chunk(AttnBwdArgs a)
     const bool second = TWO && (k & 1);
     auto request_states = [&](int h, int v0) {
         const int64_t size = a.d_k * a.d_v;
-        const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(a.rec_state) + (id * a.H + h) * size, 0, (uint32_t)size * 4u, 0x00020000);
-        const auto rd = __builtin_amdgcn_make_buffer_rsrc(a.rec_dstate + (id * a.H + h) * size, 0, (uint32_t)size * 4u, 0x00020000);
+        const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(a.rec_state) + ((int64_t)id * a.H + h) * size, 0, (uint32_t)size * 4u, 0x00020000);
+        const auto rd = __builtin_amdgcn_make_buffer_rsrc(a.rec_dstate + ((int64_t)id * a.H + h) * size, 0, (uint32_t)size * 4u, 0x00020000);
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) {
-                const int ch = ch0 + 16 * kt, col = v0 + 32 * ks + 8 * ln.q;
+                const int ch = half0 + ch0 + 16 * kt, col = v0 + 32 * ks + 8 * ln.q;
                 const uint32_t from = ch < a.d_k && col < a.d_v ? 4u * (ch * a.d_v + 16 * col + 4 * ln.n) : 0x80000000u;
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     sv[kt][ks][half] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(rs, from + 256u * half, 0, 0));
                     dsv[kt][ks][half] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(rd, from + 256u * half, 0, 0));
                     if constexpr (TWO) {
-                        const auto rz = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(a.rec_state) + ((id - second) * a.H + h) * size, 0, (uint32_t)size * 4u, 0x00020000);
+                        const auto rz = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(a.rec_state) + ((int64_t)(id - second) * a.H + h) * size, 0, (uint32_t)size * 4u, 0x00020000);
                         szv[kt][ks][half] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(rz, from + 256u * half, 0, 0));
                     }
                 }
@@ -455,8 +457,8 @@ __global__ __launch_bounds__(128 * KP) void k_attn_bwd_chunk(AttnBwdArgs a)
     request(h0, 0);
     {
         RowLoader<LY::PIECES, R, THREADS> lk, lq;
-        lk.load(static_cast<const char*>(a.K) + at.row * stride_k + 2 * hk * a.d_k, stride_k, a.d_k, at.valid, tid);
-        lq.load(static_cast<const char*>(a.Q) + at.row * stride_k + 2 * hk * a.d_k, stride_k, a.d_k, at.valid, tid);
+        lk.load(static_cast<const char*>(a.K) + at.row * stride_k + 2 * (hk * a.d_k + half0), stride_k, a.d_k - half0, at.valid, tid);
+        lq.load(static_cast<const char*>(a.Q) + at.row * stride_k + 2 * (hk * a.d_k + half0), stride_k, a.d_k - half0, at.valid, tid);
         lg.load(a.g, at, a.H, h0, tid);
         request_states(h0, 0);
         lk.store(lds + LY::K_AT, tid);
@@ -611,7 +613,7 @@ __global__ __launch_bounds__(128 * KP) void k_attn_bwd_chunk(AttnBwdArgs a)
             const float gi = gl[16 * its[j] + ln.n];
             const v4f gj = *reinterpret_cast<const v4f*>(gl + 16 * jts[j] + 4 * ln.q);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) M[j][r] *= a.scale * expf(jts[j] < its[j] || 4 * ln.q + r <= ln.n ? gi - gj[r] : -__builtin_inff());
+            for (int r = 0; r < 4; ++r) M[j][r] *= a.scale * __expf(jts[j] < its[j] || 4 * ln.q + r <= ln.n ? gi - gj[r] : -__builtin_inff());
         }
         int m_shift = 0;
         if constexpr (OP == OP_F16) {
@@ -685,7 +687,7 @@ __global__ __launch_bounds__(128 * KP) void k_attn_bwd_chunk(AttnBwdArgs a)
             float dot_q = 0.f, dot_k = 0.f;
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt) {
-                const int ch = ch0 + 16 * kt + 4 * ln.q;
+                const int ch = half0 + ch0 + 16 * kt + 4 * ln.q;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     if constexpr (OP == OP_F16) X[kt][it][r] *= down, Y[kt][it][r] *= down;
@@ -719,7 +721,9 @@ __global__ __launch_bounds__(128 * KP) void k_attn_bwd_chunk(AttnBwdArgs a)
                     for (int w = 0; w < WAVES; ++w) last += red1[WAVES + w], t += red1[2 * WAVES + w];
                     last += gl[3 * R] * t;
                 }
-                a.dg[(at.row + tid) * a.H + h] = q - kd + last;
+                float* const to = a.dg + (at.row + tid) * a.H + h;
+                if constexpr (HALVES == 1) *to = q - kd + last;
+                else unsafeAtomicAdd(to, q - kd + last);  // two terms on a zero: the same whichever comes first
             }
         }
         if constexpr (SHARED) __syncthreads();  // M, the gates and the sums are not needed any more

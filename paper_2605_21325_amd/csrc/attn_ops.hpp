@@ -29,6 +29,9 @@ __device__ __forceinline__ SeqPos seq_pos(const SeqMap& m, int s)
     return {a, m.cu_seqlens[s + 1] - a};
 }
 
+// Pieces of a power of two in n tokens (a 64-bit division is 130 instructions, and a workgroup would begin with three of them).
+__device__ __forceinline__ int64_t pieces_of(int64_t n, int size) { return (n + size - 1) >> __builtin_ctz((unsigned)size); }
+
 // Workgroups go to the eight XCDs in turn; neighbours (column groups and heads that read the same rows) are put on one of them.
 __device__ __forceinline__ unsigned xcd_neighbours(unsigned b, unsigned n)
 {
