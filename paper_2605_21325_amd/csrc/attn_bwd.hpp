@@ -325,8 +325,8 @@ __global__ __launch_bounds__(512) void k_attn_bwd_walks(AttnBwdArgs a, AttnArgs 
 // Everything that needs the states at both ends of a step: a workgroup per step and key head, which takes the heads that share it one
 // after the other and d_v in blocks of 64 columns.  A wavefront has KT tiles of 16 channels of all tokens; the products stand turned
 // (channels down, tokens across), so that a lane's four values are neighbours in memory.  The next block's rows are requested before one is used.
-template <int OP, int MT, int KP, bool DELTA> struct BwdChunkLayout {
-    static constexpr int R = 16 * MT, PIECES = 8, WAVES = 4, CB = 8;  // pieces of 64 channels; of a block of d_v
+template <int OP, int MT, int WAVES, bool DELTA> struct BwdChunkLayout {
+    static constexpr int R = 16 * MT, PIECES = 2 * WAVES, CB = 8;  // pieces of a row of channels; of a block of d_v
     static constexpr int VP = DELTA ? FULL_PARTS<OP> : 1;
     static constexpr int ROWS = R * PIECES * 16, BLOCK = R * CB * 16;
     static constexpr int TILES = MT * (MT + 1) / 2, M_BYTES = TILES * FULL_PARTS<OP> * TURN16_BYTES;
@@ -382,18 +382,18 @@ template <int PIECES> __device__ __forceinline__ v4u lds_turned_channels(const c
 }
 
 // SHARED: heads share a key head, whose dQ and dK are summed in LDS.
-template <int OP, int MT, int KP, bool DELTA, bool TWO, bool SHARED>
-__global__ __launch_bounds__(256, 2) void k_attn_bwd_chunk(AttnBwdArgs a)
+template <int OP, int MT, int KP, bool DELTA, bool TWO, bool SHARED, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void k_attn_bwd_chunk(AttnBwdArgs a)
 {
-    typedef BwdChunkLayout<OP, MT, KP, DELTA> LY;
-    constexpr int R = LY::R, WAVES = LY::WAVES, THREADS = 64 * WAVES, KT = 1, SHARE = (LY::TILES + WAVES - 1) / WAVES, FP = FULL_PARTS<OP>;
+    typedef BwdChunkLayout<OP, MT, WAVES, DELTA> LY;
+    constexpr int R = LY::R, THREADS = 64 * WAVES, KT = 1, SHARE = (LY::TILES + WAVES - 1) / WAVES, FP = FULL_PARTS<OP>;
     __shared__ __attribute__((aligned(16))) char lds[LY::BYTES + (SHARED ? LY::SUM_BYTES : 0)];
     float* const gl = reinterpret_cast<float*>(lds + LY::G_AT);
     float* const red = reinterpret_cast<float*>(lds + LY::RED_AT);  // sums over channels: [2][wavefront][token], then [3][wavefront]
     float* const red1 = red + 2 * WAVES * R;
     const Lane ln = lane_id();
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), H_k = a.H / a.group;
-    constexpr int HALVES = KP / 2;
+    constexpr int HALVES = 2 * KP / WAVES;
     const unsigned bh = xcd_neighbours(blockIdx.x, gridDim.x), b = bh / HALVES;
     const int half0 = 64 * (bh % HALVES);  // the workgroup's first channel
     const int hk = b % H_k, steps = a.C > R ? a.C / R : 1, tokens = a.C < R ? a.C : R;
