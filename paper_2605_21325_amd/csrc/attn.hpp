@@ -231,10 +231,10 @@ __global__ __launch_bounds__(512) void k_chunk_attn(AttnArgs a)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane16 = 16 * (16 * ln.q + ln.n);
 
     const unsigned groups = (a.d_v + ATTN_COLS - 1) / ATTN_COLS;
-    const unsigned b = xcd_neighbours(blockIdx.x, gridDim.x);
-    const unsigned cg = b % groups, hs = b / groups;
+    const SeqUnit mine = seq_unit(a.map, blockIdx.x, gridDim.x, groups * a.H, by_length(a.map, gridDim.x) && a.n_seg == 1, lds);
+    const unsigned cg = mine.unit % groups;
     const int seg = blockIdx.y;
-    const int h = hs % a.H, s = hs / a.H;
+    const int h = mine.unit / groups, s = mine.seq, hs = s * a.H + h;
     const int wg_col = cg * ATTN_COLS;
     const SeqPos sq = seq_pos(a.map, s);
     const int64_t n_chunk = pieces_of(sq.len, a.C);
@@ -503,7 +503,7 @@ template <int OP, int MT, int KP, bool DELTA, int WAVES> struct StatesLayout {
 };
 
 template <int OP, int MT, int KP, bool DELTA, int MODE, bool TWO, int WAVES>
-__device__ __forceinline__ void attn_states(const AttnArgs& a, char* const lds, unsigned b, int seg)
+__device__ __forceinline__ void attn_states(const AttnArgs& a, char* const lds, unsigned b, unsigned n, bool sorted, int seg)
 {
     typedef StatesLayout<OP, MT, KP, DELTA, WAVES> LY;
     constexpr bool SEGMENT = MODE == ATTN_SEGMENT;
@@ -514,8 +514,9 @@ __device__ __forceinline__ void attn_states(const AttnArgs& a, char* const lds, 
     const bool brings = SEGMENT || threadIdx.x >= THREADS;
 
     const unsigned groups_v = (a.d_v + LY::COLS - 1) / LY::COLS, groups = groups_v + (SEGMENT && DELTA ? (a.d_k + LY::COLS - 1) / LY::COLS : 0);
-    const unsigned cg = b % groups, hs = b / groups;
-    const int h = hs % a.H, s = hs / a.H, hk = h / a.group, H_k = a.H / a.group;
+    const SeqUnit mine = seq_unit(a.map, b, n, groups * a.H, sorted, lds);
+    const unsigned cg = mine.unit % groups;
+    const int h = mine.unit / groups, s = mine.seq, hs = s * a.H + h, hk = h / a.group, H_k = a.H / a.group;
     const bool trans = SEGMENT && cg >= groups_v;
     const int d_v = trans ? a.d_k : a.d_v, wg_col = (trans ? cg - groups_v : cg) * LY::COLS, col0 = wg_col + 16 * wave;
     const SeqPos sq = seq_pos(a.map, s);
@@ -640,7 +641,7 @@ template <int OP, int MT, int KP, bool DELTA, int MODE, bool TWO, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void k_attn_states(AttnArgs a)
 {
     __shared__ __attribute__((aligned(16))) char lds[StatesLayout<OP, MT, KP, DELTA, WAVES>::BYTES];
-    attn_states<OP, MT, KP, DELTA, MODE, TWO, WAVES>(a, lds, xcd_neighbours(blockIdx.x, gridDim.x), blockIdx.y);
+    attn_states<OP, MT, KP, DELTA, MODE, TWO, WAVES>(a, lds, blockIdx.x, gridDim.x, false, blockIdx.y);
 }
 
 // States before the segments, in place of what the segments add: S <- M S + L from the sequence's initial state, segment by segment.  M and S as three

@@ -55,7 +55,7 @@ template <class LY> __device__ __forceinline__ int unit_at(int jt)  // units_bef
 //     first half     K dS', dV', G_C dS' + X            W and the rows of the step before to LDS
 //     second half    dU, W^T dV', the parts of dS       P and X of the step before
 template <int OP, int MT, int KP, bool DELTA, bool TWO>
-__device__ __forceinline__ void attn_bwd_state(const AttnBwdArgs& a, char* const lds, unsigned b)
+__device__ __forceinline__ void attn_bwd_state(const AttnBwdArgs& a, char* const lds, unsigned b, unsigned n)
 {
     typedef BwdStateLayout<OP, MT, KP, DELTA> LY;
     constexpr int R = LY::R, FP = FULL_PARTS<OP>, PIECES = LY::PIECES, TILES = MT * (MT + 1) / 2;
@@ -63,8 +63,9 @@ __device__ __forceinline__ void attn_bwd_state(const AttnBwdArgs& a, char* const
     const Lane ln = lane_id();
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane16 = 16 * (16 * ln.q + ln.n);
     const unsigned groups = (a.d_v + ATTN_COLS - 1) / ATTN_COLS;
-    const unsigned cg = b % groups, hs = b / groups;
-    const int h = hs % a.H, s = hs / a.H, wg_col = cg * ATTN_COLS;
+    const SeqUnit mine = seq_unit(a.map, b, n, groups * a.H, by_length(a.map, 2 * n), lds);
+    const unsigned cg = mine.unit % groups;
+    const int h = mine.unit / groups, s = mine.seq, hs = s * a.H + h, wg_col = cg * ATTN_COLS;
     const SeqPos sq = seq_pos(a.map, s);
     const int64_t n_chunk = pieces_of(sq.len, a.C);
     const int tokens = a.C < R ? a.C : R, steps = a.C > R ? a.C / R : 1;
@@ -316,9 +317,9 @@ __global__ __launch_bounds__(512) void k_attn_bwd_walks(AttnBwdArgs a, AttnArgs 
     __shared__ __attribute__((aligned(16))) char lds[OF_DS > OF_STATES ? OF_DS : OF_STATES];
     const unsigned units = gridDim.x / 2;
     if (blockIdx.x < units) {
-        attn_bwd_state<OP, MT, KP, DELTA, TWO>(a, lds, xcd_neighbours(blockIdx.x, units));
+        attn_bwd_state<OP, MT, KP, DELTA, TWO>(a, lds, blockIdx.x, units);
     } else {
-        attn_states<OP, MT, KP, DELTA, ATTN_RECORD, TWO, 4>(f, lds, xcd_neighbours(blockIdx.x - units, units), 0);
+        attn_states<OP, MT, KP, DELTA, ATTN_RECORD, TWO, 4>(f, lds, blockIdx.x - units, units, by_length(f.map, 2 * units), 0);
     }
 }
 

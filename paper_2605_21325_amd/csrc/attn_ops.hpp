@@ -39,6 +39,40 @@ __device__ __forceinline__ unsigned xcd_neighbours(unsigned b, unsigned n)
     return x * q + (x < r ? x : r) + (b >> 3);
 }
 
+// A workgroup's sequence, and its place among the `per` that a sequence has.  Where packed sequences need more than one round of the 256 compute units the longest begin
+// (each of them on one XCD, the next on the next), so that none of them starts when the others are done.
+constexpr int LENGTHS_SORTED = 256;  // sequences at most
+__device__ __forceinline__ bool by_length(const SeqMap& m, unsigned n) { return m.cu_seqlens && n > 256u && m.n_seq <= LENGTHS_SORTED; }
+struct SeqUnit {
+    int seq;
+    unsigned unit;
+};
+__device__ __forceinline__ SeqUnit seq_unit(const SeqMap& m, unsigned b, unsigned n, unsigned per, bool sorted, char* lds)
+{
+    if (!sorted) {
+        b = xcd_neighbours(b, n);
+        return {(int)(b / per), b % per};
+    }
+    const unsigned eights = (unsigned)m.n_seq / 8u * 8u, in_eights = b >> 3, left = b - eights * per;
+    const bool whole = b < eights * per;
+    const unsigned place = whole ? in_eights / per * 8u + (b & 7u) : eights + left / per;
+    int64_t* const lengths = reinterpret_cast<int64_t*>(lds);
+    int* const found = reinterpret_cast<int*>(lengths + LENGTHS_SORTED);
+    const int t = threadIdx.x;
+    int64_t mine = 0;
+    if (t < m.n_seq) lengths[t] = mine = m.cu_seqlens[t + 1] - m.cu_seqlens[t];
+    __syncthreads();
+    if (t < m.n_seq) {
+        unsigned before = 0;
+        for (int j = 0; j < m.n_seq; ++j) before += lengths[j] > mine || (lengths[j] == mine && j < t);
+        if (before == place) *found = t;
+    }
+    __syncthreads();
+    const int seq = __builtin_amdgcn_readfirstlane(*found);
+    __syncthreads();
+    return {seq, whole ? in_eights % per : left % per};
+}
+
 template <int OP> __device__ __forceinline__ v4f mfma32(v4u a, v4u b, v4f c)
 {
     if constexpr (OP == OP_F16)

@@ -379,3 +379,24 @@ def test_state_pool_beyond_four_gigabytes():
         close(o[b], ro, 2.0 ** -8 + 4 * d * 2.0 ** -24, "o")
         close(state[slot].flatten(1), rs.reshape(H, -1), 2.0 ** -23, "state")
     assert not state[1:n - 1].any()
+
+
+@pytest.mark.parametrize("n_seq, H, Hk, delta", [(43, 4, 4, True), (43, 4, 2, False), (256, 1, 1, True), (257, 1, 1, True), (8, 17, 17, True)])
+def test_many_packed_sequences_begin_with_the_longest_and_give_the_same(n_seq, H, Hk, delta):
+    """More workgroups than compute units: sequences are taken by length, empty and equal ones among them.  Bit for bit what each gives alone."""
+    lens = [(97 * i * i + 31 * (i % 5)) % 331 if i % 6 else (0 if i % 4 else 128) for i in range(n_seq)]
+    x = make(lens, H, Hk, 128, 128, 64, BF, delta=delta, seed=5)
+    o, fin = tri.gdn_chunk_attn_varlen(x["q"], x["k"], x["u"], x["g"], lens, 64, W=x["w"], state=x["state"])
+    grads = tri.gdn_chunk_attn_bwd_varlen(x["q"], x["k"], x["u"], x["g"], x["do"], lens, 64, W=x["w"], state=x["state"], dstate=x["dstate"])
+    at = 0
+    for s, n in enumerate(lens):
+        if s % max(1, n_seq // 24) == 0 or n == max(lens):
+            part = lambda t: None if t is None else t[at:at + n].contiguous()
+            own = lambda t: t[s:s + 1].contiguous()
+            one, last = tri.gdn_chunk_attn_varlen(part(x["q"]), part(x["k"]), part(x["u"]), part(x["g"]), [n], 64, W=part(x["w"]), state=own(x["state"]))
+            assert torch.equal(one, o[at:at + n]) and torch.equal(last, fin[s:s + 1]), (s, n)
+            alone = tri.gdn_chunk_attn_bwd_varlen(part(x["q"]), part(x["k"]), part(x["u"]), part(x["g"]), part(x["do"]), [n], 64, W=part(x["w"]), state=own(x["state"]), dstate=own(x["dstate"]))
+            for i, (got, want) in enumerate(zip(grads, alone)):
+                if want is not None:
+                    assert torch.equal(got[s:s + 1] if i == 5 else got[at:at + n], want), (s, n, i)
+        at += n
