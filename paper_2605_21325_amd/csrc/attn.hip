@@ -34,7 +34,7 @@ template <int MT, int KP, bool DELTA, bool TWO> int go(const AttnCall& c)
         int rc = c.d_v > 64 ? launch_kernel(false, k_attn_states<OP, MT, KP, DELTA, ATTN_SEGMENT, TWO, 8>, by(128), dim3(512), 0, c.stream, a)
                             : launch_kernel(false, k_attn_states<OP, MT, KP, DELTA, ATTN_SEGMENT, TWO, 4>, by(64), dim3(256), 0, c.stream, a);
         if (rc != LAUNCHED) return rc;
-        rc = DELTA ? launch_kernel(false, k_attn_join<KP>, dim3(heads * ((c.d_v + 15) / 16)), dim3(256), 0, c.stream, a)
+        rc = DELTA ? launch_kernel(false, k_attn_join<KP>, dim3(heads * ((c.d_v + 15) / 16)), dim3(128 * KP), 0, c.stream, a)
                    : launch_kernel(false, k_attn_join_plain, dim3((unsigned)(((int64_t)heads * c.d_k * c.d_v + 255) / 256)), dim3(256), 0, c.stream, a);
         if (rc != LAUNCHED) return rc;
     }

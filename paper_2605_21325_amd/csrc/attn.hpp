@@ -19,6 +19,8 @@
 // 8 x 8192 tokens, 16 heads 440 us (the bytes at the rate of a copy: 246); 48 packed sequences of 1100 on average, 4 heads, no W 137 (44).
 #pragma once
 
+#include <type_traits>
+
 #include "attn_ops.hpp"
 
 namespace triinv {
@@ -645,63 +647,53 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_states(AttnArgs a)
 }
 
 // States before the segments, in place of what the segments add: S <- M S + L from the sequence's initial state, segment by segment.  M and S as three
-// bf16 parts each, the six products that matter.  A workgroup takes 16 columns, a wavefront KP / 2 tiles of their rows; the parts of S go round
-// through LDS.
-template <int KP> __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a)
+// bf16 parts each, the six products that matter.  A workgroup takes 16 columns, a wavefront a tile of their rows; the parts of S go round
+// through LDS.  M is asked for two segments ahead; a segment of 16 heads of 128 x 128 takes 2.6 us.
+template <int KP> __global__ __launch_bounds__(128 * KP) void k_attn_join(AttnArgs a)
 {
-    constexpr int TI = KP / 2;
     __shared__ __attribute__((aligned(16))) char lds[2][KP * 3 * 1024];
     const Lane ln = lane_id();
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane16 = 16 * (16 * ln.q + ln.n);
     const unsigned groups = (a.d_v + 15) / 16, b = xcd_neighbours(blockIdx.x, gridDim.x), hs = b / groups;  // (a head's groups read the same M: from one L2)
     const int col = 16 * (b % groups) + ln.n;
     const int64_t heads = (int64_t)a.map.n_seq * a.H;
-    const bool mine = col < a.d_v;
-    v4f S[TI];
-    auto at = [&](int t, int r) { return state_channel(TI * wave + t, 4 * ln.q + r); };
+    auto place = [&](int r) { return col < a.d_v ? 4u * (state_channel(wave, 4 * ln.q + r) * a.d_v + col) : 0x80000000u; };  // (channels that are not there lie outside the buffer)
+    v4f S;
+    {
+        const auto from = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(a.state) + (int64_t)hs * a.d_k * a.d_v, 0, a.state ? 4u * a.d_k * a.d_v : 0u, 0x00020000);
 #pragma unroll
-    for (int t = 0; t < TI; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) S[t][r] = a.state && mine && at(t, r) < a.d_k ? a.state[((int64_t)hs * a.d_k + at(t, r)) * a.d_v + col] : 0.f;
+        for (int r = 0; r < 4; ++r) S[r] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(from, place(r), 0, 0));
+    }
     const MinusOne<OP_BF16> minus(ln);
-    v4f m[TI][2 * KP], add[TI];  // rows of M and L, of the segment behind the one at hand
-    auto request = [&](int seg) {
+    v4f m[2][2 * KP], add[2];  // rows of M and L, of the next two segments
+    auto request = [&](int seg, auto buffer) {
+        constexpr int B = buffer;
         const bool there = seg + 1 < a.n_seg;
-        const float* const M = a.seg_trans + ((there ? seg : 0) * heads + hs) * a.d_k * a.d_k;
-        const float* const L = a.seg_state + ((there ? seg : 0) * heads + hs) * a.d_k * a.d_v;
+        const auto M = __builtin_amdgcn_make_buffer_rsrc(a.seg_trans + ((there ? seg : 0) * heads + hs) * a.d_k * a.d_k, 0, there ? 4u * a.d_k * a.d_k : 0u, 0x00020000);
+        const auto L = __builtin_amdgcn_make_buffer_rsrc(a.seg_state + ((there ? seg : 0) * heads + hs) * a.d_k * a.d_v, 0, there ? 4u * a.d_k * a.d_v : 0u, 0x00020000);
+        const uint32_t row = 4u * (state_channel(wave, ln.n) * a.d_k + 8 * ln.q);
 #pragma unroll
-        for (int t = 0; t < TI; ++t) {
-            const int row = state_channel(TI * wave + t, ln.n);
+        for (int i = 0; i < 2 * KP; ++i)
+            m[B][i] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(M, 16 * i < a.d_k ? row + 4u * (32 * (i >> 1) + 4 * (i & 1)) : 0x80000000u, 0, 0));
 #pragma unroll
-            for (int i = 0; i < 2 * KP; ++i) m[t][i] = there && row < a.d_k && 16 * i < a.d_k ? *reinterpret_cast<const v4f*>(M + (int64_t)row * a.d_k + 32 * (i >> 1) + 8 * ln.q + 4 * (i & 1)) : zero4();
-#pragma unroll
-            for (int r = 0; r < 4; ++r) add[t][r] = there && mine && at(t, r) < a.d_k ? L[(int64_t)at(t, r) * a.d_v + col] : 0.f;
-        }
+        for (int r = 0; r < 4; ++r) add[B][r] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(L, place(r), 0, 0));
     };
-    request(0);
-    for (int seg = 0; seg + 1 < a.n_seg; ++seg) {
-        Parts<3> mp[TI][KP];
-        v4f next[TI];
-#pragma unroll
-        for (int t = 0; t < TI; ++t) next[t] = add[t], split_pairs<OP_BF16, 3, KP>(m[t], mp[t], minus);
-        request(seg + 1);
-        // this wavefront's parts of S: half a pair of tiles (KP = 2), or a whole one
+    auto pass = [&](int seg, auto buffer) {
+        constexpr int B = buffer;
+        Parts<3> mp[KP];
+        v4f next = add[B], low = zero4();  // half of the products each, in chains of their own
+        split_pairs<OP_BF16, 3, KP>(m[B], mp, minus);
+        request(seg + 2, buffer);
+        // this wavefront's parts of S: half a pair of tiles
         char* const buf = lds[seg & 1];
+        v4f x = S;
 #pragma unroll
-        for (int t = 0; t < TI; ++t) {
-            const int i = TI * wave + t;
-            v4f x = S[t];
-#pragma unroll
-            for (int part = 0; part < 3; ++part) {
-                const v2u u = pack4<OP_BF16>(x);
-                *reinterpret_cast<v2u*>(buf + ((i >> 1) * 3 + part) * 1024 + lane16 + 8 * (i & 1)) = u;
-                x = minus16<OP_BF16>(x, u);
-            }
+        for (int part = 0; part < 3; ++part) {
+            const v2u u = pack4<OP_BF16>(x);
+            *reinterpret_cast<v2u*>(buf + ((wave >> 1) * 3 + part) * 1024 + lane16 + 8 * (wave & 1)) = u;
+            x = minus16<OP_BF16>(x, u);
         }
         __syncthreads();
-        v4f low[TI];  // half of the products, in chains of their own
-#pragma unroll
-        for (int t = 0; t < TI; ++t) low[t] = zero4();
 #pragma unroll
         for (int p = 0; p < KP; ++p) {
             v4u sp[3];
@@ -710,19 +702,23 @@ template <int KP> __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a)
 #pragma unroll
             for (int j = 0; j < 6; ++j) {
                 constexpr int of_m[6] = {2, 0, 1, 1, 0, 0}, of_s[6] = {0, 2, 1, 0, 1, 0};
-#pragma unroll
-                for (int t = 0; t < TI; ++t) (j & 1 ? next : low)[t] = mfma32<OP_BF16>(mp[t][p].u[of_m[j]], sp[of_s[j]], (j & 1 ? next : low)[t]);
+                (j & 1 ? next : low) = mfma32<OP_BF16>(mp[p].u[of_m[j]], sp[of_s[j]], j & 1 ? next : low);
             }
         }
-        float* const L = a.seg_state + (seg * heads + hs) * a.d_k * a.d_v;
+        const auto L = __builtin_amdgcn_make_buffer_rsrc(a.seg_state + (seg * heads + hs) * a.d_k * a.d_v, 0, 4u * a.d_k * a.d_v, 0x00020000);
 #pragma unroll
-        for (int t = 0; t < TI; ++t) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                S[t][r] = next[t][r] + low[t][r];
-                if (mine && at(t, r) < a.d_k) L[(int64_t)at(t, r) * a.d_v + col] = S[t][r];
-            }
+        for (int r = 0; r < 4; ++r) {
+            S[r] = next[r] + low[r];
+            __builtin_amdgcn_raw_buffer_store_b32(bits(S[r]), L, place(r), 0, 0);
         }
+    };
+    const std::integral_constant<int, 0> even;
+    const std::integral_constant<int, 1> odd;
+    request(0, even);
+    request(1, odd);
+    for (int seg = 0; seg + 1 < a.n_seg; seg += 2) {
+        pass(seg, even);
+        if (seg + 2 < a.n_seg) pass(seg + 1, odd);
     }
 }
 
