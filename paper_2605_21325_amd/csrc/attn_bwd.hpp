@@ -468,8 +468,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attn_bwd_chunk(AttnBwdArgs a)
         lq.store(lds + LY::Q_AT, tid);
     }
     auto put_rows = [&](void* to, const v4f x, int heads, int head, int ch, int it) {
-        const int i = 16 * it + ln.n;
-        if (i < at.valid && ch < a.d_k) *reinterpret_cast<v2u*>(static_cast<uint16_t*>(to) + ((at.row + i) * heads + head) * a.d_k + ch) = pack4<OP>(x);
+        const uint32_t stride = 2u * heads * a.d_k;
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(static_cast<char*>(to) + at.row * stride + 2 * head * a.d_k, 0, (uint32_t)(at.valid - 1) * stride + 2u * a.d_k, 0x00020000);
+        __builtin_amdgcn_raw_buffer_store_b64(pack4<OP>(x), rsrc, in_place(ch < a.d_k ? ln.n * stride + 2u * ch : 0x80000000u) + 16 * it * stride, 0, 0);
     };
 
     for (int h = h0; h < h0 + (SHARED ? a.group : 1); ++h) {
@@ -556,45 +557,52 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attn_bwd_chunk(AttnBwdArgs a)
             }
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) {
-                in_order();  // (or it takes registers for both at once)
+                // (Left alone it takes registers for all of it at once; what fp16 scales by leaves it fewer of them.)
+                in_order();
                 Parts<FP> sp[KT], dp[KT];
-                {
-                    v4f x[2 * KT], y[2 * KT];
+                v4f x[2 * KT];
 #pragma unroll
-                    for (int kt = 0; kt < KT; ++kt) x[2 * kt] = sv[kt][ks][0], x[2 * kt + 1] = sv[kt][ks][1], y[2 * kt] = dsv[kt][ks][0], y[2 * kt + 1] = dsv[kt][ks][1];
-                    split_pairs<OP, FP, KT>(x, sp, minus);
-                    split_pairs<OP, FP, KT>(y, dp, minus);
+                for (int kt = 0; kt < KT; ++kt) x[2 * kt] = sv[kt][ks][0], x[2 * kt + 1] = sv[kt][ks][1];
+                split_pairs<OP, FP, KT>(x, sp, minus);
+                if constexpr (DELTA) {
+                    Parts<2> zp[KT];
+                    if constexpr (TWO) {
+#pragma unroll
+                        for (int kt = 0; kt < KT; ++kt) x[2 * kt] = szv[kt][ks][0], x[2 * kt + 1] = szv[kt][ks][1];
+                        split_pairs<OP, 2, KT>(x, zp, minus);
+                    } else {
+#pragma unroll
+                        for (int kt = 0; kt < KT; ++kt) zp[kt].u[0] = sp[kt].u[0], zp[kt].u[1] = sp[kt].u[1];
+                    }
+                    if constexpr (OP == OP_F16) in_order();
+                    v4u d[MT];
+#pragma unroll
+                    for (int it = 0; it < MT; ++it) d[it] = lds_row<LY::CB>(lds + LY::DV_AT, 16 * it + ln.n, 4 * ks + ln.q);
+#pragma unroll
+                    for (int part = 1; part >= 0; --part)
+#pragma unroll
+                        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                            for (int it = 0; it < MT; ++it) Z[kt][it] = mfma32<OP>(zp[kt].u[part], d[it], Z[kt][it]);
                 }
-                Parts<2> zp[KT];
-                if constexpr (TWO) {
-                    v4f x[2 * KT];
+                if constexpr (OP == OP_F16) in_order();
+                v4u o[MT];
 #pragma unroll
-                    for (int kt = 0; kt < KT; ++kt) x[2 * kt] = szv[kt][ks][0], x[2 * kt + 1] = szv[kt][ks][1];
-                    split_pairs<OP, 2, KT>(x, zp, minus);
-                } else {
-#pragma unroll
-                    for (int kt = 0; kt < KT; ++kt) zp[kt].u[0] = sp[kt].u[0], zp[kt].u[1] = sp[kt].u[1];
-                }
-                v4u o[MT], d[MT];
-#pragma unroll
-                for (int it = 0; it < MT; ++it) {
-                    o[it] = lds_row<LY::CB>(lds + LY::O_AT, 16 * it + ln.n, 4 * ks + ln.q);
-                    if constexpr (DELTA) d[it] = lds_row<LY::CB>(lds + LY::DV_AT, 16 * it + ln.n, 4 * ks + ln.q);
-                }
+                for (int it = 0; it < MT; ++it) o[it] = lds_row<LY::CB>(lds + LY::O_AT, 16 * it + ln.n, 4 * ks + ln.q);
 #pragma unroll
                 for (int part = FP - 1; part >= 0; --part)
 #pragma unroll
                     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-                        for (int it = 0; it < MT; ++it) {
-                            X[kt][it] = mfma32<OP>(sp[kt].u[part], o[it], X[kt][it]);
-                            if constexpr (DELTA) {
-                                if (part < 2) Z[kt][it] = mfma32<OP>(zp[kt].u[part < 2 ? part : 0], d[it], Z[kt][it]);
-                            }
-                        }
+                        for (int it = 0; it < MT; ++it) X[kt][it] = mfma32<OP>(sp[kt].u[part], o[it], X[kt][it]);
+                if constexpr (OP == OP_F16) in_order();
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt) x[2 * kt] = dsv[kt][ks][0], x[2 * kt + 1] = dsv[kt][ks][1];
+                split_pairs<OP, FP, KT>(x, dp, minus);
                 // parts of both sides: what is left out is below the last bit kept
 #pragma unroll
                 for (int j = LY::VP - 1; j >= 0; --j) {
+                    if constexpr (OP == OP_F16) in_order();
                     v4u v[MT];
 #pragma unroll
                     for (int it = 0; it < MT; ++it) v[it] = lds_row<LY::CB>(lds + LY::V_AT + j * LY::BLOCK, 16 * it + ln.n, 4 * ks + ln.q);
