@@ -16,7 +16,7 @@
 //
 // Bound by the matrix unit and by the chain of a step: d_k = d_v = 128 takes 3.3 thousand cycles of matrix instructions a SIMD and step of 64 tokens, half of
 // them for the second and third parts of S (products of fp32 states), and a step lasts 7; a chip full of it runs at 1.6 to 1.9 GHz.  Measured, bf16:
-// 8 x 8192 tokens, 16 heads 440 us (the bytes at the rate of a copy: 246); 48 packed sequences of 1100 on average, 4 heads, no W 137 (44).
+// 8 x 8192 tokens, 16 heads 440 us (the bytes at the rate of a copy: 246); 48 packed sequences of 1100 on average, 4 heads, no W 106 (44).
 #pragma once
 
 #include <type_traits>

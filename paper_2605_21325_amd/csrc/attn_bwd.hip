@@ -29,7 +29,7 @@ template <int MT, int KP, bool DELTA, bool TWO> int go(const AttnBwdCall& c)
     const int rc = launch_kernel(false, k_attn_bwd_walks<OP, MT, KP, DELTA, TWO>, dim3(2 * heads * groups), dim3(512), 0, c.stream, a, f);
     if (rc != LAUNCHED || c.n_chunk == 0) return rc;
     // 64 channels a workgroup, two of them on a compute unit; all of them where heads share a key head, whose sums take the LDS of two (4 x 4096 tokens, 16 heads of
-    // 128: 267 us for all of them 292; 8 key heads 366 and 264).
+    // 128: 268 us, 292 with all of them; 8 key heads 366 and 262).
     const unsigned units = (unsigned)(n_step * c.H_k);
     return f.group > 1 ? launch_kernel(false, k_attn_bwd_chunk<OP, MT, KP, DELTA, TWO, true, 2 * KP>, dim3(units), dim3(128 * KP), 0, c.stream, a)
                        : launch_kernel(false, k_attn_bwd_chunk<OP, MT, KP, DELTA, TWO, false, 4>, dim3(units * (KP / 2)), dim3(256), 0, c.stream, a);
