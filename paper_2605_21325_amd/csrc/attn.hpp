@@ -354,8 +354,8 @@ __global__ __launch_bounds__(512) void k_chunk_attn(AttnArgs a)
     };
     request(k0);
     bring(k0);
-    request(k0 + 1);
     __syncthreads();
+    request(k0 + 1);
     const MinusOne<OP> minus(ln);
     // This wavefront's outputs: two column tiles, and of MT = 4 token tiles the outer or the inner two (so that all have six pairs' worth of scores).
     constexpr int NI = MT / 2;
@@ -554,10 +554,10 @@ __device__ __forceinline__ void attn_states(const AttnArgs& a, char* const lds, 
     if (brings) {
         request(k0);
         bring(k0);
-        request(k0 + 1);
     }
     if (!SEGMENT && brings) {
         __syncthreads();
+        request(k0 + 1);
         for (int64_t k = k0; k < k1; ++k) {
             __syncthreads();  // W and U are in registers
             bring(k + 1);
@@ -588,6 +588,7 @@ __device__ __forceinline__ void attn_states(const AttnArgs& a, char* const lds, 
     const TurnOne<OP> one_k(ln, true), one_t(ln, false);
     float total = 0.f;
     __syncthreads();
+    if constexpr (SEGMENT) request(k0 + 1);
     for (int64_t k = k0; k < k1; ++k) {
         const float* const gl = gates + (k & 1) * StepGates<R>::FLOATS;
         float* const state_to = SEGMENT ? nullptr : a.rec_state + ((rec0 + k) * a.H + h) * a.d_k * a.d_v;

@@ -294,8 +294,8 @@ __device__ __forceinline__ void attn_bwd_state(const AttnBwdArgs& a, char* const
     request(k1 - 1);
     request_w(k1 - 1);
     bring(k1 - 1);
-    request(k1 - 2);
     __syncthreads();
+    request(k1 - 2);
     scores(k1 - 1);
     products(k1 - 1);
     __syncthreads();
