@@ -18,7 +18,9 @@ AttnArgs args_of(const AttnCall& c)
     a.Q = c.Q, a.K = c.K, a.U = c.U, a.W = c.W, a.g = c.g, a.state = c.state, a.O = c.O, a.final_state = c.final_state;
     const int64_t heads = (int64_t)c.n_seq * c.H;
     a.seg_state = reinterpret_cast<float*>(c.workspace);
-    a.seg_trans = a.seg_state + (c.n_seg - 1) * heads * c.d_k * c.d_v;
+    float* const first = a.seg_state + (c.n_seg - 1) * heads * c.d_k * c.d_v;
+    a.seg_first = c.n_seg > 1 && c.state == c.final_state && c.state ? first : nullptr;
+    a.seg_trans = first + heads * c.d_k * c.d_v;
     a.seg_decay = a.seg_trans;  // (one or the other)
     a.map = SeqMap{c.cu_seqlens, c.cu_chunks, c.Tlen, c.n_seq};
     a.H = c.H, a.group = c.H / c.H_k, a.d_k = c.d_k, a.d_v = c.d_v, a.C = c.C, a.n_seg = c.n_seg, a.scale = c.scale;
@@ -27,7 +29,7 @@ AttnArgs args_of(const AttnCall& c)
 
 template <int MT, int KP, bool DELTA, bool TWO> int go(const AttnCall& c)
 {
-    const AttnArgs a = args_of(c);
+    AttnArgs a = args_of(c);
     const unsigned heads = (unsigned)(c.n_seq * c.H), groups = (unsigned)((c.d_v + ATTN_COLS - 1) / ATTN_COLS);
     if (c.n_seg > 1) {
         const auto by = [&](unsigned cols) { return dim3(heads * ((c.d_v + cols - 1) / cols + (DELTA ? (c.d_k + cols - 1) / cols : 0)), (unsigned)c.n_seg - 1); };
@@ -37,6 +39,7 @@ template <int MT, int KP, bool DELTA, bool TWO> int go(const AttnCall& c)
         rc = DELTA ? launch_kernel(false, k_attn_join<KP>, dim3(heads * ((c.d_v + 15) / 16)), dim3(128 * KP), 0, c.stream, a)
                    : launch_kernel(false, k_attn_join_plain, dim3((unsigned)(((int64_t)heads * c.d_k * c.d_v + 255) / 256)), dim3(256), 0, c.stream, a);
         if (rc != LAUNCHED) return rc;
+        if (a.seg_first) a.state = a.seg_first;
     }
     return launch_kernel(false, k_chunk_attn<OP, MT, KP, DELTA, TWO>, dim3(heads * groups, (unsigned)c.n_seg), dim3(512), 0, c.stream, a);
 }

@@ -33,6 +33,7 @@ struct AttnArgs {
     // Segments of the sequences (a workgroup each), where there are too few heads: what a segment adds to a state and what it does to
     // the one before it, or the states before the segments from them.
     float *seg_state, *seg_trans, *seg_decay;
+    float* seg_first;  // a copy of `state` for the first segment, which runs beside the last one that writes over it; or null
     float *rec_state, *rec_value;  // for the gradient: the states before the steps [step][H], and V' where it is not U, [first token of the step][H], as put_turned leaves them
     float* rec_dg;                 // zeroed where two workgroups add to it
     SeqMap map;
@@ -664,6 +665,9 @@ template <int KP> __global__ __launch_bounds__(128 * KP) void k_attn_join(AttnAr
         const auto from = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(a.state) + (int64_t)hs * a.d_k * a.d_v, 0, a.state ? 4u * a.d_k * a.d_v : 0u, 0x00020000);
 #pragma unroll
         for (int r = 0; r < 4; ++r) S[r] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(from, place(r), 0, 0));
+        const auto first = __builtin_amdgcn_make_buffer_rsrc(a.seg_first + (int64_t)hs * a.d_k * a.d_v, 0, a.seg_first ? 4u * a.d_k * a.d_v : 0u, 0x00020000);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) __builtin_amdgcn_raw_buffer_store_b32(bits(S[r]), first, place(r), 0, 0);
     }
     const MinusOne<OP_BF16> minus(ln);
     v4f m[2][2 * KP], add[2];  // rows of M and L, of the next two segments
@@ -730,6 +734,7 @@ static __global__ __launch_bounds__(256) void k_attn_join_plain(AttnArgs a)
     if (i >= heads * size) return;
     const int64_t hs = i / size;
     float S = a.state ? a.state[i] : 0.f;
+    if (a.seg_first) a.seg_first[i] = S;
     for (int seg = 0; seg + 1 < a.n_seg; ++seg) {
         float* const L = a.seg_state + seg * heads * size + i;
         S = a.seg_decay[seg * heads + hs] * S + *L;

@@ -44,7 +44,8 @@ int attn_segments(int n_seq, int64_t n_chunk, int H, int d_v, bool has_w)
 int64_t attn_workspace(int n_seq, int64_t n_chunk, int H, int d_k, int d_v, bool has_w)
 {
     const int64_t n_seg = attn_segments(n_seq, n_chunk, H, d_v, has_w);
-    return (n_seg - 1) * n_seq * H * 4 * ((int64_t)d_k * d_v + (has_w ? (int64_t)d_k * d_k : 1));
+    if (n_seg == 1) return 0;
+    return 4 * n_seq * H * (n_seg * d_k * d_v + (n_seg - 1) * (has_w ? (int64_t)d_k * d_k : 1));  // (a state more: the one before the first token, which final_state may lie upon)
 }
 
 // Sizes of the chunk attention.
