@@ -1,4 +1,4 @@
-"""Sequences taken in segments (few heads, many chunks): the state overwritten in place."""
+"""Sequences taken in segments (few heads, many chunks): the state overwritten in place, and the chunk sizes and layers that prompts have."""
 import ctypes
 import os
 
@@ -7,7 +7,7 @@ import torch
 
 import paper_2605_21325_amd as tri
 from paper_2605_21325_amd import build as tri_build
-from test_layer_gpu import BF, HF, make
+from test_layer_gpu import BF, HF, check_forward, make
 
 
 def workspace(n_seq, chunks, H, d_k, d_v, has_w):
@@ -55,3 +55,21 @@ def test_the_state_in_place(lens, H, d_k, d_v, C, dtype, delta):
         state = x["state"].clone()
         o1, _ = tri.gdn_chunk_attn(one["q"], one["k"], one["u"], one["g"], C, W=one["w"], state=state, final_state=state, scale=0.3)
         assert torch.equal(o1[0], o) and torch.equal(state, final)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens,H,Hk,d_k,d_v,C,dtype,gate,delta,state", [
+    ([64 * 17 + 5], 2, 1, 128, 128, 64, BF, True, True, True),
+    ([64 * 17 + 5], 2, 2, 128, 128, 64, BF, False, True, False),
+    ([64 * 24], 2, 2, 128, 128, 64, HF, True, True, False),
+    ([64 * 33 + 1, 7], 1, 1, 128, 128, 64, BF, True, False, True),
+    ([128 * 17 + 3], 2, 1, 128, 128, 128, BF, False, True, False),
+    ([128 * 16 + 65], 1, 1, 128, 64, 128, HF, True, True, True),
+    ([128 * 18 + 64], 1, 1, 64, 128, 128, BF, True, False, True),
+])
+def test_segments_of_a_prompt(lens, H, Hk, d_k, d_v, C, dtype, gate, delta, state):
+    """As test_segments of the operators' tests, at the chunk sizes and layers that prompts have."""
+    assert workspace(len(lens), sum(-(-n // C) for n in lens), H, d_k, d_v, delta) > 0
+    x = make(lens, H, Hk, d_k, d_v, C, dtype, gate, delta, state, seed=33, rate=0.02)
+    o, final = tri.gdn_chunk_attn_varlen(x["q"], x["k"], x["u"], x["g"], lens, C, W=x["w"], state=x["state"], scale=0.3)
+    check_forward(o, final, x, lens, C, 0.3, dtype)
