@@ -28,9 +28,15 @@ def _has(t: Optional[torch.Tensor], name: str, shape, dtype) -> None:
         raise TypeError(f"{name} is {t.dtype}, not {dtype}")
 
 
-def _on(stream):
-    """Allocations belong to the stream the kernels run on."""
-    return torch.cuda.stream(stream) if isinstance(stream, torch.cuda.Stream) else _NOWHERE
+def _on(stream, device):
+    """Allocations belong to the stream the kernels run on: what is dropped when the call returns goes to work that stands behind them.  A stream
+    object of another library stands for its handle (0: the device's default stream)."""
+    if stream is None:
+        return _NOWHERE
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = int(stream.cuda_stream)
+        stream = torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)
+    return torch.cuda.stream(stream)
 
 
 _connected = None  # the native argument handling that knows these entry points
@@ -101,7 +107,7 @@ def gdn_chunk_attn(Q: torch.Tensor, K: torch.Tensor, U: torch.Tensor, g: Optiona
     H, H_k, d_k, d_v = _attn_checked(Q, K, U, g, W, state, (B, T), B)
     _has(O, "O", U.shape, U.dtype)
     _has(final_state, "final_state", (B, H, d_k, d_v), torch.float32)
-    with _on(stream):
+    with _on(stream, U.device):
         O = torch.empty_like(U) if O is None else O
         final_state = torch.empty((B, H, d_k, d_v), dtype=torch.float32, device=U.device) if final_state is None else final_state
         ws, n = _workspace(B, B * ((T + C - 1) // C) if C > 0 else 0, H, d_k, d_v, W is not None, U.device)
@@ -129,8 +135,8 @@ def gdn_chunk_attn_varlen(Q: torch.Tensor, K: torch.Tensor, U: torch.Tensor, g: 
     H, H_k, d_k, d_v = _attn_checked(Q, K, U, g, W, state, (total,), n_seq)
     _has(O, "O", U.shape, U.dtype)
     _has(final_state, "final_state", (n_seq, H, d_k, d_v), torch.float32)
-    cu_s, cu_c, n_seq, n_chunk, keep = _chunk_offsets(Q, seqlens, C, stream)
-    with _on(stream):
+    with _on(stream, U.device):
+        cu_s, cu_c, n_seq, n_chunk, keep = _chunk_offsets(Q, seqlens, C, stream)
         O = torch.empty_like(U) if O is None else O
         final_state = torch.empty((n_seq, H, d_k, d_v), dtype=torch.float32, device=U.device) if final_state is None else final_state
         ws, n = _workspace(n_seq, n_chunk, H, d_k, d_v, W is not None, U.device)
@@ -139,7 +145,7 @@ def gdn_chunk_attn_varlen(Q: torch.Tensor, K: torch.Tensor, U: torch.Tensor, g: 
                                              C, dtype_code(Q.dtype), d_k ** -0.5 if scale is None else scale, _stream_ptr(stream))
     if st != OK:
         raise TriInvError(st, "gdn_chunk_attn_varlen")
-    final_state._triinv_keepalive = keep  # the launch is asynchronous: the offsets live as long as the result
+    O._triinv_keepalive = final_state._triinv_keepalive = keep  # the launch is asynchronous: the offsets live as long as a result
     return O, final_state
 
 
@@ -151,7 +157,7 @@ def _attn_bwd(where, Q, K, U, g, dO, C, W, state, dstate, scale, stream, lead, n
     st = binding.lib().gdn_chunk_attn_bwd_workspace(n_token, n_chunk, H, d_k, d_v, C, W is not None, ctypes.byref(size))
     if st != OK:
         raise TriInvError(st, where)
-    with _on(stream):
+    with _on(stream, U.device):
         dQ, dK, dU = torch.empty_like(Q), torch.empty_like(K), torch.empty_like(U)
         dW = None if W is None else torch.empty_like(W)
         dg = None if g is None else torch.empty_like(g)
@@ -188,10 +194,13 @@ def gdn_chunk_attn_bwd_varlen(Q: torch.Tensor, K: torch.Tensor, U: torch.Tensor,
         if r is not None:
             return r
     total = Q.shape[0]
-    cu_s, cu_c, n_seq, n_chunk, keep = _chunk_offsets(Q, seqlens if isinstance(seqlens, (list, tuple)) else list(seqlens), C, stream)
+    with _on(stream, Q.device):
+        cu_s, cu_c, n_seq, n_chunk, keep = _chunk_offsets(Q, seqlens if isinstance(seqlens, (list, tuple)) else list(seqlens), C, stream)
     got = _attn_bwd("gdn_chunk_attn_bwd_varlen", Q, K, U, g, dO, C, W, state, dstate, scale, stream, (total,), n_seq, total, n_chunk,
                     (cu_s, cu_c, n_seq, total, n_chunk))
-    got[0]._triinv_keepalive = keep  # the launch is asynchronous: the offsets live as long as the result
+    for x in got:
+        if x is not None:
+            x._triinv_keepalive = keep  # the launch is asynchronous: the offsets live as long as a result
     return got
 
 
@@ -214,7 +223,7 @@ def gdn_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, g: Optional[torc
     _has(state, "state", (state.shape[0], H, d_k, d_v), torch.float32)
     _has(o, "o", v.shape, v.dtype)
     if o is None:
-        with _on(stream):
+        with _on(stream, v.device):
             o = torch.empty_like(v)
     st = binding.lib().gdn_step(_dev(q, "q"), _dev(k, "k"), _dev(v, "v"), _opt(g, "g"), _opt(beta, "beta"), _dev(state, "state"), _opt(slots, "slots"),
                                 _dev(o, "o"), B, state.shape[0], H, H_k, d_k, d_v, dtype_code(q.dtype), d_k ** -0.5 if scale is None else scale, _stream_ptr(stream))
@@ -228,7 +237,7 @@ def _norm(x, weight, residual, eps, group, y, scales, stream):
     N = x.numel() // D if D else 0
     _has(weight, "weight", (D,), x.dtype)
     _has(residual, "residual", x.shape, x.dtype)
-    with _on(stream):
+    with _on(stream, x.device):
         total = None if residual is None else torch.empty_like(x)
     st = binding.lib().add_rms_norm(_dev(x, "x"), _opt(residual, "residual"), _dev(weight, "weight"), _dev(y, "y"), _opt(scales, "scales"), _opt(total, "sum"), N, D,
                                     group, dtype_code(x.dtype), eps, _stream_ptr(stream))
@@ -244,7 +253,7 @@ def add_rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch
         r = f[0].norm(f[1], f[2], x, weight, residual, eps, -1)
         if r is not None:
             return r
-    with _on(stream):
+    with _on(stream, x.device):
         y = torch.empty_like(x)
     return y, _norm(x, weight, residual, eps, -1, y, None, stream)
 
@@ -257,7 +266,7 @@ def add_rms_norm_fp8(x: torch.Tensor, weight: torch.Tensor, residual: Optional[t
         r = f[0].norm(f[1], f[2], x, weight, residual, eps, group)
         if r is not None:
             return r
-    with _on(stream):
+    with _on(stream, x.device):
         y = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device)
         # (one a row: a trailing dimension of one group)
         scales = torch.empty((*x.shape[:-1], x.shape[-1] // group if group > 0 else 1), dtype=torch.float32, device=x.device)
@@ -276,7 +285,7 @@ def add_rms_norm_bwd(dy: torch.Tensor, s: torch.Tensor, weight: torch.Tensor, ep
     _has(dy, "dy", s.shape, s.dtype)
     _has(weight, "weight", (D,), s.dtype)
     _has(dsum, "dsum", s.shape, s.dtype)
-    with _on(stream):
+    with _on(stream, s.device):
         dx = torch.empty_like(s)
         dweight = torch.empty(D, dtype=torch.float32, device=s.device)
         ws = torch.empty(max(1, min(N, 512)) * D, dtype=torch.float32, device=s.device)
