@@ -6,6 +6,13 @@
 
 namespace triinv {
 
+// Workgroups 0 to n - 1 as blockIdx.y gridDim.x + blockIdx.x, and some more behind them: a dimension of a grid has fewer than 2^32 threads.
+inline dim3 long_grid(int64_t n)
+{
+    constexpr int64_t MOST = 1 << 21;  // of up to 1024 threads
+    return n <= MOST ? dim3((unsigned)n) : dim3((unsigned)MOST, (unsigned)((n + MOST - 1) / MOST));
+}
+
 // Chunk attention: arguments checked by the entry points.
 struct AttnCall {
     const void *Q, *K, *U, *W;

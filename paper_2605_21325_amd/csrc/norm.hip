@@ -139,7 +139,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void k_norm(NormCall
     __shared__ float sums[WAVES];
     __shared__ uint32_t mosts[WAVES];
     const int lane = threadIdx.x % LANES;
-    const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES;
+    const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * ROWS + threadIdx.x / LANES;
     if (row >= a.N) return;  // (whole wavefronts; with more than one to a row there is one row a workgroup)
     const int64_t at = row * a.D;
     v8f x[PIECES];
@@ -209,7 +209,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void k_norm(NormCall
 template <int DT, int OUT, bool RESIDUAL, int WAVES> int go_pieces(const NormCall& a)
 {
     const int pieces = (a.D + 512 * WAVES - 1) / (512 * WAVES);
-    const dim3 grid((unsigned)(WAVES == 1 ? (a.N + 3) / 4 : a.N)), block(WAVES == 1 ? 256 : 64 * WAVES);
+    const dim3 grid = long_grid(WAVES == 1 ? (a.N + 3) / 4 : a.N), block(WAVES == 1 ? 256 : 64 * WAVES);
     if constexpr (WAVES <= 4) {
         if (pieces <= 1) return launch_kernel(false, k_norm<DT, OUT, RESIDUAL, WAVES, 1>, grid, block, 0, a.stream, a);
     }
