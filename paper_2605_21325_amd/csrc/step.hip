@@ -39,7 +39,9 @@ template <int DT, int CG, int ROWS> __global__ __launch_bounds__(THREADS) void k
     __shared__ v4f part[RG][CG + 1];
     const int tid = threadIdx.x, cx = tid % CG, rg = tid / CG;
     const int groups = (a.d_v + 4 * CG - 1) / (4 * CG);
-    const int cg = blockIdx.x % groups, bh = blockIdx.x / groups, h = bh % a.H, b = bh / a.H;
+    const unsigned block = blockIdx.y * gridDim.x + blockIdx.x;
+    const int cg = block % groups, bh = block / groups, h = bh % a.H, b = bh / a.H;
+    if (b >= a.B) return;
     const int hk = h / (a.H / a.H_k);
     const int64_t slot = a.slots ? a.slots[b] : b;
     const int col = 4 * (cg * CG + cx);
@@ -114,7 +116,7 @@ template <int DT, int CG> int go(const StepCall& a)
 {
     constexpr int RG = THREADS / CG;
     const int groups = (a.d_v + 4 * CG - 1) / (4 * CG);
-    const dim3 grid((unsigned)((int64_t)a.B * a.H * groups));
+    const dim3 grid = long_grid((int64_t)a.B * a.H * groups);
     if (a.d_k <= 64) return launch_kernel(false, k_gdn_step<DT, CG, 64 / RG>, grid, dim3(THREADS), 0, a.stream, a);
     if (a.d_k <= 128) return launch_kernel(false, k_gdn_step<DT, CG, 128 / RG>, grid, dim3(THREADS), 0, a.stream, a);
     return launch_kernel(false, k_gdn_step<DT, CG, 256 / RG>, grid, dim3(THREADS), 0, a.stream, a);

@@ -21,3 +21,16 @@ def test_norm_of_more_rows_than_a_grid_has_threads_for_in_one_dimension():
     q0, scales0, _ = tri.add_rms_norm_fp8(x[:1 << 12], w)
     assert torch.equal(scales[-5:], scales0[:5]) and torch.equal(q[-5:].view(torch.uint8), q0[:5].view(torch.uint8))
     assert torch.equal(scales[:-5].view(-1, 1 << 12), scales0.view(1, -1).expand(1 << 14, -1))
+
+
+@pytest.mark.gpu
+def test_step_of_more_columns_than_a_grid_has_threads_for_in_one_dimension():
+    """2^24 states and some of one row of four columns, a workgroup of 256 threads each."""
+    B, H = (1 << 23) + 3, 2
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    rand = lambda *s: torch.randn(*s, generator=gen, device="cuda")
+    q, k, v, beta, state = rand(B, 1, 1), rand(B, 1, 1), rand(B, H, 4), torch.rand(B, H, generator=gen, device="cuda"), rand(B, H, 1, 4)
+    want = state.double() + k.double()[..., None] * (beta.double()[..., None] * (v.double() - k.double() * state.double()[:, :, 0]))[:, :, None]
+    o = tri.gdn_step(q, k, v, None, state, beta=beta, scale=0.5)
+    size = 1 + want.abs().amax()  # a handful of fp32 roundings
+    assert ((state.double() - want).abs().amax() <= 2.0 ** -21 * size ** 2) and ((o.double() - 0.5 * q.double() * want[:, :, 0]).abs() <= 2.0 ** -21 * size ** 2 * (1 + q.double().abs())).all()
