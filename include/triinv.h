@@ -302,7 +302,7 @@ int gdn_chunk_tri_solve_varlen(const void* K, const float* beta, const float* g,
  *   workspace    device, workspace_bytes of it as gdn_chunk_attn_workspace says, 16-byte aligned (NULL where that is 0).
  *   d_k          a multiple of 32, <= 128.   d_v  a multiple of 8, <= 512.   C  16, 32, 64 or 128.
  * Tlen = 0 or empty sequences: nothing of O, final_state = state.  The rows a chunk covers (H * max(d_k, d_v) * C elements) must
- * stay below 2^31 bytes.  The state is kept in fp32 and its products are carried out on 24 bits of it (22 with fp16); what is rounded to the
+ * stay below 2^31 bytes, sequences times heads times ceil(d_v / 64) below 2^23.  The state is kept in fp32 and its products are carried out on 24 bits of it (22 with fp16); what is rounded to the
  * operand type on the way to O has two parts.  fp16: |scale <q, k>| must stay below 65504.  Non-finite values stay in their
  * sequence and head, from their chunk on (within the chunk earlier tokens may receive them).
  * Two to three kernels instead of one where sequences and heads are few and prompts long (see the workspace), one otherwise; results may differ in their last bits
@@ -326,7 +326,7 @@ int gdn_chunk_attn_workspace(int n_seq, int64_t total_chunks, int H, int d_k, in
  *   dstate0      device, fp32 [B][H][d_k][d_v], written: the gradient of `state`; or NULL.  May be dstate itself.
  *   workspace    device, workspace_bytes of it as gdn_chunk_attn_bwd_workspace says (8 H d_k d_v bytes a chunk, twice that at C = 128, and, with W, 4 H d_v a token), 16-byte aligned.
  * The states are computed again, nothing of the forward call is needed.  Sums are fp32 and their order is fixed.  The rows a chunk covers must stay below
- * 2^31 bytes with d_v in fp32.  fp16: the chunk's values V' must stay below 65504.
+ * 2^31 bytes with d_v in fp32, sequences times heads times ceil(d_v / 64) below 2^22, chunks (C = 128: twice their number) times H_k below 2^23.  fp16: the chunk's values V' must stay below 65504.
  */
 int gdn_chunk_attn_bwd(const void* Q, const void* K, const void* U, const void* W, const float* g, const float* state,
                        const void* dO, const float* dstate, void* dQ, void* dK, void* dU, void* dW, float* dg, float* dstate0,

@@ -31,13 +31,16 @@ template <size_t NI, size_t NO> bool aliased(const Span (&in)[NI], const Span (&
     return false;
 }
 
+// Workgroups of 64 columns.
+int64_t attn_groups(int n_seq, int H, int d_v) { return (int64_t)n_seq * H * ((d_v + 63) / 64); }
+
 // Segments of a sequence, so that its heads and groups of 64 columns fill the 256 compute units.  With W a segment's state costs as much as its outputs: it pays where
 // there are four of them at least (8192 tokens in chunks of 64, d_k = d_v = 128, in us, segments in brackets: 8 heads 376 [1], 110 [16]; 16 heads 371 [1], 135 [8]; 32
 // heads 382 [1], 232 [4], 253 [8]; 48 heads 407 [1], 418 [2], 387 [5]; 64 heads 384 [1], 452 [4]; 96 heads 417 [1], 686 [4]).  Without W the states are half the
 // work, and twice the segments: 16 heads 328 [1], 88 [16]; 32 heads 327 [1], 150 [8]; 64 heads 337 [1], 257 [4]; 80 heads 341 [1], 336 [3]; 96 heads 348 [1], 446 [3].
 int attn_segments(int n_seq, int64_t n_chunk, int H, int d_v, bool has_w)
 {
-    const int64_t units = (int64_t)n_seq * H * ((d_v + 63) / 64), by_units = (has_w ? 256 : 512) / units, by_chunks = n_chunk / n_seq / 8;
+    const int64_t units = attn_groups(n_seq, H, d_v), by_units = (has_w ? 256 : 512) / units, by_chunks = n_chunk / n_seq / 8;
     if (by_units < 4 || by_chunks < 2) return 1;
     return (int)(by_units < by_chunks ? by_units : by_chunks);
 }
@@ -56,6 +59,7 @@ int attn_shape(int n_seq, int64_t n_token, int64_t n_chunk, int H, int H_k, int 
     if (d_k <= 0 || d_k % 32 || d_k > 128 || d_v <= 0 || d_v % 8 || d_v > 512) return TRIINV_ERR_BAD_SHAPE;
     if (n_chunk > 0x7fffffffLL / H || (int64_t)n_seq > 0x7fffffffLL / ((int64_t)H * 16)) return TRIINV_ERR_BAD_SHAPE;
     if ((int64_t)H * (d_k > d_v ? d_k : d_v) * C * 2 >= (1LL << 31)) return TRIINV_ERR_UNSUPPORTED;
+    if (attn_groups(n_seq, H, d_v) >= (1LL << 23)) return TRIINV_ERR_UNSUPPORTED;  // (512 threads each: a grid has fewer than 2^32)
     return TRIINV_OK;
 }
 
@@ -95,6 +99,8 @@ int attn_bwd_common(const void* Q, const void* K, const void* U, const void* W, 
 {
     if (dtype == TRIINV_F32) return TRIINV_ERR_UNSUPPORTED;
     if ((int64_t)H * d_v * C * 4 >= (1LL << 31)) return TRIINV_ERR_UNSUPPORTED;  // (values are read back in fp32)
+    // two walks, then 512 threads (256 each where there are two) a step and key head
+    if (attn_groups(n_seq, H, d_v) >= (1LL << 22) || n_chunk * (C > 64 ? 2 : 1) * H_k >= (1LL << 23)) return TRIINV_ERR_UNSUPPORTED;
     const int64_t need = attn_bwd_workspace(n_token, n_chunk, H, d_k, d_v, C, W != nullptr);
     if (n_token > 0 && (!Q || !K || !U || !dO || !dQ || !dK || !dU || !workspace || (W != nullptr) != (dW != nullptr))) return TRIINV_ERR_NULL;
     if (dg && !g) return TRIINV_ERR_NULL;

@@ -1,8 +1,11 @@
 """Calls of the layer's operators at the far end of what their entry points take."""
+import os
+
 import pytest
 import torch
 
 import paper_2605_21325_amd as tri
+from paper_2605_21325_amd import build as tri_build
 
 BF = torch.bfloat16
 
@@ -34,3 +37,16 @@ def test_step_of_more_columns_than_a_grid_has_threads_for_in_one_dimension():
     o = tri.gdn_step(q, k, v, None, state, beta=beta, scale=0.5)
     size = 1 + want.abs().amax()  # a handful of fp32 roundings
     assert ((state.double() - want).abs().amax() <= 2.0 ** -21 * size ** 2) and ((o.double() - 0.5 * q.double() * want[:, :, 0]).abs() <= 2.0 ** -21 * size ** 2 * (1 + q.double().abs())).all()
+
+
+@pytest.mark.parametrize("B,T,H,C,forward,backward", [
+    ((1 << 23) - 1, 0, 1, 16, True, False), (1 << 23, 0, 1, 16, False, False), (1 << 22, 0, 1, 16, True, False), (1 << 20, 0, 8, 16, False, False), ((1 << 22) - 1, 0, 1, 16, True, True),
+    (1, 16 << 23, 1, 16, True, False), (1, (16 << 23) - 16, 1, 16, True, True), (1, 128 << 22, 1, 128, True, False), (1, (64 << 23) - 64, 1, 64, True, True)])
+def test_more_workgroups_than_a_grid_has_threads_for_are_refused(B, T, H, C, forward, backward):
+    """Decided on the host; what is taken is refused for its misaligned Q instead, so that no kernel runs."""
+    if not os.path.exists(tri.binding.LIB_PATH):
+        tri_build.build()
+    L, at, room, align, unsupported = tri.lib(), lambda i: (i + 1) << 44, 1 << 62, -6, -9
+    sizes = (room, B, T, H, 1, 32, 8, C, tri.BF16, 1.0, None)
+    assert L.gdn_chunk_attn(at(0) + 2, at(1), at(2), None, None, None, at(3), None, at(4), *sizes) == (align if forward else unsupported)
+    assert L.gdn_chunk_attn_bwd(at(0) + 2, at(1), at(2), None, None, None, at(3), None, at(4), at(5), at(6), None, None, None, at(7), *sizes) == (align if backward else unsupported)
