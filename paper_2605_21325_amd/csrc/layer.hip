@@ -51,13 +51,20 @@ int64_t attn_workspace(int n_seq, int64_t n_chunk, int H, int d_k, int d_v, bool
     return 4 * n_seq * H * (n_seg * d_k * d_v + (n_seg - 1) * (has_w ? (int64_t)d_k * d_k : 1));  // (a state more: the one before the first token, which final_state may lie upon)
 }
 
-// Sizes of the chunk attention.
-int attn_shape(int n_seq, int64_t n_token, int64_t n_chunk, int H, int H_k, int d_k, int d_v, int C)
+// Sizes of the chunk attention, and the part of them that a workspace depends on.
+int attn_states_shape(int n_seq, int64_t n_chunk, int H, int d_k, int d_v)
 {
-    if (C != 16 && C != 32 && C != 64 && C != 128) return TRIINV_ERR_BAD_C;
-    if (n_seq <= 0 || H <= 0 || H_k <= 0 || H % H_k || n_token < 0 || n_chunk < 0) return TRIINV_ERR_BAD_SHAPE;
+    if (n_seq <= 0 || H <= 0 || n_chunk < 0) return TRIINV_ERR_BAD_SHAPE;
     if (d_k <= 0 || d_k % 32 || d_k > 128 || d_v <= 0 || d_v % 8 || d_v > 512) return TRIINV_ERR_BAD_SHAPE;
     if (n_chunk > 0x7fffffffLL / H || (int64_t)n_seq > 0x7fffffffLL / ((int64_t)H * 16)) return TRIINV_ERR_BAD_SHAPE;
+    return TRIINV_OK;
+}
+bool attn_C(int C) { return C == 16 || C == 32 || C == 64 || C == 128; }
+int attn_shape(int n_seq, int64_t n_token, int64_t n_chunk, int H, int H_k, int d_k, int d_v, int C)
+{
+    if (!attn_C(C)) return TRIINV_ERR_BAD_C;
+    if (H_k <= 0 || H % H_k || n_token < 0) return TRIINV_ERR_BAD_SHAPE;
+    if (const int rc = attn_states_shape(n_seq, n_chunk, H, d_k, d_v)) return rc;
     if ((int64_t)H * (d_k > d_v ? d_k : d_v) * C * 2 >= (1LL << 31)) return TRIINV_ERR_UNSUPPORTED;
     if (attn_groups(n_seq, H, d_v) >= (1LL << 23)) return TRIINV_ERR_UNSUPPORTED;  // (512 threads each: a grid has fewer than 2^32)
     return TRIINV_OK;
@@ -131,7 +138,7 @@ extern "C" {
 int gdn_chunk_attn_workspace(int n_seq, int64_t total_chunks, int H, int d_k, int d_v, int has_w, int64_t* bytes)
 {
     if (!bytes) return TRIINV_ERR_NULL;
-    if (n_seq <= 0 || total_chunks < 0 || H <= 0 || d_k <= 0 || d_v <= 0) return TRIINV_ERR_BAD_SHAPE;
+    if (const int rc = attn_states_shape(n_seq, total_chunks, H, d_k, d_v)) return rc;
     *bytes = attn_workspace(n_seq, total_chunks, H, d_k, d_v, has_w != 0);
     return TRIINV_OK;
 }
@@ -165,7 +172,9 @@ int gdn_chunk_attn_varlen(const void* Q, const void* K, const void* U, const voi
 int gdn_chunk_attn_bwd_workspace(int64_t total_tokens, int64_t total_chunks, int H, int d_k, int d_v, int C, int has_w, int64_t* bytes)
 {
     if (!bytes) return TRIINV_ERR_NULL;
-    if (total_tokens < 0 || total_chunks < 0 || H <= 0 || d_k <= 0 || d_v <= 0) return TRIINV_ERR_BAD_SHAPE;
+    if (!attn_C(C)) return TRIINV_ERR_BAD_C;
+    if (const int rc = attn_states_shape(1, total_chunks, H, d_k, d_v)) return rc;
+    if (total_tokens < 0 || total_tokens > total_chunks * C) return TRIINV_ERR_BAD_SHAPE;
     *bytes = attn_bwd_workspace(total_tokens, total_chunks, H, d_k, d_v, C, has_w != 0);
     return TRIINV_OK;
 }

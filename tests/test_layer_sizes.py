@@ -1,4 +1,5 @@
 """Calls of the layer's operators at the far end of what their entry points take."""
+import ctypes
 import os
 
 import pytest
@@ -50,3 +51,24 @@ def test_more_workgroups_than_a_grid_has_threads_for_are_refused(B, T, H, C, for
     sizes = (room, B, T, H, 1, 32, 8, C, tri.BF16, 1.0, None)
     assert L.gdn_chunk_attn(at(0) + 2, at(1), at(2), None, None, None, at(3), None, at(4), *sizes) == (align if forward else unsupported)
     assert L.gdn_chunk_attn_bwd(at(0) + 2, at(1), at(2), None, None, None, at(3), None, at(4), at(5), at(6), None, None, None, at(7), *sizes) == (align if backward else unsupported)
+
+
+@pytest.mark.parametrize("n_seq,chunks,H,d_k,d_v", [
+    (1, 10, 1, 1 << 30, 64), (1, 10, 1, 128, (1 << 31) - 1), (1, 10, 1, 96 + 16, 64), (1, 10, 1, 128, 12), (1 << 30, 10, 1 << 30, 128, 64), (1, 1 << 31, 1, 128, 64), (1, 1 << 62, 4, 128, 64),
+    (1, 1 << 20, 1 << 13, 128, 64)])
+def test_workspaces_of_what_no_call_takes_are_refused(n_seq, chunks, H, d_k, d_v):
+    """Sizes whose products pass 64 bits among them."""
+    if not os.path.exists(tri.binding.LIB_PATH):
+        tri_build.build()
+    n = ctypes.c_int64(-1)
+    assert tri.lib().gdn_chunk_attn_workspace(n_seq, chunks, H, d_k, d_v, 1, ctypes.byref(n)) == -5 and n.value == -1
+    assert tri.lib().gdn_chunk_attn_bwd_workspace(0, chunks, H << (n_seq > 1), d_k, d_v, 64, 1, ctypes.byref(n)) == -5 and n.value == -1
+
+
+@pytest.mark.parametrize("tokens,chunks,C,status", [(64 * 3, 3, 64, 0), (64 * 3 + 1, 3, 64, -5), (1 << 62, 3, 64, -5), (3, 3, 48, -2), (3, 3, 0, -2), (0, 0, 128, 0)])
+def test_workspace_of_a_gradient_by_its_tokens(tokens, chunks, C, status):
+    if not os.path.exists(tri.binding.LIB_PATH):
+        tri_build.build()
+    n = ctypes.c_int64(-1)
+    assert tri.lib().gdn_chunk_attn_bwd_workspace(tokens, chunks, 4, 128, 64, C, 1, ctypes.byref(n)) == status
+    assert n.value == (-1 if status else 4 * 4 * (2 * chunks * (2 if C > 64 else 1) * 128 * 64 + tokens * 64))
