@@ -303,7 +303,7 @@ int gdn_chunk_tri_solve_varlen(const void* K, const float* beta, const float* g,
  *   d_k          a multiple of 32, <= 128.   d_v  a multiple of 8, <= 512.   C  16, 32, 64 or 128.
  * Tlen = 0 or empty sequences: nothing of O, final_state = state.  The rows a chunk covers (H * max(d_k, d_v) * C elements) must
  * stay below 2^31 bytes, sequences times heads times ceil(d_v / 64) below 2^23.  The state is kept in fp32 and its products are carried out on 24 bits of it (22 with fp16); what is rounded to the
- * operand type on the way to O has two parts.  fp16: |scale <q, k>| must stay below 65504.  Non-finite values stay in their
+ * operand type on the way to O has two parts (fp16: of what a power of two has brought into its range).  Non-finite values stay in their
  * sequence and head, from their chunk on (within the chunk earlier tokens may receive them).
  * Two to three kernels instead of one where sequences and heads are few and prompts long (see the workspace), one otherwise; results may differ in their last bits
  * between the two.  gdn_chunk_attn_varlen: sequences packed back to back, arrays as in gdn_chunk_tri_inv_varlen, states [n_seq][H][d_k][d_v].

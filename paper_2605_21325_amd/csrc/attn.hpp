@@ -371,15 +371,15 @@ __global__ __launch_bounds__(512) void k_chunk_attn(AttnArgs a)
     }
     v4f acc[NI][2];
     Parts<2> pp[NI][NI];  // scores: pairs of tiles, two parts
+    int p_shift[NI] = {};  // fp16: of those (a score may lie anywhere, and 22 bits of it are there only in fp16's range)
     // The outputs of step k, whose Q S and scores are there: the scores' product with V', and the store.
     auto finish = [&](int64_t k) {
         const StepPos at = step_pos<R>(sq, k, k1, a.C);
-        if constexpr (OP == OP_F16) {
+        v4f sum[NI][2];  // (fp16: apart from Q S, for the powers of two of scores and values together may pass what fp32 holds)
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+        for (int ii = 0; ii < NI; ++ii)
 #pragma unroll
-                for (int ii = 0; ii < NI; ++ii) acc[ii][t] = times(acc[ii][t], pow2(shifts[4 + 4 * (k & 1) + ct + t]));
-        }
+            for (int t = 0; t < 2; ++t) sum[ii][t] = OP == OP_F16 ? zero4() : acc[ii][t];
         v4u vs[NI][2][2];
 #pragma unroll
         for (int tp = 0; tp < NI; ++tp)
@@ -396,7 +396,7 @@ __global__ __launch_bounds__(512) void k_chunk_attn(AttnArgs a)
 #pragma unroll
                 for (int ii = tp; ii < NI; ++ii)
 #pragma unroll
-                    for (int t = 0; t < 2; ++t) acc[ii][t] = mfma32<OP>(vs[tp][t][order == 1], pp[ii][tp].u[order == 0], acc[ii][t]);
+                    for (int t = 0; t < 2; ++t) sum[ii][t] = mfma32<OP>(vs[tp][t][order == 1], pp[ii][tp].u[order == 0], sum[ii][t]);
         const int left = a.d_v - wg_col;
         const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(static_cast<char*>(a.O) + at.row * stride_u + 2 * ((int64_t)h * a.d_v + wg_col), 0,
                                                             at.valid > 0 ? (uint32_t)(at.valid - 1) * stride_u + 2u * left : 0u, 0x00020000);
@@ -405,7 +405,12 @@ __global__ __launch_bounds__(512) void k_chunk_attn(AttnArgs a)
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 const int i = 16 * (ii == 0 ? half : 3 - half) + ln.n, col = 16 * (ct + t) + 4 * ln.q;
-                const v4f x = OP == OP_F16 ? times(acc[ii][t], pow2(-shifts[4 + 4 * (k & 1) + ct + t])) : acc[ii][t];
+                v4f x = sum[ii][t];
+                if constexpr (OP == OP_F16) {
+                    const float of_v = pow2(-shifts[4 + 4 * (k & 1) + ct + t]), of_p = pow2(-p_shift[ii]);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[r] = acc[ii][t][r] + x[r] * of_v * of_p;
+                }
                 __builtin_amdgcn_raw_buffer_store_b64(pack4<OP>(x), rsrc, col < left ? (uint32_t)i * stride_u + 2u * col : 0x80000000u, 0, 0);
             }
     };
@@ -482,6 +487,16 @@ __global__ __launch_bounds__(512) void k_chunk_attn(AttnArgs a)
                 for (int jt = 0; jt < 2 * ii + 2; ++jt)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) x[ii][jt][r] *= a.scale * __expf(jt >= 2 * ii ? gi - gj[jt][r] + edge[ii][jt & 1][r] : gi - gj[jt][r]);
+                if constexpr (OP == OP_F16) {
+                    float most = 0.f;
+#pragma unroll
+                    for (int jt = 0; jt < 2 * ii + 2; ++jt)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) most = fmaxf(most, fabsf(x[ii][jt][r]));
+                    p_shift[ii] = f16_shift(wave_max(most));
+#pragma unroll
+                    for (int jt = 0; jt < 2 * ii + 2; ++jt) x[ii][jt] = times(x[ii][jt], pow2(p_shift[ii]));
+                }
 #pragma unroll
                 for (int tp = 0; tp <= ii; ++tp) {
                     v4f two[2] = {x[ii][2 * tp], x[ii][2 * tp + 1]};

@@ -1,0 +1,51 @@
+"""The chunk attention and its gradient in fp16 where scores and values are far from 1: two parts of 16 bits hold 22 bits of an fp32 value
+only when a power of two brings it into fp16's range first.  Tolerances as in test_layer_gpu.py, which they do not depend on.
+
+Factors are chosen so that every result in fp16 stays a normal number: one chunk's outputs are scale |q| |u| with |q|, |k| near sqrt(d_k) and 1."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2605_21325_amd as tri
+from oracle import layer
+from test_layer_gpu import HF, U_OF, check_forward, close, exact, make, split, tol32
+
+pytestmark = pytest.mark.gpu
+
+U = U_OF[HF]
+
+
+def scaled(lens, H, Hk, d_k, d_v, C, delta, state, seed, **by):
+    x = make(lens, H, Hk, d_k, d_v, C, HF, True, delta, state, seed=seed)
+    for name, factor in by.items():
+        if x[name] is not None:
+            x[name] = (x[name].float() * factor).to(x[name].dtype)
+    return x
+
+
+SMALL = dict(u=2.0 ** 12, do=2.0 ** 12, scale=2.0 ** -20)  # scores near 2^-19
+LARGE = dict(u=2.0 ** -12, do=2.0 ** -12, scale=2.0 ** 20)  # scores far beyond 65504
+
+
+@pytest.mark.parametrize("lens,H,Hk,d_k,d_v,C,delta", [([40], 2, 2, 64, 64, 64, False), ([64, 33], 2, 1, 128, 128, 64, True), ([64], 2, 2, 64, 72, 128, False), ([128], 1, 1, 128, 64, 128, True), ([16, 9], 2, 2, 64, 64, 16, True),
+                                                      ([32], 1, 1, 128, 64, 32, False)])
+@pytest.mark.parametrize("by", [SMALL, LARGE], ids=["small", "large"])
+def test_outputs_of_scores_far_from_one(lens, H, Hk, d_k, d_v, C, delta, by):
+    """No state in front and one chunk a sequence: all of an output comes through the scores."""
+    by = dict(by)
+    scale = by.pop("scale")
+    x = scaled(lens, H, Hk, d_k, d_v, C, delta, False, 41, **by)
+    o, final = tri.gdn_chunk_attn_varlen(x["q"], x["k"], x["u"], x["g"], lens, C, W=x["w"], scale=scale)
+    check_forward(o, final, x, lens, C, scale, HF)
+    zero = dict(x, u=torch.zeros_like(x["u"]))
+    assert not tri.gdn_chunk_attn_varlen(x["q"], x["k"], zero["u"], x["g"], lens, C, W=x["w"], scale=scale)[0].any()
+
+
+def test_zero_scores_and_zero_values_leave_the_states_outputs():
+    """Nothing to add, whose power of two is the largest: the outputs are those of the state."""
+    lens, C = [64], 64
+    x = scaled(lens, 2, 2, 64, 64, C, False, True, 42, u=0.0)
+    x["k"] = torch.zeros_like(x["k"])
+    x["state"] = x["state"] * 2.0 ** 30
+    o, final = tri.gdn_chunk_attn_varlen(x["q"], x["k"], x["u"], x["g"], lens, C, state=x["state"], scale=2.0 ** -28)
+    check_forward(o, final, x, lens, C, 2.0 ** -28, HF)
