@@ -40,9 +40,11 @@ template <int OP, int MT, int KP, bool DELTA> struct BwdStateLayout {
         return n;
     }
     static constexpr int UNIT = 1024 * FULL_PARTS<OP>;
+    // fp16: the wavefront that forms the pair of tiles tp, jt and brings it into range: tiles (0, 0), (1, 0), (1, 1) | (2, 0), (3, 0), (3, 3) | (2, 1), (3, 1) | (2, 2), (3, 2).
+    static constexpr int maker(int tp, int jt) { return MT == 2 ? jt : tp == 0 ? 0 : jt == 3 ? 1 : jt + 1; }
     static constexpr int K_AT = 0, W_AT = 2 * ROWS, Q_AT = W_AT + (DELTA ? ROWS : 0), O_AT = Q_AT + ROWS, O_ROWS = R * UPIECES * 16, P_AT = O_AT + 2 * O_ROWS;
     static constexpr int X_AT = P_AT + units_before(MT) * UNIT, X_WAVE = 2 * KP * 1024;  // fp32 tiles, a wavefront's columns
-    static constexpr int G_AT = X_AT + 4 * X_WAVE, BYTES = G_AT + 2 * StepGates<R>::FLOATS * 4;
+    static constexpr int G_AT = X_AT + 4 * X_WAVE, SHIFT_AT = G_AT + 2 * StepGates<R>::FLOATS * 4, BYTES = SHIFT_AT + 16;
 };
 
 template <class LY> __device__ __forceinline__ int unit_at(int jt)  // units_before at run time
@@ -62,6 +64,7 @@ __device__ __forceinline__ void attn_bwd_state(const AttnBwdArgs& a, char* const
     typedef BwdStateLayout<OP, MT, KP, DELTA> LY;
     constexpr int R = LY::R, FP = FULL_PARTS<OP>, PIECES = LY::PIECES, TILES = MT * (MT + 1) / 2;
     float* const gates = reinterpret_cast<float*>(lds + LY::G_AT);
+    int* const shifts = reinterpret_cast<int*>(lds + LY::SHIFT_AT);  // fp16: of the parts of P, by the wavefronts that form them
     const Lane ln = lane_id();
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane16 = 16 * (16 * ln.q + ln.n);
     const unsigned groups = (a.d_v + ATTN_COLS - 1) / ATTN_COLS;
@@ -116,20 +119,33 @@ __device__ __forceinline__ void attn_bwd_state(const AttnBwdArgs& a, char* const
 #pragma unroll
                     for (int jt = 0; jt <= 2 * tp + 1; ++jt) pt[tp][part][jt] = *reinterpret_cast<const v4u*>(lds + LY::P_AT + LY::UNIT * (LY::units_before(jt) + tp - jt / 2) + 1024 * part + lane16);
             }
-            const float s_down = OP == OP_F16 ? pow2(-s_shift) : 1.f, decay = gl[3 * R];
+            typedef int v4i __attribute__((ext_vector_type(4)));
+            v4i p_shift = {0, 0, 0, 0};
+            if constexpr (OP == OP_F16) p_shift = *reinterpret_cast<const v4i*>(shifts);
+            const float decay = gl[3 * R];
 #pragma unroll
             for (int tb = 0; tb < MT; ++tb) {
                 const v4f e = *reinterpret_cast<const v4f*>(gl + R + 16 * tb + 4 * ln.q);
+                const float f = OP == OP_F16 ? pow2(-s_shift) * pow2(p_shift[LY::maker(tb / 2, tb)]) : 1.f;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) dv[tb][r] *= OP == OP_F16 ? e[r] * s_down : e[r];
+                for (int r = 0; r < 4; ++r) dv[tb][r] *= OP == OP_F16 ? e[r] * f : e[r];
             }
             in_order();
 #pragma unroll
-            for (int tp = 0; tp < MT / 2; ++tp)
+            for (int tp = 0; tp < MT / 2; ++tp) {
+                if constexpr (OP == OP_F16) {
+#pragma unroll
+                    for (int jt = 0; jt < 2 * tp; ++jt) dv[jt] = times(dv[jt], pow2(p_shift[LY::maker(tp, jt)] - p_shift[LY::maker(tp - 1, jt)]));
+                }
 #pragma unroll
                 for (int part = FP - 1; part >= 0; --part)
 #pragma unroll
                     for (int jt = 0; jt <= 2 * tp + 1; ++jt) dv[jt] = mfma32<OP>(pt[tp][part][jt], o[tp], dv[jt]);
+            }
+            if constexpr (OP == OP_F16) {
+#pragma unroll
+                for (int jt = 0; jt < MT; ++jt) dv[jt] = times(dv[jt], pow2(-p_shift[LY::maker(MT / 2 - 1, jt)]));
+            }
 #pragma unroll
             for (int i = 0; i < 2 * KP; ++i) {
                 const v4f x = *reinterpret_cast<const v4f*>(lds + LY::X_AT + LY::X_WAVE * wave + 1024 * i + lane16);
@@ -214,13 +230,16 @@ __device__ __forceinline__ void attn_bwd_state(const AttnBwdArgs& a, char* const
             lw.load(static_cast<const char*>(a.W) + at.row * stride_w + 2 * (int64_t)h * a.d_k, stride_w, a.d_k, at.valid, tid);
         }
     };
-    // P, as operands of P^T: token rows 4 q + r, column n; a share of the tiles a wavefront (one without a tile forms the last one again)
-    constexpr int SHARE = (TILES + 3) / 4;
+    // P, as operands of P^T: token rows 4 q + r, column n; a share of the tiles a wavefront (one without a tile forms the last one again); fp16: both tiles of a pair
+    // by one wavefront, which brings what it forms into range by one power of two.
+    constexpr int SHARE = OP == OP_F16 && MT == 2 ? 2 : (TILES + 3) / 4;
     int its[SHARE], jts[SHARE], units[SHARE];
 #pragma unroll
     for (int j = 0; j < SHARE; ++j) {
         int idx = j * 4 + w4 < TILES ? j * 4 + w4 : TILES - 1, it = 0;
         while (idx > it) idx -= ++it;
+        if constexpr (OP == OP_F16 && MT == 2) it = w4 == 0 ? j : 1, idx = w4 == 0 ? 0 : 1;
+        if constexpr (OP == OP_F16 && MT == 4) it = w4 == 0 ? (j + 1) / 2 : j == 0 ? 2 : 3, idx = w4 == 0 ? j / 2 : j == 2 && w4 == 1 ? 3 : w4 - 1;
         its[j] = it, jts[j] = idx, units[j] = LY::UNIT * (unit_at<LY>(idx) + (it >> 1) - (idx >> 1)) + 8 * (it & 1);
     }
     auto scores = [&](int64_t k) {
@@ -253,9 +272,18 @@ __device__ __forceinline__ void attn_bwd_state(const AttnBwdArgs& a, char* const
         }
 #pragma unroll
         for (int j = 0; j < SHARE; ++j) {
-            const bool on = jts[j] == its[j];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) x[j][r] *= a.scale * __expf(on && ln.n > 4 * ln.q + r ? -__builtin_inff() : gi[j][r] - gj[j]);
+            for (int r = 0; r < 4; ++r) x[j][r] *= a.scale * __expf(jts[j] == its[j] && ln.n > 4 * ln.q + r ? -__builtin_inff() : gi[j][r] - gj[j]);
+        }
+        if constexpr (OP == OP_F16) {
+            const int shift = f16_shift(wave_max(most_of(x)));
+            if (ln.q == 0 && ln.n == 0) shifts[MT == 2 && w4 > 1 ? 1 : w4] = shift;
+#pragma unroll
+            for (int j = 0; j < SHARE; ++j) x[j] = times(x[j], pow2(shift));
+        }
+#pragma unroll
+        for (int j = 0; j < SHARE; ++j) {
+            const bool on = jts[j] == its[j];
             char* unit = lds + LY::P_AT + units[j] + in_place(lane16);
 #pragma unroll
             for (int part = 0; part < FP; ++part) {

@@ -49,3 +49,42 @@ def test_zero_scores_and_zero_values_leave_the_states_outputs():
     x["state"] = x["state"] * 2.0 ** 30
     o, final = tri.gdn_chunk_attn_varlen(x["q"], x["k"], x["u"], x["g"], lens, C, state=x["state"], scale=2.0 ** -28)
     check_forward(o, final, x, lens, C, 2.0 ** -28, HF)
+
+
+def check_gradient(x, lens, C, scale):
+    """Against the statement in 64 bits, with the tolerances of test_gradient in test_layer_gpu.py."""
+    H, d_v = x["u"].shape[-2:]
+    Hk, d_k = x["q"].shape[-2:]
+    got = tri.gdn_chunk_attn_bwd_varlen(x["q"], x["k"], x["u"], x["g"], x["do"], lens, C, W=x["w"], state=x["state"], dstate=x["dstate"], scale=scale)
+    t32 = tol32(d_k + d_v, C)
+    state, dstate = (lambda s, h=slice(None): None if x["state"] is None else exact(x["state"][s, h])), (lambda s, h=slice(None): None if x["dstate"] is None else exact(x["dstate"][s, h]))
+    for s, n in enumerate(lens):
+        part = {m: split(x[m], lens, s) for m in ("q", "k", "u", "w", "g", "do")}
+        one = lambda h, k: (part["q"][:, k], part["k"][:, k], part["u"][:, h], None if part["w"] is None else part["w"][:, h], part["g"][:, h], C, state(s, h), scale)
+        every = slice(None)
+        ref = layer.chunk_attn_bwd(*one(every, every), part["do"], dstate(s))
+        a = sum(lens[:s])
+        for name, mine, r, tol in zip(("dQ", "dK", "dU", "dW"), got[:4], ref[:4], (U, U, U, 2 * U)):
+            if r is not None:
+                assert np.abs(r).max() < 65504  # (else the inputs would be the test's mistake)
+                close(mine[a:a + n], r, tol, f"{name} of sequence {s}")
+        rep, size, last = H // Hk, [], []
+        for h in range(H):
+            args = one(slice(h, h + 1), slice(h // rep, h // rep + 1))
+            r = layer.chunk_attn_bwd(*args, part["do"][:, h:h + 1], dstate(s, slice(h, h + 1)))
+            size.append((np.abs(part["q"][:, h // rep] * r[0][:, 0]) + np.abs(part["k"][:, h // rep] * r[1][:, 0])).sum(-1))
+            final = layer.chunk_attn(*args)[1]
+            last.append(0.0 if x["dstate"] is None else np.linalg.norm(final) * np.linalg.norm(dstate(s)[h]) / np.sqrt(d_k * d_v))
+        close(got[4][a:a + n].T, ref[4].T, t32, f"dg of sequence {s}", np.stack(size) + np.array(last)[:, None] + np.abs(ref[4].T))
+        if x["state"] is not None:
+            close(got[5][s].flatten(1), ref[5].reshape(H, -1), t32, f"gradient of the state of sequence {s}")
+
+
+@pytest.mark.parametrize("lens,H,Hk,d_k,d_v,C,delta", [([40], 2, 2, 64, 64, 64, False), ([64, 33], 2, 1, 128, 128, 64, True), ([128], 1, 1, 128, 64, 128, True), ([16, 9], 2, 2, 64, 64, 16, True),
+                                                      ([32], 1, 1, 128, 64, 32, False), ([150], 2, 2, 64, 72, 64, True)])
+@pytest.mark.parametrize("by", [SMALL, dict(LARGE, do=2.0 ** -15, dstate=2.0 ** 5)], ids=["small", "large"])
+def test_gradients_of_scores_far_from_one(lens, H, Hk, d_k, d_v, C, delta, by):
+    """What arrives comes through the outputs (and large scores: little of it through the final state): dU is the scores', and what W hands on to the state."""
+    by = dict(dict(u=1.0, dstate=0.0), **{n: f for n, f in by.items() if n != "u"})
+    scale = by.pop("scale")
+    check_gradient(scaled(lens, H, Hk, d_k, d_v, C, delta, True, 43, **by), lens, C, scale)
