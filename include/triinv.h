@@ -326,7 +326,7 @@ int gdn_chunk_attn_workspace(int n_seq, int64_t total_chunks, int H, int d_k, in
  *   dstate0      device, fp32 [B][H][d_k][d_v], written: the gradient of `state`; or NULL.  May be dstate itself.
  *   workspace    device, workspace_bytes of it as gdn_chunk_attn_bwd_workspace says (8 H d_k d_v bytes a chunk, twice that at C = 128, and, with W, 4 H d_v a token), 16-byte aligned.
  * The states are computed again, nothing of the forward call is needed.  Sums are fp32 and their order is fixed.  The rows a chunk covers must stay below
- * 2^31 bytes with d_v in fp32, sequences times heads times ceil(d_v / 64) below 2^22, chunks (C = 128: twice their number) times H_k below 2^23.  fp16: the chunk's values V' must stay below 65504.
+ * 2^31 bytes with d_v in fp32, sequences times heads times ceil(d_v / 64) below 2^22, chunks (C = 128: twice their number) times H_k below 2^23.  fp16: what is not an operand as it stands is brought into the type's range before it is split.
  */
 int gdn_chunk_attn_bwd(const void* Q, const void* K, const void* U, const void* W, const float* g, const float* state,
                        const void* dO, const float* dstate, void* dQ, void* dK, void* dU, void* dW, float* dg, float* dstate0,

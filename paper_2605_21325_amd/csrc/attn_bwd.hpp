@@ -384,14 +384,22 @@ template <int OP, int N, int MT, int THREADS> struct ValueLoader {
             v[i][1] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at + 16u * of_band, 0, 0));
         }
     }
-    __device__ __forceinline__ void store(char* m, int plane, int tid) const
+    __device__ __forceinline__ float most() const
+    {
+        float x = 0.f;
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) x = fmaxf(x, most_of(v[i]));
+        return x;
+    }
+    // (fp16: times 2^shift)
+    __device__ __forceinline__ void store(char* m, int plane, int shift, int tid) const
     {
         const int tb = tid >> 7;
         if (MT < BAND && tb >= MT) return;
         char* const to = m + LdsRows<8>::at(16 * tb + (tid & 15), (tid >> 4) & 7);
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) {
-            const Parts<N> p = split_pair<OP, N>(v[i][0], v[i][1]);
+            const Parts<N> p = OP == OP_F16 ? split_pair<OP, N>(times(v[i][0], pow2(shift)), times(v[i][1], pow2(shift))) : split_pair<OP, N>(v[i][0], v[i][1]);
 #pragma unroll
             for (int j = 0; j < N; ++j) *reinterpret_cast<v4u*>(to + j * plane + i * BAND * 16 * LdsRows<8>::BYTES) = p.u[j];
         }
@@ -521,12 +529,29 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attn_bwd_chunk(AttnBwdArgs a)
             its[j] = it, jts[j] = x;
         }
         float s_ds = 0.f;
-        int s_shift = 0, d_shift = 0, z_shift = 0;
+        int s_shift = 0, d_shift = 0, z_shift = 0, v_shift = 0;
         for (int v0 = 0; v0 < a.d_v; v0 += 64) {
             lo.store(lds + LY::O_AT, tid);
             if constexpr (DELTA) {
                 lu.store(lds + LY::DV_AT, tid);
-                lv.store(lds + LY::V_AT, LY::BLOCK, tid);
+                if constexpr (OP == OP_F16) {  // V' into fp16's range, by a power of two that all wavefronts agree on, and what there is of the products with it
+                    const float mine = wave_max(lv.most());
+                    if (ln.q == 0 && ln.n == 0) red1[wave] = mine;
+                    __syncthreads();
+                    float most = red1[0];
+#pragma unroll
+                    for (int w = 1; w < WAVES; ++w) most = fmaxf(most, red1[w]);
+                    const int nv = __builtin_amdgcn_readfirstlane(f16_shift(most));
+                    const float cv = v0 ? pow2(nv - v_shift) : 1.f;
+                    v_shift = nv;
+#pragma unroll
+                    for (int j = 0; j < SHARE; ++j) M[j] = times(M[j], cv);
+#pragma unroll
+                    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                        for (int it = 0; it < MT; ++it) Y[kt][it] = times(Y[kt][it], cv);
+                }
+                lv.store(lds + LY::V_AT, LY::BLOCK, v_shift, tid);
             } else {
                 lu.store(lds + LY::V_AT, tid);
             }
@@ -534,6 +559,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attn_bwd_chunk(AttnBwdArgs a)
             const bool last_block = v0 + 64 >= a.d_v;
             const int next_h = last_block ? (SHARED && h + 1 < h0 + a.group ? h + 1 : h) : h, next_v = last_block ? (SHARED && h + 1 < h0 + a.group ? 0 : a.d_v) : v0 + 64;
             if (next_v < a.d_v) request(next_h, next_v);
+            if constexpr (OP == OP_F16) in_order();  // (registers, as below)
             // dO V'^T, turned: value tokens down, output tokens across
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks)
@@ -652,7 +678,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attn_bwd_chunk(AttnBwdArgs a)
             const float gi = gl[16 * its[j] + ln.n];
             const v4f gj = *reinterpret_cast<const v4f*>(gl + 16 * jts[j] + 4 * ln.q);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) M[j][r] *= a.scale * __expf(jts[j] < its[j] || 4 * ln.q + r <= ln.n ? gi - gj[r] : -__builtin_inff());
+            for (int r = 0; r < 4; ++r) M[j][r] *= (OP == OP_F16 && DELTA ? pow2(-v_shift) : 1.f) * a.scale * __expf(jts[j] < its[j] || 4 * ln.q + r <= ln.n ? gi - gj[r] : -__builtin_inff());
         }
         int m_shift = 0;
         if constexpr (OP == OP_F16) {
@@ -678,7 +704,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attn_bwd_chunk(AttnBwdArgs a)
         __syncthreads();
         // dQ (turned): lanes are tokens i, K^T M^T over the tokens j <= i.   dK: lanes are tokens j, Q^T M over i >= j.
         const float up = OP == OP_F16 ? pow2(m_shift) : 1.f, down = OP == OP_F16 ? pow2(-m_shift) : 1.f;
-        const float s_down = OP == OP_F16 ? pow2(-s_shift) : 1.f, d_down = OP == OP_F16 ? pow2(-d_shift) : 1.f;
+        const float s_down = OP == OP_F16 ? pow2(-s_shift) : 1.f, d_down = OP == OP_F16 ? pow2(-d_shift) * pow2(-v_shift) : 1.f;
         float inter = 0.f;
         v4u kt_op[KT][MT / 2], qt_op[KT][MT / 2];
 #pragma unroll

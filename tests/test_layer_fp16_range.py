@@ -15,8 +15,8 @@ pytestmark = pytest.mark.gpu
 U = U_OF[HF]
 
 
-def scaled(lens, H, Hk, d_k, d_v, C, delta, state, seed, **by):
-    x = make(lens, H, Hk, d_k, d_v, C, HF, True, delta, state, seed=seed)
+def scaled(lens, H, Hk, d_k, d_v, C, delta, with_state, seed, **by):
+    x = make(lens, H, Hk, d_k, d_v, C, HF, True, delta, with_state, seed=seed)
     for name, factor in by.items():
         if x[name] is not None:
             x[name] = (x[name].float() * factor).to(x[name].dtype)
@@ -88,3 +88,13 @@ def test_gradients_of_scores_far_from_one(lens, H, Hk, d_k, d_v, C, delta, by):
     by = dict(dict(u=1.0, dstate=0.0), **{n: f for n, f in by.items() if n != "u"})
     scale = by.pop("scale")
     check_gradient(scaled(lens, H, Hk, d_k, d_v, C, delta, True, 43, **by), lens, C, scale)
+
+
+@pytest.mark.parametrize("lens,H,Hk,d_k,d_v,C", [([40], 2, 2, 64, 64, 64), ([150, 33], 2, 1, 128, 128, 64), ([200], 1, 1, 128, 72, 128), ([16, 9], 2, 2, 64, 264, 16), ([70], 1, 1, 96, 64, 32)])
+@pytest.mark.parametrize("by", [dict(u=2.0 ** -18, state=2.0 ** -18, do=2.0 ** 6, dstate=2.0 ** 6), dict(u=2.0 ** 12, state=2.0 ** 17, dstate=2.0 ** -9, scale=2.0 ** -10)], ids=["small", "large"])
+def test_gradients_of_values_far_from_one(lens, H, Hk, d_k, d_v, C, by):
+    """V' = U - W S of 2^-18, and of more than 65504 (of a state in fp32)."""
+    by = dict(by)
+    scale = by.pop("scale", 1.0)
+    x = scaled(lens, H, Hk, d_k, d_v, C, True, True, 44, **by)
+    check_gradient(x, lens, C, scale)
