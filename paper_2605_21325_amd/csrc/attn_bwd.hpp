@@ -406,6 +406,10 @@ template <int OP, int N, int MT, int THREADS> struct ValueLoader {
     }
 };
 
+// fp16: the power of two of a block of columns when those before it (v0 of them) took `before`.  It only falls: what has been summed up is never
+// scaled past what fp32 holds, and a block of less than the largest needs no more bits than those.
+__device__ __forceinline__ int shift_so_far(int shift, int before, int v0) { return v0 && before < shift ? before : shift; }
+
 __device__ __forceinline__ float wave_sum(float x)
 {
     for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
@@ -541,7 +545,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attn_bwd_chunk(AttnBwdArgs a)
                     float most = red1[0];
 #pragma unroll
                     for (int w = 1; w < WAVES; ++w) most = fmaxf(most, red1[w]);
-                    const int nv = __builtin_amdgcn_readfirstlane(f16_shift(most));
+                    const int nv = shift_so_far(__builtin_amdgcn_readfirstlane(f16_shift(most)), v_shift, v0);
                     const float cv = v0 ? pow2(nv - v_shift) : 1.f;
                     v_shift = nv;
 #pragma unroll
@@ -579,7 +583,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attn_bwd_chunk(AttnBwdArgs a)
                 for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) most_s = fmaxf(most_s, fabsf(sv[kt][i >> 3][i >> 2 & 1][i & 3])), most_d = fmaxf(most_d, fabsf(dsv[kt][i >> 3][i >> 2 & 1][i & 3]));
-                const int ns = f16_shift(wave_max(most_s)), nd = f16_shift(wave_max(most_d));
+                const int ns = shift_so_far(f16_shift(wave_max(most_s)), s_shift, v0), nd = shift_so_far(f16_shift(wave_max(most_d)), d_shift, v0);
                 const float us = pow2(ns), ud = pow2(nd), cs = v0 ? pow2(ns - s_shift) : 1.f, cd = v0 ? pow2(nd - d_shift) : 1.f;
                 s_shift = ns, d_shift = nd;
                 float cz = cs;
@@ -589,7 +593,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attn_bwd_chunk(AttnBwdArgs a)
                     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) most_z = fmaxf(most_z, fabsf(szv[kt][i >> 3][i >> 2 & 1][i & 3]));
-                    const int nz = f16_shift(wave_max(most_z));
+                    const int nz = shift_so_far(f16_shift(wave_max(most_z)), z_shift, v0);
                     cz = v0 ? pow2(nz - z_shift) : 1.f;
                     z_shift = nz;
 #pragma unroll

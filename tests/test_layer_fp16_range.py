@@ -98,3 +98,14 @@ def test_gradients_of_values_far_from_one(lens, H, Hk, d_k, d_v, C, by):
     scale = by.pop("scale", 1.0)
     x = scaled(lens, H, Hk, d_k, d_v, C, True, True, 44, **by)
     check_gradient(x, lens, C, scale)
+
+
+@pytest.mark.parametrize("C,Hk,delta", [(64, 2, False), (64, 1, False), (64, 2, True), (128, 2, True), (128, 1, True)])
+@pytest.mark.parametrize("d_v", [128, 200])
+def test_gradients_of_columns_of_zeros_behind_large_ones(C, Hk, delta, d_v):
+    """Columns of the state are taken 64 at a time; those behind the first ones hold nothing, whose power of two is the largest there is."""
+    lens = [70]
+    x = scaled(lens, 2, Hk, 64, d_v, C, delta, True, 45, state=2.0 ** 70, w=0.0, **(dict(k=0.0) if delta else {}))  # (with keys a dW = -dU S^T would be 2^70)
+    for name in ("u", "state", "dstate", "do"):
+        x[name][..., 64:] = 0
+    check_gradient(x, lens, C, 2.0 ** -70)
