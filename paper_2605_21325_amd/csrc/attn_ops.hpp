@@ -40,9 +40,13 @@ __device__ __forceinline__ unsigned xcd_neighbours(unsigned b, unsigned n)
 }
 
 // A workgroup's sequence, and its place among the `per` that a sequence has.  Where packed sequences need more than one round of the 256 compute units the longest begin
-// (each of them on one XCD, the next on the next), so that none of them starts when the others are done.
-constexpr int LENGTHS_SORTED = 256;  // sequences at most
-__device__ __forceinline__ bool by_length(const SeqMap& m, unsigned n) { return m.cu_seqlens && n > 256u && m.n_seq <= LENGTHS_SORTED; }
+// (each of them on one XCD, the next on the next), so that none of them starts when the others are done.  Every workgroup ranks the lengths for itself, in time proportional to
+// their number, and from the fourth round on the order of the call does as well.  In us, order of the call / by length, 128 channels and columns, W: lengths from 1 to 2200, 4
+// heads, 48 sequences (384 workgroups) 143 / 113, 64 170 / 142, 96 (768) 236 / 207, 128 293 / 271, 160 (1280) 359 / 344; to 1000, 48 72 / 55, 96 115 / 107, 128 151 / 142, 160 181 / 182; of
+// 16 heads 16 (512) 73 / 77, 24 111 / 105, 32 (1024) 132 / 144, 64 262 / 270; to 600, 2 heads, 128 (512) 58 / 52, 160 72 / 70, 250 (1000) 100 / 113.  Equal lengths, which gain
+// nothing: 48 of 4 heads and 500 tokens 59 / 61, 128 128 / 140, 256 254 / 301.
+constexpr int LENGTHS_SORTED = 128;  // sequences at most
+__device__ __forceinline__ bool by_length(const SeqMap& m, unsigned n) { return m.cu_seqlens && n > 256u && n <= 768u && m.n_seq <= LENGTHS_SORTED; }
 struct SeqUnit {
     int seq;
     unsigned unit;
