@@ -38,10 +38,14 @@ int64_t attn_groups(int n_seq, int H, int d_v) { return (int64_t)n_seq * H * ((d
 // there are four of them at least (8192 tokens in chunks of 64, d_k = d_v = 128, in us, segments in brackets: 8 heads 376 [1], 110 [16]; 16 heads 371 [1], 135 [8]; 32
 // heads 382 [1], 232 [4], 253 [8]; 48 heads 407 [1], 418 [2], 387 [5]; 64 heads 384 [1], 452 [4]; 96 heads 417 [1], 686 [4]).  Without W the states are half the
 // work, and twice the segments: 16 heads 328 [1], 88 [16]; 32 heads 327 [1], 150 [8]; 64 heads 337 [1], 257 [4]; 80 heads 341 [1], 336 [3]; 96 heads 348 [1], 446 [3].
+// Four chunks a segment at least, and four segments: with two of them W's states cost what the outputs save.  More than sixteen segments only of eight chunks or more,
+// for the join takes them one after the other.  8 heads of 128, chunks of 64, W, one segment / segments of four chunks / of eight: 12 chunks 38 / 41 / 38, 16 50 / 43 / 60, 24 73 /
+// 48 / 63, 32 95 / 53 / 65, 64 185 / 73 / 74, of 2 heads 128 363 / 101 / 89, 256 720 / 168 / 123; without W 16 46 / 31 / 46, 32 87 / 34 / 48, 128 333 / 62 / 54, of 2 heads 330 / 40 / 51.
 int attn_segments(int n_seq, int64_t n_chunk, int H, int d_v, bool has_w)
 {
-    const int64_t units = attn_groups(n_seq, H, d_v), by_units = (has_w ? 256 : 512) / units, by_chunks = n_chunk / n_seq / 8;
-    if (by_units < 4 || by_chunks < 2) return 1;
+    const int64_t units = attn_groups(n_seq, H, d_v), by_units = (has_w ? 256 : 512) / units, chunks = n_chunk / n_seq;
+    if (by_units < 4 || chunks < 16) return 1;
+    const int64_t by_chunks = chunks < 64 ? chunks / 4 : chunks < 128 ? 16 : chunks / 8;
     return (int)(by_units < by_chunks ? by_units : by_chunks);
 }
 int64_t attn_workspace(int n_seq, int64_t n_chunk, int H, int d_k, int d_v, bool has_w)

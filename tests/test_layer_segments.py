@@ -73,3 +73,10 @@ def test_segments_of_a_prompt(lens, H, Hk, d_k, d_v, C, dtype, gate, delta, stat
     x = make(lens, H, Hk, d_k, d_v, C, dtype, gate, delta, state, seed=33, rate=0.02)
     o, final = tri.gdn_chunk_attn_varlen(x["q"], x["k"], x["u"], x["g"], lens, C, W=x["w"], state=x["state"], scale=0.3)
     check_forward(o, final, x, lens, C, 0.3, dtype)
+
+
+def test_a_prompt_has_segments_from_sixteen_chunks_on():
+    """Four at least, of four chunks at least: two segments were slower than none (1024 tokens of 8 heads with W: 60 against 50 us, four 43)."""
+    state, other = 4 * 8 * 128 * 128, 4 * 8 * 128 * 128
+    count = lambda chunks: (workspace(1, chunks, 8, 128, 128, 1) + other) // (state + other) or 1
+    assert [count(n) for n in (1, 15, 16, 24, 64, 127, 128, 200)] == [1, 1, 4, 6, 16, 16, 16, 16]  # (256 / 16 units: 16 at most)
