@@ -362,7 +362,9 @@ int gdn_step(const void* q, const void* k, const void* v, const float* g, const 
  *   scales             device, fp32: [N] (group = 0), or [N][D / 128] (group = 128): max |y| over the row or the 128 columns over 448, 1 where
  *                      that is 0.  NULL with group = -1.
  *   D                  a multiple of 8 (group = 128: of 128), <= 16384.
- * Sums and the norm are fp32.  A row with a NaN or an infinity is NaN (and its scales).
+ * Sums and the norm are fp32.  A row with a NaN is NaN, its scales too.  A row with an infinity (or whose squares sum beyond fp32's range) has a norm
+ * that is infinite: infinite elements become NaN, the others 0; in 8 bits the scale of the row, or of the 128 columns, with such an element is NaN and
+ * with it all of them, other columns' scale is 1.
  */
 int add_rms_norm(const void* x, const void* residual, const void* weight, void* y, float* scales, void* sum,
                  int64_t N, int D, int group, int dtype, float eps, void* hip_stream);
