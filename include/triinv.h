@@ -303,10 +303,10 @@ int gdn_chunk_tri_solve_varlen(const void* K, const float* beta, const float* g,
  *   d_k          a multiple of 32, <= 128.   d_v  a multiple of 8, <= 512.   C  16, 32, 64 or 128.
  * Tlen = 0 or empty sequences: nothing of O, final_state = state.  The rows a chunk covers (H * max(d_k, d_v) * C elements) must
  * stay below 2^31 bytes, sequences times heads times ceil(d_v / 64) below 2^23.  The state is kept in fp32 and its products are carried out on 24 bits of it (22 with fp16); what is rounded to the
- * operand type on the way to O has two parts (fp16: of what a power of two has brought into its range).  Non-finite values stay in their
+ * operand type on the way to O has two parts (fp16: of what a power of two has brought into its range; the states themselves must stay below 2^66).  Non-finite values stay in their
  * sequence and head, from their chunk on (within the chunk earlier tokens may receive them).
  * Two to three kernels instead of one where sequences and heads are few and prompts long (see the workspace), one otherwise; results may differ in their last bits
- * between the two.  gdn_chunk_attn_varlen: sequences packed back to back, arrays as in gdn_chunk_tri_inv_varlen, states [n_seq][H][d_k][d_v].
+ * between the two, and so with the number and the mean length of the sequences of a call.  gdn_chunk_attn_varlen: sequences packed back to back, arrays as in gdn_chunk_tri_inv_varlen, states [n_seq][H][d_k][d_v].
  */
 int gdn_chunk_attn(const void* Q, const void* K, const void* U, const void* W, const float* g, const float* state,
                    void* O, float* final_state, void* workspace, int64_t workspace_bytes,
@@ -325,7 +325,8 @@ int gdn_chunk_attn_workspace(int n_seq, int64_t total_chunks, int H, int d_k, in
  *   dg           device, fp32 [B][Tlen][H], written: the gradient of the chunk-local cumulative log-decay as it was given; or NULL.
  *   dstate0      device, fp32 [B][H][d_k][d_v], written: the gradient of `state`; or NULL.  May be dstate itself.
  *   workspace    device, workspace_bytes of it as gdn_chunk_attn_bwd_workspace says (8 H d_k d_v bytes a chunk, twice that at C = 128, and, with W, 4 H d_v a token), 16-byte aligned.
- * The states are computed again, nothing of the forward call is needed.  Sums are fp32 and their order is fixed.  The rows a chunk covers must stay below
+ * The states are computed again, nothing of the forward call is needed.  Sums are fp32 and their order is fixed.  dW is the product of dU as it is written, in the
+ * operand type, and of 16 bits (fp16: 22) of the state: its error is that of two roundings to the type, and what a dU below fp16's normal numbers has lost it lacks.  The rows a chunk covers must stay below
  * 2^31 bytes with d_v in fp32, sequences times heads times ceil(d_v / 64) below 2^22, chunks (C = 128: twice their number) times H_k below 2^23.  fp16: what is not an operand as it stands is brought into the type's range before it is split.
  */
 int gdn_chunk_attn_bwd(const void* Q, const void* K, const void* U, const void* W, const float* g, const float* state,
@@ -348,6 +349,7 @@ int gdn_chunk_attn_bwd_workspace(int64_t total_tokens, int64_t total_chunks, int
  *   slots   device, int32 [B]: sequence b's place in `state`, or NULL for b itself.  A place outside 0 .. n_slot - 1 (padding):
  *           nothing is updated and o is zero.  No two sequences may have the same place.
  *   d_k     1 to 256.   d_v   a multiple of 4, <= 512.
+ * Sums are fp32; their order follows from B * H and the sizes of a head.
  */
 int gdn_step(const void* q, const void* k, const void* v, const float* g, const float* beta, float* state, const int32_t* slots,
              void* o, int B, int64_t n_slot, int H, int H_k, int d_k, int d_v, int dtype, float scale, void* hip_stream);
@@ -362,7 +364,7 @@ int gdn_step(const void* q, const void* k, const void* v, const float* g, const 
  *   scales             device, fp32: [N] (group = 0), or [N][D / 128] (group = 128): max |y| over the row or the 128 columns over 448, 1 where
  *                      that is 0.  NULL with group = -1.
  *   D                  a multiple of 8 (group = 128: of 128), <= 16384.
- * Sums and the norm are fp32.  A row with a NaN is NaN, its scales too.  A row with an infinity (or whose squares sum beyond fp32's range) has a norm
+ * Sums and the norm are fp32, the order of the sums follows from N and D.  A row with a NaN is NaN, its scales too.  A row with an infinity (or whose squares sum beyond fp32's range) has a norm
  * that is infinite: infinite elements become NaN, the others 0; in 8 bits the scale of the row, or of the 128 columns, with such an element is NaN and
  * with it all of them, other columns' scale is 1.
  */

@@ -14,9 +14,11 @@
 // The halves are separated by barriers, across which V' and the parts of S go through LDS.  A wavefront per SIMD that waits needs another to take its place,
 // which is what the second four are for.
 //
-// Bound by the matrix unit and by the chain of a step: d_k = d_v = 128 takes 3.3 thousand cycles of matrix instructions a SIMD and step of 64 tokens, half of
-// them for the second and third parts of S (products of fp32 states), and a step lasts 7; a chip full of it runs at 1.6 to 1.9 GHz.  Measured, bf16:
-// 8 x 8192 tokens, 16 heads 440 us (the bytes at the rate of a copy: 246); 48 packed sequences of 1100 on average, 4 heads, no W 106 (44).
+// Bound by the chain of a step: d_k = d_v = 128 takes 3.3 thousand cycles of matrix instructions a SIMD and step of 64 tokens, half of them for the second and
+// third parts of S (products of fp32 states), and a step lasts 7: of a SIMD's 204 of them 124 stand in the one wavefront of the recursion, behind each other and behind two splits
+// of V', and the matrix unit works half of the time.  A chip full of it runs at 1.6 to 1.9 GHz.  Measured: 8 x 8192 tokens, 16 heads, bf16 447 to 473 us from card to card (the
+// bytes at the rate of a copy: 246); 48 packed sequences of 1100 on average, 4 heads, fp16, no W 105 to 107 (44).
+// Decays of scores by __expf: |g_i - g_j| 2^-24 of the value and a bit, which the difference in its exponent is no better than.
 #pragma once
 
 #include <type_traits>

@@ -10,9 +10,11 @@
 // Two kernels: the walks over the steps (k_attn_bwd_walks: half of its workgroups take the states and values again, half dS, last step first, with dU); everything
 // else, all steps at once (k_attn_bwd_chunk).  The states between them go through memory in fp32: 0.74 GB written and 1.1 GB read for
 // 4 x 4096 tokens of 16 heads of 128, where inputs and results are 0.61 GB.  The walks are bound by a step's chain (4.8 us) and what it moves (3.8 TB/s), the other by its instructions (half of the
-// vector unit's cycles, a quarter of the matrix unit's) and that traffic.  Measured there: 310 and 268 us, 566 to 576 in all (one walk after the other: 214 + 336 us).
-// dg is the difference of large sums, so what enters it (dO S^T, V' dS'^T, M) is formed from all 24 bits (fp16: 22) of its fp32 operands; dW ends in 16 bits
-// and is formed from dU as it is written and 16 bits of the state (its error is that of two roundings to the type in place of one: 2.3e-3 against 1.7e-3 in bf16).
+// vector unit's cycles, a quarter of the matrix unit's) and that traffic.  Measured there: 304 and 260 us at the shortest, 376 and 302 at the median of calls under the profiler,
+// 562 to 576 in all (one walk after the other: 214 + 336 us).
+// dg is the difference of large sums, so what enters it (dO S^T, V' dS'^T, M) is formed from all 24 bits (fp16: 22, in its range by powers of two) of its fp32 operands, with decays
+// as in the forward pass; dW ends in 16 bits and is formed from dU as it is written and 16 bits (fp16: 22) of the state (its error is that of two roundings to the type in place of
+// one: 2.3e-3 against 1.7e-3 in bf16; the unrounded gradient would be 4 bytes more an element to write and to read).
 #pragma once
 #include "attn.hpp"
 

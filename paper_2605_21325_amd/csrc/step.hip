@@ -122,7 +122,7 @@ template <int DT, int CG> int go(const StepCall& a)
     return launch_kernel(false, k_gdn_step<DT, CG, 256 / RG>, grid, dim3(THREADS), 0, a.stream, a);
 }
 // 32 columns a workgroup where those of 64 would leave compute units without work (16 heads of 128 x 128, bf16, in us: one sequence 4.6 and 4.6, four 5.1 and 5.4,
-// eight 6.7 and 6.2, sixteen 11.4 and 7.8, 64 34 and 26; 256 of 32 heads 217 and 187, where loads and stores that stay in the caches take 209).
+// eight 6.7 and 6.2, sixteen 12.0 and 8.1, 64 36 and 28; 256 of 32 heads 224 and 200, where loads and stores that stay in the caches take 215).
 template <int DT> int pick(const StepCall& a) { return (int64_t)a.B * a.H * ((a.d_v + 31) / 32) < 512 ? go<DT, 8>(a) : go<DT, 16>(a); }
 
 }  // namespace

@@ -2,6 +2,7 @@
 chunks with one decay per head, the same layer's single token, the root-mean-square norm with the residual's addition.
 
 A call uses the current stream (or `stream`); tensors it makes itself are allocated on it.  Everything must be contiguous and in device memory.
+Autograd records none of them (as it does none of binding.py's): a gradient is the call of its own beside each.
 """
 from __future__ import annotations
 
