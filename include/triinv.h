@@ -382,6 +382,95 @@ int add_rms_norm(const void* x, const void* residual, const void* weight, void* 
 int add_rms_norm_bwd(const void* dy, const void* s, const void* weight, const void* dsum, void* dx, float* dweight,
                      void* workspace, int64_t workspace_bytes, int64_t N, int D, int dtype, float eps, void* hip_stream);
 
+/*
+ * qk_norm_rope: norms of queries and keys for each head, rotated by position in the same pass.  For a head x of d elements, its weight w and a
+ * token's position p:
+ *     y = x w / sqrt(mean(x^2) + eps)      (TRIINV_HEADS_UNIT: x w / sqrt(sum(x^2) + eps), to unit length)
+ *     pairs (a, b) of the first rot elements of y, t = p inv_freq_i:   a' = a cos t - b sin t,   b' = b cos t + a sin t
+ * with the pairs (i, i + rot / 2), or (2 i, 2 i + 1) with TRIINV_HEADS_INTERLEAVED.
+ *   q, q_out            device, [N] rows of H heads of d elements, element type dtype (fp32, fp16 or bf16), q_stride and q_out_stride elements from a
+ *                       token to the next (columns of a projection as they are); q_out is written and may be q itself.
+ *   k, k_out            the same with H_k heads; H_k = 0: none (NULL).  k_out may be k itself.
+ *   q_weight, k_weight  device, [d], the same type, or NULL for ones.
+ *   positions           device, int32 [N] (TRIINV_HEADS_POS64: int64, up to 2^53 in magnitude); NULL with rot = 0.
+ *   inv_freq            device, fp32 [rot / 2], radians a position; NULL with rot = 0.  The angle is their exact product without its whole turns.
+ *   d  1 to 512.   rot  even, 0 (no rotation) to d.   N (H + H_k) < 2^31.
+ * Pointers need the alignment of an element only here.  Norms are fp32; a head with a NaN is NaN; a head with an infinity (or whose squares sum beyond fp32's range)
+ * has an infinite norm: its infinite elements become NaN (with their partners in a rotation), the others 0.  Rows of one stride may lie beside each other in one buffer.
+ */
+int qk_norm_rope(const void* q, const void* k, const void* q_weight, const void* k_weight, const void* positions, const float* inv_freq,
+                 void* q_out, void* k_out, int64_t N, int64_t q_stride, int64_t k_stride, int64_t q_out_stride, int64_t k_out_stride,
+                 int H, int H_k, int d, int rot, int dtype, uint32_t flags, float eps, void* hip_stream);
+#define TRIINV_HEADS_UNIT 0x1u
+#define TRIINV_HEADS_INTERLEAVED 0x2u
+#define TRIINV_HEADS_POS64 0x4u
+
+/*
+ * qk_norm_rope_bwd: its gradient, from the same inputs and the gradients of q_out and k_out.  With z the gradient turned back by the token's angles and
+ * n = 1 / sqrt(mean(x^2) + eps) (or of the sum):
+ *     dx = n (z w - x n^2 mean(z w x))  (to unit length: the sum in the mean's place);   dw = sum over tokens and heads of z x n
+ *   dq_out, dk_out, dq, dk  rows as q and k, each with its stride; dq and dk are written; dq may be dq_out itself, dk dk_out.
+ *   dq_weight, dk_weight    device, fp32 [d], written, or NULL.
+ *   workspace               device, workspace_bytes of it as qk_norm_rope_bwd_workspace says (NULL where neither weight's gradient is asked for), 16-byte aligned.
+ * The weights' sums are fp32 and have an order that follows from N, the heads, d and the type.
+ */
+int qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const void* q, const void* k, const void* q_weight, const void* k_weight,
+                     const void* positions, const float* inv_freq, void* dq, void* dk, float* dq_weight, float* dk_weight,
+                     void* workspace, int64_t workspace_bytes, int64_t N, int64_t dq_out_stride, int64_t dk_out_stride,
+                     int64_t q_stride, int64_t k_stride, int64_t dq_stride, int64_t dk_stride,
+                     int H, int H_k, int d, int rot, int dtype, uint32_t flags, float eps, void* hip_stream);
+int qk_norm_rope_bwd_workspace(int64_t N, int H, int H_k, int d, int64_t* bytes);
+
+/*
+ * gated_scan: the gated recurrence channel by channel over whole sequences, and the state behind them:
+ *     h_t = a_t h_(t-1) + b_t,   a = exp(g)  (TRIINV_SCAN_LOGIT: a = 1 / (1 + exp(-g)));   b = x  (TRIINV_SCAN_MIX: b = (1 - a) x)
+ *   x, h         device, [B * Tlen] rows of D elements, element type dtype (fp32, fp16 or bf16), x_stride and h_stride elements from a token to the
+ *                next (columns of a projection as they are); h is written.
+ *   g            device, rows of D elements of type g_dtype: dtype or fp32; g_stride.
+ *   state        device, fp32 [B][D], the state before the first token, or NULL for zeros.
+ *   final_state  device, fp32 [B][D], written, or NULL.  May be `state` itself.
+ *   workspace    device, workspace_bytes of it as gated_scan_workspace says, 16-byte aligned (NULL where that is 0).
+ *   D  1 to 2^20.   B Tlen < 2^31.   B ceil(D / 64) < 2^26.
+ * Pointers need the alignment of an element only, but for the workspace.  States and sums are fp32.  Tlen = 0 or empty sequences: final_state = state.  A log-decay of -infinity begins anew.
+ * Decays above 1 (g > 0) are taken as they are, as long as the products of neighbouring ones stay in fp32's range.  Non-finite values stay in their sequence and channel,
+ * from their token on.  gated_scan_varlen: sequences packed back to back, cu_seqlens device, [n_seq + 1] (trusted as in gdn_chunk_tri_inv_varlen), states [n_seq][D].
+ */
+int gated_scan(const void* x, const void* g, const float* state, void* h, float* final_state, void* workspace, int64_t workspace_bytes,
+               int B, int64_t Tlen, int D, int64_t x_stride, int64_t g_stride, int64_t h_stride, int dtype, int g_dtype, uint32_t flags, void* hip_stream);
+int gated_scan_varlen(const void* x, const void* g, const float* state, void* h, float* final_state, void* workspace, int64_t workspace_bytes,
+                      const int64_t* cu_seqlens, int n_seq, int64_t total_tokens, int D, int64_t x_stride, int64_t g_stride, int64_t h_stride,
+                      int dtype, int g_dtype, uint32_t flags, void* hip_stream);
+#define TRIINV_SCAN_LOGIT 0x1u
+#define TRIINV_SCAN_MIX 0x2u
+/* Bytes of workspace that these and their gradients need for n_seq sequences of total_tokens tokens together. */
+int gated_scan_workspace(int64_t total_tokens, int n_seq, int D, int64_t* bytes);
+
+/*
+ * gated_scan_bwd: its gradient, against the time, from the inputs, h as it was written and the gradients dh of h and dstate (or NULL) of final_state:
+ *     r_t = dh_t + a_(t+1) r_(t+1)  (+ dstate at the last token);   dx = r  (mix: r (1 - a));   dstate0 = a_0 r_0
+ *     dg = r (h_(t-1) - [mix: x]) a  (logit: times 1 - a)
+ *   x            may be NULL without TRIINV_SCAN_MIX.
+ *   h, dh, dx    rows of D elements of type dtype, dg of g_dtype, each with its stride; dx and dg are written.
+ *   dstate0      device, fp32 [B][D], written, or NULL.  May be dstate itself.
+ * Sums are fp32.  dg holds the rounding of h to its type.  Everything else as in gated_scan.
+ */
+int gated_scan_bwd(const void* x, const void* g, const void* h, const float* state, const void* dh, const float* dstate, void* dx, void* dg, float* dstate0,
+                   void* workspace, int64_t workspace_bytes, int B, int64_t Tlen, int D, int64_t x_stride, int64_t g_stride, int64_t h_stride, int64_t dh_stride,
+                   int64_t dx_stride, int64_t dg_stride, int dtype, int g_dtype, uint32_t flags, void* hip_stream);
+int gated_scan_bwd_varlen(const void* x, const void* g, const void* h, const float* state, const void* dh, const float* dstate, void* dx, void* dg, float* dstate0,
+                          void* workspace, int64_t workspace_bytes, const int64_t* cu_seqlens, int n_seq, int64_t total_tokens, int D, int64_t x_stride, int64_t g_stride,
+                          int64_t h_stride, int64_t dh_stride, int64_t dx_stride, int64_t dg_stride, int dtype, int g_dtype, uint32_t flags, void* hip_stream);
+
+/*
+ * gated_scan_step: one token of the recurrence, the state updated in place: state[slot] <- a state[slot] + b, h = that in dtype.
+ *   x, h     device, [B] rows of D elements of type dtype; g rows of g_dtype; each with its stride.  h is written.
+ *   state    device, fp32 [n_slot][D], read and written.
+ *   slots    device, int32 [B]: sequence b's place in `state`, or NULL for b itself.  A place outside 0 .. n_slot - 1 (padding): nothing is
+ *            updated and h is zero.  No two sequences may have the same place.
+ */
+int gated_scan_step(const void* x, const void* g, float* state, const int32_t* slots, void* h, int B, int64_t n_slot, int D, int64_t x_stride, int64_t g_stride,
+                    int64_t h_stride, int dtype, int g_dtype, uint32_t flags, void* hip_stream);
+
 /* Human-readable name of a status code (static storage, never NULL). */
 const char* triinv_status_string(int status);
 

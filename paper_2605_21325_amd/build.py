@@ -44,7 +44,7 @@ UNITS = [
     for nb in (8, 4, 2, 1) for op in (0, 1, 2)
 ] + [
     (f"{name}_op{op}", f"{name}.hip", [f"-DTRIINV_INST_OP={op}"]) for name in ("attn_bwd", "attn") for op in (1, 2)
-] + [("norm", "norm.hip", []), ("step", "step.hip", []), ("layer", "layer.hip", []), ("api", "api.hip", [])]
+] + [("scan", "scan.hip", []), ("heads", "heads.hip", []), ("mixer", "mixer.hip", []), ("norm", "norm.hip", []), ("step", "step.hip", []), ("layer", "layer.hip", []), ("api", "api.hip", [])]
 
 
 def _sources_mtime() -> float:

@@ -1,35 +1,11 @@
 // C-ABI of the layer's other operators (see include/triinv.h): arguments checked on the host, then one of the launchers of layer.hpp.
 // No allocation, no synchronisation.
+#include "entry.hpp"
 #include "layer.hpp"
 
 namespace {
 
 using namespace triinv;
-
-bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
-bool overlap(const void* a, uint64_t na, const void* b, uint64_t nb)
-{
-    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
-    return a && b && na && nb && a0 < b0 + nb && b0 < a0 + na;
-}
-int finish(int rc) { return rc == LAUNCHED ? TRIINV_OK : rc == NOT_BUILT ? TRIINV_ERR_UNSUPPORTED : TRIINV_ERR_LAUNCH; }
-bool any_dtype(int d) { return d == TRIINV_F32 || d == TRIINV_F16 || d == TRIINV_BF16; }
-
-struct Span {
-    const void* p;
-    uint64_t bytes;
-};
-// Whether a result overlaps one of the inputs or another result.
-template <size_t NI, size_t NO> bool aliased(const Span (&in)[NI], const Span (&out)[NO])
-{
-    for (size_t i = 0; i < NO; ++i) {
-        for (const Span& x : in)
-            if (overlap(x.p, x.bytes, out[i].p, out[i].bytes)) return true;
-        for (size_t j = 0; j < i; ++j)
-            if (overlap(out[j].p, out[j].bytes, out[i].p, out[i].bytes)) return true;
-    }
-    return false;
-}
 
 // Workgroups of 64 columns.
 int64_t attn_groups(int n_seq, int H, int d_v) { return (int64_t)n_seq * H * ((d_v + 63) / 64); }

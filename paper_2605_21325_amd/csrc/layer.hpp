@@ -83,4 +83,62 @@ struct NormBwdCall {
 };
 int launch_norm_bwd(const NormBwdCall& a);
 
+// Norms of queries and keys for each head with the rotation: tokens' strides in elements.
+struct HeadsCall {
+    const void *q, *k, *q_weight, *k_weight, *positions;
+    const float* inv_freq;
+    void *q_out, *k_out;
+    int64_t N, q_stride, k_stride, q_out_stride, k_out_stride;
+    int H, H_k, d, rot, dtype;  // rot = 0: no rotation
+    bool unit, interleaved, pos64;
+    float eps;
+    hipStream_t stream;
+};
+int launch_heads(const HeadsCall& a);
+
+struct HeadsBwdCall {
+    const void *dq_out, *dk_out, *q, *k, *q_weight, *k_weight, *positions;
+    const float* inv_freq;
+    void *dq, *dk;
+    float *dq_weight, *dk_weight, *partial;  // partial: [groups][2 d], or null where neither weight's gradient is asked for
+    int64_t N, dq_out_stride, dk_out_stride, q_stride, k_stride, dq_stride, dk_stride;
+    int H, H_k, d, rot, dtype, groups;
+    bool unit, interleaved, pos64;
+    float eps;
+    hipStream_t stream;
+};
+int heads_bwd_groups(int64_t N, int H, int H_k, int d);
+int launch_heads_bwd(const HeadsBwdCall& a);
+
+// The gated recurrence: tokens' strides in elements.
+struct ScanCall {
+    const void *x, *g;  // x null: not needed (gradient without mix)
+    const float* state;
+    const void *h, *dh;  // of the gradient
+    const float* dstate;
+    void *out, *dg;  // out: h, or the gradient of x
+    float* last;     // the final state, or the gradient of the initial one
+    char* workspace;
+    const int64_t* cu_seqlens;  // device, or null: n_seq sequences of Tlen tokens
+    int64_t Tlen, N, x_stride, g_stride, h_stride, dh_stride, out_stride, dg_stride;
+    int n_seq, D, dtype, g_dtype;
+    bool logit, mix;
+    hipStream_t stream;
+};
+int64_t scan_workspace(int64_t N, int n_seq, int D);
+int launch_scan(const ScanCall& a);
+int launch_scan_bwd(const ScanCall& a);
+
+struct ScanStepCall {
+    const void *x, *g;
+    float* state;
+    const int32_t* slots;
+    void* h;
+    int64_t n_slot, x_stride, g_stride, h_stride;
+    int B, D, dtype, g_dtype;
+    bool logit, mix;
+    hipStream_t stream;
+};
+int launch_scan_step(const ScanStepCall& a);
+
 }  // namespace triinv
