@@ -430,23 +430,21 @@ int qk_norm_rope_bwd_workspace(int64_t N, int H, int H_k, int d, int64_t* bytes)
  *   state        device, fp32 [B][D], the state before the first token, or NULL for zeros.
  *   final_state  device, fp32 [B][D], written, or NULL.  May be `state` itself.
  *   workspace    device, workspace_bytes of it as gated_scan_workspace says, 16-byte aligned (NULL where that is 0).
- *   D  1 to 2^20.   B Tlen < 2^31.
+ *   D  1 to 2^20.   B Tlen < 2^31.   B ceil(D / 64) < 2^31.
  * Pointers need the alignment of an element only, but for the workspace.  States and sums are fp32.  Tlen = 0 or empty sequences: final_state = state.  A log-decay of -infinity begins anew.
  * Decays above 1 (g > 0) are taken as they are, as long as the products of neighbouring ones stay in fp32's range.  Non-finite values stay in their sequence and channel,
  * from their token on.  A channel's bits depend on its sequence's values up to the token alone: not on the other sequences, their number or the packing.
- * gated_scan_varlen: sequences packed back to back, arrays as in gdn_chunk_tri_inv_varlen with chunks of TRIINV_SCAN_CHUNK tokens (trusted in the same way), states [n_seq][D].
+ * gated_scan_varlen: sequences packed back to back, cu_seqlens device, int64 [n_seq + 1], the sequences' first tokens and then total_tokens (trusted), states [n_seq][D].
  */
-#define TRIINV_SCAN_CHUNK 64
 int gated_scan(const void* x, const void* g, const float* state, void* h, float* final_state, void* workspace, int64_t workspace_bytes,
                int B, int64_t Tlen, int D, int64_t x_stride, int64_t g_stride, int64_t h_stride, int dtype, int g_dtype, uint32_t flags, void* hip_stream);
 int gated_scan_varlen(const void* x, const void* g, const float* state, void* h, float* final_state, void* workspace, int64_t workspace_bytes,
-                      const int64_t* cu_seqlens, const int64_t* cu_chunks, int n_seq, int64_t total_tokens, int64_t total_chunks, int D,
-                      int64_t x_stride, int64_t g_stride, int64_t h_stride,
+                      const int64_t* cu_seqlens, int n_seq, int64_t total_tokens, int D, int64_t x_stride, int64_t g_stride, int64_t h_stride,
                       int dtype, int g_dtype, uint32_t flags, void* hip_stream);
 #define TRIINV_SCAN_LOGIT 0x1u
 #define TRIINV_SCAN_MIX 0x2u
-/* Bytes of workspace that these and their gradients need for sequences of total_tokens tokens in total_chunks chunks (B ceil(Tlen / TRIINV_SCAN_CHUNK)). */
-int gated_scan_workspace(int64_t total_tokens, int64_t total_chunks, int D, int64_t* bytes);
+/* Bytes of workspace that these and their gradients need for n_seq sequences of total_tokens tokens together. */
+int gated_scan_workspace(int64_t total_tokens, int n_seq, int D, int64_t* bytes);
 
 /*
  * gated_scan_bwd: its gradient, against the time, from the inputs, h as it was written and the gradients dh of h and dstate (or NULL) of final_state:
@@ -461,8 +459,7 @@ int gated_scan_bwd(const void* x, const void* g, const void* h, const float* sta
                    void* workspace, int64_t workspace_bytes, int B, int64_t Tlen, int D, int64_t x_stride, int64_t g_stride, int64_t h_stride, int64_t dh_stride,
                    int64_t dx_stride, int64_t dg_stride, int dtype, int g_dtype, uint32_t flags, void* hip_stream);
 int gated_scan_bwd_varlen(const void* x, const void* g, const void* h, const float* state, const void* dh, const float* dstate, void* dx, void* dg, float* dstate0,
-                          void* workspace, int64_t workspace_bytes, const int64_t* cu_seqlens, const int64_t* cu_chunks, int n_seq, int64_t total_tokens, int64_t total_chunks,
-                          int D, int64_t x_stride, int64_t g_stride, int64_t h_stride, int64_t dh_stride, int64_t dx_stride, int64_t dg_stride, int dtype, int g_dtype, uint32_t flags, void* hip_stream);
+                          void* workspace, int64_t workspace_bytes, const int64_t* cu_seqlens, int n_seq, int64_t total_tokens, int D, int64_t x_stride, int64_t g_stride, int64_t h_stride, int64_t dh_stride, int64_t dx_stride, int64_t dg_stride, int dtype, int g_dtype, uint32_t flags, void* hip_stream);
 
 /*
  * gated_scan_step: one token of the recurrence, the state updated in place: state[slot] <- a state[slot] + b, h = that in dtype.

@@ -108,10 +108,10 @@ def lib() -> ctypes.CDLL:
         L.qk_norm_rope_bwd.argtypes = [vp] * 13 + [i64] * 8 + [i32] * 5 + [u32, f32, vp]
         L.qk_norm_rope_bwd_workspace.argtypes = [i64, i32, i32, i32, vp]
         L.gated_scan.argtypes = [vp] * 6 + [i64, i32, i64, i32] + [i64] * 3 + [i32, i32, u32, vp]
-        L.gated_scan_varlen.argtypes = [vp] * 6 + [i64, vp, vp, i32, i64, i64, i32] + [i64] * 3 + [i32, i32, u32, vp]
-        L.gated_scan_workspace.argtypes = [i64, i64, i32, vp]
+        L.gated_scan_varlen.argtypes = [vp] * 6 + [i64, vp, i32, i64, i32] + [i64] * 3 + [i32, i32, u32, vp]
+        L.gated_scan_workspace.argtypes = [i64, i32, i32, vp]
         L.gated_scan_bwd.argtypes = [vp] * 10 + [i64, i32, i64, i32] + [i64] * 6 + [i32, i32, u32, vp]
-        L.gated_scan_bwd_varlen.argtypes = [vp] * 10 + [i64, vp, vp, i32, i64, i64, i32] + [i64] * 6 + [i32, i32, u32, vp]
+        L.gated_scan_bwd_varlen.argtypes = [vp] * 10 + [i64, vp, i32, i64, i32] + [i64] * 6 + [i32, i32, u32, vp]
         L.gated_scan_step.argtypes = [vp] * 5 + [i32, i64, i32] + [i64] * 3 + [i32, i32, u32, vp]
         for f in (L.gdn_chunk_attn, L.gdn_chunk_attn_varlen, L.gdn_chunk_attn_workspace, L.gdn_chunk_attn_bwd, L.gdn_chunk_attn_bwd_varlen,
                   L.gdn_chunk_attn_bwd_workspace, L.gdn_step, L.add_rms_norm, L.add_rms_norm_bwd, L.qk_norm_rope, L.qk_norm_rope_bwd, L.qk_norm_rope_bwd_workspace,

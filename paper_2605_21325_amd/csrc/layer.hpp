@@ -119,14 +119,13 @@ struct ScanCall {
     void *out, *dg;  // out: h, or the gradient of x
     float* last;     // the final state, or the gradient of the initial one
     char* workspace;
-    const int64_t *cu_seqlens, *cu_chunks;  // device, or null: n_seq sequences of Tlen tokens
-    int64_t Tlen, N, n_tile, x_stride, g_stride, h_stride, dh_stride, out_stride, dg_stride;  // n_tile: of all sequences, SCAN_TILE tokens each
+    const int64_t* cu_seqlens;  // device, or null: n_seq sequences of Tlen tokens
+    int64_t Tlen, N, x_stride, g_stride, h_stride, dh_stride, out_stride, dg_stride;
     int n_seq, D, dtype, g_dtype;
     bool logit, mix;
     hipStream_t stream;
 };
-constexpr int SCAN_TILE = TRIINV_SCAN_CHUNK;
-int64_t scan_workspace(int64_t N, int64_t n_tile, int D);
+int64_t scan_workspace(int64_t N, int n_seq, int D);
 int launch_scan(const ScanCall& a);
 int launch_scan_bwd(const ScanCall& a);
 

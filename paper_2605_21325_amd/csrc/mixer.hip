@@ -7,7 +7,7 @@ namespace {
 
 using namespace triinv;
 
-constexpr int64_t MOST_STRIDE = 1LL << 31;  // elements from token to token: offsets stay far below 2^63
+constexpr int64_t MOST_STRIDE = 1LL << 26;  // elements from token to token: eight tokens of fp32 stay below 2^31 bytes
 
 uint64_t size_of(int dtype) { return dtype == TRIINV_F32 ? 4 : 2; }
 bool strides_ok(std::initializer_list<int64_t> strides)
@@ -47,31 +47,28 @@ int scan_types(int dtype, int g_dtype, uint32_t flags)
     if (!any_dtype(dtype) || (g_dtype != dtype && g_dtype != TRIINV_F32)) return TRIINV_ERR_BAD_DTYPE;
     return flags & ~SCAN_FLAGS ? TRIINV_ERR_BAD_METHOD : TRIINV_OK;
 }
-int scan_shape(int64_t n_token, int64_t n_chunk, int64_t n_seq, int D)
+int scan_shape(int64_t n_token, int64_t n_seq, int D)
 {
     if (n_seq <= 0 || n_seq > 0x7fffffffLL || n_token < 0 || n_token > 0x7fffffffLL || D <= 0 || D > (1 << 20)) return TRIINV_ERR_BAD_SHAPE;
-    // (chunks of each sequence: as many as the tokens need, and one more a sequence at most)
-    if (n_chunk < 0 || n_chunk > n_token || n_chunk > n_token / SCAN_TILE + n_seq || n_chunk * SCAN_TILE < n_token) return TRIINV_ERR_BAD_SHAPE;
-    return TRIINV_OK;
+    return n_seq * ((D + 63) / 64) < (1LL << 31) ? TRIINV_OK : TRIINV_ERR_UNSUPPORTED;
 }
-int64_t chunks_of(int64_t B, int64_t Tlen) { return B * ((Tlen + SCAN_TILE - 1) / SCAN_TILE); }
 
 // Both directions: a.h is null in the forward one.
 int scan_common(ScanCall a, int64_t workspace_bytes, bool back)
 {
-    const int64_t need = scan_workspace(a.N, a.n_tile, a.D);
+    const int64_t need = scan_workspace(a.N, a.n_seq, a.D);
     if (a.N > 0 && (!a.g || !a.out || (!a.x && (!back || a.mix)) || (back && (!a.h || !a.dh || !a.dg)))) return TRIINV_ERR_NULL;
     if (need > 0 && !a.workspace) return TRIINV_ERR_NULL;
     if (workspace_bytes < need || !strides_ok({a.x_stride, a.g_stride, a.h_stride, a.dh_stride, a.out_stride, a.dg_stride})) return TRIINV_ERR_BAD_SHAPE;
     if (!apart(a.N, a.out_stride, a.D) || (back && !apart(a.N, a.dg_stride, a.D))) return TRIINV_ERR_BAD_SHAPE;
     const uint64_t e = size_of(a.dtype), eg = size_of(a.g_dtype), states = (uint64_t)a.n_seq * a.D * 4;
     if (!aligned(a.x, e) || !aligned(a.h, e) || !aligned(a.dh, e) || !aligned(a.out, e) || !aligned(a.g, eg) || !aligned(a.dg, eg) || !aligned(a.state, 4) || !aligned(a.dstate, 4) ||
-        !aligned(a.last, 4) || !aligned(a.workspace, 16) || !aligned(a.cu_seqlens, 8) || !aligned(a.cu_chunks, 8))
+        !aligned(a.last, 4) || !aligned(a.workspace, 16) || !aligned(a.cu_seqlens, 8))
         return TRIINV_ERR_ALIGN;
     const auto rows = [&](const void* p, int64_t stride, uint64_t size) { return Rows{p, a.N, a.D * size, stride * size}; };
     const bool upon = !back && a.state && a.state == a.last;  // the final state upon the initial one
     const Rows in[] = {rows(a.x, a.x_stride, e), rows(a.g, a.g_stride, eg), rows(a.h, a.h_stride, e), rows(a.dh, a.dh_stride, e), flat(upon ? nullptr : a.state, states), flat(a.dstate, states),
-                       flat(a.cu_seqlens, (uint64_t)(a.n_seq + 1) * 8), flat(a.cu_chunks, (uint64_t)(a.n_seq + 1) * 8)};
+                       flat(a.cu_seqlens, (uint64_t)(a.n_seq + 1) * 8)};
     const Rows out[] = {rows(a.out, a.out_stride, e), rows(a.dg, a.dg_stride, eg), flat(a.last, states), flat(need ? a.workspace : nullptr, (uint64_t)need)};
     if (aliased(in, out)) return TRIINV_ERR_ALIAS;
     return finish(back ? launch_scan_bwd(a) : launch_scan(a));
@@ -140,11 +137,11 @@ int qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const void* q, cons
                                                 static_cast<hipStream_t>(hip_stream)}));
 }
 
-int gated_scan_workspace(int64_t total_tokens, int64_t total_chunks, int D, int64_t* bytes)
+int gated_scan_workspace(int64_t total_tokens, int n_seq, int D, int64_t* bytes)
 {
     if (!bytes) return TRIINV_ERR_NULL;
-    if (const int rc = scan_shape(total_tokens, total_chunks, 0x7fffffff, D)) return rc;
-    *bytes = scan_workspace(total_tokens, total_chunks, D);
+    if (const int rc = scan_shape(total_tokens, n_seq, D)) return rc;
+    *bytes = scan_workspace(total_tokens, n_seq, D);
     return TRIINV_OK;
 }
 
@@ -153,19 +150,19 @@ int gated_scan(const void* x, const void* g, const float* state, void* h, float*
 {
     if (const int rc = scan_types(dtype, g_dtype, flags)) return rc;
     if (B <= 0 || Tlen < 0 || Tlen > 0x7fffffffLL) return TRIINV_ERR_BAD_SHAPE;
-    if (const int rc = scan_shape(B * Tlen, chunks_of(B, Tlen), B, D)) return rc;
-    return scan_common(ScanCall{x, g, state, nullptr, nullptr, nullptr, h, nullptr, final_state, static_cast<char*>(workspace), nullptr, nullptr, Tlen, B * Tlen, chunks_of(B, Tlen), x_stride, g_stride, 0, 0, h_stride, 0, B, D,
+    if (const int rc = scan_shape(B * Tlen, B, D)) return rc;
+    return scan_common(ScanCall{x, g, state, nullptr, nullptr, nullptr, h, nullptr, final_state, static_cast<char*>(workspace), nullptr, Tlen, B * Tlen, x_stride, g_stride, 0, 0, h_stride, 0, B, D,
                                 dtype, g_dtype, (flags & TRIINV_SCAN_LOGIT) != 0, (flags & TRIINV_SCAN_MIX) != 0, static_cast<hipStream_t>(hip_stream)},
                        workspace_bytes, false);
 }
 
-int gated_scan_varlen(const void* x, const void* g, const float* state, void* h, float* final_state, void* workspace, int64_t workspace_bytes, const int64_t* cu_seqlens,
-                      const int64_t* cu_chunks, int n_seq, int64_t total_tokens, int64_t total_chunks, int D, int64_t x_stride, int64_t g_stride, int64_t h_stride, int dtype, int g_dtype, uint32_t flags, void* hip_stream)
+int gated_scan_varlen(const void* x, const void* g, const float* state, void* h, float* final_state, void* workspace, int64_t workspace_bytes, const int64_t* cu_seqlens, int n_seq,
+                      int64_t total_tokens, int D, int64_t x_stride, int64_t g_stride, int64_t h_stride, int dtype, int g_dtype, uint32_t flags, void* hip_stream)
 {
     if (const int rc = scan_types(dtype, g_dtype, flags)) return rc;
-    if (const int rc = scan_shape(total_tokens, total_chunks, n_seq, D)) return rc;
-    if (!cu_seqlens || !cu_chunks) return TRIINV_ERR_NULL;
-    return scan_common(ScanCall{x, g, state, nullptr, nullptr, nullptr, h, nullptr, final_state, static_cast<char*>(workspace), cu_seqlens, cu_chunks, 0, total_tokens, total_chunks, x_stride, g_stride, 0, 0, h_stride, 0,
+    if (const int rc = scan_shape(total_tokens, n_seq, D)) return rc;
+    if (!cu_seqlens) return TRIINV_ERR_NULL;
+    return scan_common(ScanCall{x, g, state, nullptr, nullptr, nullptr, h, nullptr, final_state, static_cast<char*>(workspace), cu_seqlens, 0, total_tokens, x_stride, g_stride, 0, 0, h_stride, 0,
                                 n_seq, D, dtype, g_dtype, (flags & TRIINV_SCAN_LOGIT) != 0, (flags & TRIINV_SCAN_MIX) != 0, static_cast<hipStream_t>(hip_stream)},
                        workspace_bytes, false);
 }
@@ -176,20 +173,20 @@ int gated_scan_bwd(const void* x, const void* g, const void* h, const float* sta
 {
     if (const int rc = scan_types(dtype, g_dtype, flags)) return rc;
     if (B <= 0 || Tlen < 0 || Tlen > 0x7fffffffLL) return TRIINV_ERR_BAD_SHAPE;
-    if (const int rc = scan_shape(B * Tlen, chunks_of(B, Tlen), B, D)) return rc;
-    return scan_common(ScanCall{x, g, state, h, dh, dstate, dx, dg, dstate0, static_cast<char*>(workspace), nullptr, nullptr, Tlen, B * Tlen, chunks_of(B, Tlen), x_stride, g_stride, h_stride, dh_stride, dx_stride, dg_stride, B,
+    if (const int rc = scan_shape(B * Tlen, B, D)) return rc;
+    return scan_common(ScanCall{x, g, state, h, dh, dstate, dx, dg, dstate0, static_cast<char*>(workspace), nullptr, Tlen, B * Tlen, x_stride, g_stride, h_stride, dh_stride, dx_stride, dg_stride, B,
                                 D, dtype, g_dtype, (flags & TRIINV_SCAN_LOGIT) != 0, (flags & TRIINV_SCAN_MIX) != 0, static_cast<hipStream_t>(hip_stream)},
                        workspace_bytes, true);
 }
 
 int gated_scan_bwd_varlen(const void* x, const void* g, const void* h, const float* state, const void* dh, const float* dstate, void* dx, void* dg, float* dstate0, void* workspace,
-                          int64_t workspace_bytes, const int64_t* cu_seqlens, const int64_t* cu_chunks, int n_seq, int64_t total_tokens, int64_t total_chunks, int D, int64_t x_stride, int64_t g_stride, int64_t h_stride, int64_t dh_stride,
+                          int64_t workspace_bytes, const int64_t* cu_seqlens, int n_seq, int64_t total_tokens, int D, int64_t x_stride, int64_t g_stride, int64_t h_stride, int64_t dh_stride,
                           int64_t dx_stride, int64_t dg_stride, int dtype, int g_dtype, uint32_t flags, void* hip_stream)
 {
     if (const int rc = scan_types(dtype, g_dtype, flags)) return rc;
-    if (const int rc = scan_shape(total_tokens, total_chunks, n_seq, D)) return rc;
-    if (!cu_seqlens || !cu_chunks) return TRIINV_ERR_NULL;
-    return scan_common(ScanCall{x, g, state, h, dh, dstate, dx, dg, dstate0, static_cast<char*>(workspace), cu_seqlens, cu_chunks, 0, total_tokens, total_chunks, x_stride, g_stride, h_stride, dh_stride, dx_stride, dg_stride,
+    if (const int rc = scan_shape(total_tokens, n_seq, D)) return rc;
+    if (!cu_seqlens) return TRIINV_ERR_NULL;
+    return scan_common(ScanCall{x, g, state, h, dh, dstate, dx, dg, dstate0, static_cast<char*>(workspace), cu_seqlens, 0, total_tokens, x_stride, g_stride, h_stride, dh_stride, dx_stride, dg_stride,
                                 n_seq, D, dtype, g_dtype, (flags & TRIINV_SCAN_LOGIT) != 0, (flags & TRIINV_SCAN_MIX) != 0, static_cast<hipStream_t>(hip_stream)},
                        workspace_bytes, true);
 }

@@ -11,96 +11,63 @@ namespace triinv {
 
 namespace {
 
-// e^x, off by an ulp or so for every x: 2^y with the rounding of y = x log2(e) put right.
-__device__ __forceinline__ float exp_full(float x)
+// e^x, off by an ulp or two: 2^y with what the product y = x log2(e) lacks put right.  x in 16 bits: the factor is cut so that the product is exact.
+template <int T> __device__ __forceinline__ float exp_of(float x)
 {
-    constexpr float LOG2E = 1.44269502f, LOW = 1.925963e-8f, LN2 = 0.693147182f;  // log2(e) in two parts
-    const float y = x * LOG2E, rest = fmaf(x, LOG2E, -y) + x * LOW, e = __builtin_amdgcn_exp2f(y);
-    return fabsf(y) < 128.f ? fmaf(e, rest * LN2, e) : e;
+    if constexpr (T == OP_F32) {
+        constexpr float LOG2E = 1.44269502f, LOW = 1.925963e-8f, LN2 = 0.693147182f;  // log2(e) in two parts
+        const float y = x * LOG2E, rest = (fmaf(x, LOG2E, -y) + x * LOW) * LN2, e = __builtin_amdgcn_exp2f(y);
+        return fmaf(e, __builtin_amdgcn_fmed3f(rest, -1.f, 1.f), e);  // (where x is infinite the rest is none)
+    } else {
+        // 13 bits of it for the 11 of an fp16 number, 15 for the 8 of a bf16 number; what they leave of log2(e), times ln 2
+        constexpr float CUT = T == OP_F16 ? 0x1.715p0f : 0x1.7154p0f, LEFT = T == OP_F16 ? 4.7194842e-5f : 4.8884952e-6f;
+        const float e = __builtin_amdgcn_exp2f(x * CUT);
+        return fmaf(e, __builtin_amdgcn_fmed3f(x * LEFT, -1.f, 1.f), e);
+    }
 }
 // 1 - e^x.
 __device__ __forceinline__ float one_less_exp(float x, float e)
 {
-    if (fabsf(x) > 0.35f) return 1.f - e;
     float p = 1.f / 40320;  // x + x^2 / 2! + ... + x^8 / 8!
     p = fmaf(p, x, 1.f / 5040), p = fmaf(p, x, 1.f / 720), p = fmaf(p, x, 1.f / 120), p = fmaf(p, x, 1.f / 24), p = fmaf(p, x, 1.f / 6), p = fmaf(p, x, 0.5f), p = fmaf(p, x, 1.f);
-    return -p * x;
+    return fabsf(x) > 0.35f ? 1.f - e : -p * x;
 }
 
 struct Gate {
     float a, rest;  // the decay and one less it, where that is asked for
 };
-template <bool LOGIT, bool REST> __device__ __forceinline__ Gate gate(float g)
+template <int T, bool LOGIT, bool REST> __device__ __forceinline__ Gate gate(float g)
 {
     if constexpr (!LOGIT) {
-        const float a = exp_full(g);
+        const float a = exp_of<T>(g);
         return {a, REST ? one_less_exp(g, a) : 0.f};
-    } else {  // both of 1 / (1 + e) and e / (1 + e), e = e^-|g|, to their last bits
-        const float e = exp_full(-fabsf(g)), d = 1.f + e;
+    } else {  // 1 / (1 + e) and e / (1 + e), e = e^-|g|: both with all their bits
+        const float e = exp_of<T>(-fabsf(g)), d = 1.f + e;
         float r = __builtin_amdgcn_rcpf(d);
-        r = fmaf(fmaf(-d, r, 1.f), r, r);
+        if constexpr (T == OP_F32) r = fmaf(fmaf(-d, r, 1.f), r, r);
         const float s = e * r;
         return g >= 0.f ? Gate{r, s} : Gate{s, r};
     }
 }
 
-// Decays and what they bring over some tokens, C <- A C + H, put together.
-__device__ __forceinline__ float carry_through(float C, float A, float H) { return fmaf(A, C, H); }
-
-// What a tile tells the tiles behind it travels as one 64-bit word a channel, A above H, that is whole or not there yet: all ones, which no value becomes.
-constexpr uint64_t NOT_YET = ~0ull;
-__device__ __forceinline__ uint64_t word(float A, float H)
-{
-    const uint32_t h = H == H ? __builtin_bit_cast(uint32_t, H) : 0x7fc00000u;  // (a NaN of the inputs may be all ones)
-    return (uint64_t)__builtin_bit_cast(uint32_t, A) << 32 | h;
-}
-__device__ __forceinline__ float high(uint64_t w) { return __builtin_bit_cast(float, (uint32_t)(w >> 32)); }
-__device__ __forceinline__ float low(uint64_t w) { return __builtin_bit_cast(float, (uint32_t)w); }
-
-constexpr int TILE = SCAN_TILE, TOK = 8, WAVES = TILE / TOK;  // tokens of a tile, of a wavefront
-constexpr int EVERY = 16;          // of a sequence's tiles the last of so many publishes the state behind it
-constexpr int TOGETHER = 8;        // words a lane waits for at once
-constexpr int PATIENCE = 1 << 22;  // polls of about a microsecond; see k_scan
+// Tokens of a strip (lanes that take VEC channels each, 64 together), strips of a workgroup, one after the other in time.
+constexpr int CHANNELS = 64, TOK = 8, STRIPS = 16, TILE = TOK * STRIPS;
 
 struct ScanPlan {
-    int64_t n_tile;          // of all sequences
-    int groups;              // of channels
-    uint32_t* tickets;       // [groups], or null: every sequence fits a tile
-    uint64_t *part, *whole;  // [n_tile][D], [n_tile / EVERY + 1][D]
+    int n_seg, groups;  // segments of a sequence; groups of channels
+    v2f* part;          // [n_seq][n_seg][D]: a segment's decay and what it brings; in the last one's place the initial state as it was (n_seg > 1)
 };
 
-__global__ __launch_bounds__(256) void k_scan_clear(uint64_t* words, int64_t n, uint32_t* tickets, int groups)
-{
-    const int64_t i = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x;
-    if (2 * i + 1 < n)
-        reinterpret_cast<v4u*>(words)[i] = v4u{~0u, ~0u, ~0u, ~0u};
-    else if (2 * i < n)
-        words[2 * i] = NOT_YET;
-    if (i < groups) tickets[i] = 0u;
-}
-
-// A tile's sequence, its place among the sequence's tiles and the sequence's tokens t0 to t1 - 1.
-struct Place {
-    int s;
-    int64_t j, tiles, t0, t1;
+// Sequence s: its tokens t0 to t0 + len - 1.
+struct Sequence {
+    int64_t t0, len;
+    int tiles;
 };
-__device__ __forceinline__ Place place_of(const ScanCall& a, int64_t tile)
+__device__ __forceinline__ Sequence sequence(const ScanCall& a, int s)
 {
-    if (!a.cu_seqlens) {  // the first tiles of all sequences, the second ones, ...: a tile waits for one that was begun long before
-        const int64_t j = tile / a.n_seq;
-        const int s = (int)(tile - j * a.n_seq);
-        return {s, j, (a.Tlen + TILE - 1) / TILE, s * a.Tlen, (s + 1) * a.Tlen};
-    }
-    int lo = 0, n = a.n_seq;  // cu_chunks[lo] <= tile < cu_chunks[lo + n]; of several with the same first tile the last
-    while (n > 1) {
-        const int step = (n + 63) / 64, at = (threadIdx.x & 63) * step;
-        const int there = __popcll(__ballot(at < n && a.cu_chunks[lo + at] <= tile)), k = there > 0 ? there - 1 : 0;
-        lo += k * step, n = n - k * step < step ? n - k * step : step;
-    }
-    // (whatever the arrays hold, tokens and tiles stay among those there are)
-    const auto among = [](int64_t x, int64_t from, int64_t to) { return x < from ? from : x > to ? to : x; };
-    const int64_t c0 = among(a.cu_chunks[lo], 0, tile), t0 = among(a.cu_seqlens[lo], 0, a.N);
-    return {lo, tile - c0, a.cu_chunks[lo + 1] - c0, t0, among(a.cu_seqlens[lo + 1], t0, a.N)};
+    const auto among = [](int64_t x, int64_t from, int64_t to) { return x < from ? from : x > to ? to : x; };  // (whatever the array holds, tokens stay among those there are)
+    const int64_t t0 = a.cu_seqlens ? among(a.cu_seqlens[s], 0, a.N) : s * a.Tlen, len = a.cu_seqlens ? among(a.cu_seqlens[s + 1], t0, a.N) - t0 : a.Tlen;
+    return {t0, len, (int)((len + TILE - 1) / TILE)};
 }
 
 template <int VEC> __device__ __forceinline__ void load_state(const float* from, int64_t i, float (&x)[VEC])
@@ -109,195 +76,213 @@ template <int VEC> __device__ __forceinline__ void load_state(const float* from,
     for (int e = 0; e < VEC; ++e) x[e] = from ? from[i + e] : 0.f;
 }
 
-// One tile of a sequence: WAVES wavefronts of TOK tokens each, one after the other in time (the gradient's runs from the last token to the first), VEC channels a lane.
-//   1  a wavefront loads its tokens, all at once, and forms its decay and what it brings;
-//   2  the tile's own, from those, is published (the first one's with the initial state in it); the state before the tile is put together from the tiles before it:
-//      from the last that published the state behind it, EVERY tiles apart;
-//   3  the wavefronts go through their tokens, in registers still, from the states before them.
-// Tiles are given out by ticket, each sequence's in order of time for each group of channels: every tile that one waits for has been begun, and publishes its own
-// before it waits itself, so that the first tile not yet done never waits for one that is not running: every wait ends.  (A wait of seconds is given up, with NaN for a state.)
-// A channel's sums have an order that follows from its place in its sequence alone: the same bits alone, in a batch and packed, and of a prompt's beginning.
-template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC> __global__ __launch_bounds__(64 * WAVES) void k_scan(ScanCall a, ScanPlan p)
-{
-    constexpr int CH = 64 * VEC;
-    constexpr bool REST = MIX || (BACK && LOGIT);
-    __shared__ float own[WAVES][CH][2];
-    __shared__ float before_tile[CH];
-    __shared__ uint32_t ticket;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
-    if (block >= p.n_tile * p.groups) return;
-    const int group = (int)(block % p.groups);
-    int64_t turn = block / p.groups;
-    if (p.tickets) {
-        if (threadIdx.x == 0) ticket = atomicAdd(p.tickets + group, 1u);
-        __syncthreads();
-        turn = __builtin_amdgcn_readfirstlane((int)ticket);
+// Rows of a strip's tokens as they are in memory.
+template <int DT, int GT, bool MIX, bool BACK, int VEC, bool ONLY> struct Raw {
+    static constexpr bool X = BACK ? MIX && !ONLY : true, H = BACK && !ONLY;
+    Elems<DT, VEC> x[X ? TOK : 1], d[BACK ? TOK : 1], h[H ? TOK : 1];
+    Elems<GT, VEC> g[TOK];
+    // The tile's tokens are all there: rows one after the other from `row` on, a wavefront's first (the gradient's: last) one; a lane's offset in bytes.
+    template <int T> static __device__ __forceinline__ void at(Elems<T, VEC>& to, const void* p, int64_t row, int64_t stride, uint32_t lane)
+    {
+        to.load(static_cast<const char*>(p) + row * stride * Elems<T, VEC>::SIZE + lane, 0);
     }
-    const Place at = place_of(a, turn);
-    const int64_t tile = a.cu_seqlens ? turn : at.s * at.tiles + at.j;  // its words' place
-    const int c = group * CH + lane * VEC;
-    const bool in = c < a.D;
-    const int64_t i0 = at.j * TILE + wave * TOK, length = at.t1 - at.t0;  // the wavefront's first token in the sequence's order
-    const int n = (int)(length - i0 < TOK ? length - i0 : TOK);           // (may be negative)
-    const int64_t first = BACK ? at.t1 - 1 - i0 : at.t0 + i0;
-    constexpr int WAY = BACK ? -1 : 1;
-
-    Elems<DT, VEC> rx[TOK], rd[BACK ? TOK : 1], rh[BACK ? TOK : 1];
-    Elems<GT, VEC> rg[TOK];
+    __device__ __forceinline__ void load(const ScanCall& a, const Sequence& q, int64_t i0, int strip, int c)
+    {
+        if (i0 + TILE <= q.len) {
+            constexpr int PER_WAVE = 64 * VEC / CHANNELS;  // strips of a wavefront
+            const int64_t k0 = i0 + __builtin_amdgcn_readfirstlane(strip / PER_WAVE * PER_WAVE) * TOK;  // the wavefront's first token
+            const uint32_t row = (BACK ? PER_WAVE - 1 - strip % PER_WAVE : strip % PER_WAVE) * TOK;
+            const auto lane = [&](int64_t stride, int size) { return (row * (uint32_t)stride + (uint32_t)c) * size; };
+            const uint32_t lx = lane(a.x_stride, Elems<DT, 1>::SIZE), lg = lane(a.g_stride, Elems<GT, 1>::SIZE), ld = lane(a.dh_stride, Elems<DT, 1>::SIZE), lh = lane(a.h_stride, Elems<DT, 1>::SIZE);
 #pragma unroll
-    for (int i = 0; i < TOK; ++i) {
-        rx[i].clear(), rg[i].clear();
-        if constexpr (BACK) rd[i].clear(), rh[i].clear();
-        if (i >= n || !in) continue;
-        const int64_t t = first + WAY * i;
-        if constexpr (!BACK || MIX) rx[i].load(a.x, t * a.x_stride + c);
-        rg[i].load(a.g, t * a.g_stride + c);
-        if constexpr (BACK) {
-            rd[i].load(a.dh, t * a.dh_stride + c);
-            if (i0 + i + 1 < length) rh[i].load(a.h, (t - 1) * a.h_stride + c);
-        }
-    }
-    const float* const init = BACK ? a.dstate : a.state;
-    if (at.j == 0 && wave == 0 && in) {  // (read before anything is published: the final state may go to the same place)
-        float h[VEC];
-        load_state<VEC>(init, (int64_t)at.s * a.D + c, h);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) before_tile[lane * VEC + e] = h[e];
-    }
-
-    float da[TOK][VEC], db[TOK][VEC];  // decays; what a token brings (gradient: one less the decay)
-    float A[VEC], C[VEC];
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) A[e] = 1.f, C[e] = 0.f;
-#pragma unroll
-    for (int i = 0; i < TOK; ++i) {
-        if (i >= n) continue;
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            const Gate f = gate<LOGIT, REST>(rg[i][e]);
-            da[i][e] = f.a;
-            if constexpr (BACK) {
-                db[i][e] = f.rest;
-                C[e] = f.a * (rd[i][e] + C[e]);
-            } else {
-                db[i][e] = MIX ? f.rest * rx[i][e] : rx[i][e];
-                C[e] = fmaf(f.a, C[e], db[i][e]);
-            }
-            A[e] *= f.a;
-        }
-    }
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) own[wave][lane * VEC + e][0] = A[e], own[wave][lane * VEC + e][1] = C[e];
-    __syncthreads();
-
-    const bool others = p.tickets && at.tiles > 1;
-    if (others) {
-        if (wave == WAVES - 1 && in && at.j + 1 < at.tiles) {
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                A[e] = own[0][lane * VEC + e][0], C[e] = own[0][lane * VEC + e][1];
-                if (at.j == 0) C[e] = carry_through(before_tile[lane * VEC + e], A[e], C[e]);
-#pragma unroll
-                for (int w = 1; w < WAVES; ++w) A[e] *= own[w][lane * VEC + e][0], C[e] = carry_through(C[e], own[w][lane * VEC + e][0], own[w][lane * VEC + e][1]);
-                __hip_atomic_store(p.part + tile * a.D + c + e, word(A[e], C[e]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            }
-        }
-        if (wave == 0 && in && at.j > 0) {
-            const int64_t back = at.j < EVERY ? at.j : at.j % EVERY + 1;  // tiles to put together
-            const uint64_t* from = at.j < EVERY ? p.part + (tile - back) * a.D + c : p.whole + (tile - back) / EVERY * a.D + c;
-            const uint64_t* const rest = p.part + (tile - back) * a.D + c;
-            float h[VEC];
-            for (int64_t j = 0; j < back; j += TOGETHER) {
-                uint64_t v[TOGETHER][VEC];
-                for (int polls = 0;; ++polls) {
-                    bool there = true;
-#pragma unroll
-                    for (int i = 0; i < TOGETHER; ++i)
-#pragma unroll
-                        for (int e = 0; e < VEC; ++e) {
-                            v[i][e] = word(1.f, 0.f);
-                            if (j + i < back) v[i][e] = __hip_atomic_load((j + i ? rest + (j + i) * a.D : from) + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                            there = there && v[i][e] != NOT_YET;
-                        }
-                    if (__all(there) || polls == PATIENCE) break;
-                    __builtin_amdgcn_s_sleep(1);
+            for (int i = 0; i < TOK; ++i) {
+                const int64_t t = BACK ? q.t0 + q.len - 1 - (k0 + i) - (PER_WAVE - 1) * TOK : q.t0 + k0 + i;
+                if constexpr (X) at(x[i], a.x, t, a.x_stride, lx);
+                at(g[i], a.g, t, a.g_stride, lg);
+                if constexpr (BACK) at(d[i], a.dh, t, a.dh_stride, ld);
+                if constexpr (H) {
+                    // (before the first token of all there is no row: its own is read instead, and not used)
+                    const bool none = i0 + TILE == q.len && i == TOK - 1 && q.t0 == 0 && strip == STRIPS - 1;
+                    at(h[i], a.h, t - 1, a.h_stride, lh + (none ? (uint32_t)a.h_stride * Elems<DT, 1>::SIZE : 0u));
                 }
-#pragma unroll
-                for (int i = 0; i < TOGETHER; ++i)
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) h[e] = j + i ? carry_through(h[e], high(v[i][e]), low(v[i][e])) : low(v[i][e]);
             }
+        } else {  // rows that are not there are replaced by the sequence's last
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) before_tile[lane * VEC + e] = h[e];
-        }
-        __syncthreads();
-        if (wave == WAVES - 1 && in && at.j % EVERY == EVERY - 1 && at.j + 1 < at.tiles) {
-#pragma unroll
-            for (int e = 0; e < VEC; ++e)
-                __hip_atomic_store(p.whole + tile / EVERY * a.D + c + e, word(0.f, carry_through(before_tile[lane * VEC + e], A[e], C[e])), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            for (int i = 0; i < TOK; ++i) {
+                const int64_t k1 = i0 + strip * TOK + i, k = k1 < q.len ? k1 : q.len - 1, t = BACK ? q.t0 + q.len - 1 - k : q.t0 + k;
+                if constexpr (X) x[i].load(a.x, t * a.x_stride + c);
+                g[i].load(a.g, t * a.g_stride + c);
+                if constexpr (BACK) d[i].load(a.dh, t * a.dh_stride + c);
+                if constexpr (H) h[i].load(a.h, (t > q.t0 ? t - 1 : t) * a.h_stride + c);
+            }
         }
     }
-    if (!in) return;
-    const auto put_last = [&](int64_t s, const float (&x)[VEC]) {
+};
+
+// A workgroup takes 64 channels through a sequence, or through a segment of it, a tile of STRIPS times TOK tokens at a time (the gradient's runs from the last token to the first):
+//   1  a strip forms the decay of its tokens and what they bring, from registers, and asks for its tokens of the next tile;
+//   2  these go through LDS, and every strip puts together the state before its tokens from those before it;
+//   3  from there it goes through its tokens, in registers still; where the last one ends the next tile begins.
+// Where sequences and channels are too few for the card a sequence is cut into segments of whole tiles: a first launch (ONLY) writes what each segment but the last brings,
+// the second begins a segment with the state that those before it leave.
+template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC, bool ONLY> __global__ __launch_bounds__(STRIPS * CHANNELS / VEC) void k_scan(ScanCall a, ScanPlan p)
+{
+    constexpr bool REST = MIX || (BACK && LOGIT);
+    constexpr int LANES = CHANNELS / VEC, PER_WAVE = 64 / LANES;  // of a strip; strips of a wavefront
+    __shared__ float own[2][STRIPS][CHANNELS][2];  // of one tile and the next: one barrier a tile
+    __shared__ float base[2][CHANNELS];
+    const int strip = threadIdx.x / LANES, i_c = threadIdx.x % LANES * VEC;
+    const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    if (block >= (int64_t)a.n_seq * p.n_seg * p.groups) return;
+    const int unit = (int)(block / p.groups), group = (int)(block - (int64_t)unit * p.groups), s = unit / p.n_seg, seg = unit - s * p.n_seg;
+    const Sequence q = sequence(a, s);
+    const int per = (q.tiles + p.n_seg - 1) / p.n_seg, j0 = seg * per, j1 = j0 + per < q.tiles ? j0 + per : q.tiles;
+    const bool in = group * CHANNELS + i_c < a.D;
+    const int c = in ? group * CHANNELS + i_c : a.D - VEC;  // (lanes without a channel read another one's)
+    const int64_t at_state = (int64_t)s * a.D + c;
+    const float* const init = BACK ? a.dstate : a.state;
+    float C[VEC];
+    const auto initial = [&] {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) C[e] = p.part && !ONLY ? p.part[((int64_t)(s + 1) * p.n_seg - 1) * a.D + c + e][1] : init ? init[at_state + e] : 0.f;
+    };
+    const auto put_last = [&] {
         if (!a.last) return;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) a.last[s * a.D + c + e] = x[e];
+        for (int e = 0; e < VEC; ++e) a.last[at_state + e] = C[e];
     };
-    if (n > 0) {
+    if (ONLY && seg == 0 && strip == 0) {
+        initial();
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            if (in) p.part[((int64_t)(s + 1) * p.n_seg - 1) * a.D + c + e] = v2f{0.f, C[e]};
+    }
+    if (j0 >= j1 || (ONLY && j1 == q.tiles)) {  // nothing to do; a sequence without tokens keeps its state
+        if (!ONLY && seg == 0 && q.len == 0 && strip == 0 && in) initial(), put_last();
+        return;
+    }
+    Raw<DT, GT, MIX, BACK, VEC, ONLY> next;
+    next.load(a, q, (int64_t)j0 * TILE, strip, c);
+    v2f all[VEC];  // ONLY: of the segment so far
+    if (strip == 0) {  // (read before anything is written: the final state may go to the same place)
+        if (seg == 0) initial();
+        if (!ONLY && seg > 0) {
+            const v2f* const from = p.part + (int64_t)s * p.n_seg * a.D + c;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) C[e] = from[e][1];
+#pragma unroll 4
+            for (int k = 1; k < seg; ++k)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const v2f w = from[(int64_t)k * a.D + e];
+                    C[e] = fmaf(w[0], C[e], w[1]);
+                }
+        }
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-            C[e] = before_tile[lane * VEC + e];
-            for (int w = 0; w < wave; ++w) C[e] = carry_through(C[e], own[w][lane * VEC + e][0], own[w][lane * VEC + e][1]);
+            all[e] = v2f{1.f, ONLY && seg == 0 ? C[e] : 0.f};
+            base[j0 & 1][i_c + e] = C[e];
         }
     }
+    for (int j = j0; j < j1; ++j) {
+        auto now = next;
+        const int64_t i0 = (int64_t)j * TILE;
+        const bool full = i0 + TILE <= q.len;
+        const int64_t left = q.len - i0 - strip * TOK;
+        const int n = full || left > TOK ? TOK : (int)left;  // (may be negative)
+        float da[TOK][VEC], db[TOK][VEC];                    // decays; what a token brings (gradient: one less the decay)
+        float A[VEC], H[VEC];
 #pragma unroll
-    for (int i = 0; i < TOK; ++i) {
-        if (i >= n) continue;
-        const int64_t t = first + WAY * i;
-        if constexpr (BACK) {
-            float dx[VEC], dg[VEC], past[VEC];
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) past[e] = rh[i][e];
-            if (i0 + i + 1 == length) load_state<VEC>(a.state, (int64_t)at.s * a.D + c, past);
+        for (int e = 0; e < VEC; ++e) A[e] = 1.f, H[e] = 0.f;
+        const auto form = [&](int i) {
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
-                const float r = rd[i][e] + C[e];
-                dx[e] = MIX ? r * db[i][e] : r;
-                dg[e] = r * (MIX ? past[e] - rx[i][e] : past[e]) * (LOGIT ? da[i][e] * db[i][e] : da[i][e]);
-                C[e] = da[i][e] * r;
+                const Gate f = gate<GT, LOGIT, REST>(now.g[i][e]);
+                da[i][e] = f.a;
+                if constexpr (BACK) {
+                    db[i][e] = f.rest;
+                    H[e] = f.a * (now.d[i][e] + H[e]);
+                } else {
+                    db[i][e] = MIX ? f.rest * now.x[i][e] : now.x[i][e];
+                    H[e] = fmaf(f.a, H[e], db[i][e]);
+                }
+                A[e] *= f.a;
             }
-            store_rounded<DT, VEC>(a.out, t * a.out_stride + c, dx);
-            store_rounded<GT, VEC>(a.dg, t * a.dg_stride + c, dg);
+        };
+        if (full) {
+#pragma unroll
+            for (int i = 0; i < TOK; ++i) form(i);
         } else {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) C[e] = fmaf(da[i][e], C[e], db[i][e]);
-            store_rounded<DT, VEC>(a.out, t * a.out_stride + c, C);
+            for (int i = 0; i < TOK; ++i)
+                if (i < n) form(i);
         }
-        if (i0 + i + 1 == length) put_last(at.s, C);
-    }
-    // Sequences without tokens have no tile: the first tile of the next sequence sees to them, the last tile of all to those at the end.
-    if (a.cu_seqlens && wave == 0) {
-        const auto put_empty = [&](int64_t s) {
-            const bool empty = a.cu_seqlens[s] == a.cu_seqlens[s + 1];
-            if (empty) {
-                float h[VEC];
-                load_state<VEC>(init, s * a.D + c, h);
-                put_last(s, h);
+        if (j + 1 < j1) next.load(a, q, i0 + TILE, strip, c);
+        float (*const mine)[CHANNELS][2] = own[j & 1];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) mine[strip][i_c + e][0] = A[e], mine[strip][i_c + e][1] = H[e];
+        __syncthreads();
+        if constexpr (ONLY) {
+            if (strip == 0) {
+#pragma unroll
+                for (int w = 0; w < STRIPS; ++w)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) all[e] = v2f{all[e][0] * mine[w][i_c + e][0], fmaf(mine[w][i_c + e][0], all[e][1], mine[w][i_c + e][1])};
             }
-            return empty;
+            continue;
+        }
+        {
+            const int first = strip / PER_WAVE * PER_WAVE;  // the wavefront's first strip
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) C[e] = base[j & 1][i_c + e];
+            for (int w = 0; w < __builtin_amdgcn_readfirstlane(first); ++w)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) C[e] = fmaf(mine[w][i_c + e][0], C[e], mine[w][i_c + e][1]);
+            if (PER_WAVE > 1 && strip != first) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) C[e] = fmaf(mine[first][i_c + e][0], C[e], mine[first][i_c + e][1]);
+            }
+        }
+        const auto go = [&](int i, bool last) {
+            const int64_t k = i0 + strip * TOK + i, t = BACK ? q.t0 + q.len - 1 - k : q.t0 + k;
+            if constexpr (BACK) {
+                float dx[VEC], dg[VEC], past[VEC];
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) past[e] = now.h[i][e];
+                if (last) load_state<VEC>(a.state, at_state, past);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const float r = now.d[i][e] + C[e];
+                    dx[e] = MIX ? r * db[i][e] : r;
+                    dg[e] = r * (MIX ? past[e] - now.x[i][e] : past[e]) * (LOGIT ? da[i][e] * db[i][e] : da[i][e]);
+                    C[e] = da[i][e] * r;
+                }
+                if (in) store_rounded<DT, VEC>(a.out, t * a.out_stride + c, dx);
+                if (in) store_rounded<GT, VEC>(a.dg, t * a.dg_stride + c, dg);
+            } else {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) C[e] = fmaf(da[i][e], C[e], db[i][e]);
+                if (in) store_rounded<DT, VEC>(a.out, t * a.out_stride + c, C);
+            }
+            if (last && in) put_last();
         };
-        if (at.j == 0)
-            for (int64_t s = at.s - 1; s >= 0 && put_empty(s); --s) {}
-        if (at.j == 0 && turn + at.tiles == p.n_tile)
-            for (int64_t s = at.s + 1; s < a.n_seq && put_empty(s); ++s) {}
+        if (i0 + TILE < q.len) {
+#pragma unroll
+            for (int i = 0; i < TOK; ++i) go(i, false);
+        } else {
+#pragma unroll
+            for (int i = 0; i < TOK; ++i)
+                if (i < n) go(i, i0 + strip * TOK + i + 1 == q.len);
+        }
+        if (strip == STRIPS - 1) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) base[j + 1 & 1][i_c + e] = C[e];
+        }
     }
-}
-
-// Final states of sequences that have no tokens, all of them.
-__global__ __launch_bounds__(256) void k_scan_nothing(const float* init, float* last, int64_t n)
-{
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) last[i] = init ? init[i] : 0.f;
+    if (ONLY && strip == 0 && in) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) p.part[((int64_t)s * p.n_seg + seg) * a.D + c + e] = all[e];
+    }
 }
 
 // A lane a channel.
@@ -314,7 +299,7 @@ template <int DT, int GT, bool LOGIT, bool MIX> __global__ __launch_bounds__(THR
         Elems<DT, 1> x;
         Elems<GT, 1> g;
         x.load(a.x, b * a.x_stride + c), g.load(a.g, b * a.g_stride + c);
-        const Gate f = gate<LOGIT, MIX>(g[0]);
+        const Gate f = gate<GT, LOGIT, MIX>(g[0]);
         float* const h = a.state + slot * a.D + c;
         *h = o[0] = fmaf(f.a, *h, MIX ? f.rest * x[0] : x[0]);
     }
@@ -334,25 +319,27 @@ template <class F> int types(int dtype, int g_dtype, bool logit, bool mix, F f)
     return g_dtype == OP_F32 ? kinds<OP_BF16, OP_F32>(logit, mix, f) : kinds<OP_BF16, OP_BF16>(logit, mix, f);
 }
 
-// Whether a sequence may have several tiles.
-bool chained(int64_t N, int64_t Tlen, bool packed) { return (packed ? N : Tlen) > TILE; }
-int64_t words(int64_t n_tile, int D) { return (n_tile + n_tile / EVERY + 1) * D; }
-constexpr int64_t aligned16(int64_t n) { return (n + 15) / 16 * 16; }
+// Segments of a sequence, by the tokens and sequences of the call.
+constexpr int SCAN_UNITS = 1024;
+int segments(int64_t N, int n_seq, int D)
+{
+    const int64_t units = (int64_t)n_seq * ((D + CHANNELS - 1) / CHANNELS), tiles = (N / n_seq + TILE - 1) / TILE, n = SCAN_UNITS / units;
+    return (int)(n < 2 || tiles < 2 ? 1 : n < tiles ? n : tiles);
+}
 
 template <bool BACK> struct Scan {
     const ScanCall& a;
     template <int DT, int GT, bool LOGIT, bool MIX, int VEC> int with() const
     {
-        ScanPlan p{a.n_tile, (a.D + 64 * VEC - 1) / (64 * VEC), nullptr, nullptr, nullptr};
-        if (chained(a.N, a.Tlen, a.cu_seqlens != nullptr)) {
-            const int64_t n = words(a.n_tile, a.D);
-            p.part = reinterpret_cast<uint64_t*>(a.workspace), p.whole = p.part + p.n_tile * a.D;
-            p.tickets = reinterpret_cast<uint32_t*>(a.workspace + aligned16(8 * n));
-            const int64_t threads = (n + 1) / 2 > p.groups ? (n + 1) / 2 : p.groups;
-            const int rc = launch_kernel(false, k_scan_clear, long_grid((threads + 255) / 256), dim3(256), 0, a.stream, p.part, n, p.tickets, p.groups);
+        const int n_seg = segments(a.N, a.n_seq, a.D);
+        ScanPlan p{n_seg, (a.D + CHANNELS - 1) / CHANNELS, nullptr};
+        const dim3 grid = long_grid((int64_t)a.n_seq * n_seg * p.groups), block(STRIPS * CHANNELS / VEC);
+        if (n_seg > 1) {
+            p.part = reinterpret_cast<v2f*>(a.workspace);
+            const int rc = launch_kernel(false, k_scan<DT, GT, LOGIT, MIX, BACK, VEC, true>, grid, block, 0, a.stream, a, p);
             if (rc != LAUNCHED) return rc;
         }
-        return launch_kernel(false, k_scan<DT, GT, LOGIT, MIX, BACK, VEC>, long_grid(p.n_tile * p.groups), dim3(64 * WAVES), 0, a.stream, a, p);
+        return launch_kernel(false, k_scan<DT, GT, LOGIT, MIX, BACK, VEC, false>, grid, block, 0, a.stream, a, p);
     }
     template <int DT, int GT, bool LOGIT, bool MIX> int go() const
     {
@@ -364,12 +351,6 @@ template <bool BACK> struct Scan {
         return with<DT, GT, LOGIT, MIX, 1>();
     }
 };
-int nothing(const ScanCall& a, const float* init)
-{
-    if (!a.last) return LAUNCHED;
-    const int64_t n = (int64_t)a.n_seq * a.D, groups = (n + 255) / 256;
-    return launch_kernel(false, k_scan_nothing, dim3((unsigned)(groups < 4096 ? groups : 4096)), dim3(256), 0, a.stream, init, a.last, n);
-}
 struct Step {
     const ScanStepCall& a;
     template <int DT, int GT, bool LOGIT, bool MIX> int go() const
@@ -381,9 +362,13 @@ struct Step {
 
 }  // namespace
 
-int64_t scan_workspace(int64_t N, int64_t n_tile, int D) { return N > TILE ? aligned16(8 * words(n_tile, D)) + aligned16(4 * ((D + 63) / 64)) : 0; }
-int launch_scan(const ScanCall& a) { return a.N == 0 ? nothing(a, a.state) : types(a.dtype, a.g_dtype, a.logit, a.mix, Scan<false>{a}); }
-int launch_scan_bwd(const ScanCall& a) { return a.N == 0 ? nothing(a, a.dstate) : types(a.dtype, a.g_dtype, a.logit, a.mix, Scan<true>{a}); }
+int64_t scan_workspace(int64_t N, int n_seq, int D)
+{
+    const int n = segments(N, n_seq, D);
+    return n > 1 ? (int64_t)8 * n_seq * n * D : 0;
+}
+int launch_scan(const ScanCall& a) { return types(a.dtype, a.g_dtype, a.logit, a.mix, Scan<false>{a}); }
+int launch_scan_bwd(const ScanCall& a) { return types(a.dtype, a.g_dtype, a.logit, a.mix, Scan<true>{a}); }
 int launch_scan_step(const ScanStepCall& a) { return types(a.dtype, a.g_dtype, a.logit, a.mix, Step{a}); }
 
 }  // namespace triinv

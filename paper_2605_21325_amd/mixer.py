@@ -17,7 +17,7 @@ from .binding import OK, TriInvError, _chunk_offsets, _dev, _stream_ptr, dtype_c
 from .layer import _has, _on, _opt
 
 HEADS_UNIT, HEADS_INTERLEAVED, HEADS_POS64 = 1, 2, 4
-SCAN_LOGIT, SCAN_MIX, SCAN_CHUNK = 1, 2, 64
+SCAN_LOGIT, SCAN_MIX = 1, 2
 
 
 def _rows(t: Optional[torch.Tensor], name: str, inner: int, shape=None, dtype=None):
@@ -143,9 +143,9 @@ def _gate_type(g, x_dtype):
     return dtype_code(g.dtype)
 
 
-def _scan_workspace(where, N, n_chunk, D, device):
+def _scan_workspace(where, N, n_seq, D, device):
     n = ctypes.c_int64()
-    st = binding.lib().gated_scan_workspace(N, n_chunk, D, ctypes.byref(n))
+    st = binding.lib().gated_scan_workspace(N, n_seq, D, ctypes.byref(n))
     if st != OK:
         raise TriInvError(st, where)
     return (torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None), n.value
@@ -155,7 +155,7 @@ def _flags(logit, mix):
     return SCAN_LOGIT * bool(logit) | SCAN_MIX * bool(mix)
 
 
-def _scan(where, x, g, n_seq, N, n_chunk, where_args, state, logit, mix, h, final_state, stream):
+def _scan(where, x, g, n_seq, N, where_args, state, logit, mix, h, final_state, stream):
     D = x.shape[-1]
     _has(g, "g", x.shape, g.dtype)
     g_code = _gate_type(g, x.dtype)
@@ -165,7 +165,7 @@ def _scan(where, x, g, n_seq, N, n_chunk, where_args, state, logit, mix, h, fina
     with _on(stream, x.device):
         h = torch.empty(x.shape, dtype=x.dtype, device=x.device) if h is None else h
         final_state = torch.empty((n_seq, D), dtype=torch.float32, device=x.device) if final_state is None else final_state
-        ws, n = _scan_workspace(where, N, n_chunk, D, x.device)
+        ws, n = _scan_workspace(where, N, n_seq, D, x.device)
     ph, sh = _rows(h, "h", 1, x.shape, x.dtype)
     st = getattr(binding.lib(), where)(px, pg, _opt(state, "state"), ph, _dev(final_state, "final_state"), _opt(ws, "workspace"), n, *where_args, D, sx, sg, sh, dtype_code(x.dtype), g_code,
                                        _flags(logit, mix), _stream_ptr(stream))
@@ -182,7 +182,7 @@ def gated_scan(x: torch.Tensor, g: torch.Tensor, state: Optional[torch.Tensor] =
     if x.dim() != 3:
         raise ValueError(f"x must be [B, Tlen, D], not {list(x.shape)}")
     B, T = x.shape[:2]
-    return _scan("gated_scan", x, g, B, B * T, B * -(-T // SCAN_CHUNK), (B, T), state, logit, mix, h, final_state, stream)
+    return _scan("gated_scan", x, g, B, B * T, (B, T), state, logit, mix, h, final_state, stream)
 
 
 def gated_scan_varlen(x: torch.Tensor, g: torch.Tensor, seqlens, state: Optional[torch.Tensor] = None, logit: bool = False, mix: bool = False,
@@ -193,13 +193,13 @@ def gated_scan_varlen(x: torch.Tensor, g: torch.Tensor, seqlens, state: Optional
         raise ValueError(f"x must be [total, D], not {list(x.shape)}")
     total = x.shape[0]
     with _on(stream, x.device):
-        cu, cu_c, n_seq, n_chunk, keep = _chunk_offsets(x, seqlens if isinstance(seqlens, (list, tuple)) else list(seqlens), SCAN_CHUNK, stream)
-    r = _scan("gated_scan_varlen", x, g, n_seq, total, n_chunk, (cu, cu_c, n_seq, total, n_chunk), state, logit, mix, h, final_state, stream)
+        cu, _, n_seq, _, keep = _chunk_offsets(x, seqlens if isinstance(seqlens, (list, tuple)) else list(seqlens), 128, stream)
+    r = _scan("gated_scan_varlen", x, g, n_seq, total, (cu, n_seq, total), state, logit, mix, h, final_state, stream)
     r[0]._triinv_keepalive = r[1]._triinv_keepalive = keep  # the launch is asynchronous: the offsets live as long as a result
     return r
 
 
-def _scan_bwd(where, x, g, h, dh, n_seq, N, n_chunk, where_args, state, dstate, logit, mix, dx, dg, stream):
+def _scan_bwd(where, x, g, h, dh, n_seq, N, where_args, state, dstate, logit, mix, dx, dg, stream):
     D = h.shape[-1]
     if x is None and mix:
         raise ValueError("the gradient with mix needs x")
@@ -213,7 +213,7 @@ def _scan_bwd(where, x, g, h, dh, n_seq, N, n_chunk, where_args, state, dstate, 
         dx = torch.empty(h.shape, dtype=h.dtype, device=h.device) if dx is None else dx
         dg = torch.empty(h.shape, dtype=g.dtype, device=h.device) if dg is None else dg
         dstate0 = None if state is None else torch.empty_like(state)
-        ws, n = _scan_workspace(where, N, n_chunk, D, h.device)
+        ws, n = _scan_workspace(where, N, n_seq, D, h.device)
     (ox, sox), (og, sog) = _rows(dx, "dx", 1, h.shape, h.dtype), _rows(dg, "dg", 1, h.shape, g.dtype)
     st = getattr(binding.lib(), where)(px, pg, ph, _opt(state, "state"), pd, _opt(dstate, "dstate"), ox, og, _opt(dstate0, "dstate0"), _opt(ws, "workspace"), n, *where_args, D,
                                        sx, sg, sh, sd, sox, sog, dtype_code(h.dtype), g_code, _flags(logit, mix), _stream_ptr(stream))
@@ -230,7 +230,7 @@ def gated_scan_bwd(x: Optional[torch.Tensor], g: torch.Tensor, h: torch.Tensor, 
     if h.dim() != 3:
         raise ValueError(f"h must be [B, Tlen, D], not {list(h.shape)}")
     B, T = h.shape[:2]
-    return _scan_bwd("gated_scan_bwd", x, g, h, dh, B, B * T, B * -(-T // SCAN_CHUNK), (B, T), state, dstate, logit, mix, dx, dg, stream)
+    return _scan_bwd("gated_scan_bwd", x, g, h, dh, B, B * T, (B, T), state, dstate, logit, mix, dx, dg, stream)
 
 
 def gated_scan_bwd_varlen(x: Optional[torch.Tensor], g: torch.Tensor, h: torch.Tensor, dh: torch.Tensor, seqlens, state: Optional[torch.Tensor] = None,
@@ -242,8 +242,8 @@ def gated_scan_bwd_varlen(x: Optional[torch.Tensor], g: torch.Tensor, h: torch.T
         raise ValueError(f"h must be [total, D], not {list(h.shape)}")
     total = h.shape[0]
     with _on(stream, h.device):
-        cu, cu_c, n_seq, n_chunk, keep = _chunk_offsets(h, seqlens if isinstance(seqlens, (list, tuple)) else list(seqlens), SCAN_CHUNK, stream)
-    r = _scan_bwd("gated_scan_bwd_varlen", x, g, h, dh, n_seq, total, n_chunk, (cu, cu_c, n_seq, total, n_chunk), state, dstate, logit, mix, dx, dg, stream)
+        cu, _, n_seq, _, keep = _chunk_offsets(h, seqlens if isinstance(seqlens, (list, tuple)) else list(seqlens), 128, stream)
+    r = _scan_bwd("gated_scan_bwd_varlen", x, g, h, dh, n_seq, total, (cu, n_seq, total), state, dstate, logit, mix, dx, dg, stream)
     for t in r:
         if t is not None:
             t._triinv_keepalive = keep  # the launch is asynchronous: the offsets live as long as a result

@@ -57,7 +57,7 @@ SCAN = dict(x=address(0), g=address(1), state=address(2), h=address(3), final=ad
 
 
 @pytest.mark.parametrize("change,status", [
-    (dict(B=0), BAD_SHAPE), (dict(T=-1), BAD_SHAPE), (dict(T=1 << 31), BAD_SHAPE), (dict(B=1 << 20, T=1 << 12), BAD_SHAPE), (dict(D=0), BAD_SHAPE), (dict(D=(1 << 20) + 1), BAD_SHAPE),
+    (dict(B=0), BAD_SHAPE), (dict(T=-1), BAD_SHAPE), (dict(T=1 << 31), BAD_SHAPE), (dict(B=1 << 20, T=1 << 12), BAD_SHAPE), (dict(B=1 << 30, T=0, D=128), UNSUPPORTED), (dict(D=0), BAD_SHAPE), (dict(D=(1 << 20) + 1), BAD_SHAPE),
     (dict(dtype=4), BAD_DTYPE), (dict(gtype=tri.F16), BAD_DTYPE), (dict(dtype=tri.F32, gtype=tri.BF16), BAD_DTYPE), (dict(flags=4), BAD_METHOD), (dict(xs=-1), BAD_SHAPE),
     (dict(hs=99), BAD_SHAPE), (dict(gs=1 << 40), BAD_SHAPE), (dict(x=None), NULL), (dict(g=None), NULL), (dict(h=None), NULL), (dict(x=address(0) + 1), ALIGN), (dict(g=address(1) + 2), ALIGN),
     (dict(state=address(2) + 2), ALIGN), (dict(ws=address(5) + 8), ALIGN), (dict(h=address(0)), ALIAS), (dict(h=address(1) + 8), ALIAS), (dict(final=address(0)), ALIAS), (dict(final=address(2) + 4), ALIAS),
@@ -67,10 +67,9 @@ def test_scan(L, change, status):
 
 
 def test_scan_packed(L):
-    a = dict(x=address(0), g=address(1), state=address(2), h=address(3), final=address(4), ws=address(5), ws_bytes=1 << 40, cu=address(6), cc=address(7), n=3, total=100, chunks=4, D=64, xs=64, gs=64, hs=64, dtype=tri.F16,
+    a = dict(x=address(0), g=address(1), state=address(2), h=address(3), final=address(4), ws=address(5), ws_bytes=1 << 40, cu=address(6), n=3, total=100, D=64, xs=64, gs=64, hs=64, dtype=tri.F16,
              gtype=tri.F16, flags=3, stream=None)
-    for change, status in [(dict(cu=None), NULL), (dict(cu=address(6) + 4), ALIGN), (dict(cu=address(3)), ALIAS), (dict(cc=None), NULL), (dict(cc=address(4)), ALIAS), (dict(cc=address(7) + 2), ALIGN),
-                           (dict(n=0), BAD_SHAPE), (dict(total=-1), BAD_SHAPE), (dict(total=1 << 31), BAD_SHAPE), (dict(chunks=1), BAD_SHAPE), (dict(chunks=5), BAD_SHAPE), (dict(chunks=-1), BAD_SHAPE)]:
+    for change, status in [(dict(cu=None), NULL), (dict(cu=address(6) + 4), ALIGN), (dict(cu=address(3)), ALIAS), (dict(n=0), BAD_SHAPE), (dict(total=-1), BAD_SHAPE), (dict(total=1 << 31), BAD_SHAPE)]:
         assert L.gated_scan_varlen(*dict(a, **change).values()) == status
 
 
