@@ -51,23 +51,24 @@ template <int T, bool LOGIT, bool REST> __device__ __forceinline__ Gate gate(flo
 }
 
 // Tokens of a strip (lanes that take VEC channels each, 64 together), strips of a workgroup, one after the other in time.
-constexpr int CHANNELS = 64, TOK = 8, STRIPS = 16, TILE = TOK * STRIPS;
+constexpr int CHANNELS = 64, STRIPS = 16;
+template <int DT, int GT, bool BACK> constexpr int TOKENS = !BACK && DT != OP_F32 && GT != OP_F32 ? 16 : 8;
 
 struct ScanPlan {
     int n_seg, groups;  // segments of a sequence; groups of channels
+    bool neighbours;    // on one XCD
     v2f* part;          // [n_seq][n_seg][D]: a segment's decay and what it brings; in the last one's place the initial state as it was (n_seg > 1)
 };
 
 // Sequence s: its tokens t0 to t0 + len - 1.
 struct Sequence {
     int64_t t0, len;
-    int tiles;
 };
 __device__ __forceinline__ Sequence sequence(const ScanCall& a, int s)
 {
     const auto among = [](int64_t x, int64_t from, int64_t to) { return x < from ? from : x > to ? to : x; };  // (whatever the array holds, tokens stay among those there are)
     const int64_t t0 = a.cu_seqlens ? among(a.cu_seqlens[s], 0, a.N) : s * a.Tlen, len = a.cu_seqlens ? among(a.cu_seqlens[s + 1], t0, a.N) - t0 : a.Tlen;
-    return {t0, len, (int)((len + TILE - 1) / TILE)};
+    return {t0, len};
 }
 
 template <int VEC> __device__ __forceinline__ void load_state(const float* from, int64_t i, float (&x)[VEC])
@@ -78,6 +79,7 @@ template <int VEC> __device__ __forceinline__ void load_state(const float* from,
 
 // Rows of a strip's tokens as they are in memory.
 template <int DT, int GT, bool MIX, bool BACK, int VEC, bool ONLY> struct Raw {
+    static constexpr int TOK = TOKENS<DT, GT, BACK>, TILE = TOK * STRIPS;
     static constexpr bool X = BACK ? MIX && !ONLY : true, H = BACK && !ONLY;
     Elems<DT, VEC> x[X ? TOK : 1], d[BACK ? TOK : 1], h[H ? TOK : 1];
     Elems<GT, VEC> g[TOK];
@@ -128,15 +130,21 @@ template <int DT, int GT, bool MIX, bool BACK, int VEC, bool ONLY> struct Raw {
 template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC, bool ONLY> __global__ __launch_bounds__(STRIPS * CHANNELS / VEC) void k_scan(ScanCall a, ScanPlan p)
 {
     constexpr bool REST = MIX || (BACK && LOGIT);
+    constexpr int TOK = TOKENS<DT, GT, BACK>, TILE = TOK * STRIPS;
     constexpr int LANES = CHANNELS / VEC, PER_WAVE = 64 / LANES;  // of a strip; strips of a wavefront
     __shared__ float own[2][STRIPS][CHANNELS][2];  // of one tile and the next: one barrier a tile
     __shared__ float base[2][CHANNELS];
     const int strip = threadIdx.x / LANES, i_c = threadIdx.x % LANES * VEC;
-    const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
-    if (block >= (int64_t)a.n_seq * p.n_seg * p.groups) return;
+    int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    const int64_t blocks = (int64_t)a.n_seq * p.n_seg * p.groups;
+    if (block >= blocks) return;
+    if (p.neighbours) {  // workgroups go to the eight XCDs in turn
+        const int64_t x = block & 7, most = blocks & 7;
+        block = x * (blocks >> 3) + (x < most ? x : most) + (block >> 3);
+    }
     const int unit = (int)(block / p.groups), group = (int)(block - (int64_t)unit * p.groups), s = unit / p.n_seg, seg = unit - s * p.n_seg;
     const Sequence q = sequence(a, s);
-    const int per = (q.tiles + p.n_seg - 1) / p.n_seg, j0 = seg * per, j1 = j0 + per < q.tiles ? j0 + per : q.tiles;
+    const int tiles = (int)((q.len + TILE - 1) / TILE), per = (tiles + p.n_seg - 1) / p.n_seg, j0 = seg * per, j1 = j0 + per < tiles ? j0 + per : tiles;
     const bool in = group * CHANNELS + i_c < a.D;
     const int c = in ? group * CHANNELS + i_c : a.D - VEC;  // (lanes without a channel read another one's)
     const int64_t at_state = (int64_t)s * a.D + c;
@@ -157,7 +165,7 @@ template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC, bool ONLY> _
         for (int e = 0; e < VEC; ++e)
             if (in) p.part[((int64_t)(s + 1) * p.n_seg - 1) * a.D + c + e] = v2f{0.f, C[e]};
     }
-    if (j0 >= j1 || (ONLY && j1 == q.tiles)) {  // nothing to do; a sequence without tokens keeps its state
+    if (j0 >= j1 || (ONLY && j1 == tiles)) {  // nothing to do; a sequence without tokens keeps its state
         if (!ONLY && seg == 0 && q.len == 0 && strip == 0 && in) initial(), put_last();
         return;
     }
@@ -319,20 +327,35 @@ template <class F> int types(int dtype, int g_dtype, bool logit, bool mix, F f)
     return g_dtype == OP_F32 ? kinds<OP_BF16, OP_F32>(logit, mix, f) : kinds<OP_BF16, OP_BF16>(logit, mix, f);
 }
 
-// Segments of a sequence, by the tokens and sequences of the call.
-constexpr int SCAN_UNITS = 1024;
-int segments(int64_t N, int n_seq, int D)
+// Segments of a sequence, by the tokens, sequences and channels of the call: so many that one to four rounds of the 256 compute units are full, whichever costs least with
+// the first launch's reading, AGAIN of the whole's, counted for all segments but one.  In us, one segment / about 256 / 512 / 1024 workgroups (bf16, logits and
+// mix, 4096 tokens of 2048 channels): 1 sequence (32 workgroups) - / 24 / 22 / 24, 3 (96) 91 / 78 / 69 / 60, 4 (128) - / 81 / 80 / -, 5 94 / 94 / 100 / 101, 6 97 / 97 / 131 /
+// 118; gradient 1 164 / 38 / 41 / 43, 3 170 / 121 / 109 / 103, 4 302 / 124 / 126 / 131, 5 177 / 178 / 166 / 180, 6 180 / 180 / 219 / 212.  Sequences of fewer than four
+// tiles are walked through as they are: 512 tokens 11.7 in one, 13.5 in two, 1024 20 and 14.
+int segments(int64_t N, int n_seq, int D, int tile, bool back)
 {
-    const int64_t units = (int64_t)n_seq * ((D + CHANNELS - 1) / CHANNELS), tiles = (N / n_seq + TILE - 1) / TILE, n = SCAN_UNITS / units;
-    return (int)(n < 2 || tiles < 2 ? 1 : n < tiles ? n : tiles);
+    const double AGAIN = back ? 0.45 : 0.67;
+    const int64_t units = (int64_t)n_seq * ((D + CHANNELS - 1) / CHANNELS), tiles = (N / n_seq + tile - 1) / tile;
+    if (units >= 256 || tiles < 4) return 1;
+    int64_t best = 1;
+    double least = 1;
+    for (int rounds = 1; rounds <= 4; ++rounds) {
+        const int64_t n = 256 * rounds / units < tiles ? 256 * rounds / units : tiles;
+        const double cost = (double)rounds / n * (1 + AGAIN * (n - 1) / n);
+        if (cost < least) best = n, least = cost;
+    }
+    return (int)best;
 }
 
 template <bool BACK> struct Scan {
     const ScanCall& a;
     template <int DT, int GT, bool LOGIT, bool MIX, int VEC> int with() const
     {
-        const int n_seg = segments(a.N, a.n_seq, a.D);
-        ScanPlan p{n_seg, (a.D + CHANNELS - 1) / CHANNELS, nullptr};
+        const int n_seg = segments(a.N, a.n_seq, a.D, TOKENS<DT, GT, BACK> * STRIPS, BACK);
+        // Neighbouring groups of channels share cache lines where rows do not begin on one: these are put on one XCD.  48 packed sequences of 1100 tokens of 1000 channels,
+        // fp16, 138 us as they come, 114 so; 16 of 2048 tokens of 4096 channels, where there is nothing to share, 194 and 223.
+        const bool share = (a.x_stride * Elems<DT, 1>::SIZE | a.g_stride * Elems<GT, 1>::SIZE | a.out_stride * Elems<DT, 1>::SIZE) % 128 != 0;
+        ScanPlan p{n_seg, (a.D + CHANNELS - 1) / CHANNELS, share, nullptr};
         const dim3 grid = long_grid((int64_t)a.n_seq * n_seg * p.groups), block(STRIPS * CHANNELS / VEC);
         if (n_seg > 1) {
             p.part = reinterpret_cast<v2f*>(a.workspace);
@@ -364,8 +387,11 @@ struct Step {
 
 int64_t scan_workspace(int64_t N, int n_seq, int D)
 {
-    const int n = segments(N, n_seq, D);
-    return n > 1 ? (int64_t)8 * n_seq * n * D : 0;
+    int most = 1;  // (of either direction and every type)
+    for (const int n : {segments(N, n_seq, D, TOKENS<OP_BF16, OP_BF16, false> * STRIPS, false), segments(N, n_seq, D, TOKENS<OP_F32, OP_F32, false> * STRIPS, false),
+                        segments(N, n_seq, D, TOKENS<OP_F32, OP_F32, true> * STRIPS, true)})
+        most = n > most ? n : most;
+    return most > 1 ? (int64_t)8 * n_seq * most * D : 0;
 }
 int launch_scan(const ScanCall& a) { return types(a.dtype, a.g_dtype, a.logit, a.mix, Scan<false>{a}); }
 int launch_scan_bwd(const ScanCall& a) { return types(a.dtype, a.g_dtype, a.logit, a.mix, Scan<true>{a}); }
