@@ -16,20 +16,33 @@ namespace {
 constexpr int WAVES = 4;  // of a workgroup
 constexpr int MOST_PAIRS = 256;
 
-__device__ __forceinline__ float lanes_sum(float x, int from, int to)
+// A neighbour's value, within a row of sixteen lanes.
+template <int CTRL> __device__ __forceinline__ float from_lane(float x)
 {
-    for (int d = from; d < to; d *= 2) x += __shfl_xor(x, d);
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+// The sum over G neighbouring lanes, in all of them; the same order in each.
+template <int G> __device__ __forceinline__ float lanes_sum(float x)
+{
+    if constexpr (G > 1) x += from_lane<0xb1>(x);   // lane ^ 1
+    if constexpr (G > 2) x += from_lane<0x4e>(x);   // lane ^ 2
+    if constexpr (G > 4) x += from_lane<0x141>(x);  // 7 - lane of eight
+    if constexpr (G > 8) x += from_lane<0x140>(x);  // 15 - lane of sixteen
+    if constexpr (G > 16) x += __shfl_xor(x, 16);
+    if constexpr (G > 32) x += __shfl_xor(x, 32);
     return x;
 }
 
 struct Angles {
     float c[WAVES][MOST_PAIRS], s[WAVES][MOST_PAIRS];
 };
+struct NoAngles {};
 
 // cos and sin of a token's angles, a lane each, for the wavefront that asks.
 __device__ __forceinline__ void turn_angles(Angles& at, int wave, const void* positions, bool pos64, const float* inv_freq, int pairs, int64_t n)
 {
 #pragma clang fp contract(off)  // (what a product loses is taken apart: no product may be fused into the difference)
+    __builtin_amdgcn_wave_barrier();
     const double p = pos64 ? (double)static_cast<const int64_t*>(positions)[n] : (double)static_cast<const int32_t*>(positions)[n];
     for (int i = threadIdx.x & 63; i < pairs; i += 64) {
         constexpr double TURN = 0.15915494309189535, LOW = -9.839338337591243e-18;  // 1 / (2 pi) in two parts
@@ -43,142 +56,269 @@ __device__ __forceinline__ void turn_angles(Angles& at, int wave, const void* po
     __builtin_amdgcn_wave_barrier();
 }
 
-// Elements of a pair: rotated ones first, then those that stay, two and two.
-struct Pair {
-    int i, j;  // j < 0: none
-    bool turned;
+// A head lies in pieces of VEC elements, two to a slot, SLOTS slots a lane of the G that share it.  HALVES: what is rotated first, a piece and the one rot / 2 elements behind it
+// (or, of single elements, its neighbour); then the rest, in two halves.  NEIGHBOURS: pairs lie inside a piece.
+enum : int { STILL = 0, HALVES = 1, NEIGHBOURS = 2 };
+struct Slot {
+    int i[2];     // first elements of its pieces
+    bool there[2];
+    bool turned;  // (HALVES)
 };
-__device__ __forceinline__ Pair pair_of(int s, int d, int rot, bool interleaved)
+template <int VEC, int ROT> __device__ __forceinline__ Slot slot_of(int s, int d, int rot, bool interleaved)
 {
-    const int r = rot / 2;
-    if (s < r) return interleaved ? Pair{2 * s, 2 * s + 1, true} : Pair{s, s + r, true};
-    const int i = rot + 2 * (s - r);
-    return {i, i + 1 < d ? i + 1 : -1, false};
-}
-
-// A wavefront a head.
-template <int DT, int SLOTS> __global__ __launch_bounds__(64 * WAVES) void k_heads(HeadsCall a)
-{
-    __shared__ Angles angles;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, heads = a.H + a.H_k, pairs = (a.d + 1) / 2;
-    const int64_t unit = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * WAVES + wave;
-    const int64_t n = unit / heads;
-    const int head = (int)(unit - n * heads);
-    if (n >= a.N) return;
-    const bool key = head >= a.H;
-    const int64_t from = key ? n * a.k_stride + (int64_t)(head - a.H) * a.d : n * a.q_stride + (int64_t)head * a.d;
-    const int64_t to = key ? n * a.k_out_stride + (int64_t)(head - a.H) * a.d : n * a.q_out_stride + (int64_t)head * a.d;
-    const void *const x = key ? a.k : a.q, *const weight = key ? a.k_weight : a.q_weight;
-    void* const y = key ? a.k_out : a.q_out;
-    float u[SLOTS], v[SLOTS], sq = 0.f;
-#pragma unroll
-    for (int i = 0; i < SLOTS; ++i) {
-        const int s = lane + 64 * i;
-        u[i] = v[i] = 0.f;
-        if (s >= pairs) continue;
-        const Pair p = pair_of(s, a.d, a.rot, a.interleaved);
-        Elems<DT, 1> e;
-        e.load(x, from + p.i), u[i] = e[0];
-        if (p.j >= 0) e.load(x, from + p.j), v[i] = e[0];
-        sq += u[i] * u[i] + v[i] * v[i];
+    const int pieces = d / VEC, first = ROT == HALVES ? rot / 2 / VEC : 0;  // turned slots
+    if (ROT == HALVES && s < first) {
+        if (VEC == 1 && interleaved) return {{2 * s, 2 * s + 1}, {true, true}, true};
+        return {{s * VEC, s * VEC + rot / 2}, {true, true}, true};
     }
-    if (a.rot) turn_angles(angles, wave, a.positions, a.pos64, a.inv_freq, a.rot / 2, n);
-    sq = lanes_sum(sq, 1, 64);
-    const float norm = 1.f / sqrtf((a.unit ? sq : sq / (float)a.d) + a.eps);
-#pragma unroll
-    for (int i = 0; i < SLOTS; ++i) {
-        const int s = lane + 64 * i;
-        if (s >= pairs) continue;
-        const Pair p = pair_of(s, a.d, a.rot, a.interleaved);
-        float b[1] = {u[i] * norm}, c[1] = {v[i] * norm};
-        if (weight) {
-            Elems<DT, 1> w;
-            w.load(weight, p.i), b[0] *= w[0];
-            if (p.j >= 0) w.load(weight, p.j), c[0] *= w[0];
-        }
-        if (p.turned) {
-            const float co = angles.c[wave][s], si = angles.s[wave][s], t = b[0];
-            b[0] = t * co - c[0] * si, c[0] = c[0] * co + t * si;
-        }
-        store_rounded<DT, 1>(y, to + p.i, b);
-        if (p.j >= 0) store_rounded<DT, 1>(y, to + p.j, c);
-    }
+    const int rest = pieces - 2 * first, half = (rest + 1) / 2, r = s - first, i = 2 * first + r;
+    return {{i * VEC, (i + half) * VEC}, {r < half, r < half && r + half < rest}, false};
 }
-
-// The gradient: a wavefront takes tokens in turn, all heads of each, and keeps its sums of the weights' gradients; those of a workgroup are written out and
-// added up by k_heads_dweight, always in the same order.
-template <int DT, int SLOTS> __global__ __launch_bounds__(64 * WAVES) void k_heads_bwd(HeadsBwdCall a)
-{
-    __shared__ Angles angles;
-    __shared__ float sums[WAVES][2 * 2 * MOST_PAIRS];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, heads = a.H + a.H_k, pairs = (a.d + 1) / 2;
-    float dw[2][SLOTS][2] = {};
-    for (int64_t n = (int64_t)blockIdx.x * WAVES + wave; n < a.N; n += (int64_t)gridDim.x * WAVES) {
-        if (a.rot) turn_angles(angles, wave, a.positions, a.pos64, a.inv_freq, a.rot / 2, n);
-        for (int head = 0; head < heads; ++head) {
-            const bool key = head >= a.H;
-            const int64_t h = (int64_t)(key ? head - a.H : head) * a.d;
-            const int64_t at = n * (key ? a.k_stride : a.q_stride) + h, up = n * (key ? a.dk_out_stride : a.dq_out_stride) + h, to = n * (key ? a.dk_stride : a.dq_stride) + h;
-            const void *const x = key ? a.k : a.q, *const dy = key ? a.dk_out : a.dq_out, *const weight = key ? a.k_weight : a.q_weight;
-            float u[SLOTS][2], e[SLOTS][2], f[SLOTS][2], sq = 0.f, dot = 0.f;
+// cos and sin for the pairs of a slot.
+template <int VEC, int ROT> struct Turn {
+    float c[ROT == STILL ? 1 : VEC], s[ROT == STILL ? 1 : VEC];
+    __device__ __forceinline__ void load(const Angles& at, int wave, const Slot& p, int rot, int slot)
+    {
 #pragma unroll
-            for (int i = 0; i < SLOTS; ++i) {
-                const int s = lane + 64 * i;
-                u[i][0] = u[i][1] = e[i][0] = e[i][1] = f[i][0] = f[i][1] = 0.f;
-                if (s >= pairs) continue;
-                const Pair p = pair_of(s, a.d, a.rot, a.interleaved);
-                Elems<DT, 1> r;
-                r.load(x, at + p.i), u[i][0] = r[0];
-                r.load(dy, up + p.i), e[i][0] = r[0];
-                if (p.j >= 0) r.load(x, at + p.j), u[i][1] = r[0];
-                if (p.j >= 0) r.load(dy, up + p.j), e[i][1] = r[0];
-                if (p.turned) {
-                    const float co = angles.c[wave][s], si = angles.s[wave][s], t = e[i][0];
-                    e[i][0] = t * co + e[i][1] * si, e[i][1] = e[i][1] * co - t * si;
-                }
-                f[i][0] = e[i][0], f[i][1] = e[i][1];
-                if (weight) {
-                    r.load(weight, p.i), f[i][0] *= r[0];
-                    if (p.j >= 0) r.load(weight, p.j), f[i][1] *= r[0];
-                }
-                sq += u[i][0] * u[i][0] + u[i][1] * u[i][1];
-                dot += f[i][0] * u[i][0] + f[i][1] * u[i][1];
+        for (int e = 0; e < VEC; ++e) {
+            if constexpr (ROT == HALVES) {
+                c[e] = p.turned ? at.c[wave][slot * VEC + e] : 1.f, s[e] = p.turned ? at.s[wave][slot * VEC + e] : 0.f;
+            } else if constexpr (ROT == NEIGHBOURS) {
+                const int i = p.i[e / (VEC / 2)] / 2 + e % (VEC / 2);
+                const bool on = p.there[e / (VEC / 2)] && 2 * i < rot;
+                c[e] = on ? at.c[wave][i] : 1.f, s[e] = on ? at.s[wave][i] : 0.f;
             }
-            sq = lanes_sum(sq, 1, 64), dot = lanes_sum(dot, 1, 64);
-            const float norm = 1.f / sqrtf((a.unit ? sq : sq / (float)a.d) + a.eps), m = (a.unit ? dot : dot / (float)a.d) * norm * norm;
+        }
+    }
+    // The slot's elements turned; WAY = -1: back.  What is not turned stays as it is (an infinity beside it too).
+    template <int WAY> __device__ __forceinline__ void turn(float (&x)[2][VEC]) const
+    {
 #pragma unroll
-            for (int i = 0; i < SLOTS; ++i) {
-                const int s = lane + 64 * i;
-                if (s >= pairs) continue;
-                const Pair p = pair_of(s, a.d, a.rot, a.interleaved);
+        for (int e = 0; e < VEC; ++e) {
+            if constexpr (ROT == STILL) continue;
+            float& a = ROT == HALVES ? x[0][e] : x[e / (VEC / 2 ? VEC / 2 : 1)][2 * (e % (VEC / 2 ? VEC / 2 : 1))];
+            float& b = ROT == HALVES ? x[1][e] : x[e / (VEC / 2 ? VEC / 2 : 1)][2 * (e % (VEC / 2 ? VEC / 2 : 1)) + 1 < VEC ? 2 * (e % (VEC / 2 ? VEC / 2 : 1)) + 1 : 0];
+            const float t = a, sn = WAY * s[e];
+            const bool on = s[e] != 0.f || c[e] != 1.f;
+            a = on ? t * c[e] - b * sn : t, b = on ? b * c[e] + t * sn : b;
+        }
+    }
+};
+
+// Heads [first, end) of a token for one wavefront.
+struct Part {
+    int64_t n;
+    int first, end;
+};
+__device__ __forceinline__ Part part_of(int64_t unit, int parts, int per, int heads)
+{
+    const int64_t n = unit / parts;
+    const int first = (int)(unit - n * parts) * per;
+    return {n, first, first + per < heads ? first + per : heads};
+}
+struct HeadsPlan {
+    int64_t units;   // N parts
+    int parts, per;  // of a token's heads; heads of a part
+};
+
+// A wavefront takes a part of a token's heads, 64 / G side by side; rows are requested AT_ONCE heads of a lane at a time.  Bound by memory: each element is read and written once,
+// 16 bytes a lane where rows begin on 16 bytes (VEC = 8; of fp32 twice as many).
+template <int DT, int VEC, int G, int SLOTS, int ROT> __global__ __launch_bounds__(64 * WAVES) void k_heads(HeadsCall a, HeadsPlan p)
+{
+    constexpr int SIDE = 64 / G, AT_ONCE = VEC * SLOTS >= 8 ? 2 : 4;
+    __shared__ std::conditional_t<ROT == STILL, NoAngles, Angles> angles;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, heads = a.H + a.H_k;
+    const int64_t unit = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * WAVES + __builtin_amdgcn_readfirstlane(wave);
+    if (unit >= p.units) return;
+    const Part part = part_of(unit, p.parts, p.per, heads);
+    const int64_t n = part.n;
+    Slot slots[SLOTS];
+    Elems<DT, VEC> w[2][SLOTS][2];  // of queries and keys
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i) {
+        slots[i] = slot_of<VEC, ROT>(lane % G + G * i, a.d, a.rot, a.interleaved);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            w[0][i][j].clear(), w[1][i][j].clear();
+            if (a.q_weight && slots[i].there[j]) w[0][i][j].load(a.q_weight, slots[i].i[j]);
+            if (a.k_weight && slots[i].there[j]) w[1][i][j].load(a.k_weight, slots[i].i[j]);
+        }
+    }
+    Turn<VEC, ROT> turn[SLOTS];
+    for (int h0 = part.first + lane / G; __any(h0 < part.end); h0 += SIDE * AT_ONCE) {
+        Elems<DT, VEC> raw[AT_ONCE][SLOTS][2];
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const int head = h0 + SIDE * u;
+            const bool key = head >= a.H;
+            const int64_t from = key ? n * a.k_stride + (int64_t)(head - a.H) * a.d : n * a.q_stride + (int64_t)head * a.d;
+            const void* const x = key ? a.k : a.q;
+#pragma unroll
+            for (int i = 0; i < SLOTS; ++i)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    dw[0][i][j] += key ? 0.f : e[i][j] * (u[i][j] * norm);
-                    dw[1][i][j] += key ? e[i][j] * (u[i][j] * norm) : 0.f;
-                    const float dx[1] = {norm * (f[i][j] - u[i][j] * m)};
-                    if (j == 0 || p.j >= 0) store_rounded<DT, 1>(key ? a.dk : a.dq, to + (j ? p.j : p.i), dx);
+                    raw[u][i][j].clear();
+                    if (head < part.end && slots[i].there[j]) raw[u][i][j].load(x, from + slots[i].i[j]);
+                }
+        }
+        if constexpr (ROT != STILL) {
+            if (h0 < part.first + SIDE) {  // (behind the first requests)
+                turn_angles(angles, wave, a.positions, a.pos64, a.inv_freq, a.rot / 2, n);
+#pragma unroll
+                for (int i = 0; i < SLOTS; ++i) turn[i].load(angles, wave, slots[i], a.rot, lane % G + G * i);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const int head = h0 + SIDE * u;
+            const bool key = head >= a.H, weighted = key ? a.k_weight != nullptr : a.q_weight != nullptr;
+            float x[SLOTS][2][VEC], sq = 0.f;
+#pragma unroll
+            for (int i = 0; i < SLOTS; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) x[i][j][e] = raw[u][i][j][e], sq += x[i][j][e] * x[i][j][e];
+            sq = lanes_sum<G>(sq);
+            const float norm = 1.f / sqrtf((a.unit ? sq : sq / (float)a.d) + a.eps);
+            if (head >= part.end) continue;
+            const int64_t to = key ? n * a.k_out_stride + (int64_t)(head - a.H) * a.d : n * a.q_out_stride + (int64_t)head * a.d;
+            void* const y = key ? a.k_out : a.q_out;
+#pragma unroll
+            for (int i = 0; i < SLOTS; ++i) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    Elems<DT, VEC> v;
+#pragma unroll
+                    for (int k = 0; k < Elems<DT, VEC>::WORDS; ++k) {
+                        const uint32_t of_q = w[0][i][j].w[k], of_k = w[1][i][j].w[k];
+                        v.w[k] = key ? of_k : of_q;
+                    }
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) x[i][j][e] *= norm, x[i][j][e] *= weighted ? v[e] : 1.f;
+                }
+                turn[i].template turn<1>(x[i]);
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    if (slots[i].there[j]) store_rounded<DT, VEC>(y, to + slots[i].i[j], x[i][j]);
+            }
+        }
+    }
+}
+
+// The gradient, the same way; a wavefront takes parts in turn and keeps its sums of the weights' gradients; those of a workgroup are written out and added up by k_heads_dweight,
+// always in the same order.
+template <int DT, int VEC, int G, int SLOTS, int ROT> __global__ __launch_bounds__(64 * WAVES) void k_heads_bwd(HeadsBwdCall a, HeadsPlan p)
+{
+    constexpr int SIDE = 64 / G;
+    __shared__ std::conditional_t<ROT == STILL, NoAngles, Angles> angles;
+    extern __shared__ float sums[];  // [WAVES][2 d] where weights' gradients are asked for
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, heads = a.H + a.H_k;
+    Slot slots[SLOTS];
+    Elems<DT, VEC> w[2][SLOTS][2];
+    float dw[2][SLOTS][2][VEC];
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i) {
+        slots[i] = slot_of<VEC, ROT>(lane % G + G * i, a.d, a.rot, a.interleaved);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) dw[0][i][j][e] = dw[1][i][j][e] = 0.f;
+            w[0][i][j].clear(), w[1][i][j].clear();
+            if (a.q_weight && slots[i].there[j]) w[0][i][j].load(a.q_weight, slots[i].i[j]);
+            if (a.k_weight && slots[i].there[j]) w[1][i][j].load(a.k_weight, slots[i].i[j]);
+        }
+    }
+    Turn<VEC, ROT> turn[SLOTS];
+    const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x, blocks = (int64_t)gridDim.y * gridDim.x;
+    for (int64_t unit = block * WAVES + __builtin_amdgcn_readfirstlane(wave); unit < p.units; unit += blocks * WAVES) {
+        const Part part = part_of(unit, p.parts, p.per, heads);
+        const int64_t n = part.n;
+        for (int h0 = part.first + lane / G; __any(h0 < part.end); h0 += SIDE) {
+            const int head = h0;
+            const bool key = head >= a.H, on = head < part.end, weighted = key ? a.k_weight != nullptr : a.q_weight != nullptr;
+            const int64_t h = (int64_t)(key ? head - a.H : head) * a.d;
+            Elems<DT, VEC> rx[SLOTS][2], rd[SLOTS][2];
+#pragma unroll
+            for (int i = 0; i < SLOTS; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    rx[i][j].clear(), rd[i][j].clear();
+                    if (!on || !slots[i].there[j]) continue;
+                    rx[i][j].load(key ? a.k : a.q, n * (key ? a.k_stride : a.q_stride) + h + slots[i].i[j]);
+                    rd[i][j].load(key ? a.dk_out : a.dq_out, n * (key ? a.dk_out_stride : a.dq_out_stride) + h + slots[i].i[j]);
+                }
+            if constexpr (ROT != STILL) {
+                if (h0 < part.first + SIDE) {
+                    turn_angles(angles, wave, a.positions, a.pos64, a.inv_freq, a.rot / 2, n);
+#pragma unroll
+                    for (int i = 0; i < SLOTS; ++i) turn[i].load(angles, wave, slots[i], a.rot, lane % G + G * i);
                 }
             }
+            float x[SLOTS][2][VEC], z[SLOTS][2][VEC], sq = 0.f, dot = 0.f;
+#pragma unroll
+            for (int i = 0; i < SLOTS; ++i) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) x[i][j][e] = rx[i][j][e], z[i][j][e] = rd[i][j][e], sq += x[i][j][e] * x[i][j][e];
+                turn[i].template turn<-1>(z[i]);
+            }
+            const float sum = lanes_sum<G>(sq), norm = 1.f / sqrtf((a.unit ? sum : sum / (float)a.d) + a.eps);
+#pragma unroll
+            for (int i = 0; i < SLOTS; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    Elems<DT, VEC> v;
+#pragma unroll
+                    for (int k = 0; k < Elems<DT, VEC>::WORDS; ++k) {
+                        const uint32_t of_q = w[0][i][j].w[k], of_k = w[1][i][j].w[k];
+                        v.w[k] = key ? of_k : of_q;
+                    }
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        const float t = z[i][j][e] * (x[i][j][e] * norm);
+                        if (on && key) dw[1][i][j][e] += t;
+                        if (on && !key) dw[0][i][j][e] += t;
+                        z[i][j][e] *= weighted ? v[e] : 1.f;
+                        dot += z[i][j][e] * x[i][j][e];
+                    }
+                }
+            dot = lanes_sum<G>(dot);
+            const float m = (a.unit ? dot : dot / (float)a.d) * norm * norm;
+            if (!on) continue;
+            const int64_t to = n * (key ? a.dk_stride : a.dq_stride) + h;
+#pragma unroll
+            for (int i = 0; i < SLOTS; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    if (!slots[i].there[j]) continue;
+                    float dx[VEC];
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) dx[e] = norm * (z[i][j][e] - x[i][j][e] * m);
+                    store_rounded<DT, VEC>(key ? a.dk : a.dq, to + slots[i].i[j], dx);
+                }
         }
     }
     if (!a.partial) return;
 #pragma unroll
-    for (int i = 0; i < SLOTS; ++i) {
-        const int s = lane + 64 * i;
-        if (s >= pairs) continue;
-        const Pair p = pair_of(s, a.d, a.rot, a.interleaved);
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            sums[wave][k * a.d + p.i] = dw[k][i][0];
-            if (p.j >= 0) sums[wave][k * a.d + p.j] = dw[k][i][1];
-        }
-    }
+        for (int i = 0; i < SLOTS; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    float t = dw[k][i][j][e];
+                    for (int o = G; o < 64; o *= 2) t += __shfl_xor(t, o);
+                    if (lane < G && slots[i].there[j]) sums[wave * 2 * a.d + k * a.d + slots[i].i[j] + e] = t;
+                }
     __syncthreads();
     for (int c = threadIdx.x; c < 2 * a.d; c += 64 * WAVES) {
-        float t = sums[0][c];
+        float t = sums[c];
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) t += sums[w][c];
-        a.partial[(int64_t)blockIdx.x * 2 * a.d + c] = t;
+        for (int w = 1; w < WAVES; ++w) t += sums[w * 2 * a.d + c];
+        a.partial[block * 2 * a.d + c] = t;
     }
 }
 
@@ -202,21 +342,67 @@ __global__ __launch_bounds__(1024) void k_heads_dweight(const float* partial, fl
     if (y == 0 && c < 2 * d && to) to[c < d ? c : c - d] = s;
 }
 
+// A wavefront's part of a token: all its heads where tokens are many, as few as stand side by side where they are few.
+HeadsPlan plan(int64_t N, int heads, int side)
+{
+    const int64_t steps = (heads + side - 1) / side, wanted = N > 0 ? (2048 + N - 1) / N : 1;
+    const int per = (int)((steps + (wanted < steps ? wanted : steps) - 1) / (wanted < steps ? wanted : steps)) * side, parts = (heads + per - 1) / per;
+    return {N * parts, parts, per};
+}
+// Elements of a piece: what all rows and weights allow.
+template <class... P> int piece(int d, int rot, bool interleaved, int size, std::initializer_list<int64_t> strides, P... pointers)
+{
+    for (const int v : {8, 2}) {
+        bool good = d % v == 0 && (interleaved || rot % (2 * v) == 0);
+        for (const int64_t s : strides) good = good && s % v == 0;
+        for (const void* p : {static_cast<const void*>(pointers)...}) good = good && reinterpret_cast<uintptr_t>(p) % (v * size < 16 ? v * size : 16) == 0;
+        if (good) return v;
+    }
+    return 1;
+}
+
+// f with the piece, the lanes of a head and the slots of a lane as its template's arguments: slots of two pieces each.
+template <int ROT, class F> int shapes(int vec, int d, F f)
+{
+    if (vec == 8) return d <= 64 ? f.template go<8, 4, 1, ROT>() : d <= 128 ? f.template go<8, 8, 1, ROT>() : d <= 256 ? f.template go<8, 16, 1, ROT>() : f.template go<8, 32, 1, ROT>();
+    if (vec == 2) return d <= 64 ? f.template go<2, 16, 1, ROT>() : d <= 256 ? f.template go<2, 64, 1, ROT>() : f.template go<2, 64, 2, ROT>();
+    constexpr int R = ROT == NEIGHBOURS ? HALVES : ROT;  // (pairs of single elements are slots either way)
+    return d <= 32 ? f.template go<1, 16, 1, R>() : d <= 128 ? f.template go<1, 64, 1, R>() : f.template go<1, 64, 4, R>();
+}
+template <class F> int rotations(int rot, bool interleaved, int vec, int d, F f)
+{
+    return rot == 0 ? shapes<STILL>(vec, d, f) : interleaved ? shapes<NEIGHBOURS>(vec, d, f) : shapes<HALVES>(vec, d, f);
+}
+
+template <int DT> struct Forward {
+    const HeadsCall& a;
+    template <int VEC, int G, int SLOTS, int ROT> int go() const
+    {
+        const HeadsPlan p = plan(a.N, a.H + a.H_k, 64 / G);
+        return launch_kernel(false, k_heads<DT, VEC, G, SLOTS, ROT>, long_grid((p.units + WAVES - 1) / WAVES), dim3(64 * WAVES), 0, a.stream, a, p);
+    }
+};
+template <int DT> struct Backward {
+    const HeadsBwdCall& a;
+    template <int VEC, int G, int SLOTS, int ROT> int go() const
+    {
+        const HeadsPlan p = plan(a.N, a.H + a.H_k, 64 / G);
+        const dim3 grid = a.partial ? dim3((unsigned)a.groups) : long_grid((p.units + WAVES - 1) / WAVES);
+        return launch_kernel(false, k_heads_bwd<DT, VEC, G, SLOTS, ROT>, grid, dim3(64 * WAVES), a.partial ? WAVES * 2 * a.d * 4 : 0, a.stream, a, p);
+    }
+};
 template <int DT> int heads(const HeadsCall& a)
 {
-    const dim3 grid = long_grid((a.N * (a.H + a.H_k) + WAVES - 1) / WAVES), block(64 * WAVES);
-    if (a.d <= 128) return launch_kernel(false, k_heads<DT, 1>, grid, block, 0, a.stream, a);
-    if (a.d <= 256) return launch_kernel(false, k_heads<DT, 2>, grid, block, 0, a.stream, a);
-    return launch_kernel(false, k_heads<DT, 4>, grid, block, 0, a.stream, a);
+    const int vec = piece(a.d, a.rot, a.interleaved, DT == OP_F32 ? 4 : 2, {a.q_stride, a.k_stride, a.q_out_stride, a.k_out_stride}, a.q, a.k, a.q_out, a.k_out, a.q_weight, a.k_weight);
+    return rotations(a.rot, a.interleaved, vec, a.d, Forward<DT>{a});
 }
 template <int DT> int heads_bwd(const HeadsBwdCall& a)
 {
     int rc = LAUNCHED;
-    if (a.groups > 0) {
-        const dim3 grid((unsigned)a.groups), block(64 * WAVES);
-        rc = a.d <= 128   ? launch_kernel(false, k_heads_bwd<DT, 1>, grid, block, 0, a.stream, a)
-             : a.d <= 256 ? launch_kernel(false, k_heads_bwd<DT, 2>, grid, block, 0, a.stream, a)
-                          : launch_kernel(false, k_heads_bwd<DT, 4>, grid, block, 0, a.stream, a);
+    if (a.N > 0) {
+        const int vec = piece(a.d, a.rot, a.interleaved, DT == OP_F32 ? 4 : 2, {a.q_stride, a.k_stride, a.dq_out_stride, a.dk_out_stride, a.dq_stride, a.dk_stride}, a.q, a.k, a.dq_out, a.dk_out,
+                              a.dq, a.dk, a.q_weight, a.k_weight);
+        rc = rotations(a.rot, a.interleaved, vec, a.d, Backward<DT>{a});
     }
     if (rc != LAUNCHED || (!a.dq_weight && !a.dk_weight)) return rc;
     return launch_kernel(false, k_heads_dweight, dim3((unsigned)((2 * a.d + 15) / 16)), dim3(1024), 0, a.stream, a.partial, a.dq_weight, a.dk_weight, a.groups, a.d);
@@ -224,9 +410,9 @@ template <int DT> int heads_bwd(const HeadsBwdCall& a)
 
 }  // namespace
 
-int heads_bwd_groups(int64_t N, int, int, int)
+int heads_bwd_groups(int64_t N, int H, int H_k, int)
 {
-    const int64_t n = (N + WAVES - 1) / WAVES;
+    const int64_t n = (N * (H + H_k) + 4 * WAVES - 1) / (4 * WAVES);
     return (int)(n < 1024 ? n : 1024);
 }
 int launch_heads(const HeadsCall& a) { return a.dtype == OP_F32 ? heads<OP_F32>(a) : a.dtype == OP_F16 ? heads<OP_F16>(a) : heads<OP_BF16>(a); }
