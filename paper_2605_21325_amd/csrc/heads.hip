@@ -6,6 +6,7 @@
 //
 // Angles: p f as a part of a turn, in two 64-bit parts (positions up to 2^53 in magnitude are whole numbers there, a turn is 1 / (2 pi) to 106 bits), the part of a turn
 // that is left in 32.
+#include <algorithm>
 #include "layer.hpp"
 #include "elems.hpp"
 
@@ -14,7 +15,7 @@ namespace triinv {
 namespace {
 
 constexpr int WAVES = 4;  // of a workgroup
-constexpr int MOST_PAIRS = 256;
+constexpr int MOST_D = 512;
 
 // A neighbour's value, within a row of sixteen lanes.
 template <int CTRL> __device__ __forceinline__ float from_lane(float x)
@@ -33,20 +34,23 @@ template <int G> __device__ __forceinline__ float lanes_sum(float x)
     return x;
 }
 
+constexpr int MOST_ANGLES = 512;  // of the tokens that a wavefront has at a time
 struct Angles {
-    float c[WAVES][MOST_PAIRS], s[WAVES][MOST_PAIRS];
+    float c[WAVES][MOST_ANGLES], s[WAVES][MOST_ANGLES];
 };
-struct NoAngles {};
+struct Nothing {};
 
-// cos and sin of a token's angles, a lane each, for the wavefront that asks.
-__device__ __forceinline__ void turn_angles(Angles& at, int wave, const void* positions, bool pos64, const float* inv_freq, int pairs, int64_t n)
+// cos and sin of the angles of tokens n to n + tokens - 1, a lane each, for the wavefront that asks; not beyond the last token.
+template <class Call> __device__ __forceinline__ void turn_angles(Angles& at, int wave, const Call& a, int64_t n, int tokens)
 {
 #pragma clang fp contract(off)  // (what a product loses is taken apart: no product may be fused into the difference)
+    const int pairs = a.rot / 2, left = (int)(a.N - n < tokens ? a.N - n : tokens);
     __builtin_amdgcn_wave_barrier();
-    const double p = pos64 ? (double)static_cast<const int64_t*>(positions)[n] : (double)static_cast<const int32_t*>(positions)[n];
-    for (int i = threadIdx.x & 63; i < pairs; i += 64) {
+    for (int i = threadIdx.x & 63; i < pairs * left; i += 64) {
         constexpr double TURN = 0.15915494309189535, LOW = -9.839338337591243e-18;  // 1 / (2 pi) in two parts
-        const double f = (double)inv_freq[i], t = p * f, turns = t * TURN;
+        const int token = tokens == 1 ? 0 : (int)((uint32_t)i / (uint32_t)pairs);
+        const double p = a.pos64 ? (double)static_cast<const int64_t*>(a.positions)[n + token] : (double)static_cast<const int32_t*>(a.positions)[n + token];
+        const double f = (double)a.inv_freq[i - token * pairs], t = p * f, turns = t * TURN;
         const double rest = fma(t, TURN, -turns) + fma(t, LOW, fma(p, f, -t) * TURN);
         float s, c;
         sincospif(2.f * (float)(turns - rint(turns) + rest), &s, &c);
@@ -77,16 +81,17 @@ template <int VEC, int ROT> __device__ __forceinline__ Slot slot_of(int s, int d
 // cos and sin for the pairs of a slot.
 template <int VEC, int ROT> struct Turn {
     float c[ROT == STILL ? 1 : VEC], s[ROT == STILL ? 1 : VEC];
-    __device__ __forceinline__ void load(const Angles& at, int wave, const Slot& p, int rot, int slot)
+    // From the wavefront's angle `first` on, the token's first one.
+    __device__ __forceinline__ void load(const Angles& at, int wave, int first, const Slot& p, int rot, int slot)
     {
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
             if constexpr (ROT == HALVES) {
-                c[e] = p.turned ? at.c[wave][slot * VEC + e] : 1.f, s[e] = p.turned ? at.s[wave][slot * VEC + e] : 0.f;
+                c[e] = p.turned ? at.c[wave][first + slot * VEC + e] : 1.f, s[e] = p.turned ? at.s[wave][first + slot * VEC + e] : 0.f;
             } else if constexpr (ROT == NEIGHBOURS) {
                 const int i = p.i[e / (VEC / 2)] / 2 + e % (VEC / 2);
                 const bool on = p.there[e / (VEC / 2)] && 2 * i < rot;
-                c[e] = on ? at.c[wave][i] : 1.f, s[e] = on ? at.s[wave][i] : 0.f;
+                c[e] = on ? at.c[wave][first + i] : 1.f, s[e] = on ? at.s[wave][first + i] : 0.f;
             }
         }
     }
@@ -105,73 +110,98 @@ template <int VEC, int ROT> struct Turn {
     }
 };
 
-// Heads [first, end) of a token for one wavefront.
-struct Part {
+// Queries and keys are taken by workgroups of their own.  What a wavefront has at a time, a unit: `tokens` tokens with few heads, or a part of one token's heads (parts of `per`).
+// Their heads are counted on: row k of the unit is head k mod H of its token k / H.
+struct HeadsPlan {
+    int64_t units;
+    int blocks, tokens, parts, per;
+};
+struct Unit {
     int64_t n;
     int first, end;
 };
-__device__ __forceinline__ Part part_of(int64_t unit, int parts, int per, int heads)
+__device__ __forceinline__ Unit unit_of(int64_t unit, const HeadsPlan& p, int64_t N, int H)
 {
-    const int64_t n = unit / parts;
-    const int first = (int)(unit - n * parts) * per;
-    return {n, first, first + per < heads ? first + per : heads};
+    if (p.parts == 1) {
+        const int64_t n = unit * p.tokens;
+        return {n, 0, (int)(N - n < p.tokens ? N - n : p.tokens) * H};
+    }
+    const int64_t n = unit / p.parts;
+    const int first = (int)(unit - n * p.parts) * p.per;
+    return {n, first, first + p.per < H ? first + p.per : H};
 }
-struct HeadsPlan {
-    int64_t units;   // N parts
-    int parts, per;  // of a token's heads; heads of a part
-};
+__device__ __forceinline__ int token_of(int k, const HeadsPlan& p, int H) { return p.tokens == 1 ? 0 : (int)((uint32_t)k / (uint32_t)H); }
 
-// A wavefront takes a part of a token's heads, 64 / G side by side; rows are requested AT_ONCE heads of a lane at a time.  Bound by memory: each element is read and written once,
-// 16 bytes a lane where rows begin on 16 bytes (VEC = 8; of fp32 twice as many).
-template <int DT, int VEC, int G, int SLOTS, int ROT> __global__ __launch_bounds__(64 * WAVES) void k_heads(HeadsCall a, HeadsPlan p)
+// The weight in LDS as it is.
+template <int DT, class Call> __device__ __forceinline__ void stage_weight(void* lds, const void* weight, const Call& a)
+{
+    if (!weight) return;
+    for (int i = threadIdx.x; i < a.d; i += 64 * WAVES) {
+        Elems<DT, 1> e;
+        e.load(weight, i);
+        e.store(lds, i);
+    }
+    __syncthreads();
+}
+template <int DT, int VEC> __device__ __forceinline__ void weigh(float (&x)[VEC], const void* lds, int i)
+{
+    Elems<DT, VEC> w;
+    w.load(lds, i);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) x[e] *= w[e];
+}
+// Rows of the unit's tokens from its first one's on: a slot's pieces, `row` elements behind that.
+template <int DT, int VEC> __device__ __forceinline__ void load_slot(Elems<DT, VEC> (&to)[2], const void* base, uint32_t row, const Slot& s, bool on)
+{
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        to[j].clear();
+        if (on && s.there[j]) to[j].load(static_cast<const char*>(base) + (row + (uint32_t)s.i[j]) * Elems<DT, 1>::SIZE, 0);
+    }
+}
+template <int DT> __device__ __forceinline__ char* rows_of(const void* p, int64_t n, int64_t stride)
+{
+    return const_cast<char*>(static_cast<const char*>(p)) + n * stride * Elems<DT, 1>::SIZE;
+}
+
+// A wavefront takes 64 / G heads side by side, requested AT_ONCE of a lane at a time.  Bound by memory: each element is read and written once, 16 bytes a lane where rows
+// begin on 16 bytes (VEC = 8; of fp32 twice as many).
+template <int DT, int VEC, int G, int SLOTS, int ROT> __global__ __launch_bounds__(64 * WAVES) void k_heads(HeadsCall a, HeadsPlan of_q, HeadsPlan of_k)
 {
     constexpr int SIDE = 64 / G, AT_ONCE = VEC * SLOTS >= 8 ? 2 : 4;
-    __shared__ std::conditional_t<ROT == STILL, NoAngles, Angles> angles;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, heads = a.H + a.H_k;
-    const int64_t unit = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * WAVES + __builtin_amdgcn_readfirstlane(wave);
+    __shared__ std::conditional_t<ROT == STILL, Nothing, Angles> angles;
+    __shared__ alignas(16) uint32_t lds[MOST_D * Elems<DT, 1>::SIZE / 4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    const bool key = block >= of_q.blocks;
+    if (key) block -= of_q.blocks;
+    const HeadsPlan p = key ? of_k : of_q;
+    const int H = key ? a.H_k : a.H;
+    const void *const x_rows = key ? a.k : a.q, *const weight = key ? a.k_weight : a.q_weight;
+    const int64_t stride = key ? a.k_stride : a.q_stride, out_stride = key ? a.k_out_stride : a.q_out_stride;
+    if (block >= p.blocks) return;
+    stage_weight<DT>(lds, weight, a);
+    const int64_t unit = block * WAVES + __builtin_amdgcn_readfirstlane(wave);
     if (unit >= p.units) return;
-    const Part part = part_of(unit, p.parts, p.per, heads);
-    const int64_t n = part.n;
+    const Unit u0 = unit_of(unit, p, a.N, H);
+    const char* const from = rows_of<DT>(x_rows, u0.n, stride);
+    char* const to = rows_of<DT>(key ? a.k_out : a.q_out, u0.n, out_stride);
     Slot slots[SLOTS];
-    Elems<DT, VEC> w[2][SLOTS][2];  // of queries and keys
 #pragma unroll
-    for (int i = 0; i < SLOTS; ++i) {
-        slots[i] = slot_of<VEC, ROT>(lane % G + G * i, a.d, a.rot, a.interleaved);
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            w[0][i][j].clear(), w[1][i][j].clear();
-            if (a.q_weight && slots[i].there[j]) w[0][i][j].load(a.q_weight, slots[i].i[j]);
-            if (a.k_weight && slots[i].there[j]) w[1][i][j].load(a.k_weight, slots[i].i[j]);
-        }
-    }
-    Turn<VEC, ROT> turn[SLOTS];
-    for (int h0 = part.first + lane / G; __any(h0 < part.end); h0 += SIDE * AT_ONCE) {
+    for (int i = 0; i < SLOTS; ++i) slots[i] = slot_of<VEC, ROT>(lane % G + G * i, a.d, a.rot, a.interleaved);
+    for (int k0 = u0.first; k0 < u0.end; k0 += SIDE * AT_ONCE) {
         Elems<DT, VEC> raw[AT_ONCE][SLOTS][2];
 #pragma unroll
         for (int u = 0; u < AT_ONCE; ++u) {
-            const int head = h0 + SIDE * u;
-            const bool key = head >= a.H;
-            const int64_t from = key ? n * a.k_stride + (int64_t)(head - a.H) * a.d : n * a.q_stride + (int64_t)head * a.d;
-            const void* const x = key ? a.k : a.q;
+            const int k = k0 + SIDE * u + lane / G, token = token_of(k, p, H);
 #pragma unroll
-            for (int i = 0; i < SLOTS; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    raw[u][i][j].clear();
-                    if (head < part.end && slots[i].there[j]) raw[u][i][j].load(x, from + slots[i].i[j]);
-                }
+            for (int i = 0; i < SLOTS; ++i) load_slot<DT, VEC>(raw[u][i], from, (uint32_t)token * (uint32_t)stride + (uint32_t)(k - token * H) * a.d, slots[i], k < u0.end);
         }
         if constexpr (ROT != STILL) {
-            if (h0 < part.first + SIDE) {  // (behind the first requests)
-                turn_angles(angles, wave, a.positions, a.pos64, a.inv_freq, a.rot / 2, n);
-#pragma unroll
-                for (int i = 0; i < SLOTS; ++i) turn[i].load(angles, wave, slots[i], a.rot, lane % G + G * i);
-            }
+            if (k0 == u0.first) turn_angles(angles, wave, a, u0.n, p.tokens);  // (behind the first requests)
         }
 #pragma unroll
         for (int u = 0; u < AT_ONCE; ++u) {
-            const int head = h0 + SIDE * u;
-            const bool key = head >= a.H, weighted = key ? a.k_weight != nullptr : a.q_weight != nullptr;
             float x[SLOTS][2][VEC], sq = 0.f;
 #pragma unroll
             for (int i = 0; i < SLOTS; ++i)
@@ -181,113 +211,111 @@ template <int DT, int VEC, int G, int SLOTS, int ROT> __global__ __launch_bounds
                     for (int e = 0; e < VEC; ++e) x[i][j][e] = raw[u][i][j][e], sq += x[i][j][e] * x[i][j][e];
             sq = lanes_sum<G>(sq);
             const float norm = 1.f / sqrtf((a.unit ? sq : sq / (float)a.d) + a.eps);
-            if (head >= part.end) continue;
-            const int64_t to = key ? n * a.k_out_stride + (int64_t)(head - a.H) * a.d : n * a.q_out_stride + (int64_t)head * a.d;
-            void* const y = key ? a.k_out : a.q_out;
+            const int k = k0 + SIDE * u + lane / G, token = token_of(k, p, H);
+            if (k >= u0.end) continue;
+            const uint32_t row = (uint32_t)token * (uint32_t)out_stride + (uint32_t)(k - token * H) * a.d;
 #pragma unroll
             for (int i = 0; i < SLOTS; ++i) {
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    Elems<DT, VEC> v;
 #pragma unroll
-                    for (int k = 0; k < Elems<DT, VEC>::WORDS; ++k) {
-                        const uint32_t of_q = w[0][i][j].w[k], of_k = w[1][i][j].w[k];
-                        v.w[k] = key ? of_k : of_q;
-                    }
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) x[i][j][e] *= norm, x[i][j][e] *= weighted ? v[e] : 1.f;
+                    for (int e = 0; e < VEC; ++e) x[i][j][e] *= norm;
+                    if (weight) weigh<DT, VEC>(x[i][j], lds, slots[i].there[j] ? slots[i].i[j] : 0);
                 }
-                turn[i].template turn<1>(x[i]);
+                if constexpr (ROT != STILL) {
+                    Turn<VEC, ROT> turn;
+                    turn.load(angles, wave, token * (a.rot / 2), slots[i], a.rot, lane % G + G * i);
+                    turn.template turn<1>(x[i]);
+                }
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
-                    if (slots[i].there[j]) store_rounded<DT, VEC>(y, to + slots[i].i[j], x[i][j]);
+                    if (slots[i].there[j]) store_rounded<DT, VEC>(to + (row + (uint32_t)slots[i].i[j]) * Elems<DT, 1>::SIZE, 0, x[i][j]);
             }
         }
     }
 }
 
-// The gradient, the same way; a wavefront takes parts in turn and keeps its sums of the weights' gradients; those of a workgroup are written out and added up by k_heads_dweight,
-// always in the same order.
-template <int DT, int VEC, int G, int SLOTS, int ROT> __global__ __launch_bounds__(64 * WAVES) void k_heads_bwd(HeadsBwdCall a, HeadsPlan p)
+// The gradient, the same way; a wavefront takes units in turn, asks for its next heads before it works on those it has, and (WEIGHT) keeps its sums of the weight's gradient; those
+// of a workgroup are written out and added up by k_heads_dweight, always in the same order.
+template <int DT, int VEC, int G, int SLOTS, int ROT, bool WEIGHT> __global__ __launch_bounds__(64 * WAVES) void k_heads_bwd(HeadsBwdCall a, HeadsPlan of_q, HeadsPlan of_k)
 {
     constexpr int SIDE = 64 / G;
-    __shared__ std::conditional_t<ROT == STILL, NoAngles, Angles> angles;
-    extern __shared__ float sums[];  // [WAVES][2 d] where weights' gradients are asked for
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, heads = a.H + a.H_k;
+    __shared__ std::conditional_t<ROT == STILL, Nothing, Angles> angles;
+    __shared__ alignas(16) uint32_t lds[MOST_D * Elems<DT, 1>::SIZE / 4];
+    extern __shared__ float sums[];  // [WAVES][d] (WEIGHT)
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    const int64_t place = block;
+    const bool key = block >= of_q.blocks;
+    if (key) block -= of_q.blocks;
+    const HeadsPlan p = key ? of_k : of_q;
+    const int H = key ? a.H_k : a.H;
+    const void *const x_rows = key ? a.k : a.q, *const d_rows = key ? a.dk_out : a.dq_out, *const weight = key ? a.k_weight : a.q_weight;
+    void* const out_rows = key ? a.dk : a.dq;
+    const int64_t stride = key ? a.k_stride : a.q_stride, d_stride = key ? a.dk_out_stride : a.dq_out_stride, out_stride = key ? a.dk_stride : a.dq_stride;
+    if (block >= p.blocks) return;
+    stage_weight<DT>(lds, weight, a);
     Slot slots[SLOTS];
-    Elems<DT, VEC> w[2][SLOTS][2];
-    float dw[2][SLOTS][2][VEC];
+    float dw[WEIGHT ? SLOTS : 1][2][VEC];
 #pragma unroll
     for (int i = 0; i < SLOTS; ++i) {
         slots[i] = slot_of<VEC, ROT>(lane % G + G * i, a.d, a.rot, a.interleaved);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) dw[0][i][j][e] = dw[1][i][j][e] = 0.f;
-            w[0][i][j].clear(), w[1][i][j].clear();
-            if (a.q_weight && slots[i].there[j]) w[0][i][j].load(a.q_weight, slots[i].i[j]);
-            if (a.k_weight && slots[i].there[j]) w[1][i][j].load(a.k_weight, slots[i].i[j]);
-        }
+        for (int e = 0; e < VEC; ++e)
+            if constexpr (WEIGHT) dw[i][0][e] = dw[i][1][e] = 0.f;
     }
-    Turn<VEC, ROT> turn[SLOTS];
-    const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x, blocks = (int64_t)gridDim.y * gridDim.x;
-    for (int64_t unit = block * WAVES + __builtin_amdgcn_readfirstlane(wave); unit < p.units; unit += blocks * WAVES) {
-        const Part part = part_of(unit, p.parts, p.per, heads);
-        const int64_t n = part.n;
-        for (int h0 = part.first + lane / G; __any(h0 < part.end); h0 += SIDE) {
-            const int head = h0;
-            const bool key = head >= a.H, on = head < part.end, weighted = key ? a.k_weight != nullptr : a.q_weight != nullptr;
-            const int64_t h = (int64_t)(key ? head - a.H : head) * a.d;
-            Elems<DT, VEC> rx[SLOTS][2], rd[SLOTS][2];
-#pragma unroll
-            for (int i = 0; i < SLOTS; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    rx[i][j].clear(), rd[i][j].clear();
-                    if (!on || !slots[i].there[j]) continue;
-                    rx[i][j].load(key ? a.k : a.q, n * (key ? a.k_stride : a.q_stride) + h + slots[i].i[j]);
-                    rd[i][j].load(key ? a.dk_out : a.dq_out, n * (key ? a.dk_out_stride : a.dq_out_stride) + h + slots[i].i[j]);
-                }
-            if constexpr (ROT != STILL) {
-                if (h0 < part.first + SIDE) {
-                    turn_angles(angles, wave, a.positions, a.pos64, a.inv_freq, a.rot / 2, n);
-#pragma unroll
-                    for (int i = 0; i < SLOTS; ++i) turn[i].load(angles, wave, slots[i], a.rot, lane % G + G * i);
-                }
-            }
-            float x[SLOTS][2][VEC], z[SLOTS][2][VEC], sq = 0.f, dot = 0.f;
+    for (int64_t unit = block * WAVES + __builtin_amdgcn_readfirstlane(wave); unit < p.units; unit += (int64_t)p.blocks * WAVES) {
+        const Unit u0 = unit_of(unit, p, a.N, H);
+        const char *const from = rows_of<DT>(x_rows, u0.n, stride), *const d_from = rows_of<DT>(d_rows, u0.n, d_stride);
+        char* const to = rows_of<DT>(out_rows, u0.n, out_stride);
+        Elems<DT, VEC> rx[SLOTS][2], rd[SLOTS][2];
+        const auto request = [&](int k) {
+            const int token = token_of(k, p, H);
+            const uint32_t h = (uint32_t)(k - token * H) * a.d;
 #pragma unroll
             for (int i = 0; i < SLOTS; ++i) {
+                load_slot<DT, VEC>(rx[i], from, (uint32_t)token * (uint32_t)stride + h, slots[i], k < u0.end);
+                load_slot<DT, VEC>(rd[i], d_from, (uint32_t)token * (uint32_t)d_stride + h, slots[i], k < u0.end);
+            }
+        };
+        request(u0.first + lane / G);
+        if constexpr (ROT != STILL) turn_angles(angles, wave, a, u0.n, p.tokens);
+        for (int k0 = u0.first; k0 < u0.end; k0 += SIDE) {
+            const int k = k0 + lane / G, token = token_of(k, p, H);
+            const bool on = k < u0.end;
+            float x[SLOTS][2][VEC], z[SLOTS][2][VEC], sq = 0.f, dot = 0.f;
+#pragma unroll
+            for (int i = 0; i < SLOTS; ++i)
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) x[i][j][e] = rx[i][j][e], z[i][j][e] = rd[i][j][e], sq += x[i][j][e] * x[i][j][e];
-                turn[i].template turn<-1>(z[i]);
+            if (k0 + SIDE < u0.end) request(k + SIDE);
+            if constexpr (ROT != STILL) {
+#pragma unroll
+                for (int i = 0; i < SLOTS; ++i) {
+                    Turn<VEC, ROT> turn;
+                    turn.load(angles, wave, (on ? token : 0) * (a.rot / 2), slots[i], a.rot, lane % G + G * i);
+                    turn.template turn<-1>(z[i]);
+                }
             }
             const float sum = lanes_sum<G>(sq), norm = 1.f / sqrtf((a.unit ? sum : sum / (float)a.d) + a.eps);
 #pragma unroll
             for (int i = 0; i < SLOTS; ++i)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    Elems<DT, VEC> v;
+                    if constexpr (WEIGHT) {
 #pragma unroll
-                    for (int k = 0; k < Elems<DT, VEC>::WORDS; ++k) {
-                        const uint32_t of_q = w[0][i][j].w[k], of_k = w[1][i][j].w[k];
-                        v.w[k] = key ? of_k : of_q;
+                        for (int e = 0; e < VEC; ++e) dw[i][j][e] += on ? z[i][j][e] * (x[i][j][e] * norm) : 0.f;
                     }
+                    if (weight) weigh<DT, VEC>(z[i][j], lds, slots[i].there[j] ? slots[i].i[j] : 0);
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        const float t = z[i][j][e] * (x[i][j][e] * norm);
-                        if (on && key) dw[1][i][j][e] += t;
-                        if (on && !key) dw[0][i][j][e] += t;
-                        z[i][j][e] *= weighted ? v[e] : 1.f;
-                        dot += z[i][j][e] * x[i][j][e];
-                    }
+                    for (int e = 0; e < VEC; ++e) dot += z[i][j][e] * x[i][j][e];
                 }
             dot = lanes_sum<G>(dot);
             const float m = (a.unit ? dot : dot / (float)a.d) * norm * norm;
             if (!on) continue;
-            const int64_t to = n * (key ? a.dk_stride : a.dq_stride) + h;
+            const uint32_t row = (uint32_t)token * (uint32_t)out_stride + (uint32_t)(k - token * H) * a.d;
 #pragma unroll
             for (int i = 0; i < SLOTS; ++i)
 #pragma unroll
@@ -296,58 +324,70 @@ template <int DT, int VEC, int G, int SLOTS, int ROT> __global__ __launch_bounds
                     float dx[VEC];
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) dx[e] = norm * (z[i][j][e] - x[i][j][e] * m);
-                    store_rounded<DT, VEC>(key ? a.dk : a.dq, to + slots[i].i[j], dx);
+                    store_rounded<DT, VEC>(to + (row + (uint32_t)slots[i].i[j]) * Elems<DT, 1>::SIZE, 0, dx);
                 }
         }
     }
-    if (!a.partial) return;
-#pragma unroll
-    for (int k = 0; k < 2; ++k)
+    if constexpr (WEIGHT) {
 #pragma unroll
         for (int i = 0; i < SLOTS; ++i)
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
-                    float t = dw[k][i][j][e];
+                    float t = dw[i][j][e];
                     for (int o = G; o < 64; o *= 2) t += __shfl_xor(t, o);
-                    if (lane < G && slots[i].there[j]) sums[wave * 2 * a.d + k * a.d + slots[i].i[j] + e] = t;
+                    if (lane < G && slots[i].there[j]) sums[wave * a.d + slots[i].i[j] + e] = t;
                 }
-    __syncthreads();
-    for (int c = threadIdx.x; c < 2 * a.d; c += 64 * WAVES) {
-        float t = sums[c];
+        __syncthreads();
+        for (int c = threadIdx.x; c < a.d; c += 64 * WAVES) {
+            float t = sums[c];
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) t += sums[w * 2 * a.d + c];
-        a.partial[block * 2 * a.d + c] = t;
+            for (int w = 1; w < WAVES; ++w) t += sums[w * a.d + c];
+            a.partial[place * a.d + c] = t;
+        }
     }
 }
 
-// Column c of [dq_weight, dk_weight] = sum of partial[group][c]: 16 columns a workgroup, 64 threads a column, in the same order every time.
-__global__ __launch_bounds__(1024) void k_heads_dweight(const float* partial, float* dq, float* dk, int groups, int d)
+// dq_weight[c] and, behind its workgroups, dk_weight[c] = sum of the groups' partial[group][c]: four columns a workgroup, 256 threads a column, in the same order every time.
+__global__ __launch_bounds__(1024) void k_heads_dweight(const float* partial, float* dq, float* dk, int groups_q, int groups_k, int d)
 {
-    __shared__ float part[64][17];
-    const int cx = threadIdx.x & 15, y = threadIdx.x >> 4, c = 16 * blockIdx.x + cx;
+    __shared__ float part[256][5];
+    const bool key = blockIdx.y == 1;
+    const int groups = key ? groups_k : groups_q;
+    const int cx = threadIdx.x & 3, y = threadIdx.x >> 2, c = 4 * blockIdx.x + cx;
+    float* const to = key ? dk : dq;
+    if (!to) return;
+    if (key) partial += (int64_t)groups_q * d;
     float s = 0.f;
-    if (c < 2 * d) {
+    if (c < d) {
 #pragma unroll 8
-        for (int g = y; g < groups; g += 64) s += partial[(int64_t)g * 2 * d + c];
+        for (int g = y; g < groups; g += 256) s += partial[(int64_t)g * d + c];
     }
     part[y][cx] = s;
     __syncthreads();
-    for (int half = 32; half > 0; half /= 2) {
+    for (int half = 128; half > 0; half /= 2) {
         if (y < half) part[y][cx] = s += part[y + half][cx];
         __syncthreads();
     }
-    float* const to = c < d ? dq : dk;
-    if (y == 0 && c < 2 * d && to) to[c < d ? c : c - d] = s;
+    if (y == 0 && c < d) to[c] = s;
 }
 
-// A wavefront's part of a token: all its heads where tokens are many, as few as stand side by side where they are few.
-HeadsPlan plan(int64_t N, int heads, int side)
+// A wavefront's unit.  Where tokens are many: as many of them as have ROWS times the heads that stand side by side, so that one's angles and addresses and the way to memory
+// come once for several rows (their rows by 32-bit offsets, their angles as far as LDS has room).  Where they are few: a part of a token's heads.
+constexpr int ROWS = 2;
+HeadsPlan plan(int64_t N, int H, int side, int64_t stride, int pairs)
 {
-    const int64_t steps = (heads + side - 1) / side, wanted = N > 0 ? (2048 + N - 1) / N : 1;
-    const int per = (int)((steps + (wanted < steps ? wanted : steps) - 1) / (wanted < steps ? wanted : steps)) * side, parts = (heads + per - 1) / per;
-    return {N * parts, parts, per};
+    if (H <= 0 || N <= 0) return {0, 0, 1, 1, 1};
+    const auto blocks = [](int64_t units) { return (int)((units + WAVES - 1) / WAVES); };
+    const int64_t tokens = std::min<int64_t>({(int64_t)ROWS * side / H, N / 2048, (int64_t)(pairs ? MOST_ANGLES / pairs : 64), (1LL << 29) / std::max<int64_t>(stride, 1)});
+    if (tokens > 1) {
+        const int64_t units = (N + tokens - 1) / tokens;
+        return {units, blocks(units), (int)tokens, 1, H};
+    }
+    const int64_t steps = (H + side - 1) / side, most = (2048 + N - 1) / N, wanted = most < steps ? most : steps;
+    const int per = (int)((steps + wanted - 1) / wanted) * side, parts = (H + per - 1) / per;
+    return {N * parts, blocks(N * parts), 1, parts, per};
 }
 // Elements of a piece: what all rows and weights allow.
 template <class... P> int piece(int d, int rot, bool interleaved, int size, std::initializer_list<int64_t> strides, P... pointers)
@@ -378,17 +418,20 @@ template <int DT> struct Forward {
     const HeadsCall& a;
     template <int VEC, int G, int SLOTS, int ROT> int go() const
     {
-        const HeadsPlan p = plan(a.N, a.H + a.H_k, 64 / G);
-        return launch_kernel(false, k_heads<DT, VEC, G, SLOTS, ROT>, long_grid((p.units + WAVES - 1) / WAVES), dim3(64 * WAVES), 0, a.stream, a, p);
+        const HeadsPlan q = plan(a.N, a.H, 64 / G, std::max<int64_t>({a.q_stride, a.q_out_stride}), a.rot / 2), k = plan(a.N, a.H_k, 64 / G, std::max<int64_t>({a.k_stride, a.k_out_stride}), a.rot / 2);
+        return launch_kernel(false, k_heads<DT, VEC, G, SLOTS, ROT>, long_grid((int64_t)q.blocks + k.blocks), dim3(64 * WAVES), 0, a.stream, a, q, k);
     }
 };
 template <int DT> struct Backward {
     const HeadsBwdCall& a;
     template <int VEC, int G, int SLOTS, int ROT> int go() const
     {
-        const HeadsPlan p = plan(a.N, a.H + a.H_k, 64 / G);
-        const dim3 grid = a.partial ? dim3((unsigned)a.groups) : long_grid((p.units + WAVES - 1) / WAVES);
-        return launch_kernel(false, k_heads_bwd<DT, VEC, G, SLOTS, ROT>, grid, dim3(64 * WAVES), a.partial ? WAVES * 2 * a.d * 4 : 0, a.stream, a, p);
+        HeadsPlan q = plan(a.N, a.H, 64 / G, std::max<int64_t>({a.q_stride, a.dq_out_stride, a.dq_stride}), a.rot / 2), k = plan(a.N, a.H_k, 64 / G, std::max<int64_t>({a.k_stride, a.dk_out_stride, a.dk_stride}), a.rot / 2);
+        if (a.partial) {
+            q.blocks = a.groups_q, k.blocks = a.groups_k;
+            return launch_kernel(false, k_heads_bwd<DT, VEC, G, SLOTS, ROT, true>, dim3((unsigned)(a.groups_q + a.groups_k)), dim3(64 * WAVES), WAVES * a.d * 4, a.stream, a, q, k);
+        }
+        return launch_kernel(false, k_heads_bwd<DT, VEC, G, SLOTS, ROT, false>, long_grid((int64_t)q.blocks + k.blocks), dim3(64 * WAVES), 0, a.stream, a, q, k);
     }
 };
 template <int DT> int heads(const HeadsCall& a)
@@ -405,15 +448,18 @@ template <int DT> int heads_bwd(const HeadsBwdCall& a)
         rc = rotations(a.rot, a.interleaved, vec, a.d, Backward<DT>{a});
     }
     if (rc != LAUNCHED || (!a.dq_weight && !a.dk_weight)) return rc;
-    return launch_kernel(false, k_heads_dweight, dim3((unsigned)((2 * a.d + 15) / 16)), dim3(1024), 0, a.stream, a.partial, a.dq_weight, a.dk_weight, a.groups, a.d);
+    return launch_kernel(false, k_heads_dweight, dim3((unsigned)((a.d + 3) / 4), 2), dim3(1024), 0, a.stream, a.partial, a.dq_weight, a.dk_weight, a.groups_q, a.groups_k, a.d);
 }
 
 }  // namespace
 
-int heads_bwd_groups(int64_t N, int H, int H_k, int)
+// Workgroups that keep a sum each, for queries and keys together in proportion; each with sixteen rows a wavefront, 2048 of them at most.  In us, both launches, with 512 / 768 / 1024 /
+// 2048 / 4096 of them at most (heads of 128, bf16, rotated): 16384 tokens of 40 heads 129 / 140 / 127 / 115 / 117, 65536 of 10 182 / 172 / 153 / 131 / 130; rows a wavefront 4 / 16
+// / 32 / 64: 256 tokens of 24 heads 9.5 / 10 / 13 / 20, 1024 17.8 / 13.8 / 16 / 23, 4096 31 / 29 / 26 / 30.
+int heads_bwd_groups(int64_t N, int H, int heads)
 {
-    const int64_t n = (N * (H + H_k) + 4 * WAVES - 1) / (4 * WAVES);
-    return (int)(n < 1024 ? n : 1024);
+    const int64_t n = (N * H + 16 * WAVES - 1) / (16 * WAVES), share = ((int64_t)2048 * H + heads - 1) / heads;
+    return (int)(n < share ? n : share);
 }
 int launch_heads(const HeadsCall& a) { return a.dtype == OP_F32 ? heads<OP_F32>(a) : a.dtype == OP_F16 ? heads<OP_F16>(a) : heads<OP_BF16>(a); }
 int launch_heads_bwd(const HeadsBwdCall& a) { return a.dtype == OP_F32 ? heads_bwd<OP_F32>(a) : a.dtype == OP_F16 ? heads_bwd<OP_F16>(a) : heads_bwd<OP_BF16>(a); }

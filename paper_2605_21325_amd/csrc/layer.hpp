@@ -100,14 +100,14 @@ struct HeadsBwdCall {
     const void *dq_out, *dk_out, *q, *k, *q_weight, *k_weight, *positions;
     const float* inv_freq;
     void *dq, *dk;
-    float *dq_weight, *dk_weight, *partial;  // partial: [groups][2 d], or null where neither weight's gradient is asked for
+    float *dq_weight, *dk_weight, *partial;  // partial: [groups_q + groups_k][d], or null where neither weight's gradient is asked for
     int64_t N, dq_out_stride, dk_out_stride, q_stride, k_stride, dq_stride, dk_stride;
-    int H, H_k, d, rot, dtype, groups;
+    int H, H_k, d, rot, dtype, groups_q, groups_k;
     bool unit, interleaved, pos64;
     float eps;
     hipStream_t stream;
 };
-int heads_bwd_groups(int64_t N, int H, int H_k, int d);
+int heads_bwd_groups(int64_t N, int H, int heads);  // workgroups for H of the heads
 int launch_heads_bwd(const HeadsBwdCall& a);
 
 // The gated recurrence: tokens' strides in elements.

@@ -39,7 +39,7 @@ int heads_shape(int64_t N, int H, int H_k, int d, int rot, int dtype, uint32_t f
     if ((int64_t)H + H_k > (1 << 20) || N * ((int64_t)H + H_k) > 0x7fffffffLL) return TRIINV_ERR_UNSUPPORTED;
     return TRIINV_OK;
 }
-int64_t heads_workspace(int64_t N, int H, int H_k, int d) { return (int64_t)heads_bwd_groups(N, H, H_k, d) * 2 * d * 4; }
+int64_t heads_workspace(int64_t N, int H, int H_k, int d) { return ((int64_t)heads_bwd_groups(N, H, H + H_k) + heads_bwd_groups(N, H_k, H + H_k)) * d * 4; }
 
 constexpr uint32_t SCAN_FLAGS = TRIINV_SCAN_LOGIT | TRIINV_SCAN_MIX;
 int scan_types(int dtype, int g_dtype, uint32_t flags)
@@ -132,7 +132,7 @@ int qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const void* q, cons
         for (int j = 0; j < 5; ++j)
             if (overlap(up[i], out[j]) && !(i == j && same(up[i], out[j]))) return TRIINV_ERR_ALIAS;
     return finish(launch_heads_bwd(HeadsBwdCall{dq_out, dk_out, q, k, q_weight, k_weight, positions, inv_freq, dq, dk, dq_weight, dk_weight, weights ? static_cast<float*>(workspace) : nullptr, N,
-                                                dq_out_stride, dk_out_stride, q_stride, k_stride, dq_stride, dk_stride, H, H_k, d, rot, dtype, heads_bwd_groups(N, H, H_k, d),
+                                                dq_out_stride, dk_out_stride, q_stride, k_stride, dq_stride, dk_stride, H, H_k, d, rot, dtype, heads_bwd_groups(N, H, H + H_k), heads_bwd_groups(N, H_k, H + H_k),
                                                 (flags & TRIINV_HEADS_UNIT) != 0, (flags & TRIINV_HEADS_INTERLEAVED) != 0, (flags & TRIINV_HEADS_POS64) != 0, eps,
                                                 static_cast<hipStream_t>(hip_stream)}));
 }

@@ -293,25 +293,30 @@ template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC, bool ONLY> _
     }
 }
 
-// A lane a channel.
-constexpr int THREADS = 64;
-template <int DT, int GT, bool LOGIT, bool MIX> __global__ __launch_bounds__(THREADS) void k_scan_step(ScanStepCall a)
+// One token: VEC channels a lane.  Bound by memory: the state is read and written once, 8 bytes a channel.
+constexpr int THREADS = 256;
+template <int DT, int GT, bool LOGIT, bool MIX, int VEC> __global__ __launch_bounds__(THREADS) void k_scan_step(ScanStepCall a)
 {
-    const int groups = (a.D + THREADS - 1) / THREADS;
-    const int64_t b = blockIdx.x / groups;
-    const int c = (int)(blockIdx.x % groups) * THREADS + threadIdx.x;
+    const int groups = (a.D + THREADS * VEC - 1) / (THREADS * VEC);
+    const int b = (int)(blockIdx.x / (unsigned)groups), c = ((int)(blockIdx.x - (unsigned)(b * groups)) * THREADS + (int)threadIdx.x) * VEC;
     if (c >= a.D) return;
+    Elems<DT, VEC> x;
+    Elems<GT, VEC> g;
+    x.load(a.x, b * a.x_stride + c), g.load(a.g, b * a.g_stride + c);
     const int64_t slot = a.slots ? a.slots[b] : b;
-    float o[1] = {0.f};
+    float o[VEC] = {};
     if (slot >= 0 && slot < a.n_slot) {
-        Elems<DT, 1> x;
-        Elems<GT, 1> g;
-        x.load(a.x, b * a.x_stride + c), g.load(a.g, b * a.g_stride + c);
-        const Gate f = gate<GT, LOGIT, MIX>(g[0]);
-        float* const h = a.state + slot * a.D + c;
-        *h = o[0] = fmaf(f.a, *h, MIX ? f.rest * x[0] : x[0]);
+        float* const at = a.state + slot * a.D + c;
+        Elems<OP_F32, VEC> h;
+        h.load(at, 0);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            const Gate f = gate<GT, LOGIT, MIX>(g[e]);
+            o[e] = fmaf(f.a, h[e], MIX ? f.rest * x[e] : x[e]);
+        }
+        store_rounded<OP_F32, VEC>(at, 0, o);
     }
-    store_rounded<DT, 1>(a.h, b * a.h_stride + c, o);
+    store_rounded<DT, VEC>(a.h, b * a.h_stride + c, o);
 }
 
 // f with the kinds of the call as its template's arguments.
@@ -376,10 +381,18 @@ template <bool BACK> struct Scan {
 };
 struct Step {
     const ScanStepCall& a;
+    template <int DT, int GT, bool LOGIT, bool MIX, int VEC> int with() const
+    {
+        const dim3 grid((unsigned)((int64_t)a.B * ((a.D + THREADS * VEC - 1) / (THREADS * VEC))));
+        return launch_kernel(false, k_scan_step<DT, GT, LOGIT, MIX, VEC>, grid, dim3(THREADS), 0, a.stream, a);
+    }
     template <int DT, int GT, bool LOGIT, bool MIX> int go() const
     {
-        const dim3 grid((unsigned)((int64_t)a.B * ((a.D + THREADS - 1) / THREADS)));
-        return launch_kernel(false, k_scan_step<DT, GT, LOGIT, MIX>, grid, dim3(THREADS), 0, a.stream, a);
+        // Four channels a lane where every row's begin allows it: 256 sequences of 8192 channels, bf16, 9.0 us one by one, 6.4 so (eight 7.2); 16 of 4096 1.9 either way.
+        const auto fours = [](const void* p, int64_t stride, int dtype) { return stride % 4 == 0 && reinterpret_cast<uintptr_t>(p) % (dtype == OP_F32 ? 16 : 8) == 0; };
+        if (a.D % 4 == 0 && fours(a.x, a.x_stride, DT) && fours(a.g, a.g_stride, GT) && fours(a.h, a.h_stride, DT) && fours(a.state, a.D, OP_F32))
+            return with<DT, GT, LOGIT, MIX, 4>();
+        return with<DT, GT, LOGIT, MIX, 1>();
     }
 };
 

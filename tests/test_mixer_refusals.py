@@ -100,7 +100,7 @@ def test_workspaces(L):
     assert L.gated_scan_workspace(100, 0, 64, ctypes.byref(n)) == BAD_SHAPE
     assert L.gated_scan_workspace(64, 64, 64, ctypes.byref(n)) == OK and n.value == 0
     assert L.gated_scan_workspace(100, 2, 64, None) == NULL
-    assert L.qk_norm_rope_bwd_workspace(100, 4, 2, 64, ctypes.byref(n)) == OK and n.value >= 2 * 64 * 4
+    assert L.qk_norm_rope_bwd_workspace(100, 4, 2, 64, ctypes.byref(n)) == OK and n.value >= 2 * 64 * 4 and n.value % (64 * 4) == 0
     assert L.qk_norm_rope_bwd_workspace(0, 4, 2, 64, ctypes.byref(n)) == OK and n.value == 0
     assert L.qk_norm_rope_bwd_workspace(100, 4, 2, 600, ctypes.byref(n)) == BAD_SHAPE
 
