@@ -2,7 +2,7 @@
 // tensor and the call of the C-ABI.  In Python a call takes the host 5.5 to 12 us, here 4.1 to 5.6, and small kernels take 4 to 10.
 //
 // A function returns the result, or None when anything about its arguments is not plain (no exact torch.Tensor on the current
-// device, not contiguous, another number of dimensions or element type, a chunk size there is no kernel for, an argument of the
+// device, not contiguous or, where tokens' rows are taken, not one stride apart, another number of dimensions or element type, a chunk size there is no kernel for, an argument of the
 // wrong kind) or when the C-ABI refused the call.  No matrix has been formed or written then, and the caller goes through the Python route,
 // which raises what there is to raise: this file has no error messages of its own.  (Packed sequences: their offsets may have been
 // written already, by a kernel on the call's stream, into a tensor that is then given back to the allocator of that stream.  Whoever gets its
@@ -59,6 +59,23 @@ struct LayerAbi {
     int (*norm_bwd)(const void*, const void*, const void*, const void*, void*, void*, void*, int64_t, int64_t, int, int, float, void*);
 } layer;
 
+// The head norms and the gated recurrence (connect_mixer).
+struct MixerAbi {
+    int (*heads)(const void*, const void*, const void*, const void*, const void*, const void*, void*, void*, int64_t, int64_t, int64_t, int64_t, int64_t, int, int, int, int, int, uint32_t,
+                 float, void*);
+    int (*heads_bwd)(const void*, const void*, const void*, const void*, const void*, const void*, const void*, const void*, void*, void*, void*, void*, void*, int64_t, int64_t, int64_t,
+                     int64_t, int64_t, int64_t, int64_t, int64_t, int, int, int, int, int, uint32_t, float, void*);
+    int (*heads_bwd_workspace)(int64_t, int, int, int, int64_t*);
+    int (*scan)(const void*, const void*, const void*, void*, void*, void*, int64_t, int, int64_t, int, int64_t, int64_t, int64_t, int, int, uint32_t, void*);
+    int (*scan_varlen)(const void*, const void*, const void*, void*, void*, void*, int64_t, const int64_t*, int, int64_t, int, int64_t, int64_t, int64_t, int, int, uint32_t, void*);
+    int (*scan_workspace)(int64_t, int, int, int64_t*);
+    int (*scan_bwd)(const void*, const void*, const void*, const void*, const void*, const void*, void*, void*, void*, void*, int64_t, int, int64_t, int, int64_t, int64_t, int64_t, int64_t,
+                    int64_t, int64_t, int, int, uint32_t, void*);
+    int (*scan_bwd_varlen)(const void*, const void*, const void*, const void*, const void*, const void*, void*, void*, void*, void*, int64_t, const int64_t*, int, int64_t, int, int64_t, int64_t,
+                           int64_t, int64_t, int64_t, int64_t, int, int, uint32_t, void*);
+    int (*scan_step)(const void*, const void*, void*, const void*, void*, int, int64_t, int, int64_t, int64_t, int64_t, int, int, uint32_t, void*);
+} mixer;
+
 int code_of(at::ScalarType t) { return t == at::kFloat ? F32 : t == at::kHalf ? F16 : t == at::kBFloat16 ? BF16 : -1; }
 
 // Reads the arguments of one call in order; ok() is false once one of them was not plain.
@@ -84,13 +101,43 @@ public:
     at::Tensor tensor(int dims, bool none = false) { return as_tensor(next(), dims, none); }
     at::Tensor as_tensor(PyObject* o, int dims, bool none = false)
     {
-        if (!ok_ || (none && o == Py_None)) return {};
-        if (!THPVariable_CheckExact(o)) return fail(), at::Tensor();
-        at::Tensor t = THPVariable_Unpack(o);
-        if ((device_ < 0 ? !t.is_cpu() : !t.is_cuda() || t.get_device() != device_) || t.is_nested() || t.layout() != at::kStrided ||
-            !t.is_contiguous() || (dims >= 0 && t.dim() != dims) || code_of(t.scalar_type()) < 0)
-            return fail(), at::Tensor();
+        const at::Tensor t = plain(o, none);
+        if (t.defined() && (!t.is_contiguous() || (dims >= 0 && t.dim() != dims) || code_of(t.scalar_type()) < 0)) return fail(), at::Tensor();
         return t;
+    }
+    // a tensor whose last `inner` dimensions, a token's, are contiguous, and its tokens one stride apart: that many elements, in step
+    at::Tensor rows(int inner, int64_t& step, bool none = false)
+    {
+        const at::Tensor t = plain(next(), none);
+        step = 0;
+        if (!t.defined()) return t;
+        if (code_of(t.scalar_type()) < 0 || t.dim() < inner) return fail(), at::Tensor();
+        int64_t width = 1, span = -1;
+        for (int64_t i = t.dim() - 1; i >= t.dim() - inner; width *= t.size(i--))
+            if (t.size(i) != 1 && t.stride(i) != width && t.numel()) return fail(), at::Tensor();
+        step = width;
+        for (int64_t i = t.dim() - inner - 1; i >= 0; --i) {
+            if (t.size(i) == 1 || !t.numel()) continue;
+            if (span < 0)
+                step = t.stride(i);
+            else if (t.stride(i) != span)
+                return fail(), at::Tensor();
+            span = t.stride(i) * t.size(i);
+        }
+        return t;
+    }
+    // a contiguous tensor of whole numbers, int32 or int64, or None
+    at::Tensor whole_numbers()
+    {
+        const at::Tensor t = plain(next(), true);
+        if (t.defined() && (!t.is_contiguous() || (t.scalar_type() != at::kInt && t.scalar_type() != at::kLong))) return fail(), at::Tensor();
+        return t;
+    }
+    bool truth()
+    {
+        PyObject* const o = next();
+        if (!ok_ || !PyBool_Check(o)) return fail();
+        return o == Py_True;
     }
     double number()
     {
@@ -124,6 +171,15 @@ public:
         if (!given) return at::kFloat;
         if (!THPDtype_Check(o)) return fail(), at::kFloat;
         return reinterpret_cast<THPDtype*>(o)->scalar_type;
+    }
+    // a tensor of any layout of elements on the device of the call; none: None may stand for it
+    at::Tensor plain(PyObject* o, bool none)
+    {
+        if (!ok_ || (none && o == Py_None)) return {};
+        if (!THPVariable_CheckExact(o)) return fail(), at::Tensor();
+        at::Tensor t = THPVariable_Unpack(o);
+        if ((device_ < 0 ? !t.is_cpu() : !t.is_cuda() || t.get_device() != device_) || t.is_nested() || t.layout() != at::kStrided) return fail(), at::Tensor();
+        return t;
     }
     PyObject* next() { return ok_ ? *v_++ : nullptr; }
     int fail() { return ok_ = false, 0; }
@@ -613,6 +669,238 @@ PyObject* norm_bwd(PyObject*, PyObject* const* v, Py_ssize_t n)
     return tuple_of(r);
 }
 
+// What the head norms and their gradient share.
+struct HeadsArguments {
+    at::Tensor q, k, qw, kw, positions, freq;
+    int64_t sq = 0, sk = 0, N = 0, H = 0, Hk = 0, d = 0, rot = 0;
+    uint32_t flags = 0;
+    float eps = 0;
+    // q, k, q_weight, k_weight, positions, inv_freq, unit, interleaved, eps
+    bool read(Args& a)
+    {
+        q = a.rows(2, sq), k = a.rows(2, sk, true), qw = a.tensor(1, true), kw = a.tensor(1, true), positions = a.whole_numbers(), freq = a.tensor(1, true);
+        const bool unit = a.truth(), interleaved = a.truth();
+        eps = (float)a.number();
+        if (!a.ok() || !q.numel()) return false;
+        const int64_t lead = q.dim() - 2;
+        H = q.size(lead), d = q.size(lead + 1), N = q.numel() / (H * d);
+        std::vector<int64_t> shape(q.sizes().begin(), q.sizes().end());
+        if (k.defined()) {
+            if (k.dim() != q.dim() || !k.numel()) return false;
+            Hk = shape[lead] = k.size(lead);
+            if (!has(k, shape, q.scalar_type())) return false;
+        } else if (kw.defined()) {
+            return false;
+        }
+        shape.resize(lead);
+        if (!has(qw, {d}, q.scalar_type()) || !has(kw, {d}, q.scalar_type()) || positions.defined() != freq.defined()) return false;
+        if (freq.defined()) {
+            rot = 2 * freq.size(0);
+            if (positions.sizes() != at::IntArrayRef(shape) || freq.scalar_type() != at::kFloat || rot > d) return false;
+        }
+        flags = (uint32_t)unit | (uint32_t)interleaved << 1 | (uint32_t)(positions.defined() && positions.scalar_type() == at::kLong) << 2;
+        for (const int64_t x : {H, Hk, d}) a.narrow(x);
+        return a.ok();
+    }
+    int type() const { return code_of(q.scalar_type()); }
+};
+bool like(const at::Tensor& t, const at::Tensor& of) { return !t.defined() || (of.defined() && t.sizes() == of.sizes() && t.scalar_type() == of.scalar_type()); }
+// Elements from a token to the next of a tensor made here, a token of `width` elements.
+void make_rows(at::Tensor& t, const at::Tensor& of, int64_t& step, int64_t width)
+{
+    if (t.defined() || !of.defined()) return;
+    t = at::empty(of.sizes(), of.options());
+    step = width;
+}
+
+// (device, stream, q, k, q_weight, k_weight, positions, inv_freq, unit, interleaved, eps, q_out, k_out): (q_out, k_out)
+PyObject* heads(PyObject*, PyObject* const* v, Py_ssize_t n)
+{
+    Args a(v, n, 13);
+    a.device_and_stream();
+    HeadsArguments x;
+    if (!x.read(a)) return none();
+    int64_t soq = 0, sok = 0;
+    at::Tensor r[2];
+    r[0] = a.rows(2, soq, true), r[1] = a.rows(2, sok, true);
+    if (!a.ok() || !like(r[0], x.q) || !like(r[1], x.k)) return none();
+    if (!unlocked([&] {
+            make_rows(r[0], x.q, soq, x.H * x.d), make_rows(r[1], x.k, sok, x.Hk * x.d);
+            return mixer.heads(x.q.data_ptr(), opt(x.k), opt(x.qw), opt(x.kw), opt(x.positions), opt(x.freq), r[0].data_ptr(), const_cast<void*>(opt(r[1])), x.N, x.sq, x.sk, soq, sok, (int)x.H,
+                               (int)x.Hk, (int)x.d, (int)x.rot, x.type(), x.flags, x.eps, a.stream()) == 0;
+        }))
+        return none();
+    return tuple_of(r);
+}
+
+// (device, stream, dq_out, dk_out, q, k, q_weight, k_weight, positions, inv_freq, unit, interleaved, eps, dq, dk): (dq, dk, dq_weight, dk_weight)
+PyObject* heads_bwd(PyObject*, PyObject* const* v, Py_ssize_t n)
+{
+    Args a(v, n, 15);
+    a.device_and_stream();
+    int64_t suq = 0, suk = 0, soq = 0, sok = 0;
+    const at::Tensor uq = a.rows(2, suq), uk = a.rows(2, suk, true);
+    HeadsArguments x;
+    if (!x.read(a) || !like(uq, x.q) || !like(uk, x.k) || uk.defined() != x.k.defined()) return none();
+    at::Tensor r[4];
+    r[0] = a.rows(2, soq, true), r[1] = a.rows(2, sok, true);
+    if (!a.ok() || !like(r[0], x.q) || !like(r[1], x.k)) return none();
+    if (!unlocked([&] {
+            int64_t bytes = 0;
+            at::Tensor ws;
+            if (x.qw.defined() || x.kw.defined()) {
+                if (mixer.heads_bwd_workspace(x.N, (int)x.H, (int)x.Hk, (int)x.d, &bytes) != 0) return false;
+                ws = at::empty({bytes}, x.q.options().dtype(at::kByte));
+                if (x.qw.defined()) r[2] = at::empty({x.d}, x.q.options().dtype(at::kFloat));
+                if (x.kw.defined()) r[3] = at::empty({x.d}, x.q.options().dtype(at::kFloat));
+            }
+            make_rows(r[0], x.q, soq, x.H * x.d), make_rows(r[1], x.k, sok, x.Hk * x.d);
+            const auto p = [&](int i) { return const_cast<void*>(opt(r[i])); };
+            return mixer.heads_bwd(uq.data_ptr(), opt(uk), x.q.data_ptr(), opt(x.k), opt(x.qw), opt(x.kw), opt(x.positions), opt(x.freq), p(0), p(1), p(2), p(3), const_cast<void*>(opt(ws)), bytes, x.N,
+                                   suq, suk, x.sq, x.sk, soq, sok, (int)x.H, (int)x.Hk, (int)x.d, (int)x.rot, x.type(), x.flags, x.eps, a.stream()) == 0;
+        }))
+        return none();
+    return tuple_of(r);
+}
+
+// Sequences of a recurrence's call: [B, Tlen, D], or packed [total, D] with their lengths.
+struct ScanArguments {
+    std::vector<int64_t> lens;
+    at::Tensor cu;
+    int64_t n_seq = 0, T = 0, N = 0, D = 0;
+    bool packed = false;
+    bool read(const at::Tensor& t, PyObject* seqlens)
+    {
+        if (t.dim() != (packed ? 2 : 3) || !t.numel() || (packed && !lengths(seqlens, lens))) return false;
+        n_seq = packed ? (int64_t)lens.size() : t.size(0), T = packed ? 0 : t.size(1), D = t.size(-1), N = t.numel() / D;
+        return true;
+    }
+    bool prepare(const at::Tensor& t, void* stream, at::Tensor& ws, int64_t& bytes)
+    {
+        if (packed) {
+            int64_t n_chunk = 0;
+            cu = at::empty({2 * (n_seq + 1)}, t.options().dtype(at::kLong));
+            if (abi.offsets(lens.data(), (int)n_seq, 128, N, cu.data_ptr<int64_t>(), &n_chunk, stream) != 0) return false;
+        }
+        if (mixer.scan_workspace(N, (int)n_seq, (int)D, &bytes) != 0) return false;
+        if (bytes > 0) ws = at::empty({bytes}, t.options().dtype(at::kByte));
+        return true;
+    }
+};
+bool gate_type_ok(const at::Tensor& g, const at::Tensor& x) { return g.sizes() == x.sizes() && (g.scalar_type() == x.scalar_type() || g.scalar_type() == at::kFloat); }
+
+// (device, stream, x, g, [seqlens,] state, logit, mix, h, final_state): (h, final_state)
+PyObject* scan_call(PyObject* const* v, Py_ssize_t n, bool packed)
+{
+    Args a(v, n, packed ? 10 : 9);
+    a.device_and_stream();
+    int64_t sx = 0, sg = 0, sh = 0;
+    const at::Tensor x = a.rows(1, sx), g = a.rows(1, sg);
+    PyObject* const seqlens = packed ? a.next() : nullptr;
+    const at::Tensor state = a.tensor(2, true);
+    const bool logit = a.truth(), mix = a.truth();
+    at::Tensor r[2];
+    r[0] = a.rows(1, sh, true), r[1] = a.tensor(2, true);
+    ScanArguments s;
+    s.packed = packed;
+    if (!a.ok() || !s.read(x, seqlens) || !gate_type_ok(g, x) || !like(r[0], x) || !has(state, {s.n_seq, s.D}, at::kFloat) || !has(r[1], {s.n_seq, s.D}, at::kFloat)) return none();
+    a.narrow(s.n_seq), a.narrow(s.D);
+    const uint32_t flags = (uint32_t)logit | (uint32_t)mix << 1;
+    if (!a.ok() || !unlocked([&] {
+            at::Tensor ws;
+            int64_t bytes = 0;
+            if (!s.prepare(x, a.stream(), ws, bytes)) return false;
+            make_rows(r[0], x, sh, s.D);
+            if (!r[1].defined()) r[1] = at::empty({s.n_seq, s.D}, x.options().dtype(at::kFloat));
+            void* const w = const_cast<void*>(opt(ws));
+            const int type = code_of(x.scalar_type()), g_type = code_of(g.scalar_type());
+            return (packed ? mixer.scan_varlen(x.data_ptr(), g.data_ptr(), opt(state), r[0].data_ptr(), r[1].data_ptr(), w, bytes, s.cu.data_ptr<int64_t>(), (int)s.n_seq, s.N, (int)s.D, sx, sg, sh,
+                                               type, g_type, flags, a.stream())
+                           : mixer.scan(x.data_ptr(), g.data_ptr(), opt(state), r[0].data_ptr(), r[1].data_ptr(), w, bytes, (int)s.n_seq, s.T, (int)s.D, sx, sg, sh, type, g_type, flags,
+                                        a.stream())) == 0;
+        }))
+        return none();
+    return keep_offsets(keep_offsets(tuple_of(r), 0, s.cu), 1, s.cu);
+}
+PyObject* scan(PyObject*, PyObject* const* v, Py_ssize_t n) { return scan_call(v, n, false); }
+PyObject* scan_varlen(PyObject*, PyObject* const* v, Py_ssize_t n) { return scan_call(v, n, true); }
+
+// (device, stream, x, g, h, dh, [seqlens,] state, dstate, logit, mix, dx, dg): (dx, dg, dstate0)
+PyObject* scan_bwd_call(PyObject* const* v, Py_ssize_t n, bool packed)
+{
+    Args a(v, n, packed ? 13 : 12);
+    a.device_and_stream();
+    int64_t sx = 0, sg = 0, sh = 0, sd = 0, sox = 0, sog = 0;
+    const at::Tensor x = a.rows(1, sx, true), g = a.rows(1, sg), h = a.rows(1, sh), dh = a.rows(1, sd);
+    PyObject* const seqlens = packed ? a.next() : nullptr;
+    const at::Tensor state = a.tensor(2, true), dstate = a.tensor(2, true);
+    const bool logit = a.truth(), mix = a.truth();
+    at::Tensor r[3];
+    r[0] = a.rows(1, sox, true), r[1] = a.rows(1, sog, true);
+    ScanArguments s;
+    s.packed = packed;
+    if (!a.ok() || (mix && !x.defined()) || !s.read(h, seqlens) || !like(x, h) || !like(dh, h) || !gate_type_ok(g, h) || !like(r[0], h) || !like(r[1], g) ||
+        !has(state, {s.n_seq, s.D}, at::kFloat) || !has(dstate, {s.n_seq, s.D}, at::kFloat))
+        return none();
+    a.narrow(s.n_seq), a.narrow(s.D);
+    const uint32_t flags = (uint32_t)logit | (uint32_t)mix << 1;
+    if (!a.ok() || !unlocked([&] {
+            at::Tensor ws;
+            int64_t bytes = 0;
+            if (!s.prepare(h, a.stream(), ws, bytes)) return false;
+            make_rows(r[0], h, sox, s.D), make_rows(r[1], g, sog, s.D);
+            if (state.defined()) r[2] = at::empty(state.sizes(), state.options());
+            const auto p = [&](int i) { return const_cast<void*>(opt(r[i])); };
+            const void* const from = mix ? opt(x) : nullptr;
+            void* const w = const_cast<void*>(opt(ws));
+            const int type = code_of(h.scalar_type()), g_type = code_of(g.scalar_type());
+            return (packed ? mixer.scan_bwd_varlen(from, g.data_ptr(), h.data_ptr(), opt(state), dh.data_ptr(), opt(dstate), p(0), p(1), p(2), w, bytes, s.cu.data_ptr<int64_t>(), (int)s.n_seq, s.N,
+                                                   (int)s.D, mix ? sx : 0, sg, sh, sd, sox, sog, type, g_type, flags, a.stream())
+                           : mixer.scan_bwd(from, g.data_ptr(), h.data_ptr(), opt(state), dh.data_ptr(), opt(dstate), p(0), p(1), p(2), w, bytes, (int)s.n_seq, s.T, (int)s.D, mix ? sx : 0, sg, sh,
+                                            sd, sox, sog, type, g_type, flags, a.stream())) == 0;
+        }))
+        return none();
+    PyObject* t = keep_offsets(keep_offsets(tuple_of(r), 0, s.cu), 1, s.cu);
+    return r[2].defined() ? keep_offsets(t, 2, s.cu) : t;
+}
+PyObject* scan_bwd(PyObject*, PyObject* const* v, Py_ssize_t n) { return scan_bwd_call(v, n, false); }
+PyObject* scan_bwd_varlen(PyObject*, PyObject* const* v, Py_ssize_t n) { return scan_bwd_call(v, n, true); }
+
+// (device, stream, x, g, state, slots, logit, mix, h): h
+PyObject* scan_step(PyObject*, PyObject* const* v, Py_ssize_t n)
+{
+    Args a(v, n, 9);
+    a.device_and_stream();
+    int64_t sx = 0, sg = 0, sh = 0;
+    const at::Tensor x = a.rows(1, sx), g = a.rows(1, sg), state = a.tensor(2), slots = a.places();
+    const bool logit = a.truth(), mix = a.truth();
+    at::Tensor h = a.rows(1, sh, true);
+    if (!a.ok() || x.dim() != 2 || !x.numel() || !state.numel() || !gate_type_ok(g, x) || !like(h, x)) return none();
+    const int64_t B = x.size(0), D = x.size(1);
+    if (!has(state, {state.size(0), D}, at::kFloat) || !has(slots, {B}, at::kInt) || (a.narrow(B), a.narrow(D), !a.ok())) return none();
+    if (!unlocked([&] {
+            make_rows(h, x, sh, D);
+            return mixer.scan_step(x.data_ptr(), g.data_ptr(), state.data_ptr(), opt(slots), h.data_ptr(), (int)B, state.size(0), (int)D, sx, sg, sh, code_of(x.scalar_type()),
+                                   code_of(g.scalar_type()), (uint32_t)logit | (uint32_t)mix << 1, a.stream()) == 0;
+        }))
+        return none();
+    return THPVariable_Wrap(h);
+}
+
+// connect_mixer(addresses): the C-ABI functions in the order of MixerAbi
+PyObject* connect_mixer(PyObject*, PyObject* const* v, Py_ssize_t n)
+{
+    constexpr int N = sizeof(MixerAbi) / sizeof(void*);
+    void* p[N] = {};
+    if (n != N) return PyErr_SetString(PyExc_TypeError, "nine addresses"), nullptr;
+    for (int i = 0; i < N; ++i) {
+        p[i] = PyLong_AsVoidPtr(v[i]);
+        if (!p[i]) return PyErr_Occurred() ? nullptr : (PyErr_SetString(PyExc_ValueError, "null address"), nullptr);
+    }
+    std::memcpy(&mixer, p, sizeof mixer);
+    Py_RETURN_NONE;
+}
+
 // connect_layer(addresses): the C-ABI functions in the order of LayerAbi
 PyObject* connect_layer(PyObject*, PyObject* const* v, Py_ssize_t n)
 {
@@ -662,7 +950,9 @@ template <PyObject* (*f)(PyObject*, PyObject* const*, Py_ssize_t)> PyObject* gua
 PyMethodDef methods[] = {TRIINV_METHOD(connect), TRIINV_METHOD(tri_inv), TRIINV_METHOD(gdn_inv), TRIINV_METHOD(gdn_solve),
                          TRIINV_METHOD(gdn_inv_varlen), TRIINV_METHOD(gdn_solve_varlen),
                          TRIINV_METHOD(connect_layer), TRIINV_METHOD(chunk_attn), TRIINV_METHOD(chunk_attn_varlen), TRIINV_METHOD(chunk_attn_bwd),
-                         TRIINV_METHOD(chunk_attn_bwd_varlen), TRIINV_METHOD(step), TRIINV_METHOD(norm), TRIINV_METHOD(norm_bwd), {nullptr, nullptr, 0, nullptr}};
+                         TRIINV_METHOD(chunk_attn_bwd_varlen), TRIINV_METHOD(step), TRIINV_METHOD(norm), TRIINV_METHOD(norm_bwd),
+                         TRIINV_METHOD(connect_mixer), TRIINV_METHOD(heads), TRIINV_METHOD(heads_bwd), TRIINV_METHOD(scan), TRIINV_METHOD(scan_varlen), TRIINV_METHOD(scan_bwd),
+                         TRIINV_METHOD(scan_bwd_varlen), TRIINV_METHOD(scan_step), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -20,14 +20,37 @@ HEADS_UNIT, HEADS_INTERLEAVED, HEADS_POS64 = 1, 2, 4
 SCAN_LOGIT, SCAN_MIX = 1, 2
 
 
+_connected = None  # the native argument handling that knows these entry points
+
+
+def _fast(t: torch.Tensor, stream):
+    """(native argument handling, device, stream) for a plain call on the current stream, or None (see binding.py)."""
+    global _connected
+    if binding._lib is not binding._fast_lib or stream is not None or not t.is_cuda:
+        return None
+    if binding._fast is not _connected:
+        L = binding.lib()
+        binding._fast.connect_mixer(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+            L.qk_norm_rope, L.qk_norm_rope_bwd, L.qk_norm_rope_bwd_workspace, L.gated_scan, L.gated_scan_varlen, L.gated_scan_workspace, L.gated_scan_bwd, L.gated_scan_bwd_varlen,
+            L.gated_scan_step)))
+        _connected = binding._fast
+    dev = binding._device_index()
+    return binding._fast, dev, binding._raw_stream(dev)
+
+
+def _address(t: torch.Tensor, name: str) -> int:
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live in device memory")
+    return t.data_ptr()
+
+
 def _rows(t: Optional[torch.Tensor], name: str, inner: int, shape=None, dtype=None):
     """(address, elements from a token to the next) of a tensor whose last `inner` dimensions are a token's."""
     if t is None:
         return None, 0
     if shape is not None:
         _has(t, name, shape, dtype)
-    if not t.is_cuda:
-        raise ValueError(f"{name} must live in device memory")
+    address = _address(t, name)
     sizes, strides = t.shape, t.stride()
     width = 1
     for n, s in zip(reversed(sizes[len(sizes) - inner:]), reversed(strides[len(sizes) - inner:])):
@@ -43,7 +66,7 @@ def _rows(t: Optional[torch.Tensor], name: str, inner: int, shape=None, dtype=No
         elif s != span:
             raise ValueError(f"{name}: tokens must stand one stride apart")
         span = s * n
-    return t.data_ptr(), step
+    return address, step
 
 
 def _one_device(*tensors) -> None:
@@ -91,6 +114,11 @@ def qk_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], q_weight: Optional[
     """(q_out, k_out): the heads of q [..., H, d] and k [..., H_k, d] (or None) over sqrt(mean(x^2) + eps), or with unit over sqrt(sum(x^2) + eps), times their
     weight [d], their first 2 len(inv_freq) elements rotated by the angles positions [...] (int32 or int64) times inv_freq (fp32): pairs (i, i + rot / 2), or
     interleaved (2 i, 2 i + 1).  q and k may be columns of a projection; q_out and k_out (q and k themselves too) likewise."""
+    f = _fast(q, stream)
+    if f:
+        r = f[0].heads(f[1], f[2], q, k, q_weight, k_weight, positions, inv_freq, unit, interleaved, eps, q_out, k_out)
+        if r is not None:
+            return r
     _one_device(q, k, q_weight, k_weight, positions, inv_freq, q_out, k_out)
     lead, N, H, H_k, d, rot = _heads_checked(q, k, q_weight, k_weight, positions, inv_freq)
     (pq, sq), (pk, sk) = _rows(q, "q", 2), _rows(k, "k", 2)
@@ -110,6 +138,11 @@ def qk_norm_rope_bwd(dq_out: torch.Tensor, dk_out: Optional[torch.Tensor], q: to
                      interleaved: bool = False, eps: float = 1e-6, dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None, stream=None):
     """(dq, dk, dq_weight, dk_weight) of qk_norm_rope, from its inputs and the gradients of its results; the weights' are fp32, None in the place of the gradient of
     what was not given.  dq and dk may be columns of a wider tensor (a projection's gradient), or dq_out and dk_out themselves."""
+    f = _fast(q, stream)
+    if f:
+        r = f[0].heads_bwd(f[1], f[2], dq_out, dk_out, q, k, q_weight, k_weight, positions, inv_freq, unit, interleaved, eps, dq, dk)
+        if r is not None:
+            return r
     _one_device(q, k, q_weight, k_weight, positions, inv_freq, dq_out, dk_out, dq, dk)
     lead, N, H, H_k, d, rot = _heads_checked(q, k, q_weight, k_weight, positions, inv_freq)
     if (k is None) != (dk_out is None):
@@ -178,6 +211,11 @@ def gated_scan(x: torch.Tensor, g: torch.Tensor, state: Optional[torch.Tensor] =
                final_state: Optional[torch.Tensor] = None, stream=None):
     """(h, final_state) of the gated recurrence h_t = a_t h_(t-1) + b_t over x, g [B, Tlen, D]: a = e^g, or with logit sigmoid(g); b = x, or with mix (1 - a) x.
     g is of x's type or fp32.  state: [B, D] fp32, the state before the first token (None: zeros)."""
+    f = _fast(x, stream)
+    if f:
+        r = f[0].scan(f[1], f[2], x, g, state, logit, mix, h, final_state)
+        if r is not None:
+            return r
     _one_device(x, g, state, h, final_state)
     if x.dim() != 3:
         raise ValueError(f"x must be [B, Tlen, D], not {list(x.shape)}")
@@ -188,6 +226,11 @@ def gated_scan(x: torch.Tensor, g: torch.Tensor, state: Optional[torch.Tensor] =
 def gated_scan_varlen(x: torch.Tensor, g: torch.Tensor, seqlens, state: Optional[torch.Tensor] = None, logit: bool = False, mix: bool = False,
                       h: Optional[torch.Tensor] = None, final_state: Optional[torch.Tensor] = None, stream=None):
     """gated_scan on packed sequences: x, g [total, D]; seqlens = host sequence of lengths; states [len(seqlens), D]."""
+    f = _fast(x, stream)
+    if f:
+        r = f[0].scan_varlen(f[1], f[2], x, g, seqlens, state, logit, mix, h, final_state)
+        if r is not None:
+            return r
     _one_device(x, g, state, h, final_state)
     if x.dim() != 2:
         raise ValueError(f"x must be [total, D], not {list(x.shape)}")
@@ -226,6 +269,11 @@ def gated_scan_bwd(x: Optional[torch.Tensor], g: torch.Tensor, h: torch.Tensor, 
                    logit: bool = False, mix: bool = False, dx: Optional[torch.Tensor] = None, dg: Optional[torch.Tensor] = None, stream=None):
     """(dx, dg, dstate0) of gated_scan, from its inputs, h as it returned it and the gradients dh of h and dstate (or None) of final_state; dstate0 is None where no
     state was given.  x may be None without mix.  dx and dg may be columns of a wider tensor (a projection's gradient)."""
+    f = _fast(h, stream)
+    if f:
+        r = f[0].scan_bwd(f[1], f[2], x, g, h, dh, state, dstate, logit, mix, dx, dg)
+        if r is not None:
+            return r
     _one_device(x, g, h, dh, state, dstate, dx, dg)
     if h.dim() != 3:
         raise ValueError(f"h must be [B, Tlen, D], not {list(h.shape)}")
@@ -237,6 +285,11 @@ def gated_scan_bwd_varlen(x: Optional[torch.Tensor], g: torch.Tensor, h: torch.T
                           dstate: Optional[torch.Tensor] = None, logit: bool = False, mix: bool = False, dx: Optional[torch.Tensor] = None, dg: Optional[torch.Tensor] = None,
                           stream=None):
     """gated_scan_bwd on packed sequences (see gated_scan_varlen)."""
+    f = _fast(h, stream)
+    if f:
+        r = f[0].scan_bwd_varlen(f[1], f[2], x, g, h, dh, seqlens, state, dstate, logit, mix, dx, dg)
+        if r is not None:
+            return r
     _one_device(x, g, h, dh, state, dstate, dx, dg)
     if h.dim() != 2:
         raise ValueError(f"h must be [total, D], not {list(h.shape)}")
@@ -254,6 +307,11 @@ def gated_scan_step(x: torch.Tensor, g: torch.Tensor, state: torch.Tensor, slots
                     h: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """One token of gated_scan: x, g [B, D]; state [n_slot, D] fp32 is updated in place; the new states' values in x's type are returned.  slots [B] int32: each
     sequence's place in state (outside of it: padding)."""
+    f = _fast(x, stream)
+    if f:
+        r = f[0].scan_step(f[1], f[2], x, g, state, slots, logit, mix, h)
+        if r is not None:
+            return r
     _one_device(x, g, state, slots, h)
     if x.dim() != 2 or state.dim() != 2:
         raise ValueError(f"x must be [B, D] and state [n_slot, D], not {list(x.shape)} and {list(state.shape)}")
