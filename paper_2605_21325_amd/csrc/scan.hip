@@ -41,12 +41,14 @@ template <int T, bool LOGIT, bool REST> __device__ __forceinline__ Gate gate(flo
     if constexpr (!LOGIT) {
         const float a = exp_of<T>(g);
         return {a, REST ? one_less_exp(g, a) : 0.f};
-    } else {  // 1 / (1 + e) and e / (1 + e), e = e^-|g|: both with all their bits
+    } else {
+        // s = e / (1 + e), e = e^-|g|, with all its bits, and 1 - s, which has one rounding: a decay near 1 is a factor of thousands of tokens (as 1 / (1 + e) from the
+        // approximate reciprocal it left the state behind 6000 tokens 2e-6 off, so it is 4e-7).
         const float e = exp_of<T>(-fabsf(g)), d = 1.f + e;
         float r = __builtin_amdgcn_rcpf(d);
         if constexpr (T == OP_F32) r = fmaf(fmaf(-d, r, 1.f), r, r);
-        const float s = e * r;
-        return g >= 0.f ? Gate{r, s} : Gate{s, r};
+        const float s = e * r, most = 1.f - s;
+        return g >= 0.f ? Gate{most, s} : Gate{s, most};
     }
 }
 
@@ -335,18 +337,19 @@ template <class F> int types(int dtype, int g_dtype, bool logit, bool mix, F f)
 // Segments of a sequence, by the tokens, sequences and channels of the call: so many that one to four rounds of the 256 compute units are full, whichever costs least with
 // the first launch's reading, AGAIN of the whole's, counted for all segments but one.  In us, one segment / about 256 / 512 / 1024 workgroups (bf16, logits and
 // mix, 4096 tokens of 2048 channels): 1 sequence (32 workgroups) - / 24 / 22 / 24, 3 (96) 91 / 78 / 69 / 60, 4 (128) - / 81 / 80 / -, 5 94 / 94 / 100 / 101, 6 97 / 97 / 131 /
-// 118; gradient 1 164 / 38 / 41 / 43, 3 170 / 121 / 109 / 103, 4 302 / 124 / 126 / 131, 5 177 / 178 / 166 / 180, 6 180 / 180 / 219 / 212.  Sequences of fewer than four
-// tiles are walked through as they are: 512 tokens 11.7 in one, 13.5 in two, 1024 20 and 14.
+// 118; gradient 1 164 / 38 / 41 / 43, 3 170 / 121 / 109 / 103, 4 302 / 124 / 126 / 131, 5 177 / 178 / 166 / 180, 6 180 / 180 / 219 / 212.  One round, which has a workgroup a
+// compute unit and leaves room for a second one, is counted a tenth dearer forward.  Sequences of fewer than three tiles are walked through as they are: 512 tokens (2 tiles) 11.7 in
+// one, 13.5 in two, 1024 (4) 20 and 14; gradient of 333 in fp32 (3) 15.3 and 12.8.
 int segments(int64_t N, int n_seq, int D, int tile, bool back)
 {
     const double AGAIN = back ? 0.45 : 0.67;
     const int64_t units = (int64_t)n_seq * ((D + CHANNELS - 1) / CHANNELS), tiles = (N / n_seq + tile - 1) / tile;
-    if (units >= 256 || tiles < 4) return 1;
+    if (units >= 256 || tiles < 3) return 1;
     int64_t best = 1;
     double least = 1;
     for (int rounds = 1; rounds <= 4; ++rounds) {
         const int64_t n = 256 * rounds / units < tiles ? 256 * rounds / units : tiles;
-        const double cost = (double)rounds / n * (1 + AGAIN * (n - 1) / n);
+        const double cost = (double)rounds / n * (1 + AGAIN * (n - 1) / n) * (rounds == 1 && !back ? 1.1 : 1);
         if (cost < least) best = n, least = cost;
     }
     return (int)best;
