@@ -57,9 +57,9 @@ constexpr int CHANNELS = 64, STRIPS = 16;
 template <int DT, int GT, bool BACK> constexpr int TOKENS = !BACK && DT != OP_F32 && GT != OP_F32 ? 16 : 8;
 
 struct ScanPlan {
-    int n_seg, groups;  // segments of a sequence; groups of channels
+    int n_seg, fine, groups;  // segments of a sequence; parts of a segment; groups of channels
     bool neighbours;    // on one XCD
-    v2f* part;          // [n_seq][n_seg][D]: a segment's decay and what it brings; in the last one's place the initial state as it was (n_seg > 1)
+    v2f* part;          // [n_seq][n_seg fine][D]: a part's decay and what it brings; in the last one's place the initial state as it was (n_seg > 1)
 };
 
 // Sequence s: its tokens t0 to t0 + len - 1.
@@ -127,8 +127,8 @@ template <int DT, int GT, bool MIX, bool BACK, int VEC, bool ONLY> struct Raw {
 //   1  a strip forms the decay of its tokens and what they bring, from registers, and asks for its tokens of the next tile;
 //   2  these go through LDS, and every strip puts together the state before its tokens from those before it;
 //   3  from there it goes through its tokens, in registers still; where the last one ends the next tile begins.
-// Where sequences and channels are too few for the card a sequence is cut into segments of whole tiles: a first launch (ONLY) writes what each segment but the last brings,
-// the second begins a segment with the state that those before it leave.
+// Where sequences and channels are too few for the card a sequence is cut into segments of whole tiles: a first launch (ONLY) writes what each segment but the last brings, in
+// parts, so many that they fill the card too; the second begins a segment with the state that those before it leave.
 template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC, bool ONLY> __global__ __launch_bounds__(STRIPS * CHANNELS / VEC) void k_scan(ScanCall a, ScanPlan p)
 {
     constexpr bool REST = MIX || (BACK && LOGIT);
@@ -138,15 +138,17 @@ template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC, bool ONLY> _
     __shared__ float base[2][CHANNELS];
     const int strip = threadIdx.x / LANES, i_c = threadIdx.x % LANES * VEC;
     int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
-    const int64_t blocks = (int64_t)a.n_seq * p.n_seg * p.groups;
+    const int parts = p.n_seg * p.fine, units = ONLY ? parts : p.n_seg;  // of a sequence
+    const int64_t blocks = (int64_t)a.n_seq * units * p.groups;
     if (block >= blocks) return;
     if (p.neighbours) {  // workgroups go to the eight XCDs in turn
         const int64_t x = block & 7, most = blocks & 7;
         block = x * (blocks >> 3) + (x < most ? x : most) + (block >> 3);
     }
-    const int unit = (int)(block / p.groups), group = (int)(block - (int64_t)unit * p.groups), s = unit / p.n_seg, seg = unit - s * p.n_seg;
+    const int unit = (int)(block / p.groups), group = (int)(block - (int64_t)unit * p.groups), s = unit / units, part = unit - s * units, seg = ONLY ? part / p.fine : part;
     const Sequence q = sequence(a, s);
-    const int tiles = (int)((q.len + TILE - 1) / TILE), per = (tiles + p.n_seg - 1) / p.n_seg, j0 = seg * per, j1 = j0 + per < tiles ? j0 + per : tiles;
+    const int tiles = (int)((q.len + TILE - 1) / TILE), per = (tiles + p.n_seg - 1) / p.n_seg, end = seg * per + per < tiles ? seg * per + per : tiles;
+    const int step = ONLY ? (per + p.fine - 1) / p.fine : per, j0 = ONLY ? seg * per + (part - seg * p.fine) * step : seg * per, j1 = j0 + step < end ? j0 + step : end;
     const bool in = group * CHANNELS + i_c < a.D;
     const int c = in ? group * CHANNELS + i_c : a.D - VEC;  // (lanes without a channel read another one's)
     const int64_t at_state = (int64_t)s * a.D + c;
@@ -154,20 +156,24 @@ template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC, bool ONLY> _
     float C[VEC];
     const auto initial = [&] {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) C[e] = p.part && !ONLY ? p.part[((int64_t)(s + 1) * p.n_seg - 1) * a.D + c + e][1] : init ? init[at_state + e] : 0.f;
+        for (int e = 0; e < VEC; ++e) C[e] = p.part && !ONLY ? p.part[((int64_t)(s + 1) * parts - 1) * a.D + c + e][1] : init ? init[at_state + e] : 0.f;
     };
     const auto put_last = [&] {
         if (!a.last) return;
 #pragma unroll
         for (int e = 0; e < VEC; ++e) a.last[at_state + e] = C[e];
     };
-    if (ONLY && seg == 0 && strip == 0) {
+    if (ONLY && part == 0 && strip == 0) {
         initial();
 #pragma unroll
         for (int e = 0; e < VEC; ++e)
-            if (in) p.part[((int64_t)(s + 1) * p.n_seg - 1) * a.D + c + e] = v2f{0.f, C[e]};
+            if (in) p.part[((int64_t)(s + 1) * parts - 1) * a.D + c + e] = v2f{0.f, C[e]};
     }
-    if (j0 >= j1 || (ONLY && j1 == tiles)) {  // nothing to do; a sequence without tokens keeps its state
+    if (ONLY && end < tiles && j0 >= j1 && strip == 0 && in) {  // a part of no tiles
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) p.part[((int64_t)s * parts + part) * a.D + c + e] = v2f{1.f, 0.f};
+    }
+    if (j0 >= j1 || (ONLY && end == tiles)) {  // nothing to do; a sequence without tokens keeps its state
         if (!ONLY && seg == 0 && q.len == 0 && strip == 0 && in) initial(), put_last();
         return;
     }
@@ -175,13 +181,13 @@ template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC, bool ONLY> _
     next.load(a, q, (int64_t)j0 * TILE, strip, c);
     v2f all[VEC];  // ONLY: of the segment so far
     if (strip == 0) {  // (read before anything is written: the final state may go to the same place)
-        if (seg == 0) initial();
+        if (part == 0) initial();
         if (!ONLY && seg > 0) {
-            const v2f* const from = p.part + (int64_t)s * p.n_seg * a.D + c;
+            const v2f* const from = p.part + (int64_t)s * parts * a.D + c;
 #pragma unroll
             for (int e = 0; e < VEC; ++e) C[e] = from[e][1];
 #pragma unroll 4
-            for (int k = 1; k < seg; ++k)
+            for (int k = 1; k < seg * p.fine; ++k)
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
                     const v2f w = from[(int64_t)k * a.D + e];
@@ -190,7 +196,7 @@ template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC, bool ONLY> _
         }
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-            all[e] = v2f{1.f, ONLY && seg == 0 ? C[e] : 0.f};
+            all[e] = v2f{1.f, ONLY && part == 0 ? C[e] : 0.f};
             base[j0 & 1][i_c + e] = C[e];
         }
     }
@@ -291,7 +297,7 @@ template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC, bool ONLY> _
     }
     if (ONLY && strip == 0 && in) {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) p.part[((int64_t)s * p.n_seg + seg) * a.D + c + e] = all[e];
+        for (int e = 0; e < VEC; ++e) p.part[((int64_t)s * parts + part) * a.D + c + e] = all[e];
     }
 }
 
@@ -355,6 +361,14 @@ int segments(int64_t N, int n_seq, int D, int tile, bool back)
     return (int)best;
 }
 
+// Parts of a segment: three workgroups a compute unit in the first launch.  (Gradient of 4 sequences of 4096 tokens of 2048 channels, two segments: 30 us of 128 were the first launch's
+// when it had one part a segment, on half of the compute units.)
+int parts_of(int64_t N, int n_seq, int D, int tile, int n_seg)
+{
+    const int64_t units = (int64_t)n_seq * ((D + CHANNELS - 1) / CHANNELS) * (n_seg - 1), per = ((N / n_seq + tile - 1) / tile + n_seg - 1) / n_seg, n = 768 / units;
+    return (int)(n < 1 ? 1 : n < per ? n : per);
+}
+
 template <bool BACK> struct Scan {
     const ScanCall& a;
     template <int DT, int GT, bool LOGIT, bool MIX, int VEC> int with() const
@@ -363,11 +377,11 @@ template <bool BACK> struct Scan {
         // Neighbouring groups of channels share cache lines where rows do not begin on one: these are put on one XCD.  48 packed sequences of 1100 tokens of 1000 channels,
         // fp16, 138 us as they come, 114 so; 16 of 2048 tokens of 4096 channels, where there is nothing to share, 194 and 223.
         const bool share = (a.x_stride * Elems<DT, 1>::SIZE | a.g_stride * Elems<GT, 1>::SIZE | a.out_stride * Elems<DT, 1>::SIZE) % 128 != 0;
-        ScanPlan p{n_seg, (a.D + CHANNELS - 1) / CHANNELS, share, nullptr};
+        ScanPlan p{n_seg, n_seg > 1 ? parts_of(a.N, a.n_seq, a.D, TOKENS<DT, GT, BACK> * STRIPS, n_seg) : 1, (a.D + CHANNELS - 1) / CHANNELS, share, nullptr};
         const dim3 grid = long_grid((int64_t)a.n_seq * n_seg * p.groups), block(STRIPS * CHANNELS / VEC);
         if (n_seg > 1) {
             p.part = reinterpret_cast<v2f*>(a.workspace);
-            const int rc = launch_kernel(false, k_scan<DT, GT, LOGIT, MIX, BACK, VEC, true>, grid, block, 0, a.stream, a, p);
+            const int rc = launch_kernel(false, k_scan<DT, GT, LOGIT, MIX, BACK, VEC, true>, long_grid((int64_t)a.n_seq * n_seg * p.fine * p.groups), block, 0, a.stream, a, p);
             if (rc != LAUNCHED) return rc;
         }
         return launch_kernel(false, k_scan<DT, GT, LOGIT, MIX, BACK, VEC, false>, grid, block, 0, a.stream, a, p);
@@ -403,11 +417,14 @@ struct Step {
 
 int64_t scan_workspace(int64_t N, int n_seq, int D)
 {
-    int most = 1;  // (of either direction and every type)
-    for (const int n : {segments(N, n_seq, D, TOKENS<OP_BF16, OP_BF16, false> * STRIPS, false), segments(N, n_seq, D, TOKENS<OP_F32, OP_F32, false> * STRIPS, false),
-                        segments(N, n_seq, D, TOKENS<OP_F32, OP_F32, true> * STRIPS, true)})
-        most = n > most ? n : most;
-    return most > 1 ? (int64_t)8 * n_seq * most * D : 0;
+    int64_t most = 0;  // (of either direction and every type)
+    const auto count = [&](int tile, bool back) {
+        const int n = segments(N, n_seq, D, tile, back);
+        const int64_t parts = n > 1 ? (int64_t)n * parts_of(N, n_seq, D, tile, n) : 0;
+        most = parts > most ? parts : most;
+    };
+    count(TOKENS<OP_BF16, OP_BF16, false> * STRIPS, false), count(TOKENS<OP_F32, OP_F32, false> * STRIPS, false), count(TOKENS<OP_F32, OP_F32, true> * STRIPS, true);
+    return 8 * n_seq * most * D;
 }
 int launch_scan(const ScanCall& a) { return types(a.dtype, a.g_dtype, a.logit, a.mix, Scan<false>{a}); }
 int launch_scan_bwd(const ScanCall& a) { return types(a.dtype, a.g_dtype, a.logit, a.mix, Scan<true>{a}); }
