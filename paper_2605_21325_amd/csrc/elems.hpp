@@ -32,6 +32,28 @@ template <int DT, int VEC> struct Elems {
             w[0] = *reinterpret_cast<const uint16_t*>(from);
         }
     }
+    // From a buffer, `lane` bytes (of the lane) and `row` (of all of them) behind its beginning; nothing where `lane` is beyond the buffer's end: zeros.  Up to 8 bytes.
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t from, uint32_t lane, uint32_t row)
+    {
+        if constexpr (BYTES == 8) {
+            const v2u x = __builtin_bit_cast(v2u, __builtin_amdgcn_raw_buffer_load_b64(from, lane, row, 0));
+            w[0] = x[0], w[1] = x[1];
+        } else if constexpr (BYTES == 4) {
+            w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_raw_buffer_load_b32(from, lane, row, 0));
+        } else {
+            static_assert(BYTES == 2);
+            w[0] = __builtin_bit_cast(uint16_t, __builtin_amdgcn_raw_buffer_load_b16(from, lane, row, 0));
+        }
+    }
+    __device__ __forceinline__ void store(__amdgpu_buffer_rsrc_t to, uint32_t lane, uint32_t row) const
+    {
+        if constexpr (BYTES == 8)
+            __builtin_amdgcn_raw_buffer_store_b64(v2u{w[0], w[1]}, to, lane, row, 0);
+        else if constexpr (BYTES == 4)
+            __builtin_amdgcn_raw_buffer_store_b32(w[0], to, lane, row, 0);
+        else
+            __builtin_amdgcn_raw_buffer_store_b16((uint16_t)w[0], to, lane, row, 0);
+    }
     __device__ __forceinline__ float operator[](int e) const
     {
         if constexpr (DT == OP_F32) return __builtin_bit_cast(float, w[e]);

@@ -7,7 +7,7 @@ namespace {
 
 using namespace triinv;
 
-constexpr int64_t MOST_STRIDE = 1LL << 26;  // elements from token to token: eight tokens of fp32 stay below 2^31 bytes
+constexpr int64_t MOST_STRIDE = 1LL << 24;  // elements from token to token: a wavefront's rows stay below 2^31 bytes
 
 uint64_t size_of(int dtype) { return dtype == TRIINV_F32 ? 4 : 2; }
 bool strides_ok(std::initializer_list<int64_t> strides)

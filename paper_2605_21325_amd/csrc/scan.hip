@@ -11,8 +11,8 @@ namespace triinv {
 
 namespace {
 
-// e^x, off by an ulp or two: 2^y with what the product y = x log2(e) lacks put right.  x in 16 bits: the factor is cut so that the product is exact.
-template <int T> __device__ __forceinline__ float exp_of(float x)
+// e^x, off by an ulp or two: 2^y with what the product y = x log2(e) lacks put right.  x in 16 bits: the factor is cut so that the product is exact.  BELOW: x <= 0.
+template <int T, bool BELOW = false> __device__ __forceinline__ float exp_of(float x)
 {
     if constexpr (T == OP_F32) {
         constexpr float LOG2E = 1.44269502f, LOW = 1.925963e-8f, LN2 = 0.693147182f;  // log2(e) in two parts
@@ -22,6 +22,7 @@ template <int T> __device__ __forceinline__ float exp_of(float x)
         // 13 bits of it for the 11 of an fp16 number, 15 for the 8 of a bf16 number; what they leave of log2(e), times ln 2
         constexpr float CUT = T == OP_F16 ? 0x1.715p0f : 0x1.7154p0f, LEFT = T == OP_F16 ? 4.7194842e-5f : 4.8884952e-6f;
         const float e = __builtin_amdgcn_exp2f(x * CUT);
+        if constexpr (BELOW) return fmaf(-e, __builtin_amdgcn_fmed3f(-x * LEFT, 0.f, 1.f), e);  // (one instruction less: its result clamped)
         return fmaf(e, __builtin_amdgcn_fmed3f(x * LEFT, -1.f, 1.f), e);
     }
 }
@@ -44,7 +45,7 @@ template <int T, bool LOGIT, bool REST> __device__ __forceinline__ Gate gate(flo
     } else {
         // s = e / (1 + e), e = e^-|g|, with all its bits, and 1 - s, which has one rounding: a decay near 1 is a factor of thousands of tokens (as 1 / (1 + e) from the
         // approximate reciprocal it left the state behind 6000 tokens 2e-6 off, so it is 4e-7).
-        const float e = exp_of<T>(-fabsf(g)), d = 1.f + e;
+        const float e = exp_of<T, true>(-fabsf(g)), d = 1.f + e;
         float r = __builtin_amdgcn_rcpf(d);
         if constexpr (T == OP_F32) r = fmaf(fmaf(-d, r, 1.f), r, r);
         const float s = e * r, most = 1.f - s;
@@ -79,47 +80,71 @@ template <int VEC> __device__ __forceinline__ void load_state(const float* from,
     for (int e = 0; e < VEC; ++e) x[e] = from ? from[i + e] : 0.f;
 }
 
-// Rows of a strip's tokens as they are in memory.
+// Rows of a tensor for a wavefront's tokens, as a buffer from the first of them (in memory) on: a lane's place in it is an offset of 32 bits, a token's row another one of all lanes
+// (8 x 8192 tokens of 2048 channels took 198 us with a 64-bit product for each row and lane, 178 with a sum).  OUT in a lane's place: nothing is read or written.
+constexpr uint32_t OUT = 0x80000000u;
+template <int T, int TOK, bool BACK> struct RowsOf {
+    static constexpr int SIZE = Elems<T, 1>::SIZE;
+    __amdgpu_buffer_rsrc_t buffer;
+    uint32_t lane, stride;
+    __device__ __forceinline__ RowsOf(const void* p, int64_t first, int64_t s, uint32_t row, int c, bool in)
+        : buffer(__builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(p)) + first * s * SIZE, 0, OUT, 0x00020000)), lane(in ? (row * (uint32_t)s + (uint32_t)c) * SIZE : OUT),
+          stride((uint32_t)s * SIZE)
+    {
+    }
+    __device__ __forceinline__ uint32_t row(int i) const { return (BACK ? TOK - 1 - i : i) * stride; }
+    template <int VEC> __device__ __forceinline__ void load(Elems<T, VEC>& to, int i, bool there) const { to.load(buffer, there ? lane : OUT, row(i)); }
+    template <int VEC> __device__ __forceinline__ void store(const float (&x)[VEC], int i, bool there) const
+    {
+        Elems<T, VEC> e;
+        e.set(x);
+        e.store(buffer, there ? lane : OUT, row(i));
+    }
+};
+// Where a strip is: its wavefront's first token in the order of the run and first row in memory, its own first row behind that.
+template <int TOK, int PER_WAVE, bool BACK> struct Strip {
+    int64_t k0, first;
+    uint32_t row;
+    int left;   // tokens from its first one on, counted up to one more than it has (may be negative)
+    bool full;  // the wavefront's tokens are all there, and others behind them
+    __device__ __forceinline__ Strip(const Sequence& q, int64_t i0, int strip)
+    {
+        const int r = strip % PER_WAVE;
+        k0 = i0 + __builtin_amdgcn_readfirstlane(strip - r) * TOK;
+        first = BACK ? q.t0 + q.len - k0 - PER_WAVE * TOK : q.t0 + k0;
+        row = (BACK ? PER_WAVE - 1 - r : r) * TOK;
+        full = k0 + PER_WAVE * TOK < q.len;
+        const int64_t n = q.len - k0 - r * TOK;
+        left = n > TOK ? TOK + 1 : (int)n;
+    }
+};
+
+// A strip's rows as they are in memory.
 template <int DT, int GT, bool MIX, bool BACK, int VEC, bool ONLY> struct Raw {
-    static constexpr int TOK = TOKENS<DT, GT, BACK>, TILE = TOK * STRIPS;
+    static constexpr int TOK = TOKENS<DT, GT, BACK>, PER_WAVE = 64 * VEC / CHANNELS;
     static constexpr bool X = BACK ? MIX && !ONLY : true, H = BACK && !ONLY;
     Elems<DT, VEC> x[X ? TOK : 1], d[BACK ? TOK : 1], h[H ? TOK : 1];
     Elems<GT, VEC> g[TOK];
-    // The tile's tokens are all there: rows one after the other from `row` on, a wavefront's first (the gradient's: last) one; a lane's offset in bytes.
-    template <int T> static __device__ __forceinline__ void at(Elems<T, VEC>& to, const void* p, int64_t row, int64_t stride, uint32_t lane)
+    template <bool FULL> __device__ __forceinline__ void load(const ScanCall& a, const Strip<TOK, PER_WAVE, BACK>& at, int c, bool in)
     {
-        to.load(static_cast<const char*>(p) + row * stride * Elems<T, VEC>::SIZE + lane, 0);
-    }
-    __device__ __forceinline__ void load(const ScanCall& a, const Sequence& q, int64_t i0, int strip, int c)
-    {
-        if (i0 + TILE <= q.len) {
-            constexpr int PER_WAVE = 64 * VEC / CHANNELS;  // strips of a wavefront
-            const int64_t k0 = i0 + __builtin_amdgcn_readfirstlane(strip / PER_WAVE * PER_WAVE) * TOK;  // the wavefront's first token
-            const uint32_t row = (BACK ? PER_WAVE - 1 - strip % PER_WAVE : strip % PER_WAVE) * TOK;
-            const auto lane = [&](int64_t stride, int size) { return (row * (uint32_t)stride + (uint32_t)c) * size; };
-            const uint32_t lx = lane(a.x_stride, Elems<DT, 1>::SIZE), lg = lane(a.g_stride, Elems<GT, 1>::SIZE), ld = lane(a.dh_stride, Elems<DT, 1>::SIZE), lh = lane(a.h_stride, Elems<DT, 1>::SIZE);
+        const RowsOf<DT, TOK, BACK> of_x(a.x, at.first, a.x_stride, at.row, c, in), of_d(a.dh, at.first, a.dh_stride, at.row, c, in), of_h(a.h, at.first - 1, a.h_stride, at.row, c, in);
+        const RowsOf<GT, TOK, BACK> of_g(a.g, at.first, a.g_stride, at.row, c, in);
 #pragma unroll
-            for (int i = 0; i < TOK; ++i) {
-                const int64_t t = BACK ? q.t0 + q.len - 1 - (k0 + i) - (PER_WAVE - 1) * TOK : q.t0 + k0 + i;
-                if constexpr (X) at(x[i], a.x, t, a.x_stride, lx);
-                at(g[i], a.g, t, a.g_stride, lg);
-                if constexpr (BACK) at(d[i], a.dh, t, a.dh_stride, ld);
-                if constexpr (H) {
-                    // (before the first token of all there is no row: its own is read instead, and not used)
-                    const bool none = i0 + TILE == q.len && i == TOK - 1 && q.t0 == 0 && strip == STRIPS - 1;
-                    at(h[i], a.h, t - 1, a.h_stride, lh + (none ? (uint32_t)a.h_stride * Elems<DT, 1>::SIZE : 0u));
-                }
-            }
-        } else {  // rows that are not there are replaced by the sequence's last
-#pragma unroll
-            for (int i = 0; i < TOK; ++i) {
-                const int64_t k1 = i0 + strip * TOK + i, k = k1 < q.len ? k1 : q.len - 1, t = BACK ? q.t0 + q.len - 1 - k : q.t0 + k;
-                if constexpr (X) x[i].load(a.x, t * a.x_stride + c);
-                g[i].load(a.g, t * a.g_stride + c);
-                if constexpr (BACK) d[i].load(a.dh, t * a.dh_stride + c);
-                if constexpr (H) h[i].load(a.h, (t > q.t0 ? t - 1 : t) * a.h_stride + c);
-            }
+        for (int i = 0; i < TOK; ++i) {
+            const bool there = FULL || i < at.left;
+            if constexpr (X) of_x.load(x[i], i, there);
+            of_g.load(g[i], i, there);
+            if constexpr (BACK) of_d.load(d[i], i, there);
+            if constexpr (H) of_h.load(h[i], i, FULL || i + 1 < at.left);
         }
+    }
+    __device__ __forceinline__ void load(const ScanCall& a, const Sequence& q, int64_t i0, int strip, int c, bool in)
+    {
+        const Strip<TOK, PER_WAVE, BACK> at(q, i0, strip);
+        if (at.full)
+            load<true>(a, at, c, in);
+        else
+            load<false>(a, at, c, in);
     }
 };
 
@@ -158,7 +183,7 @@ template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC, bool ONLY> _
 #pragma unroll
         for (int e = 0; e < VEC; ++e) C[e] = p.part && !ONLY ? p.part[((int64_t)(s + 1) * parts - 1) * a.D + c + e][1] : init ? init[at_state + e] : 0.f;
     };
-    const auto put_last = [&] {
+    const auto put_last = [&] {  // (of lanes with a channel)
         if (!a.last) return;
 #pragma unroll
         for (int e = 0; e < VEC; ++e) a.last[at_state + e] = C[e];
@@ -178,7 +203,7 @@ template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC, bool ONLY> _
         return;
     }
     Raw<DT, GT, MIX, BACK, VEC, ONLY> next;
-    next.load(a, q, (int64_t)j0 * TILE, strip, c);
+    next.load(a, q, (int64_t)j0 * TILE, strip, c, in);
     v2f all[VEC];  // ONLY: of the segment so far
     if (strip == 0) {  // (read before anything is written: the final state may go to the same place)
         if (part == 0) initial();
@@ -203,10 +228,8 @@ template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC, bool ONLY> _
     for (int j = j0; j < j1; ++j) {
         auto now = next;
         const int64_t i0 = (int64_t)j * TILE;
-        const bool full = i0 + TILE <= q.len;
-        const int64_t left = q.len - i0 - strip * TOK;
-        const int n = full || left > TOK ? TOK : (int)left;  // (may be negative)
-        float da[TOK][VEC], db[TOK][VEC];                    // decays; what a token brings (gradient: one less the decay)
+        const Strip<TOK, PER_WAVE, BACK> at(q, i0, strip);
+        float da[TOK][VEC], db[TOK][VEC];  // decays; what a token brings (gradient: one less the decay)
         float A[VEC], H[VEC];
 #pragma unroll
         for (int e = 0; e < VEC; ++e) A[e] = 1.f, H[e] = 0.f;
@@ -225,15 +248,15 @@ template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC, bool ONLY> _
                 A[e] *= f.a;
             }
         };
-        if (full) {
+        if (at.full) {
 #pragma unroll
             for (int i = 0; i < TOK; ++i) form(i);
         } else {
 #pragma unroll
             for (int i = 0; i < TOK; ++i)
-                if (i < n) form(i);
+                if (i < at.left) form(i);
         }
-        if (j + 1 < j1) next.load(a, q, i0 + TILE, strip, c);
+        if (j + 1 < j1) next.load(a, q, i0 + TILE, strip, c, in);
         float (*const mine)[CHANNELS][2] = own[j & 1];
 #pragma unroll
         for (int e = 0; e < VEC; ++e) mine[strip][i_c + e][0] = A[e], mine[strip][i_c + e][1] = H[e];
@@ -251,16 +274,29 @@ template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC, bool ONLY> _
             const int first = strip / PER_WAVE * PER_WAVE;  // the wavefront's first strip
 #pragma unroll
             for (int e = 0; e < VEC; ++e) C[e] = base[j & 1][i_c + e];
-            for (int w = 0; w < __builtin_amdgcn_readfirstlane(first); ++w)
+            const int before = __builtin_amdgcn_readfirstlane(first);
+#pragma unroll 1
+            for (int w = 0; w < before; w += 2) {  // two at a time are asked for together (four leave no room for a second workgroup: 64 sequences of 100 tokens 34 us, so 23)
+                float d[2][VEC], b[2][VEC];
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) C[e] = fmaf(mine[w][i_c + e][0], C[e], mine[w][i_c + e][1]);
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) d[i][e] = mine[w + i][i_c + e][0], b[i][e] = mine[w + i][i_c + e][1];
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if (w + i < before) {
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) C[e] = fmaf(d[i][e], C[e], b[i][e]);
+                    }
+            }
             if (PER_WAVE > 1 && strip != first) {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) C[e] = fmaf(mine[first][i_c + e][0], C[e], mine[first][i_c + e][1]);
             }
         }
+        const RowsOf<DT, TOK, BACK> out(a.out, at.first, a.out_stride, at.row, c, in);
+        const RowsOf<GT, TOK, BACK> out_g(a.dg, at.first, a.dg_stride, at.row, c, in);
         const auto go = [&](int i, bool last) {
-            const int64_t k = i0 + strip * TOK + i, t = BACK ? q.t0 + q.len - 1 - k : q.t0 + k;
             if constexpr (BACK) {
                 float dx[VEC], dg[VEC], past[VEC];
 #pragma unroll
@@ -273,22 +309,22 @@ template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC, bool ONLY> _
                     dg[e] = r * (MIX ? past[e] - now.x[i][e] : past[e]) * (LOGIT ? da[i][e] * db[i][e] : da[i][e]);
                     C[e] = da[i][e] * r;
                 }
-                if (in) store_rounded<DT, VEC>(a.out, t * a.out_stride + c, dx);
-                if (in) store_rounded<GT, VEC>(a.dg, t * a.dg_stride + c, dg);
+                out.template store<VEC>(dx, i, true);
+                out_g.template store<VEC>(dg, i, true);
             } else {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) C[e] = fmaf(da[i][e], C[e], db[i][e]);
-                if (in) store_rounded<DT, VEC>(a.out, t * a.out_stride + c, C);
+                out.template store<VEC>(C, i, true);
             }
             if (last && in) put_last();
         };
-        if (i0 + TILE < q.len) {
+        if (at.full) {
 #pragma unroll
             for (int i = 0; i < TOK; ++i) go(i, false);
         } else {
 #pragma unroll
             for (int i = 0; i < TOK; ++i)
-                if (i < n) go(i, i0 + strip * TOK + i + 1 == q.len);
+                if (i < at.left) go(i, i + 1 == at.left);
         }
         if (strip == STRIPS - 1) {
 #pragma unroll

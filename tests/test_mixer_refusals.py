@@ -59,7 +59,7 @@ SCAN = dict(x=address(0), g=address(1), state=address(2), h=address(3), final=ad
 @pytest.mark.parametrize("change,status", [
     (dict(B=0), BAD_SHAPE), (dict(T=-1), BAD_SHAPE), (dict(T=1 << 31), BAD_SHAPE), (dict(B=1 << 20, T=1 << 12), BAD_SHAPE), (dict(B=1 << 30, T=0, D=128), UNSUPPORTED), (dict(D=0), BAD_SHAPE), (dict(D=(1 << 20) + 1), BAD_SHAPE),
     (dict(dtype=4), BAD_DTYPE), (dict(gtype=tri.F16), BAD_DTYPE), (dict(dtype=tri.F32, gtype=tri.BF16), BAD_DTYPE), (dict(flags=4), BAD_METHOD), (dict(xs=-1), BAD_SHAPE),
-    (dict(hs=99), BAD_SHAPE), (dict(gs=1 << 40), BAD_SHAPE), (dict(x=None), NULL), (dict(g=None), NULL), (dict(h=None), NULL), (dict(x=address(0) + 1), ALIGN), (dict(g=address(1) + 2), ALIGN),
+    (dict(hs=99), BAD_SHAPE), (dict(gs=(1 << 24) + 1), BAD_SHAPE), (dict(x=None), NULL), (dict(g=None), NULL), (dict(h=None), NULL), (dict(x=address(0) + 1), ALIGN), (dict(g=address(1) + 2), ALIGN),
     (dict(state=address(2) + 2), ALIGN), (dict(ws=address(5) + 8), ALIGN), (dict(h=address(0)), ALIAS), (dict(h=address(1) + 8), ALIAS), (dict(final=address(0)), ALIAS), (dict(final=address(2) + 4), ALIAS),
     (dict(final=address(3)), ALIAS), (dict(state=address(3), final=address(3)), ALIAS)])
 def test_scan(L, change, status):
