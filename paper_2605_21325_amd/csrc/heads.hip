@@ -78,37 +78,28 @@ template <int VEC, int ROT> __device__ __forceinline__ Slot slot_of(int s, int d
     const int rest = pieces - 2 * first, half = (rest + 1) / 2, r = s - first, i = 2 * first + r;
     return {{i * VEC, (i + half) * VEC}, {r < half, r < half && r + half < rest}, false};
 }
-// cos and sin for the pairs of a slot.
-template <int VEC, int ROT> struct Turn {
-    float c[ROT == STILL ? 1 : VEC], s[ROT == STILL ? 1 : VEC];
-    // From the wavefront's angle `first` on, the token's first one.
-    __device__ __forceinline__ void load(const Angles& at, int wave, int first, const Slot& p, int rot, int slot)
-    {
+// The slot's elements turned by the angles of its token, which are the wavefront's from `first` on; WAY = -1: back.  What is not turned stays as it is (beside an infinity too).
+template <int WAY> __device__ __forceinline__ void turn_pair(float& a, float& b, float c, float s)
+{
+    const float t = a;
+    a = t * c - b * (WAY * s), b = b * c + t * (WAY * s);
+}
+template <int WAY, int VEC, int ROT, class Lds> __device__ __forceinline__ void turn(float (&x)[2][VEC], const Lds& at, int wave, int first, const Slot& p, int rot, int slot)
+{
+    if constexpr (ROT == HALVES) {
+        if (!p.turned) return;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            if constexpr (ROT == HALVES) {
-                c[e] = p.turned ? at.c[wave][first + slot * VEC + e] : 1.f, s[e] = p.turned ? at.s[wave][first + slot * VEC + e] : 0.f;
-            } else if constexpr (ROT == NEIGHBOURS) {
-                const int i = p.i[e / (VEC / 2)] / 2 + e % (VEC / 2);
-                const bool on = p.there[e / (VEC / 2)] && 2 * i < rot;
-                c[e] = on ? at.c[wave][first + i] : 1.f, s[e] = on ? at.s[wave][first + i] : 0.f;
-            }
+        for (int e = 0; e < VEC; ++e) turn_pair<WAY>(x[0][e], x[1][e], at.c[wave][first + slot * VEC + e], at.s[wave][first + slot * VEC + e]);
+    } else if constexpr (ROT == NEIGHBOURS) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            if (!p.there[j] || p.i[j] >= rot) continue;
+#pragma unroll
+            for (int e = 0; e < VEC / 2; ++e)
+                if (p.i[j] + 2 * e < rot) turn_pair<WAY>(x[j][2 * e], x[j][2 * e + 1], at.c[wave][first + p.i[j] / 2 + e], at.s[wave][first + p.i[j] / 2 + e]);
         }
     }
-    // The slot's elements turned; WAY = -1: back.  What is not turned stays as it is (an infinity beside it too).
-    template <int WAY> __device__ __forceinline__ void turn(float (&x)[2][VEC]) const
-    {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            if constexpr (ROT == STILL) continue;
-            float& a = ROT == HALVES ? x[0][e] : x[e / (VEC / 2 ? VEC / 2 : 1)][2 * (e % (VEC / 2 ? VEC / 2 : 1))];
-            float& b = ROT == HALVES ? x[1][e] : x[e / (VEC / 2 ? VEC / 2 : 1)][2 * (e % (VEC / 2 ? VEC / 2 : 1)) + 1 < VEC ? 2 * (e % (VEC / 2 ? VEC / 2 : 1)) + 1 : 0];
-            const float t = a, sn = WAY * s[e];
-            const bool on = s[e] != 0.f || c[e] != 1.f;
-            a = on ? t * c[e] - b * sn : t, b = on ? b * c[e] + t * sn : b;
-        }
-    }
-};
+}
 
 // Queries and keys are taken by workgroups of their own.  What a wavefront has at a time, a unit: `tokens` tokens with few heads, or a part of one token's heads (parts of `per`).
 // Their heads are counted on: row k of the unit is head k mod H of its token k / H.
@@ -222,11 +213,7 @@ template <int DT, int VEC, int G, int SLOTS, int ROT> __global__ __launch_bounds
                     for (int e = 0; e < VEC; ++e) x[i][j][e] *= norm;
                     if (weight) weigh<DT, VEC>(x[i][j], lds, slots[i].there[j] ? slots[i].i[j] : 0);
                 }
-                if constexpr (ROT != STILL) {
-                    Turn<VEC, ROT> turn;
-                    turn.load(angles, wave, token * (a.rot / 2), slots[i], a.rot, lane % G + G * i);
-                    turn.template turn<1>(x[i]);
-                }
+                if constexpr (ROT != STILL) turn<1, VEC, ROT>(x[i], angles, wave, token * (a.rot / 2), slots[i], a.rot, lane % G + G * i);
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
                     if (slots[i].there[j]) store_rounded<DT, VEC>(to + (row + (uint32_t)slots[i].i[j]) * Elems<DT, 1>::SIZE, 0, x[i][j]);
@@ -293,20 +280,16 @@ template <int DT, int VEC, int G, int SLOTS, int ROT, bool WEIGHT> __global__ __
             if (k0 + SIDE < u0.end) request(k + SIDE);
             if constexpr (ROT != STILL) {
 #pragma unroll
-                for (int i = 0; i < SLOTS; ++i) {
-                    Turn<VEC, ROT> turn;
-                    turn.load(angles, wave, (on ? token : 0) * (a.rot / 2), slots[i], a.rot, lane % G + G * i);
-                    turn.template turn<-1>(z[i]);
-                }
+                for (int i = 0; i < SLOTS; ++i) turn<-1, VEC, ROT>(z[i], angles, wave, (on ? token : 0) * (a.rot / 2), slots[i], a.rot, lane % G + G * i);
             }
-            const float sum = lanes_sum<G>(sq), norm = 1.f / sqrtf((a.unit ? sum : sum / (float)a.d) + a.eps);
+            const float sum = lanes_sum<G>(sq), norm = 1.f / sqrtf((a.unit ? sum : sum / (float)a.d) + a.eps), counted = on ? norm : 0.f;
 #pragma unroll
             for (int i = 0; i < SLOTS; ++i)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     if constexpr (WEIGHT) {
 #pragma unroll
-                        for (int e = 0; e < VEC; ++e) dw[i][j][e] += on ? z[i][j][e] * (x[i][j][e] * norm) : 0.f;
+                        for (int e = 0; e < VEC; ++e) dw[i][j][e] += z[i][j][e] * (x[i][j][e] * counted);
                     }
                     if (weight) weigh<DT, VEC>(z[i][j], lds, slots[i].there[j] ? slots[i].i[j] : 0);
 #pragma unroll
