@@ -46,7 +46,7 @@ __device__ __forceinline__ unsigned xcd_neighbours(unsigned b, unsigned n)
 // 16 heads 16 (512) 73 / 77, 24 111 / 105, 32 (1024) 132 / 144, 64 262 / 270; to 600, 2 heads, 128 (512) 58 / 52, 160 72 / 70, 250 (1000) 100 / 113.  Equal lengths, which gain
 // nothing: 48 of 4 heads and 500 tokens 59 / 61, 128 128 / 140, 256 254 / 301.
 constexpr int LENGTHS_SORTED = 128;  // sequences at most
-__device__ __forceinline__ bool by_length(const SeqMap& m, unsigned n) { return m.cu_seqlens && n > 256u && n <= 768u && m.n_seq <= LENGTHS_SORTED; }
+__host__ __device__ __forceinline__ bool by_length(const SeqMap& m, unsigned n) { return m.cu_seqlens && n > 256u && n <= 768u && m.n_seq <= LENGTHS_SORTED; }
 struct SeqUnit {
     int seq;
     unsigned unit;

@@ -4,7 +4,9 @@
 // behind a token that comes from the tokens after it:
 //     r_t = dh_t + R;   dx = r or r (1 - a);   dg = r (h_(t-1) - [mix] x) a [or a (1 - a)];   R <- a_t r_t
 // and the initial state's gradient is the last R.  h is read as it was written.
+#include <algorithm>
 #include "layer.hpp"
+#include "attn_ops.hpp"
 #include "elems.hpp"
 
 namespace triinv {
@@ -60,6 +62,7 @@ template <int DT, int GT, bool BACK> constexpr int TOKENS = !BACK && DT != OP_F3
 struct ScanPlan {
     int n_seg, fine, groups;  // segments of a sequence; parts of a segment; groups of channels
     bool neighbours;    // on one XCD
+    bool longest_first;  // packed sequences, one segment each
     v2f* part;          // [n_seq][n_seg fine][D]: a part's decay and what it brings; in the last one's place the initial state as it was (n_seg > 1)
 };
 
@@ -170,7 +173,12 @@ template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC, bool ONLY> _
         const int64_t x = block & 7, most = blocks & 7;
         block = x * (blocks >> 3) + (x < most ? x : most) + (block >> 3);
     }
-    const int unit = (int)(block / p.groups), group = (int)(block - (int64_t)unit * p.groups), s = unit / units, part = unit - s * units, seg = ONLY ? part / p.fine : part;
+    int unit = (int)(block / p.groups), group = (int)(block - (int64_t)unit * p.groups);
+    if (!ONLY && p.longest_first) {
+        const SeqUnit of = seq_unit(SeqMap{a.cu_seqlens, nullptr, 0, a.n_seq}, (unsigned)block, (unsigned)blocks, (unsigned)p.groups, true, reinterpret_cast<char*>(own));
+        unit = of.seq, group = (int)of.unit;
+    }
+    const int s = unit / units, part = unit - s * units, seg = ONLY ? part / p.fine : part;
     const Sequence q = sequence(a, s);
     const int tiles = (int)((q.len + TILE - 1) / TILE), per = (tiles + p.n_seg - 1) / p.n_seg, end = seg * per + per < tiles ? seg * per + per : tiles;
     const int step = ONLY ? (per + p.fine - 1) / p.fine : per, j0 = ONLY ? seg * per + (part - seg * p.fine) * step : seg * per, j1 = j0 + step < end ? j0 + step : end;
@@ -413,7 +421,11 @@ template <bool BACK> struct Scan {
         // Neighbouring groups of channels share cache lines where rows do not begin on one: these are put on one XCD.  48 packed sequences of 1100 tokens of 1000 channels,
         // fp16, 138 us as they come, 114 so; 16 of 2048 tokens of 4096 channels, where there is nothing to share, 194 and 223.
         const bool share = (a.x_stride * Elems<DT, 1>::SIZE | a.g_stride * Elems<GT, 1>::SIZE | a.out_stride * Elems<DT, 1>::SIZE) % 128 != 0;
-        ScanPlan p{n_seg, n_seg > 1 ? parts_of(a.N, a.n_seq, a.D, TOKENS<DT, GT, BACK> * STRIPS, n_seg) : 1, (a.D + CHANNELS - 1) / CHANNELS, share, nullptr};
+        ScanPlan p{n_seg, n_seg > 1 ? parts_of(a.N, a.n_seq, a.D, TOKENS<DT, GT, BACK> * STRIPS, n_seg) : 1, (a.D + CHANNELS - 1) / CHANNELS, share, false, nullptr};
+        // Packed sequences of different lengths begin with the longest, each on one XCD and the next on the next, where the chunk attention's do.  In us, order of the call / by length: 48
+        // of 1000 channels to 2199 tokens 111 / 106, 24 of 2048 to 3000 126 / 115, 20 of 1024 to 4000 85 / 73; gradient of 20 of 2048 to 2000 141 / 130; equal lengths 104 / 104.
+        p.longest_first = n_seg == 1 && by_length(SeqMap{a.cu_seqlens, nullptr, 0, a.n_seq}, (unsigned)std::min<int64_t>((int64_t)a.n_seq * p.groups, 1 << 20));
+        p.neighbours = share && !p.longest_first;
         const dim3 grid = long_grid((int64_t)a.n_seq * n_seg * p.groups), block(STRIPS * CHANNELS / VEC);
         if (n_seg > 1) {
             p.part = reinterpret_cast<v2f*>(a.workspace);
