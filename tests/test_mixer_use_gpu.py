@@ -99,6 +99,17 @@ def test_sequences_in_segments(lens, D, dtype, gtype, logit, mix):
     assert torch.equal(again, got[0]) and torch.equal(state, got[1])
 
 
+@pytest.mark.parametrize("lens,D,dtype,gtype,logit,mix", [
+    ([(37 * i) % 50 * 7 for i in range(24)], 1000, BF, BF, True, True), ([(11 * i) % 17 for i in range(100)], 256, HF, F, False, False), ([5] * 127 + [300], 320, F, F, True, False),
+    ([i % 3 for i in range(1000)], 64, BF, F, False, True), ([0] * 20 + [130] + [0] * 20 + [1], 1024, BF, BF, True, True)])
+def test_many_packed_sequences(lens, D, dtype, gtype, logit, mix):
+    """Where the longest begin, and beyond."""
+    v, up = make_scan(lens, D, dtype, gtype, logit)
+    got = tri.gated_scan_varlen(**v, seqlens=lens, logit=logit, mix=mix)
+    check_scan(lens, v, got, logit, mix)
+    check_scan_bwd(lens, v, got[0], up, tri.gated_scan_bwd_varlen(v["x"], v["g"], got[0], up["dh"], lens, v["state"], up["dstate"], logit=logit, mix=mix), logit, mix)
+
+
 @pytest.mark.parametrize("N,H,Hk,d,rot,inter,dtype", [(4200, 2, 1, 64, 16, False, BF), (6001, 1, 1, 32, 8, True, HF), (4100, 3, 2, 128, 0, False, F), (9000, 1, 0, 16, 0, False, BF), (2100, 5, 1, 96, 0, True, BF)])
 def test_several_tokens_to_a_wavefront(N, H, Hk, d, rot, inter, dtype):
     x, up = make_heads(N, H, Hk, d, rot, True, dtype)
