@@ -19,13 +19,14 @@ template <int T, bool BELOW = false> __device__ __forceinline__ float exp_of(flo
     if constexpr (T == OP_F32) {
         constexpr float LOG2E = 1.44269502f, LOW = 1.925963e-8f, LN2 = 0.693147182f;  // log2(e) in two parts
         const float y = x * LOG2E, rest = (fmaf(x, LOG2E, -y) + x * LOW) * LN2, e = __builtin_amdgcn_exp2f(y);
-        return fmaf(e, __builtin_amdgcn_fmed3f(rest, -1.f, 1.f), e);  // (where x is infinite the rest is none)
+        // (where x is infinite the rest is none; where e is, what the rest takes away is not)
+        return fmaf(BELOW ? e : fminf(e, 3.402823466e38f), __builtin_amdgcn_fmed3f(rest, -1.f, 1.f), e);
     } else {
         // 13 bits of it for the 11 of an fp16 number, 15 for the 8 of a bf16 number; what they leave of log2(e), times ln 2
         constexpr float CUT = T == OP_F16 ? 0x1.715p0f : 0x1.7154p0f, LEFT = T == OP_F16 ? 4.7194842e-5f : 4.8884952e-6f;
-        const float e = __builtin_amdgcn_exp2f(x * CUT);
-        if constexpr (BELOW) return fmaf(-e, __builtin_amdgcn_fmed3f(-x * LEFT, 0.f, 1.f), e);  // (one instruction less: its result clamped)
-        return fmaf(e, __builtin_amdgcn_fmed3f(x * LEFT, -1.f, 1.f), e);
+        const float e = __builtin_amdgcn_exp2f(x * CUT), r = BELOW ? __builtin_amdgcn_fmed3f(-x * LEFT, 0.f, 1.f) : __builtin_amdgcn_fmed3f(x * LEFT, -1.f, 1.f);  // (BELOW: one instruction less, its result clamped)
+        const float t = T == OP_F16 ? fmaf((BELOW ? -0.5f : 0.5f) * r, r, r) : r;  // (of 88 LEFT the square is 150 halves of an ulp in fp16, 2 in bf16)
+        return fmaf(BELOW ? -e : e, t, e);
     }
 }
 // 1 - e^x.

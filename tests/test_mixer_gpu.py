@@ -351,6 +351,24 @@ def test_scan_decays_above_one():
     check_scan_bwd([40, 90], v, got[0], up, tri.gated_scan_bwd_varlen(v["x"], v["g"], got[0], up["dh"], [40, 90], v["state"], up["dstate"]), False, False)
 
 
+@pytest.mark.parametrize("dtype,gtype", [(F, F), (BF, F), (BF, BF), (HF, HF)])
+def test_scan_decays_beyond_the_range(dtype, gtype):
+    """e^g is infinite from 88.73 on, and a finite state becomes infinite by it, not NaN; what comes to nothing is nothing."""
+    g = torch.tensor([88.5, -88.5, -87, -60, -30, 45, 89.0, 89.25, 90, 91.5, 95, 100, 127, 300, 1000, 60000, float("inf"), -89, -105, -150, -60000, float("-inf")], device=DEV).to(gtype).view(1, 1, -1)
+    x = torch.zeros(g.shape, dtype=dtype, device=DEV)
+    _, last = tri.gated_scan(x, g, state=torch.ones(1, g.shape[-1], device=DEV))
+    got = exact(last)
+    with np.errstate(over="ignore"):
+        ref = np.exp(exact(g)).reshape(got.shape)
+        ref32 = ref.astype(np.float32).astype(np.float64)
+    assert (np.isinf(got) == np.isinf(ref32)).all()
+    finite = np.isfinite(ref32)
+    assert (np.abs(got[finite] - ref[finite]) <= 16 * E * ref[finite] + TINY[F]).all()
+    pool = torch.ones(1, g.shape[-1], device=DEV)
+    tri.gated_scan_step(x[0], g[0], pool)
+    assert torch.equal(pool, last)
+
+
 @pytest.mark.parametrize("T", [50, 900])
 def test_what_is_not_finite_stays_in_its_sequence_and_channel(T):
     v, _ = make_scan([T, T, T], 64, BF, BF, True)
