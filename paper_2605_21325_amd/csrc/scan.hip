@@ -56,8 +56,8 @@ template <int T, bool LOGIT, bool REST> __device__ __forceinline__ Gate gate(flo
     }
 }
 
-// Tokens of a strip (lanes that take VEC channels each, 64 together), strips of a workgroup, one after the other in time.
-constexpr int CHANNELS = 64, STRIPS = 16;
+// Tokens of a strip (lanes that take VEC channels each, CH together: 64, or where workgroups are many 128), strips of a workgroup, one after the other in time.
+constexpr int STRIPS = 16;
 template <int DT, int GT, bool BACK> constexpr int TOKENS = !BACK && DT != OP_F32 && GT != OP_F32 ? 16 : 8;
 
 struct ScanPlan {
@@ -124,8 +124,8 @@ template <int TOK, int PER_WAVE, bool BACK> struct Strip {
 };
 
 // A strip's rows as they are in memory.
-template <int DT, int GT, bool MIX, bool BACK, int VEC, bool ONLY> struct Raw {
-    static constexpr int TOK = TOKENS<DT, GT, BACK>, PER_WAVE = 64 * VEC / CHANNELS;
+template <int DT, int GT, bool MIX, bool BACK, int VEC, int CH, bool ONLY> struct Raw {
+    static constexpr int TOK = TOKENS<DT, GT, BACK>, PER_WAVE = 64 * VEC / CH;
     static constexpr bool X = BACK ? MIX && !ONLY : true, H = BACK && !ONLY;
     Elems<DT, VEC> x[X ? TOK : 1], d[BACK ? TOK : 1], h[H ? TOK : 1];
     Elems<GT, VEC> g[TOK];
@@ -152,19 +152,19 @@ template <int DT, int GT, bool MIX, bool BACK, int VEC, bool ONLY> struct Raw {
     }
 };
 
-// A workgroup takes 64 channels through a sequence, or through a segment of it, a tile of STRIPS times TOK tokens at a time (the gradient's runs from the last token to the first):
+// A workgroup takes CH channels through a sequence, or through a segment of it, a tile of STRIPS times TOK tokens at a time (the gradient's runs from the last token to the first):
 //   1  a strip forms the decay of its tokens and what they bring, from registers, and asks for its tokens of the next tile;
 //   2  these go through LDS, and every strip puts together the state before its tokens from those before it;
 //   3  from there it goes through its tokens, in registers still; where the last one ends the next tile begins.
 // Where sequences and channels are too few for the card a sequence is cut into segments of whole tiles: a first launch (ONLY) writes what each segment but the last brings, in
 // parts, so many that they fill the card too; the second begins a segment with the state that those before it leave.
-template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC, bool ONLY> __global__ __launch_bounds__(STRIPS * CHANNELS / VEC) void k_scan(ScanCall a, ScanPlan p)
+template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC, int CH, bool ONLY> __global__ __launch_bounds__(STRIPS * CH / VEC) void k_scan(ScanCall a, ScanPlan p)
 {
     constexpr bool REST = MIX || (BACK && LOGIT);
     constexpr int TOK = TOKENS<DT, GT, BACK>, TILE = TOK * STRIPS;
-    constexpr int LANES = CHANNELS / VEC, PER_WAVE = 64 / LANES;  // of a strip; strips of a wavefront
-    __shared__ float own[2][STRIPS][CHANNELS][2];  // of one tile and the next: one barrier a tile
-    __shared__ float base[2][CHANNELS];
+    constexpr int LANES = CH / VEC, PER_WAVE = 64 / LANES;  // of a strip; strips of a wavefront
+    __shared__ float own[2][STRIPS][CH][2];  // of one tile and the next: one barrier a tile
+    __shared__ float base[2][CH];
     const int strip = threadIdx.x / LANES, i_c = threadIdx.x % LANES * VEC;
     int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     const int parts = p.n_seg * p.fine, units = ONLY ? parts : p.n_seg;  // of a sequence
@@ -183,8 +183,8 @@ template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC, bool ONLY> _
     const Sequence q = sequence(a, s);
     const int tiles = (int)((q.len + TILE - 1) / TILE), per = (tiles + p.n_seg - 1) / p.n_seg, end = seg * per + per < tiles ? seg * per + per : tiles;
     const int step = ONLY ? (per + p.fine - 1) / p.fine : per, j0 = ONLY ? seg * per + (part - seg * p.fine) * step : seg * per, j1 = j0 + step < end ? j0 + step : end;
-    const bool in = group * CHANNELS + i_c < a.D;
-    const int c = in ? group * CHANNELS + i_c : a.D - VEC;  // (lanes without a channel read another one's)
+    const bool in = group * CH + i_c < a.D;
+    const int c = in ? group * CH + i_c : a.D - VEC;  // (lanes without a channel read another one's)
     const int64_t at_state = (int64_t)s * a.D + c;
     const float* const init = BACK ? a.dstate : a.state;
     float C[VEC];
@@ -211,7 +211,7 @@ template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC, bool ONLY> _
         if (!ONLY && seg == 0 && q.len == 0 && strip == 0 && in) initial(), put_last();
         return;
     }
-    Raw<DT, GT, MIX, BACK, VEC, ONLY> next;
+    Raw<DT, GT, MIX, BACK, VEC, CH, ONLY> next;
     next.load(a, q, (int64_t)j0 * TILE, strip, c, in);
     v2f all[VEC];  // ONLY: of the segment so far
     if (strip == 0) {  // (read before anything is written: the final state may go to the same place)
@@ -266,7 +266,7 @@ template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC, bool ONLY> _
                 if (i < at.left) form(i);
         }
         if (j + 1 < j1) next.load(a, q, i0 + TILE, strip, c, in);
-        float (*const mine)[CHANNELS][2] = own[j & 1];
+        float (*const mine)[CH][2] = own[j & 1];
 #pragma unroll
         for (int e = 0; e < VEC; ++e) mine[strip][i_c + e][0] = A[e], mine[strip][i_c + e][1] = H[e];
         __syncthreads();
@@ -394,7 +394,7 @@ template <class F> int types(int dtype, int g_dtype, bool logit, bool mix, F f)
 int segments(int64_t N, int n_seq, int D, int tile, bool back)
 {
     const double AGAIN = back ? 0.45 : 0.67;
-    const int64_t units = (int64_t)n_seq * ((D + CHANNELS - 1) / CHANNELS), tiles = (N / n_seq + tile - 1) / tile;
+    const int64_t units = (int64_t)n_seq * ((D + 63) / 64), tiles = (N / n_seq + tile - 1) / tile;
     if (units >= 256 || tiles < 3) return 1;
     int64_t best = 1;
     double least = 1;
@@ -410,39 +410,55 @@ int segments(int64_t N, int n_seq, int D, int tile, bool back)
 // when it had one part a segment, on half of the compute units.)
 int parts_of(int64_t N, int n_seq, int D, int tile, int n_seg)
 {
-    const int64_t units = (int64_t)n_seq * ((D + CHANNELS - 1) / CHANNELS) * (n_seg - 1), per = ((N / n_seq + tile - 1) / tile + n_seg - 1) / n_seg, n = 768 / units;
+    const int64_t units = (int64_t)n_seq * ((D + 63) / 64) * (n_seg - 1), per = ((N / n_seq + tile - 1) / tile + n_seg - 1) / n_seg, n = 768 / units;
     return (int)(n < 1 ? 1 : n < per ? n : per);
+}
+
+// Whether a workgroup takes 128 channels in place of 64, 256 bytes of a 16-bit row: where such workgroups, one to a compute unit, leave few of these without work in the last
+// round.  us with 64 / 128, bf16, logits and mix, sequences of 1500 tokens of 2048 channels: 12 (192 workgroups of 128) 58 / 48, 16 65 / 59, 20 (320) 94 / 98, 24 104 / 104, 32
+// 138 / 126, 48 203 / 184; gradient 114 / 101, 133 / 122, 176 / 190, 198 / 200, 266 / 244, 396 / 362; packed sequences to 1399 tokens, 200 of 1000 channels 218 / 198, 64 of 2048
+// 146 / 132.
+bool wide(int n_seq, int D)
+{
+    const int64_t n = (int64_t)n_seq * ((D + 127) / 128), last = n % 256;
+    return (D + 63) / 64 % 2 == 0 && n >= 192 && (last == 0 || last >= 128 || n > 1024);
 }
 
 template <bool BACK> struct Scan {
     const ScanCall& a;
-    template <int DT, int GT, bool LOGIT, bool MIX, int VEC> int with() const
+    template <int DT, int GT, bool LOGIT, bool MIX, int VEC, int CH> int with(int n_seg) const
     {
-        const int n_seg = segments(a.N, a.n_seq, a.D, TOKENS<DT, GT, BACK> * STRIPS, BACK);
+        const int groups = (a.D + CH - 1) / CH;
         // Neighbouring groups of channels share cache lines where rows do not begin on one: these are put on one XCD.  48 packed sequences of 1100 tokens of 1000 channels,
         // fp16, 138 us as they come, 114 so; 16 of 2048 tokens of 4096 channels, where there is nothing to share, 194 and 223.
         const bool share = (a.x_stride * Elems<DT, 1>::SIZE | a.g_stride * Elems<GT, 1>::SIZE | a.out_stride * Elems<DT, 1>::SIZE) % 128 != 0;
-        ScanPlan p{n_seg, n_seg > 1 ? parts_of(a.N, a.n_seq, a.D, TOKENS<DT, GT, BACK> * STRIPS, n_seg) : 1, (a.D + CHANNELS - 1) / CHANNELS, share, false, nullptr};
+        ScanPlan p{n_seg, n_seg > 1 ? parts_of(a.N, a.n_seq, a.D, TOKENS<DT, GT, BACK> * STRIPS, n_seg) : 1, groups, share, false, nullptr};
         // Packed sequences of different lengths begin with the longest, each on one XCD and the next on the next, where the chunk attention's do.  In us, order of the call / by length: 48
         // of 1000 channels to 2199 tokens 111 / 106, 24 of 2048 to 3000 126 / 115, 20 of 1024 to 4000 85 / 73; gradient of 20 of 2048 to 2000 141 / 130; equal lengths 104 / 104.
         p.longest_first = n_seg == 1 && by_length(SeqMap{a.cu_seqlens, nullptr, 0, a.n_seq}, (unsigned)std::min<int64_t>((int64_t)a.n_seq * p.groups, 1 << 20));
         p.neighbours = share && !p.longest_first;
-        const dim3 grid = long_grid((int64_t)a.n_seq * n_seg * p.groups), block(STRIPS * CHANNELS / VEC);
-        if (n_seg > 1) {
-            p.part = reinterpret_cast<v2f*>(a.workspace);
-            const int rc = launch_kernel(false, k_scan<DT, GT, LOGIT, MIX, BACK, VEC, true>, long_grid((int64_t)a.n_seq * n_seg * p.fine * p.groups), block, 0, a.stream, a, p);
-            if (rc != LAUNCHED) return rc;
+        const dim3 grid = long_grid((int64_t)a.n_seq * n_seg * p.groups), block(STRIPS * CH / VEC);
+        if constexpr (CH == 64) {
+            if (n_seg > 1) {
+                p.part = reinterpret_cast<v2f*>(a.workspace);
+                const int rc = launch_kernel(false, k_scan<DT, GT, LOGIT, MIX, BACK, VEC, CH, true>, long_grid((int64_t)a.n_seq * n_seg * p.fine * p.groups), block, 0, a.stream, a, p);
+                if (rc != LAUNCHED) return rc;
+            }
         }
-        return launch_kernel(false, k_scan<DT, GT, LOGIT, MIX, BACK, VEC, false>, grid, block, 0, a.stream, a, p);
+        return launch_kernel(false, k_scan<DT, GT, LOGIT, MIX, BACK, VEC, CH, false>, grid, block, 0, a.stream, a, p);
     }
     template <int DT, int GT, bool LOGIT, bool MIX> int go() const
     {
+        const int n_seg = segments(a.N, a.n_seq, a.D, TOKENS<DT, GT, BACK> * STRIPS, BACK);
         // Two channels a lane where every row's begin allows it.
         const auto even = [](const void* p, int64_t stride, int dtype) { return !p || (stride % 2 == 0 && reinterpret_cast<uintptr_t>(p) % (dtype == OP_F32 ? 8 : 4) == 0); };
         if (a.D % 2 == 0 && even(a.x, a.x_stride, DT) && even(a.g, a.g_stride, GT) && even(a.h, a.h_stride, DT) && even(a.dh, a.dh_stride, DT) && even(a.out, a.out_stride, DT) &&
-            even(a.dg, a.dg_stride, GT))
-            return with<DT, GT, LOGIT, MIX, 2>();
-        return with<DT, GT, LOGIT, MIX, 1>();
+            even(a.dg, a.dg_stride, GT)) {
+            if constexpr (!BACK || DT != OP_F32)  // (whose 128 registers a lane do not hold a strip of it)
+                if (n_seg == 1 && wide(a.n_seq, a.D)) return with<DT, GT, LOGIT, MIX, 2, 128>(1);
+            return with<DT, GT, LOGIT, MIX, 2, 64>(n_seg);
+        }
+        return with<DT, GT, LOGIT, MIX, 1, 64>(n_seg);
     }
 };
 struct Step {
