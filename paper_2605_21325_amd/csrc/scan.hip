@@ -57,7 +57,7 @@ template <int T, bool LOGIT, bool REST> __device__ __forceinline__ Gate gate(flo
 }
 
 // Tokens of a strip (lanes that take VEC channels each, CH together: 64, or where workgroups are many 128), strips of a workgroup, one after the other in time.
-constexpr int STRIPS = 16;
+constexpr int MOST_STRIPS = 16, SHORT = 64;  // (sequences of up to SHORT tokens: as many strips as hold them)
 template <int DT, int GT, bool BACK> constexpr int TOKENS = !BACK && DT != OP_F32 && GT != OP_F32 ? 16 : 8;
 
 struct ScanPlan {
@@ -158,7 +158,7 @@ template <int DT, int GT, bool MIX, bool BACK, int VEC, int CH, bool ONLY> struc
 //   3  from there it goes through its tokens, in registers still; where the last one ends the next tile begins.
 // Where sequences and channels are too few for the card a sequence is cut into segments of whole tiles: a first launch (ONLY) writes what each segment but the last brings, in
 // parts, so many that they fill the card too; the second begins a segment with the state that those before it leave.
-template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC, int CH, bool ONLY> __global__ __launch_bounds__(STRIPS * CH / VEC) void k_scan(ScanCall a, ScanPlan p)
+template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC, int CH, int STRIPS, bool ONLY> __global__ __launch_bounds__(STRIPS * CH / VEC) void k_scan(ScanCall a, ScanPlan p)
 {
     constexpr bool REST = MIX || (BACK && LOGIT);
     constexpr int TOK = TOKENS<DT, GT, BACK>, TILE = TOK * STRIPS;
@@ -426,7 +426,7 @@ bool wide(int n_seq, int D)
 
 template <bool BACK> struct Scan {
     const ScanCall& a;
-    template <int DT, int GT, bool LOGIT, bool MIX, int VEC, int CH> int with(int n_seg) const
+    template <int DT, int GT, bool LOGIT, bool MIX, int VEC, int CH, int STRIPS> int with(int n_seg) const
     {
         const int groups = (a.D + CH - 1) / CH;
         // Neighbouring groups of channels share cache lines where rows do not begin on one: these are put on one XCD.  48 packed sequences of 1100 tokens of 1000 channels,
@@ -441,24 +441,25 @@ template <bool BACK> struct Scan {
         if constexpr (CH == 64) {
             if (n_seg > 1) {
                 p.part = reinterpret_cast<v2f*>(a.workspace);
-                const int rc = launch_kernel(false, k_scan<DT, GT, LOGIT, MIX, BACK, VEC, CH, true>, long_grid((int64_t)a.n_seq * n_seg * p.fine * p.groups), block, 0, a.stream, a, p);
+                const int rc = launch_kernel(false, k_scan<DT, GT, LOGIT, MIX, BACK, VEC, CH, STRIPS, true>, long_grid((int64_t)a.n_seq * n_seg * p.fine * p.groups), block, 0, a.stream, a, p);
                 if (rc != LAUNCHED) return rc;
             }
         }
-        return launch_kernel(false, k_scan<DT, GT, LOGIT, MIX, BACK, VEC, CH, false>, grid, block, 0, a.stream, a, p);
+        return launch_kernel(false, k_scan<DT, GT, LOGIT, MIX, BACK, VEC, CH, STRIPS, false>, grid, block, 0, a.stream, a, p);
     }
     template <int DT, int GT, bool LOGIT, bool MIX> int go() const
     {
-        const int n_seg = segments(a.N, a.n_seq, a.D, TOKENS<DT, GT, BACK> * STRIPS, BACK);
+        const int n_seg = segments(a.N, a.n_seq, a.D, TOKENS<DT, GT, BACK> * MOST_STRIPS, BACK);
         // Two channels a lane where every row's begin allows it.
         const auto even = [](const void* p, int64_t stride, int dtype) { return !p || (stride % 2 == 0 && reinterpret_cast<uintptr_t>(p) % (dtype == OP_F32 ? 8 : 4) == 0); };
         if (a.D % 2 == 0 && even(a.x, a.x_stride, DT) && even(a.g, a.g_stride, GT) && even(a.h, a.h_stride, DT) && even(a.dh, a.dh_stride, DT) && even(a.out, a.out_stride, DT) &&
             even(a.dg, a.dg_stride, GT)) {
+            if (!a.cu_seqlens && a.Tlen <= SHORT) return with<DT, GT, LOGIT, MIX, 2, 128, SHORT / TOKENS<DT, GT, BACK>>(1);
             if constexpr (!BACK || DT != OP_F32)  // (whose 128 registers a lane do not hold a strip of it)
-                if (n_seg == 1 && wide(a.n_seq, a.D)) return with<DT, GT, LOGIT, MIX, 2, 128>(1);
-            return with<DT, GT, LOGIT, MIX, 2, 64>(n_seg);
+                if (n_seg == 1 && wide(a.n_seq, a.D)) return with<DT, GT, LOGIT, MIX, 2, 128, MOST_STRIPS>(1);
+            return with<DT, GT, LOGIT, MIX, 2, 64, MOST_STRIPS>(n_seg);
         }
-        return with<DT, GT, LOGIT, MIX, 1, 64>(n_seg);
+        return with<DT, GT, LOGIT, MIX, 1, 64, MOST_STRIPS>(n_seg);
     }
 };
 struct Step {
@@ -488,7 +489,7 @@ int64_t scan_workspace(int64_t N, int n_seq, int D)
         const int64_t parts = n > 1 ? (int64_t)n * parts_of(N, n_seq, D, tile, n) : 0;
         most = parts > most ? parts : most;
     };
-    count(TOKENS<OP_BF16, OP_BF16, false> * STRIPS, false), count(TOKENS<OP_F32, OP_F32, false> * STRIPS, false), count(TOKENS<OP_F32, OP_F32, true> * STRIPS, true);
+    count(TOKENS<OP_BF16, OP_BF16, false> * MOST_STRIPS, false), count(TOKENS<OP_F32, OP_F32, false> * MOST_STRIPS, false), count(TOKENS<OP_F32, OP_F32, true> * MOST_STRIPS, true);
     return 8 * n_seq * most * D;
 }
 int launch_scan(const ScanCall& a) { return types(a.dtype, a.g_dtype, a.logit, a.mix, Scan<false>{a}); }

@@ -312,7 +312,8 @@ def test_scan(case, joint):
     check_scan_bwd(lens, v, got[0], up, back, logit, mix)
 
 
-@pytest.mark.parametrize("B,T,D,dtype,gtype", [(1, 1, 2048, BF, BF), (3, 100, 96, BF, BF), (2, 64, 130, HF, F), (5, 0, 64, BF, BF), (70, 3, 40, F, F), (2, 900, 64, BF, F), (4, 256, 128, HF, HF)])
+@pytest.mark.parametrize("B,T,D,dtype,gtype", [(1, 1, 2048, BF, BF), (3, 100, 96, BF, BF), (2, 64, 130, HF, F), (5, 0, 64, BF, BF), (70, 3, 40, F, F), (2, 900, 64, BF, F), (4, 256, 128, HF, HF),
+                                              (40, 63, 512, BF, BF), (9, 33, 1000, HF, F), (300, 17, 256, BF, F), (7, 48, 66, F, F), (3, 65, 256, HF, HF)])
 @pytest.mark.parametrize("logit,mix", [(True, True), (True, False), (False, True), (False, False)])
 def test_scan_of_sequences_of_one_length(B, T, D, dtype, gtype, logit, mix):
     for state in (True, False):
