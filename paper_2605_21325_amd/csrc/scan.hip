@@ -57,7 +57,7 @@ template <int T, bool LOGIT, bool REST> __device__ __forceinline__ Gate gate(flo
 }
 
 // Tokens of a strip (lanes that take VEC channels each, CH together: 64, or where workgroups are many 128), strips of a workgroup, one after the other in time.
-constexpr int MOST_STRIPS = 16, SHORT = 64;  // (sequences of up to SHORT tokens: as many strips as hold them)
+constexpr int MOST_STRIPS = 16, SHORT = 64;  // SHORT: tokens of the fewest strips
 template <int DT, int GT, bool BACK> constexpr int TOKENS = !BACK && DT != OP_F32 && GT != OP_F32 ? 16 : 8;
 
 struct ScanPlan {
@@ -454,7 +454,10 @@ template <bool BACK> struct Scan {
         const auto even = [](const void* p, int64_t stride, int dtype) { return !p || (stride % 2 == 0 && reinterpret_cast<uintptr_t>(p) % (dtype == OP_F32 ? 8 : 4) == 0); };
         if (a.D % 2 == 0 && even(a.x, a.x_stride, DT) && even(a.g, a.g_stride, GT) && even(a.h, a.h_stride, DT) && even(a.dh, a.dh_stride, DT) && even(a.out, a.out_stride, DT) &&
             even(a.dg, a.dg_stride, GT)) {
-            if (!a.cu_seqlens && a.Tlen <= SHORT) return with<DT, GT, LOGIT, MIX, 2, 128, SHORT / TOKENS<DT, GT, BACK>>(1);
+            // Short sequences (packed: of half of SHORT in the mean) take as many strips as hold SHORT tokens: what counts is to begin and end workgroups.  In us, 16
+            // strips / so: 512 of 1024 channels of 1 token 63 / 13, 16 66 / 22, 64 71 / 38, packed of 20 in the mean 77 / 32; gradient of 16 74 / 43, packed 81 / 51.  (Packed of 60 86 / 49
+            // too, but one of 4000 among 63 of one token, 63 in the mean as well, 100 / 132.)
+            if (a.N <= (int64_t)a.n_seq * (a.cu_seqlens ? SHORT / 2 : SHORT)) return with<DT, GT, LOGIT, MIX, 2, 128, SHORT / TOKENS<DT, GT, BACK>>(1);
             if constexpr (!BACK || DT != OP_F32)  // (whose 128 registers a lane do not hold a strip of it)
                 if (n_seg == 1 && wide(a.n_seq, a.D)) return with<DT, GT, LOGIT, MIX, 2, 128, MOST_STRIPS>(1);
             return with<DT, GT, LOGIT, MIX, 2, 64, MOST_STRIPS>(n_seg);

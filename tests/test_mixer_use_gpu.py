@@ -103,7 +103,7 @@ def test_sequences_in_segments(lens, D, dtype, gtype, logit, mix):
     ([(37 * i) % 50 * 7 for i in range(24)], 1000, BF, BF, True, True), ([(11 * i) % 17 for i in range(100)], 256, HF, F, False, False), ([5] * 127 + [300], 320, F, F, True, False),
     ([i % 3 for i in range(1000)], 64, BF, F, False, True), ([0] * 20 + [130] + [0] * 20 + [1], 1024, BF, BF, True, True),
     ([(29 * i) % 300 for i in range(50)], 510, F, F, True, True), ([(29 * i) % 270 for i in range(52)], 512, HF, F, False, True), ([257] * 260, 66, HF, HF, True, False),
-    ([256, 255] * 130, 128, BF, BF, True, True)])
+    ([256, 255] * 130, 128, BF, BF, True, True), ([1] * 30 + [700] + [0] * 10 + [3], 512, BF, BF, True, True), ([1] * 30 + [700] + [0] * 10 + [3], 130, F, F, False, False)])
 def test_many_packed_sequences(lens, D, dtype, gtype, logit, mix):
     """Where the longest begin, and beyond."""
     v, up = make_scan(lens, D, dtype, gtype, logit)
