@@ -394,7 +394,7 @@ int add_rms_norm_bwd(const void* dy, const void* s, const void* weight, const vo
  *   q_weight, k_weight  device, [d], the same type, or NULL for ones.
  *   positions           device, int32 [N] (TRIINV_HEADS_POS64: int64, up to 2^53 in magnitude); NULL with rot = 0.
  *   inv_freq            device, fp32 [rot / 2], radians a position; NULL with rot = 0.  The angle is their exact product without its whole turns.
- *   d  1 to 512.   rot  even, 0 (no rotation) to d.   N (H + H_k) < 2^31.   Strides up to 2^24.
+ *   d  1 to 512.   rot  even, 0 (no rotation) to d.   N (H + H_k) < 2^31.   Strides up to 2^29 (one token of each of long sequences is a call too).
  * Pointers need the alignment of an element only here.  Norms are fp32; a head with a NaN is NaN; a head with an infinity (or whose squares sum beyond fp32's range)
  * has an infinite norm: its infinite elements become NaN (with their partners in a rotation), the others 0.  Rows of one stride may lie beside each other in one buffer.
  */
@@ -464,7 +464,7 @@ int gated_scan_bwd_varlen(const void* x, const void* g, const void* h, const flo
 
 /*
  * gated_scan_step: one token of the recurrence, the state updated in place: state[slot] <- a state[slot] + b, h = that in dtype.
- *   x, h     device, [B] rows of D elements of type dtype; g rows of g_dtype; each with its stride.  h is written.
+ *   x, h     device, [B] rows of D elements of type dtype; g rows of g_dtype; each with its stride, up to 2^29.  h is written.
  *   state    device, fp32 [n_slot][D], read and written.
  *   slots    device, int32 [B]: sequence b's place in `state`, or NULL for b itself.  A place outside 0 .. n_slot - 1 (padding): nothing is
  *            updated and h is zero.  No two sequences may have the same place.

@@ -7,13 +7,14 @@ namespace {
 
 using namespace triinv;
 
-constexpr int64_t MOST_STRIDE = 1LL << 24;  // elements from token to token: a wavefront's rows stay below 2^31 bytes
+constexpr int64_t MOST_STRIDE = 1LL << 24;  // elements from token to token of a recurrence: a wavefront's rows stay below 2^31 bytes
+constexpr int64_t ANY_STRIDE = 1LL << 29;   // elsewhere: N rows stay below 2^62 bytes
 
 uint64_t size_of(int dtype) { return dtype == TRIINV_F32 ? 4 : 2; }
-bool strides_ok(std::initializer_list<int64_t> strides)
+bool strides_ok(std::initializer_list<int64_t> strides, int64_t most)
 {
     for (const int64_t s : strides)
-        if (s < 0 || s > MOST_STRIDE) return false;
+        if (s < 0 || s > most) return false;
     return true;
 }
 // Tokens of a result do not lie upon each other.
@@ -59,7 +60,7 @@ int scan_common(ScanCall a, int64_t workspace_bytes, bool back)
     const int64_t need = scan_workspace(a.N, a.n_seq, a.D);
     if (a.N > 0 && (!a.g || !a.out || (!a.x && (!back || a.mix)) || (back && (!a.h || !a.dh || !a.dg)))) return TRIINV_ERR_NULL;
     if (need > 0 && !a.workspace) return TRIINV_ERR_NULL;
-    if (workspace_bytes < need || !strides_ok({a.x_stride, a.g_stride, a.h_stride, a.dh_stride, a.out_stride, a.dg_stride})) return TRIINV_ERR_BAD_SHAPE;
+    if (workspace_bytes < need || !strides_ok({a.x_stride, a.g_stride, a.h_stride, a.dh_stride, a.out_stride, a.dg_stride}, MOST_STRIDE)) return TRIINV_ERR_BAD_SHAPE;
     if (!apart(a.N, a.out_stride, a.D) || (back && !apart(a.N, a.dg_stride, a.D))) return TRIINV_ERR_BAD_SHAPE;
     const uint64_t e = size_of(a.dtype), eg = size_of(a.g_dtype), states = (uint64_t)a.n_seq * a.D * 4;
     if (!aligned(a.x, e) || !aligned(a.h, e) || !aligned(a.dh, e) || !aligned(a.out, e) || !aligned(a.g, eg) || !aligned(a.dg, eg) || !aligned(a.state, 4) || !aligned(a.dstate, 4) ||
@@ -83,7 +84,7 @@ int qk_norm_rope(const void* q, const void* k, const void* q_weight, const void*
 {
     if (const int rc = heads_shape(N, H, H_k, d, rot, dtype, flags)) return rc;
     const int64_t wq = (int64_t)H * d, wk = (int64_t)H_k * d;
-    if (!strides_ok({q_stride, k_stride, q_out_stride, k_out_stride}) || !apart(N, q_out_stride, wq) || (H_k > 0 && !apart(N, k_out_stride, wk))) return TRIINV_ERR_BAD_SHAPE;
+    if (!strides_ok({q_stride, k_stride, q_out_stride, k_out_stride}, ANY_STRIDE) || !apart(N, q_out_stride, wq) || (H_k > 0 && !apart(N, k_out_stride, wk))) return TRIINV_ERR_BAD_SHAPE;
     if (N == 0) return TRIINV_OK;
     if (!q || !q_out || (H_k > 0 && (!k || !k_out)) || (rot > 0 && (!positions || !inv_freq))) return TRIINV_ERR_NULL;
     const uint64_t e = size_of(dtype), pos = flags & TRIINV_HEADS_POS64 ? 8 : 4;
@@ -113,7 +114,7 @@ int qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const void* q, cons
 {
     if (const int rc = heads_shape(N, H, H_k, d, rot, dtype, flags)) return rc;
     const int64_t wq = (int64_t)H * d, wk = (int64_t)H_k * d;
-    if (!strides_ok({dq_out_stride, dk_out_stride, q_stride, k_stride, dq_stride, dk_stride}) || !apart(N, dq_stride, wq) || (H_k > 0 && !apart(N, dk_stride, wk))) return TRIINV_ERR_BAD_SHAPE;
+    if (!strides_ok({dq_out_stride, dk_out_stride, q_stride, k_stride, dq_stride, dk_stride}, ANY_STRIDE) || !apart(N, dq_stride, wq) || (H_k > 0 && !apart(N, dk_stride, wk))) return TRIINV_ERR_BAD_SHAPE;
     const bool weights = dq_weight || dk_weight;
     const int64_t need = weights ? heads_workspace(N, H, H_k, d) : 0;
     if (N > 0 && (!dq_out || !q || !dq || (H_k > 0 && (!dk_out || !k || !dk)) || (rot > 0 && (!positions || !inv_freq)) || (need > 0 && !workspace))) return TRIINV_ERR_NULL;
@@ -196,7 +197,7 @@ int gated_scan_step(const void* x, const void* g, float* state, const int32_t* s
 {
     if (const int rc = scan_types(dtype, g_dtype, flags)) return rc;
     if (B < 0 || n_slot < 0 || n_slot > 0x7fffffffLL || D <= 0 || D > (1 << 20) || (!slots && n_slot < B)) return TRIINV_ERR_BAD_SHAPE;
-    if (!strides_ok({x_stride, g_stride, h_stride}) || !apart(B, h_stride, D)) return TRIINV_ERR_BAD_SHAPE;
+    if (!strides_ok({x_stride, g_stride, h_stride}, ANY_STRIDE) || !apart(B, h_stride, D)) return TRIINV_ERR_BAD_SHAPE;
     if ((int64_t)B * ((D + 63) / 64) >= (1LL << 26)) return TRIINV_ERR_UNSUPPORTED;
     if (B == 0) return TRIINV_OK;
     if (!x || !g || !h || (n_slot > 0 && !state)) return TRIINV_ERR_NULL;

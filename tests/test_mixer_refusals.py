@@ -88,7 +88,8 @@ def test_scan_gradient(L, change, status):
 @pytest.mark.parametrize("change,status", [
     (dict(B=0), OK), (dict(B=-1), BAD_SHAPE), (dict(n_slot=2, slots=None), BAD_SHAPE), (dict(n_slot=-1), BAD_SHAPE), (dict(n_slot=1 << 31), BAD_SHAPE), (dict(D=0), BAD_SHAPE), (dict(dtype=9), BAD_DTYPE),
     (dict(flags=4), BAD_METHOD), (dict(hs=10), BAD_SHAPE), (dict(x=None), NULL), (dict(g=None), NULL), (dict(h=None), NULL), (dict(state=None), NULL), (dict(state=address(2) + 2), ALIGN),
-    (dict(slots=address(3) + 2), ALIGN), (dict(h=address(0)), ALIAS), (dict(state=address(1)), ALIAS), (dict(h=address(2) + 400), ALIAS), (dict(B=1 << 27, n_slot=1 << 28), UNSUPPORTED)])
+    (dict(slots=address(3) + 2), ALIGN), (dict(h=address(0)), ALIAS), (dict(state=address(1)), ALIAS), (dict(h=address(2) + 400), ALIAS), (dict(B=1 << 27, n_slot=1 << 28), UNSUPPORTED), (dict(xs=(1 << 29) + 1), BAD_SHAPE),
+    (dict(xs=1 << 29, gs=1 << 25, h=None), NULL)])
 def test_scan_step(L, change, status):
     a = dict(x=address(0), g=address(1), state=address(2), slots=address(3), h=address(4), B=3, n_slot=8, D=100, xs=100, gs=100, hs=100, dtype=tri.BF16, gtype=tri.F32, flags=1, stream=None)
     assert L.gated_scan_step(*dict(a, **change).values()) == status

@@ -146,6 +146,28 @@ def test_offsets_beyond_4_gb():
     assert torch.equal(pool[[19999, 1]].to(BF), h) and (h[0] != 0).any() and int(torch.count_nonzero(pool[2:19999])) == 0
 
 
+def test_one_token_of_each_of_long_sequences():
+    """Rows further apart than a recurrence's may be."""
+    B, row = 5, (1 << 24) + 8192
+    wide = torch.zeros(B, row, dtype=BF, device=DEV)
+    v, _ = make_scan([B], 320, BF, BF, True)
+    x, up = make_heads(B, 3, 2, 64, 32, True, BF)
+    p = [wide[:, i * 320:(i + 1) * 320] for i in range(6)]
+    p[0].copy_(v["x"]), p[1].copy_(v["g"])
+    pools = torch.ones(2, B, 320, device=DEV)
+    want = tri.gated_scan_step(v["x"], v["g"], pools[0], logit=True, mix=True)
+    tri.gated_scan_step(p[0], p[1], pools[1], logit=True, mix=True, h=p[2])
+    assert torch.equal(p[2], want) and torch.equal(pools[0], pools[1])
+    q, k = p[3][:, :192].view(B, 3, 64), p[3][:, 192:].view(B, 2, 64)
+    q.copy_(x["q"]), k.copy_(x["k"])
+    want = tri.qk_norm_rope(**x)
+    got = tri.qk_norm_rope(**dict(x, q=q, k=k), q_out=p[4][:, :192].view(B, 3, 64), k_out=p[4][:, 192:].view(B, 2, 64))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    back = tri.qk_norm_rope_bwd(**up, **x)
+    got = tri.qk_norm_rope_bwd(**up, **dict(x, q=q, k=k), dq=p[5][:, :192].view(B, 3, 64), dk=p[5][:, 192:].view(B, 2, 64))
+    assert all(torch.equal(a, b) for a, b in zip(got, back))
+
+
 def test_rows_behind_the_last_sequence_stay_as_they_are():
     v, up = make_scan([70, 58], 64, BF, BF, True)
     h = torch.full((140, 64), 7.0, dtype=BF, device=DEV)
