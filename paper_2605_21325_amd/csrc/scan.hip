@@ -5,6 +5,7 @@
 //     r_t = dh_t + R;   dx = r or r (1 - a);   dg = r (h_(t-1) - [mix] x) a [or a (1 - a)];   R <- a_t r_t
 // and the initial state's gradient is the last R.  h is read as it was written.
 #include <algorithm>
+#include <cmath>
 #include "layer.hpp"
 #include "attn_ops.hpp"
 #include "elems.hpp"
@@ -391,23 +392,27 @@ template <class F> int types(int dtype, int g_dtype, bool logit, bool mix, F f)
     return g_dtype == OP_F32 ? kinds<OP_BF16, OP_F32>(logit, mix, f) : kinds<OP_BF16, OP_BF16>(logit, mix, f);
 }
 
-// Segments of a sequence, by the tokens, sequences and channels of the call: so many that one to four rounds of the 256 compute units are full, whichever costs least with
-// the first launch's reading, AGAIN of the whole's, counted for all segments but one.  In us, one segment / about 256 / 512 / 1024 workgroups (bf16, logits and
-// mix, 4096 tokens of 2048 channels): 1 sequence (32 workgroups) - / 24 / 22 / 24, 3 (96) 91 / 78 / 69 / 60, 4 (128) - / 81 / 80 / -, 5 94 / 94 / 100 / 101, 6 97 / 97 / 131 /
-// 118; gradient 1 164 / 38 / 41 / 43, 3 170 / 121 / 109 / 103, 4 302 / 124 / 126 / 131, 5 177 / 178 / 166 / 180, 6 180 / 180 / 219 / 212.  One round, which has a workgroup a
-// compute unit and leaves room for a second one, is counted a tenth dearer forward.  Sequences of fewer than three tiles are walked through as they are: 512 tokens (2 tiles) 11.7 in
-// one, 13.5 in two, 1024 (4) 20 and 14; gradient of 333 in fp32 (3) 15.3 and 12.8.
+// Segments of a sequence, by the tokens, sequences and channels of the call: so many that one to four rounds of the 256 compute units are full, whichever costs least, as parts of a
+// walk with all compute units at work to its end: the walk (what part of a round stays empty costs about half of itself; segments take as long as the longest), the first launch's
+// reading, AGAIN of the whole's for all segments but one, LAUNCH for the launch and CHAIN for each tile, one after the other.  In us, 1 / 2 / 3 / 4 / 6 segments, sequences of 3000 tokens of 2048
+// channels (32 workgroups each), bf16, logits and mix: 2 sequences 45 / 36 / 31 / 30 / 31, 3 48 / 41 / 45 / 49 / 47, 4 50 / 45 / 56 / 54 / 54, 5 53 / 72 / 62 / 69 / 65, 6 54 / 78 / 76 / 82 / 78;
+// gradient 2 85 / 60 / 50 / 45 / 48, 3 88 / 66 / 75 / 66 / 70, 4 92 / 78 / 90 / 81 / 82, 5 101 / 120 / 101 / 111 / 106; fp32 log-decays 3 76 / 64 / 72 / 70 / 77, 5 88 / 113 / 103 / 114 / 115.
+// One of 4096 tokens in 8 and 16 segments 23 / 21.  Sequences of fewer than three tiles are walked through as they are: 512 tokens (2 tiles) 11.7 in one, 13.5 in two.
 int segments(int64_t N, int n_seq, int D, int tile, bool back)
 {
-    const double AGAIN = back ? 0.45 : 0.67;
+    const double AGAIN = back ? 0.4 : 0.67, LAUNCH = (back ? 1.0e6 : 1.7e6) / ((double)N * D), CHAIN = back ? 0 : 0.29 * LAUNCH * tile / 256;
     const int64_t units = (int64_t)n_seq * ((D + 63) / 64), tiles = (N / n_seq + tile - 1) / tile;
     if (units >= 256 || tiles < 3) return 1;
+    const auto cost = [&](int64_t n, int64_t per) {
+        const double r = units * n / 256.0, walk = (1 + (std::ceil(r) - r) / (2 * r)) * (per * n) / tiles;
+        return walk + CHAIN * per + (n > 1 ? AGAIN * (n - 1) / n + LAUNCH : 0);
+    };
     int64_t best = 1;
-    double least = 1;
+    double least = cost(1, tiles);
     for (int rounds = 1; rounds <= 4; ++rounds) {
-        const int64_t n = 256 * rounds / units < tiles ? 256 * rounds / units : tiles;
-        const double cost = (double)rounds / n * (1 + AGAIN * (n - 1) / n) * (rounds == 1 && !back ? 1.1 : 1);
-        if (cost < least) best = n, least = cost;
+        const int64_t most = std::min(256 * rounds / units, tiles), per = (tiles + most - 1) / most, n = (tiles + per - 1) / per;
+        const double c = cost(n, per);
+        if (c < least) best = n, least = c;
     }
     return (int)best;
 }
