@@ -412,7 +412,7 @@ int qk_norm_rope(const void* q, const void* k, const void* q_weight, const void*
  *   dq_out, dk_out, dq, dk  rows as q and k, each with its stride; dq and dk are written; dq may be dq_out itself, dk dk_out.
  *   dq_weight, dk_weight    device, fp32 [d], written, or NULL.
  *   workspace               device, workspace_bytes of it as qk_norm_rope_bwd_workspace says (NULL where neither weight's gradient is asked for), 16-byte aligned.
- * The weights' sums are fp32 and have an order that follows from N, the heads, d and the type.
+ * The weights' sums are fp32 and have an order that follows from N, the heads, d, the type and how rows are aligned.
  */
 int qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const void* q, const void* k, const void* q_weight, const void* k_weight,
                      const void* positions, const float* inv_freq, void* dq, void* dk, float* dq_weight, float* dk_weight,

@@ -359,13 +359,15 @@ __global__ __launch_bounds__(1024) void k_heads_dweight(const float* partial, fl
 }
 
 // A wavefront's unit.  Where tokens are many: as many of them as have ROWS times the heads that stand side by side, so that one's angles and addresses and the way to memory
-// come once for several rows (their rows by 32-bit offsets, their angles as far as LDS has room).  Where they are few: a part of a token's heads.
+// come once for several rows (their rows by 32-bit offsets, their angles as far as LDS has room), as long as all of `waves` have a unit (the gradient with weights: 3154 tokens of 6 heads
+// of 80 18 us with a token each, 12.5 so).  Where they are few: a part of a token's heads.
 constexpr int ROWS = 2;
-HeadsPlan plan(int64_t N, int H, int side, int64_t stride, int pairs)
+HeadsPlan plan(int64_t N, int H, int side, int64_t stride, int pairs, int64_t waves = 2048)
 {
     if (H <= 0 || N <= 0) return {0, 0, 1, 1, 1};
     const auto blocks = [](int64_t units) { return (int)((units + WAVES - 1) / WAVES); };
-    const int64_t tokens = std::min<int64_t>({(int64_t)ROWS * side / H, N / 2048, (int64_t)(pairs ? MOST_ANGLES / pairs : 64), (1LL << 29) / std::max<int64_t>(stride, 1)});
+    int64_t tokens = std::min<int64_t>({(int64_t)ROWS * side / H, N / waves, (int64_t)(pairs ? MOST_ANGLES / pairs : 64), (1LL << 29) / std::max<int64_t>(stride, 1)});
+    if (tokens * H > side && tokens * H % side < side / 2) tokens = tokens * H / side * side / H;  // (no step for a few rows)
     if (tokens > 1) {
         const int64_t units = (N + tokens - 1) / tokens;
         return {units, blocks(units), (int)tokens, 1, H};
@@ -411,7 +413,9 @@ template <int DT> struct Backward {
     const HeadsBwdCall& a;
     template <int VEC, int G, int SLOTS, int ROT> int go() const
     {
-        HeadsPlan q = plan(a.N, a.H, 64 / G, std::max<int64_t>({a.q_stride, a.dq_out_stride, a.dq_stride}), a.rot / 2), k = plan(a.N, a.H_k, 64 / G, std::max<int64_t>({a.k_stride, a.dk_out_stride, a.dk_stride}), a.rot / 2);
+        const auto waves = [&](int groups) { return a.partial ? (int64_t)groups * WAVES : 2048; };
+        HeadsPlan q = plan(a.N, a.H, 64 / G, std::max<int64_t>({a.q_stride, a.dq_out_stride, a.dq_stride}), a.rot / 2, waves(a.groups_q));
+        HeadsPlan k = plan(a.N, a.H_k, 64 / G, std::max<int64_t>({a.k_stride, a.dk_out_stride, a.dk_stride}), a.rot / 2, waves(a.groups_k));
         if (a.partial) {
             q.blocks = a.groups_q, k.blocks = a.groups_k;
             return launch_kernel(false, k_heads_bwd<DT, VEC, G, SLOTS, ROT, true>, dim3((unsigned)(a.groups_q + a.groups_k)), dim3(64 * WAVES), WAVES * a.d * 4, a.stream, a, q, k);
@@ -438,12 +442,13 @@ template <int DT> int heads_bwd(const HeadsBwdCall& a)
 
 }  // namespace
 
-// Workgroups that keep a sum each, for queries and keys together in proportion; each with sixteen rows a wavefront, 2048 of them at most.  In us, both launches, with 512 / 768 / 1024 /
+// Workgroups that keep a sum each, for queries and keys together in proportion; each with sixteen rows a wavefront, 1024 of them at most, which the card holds at once, and more, up to
+// 2048, from 64 rows a wavefront on (42115 tokens of two heads of 32 17.4 us with 1318, 13.1 so, with 512 14.6; 3898 of 48 22.4 with 2048, 19).  In us, both launches, with 512 / 768 / 1024 /
 // 2048 / 4096 of them at most (heads of 128, bf16, rotated): 16384 tokens of 40 heads 129 / 140 / 127 / 115 / 117, 65536 of 10 182 / 172 / 153 / 131 / 130; rows a wavefront 4 / 16
 // / 32 / 64: 256 tokens of 24 heads 9.5 / 10 / 13 / 20, 1024 17.8 / 13.8 / 16 / 23, 4096 31 / 29 / 26 / 30.
 int heads_bwd_groups(int64_t N, int H, int heads)
 {
-    const int64_t n = (N * H + 16 * WAVES - 1) / (16 * WAVES), share = ((int64_t)2048 * H + heads - 1) / heads;
+    const int64_t n = (N * H + 16 * WAVES - 1) / (16 * WAVES), most = std::clamp<int64_t>(N * heads / (64 * WAVES), 1024, 2048), share = (most * H + heads - 1) / heads;
     return (int)(n < share ? n : share);
 }
 int launch_heads(const HeadsCall& a) { return a.dtype == OP_F32 ? heads<OP_F32>(a) : a.dtype == OP_F16 ? heads<OP_F16>(a) : heads<OP_BF16>(a); }

@@ -112,7 +112,8 @@ def test_many_packed_sequences(lens, D, dtype, gtype, logit, mix):
     check_scan_bwd(lens, v, got[0], up, tri.gated_scan_bwd_varlen(v["x"], v["g"], got[0], up["dh"], lens, v["state"], up["dstate"], logit=logit, mix=mix), logit, mix)
 
 
-@pytest.mark.parametrize("N,H,Hk,d,rot,inter,dtype", [(4200, 2, 1, 64, 16, False, BF), (6001, 1, 1, 32, 8, True, HF), (4100, 3, 2, 128, 0, False, F), (9000, 1, 0, 16, 0, False, BF), (2100, 5, 1, 96, 0, True, BF)])
+@pytest.mark.parametrize("N,H,Hk,d,rot,inter,dtype", [(4200, 2, 1, 64, 16, False, BF), (6001, 1, 1, 32, 8, True, HF), (4100, 3, 2, 128, 0, False, F), (9000, 1, 0, 16, 0, False, BF), (2100, 5, 1, 96, 0, True, BF),
+                                                      (3154, 4, 2, 80, 0, True, BF), (30011, 1, 1, 32, 0, False, HF), (333, 3, 1, 48, 16, False, F), (40, 1, 1, 64, 64, True, BF), (700, 7, 3, 512, 512, True, BF)])
 def test_several_tokens_to_a_wavefront(N, H, Hk, d, rot, inter, dtype):
     x, up = make_heads(N, H, Hk, d, rot, True, dtype)
     check_heads(x, tri.qk_norm_rope(**x, interleaved=inter), False, inter)
