@@ -397,7 +397,8 @@ template <class F> int types(int dtype, int g_dtype, bool logit, bool mix, F f)
 // reading, AGAIN of the whole's for all segments but one, LAUNCH for the launch and CHAIN for each tile, one after the other.  In us, 1 / 2 / 3 / 4 / 6 segments, sequences of 3000 tokens of 2048
 // channels (32 workgroups each), bf16, logits and mix: 2 sequences 45 / 36 / 31 / 30 / 31, 3 48 / 41 / 45 / 49 / 47, 4 50 / 45 / 56 / 54 / 54, 5 53 / 72 / 62 / 69 / 65, 6 54 / 78 / 76 / 82 / 78;
 // gradient 2 85 / 60 / 50 / 45 / 48, 3 88 / 66 / 75 / 66 / 70, 4 92 / 78 / 90 / 81 / 82, 5 101 / 120 / 101 / 111 / 106; fp32 log-decays 3 76 / 64 / 72 / 70 / 77, 5 88 / 113 / 103 / 114 / 115.
-// One of 4096 tokens in 8 and 16 segments 23 / 21.  Sequences of fewer than three tiles are walked through as they are: 512 tokens (2 tiles) 11.7 in one, 13.5 in two.
+// One of 4096 tokens in 8 and 16 segments 23 / 21.  256 at most, for a segment reads what all before it bring: one of 262144 tokens of 64 channels in 128 / 256 / 1024 132 / 123 / 143.
+// Sequences of fewer than three tiles are walked through as they are: 512 tokens (2 tiles) 11.7 in one, 13.5 in two.
 int segments(int64_t N, int n_seq, int D, int tile, bool back)
 {
     const double AGAIN = back ? 0.4 : 0.67, LAUNCH = (back ? 1.0e6 : 1.7e6) / ((double)N * D), CHAIN = back ? 0 : 0.29 * LAUNCH * tile / 256;
@@ -410,7 +411,7 @@ int segments(int64_t N, int n_seq, int D, int tile, bool back)
     int64_t best = 1;
     double least = cost(1, tiles);
     for (int rounds = 1; rounds <= 4; ++rounds) {
-        const int64_t most = std::min(256 * rounds / units, tiles), per = (tiles + most - 1) / most, n = (tiles + per - 1) / per;
+        const int64_t most = std::min<int64_t>({256 * rounds / units, tiles, 256}), per = (tiles + most - 1) / most, n = (tiles + per - 1) / per;
         const double c = cost(n, per);
         if (c < least) best = n, least = c;
     }
@@ -420,7 +421,8 @@ int segments(int64_t N, int n_seq, int D, int tile, bool back)
 // Packed sequences that are cut have as many times the segments that they would have if all were as long as the mean one, for the longest to be shorter.  In us, once / twice / three times,
 // lengths up to twice the mean, bf16, 1024 channels: 2 sequences of 1000 tokens 21 / 15 / 15, 8 of 1000 33 / 28 / 31, 3 of 5000 55 / 48 / 43, 5 of 5000 76 / 82 / 71, 8 of 5000 112 / 99 / 98;
 // gradient 27 (3 of 1000) / 22 / 24, 48 (8 of 1000) / 40 / 40, 61 (2 of 5000) / 41 / 52, 130 (5) / 133 / 115, 185 (8) / 165 / 164; 30 of 7408 of 32 channels 42 / 46 / 50.
-constexpr int PACKED = 2;
+// 128 at most: 2 of 65536 of 128 channels in 64 / 128 / 256 / 512 72 / 52 / 62 / 88.
+int packed_segments(int n) { return n > 1 ? std::min(2 * n, 128) : 1; }
 
 // Parts of a segment: three workgroups a compute unit in the first launch.  (Gradient of 4 sequences of 4096 tokens of 2048 channels, two segments: 30 us of 128 were the first launch's
 // when it had one part a segment, on half of the compute units.)
@@ -465,7 +467,7 @@ template <bool BACK> struct Scan {
     }
     template <int DT, int GT, bool LOGIT, bool MIX> int go() const
     {
-        const int n_mean = segments(a.N, a.n_seq, a.D, TOKENS<DT, GT, BACK> * MOST_STRIPS, BACK), n_seg = a.cu_seqlens && n_mean > 1 ? PACKED * n_mean : n_mean;
+        const int n_mean = segments(a.N, a.n_seq, a.D, TOKENS<DT, GT, BACK> * MOST_STRIPS, BACK), n_seg = a.cu_seqlens ? packed_segments(n_mean) : n_mean;
         // Two channels a lane where every row's begin allows it.
         const auto even = [](const void* p, int64_t stride, int dtype) { return !p || (stride % 2 == 0 && reinterpret_cast<uintptr_t>(p) % (dtype == OP_F32 ? 8 : 4) == 0); };
         if (a.D % 2 == 0 && even(a.x, a.x_stride, DT) && even(a.g, a.g_stride, GT) && even(a.h, a.h_stride, DT) && even(a.dh, a.dh_stride, DT) && even(a.out, a.out_stride, DT) &&
@@ -505,7 +507,7 @@ int64_t scan_workspace(int64_t N, int n_seq, int D)
     int64_t most = 0;  // (of either direction and every type)
     const auto count = [&](int tile, bool back) {
         const int n = segments(N, n_seq, D, tile, back);
-        for (const int m : {n, PACKED * n}) {
+        for (const int m : {n, packed_segments(n)}) {
             const int64_t parts = n > 1 ? (int64_t)m * parts_of(N, n_seq, D, tile, m) : 0;
             most = parts > most ? parts : most;
         }

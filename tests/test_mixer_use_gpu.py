@@ -88,7 +88,7 @@ def test_a_stream_as_an_argument():
 
 @pytest.mark.parametrize("lens,D,dtype,gtype,logit,mix", [
     ([1500], 4480, F, F, True, True), ([3000, 5, 0, 700], 1000, BF, BF, True, False), ([2600, 2600], 320, BF, F, False, True), ([1100] * 4, 2048, HF, HF, False, False), ([385], 64, F, F, False, False),
-    ([769, 0, 0, 1], 128, BF, BF, True, True), ([5000], 33, HF, F, False, True)])
+    ([769, 0, 0, 1], 128, BF, BF, True, True), ([5000], 33, HF, F, False, True), ([70000, 3], 16, BF, BF, True, True)])
 def test_sequences_in_segments(lens, D, dtype, gtype, logit, mix):
     v, up = make_scan(lens, D, dtype, gtype, logit)
     got = tri.gated_scan_varlen(**v, seqlens=lens, logit=logit, mix=mix)
