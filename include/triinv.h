@@ -468,6 +468,7 @@ int gated_scan_bwd_varlen(const void* x, const void* g, const void* h, const flo
  *   state    device, fp32 [n_slot][D], read and written.
  *   slots    device, int32 [B]: sequence b's place in `state`, or NULL for b itself.  A place outside 0 .. n_slot - 1 (padding): nothing is
  *            updated and h is zero.  No two sequences may have the same place.
+ *   B  from 0 (nothing is done) on.   D  1 to 2^20.   B ceil(D / 64) < 2^26.   n_slot < 2^31.
  */
 int gated_scan_step(const void* x, const void* g, float* state, const int32_t* slots, void* h, int B, int64_t n_slot, int D, int64_t x_stride, int64_t g_stride,
                     int64_t h_stride, int dtype, int g_dtype, uint32_t flags, void* hip_stream);

@@ -358,8 +358,9 @@ constexpr int THREADS = 256;
 template <int DT, int GT, bool LOGIT, bool MIX, int VEC> __global__ __launch_bounds__(THREADS) void k_scan_step(ScanStepCall a)
 {
     const int groups = (a.D + THREADS * VEC - 1) / (THREADS * VEC);
-    const int b = (int)(blockIdx.x / (unsigned)groups), c = ((int)(blockIdx.x - (unsigned)(b * groups)) * THREADS + (int)threadIdx.x) * VEC;
-    if (c >= a.D) return;
+    const unsigned block = blockIdx.y * gridDim.x + blockIdx.x;
+    const int b = (int)(block / (unsigned)groups), c = ((int)(block - (unsigned)b * (unsigned)groups) * THREADS + (int)threadIdx.x) * VEC;
+    if (b >= a.B || c >= a.D) return;
     Elems<DT, VEC> x;
     Elems<GT, VEC> g;
     x.load(a.x, b * a.x_stride + c), g.load(a.g, b * a.g_stride + c);
@@ -487,7 +488,7 @@ struct Step {
     const ScanStepCall& a;
     template <int DT, int GT, bool LOGIT, bool MIX, int VEC> int with() const
     {
-        const dim3 grid((unsigned)((int64_t)a.B * ((a.D + THREADS * VEC - 1) / (THREADS * VEC))));
+        const dim3 grid = long_grid((int64_t)a.B * ((a.D + THREADS * VEC - 1) / (THREADS * VEC)));
         return launch_kernel(false, k_scan_step<DT, GT, LOGIT, MIX, VEC>, grid, dim3(THREADS), 0, a.stream, a);
     }
     template <int DT, int GT, bool LOGIT, bool MIX> int go() const
