@@ -432,8 +432,8 @@ int qk_norm_rope_bwd_workspace(int64_t N, int H, int H_k, int d, int64_t* bytes)
  *   workspace    device, workspace_bytes of it as gated_scan_workspace says, 16-byte aligned (NULL where that is 0).
  *   D  1 to 2^20.   B Tlen < 2^31.   B ceil(D / 64) < 2^31.   Strides up to 2^24.
  * Pointers need the alignment of an element only, but for the workspace.  States and sums are fp32.  Tlen = 0 or empty sequences: final_state = state.  A log-decay of -infinity begins anew.
- * Decays above 1 (g > 0) are taken as they are, as long as the products of neighbouring ones stay in fp32's range.  Non-finite values stay in their sequence and channel,
- * from their token on.  The same call gives the same bits; few channels and sequences are walked through in segments, whose number follows from all sizes of the call, so that last bits may
+ * Decays above 1 (g > 0) are taken as they are; where the product of neighbouring ones leaves fp32's range and the states do not, they are walked through token by token, which takes
+ * longer (and last bits of other channels of the sequence may change).  Non-finite values stay in their sequence and channel, from their token on.  The same call gives the same bits; few channels and sequences are walked through in segments, whose number follows from all sizes of the call, so that last bits may
  * change with the batch.
  * gated_scan_varlen: sequences packed back to back, cu_seqlens device, int64 [n_seq + 1], the sequences' first tokens and then total_tokens (trusted), states [n_seq][D].
  */

@@ -61,6 +61,19 @@ template <int T, bool LOGIT, bool REST> __device__ __forceinline__ Gate gate(flo
 constexpr int MOST_STRIPS = 16, SHORT = 64;  // SHORT: tokens of the fewest strips
 template <int DT, int GT, bool BACK> constexpr int TOKENS = !BACK && DT != OP_F32 && GT != OP_F32 ? 16 : 8;
 
+// A byte for each strip of a tile, read together.
+template <int STRIPS> union StripMarks {
+    uint8_t of[STRIPS];
+    uint32_t words[STRIPS / 4];
+    __device__ __forceinline__ bool any() const
+    {
+        uint32_t x = 0u;
+#pragma unroll
+        for (int i = 0; i < STRIPS / 4; ++i) x |= words[i];
+        return __builtin_amdgcn_readfirstlane(x) != 0u;
+    }
+};
+
 struct ScanPlan {
     int n_seg, fine, groups;  // segments of a sequence; parts of a segment; groups of channels
     bool neighbours;    // on one XCD
@@ -78,6 +91,9 @@ __device__ __forceinline__ Sequence sequence(const ScanCall& a, int s)
     const int64_t t0 = a.cu_seqlens ? among(a.cu_seqlens[s], 0, a.N) : s * a.Tlen, len = a.cu_seqlens ? among(a.cu_seqlens[s + 1], t0, a.N) - t0 : a.Tlen;
     return {t0, len};
 }
+
+// Whether a product of decays, none of them below 0, is in fp32's range.
+__device__ __forceinline__ bool in_range(float a) { return a <= 3.402823466e38f; }
 
 template <int VEC> __device__ __forceinline__ void load_state(const float* from, int64_t i, float (&x)[VEC])
 {
@@ -160,6 +176,11 @@ template <int DT, int GT, bool MIX, bool BACK, int VEC, int CH, bool ONLY> struc
 // Where sequences and channels are too few for the card a sequence is cut into segments of whole tiles: a first launch (ONLY) writes what each segment but the last brings, in
 // parts, so many that they fill the card too; the second begins a segment with the state that those before it leave.
 //
+// Log-decays may be above 0, and a product of decays may leave fp32's range where the states do not (they are zero or small, or a decay of 0 follows): infinite times nothing is not a
+// number.  In a tile with such a strip the strips find the states before them one after the other, token by token; so does, from the sequence's first token on, a lane whose segment is
+// behind such a part.  us, bf16 log-decays, half of the channels zeros and decays of 1 / e^20: 16 x 1500 tokens of 2048 channels 51 / 59, gradient 102 / 125, 512 x 16 of 1024
+// 20 / 23; 4096 tokens of 2048 in segments 17 / 360.  Looking for them costs up to 3 in a hundred, and nothing with logits.
+//
 // Bound by memory: x, g (gradient: dh, h too) are read and h (dx, dg) written once.  8 x 8192 tokens of 2048 channels, bf16, logits and mix, 176 us, 4.6 TB/s: pieces of 128 bytes of a
 // row, vector instructions in two fifths of the cycles; 16 x 1500, in pieces of 256, 58 us, 5.1 TB/s, its gradient 123, 4.8.  In LDS go a strip's two numbers a channel, nothing else.
 // Tried: tiles in workgroups of their own that hand states on (8 x 8192 229 to 275 us, the waiting), 32 channels a workgroup (250), 32 strips (179), 8 (184), the next tile's tokens
@@ -171,6 +192,8 @@ template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC, int CH, int 
     constexpr int LANES = CH / VEC, PER_WAVE = 64 / LANES;  // of a strip; strips of a wavefront
     __shared__ float own[2][STRIPS][CH][2];  // of one tile and the next: one barrier a tile
     __shared__ float base[2][CH];
+    constexpr bool STEEP = !LOGIT && !ONLY;  // whether products of decays may leave the range (the first launch hands them on as they are)
+    __shared__ StripMarks<STRIPS> steep[2];  // (STEEP) of one tile and the next: which strips have one
     const int strip = threadIdx.x / LANES, i_c = threadIdx.x % LANES * VEC;
     int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     const int parts = p.n_seg * p.fine, units = ONLY ? parts : p.n_seg;  // of a sequence
@@ -224,15 +247,36 @@ template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC, int CH, int 
         if (part == 0) initial();
         if (!ONLY && seg > 0) {
             const v2f* const from = p.part + (int64_t)s * parts * a.D + c;
+            bool finite = true;
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) C[e] = from[e][1];
+            for (int e = 0; e < VEC; ++e) C[e] = from[e][1], finite &= in_range(from[e][0]);
 #pragma unroll 4
             for (int k = 1; k < seg * p.fine; ++k)
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
                     const v2f w = from[(int64_t)k * a.D + e];
-                    C[e] = fmaf(w[0], C[e], w[1]);
+                    C[e] = fmaf(w[0], C[e], w[1]), finite &= in_range(w[0]);
                 }
+            if (STEEP && CH == 64 && !finite) {  // from the sequence's first token on
+                initial();
+                constexpr int AT_ONCE = 4;
+                for (int64_t i = 0; i < (int64_t)j0 * TILE; i += AT_ONCE) {
+                    Elems<GT, VEC> g[AT_ONCE];
+                    Elems<DT, VEC> b[AT_ONCE];
+#pragma unroll
+                    for (int u = 0; u < AT_ONCE; ++u) {
+                        const int64_t row = BACK ? q.t0 + q.len - 1 - i - u : q.t0 + i + u;
+                        g[u].load(a.g, row * a.g_stride + c), b[u].load(BACK ? a.dh : a.x, row * (BACK ? a.dh_stride : a.x_stride) + c);
+                    }
+#pragma unroll
+                    for (int u = 0; u < AT_ONCE; ++u)
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) {
+                            const Gate f = gate<GT, LOGIT, MIX && !BACK>(g[u][e]);
+                            C[e] = BACK ? f.a * (b[u][e] + C[e]) : fmaf(f.a, C[e], MIX ? f.rest * b[u][e] : b[u][e]);
+                        }
+                }
+            }
         }
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
@@ -268,13 +312,25 @@ template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC, int CH, int 
             for (int i = 0; i < TOK; ++i) form(i);
         } else {
 #pragma unroll
-            for (int i = 0; i < TOK; ++i)
-                if (i < at.left) form(i);
+            for (int i = 0; i < TOK; ++i) {
+                if (i < at.left) {
+                    form(i);
+                } else if constexpr (STEEP && !BACK) {
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) da[i][e] = 1.f, db[i][e] = 0.f;
+                }
+            }
         }
         if (j + 1 < j1) next.load(a, q, i0 + TILE, strip, c, in);
         float (*const mine)[CH][2] = own[j & 1];
 #pragma unroll
         for (int e = 0; e < VEC; ++e) mine[strip][i_c + e][0] = A[e], mine[strip][i_c + e][1] = H[e];
+        if constexpr (STEEP) {
+            bool good = true;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) good &= in_range(A[e]);
+            steep[j & 1].of[strip] = __all(good) ? 0 : 1;
+        }
         __syncthreads();
         if constexpr (ONLY) {
             if (strip == 0) {
@@ -307,6 +363,30 @@ template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC, int CH, int 
             if (PER_WAVE > 1 && strip != first) {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) C[e] = fmaf(mine[first][i_c + e][0], C[e], mine[first][i_c + e][1]);
+            }
+        }
+        if (STEEP && steep[j & 1].any()) {
+#pragma unroll 1
+            for (int turn = 0; turn < STRIPS; ++turn) {
+                __syncthreads();
+                if (strip != turn) continue;
+                float S[VEC];
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) S[e] = C[e] = base[j & 1][i_c + e];
+#pragma unroll
+                for (int i = 0; i < TOK; ++i) {
+                    auto d = now.d[BACK ? i : 0];
+                    if constexpr (BACK) {  // (widened here, not before the loop: registers)
+#pragma unroll
+                        for (uint32_t& w : d.w) asm volatile("" : "+v"(w));
+                    }
+                    if (!BACK || i < at.left) {  // (forward: what is not there is a decay of 1 that brings nothing)
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) S[e] = BACK ? da[i][e] * (d[e] + S[e]) : fmaf(da[i][e], S[e], db[i][e]);
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) base[j & 1][i_c + e] = S[e];
             }
         }
         const RowsOf<DT, TOK, BACK> out(a.out, at.first, a.out_stride, at.row, c, in);
