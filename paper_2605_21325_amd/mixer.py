@@ -121,6 +121,8 @@ def qk_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], q_weight: Optional[
             return r
     _one_device(q, k, q_weight, k_weight, positions, inv_freq, q_out, k_out)
     lead, N, H, H_k, d, rot = _heads_checked(q, k, q_weight, k_weight, positions, inv_freq)
+    if k is None and k_out is not None:
+        raise ValueError("k_out without k")
     (pq, sq), (pk, sk) = _rows(q, "q", 2), _rows(k, "k", 2)
     with _on(stream, q.device):
         q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
@@ -147,6 +149,8 @@ def qk_norm_rope_bwd(dq_out: torch.Tensor, dk_out: Optional[torch.Tensor], q: to
     lead, N, H, H_k, d, rot = _heads_checked(q, k, q_weight, k_weight, positions, inv_freq)
     if (k is None) != (dk_out is None):
         raise ValueError("k and dk_out belong together")
+    if k is None and dk is not None:
+        raise ValueError("dk without k")
     k_shape = None if k is None else k.shape
     (pq, sq), (pk, sk) = _rows(q, "q", 2), _rows(k, "k", 2)
     (uq, suq), (uk, suk) = _rows(dq_out, "dq_out", 2, q.shape, q.dtype), _rows(dk_out, "dk_out", 2, k_shape, q.dtype)
