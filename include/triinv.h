@@ -88,7 +88,8 @@ typedef enum {
     TRIINV_ERR_ALIGN = -6,       /* a pointer is not 16-byte aligned */
     TRIINV_ERR_ALIAS = -7,       /* T (or W) overlaps an input buffer */
     TRIINV_ERR_LAUNCH = -8,      /* the HIP runtime refused the launch */
-    TRIINV_ERR_UNSUPPORTED = -9  /* valid arguments, but this combination is not built */
+    TRIINV_ERR_UNSUPPORTED = -9  /* valid arguments, but this combination is not built, or the call needs a grid of 2^32 threads
+                                    (2^26 matrices of C = 16 and more) */
 } triinv_status;
 
 /* Bits of `flags` (0 = none). */

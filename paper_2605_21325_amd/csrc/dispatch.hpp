@@ -160,7 +160,8 @@ template <class Param, class Arg> inline bool holds(const Arg& a)
 
 // One kernel launch whose own status is returned (the runtime's sticky per-thread error state, which may hold an
 // unrelated earlier error of the caller, is neither read nor cleared).  The arguments are converted to the kernel's
-// exact parameter types first.  dry: report LAUNCHED without launching.  Lengths of packed sequences for a kernel that cannot be given them: NOT_BUILT.
+// exact parameter types first.  dry: report LAUNCHED without launching.  Lengths of packed sequences for a kernel that cannot be given them, and grids of 2^32 threads or more in a
+// dimension, of which the runtime launches a part without an error: NOT_BUILT.
 template <class... KArgs, class... Args, size_t... I>
 inline int launch_kernel_impl(void (*kernel)(KArgs...), dim3 grid, dim3 block, unsigned lds_bytes, hipStream_t stream,
                               std::index_sequence<I...>, Args&&... args)
@@ -174,6 +175,7 @@ inline int launch_kernel(bool dry, void (*kernel)(KArgs...), dim3 grid, dim3 blo
 {
     static_assert(sizeof...(KArgs) == sizeof...(Args), "one argument per kernel parameter");
     if (!(holds<KArgs>(args) && ...)) return NOT_BUILT;
+    if ((uint64_t)grid.x * block.x > 0xffffffffu) return NOT_BUILT;
     if (dry) return LAUNCHED;
     return launch_kernel_impl(kernel, grid, block, lds_bytes, stream, std::index_sequence_for<KArgs...>{}, std::forward<Args>(args)...);
 }
