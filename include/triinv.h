@@ -395,7 +395,7 @@ int add_rms_norm_bwd(const void* dy, const void* s, const void* weight, const vo
  *   q_weight, k_weight  device, [d], the same type, or NULL for ones.
  *   positions           device, int32 [N] (TRIINV_HEADS_POS64: int64, up to 2^53 in magnitude); NULL with rot = 0.
  *   inv_freq            device, fp32 [rot / 2], radians a position; NULL with rot = 0.  The angle is their exact product without its whole turns.
- *   d  1 to 512.   rot  even, 0 (no rotation) to d.   N (H + H_k) < 2^31.   Strides up to 2^29 (one token of each of long sequences is a call too).
+ *   N  from 0 on (nothing is done; weights' gradients are zeros).   H  from 1, H + H_k up to 2^20.   d  1 to 512.   rot  even, 0 (no rotation) to d.   N (H + H_k) < 2^31.   Strides up to 2^29 (one token of each of long sequences is a call too).
  * Pointers need the alignment of an element only here.  Norms are fp32; a head with a NaN is NaN; a head with an infinity (or whose squares sum beyond fp32's range)
  * has an infinite norm: its infinite elements become NaN (with their partners in a rotation), the others 0.  Rows of one stride may lie beside each other in one buffer.
  */
@@ -431,7 +431,7 @@ int qk_norm_rope_bwd_workspace(int64_t N, int H, int H_k, int d, int64_t* bytes)
  *   state        device, fp32 [B][D], the state before the first token, or NULL for zeros.
  *   final_state  device, fp32 [B][D], written, or NULL.  May be `state` itself.
  *   workspace    device, workspace_bytes of it as gated_scan_workspace says, 16-byte aligned (NULL where that is 0).
- *   D  1 to 2^20.   B Tlen < 2^31.   B ceil(D / 64) < 2^31.   Strides up to 2^24.
+ *   B (n_seq)  from 1 on, as in gdn_chunk_attn; Tlen (total_tokens) may be 0.   D  1 to 2^20.   B Tlen < 2^31.   B ceil(D / 64) < 2^31.   Strides up to 2^24.
  * Pointers need the alignment of an element only, but for the workspace.  States and sums are fp32.  Tlen = 0 or empty sequences: final_state = state.  A log-decay of -infinity begins anew.
  * Decays above 1 (g > 0) are taken as they are; where the product of neighbouring ones leaves fp32's range and the states do not, they are walked through token by token, which takes
  * longer (and last bits of other channels of the sequence may change).  Non-finite values stay in their sequence and channel, from their token on.  The same call gives the same bits; few channels and sequences are walked through in segments, whose number follows from all sizes of the call, so that last bits may

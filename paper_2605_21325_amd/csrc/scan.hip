@@ -184,7 +184,7 @@ template <int DT, int GT, bool MIX, bool BACK, int VEC, int CH, bool ONLY> struc
 // Bound by memory: x, g (gradient: dh, h too) are read and h (dx, dg) written once.  8 x 8192 tokens of 2048 channels, bf16, logits and mix, 176 us, 4.6 TB/s: pieces of 128 bytes of a
 // row, vector instructions in two fifths of the cycles; 16 x 1500, in pieces of 256, 58 us, 5.1 TB/s, its gradient 123, 4.8.  In LDS go a strip's two numbers a channel, nothing else.
 // Tried: tiles in workgroups of their own that hand states on (8 x 8192 229 to 275 us, the waiting), 32 channels a workgroup (250), 32 strips (179), 8 (184), the next tile's tokens
-// asked for before this one's decays (185).  4096 tokens of one sequence take 21 us, 9 of them the first launch; of 4 sequences' gradient 24 of 110.
+// asked for before this one's decays (185).  4096 tokens of one sequence take 21 us, 9 of them the first launch; of 4 sequences' gradient 24 of 107.
 template <int DT, int GT, bool LOGIT, bool MIX, bool BACK, int VEC, int CH, int STRIPS, bool ONLY> __global__ __launch_bounds__(STRIPS * CH / VEC) void k_scan(ScanCall a, ScanPlan p)
 {
     constexpr bool REST = MIX || (BACK && LOGIT);
@@ -475,7 +475,7 @@ template <class F> int types(int dtype, int g_dtype, bool logit, bool mix, F f)
 
 // Segments of a sequence, by the tokens, sequences and channels of the call: so many that one to four rounds of the 256 compute units are full, whichever costs least, as parts of a
 // walk with all compute units at work to its end: the walk (what part of a round stays empty costs about half of itself; segments take as long as the longest), the first launch's
-// reading, AGAIN of the whole's for all segments but one, LAUNCH for the launch and CHAIN for each tile, one after the other.  In us, 1 / 2 / 3 / 4 / 6 segments, sequences of 3000 tokens of 2048
+// time, AGAIN of the whole's for all segments but one (it reads two thirds of the call's bytes, in the gradient one third, at a lower rate), LAUNCH for the launch and CHAIN for each tile, one after the other.  In us, 1 / 2 / 3 / 4 / 6 segments, sequences of 3000 tokens of 2048
 // channels (32 workgroups each), bf16, logits and mix: 2 sequences 45 / 36 / 31 / 30 / 31, 3 48 / 41 / 45 / 49 / 47, 4 50 / 45 / 56 / 54 / 54, 5 53 / 72 / 62 / 69 / 65, 6 54 / 78 / 76 / 82 / 78;
 // gradient 2 85 / 60 / 50 / 45 / 48, 3 88 / 66 / 75 / 66 / 70, 4 92 / 78 / 90 / 81 / 82, 5 101 / 120 / 101 / 111 / 106; fp32 log-decays 3 76 / 64 / 72 / 70 / 77, 5 88 / 113 / 103 / 114 / 115.
 // One of 4096 tokens in 8 and 16 segments 23 / 21.  256 at most, for a segment reads what all before it bring: one of 262144 tokens of 64 channels in 128 / 256 / 1024 132 / 123 / 143.

@@ -213,7 +213,7 @@ def _scan(where, x, g, n_seq, N, where_args, state, logit, mix, h, final_state, 
 
 def gated_scan(x: torch.Tensor, g: torch.Tensor, state: Optional[torch.Tensor] = None, logit: bool = False, mix: bool = False, h: Optional[torch.Tensor] = None,
                final_state: Optional[torch.Tensor] = None, stream=None):
-    """(h, final_state) of the gated recurrence h_t = a_t h_(t-1) + b_t over x, g [B, Tlen, D]: a = e^g, or with logit sigmoid(g); b = x, or with mix (1 - a) x.
+    """(h, final_state) of the gated recurrence h_t = a_t h_(t-1) + b_t over x, g [B, Tlen, D] (one sequence at least, tokens may be none): a = e^g, or with logit sigmoid(g); b = x, or with mix (1 - a) x.
     g is of x's type or fp32.  state: [B, D] fp32, the state before the first token (None: zeros)."""
     f = _fast(x, stream)
     if f:
@@ -229,7 +229,7 @@ def gated_scan(x: torch.Tensor, g: torch.Tensor, state: Optional[torch.Tensor] =
 
 def gated_scan_varlen(x: torch.Tensor, g: torch.Tensor, seqlens, state: Optional[torch.Tensor] = None, logit: bool = False, mix: bool = False,
                       h: Optional[torch.Tensor] = None, final_state: Optional[torch.Tensor] = None, stream=None):
-    """gated_scan on packed sequences: x, g [total, D]; seqlens = host sequence of lengths; states [len(seqlens), D]."""
+    """gated_scan on packed sequences: x, g [total, D]; seqlens = host sequence of lengths (one at least; lengths of 0 are sequences too); states [len(seqlens), D]."""
     f = _fast(x, stream)
     if f:
         r = f[0].scan_varlen(f[1], f[2], x, g, seqlens, state, logit, mix, h, final_state)
